@@ -222,7 +222,7 @@ def prepare(case, seed):
     free[: pages - sum(before)] = order[sum(before):]
     s = {"case": case, "lens": lens, "R": R, "T": T, "kv_len": kv_len, "q_len": q_len, "table": table,
          "free": free, "free_count": torch.tensor([pages - sum(before)], **i32), "pages": pages, "cap": cap,
-         "max_pos": max(kv + q for kv, q in lens)}
+         "max_q": max(q for _, q in lens), "max_pos": max(kv + q for kv, q in lens)}
     op = case["op"]
     # the fused projection's output: one row a token, query heads, then key heads, then value heads
     if op in ("norm_rope", "append"):
@@ -436,7 +436,8 @@ def _attach(s):
     if c["op"] == "attention":
         # the pages are the same as those of full_table: the stack and the order of requests are
         kv.build_tables(s["kv_len"], s["q_len"], s["T"], s["free"], s["free_count"].clone(), s["table"].clone(),
-                        window=c["window"], kv_len_out=torch.empty_like(s["kv_len"]))
+                        max_q=s["max_q"], window=c["window"],
+                        kv_len_out=torch.empty_like(s["kv_len"]))
     if c["op"] in ("norm_rope", "append"):
         T, hq, hkv, d = s["T"], c["hq"], c["hkv"], c["d"]
         qkv = s["qkv"]
@@ -449,7 +450,7 @@ def _attach(s):
 def _own_tables(s):
     kv = s["kv"]
     kv.build_tables(s["kv_len"], s["q_len"], s["T"], s["free"], s["free_count"], s["table_own"],
-                    kv_len_out=s["kv_out"], free_count_out=s["count_out"])
+                    max_q=s["max_q"], stream=torch.cuda.current_stream(), kv_len_out=s["kv_out"], free_count_out=s["count_out"])
     return {"starts": kv.starts, "kv_len": s["kv_out"], "positions": kv.positions, "slots": kv.slots,
             "table": s["table_own"], "free_count": s["count_out"]}
 

@@ -18,6 +18,15 @@
  *   lora_bgmv_apply       decode batches (one token per request)
  *   lora_sgmv_apply       prefill / chunked-prefill batches (per-adapter segments)
  *
+ * and what a served batch needs between two such projections, on a cache that leaves the GPU's
+ * memory to adapter slots (4 bits a value):
+ *
+ *   lora_kv_create        a paged key/value cache in caller-owned device memory
+ *   lora_kv_build_tables  block tables, positions and slot maps from the requests' lengths
+ *   lora_qk_norm_rope     per-head norm and rotation of queries and keys in one pass
+ *   lora_kv_append        the same pass, with the keys and values going to the cache as 4-bit rows
+ *   lora_kv_attention     attention of a batch (single tokens and prompts together) over the cache
+ *
  * Conventions
  *  - plain C ABI; every call returns a lora_status_t; nothing aborts, traps or resets a device;
  *  - "dev" pointers are device memory, "host" pointers are host memory; all buffers are owned
@@ -389,6 +398,158 @@ lora_status_t lora_apply_host(lora_pool_t *pool, int32_t target, int32_t kind,
                               const int32_t *slot_idx_host, int32_t T,
                               int32_t tile_m, int32_t long_min,
                               const lora_step_buffers_t *dev, void *stream);
+
+/* ----------------------------------------------------------------------------------------
+ * Paged key/value cache in 4 bits.
+ *
+ * Adapter slots and the cache of running requests share one GPU's memory (paper Section 2.2: the
+ * A_max x S_max region is taken from what the requests' keys and values could use), so a row of
+ * head_dim values is kept as head_dim 4-bit codes with one scale and one low value:
+ *     value_i = low + scale * code_i ,  code_i in 0 .. 15 ,
+ *     low = bf16(min x) , scale = bf16((max x - low) / 15) ,
+ *     code_i = clamp(rint((x_i - low) * (1 / scale)), 0, 15)      (all in fp32, IEEE rounding;
+ *     a scale below the smallest normal number counts as 0, and then every code is 0;
+ *     a row with a value that is not finite, or whose scale is not, reads back as NaN throughout)
+ * in head_dim / 2 + 4 bytes: 3.76 times less than bf16 at head_dim 128.
+ *
+ * A page holds page_size tokens of every key/value head of one layer; pages are numbered alike in
+ * all layers.  Memory order: layer, page, head, cell of 16 tokens; a cell is
+ *     [16 x head_dim/2 K codes][16 x head_dim/2 V codes][16 x (scale, low) K][16 x (scale, low) V]
+ * with scale and low as bf16 and, in each 32-bit word of codes, nibble n (from the low end) holding
+ * element {0,2,4,6,1,3,5,7}[n] of the word's eight.
+ *
+ * A token's place is its slot: page * page_size + offset.  The handle keeps host-side state only
+ * and is not thread-safe (as lora_pool_t).
+ * -------------------------------------------------------------------------------------- */
+typedef struct lora_kv lora_kv_t;
+
+typedef struct {
+    int32_t device;
+    int32_t num_layers;       /* >= 1 */
+    int32_t num_pages;        /* per layer; num_pages * page_size < 2^31 */
+    int32_t page_size;        /* tokens: 16, 32, 64 or 128 */
+    int32_t num_q_heads;      /* a multiple of num_kv_heads; at most 128 per key/value head */
+    int32_t num_kv_heads;
+    int32_t head_dim;         /* 64 or 128 */
+    void *device_buf;         /* dev, 256-byte aligned, >= lora_kv_bytes(); caller-owned */
+    size_t device_buf_bytes;
+} lora_kv_desc_t;
+
+/* Bytes of device memory the cache needs (a control block, then the layers).  device_buf is
+ * ignored.  Errors: INVALID_ARG, SHAPE. */
+lora_status_t lora_kv_bytes(const lora_kv_desc_t *desc, size_t *bytes);
+/* Byte offset of a layer's first page inside device_buf, and the bytes of one layer. */
+lora_status_t lora_kv_layer_range(const lora_kv_desc_t *desc, int32_t layer, size_t *offset, size_t *bytes);
+/* Creates the handle and clears the control block (synchronous).  The pages are left as they are:
+ * nothing reads a row that was not written.  Errors: INVALID_ARG, SHAPE, BUFFER_TOO_SMALL, CUDA. */
+lora_status_t lora_kv_create(const lora_kv_desc_t *desc, lora_kv_t **out);
+lora_status_t lora_kv_destroy(lora_kv_t *kv);
+
+/* Device status words since creation: [0] slots, positions or pages outside their range (such tokens
+ * are not rotated, not stored or not seen), [1] expired device-side waits (that call's outputs are
+ * not to be trusted), [2..3] reserved.  Synchronises `stream`; returns LORA_ERR_TIMEOUT when word 1
+ * is non-zero.  words_out (host, [4]) may be NULL. */
+lora_status_t lora_kv_check_status(lora_kv_t *kv, void *stream, int32_t *words_out);
+
+/*
+ * Tables of one batch of R requests that bring T new tokens in all, request r's q_len[r] tokens
+ * after the kv_len[r] it has in the cache (either may be 0).  Takes the pages that the new tokens
+ * need from a stack of free pages and writes, in `tables`, all int32, in this order:
+ *   header[16]    {R, T, sum of q_len, failed requests, negative lengths, pages taken, 0 ..}
+ *   start[R + 1]  first token of each request; start[R] = sum of q_len (no entry exceeds T)
+ *   kv_len[R]     lengths after the batch
+ *   position[T]   a token's position in its request (0 behind the last request's tokens)
+ *   slot[T]       its place in the cache, -1: none
+ *   (then words private to the library; lora_kv_tables_bytes counts them)
+ * Page k of the batch (k = 0, 1, .. in request order) is free_pages[*free_count - 1 - k]; block_table
+ * [r, i] (row r at r * ld_table, i = page number inside the request) is written for new pages and
+ * read for old ones.  A request gets all the pages it needs or fails: a request that needs pages
+ * fails once the pages needed up to and including it exceed the stack; so does one that needs more
+ * than ld_table pages, has more than max_q new tokens or tokens past T.  A failed request keeps its
+ * length, its slots are -1 and its attention is zero.  A negative length counts as 0.
+ * kv_len_out [R] and free_count_out [1] may be the inputs themselves or NULL.  window: 0, or how many
+ * keys a query sees, itself included (for the attention calls on these tables).  max_q bounds the
+ * batch's q_len; batches of single tokens (max_q = 1) skip what only prompts need.  0 = T.
+ * R <= 4096.  The result is an exact integer function of its inputs.
+ * Errors: INVALID_ARG, SHAPE, BUFFER_TOO_SMALL, CUDA.
+ */
+lora_status_t lora_kv_tables_bytes(const lora_kv_t *kv, int32_t R, int32_t T, size_t *bytes);
+lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const int32_t *q_len,
+                                   int32_t R, int32_t T, int32_t max_q, int32_t window,
+                                   const int32_t *free_pages, const int32_t *free_count,
+                                   int32_t *block_table, int64_t ld_table,
+                                   int32_t *kv_len_out, int32_t *free_count_out,
+                                   void *tables, size_t tables_bytes, void *stream);
+
+/* Gives the pages of n requests (dev int32 ids; an id outside 0 .. R - 1, a second mention and a page
+ * outside the cache are skipped) back to the stack: request by request in the order of the list, each
+ * one's pages in their order.  Their kv_len becomes 0 and their block-table entries -1.  A stack that
+ * would pass num_pages entries is cut there (a page was given back twice) and counted in status word 0.
+ * n <= 4096. */
+lora_status_t lora_kv_release(lora_kv_t *kv, const int32_t *requests, int32_t n, int32_t R,
+                              int32_t *kv_len, int32_t *block_table, int64_t ld_table,
+                              int32_t *free_pages, int32_t *free_count, void *stream);
+
+/*
+ * Norm and rotation of the queries and keys of T tokens, per head h of head_dim values x:
+ *     y_i = x_i * (1 / sqrt(mean(x^2) + eps)) * weight_i            (skipped where weight is NULL)
+ *     (y_a, y_b) -> (y_a c - y_b s, y_b c + y_a s)                  (skipped where cos_sin is NULL)
+ * in fp32, every operation rounded by itself (no fused multiply-add), the sum of squares taken as a
+ * tree: x_i^2 + x_{i + head_dim/2}^2 first, then neighbours with neighbours; so the result, and the
+ * 4-bit code of a key, does not depend on how the work is split.  Rounded once to bf16 at the store.
+ * cos_sin: fp32 [num_positions, rot_dim], rot_dim/2 cosines, then rot_dim/2 sines; pair p is elements
+ * (p, p + rot_dim/2), or (2p, 2p + 1) when interleaved; elements from rot_dim on are not rotated.
+ * q, k, v rows start at t * ld (elements) and hold heads * head_dim values each; they may be parts of
+ * one fused projection's rows.  q_out may be q and k_out may be k (same leading dimension).
+ */
+typedef struct {
+    int32_t device;
+    int32_t num_q_heads, num_kv_heads, head_dim;   /* head_dim 64 or 128; either count may be 0 */
+    int32_t rot_dim, interleaved;                  /* rot_dim: a multiple of 16, <= head_dim */
+    float eps;
+    int32_t num_positions;
+    const void *q;  int64_t ldq;                   /* dev bf16 */
+    const void *k;  int64_t ldk;
+    const void *v;  int64_t ldv;                   /* read by lora_kv_append only */
+    const void *q_weight, *k_weight;               /* dev bf16 [head_dim] or NULL */
+    const float *cos_sin;                          /* dev or NULL */
+    const int32_t *positions;                      /* dev [T]; needed with cos_sin */
+    void *q_out;    int64_t ldqo;                  /* dev bf16, or NULL with num_q_heads = 0 */
+    void *k_out;    int64_t ldko;                  /* may be NULL in lora_kv_append */
+} lora_qk_args_t;
+/* A token whose position is outside 0 .. num_positions - 1 is not rotated.
+ * Errors: INVALID_ARG, SHAPE, CUDA. */
+lora_status_t lora_qk_norm_rope(const lora_qk_args_t *args, int32_t T, void *stream);
+/* The same pass; the keys (before their rounding to bf16) and the values also go to their slots of
+ * `layer` as 4-bit rows.  slots: dev int32 [T], -1 = not stored; two tokens with one slot leave that
+ * row undefined.  The heads must be the cache's.  Errors: INVALID_ARG, SHAPE, SLOT_RANGE (layer), CUDA. */
+lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args,
+                             const int32_t *slots, int32_t T, void *stream);
+/* Rows of the cache as bf16, one per slot (zeros for a slot that is -1 or outside the cache): k_out
+ * and v_out are [n, num_kv_heads * head_dim] with leading dimensions; either may be NULL. */
+lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, int32_t n,
+                           void *k_out, int64_t ldk, void *v_out, int64_t ldv, void *stream);
+
+/*
+ * Attention of a batch over one layer of the cache: for token t of request r at position p and query
+ * head h, over the keys j in [max(0, p + 1 - window), p] of r that key/value head h / (num_q_heads /
+ * num_kv_heads) holds,
+ *     out[t, h] = sum_j softmax_j(scale * q[t, h] . k_j) v_j ,   lse[t, h] = log sum_j exp(scale * q . k_j)
+ * with k and v the values that the cache's rows stand for.  Call it after the batch's keys have been
+ * appended.  Queries of tokens without a request, of a failed request or without a key give zeros and
+ * lse = -inf; a key in a page outside the cache is not seen.  q, out: dev bf16 [T, num_q_heads *
+ * head_dim] with leading dimensions, out may not overlap q; lse: dev fp32 [T, num_q_heads] or NULL.
+ * tables: as written by lora_kv_build_tables for this R and T (and through this handle), block_table
+ * the one it was given.  Statistics and sums in fp32; probabilities enter the second product in
+ * fp16 (11 bits), everything else exactly.
+ * Errors: INVALID_ARG, SHAPE, SLOT_RANGE (layer), BUFFER_TOO_SMALL (workspace), CUDA.
+ */
+lora_status_t lora_kv_workspace_bytes(const lora_kv_t *kv, size_t *bytes);
+lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int64_t ldq,
+                                void *out, int64_t ldo, float *lse, float scale,
+                                const void *tables, int32_t R, int32_t T,
+                                const int32_t *block_table, int64_t ld_table,
+                                void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,9 @@ EXPORTS = [
     "lora_policy_create", "lora_policy_destroy", "lora_policy_lookup", "lora_policy_slot",
     "lora_policy_touch", "lora_policy_pin", "lora_policy_unpin", "lora_policy_choose_victim",
     "lora_policy_assign", "lora_policy_release", "lora_policy_admit", "lora_policy_stats",
+    "lora_kv_bytes", "lora_kv_layer_range", "lora_kv_create", "lora_kv_destroy", "lora_kv_check_status",
+    "lora_kv_tables_bytes", "lora_kv_build_tables", "lora_kv_release", "lora_qk_norm_rope",
+    "lora_kv_append", "lora_kv_read", "lora_kv_workspace_bytes", "lora_kv_attention",
 ]
 STATIC_SCRATCH_BYTES = 2 * 1024 * 1024
 
@@ -73,6 +76,28 @@ class _StepBuffers(ctypes.Structure):
                 ("y_dev", ctypes.c_void_p), ("slot_idx_dev", ctypes.c_void_p),
                 ("meta_dev", ctypes.c_void_p), ("meta_bytes", ctypes.c_size_t),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class _KvDesc(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("num_layers", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("device_buf", ctypes.c_void_p),
+                ("device_buf_bytes", ctypes.c_size_t)]
+
+
+class _QkArgs(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("num_positions", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+                ("k", ctypes.c_void_p), ("ldk", ctypes.c_int64),
+                ("v", ctypes.c_void_p), ("ldv", ctypes.c_int64),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("ldqo", ctypes.c_int64),
+                ("k_out", ctypes.c_void_p), ("ldko", ctypes.c_int64)]
 
 
 _handle = None
@@ -134,6 +159,20 @@ def _lib():
             "lora_policy_admit": [vp, ctypes.POINTER(i64), i32, ctypes.POINTER(i32),
                                   ctypes.POINTER(i32), ctypes.POINTER(i64), i32, ctypes.POINTER(i32)],
             "lora_policy_stats": [vp, ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(i64)],
+            "lora_kv_bytes": [ctypes.POINTER(_KvDesc), ctypes.POINTER(sz)],
+            "lora_kv_layer_range": [ctypes.POINTER(_KvDesc), i32, ctypes.POINTER(sz), ctypes.POINTER(sz)],
+            "lora_kv_create": [ctypes.POINTER(_KvDesc), ctypes.POINTER(vp)],
+            "lora_kv_destroy": [vp],
+            "lora_kv_check_status": [vp, vp, ctypes.POINTER(i32)],
+            "lora_kv_tables_bytes": [vp, i32, i32, ctypes.POINTER(sz)],
+            "lora_kv_build_tables": [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp, sz, vp],
+            "lora_kv_release": [vp, vp, i32, i32, vp, vp, i64, vp, vp, vp],
+            "lora_qk_norm_rope": [ctypes.POINTER(_QkArgs), i32, vp],
+            "lora_kv_append": [vp, i32, ctypes.POINTER(_QkArgs), vp, i32, vp],
+            "lora_kv_read": [vp, i32, vp, i32, vp, i64, vp, i64, vp],
+            "lora_kv_workspace_bytes": [vp, ctypes.POINTER(sz)],
+            "lora_kv_attention": [vp, i32, vp, i64, vp, i64, vp, ctypes.c_float, vp, i32, i32, vp, i64,
+                                  vp, sz, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -446,6 +485,134 @@ def apply_host(pool: int, target: int, kind: int, x_host, y_base_host, y_host, s
 
 
 # ------------------------------------------------------------------------------------------
+# the paged 4-bit key/value cache and the operators around it
+# ------------------------------------------------------------------------------------------
+def _kv_desc(num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim, device, buf=None,
+             buf_bytes=0):
+    return _KvDesc(int(device), int(num_layers), int(num_pages), int(page_size), int(num_q_heads),
+                   int(num_kv_heads), int(head_dim), _ptr(buf), int(buf_bytes))
+
+
+def kv_bytes(num_layers: int, num_pages: int, page_size: int, num_q_heads: int, num_kv_heads: int,
+             head_dim: int, device: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    d = _kv_desc(num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim, device)
+    _check(_lib().lora_kv_bytes(ctypes.byref(d), ctypes.byref(out)), "lora_kv_bytes")
+    return int(out.value)
+
+
+def kv_layer_range(layer: int, num_layers: int, num_pages: int, page_size: int, num_q_heads: int,
+                   num_kv_heads: int, head_dim: int, device: int = 0):
+    """(byte offset inside the device buffer, bytes) of one layer's pages."""
+    off, n = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    d = _kv_desc(num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim, device)
+    _check(_lib().lora_kv_layer_range(ctypes.byref(d), int(layer), ctypes.byref(off), ctypes.byref(n)),
+           "lora_kv_layer_range")
+    return int(off.value), int(n.value)
+
+
+def kv_create(num_layers: int, num_pages: int, page_size: int, num_q_heads: int, num_kv_heads: int,
+              head_dim: int, device_buf, device: int = 0, device_buf_bytes: Optional[int] = None) -> int:
+    out = ctypes.c_void_p(None)
+    nbytes = _nbytes(device_buf) if device_buf_bytes is None else device_buf_bytes
+    d = _kv_desc(num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim, device,
+                 device_buf, nbytes)
+    _check(_lib().lora_kv_create(ctypes.byref(d), ctypes.byref(out)), "lora_kv_create")
+    return int(out.value)
+
+
+def kv_destroy(kv: int) -> None:
+    _check(_lib().lora_kv_destroy(kv), "lora_kv_destroy")
+
+
+def kv_check_status(kv: int, stream=None):
+    """Synchronises `stream`; returns the four status words.  Raises LoraError(10) when a bounded
+    device-side wait has expired since the handle was created."""
+    w = (ctypes.c_int32 * 4)()
+    _check(_lib().lora_kv_check_status(kv, _stream(stream), w), "lora_kv_check_status")
+    return [int(v) for v in w]
+
+
+def kv_tables_bytes(kv: int, R: int, T: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib().lora_kv_tables_bytes(kv, int(R), int(T), ctypes.byref(out)), "lora_kv_tables_bytes")
+    return int(out.value)
+
+
+def kv_build_tables(kv: int, kv_len, q_len, R: int, T: int, free_pages, free_count, block_table,
+                    ld_table: int, tables, *, max_q: int = 0, window: int = 0, kv_len_out=None,
+                    free_count_out=None, tables_bytes: Optional[int] = None, stream=None) -> None:
+    nbytes = _nbytes(tables) if tables_bytes is None else tables_bytes
+    _check(_lib().lora_kv_build_tables(kv, _ptr(kv_len), _ptr(q_len), R, T, max_q, window,
+                                       _ptr(free_pages), _ptr(free_count), _ptr(block_table), ld_table,
+                                       _ptr(kv_len_out), _ptr(free_count_out), _ptr(tables), nbytes,
+                                       _stream(stream)), "lora_kv_build_tables")
+
+
+def kv_release(kv: int, requests, n: int, R: int, kv_len, block_table, ld_table: int, free_pages,
+               free_count, stream=None) -> None:
+    _check(_lib().lora_kv_release(kv, _ptr(requests), int(n), int(R), _ptr(kv_len), _ptr(block_table),
+                                  int(ld_table), _ptr(free_pages), _ptr(free_count), _stream(stream)),
+           "lora_kv_release")
+
+
+def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: int = 0, k=None,
+            ldk: int = 0, v=None, ldv: int = 0, q_weight=None, k_weight=None, eps: float = 0.0,
+            cos_sin=None, rot_dim: Optional[int] = None, num_positions: Optional[int] = None,
+            interleaved: bool = False, positions=None, q_out=None, ldqo: Optional[int] = None, k_out=None,
+            ldko: Optional[int] = None, device: int = 0):
+    """The argument block of qk_norm_rope and kv_append (build it once when the same buffers are used
+    again).  rot_dim, num_positions and the outputs' leading dimensions default to those of the tensors
+    given.  The tensors must stay alive while the block is used; it keeps them."""
+    if cos_sin is not None:
+        num_positions = int(cos_sin.shape[0]) if num_positions is None else num_positions
+        rot_dim = int(cos_sin.shape[1]) if rot_dim is None else rot_dim
+    if q_out is not None and ldqo is None:
+        ldqo = int(q_out.stride(0))
+    if k_out is not None and ldko is None:
+        ldko = int(k_out.stride(0))
+    a = _QkArgs(int(device), int(num_q_heads), int(num_kv_heads), int(head_dim), int(rot_dim or 0),
+                int(bool(interleaved)), float(eps), int(num_positions or 0), _ptr(q), int(ldq), _ptr(k),
+                int(ldk), _ptr(v), int(ldv), _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin),
+                _ptr(positions), _ptr(q_out), int(ldqo or 0), _ptr(k_out), int(ldko or 0))
+    a._keep = (q, k, v, q_weight, k_weight, cos_sin, positions, q_out, k_out)
+    return a
+
+
+def qk_norm_rope(args, T: int, stream=None) -> None:
+    """Per-head norm and rotation of T tokens' queries and keys; `args` from qk_args."""
+    _check(_lib().lora_qk_norm_rope(ctypes.byref(args), T, _stream(stream)), "lora_qk_norm_rope")
+
+
+def kv_append(kv: int, layer: int, args, slots, T: int, stream=None) -> None:
+    """qk_norm_rope with the keys and values also going to their slots of the cache as 4-bit rows."""
+    _check(_lib().lora_kv_append(kv, layer, ctypes.byref(args), _ptr(slots), T, _stream(stream)),
+           "lora_kv_append")
+
+
+def kv_read(kv: int, layer: int, slots, n: int, k_out, ldk: int, v_out, ldv: int, stream=None) -> None:
+    """Rows of the cache as the bf16 values they stand for."""
+    _check(_lib().lora_kv_read(kv, layer, _ptr(slots), n, _ptr(k_out), ldk, _ptr(v_out), ldv,
+                               _stream(stream)), "lora_kv_read")
+
+
+def kv_workspace_bytes(kv: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib().lora_kv_workspace_bytes(kv, ctypes.byref(out)), "lora_kv_workspace_bytes")
+    return int(out.value)
+
+
+def kv_attention(kv: int, layer: int, q, ldq: int, out, ldo: int, lse, scale: float, tables, R: int,
+                 T: int, block_table, ld_table: int, workspace, workspace_bytes_: Optional[int] = None,
+                 stream=None) -> None:
+    nbytes = (_nbytes(workspace) if workspace is not None else 0) \
+        if workspace_bytes_ is None else workspace_bytes_
+    _check(_lib().lora_kv_attention(kv, layer, _ptr(q), ldq, _ptr(out), ldo, _ptr(lse), scale, _ptr(tables),
+                                    R, T, _ptr(block_table), ld_table, _ptr(workspace), nbytes,
+                                    _stream(stream)), "lora_kv_attention")
+
+
+# ------------------------------------------------------------------------------------------
 # reading a metadata buffer copied back to the host
 # ------------------------------------------------------------------------------------------
 def unpack_segments(meta: np.ndarray, T: int, num_slots: int, tile_m: int) -> Dict[str, np.ndarray]:
@@ -463,4 +630,14 @@ def unpack_segments(meta: np.ndarray, T: int, num_slots: int, tile_m: int) -> Di
         o += n
     o = (o + 3) & ~3
     out["tile_desc"] = meta[o:o + 4 * cap_tile].reshape(cap_tile, 4).copy()   # library-private
+    return out
+
+
+def kv_table_views(tables, R: int, T: int):
+    """The public arrays inside a table buffer (a flat int32 tensor or array), as views of it."""
+    o = META_HEADER_WORDS
+    out = {"header": tables[:o]}
+    for name, n in [("start", R + 1), ("kv_len", R), ("position", T), ("slot", T)]:
+        out[name] = tables[o:o + n]
+        o += n
     return out

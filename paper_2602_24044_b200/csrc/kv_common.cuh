@@ -1,0 +1,130 @@
+// Shared declarations of the 4-bit paged key/value cache: host handle, cell format, batch tables.
+#pragma once
+
+#include "common.cuh"
+
+namespace lora {
+
+constexpr int KV_CELL = 16;            // tokens of one cell
+constexpr int KV_MAX_REQUESTS = 4096;  // of one batch (the table builder keeps them in shared memory)
+
+// One cell: [16 x D/2 K codes][16 x D/2 V codes][16 x (scale, low) of K][16 x (scale, low) of V].
+__host__ __device__ constexpr int kv_cell_bytes(int d) { return KV_CELL * (d + 8); }
+__host__ __device__ constexpr int kv_cell_params(int d) { return KV_CELL * d; }   // offset of K's (scale, low)
+
+struct KvView {                 // one layer, passed to kernels by value
+    unsigned char *cells;       // page 0 of the layer
+    int64_t page_bytes;         // heads * cells of a page * bytes of a cell
+    int64_t head_bytes;         // cells of a page * bytes of a cell
+    int32_t num_pages, page_size, page_shift;
+    int32_t hq, hkv, group;
+    int32_t *status;            // [STATUS_WORDS]
+};
+
+// Address of the cell that holds token `offset` (a multiple of 16 inside page `page`) of a head.
+__device__ __forceinline__ unsigned char *kv_cell(const KvView &v, int32_t page, int32_t head, int32_t offset,
+                                                  int cell_bytes) {
+    return v.cells + page * v.page_bytes + head * v.head_bytes + (int64_t)(offset / KV_CELL) * cell_bytes;
+}
+
+// ---------------------------------------------------------------------------------------------
+// batch tables (int32 words): public part as documented, then the attention's work lists
+// ---------------------------------------------------------------------------------------------
+enum { KVH_R = 0, KVH_T = 1, KVH_TOKENS = 2, KVH_FAILED = 3, KVH_NEGATIVE = 4, KVH_TAKEN = 5, KVH_WORDS = 16 };
+
+// A piece of attention work before it is multiplied by the key/value heads: some rows of one request
+// (row = token * group + query head inside its group) against a run of key chunks.  An item of n
+// chunks stands for hkv runs of n chunks, one per head, at hkv * start + head * n of the list's walk.
+struct __align__(16) KvItem {
+    int64_t start;     // chunks of the items before it (one head's)
+    int32_t req;
+    int32_t row0, nrows;
+    int32_t k_lo;      // first key, a multiple of the chunk
+    int32_t n;         // chunks, at least one
+    int32_t tok0;      // the request's first token
+    int32_t lim0;      // its token i sees keys below lim0 + i
+    int32_t reserved[3];
+};
+static_assert(sizeof(KvItem) == 48, "three 16-byte words");
+
+// The walk over a list (all items, heads and chunks in order) is cut into equal spans, one per walker:
+// a warp of the single-token kernel, a block of the prompt kernel.
+struct __align__(16) KvWalk {
+    int64_t total;     // hkv * chunks
+    int64_t span;
+    int32_t n_items;
+    int32_t reserved[3];
+};
+
+constexpr int KV_DEC_CHUNK = 32;       // keys of a chunk of the single-token walk
+constexpr int KV_PROMPT_CHUNK = 128;   // keys of a chunk of the prompt walk
+constexpr int KV_PROMPT_ROWS = 256;    // rows of an item of the prompt walk
+constexpr int KV_DEC_MAX_ROWS = 64;    // requests with more rows than this go to the prompt walk
+
+struct KvTables {
+    int64_t start, kv_len, position, slot;         // word offsets
+    int64_t walk;                                  // two KvWalk: single tokens, prompts
+    int64_t dec_items, pr_items;                   // KvItem lists
+    int64_t dec_first, pr_first;                   // first item of each walker
+    int64_t words;
+    int32_t cap_dec, cap_pr;
+};
+
+__host__ __device__ inline KvTables kv_tables(int32_t R, int32_t T, int32_t group, int32_t dec_walkers,
+                                              int32_t pr_walkers) {
+    KvTables L;
+    int64_t o = KVH_WORDS;
+    L.start = o;    o += (int64_t)R + 1;
+    L.kv_len = o;   o += R;
+    L.position = o; o += T;
+    L.slot = o;     o += T;
+    o = (o + 3) & ~(int64_t)3;
+    // a request of q tokens has ceil(q * group / rows) items: at most one more than q * group / rows
+    const int64_t rows = (int64_t)T * group;
+    int64_t cd = R + rows / 8, cp = R + rows / KV_PROMPT_ROWS;
+    L.cap_dec = (int32_t)(cd < 0x7fffffff ? cd : 0x7fffffff);
+    L.cap_pr = (int32_t)(cp < 0x7fffffff ? cp : 0x7fffffff);
+    L.walk = o;      o += 2 * (int64_t)(sizeof(KvWalk) / 4);
+    L.dec_items = o; o += cd * (int64_t)(sizeof(KvItem) / 4);
+    L.pr_items = o;  o += cp * (int64_t)(sizeof(KvItem) / 4);
+    L.dec_first = o; o += dec_walkers;
+    L.pr_first = o;  o += pr_walkers;
+    L.words = (o + 3) & ~(int64_t)3;
+    return L;
+}
+
+struct KvTableRecord {        // what the host knows of a table it built
+    const void *ptr;
+    int32_t R, T, max_q, window;
+};
+
+}  // namespace lora
+
+struct lora_kv {
+    int32_t device = 0, num_layers = 0, num_pages = 0, page_size = 0, page_shift = 0;
+    int32_t hq = 0, hkv = 0, group = 0, d = 0;
+    unsigned char *base = nullptr;
+    int32_t *status_dev = nullptr;
+    int64_t page_bytes = 0, layer_bytes = 0;
+    int32_t sm_count = 148;
+    size_t tables_attr_smem = 0;      // dynamic shared memory the table builder has been allowed
+    std::vector<lora::KvTableRecord> tables;
+
+    void remember(const void *ptr, int32_t R, int32_t T, int32_t max_q, int32_t window) {
+        for (lora::KvTableRecord &t : tables)
+            if (t.ptr == ptr) { t = {ptr, R, T, max_q, window}; return; }
+        if (tables.size() >= 256) tables.erase(tables.begin());
+        tables.push_back({ptr, R, T, max_q, window});
+    }
+    const lora::KvTableRecord *find(const void *ptr, int32_t R, int32_t T) const {
+        for (const lora::KvTableRecord &t : tables)
+            if (t.ptr == ptr && t.R == R && t.T == T) return &t;
+        return nullptr;
+    }
+    lora::KvView view(int32_t layer) const;
+    // Rows of one item of the single-token walk: 8, or 16 where a token alone has more than 8 or a
+    // request may bring several tokens.
+    int32_t dec_rows(int32_t max_q) const { return (int64_t)max_q * group <= 8 ? 8 : 16; }
+    int32_t dec_walkers() const { return sm_count * 16; }
+    int32_t pr_walkers() const { return sm_count; }
+};

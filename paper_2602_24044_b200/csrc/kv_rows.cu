@@ -1,0 +1,481 @@
+// Rows into and out of the cache: per-head norm and rotation of queries and keys, the 4-bit write of
+// keys and values in the same pass, and the read back.
+//
+// y = x / sqrt(mean(x^2) + eps) * w, rotated; a key or value row then becomes 4-bit codes with one scale
+// and one low value.  A stream: every input is read once and every output written once, with no reuse but
+// the angles of a token, which all its heads share.  A head is held by head_dim / 16 lanes of a warp, each
+// with two runs of 8 elements (i.. and head_dim/2 + i..: both partners of a rotation pair when the whole
+// head is rotated, and two 16-byte loads), so the norm's sum and a row's minimum and maximum are three
+// shuffles and nothing goes through shared memory.  Every operation is rounded by itself (the _rn
+// intrinsics are never contracted), the sum is a fixed tree: the codes do not depend on the launch.
+#include <cstring>
+
+#include "kv_common.cuh"
+
+namespace lora {
+
+struct RowParams {
+    const __nv_bfloat16 *q, *k, *v, *qw, *kw;
+    const float *cos_sin;
+    const int32_t *positions, *slots;
+    __nv_bfloat16 *q_out, *k_out;
+    int64_t ldq, ldk, ldv, ldqo, ldko;
+    int32_t T, hq, hk, num_positions, rot_dim, heads_per_warp;
+    float eps;
+    KvView kv;          // with slots
+    int32_t *status;    // NULL without a cache
+};
+
+struct Row { float a[8], b[8]; };   // elements 8 j .. 8 j + 7 and D/2 + 8 j .. of lane j of the head
+
+__device__ __forceinline__ void unpack8(const uint4 &u, float (&f)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int D>
+__device__ __forceinline__ void norm_row(Row &x, const float (&wa)[8], const float (&wb)[8], float eps) {
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = __fadd_rn(__fmul_rn(x.a[i], x.a[i]), __fmul_rn(x.b[i], x.b[i]));
+#pragma unroll
+    for (int n = 4; n; n >>= 1)
+#pragma unroll
+        for (int i = 0; i < n; ++i) s[i] = __fadd_rn(s[2 * i], s[2 * i + 1]);
+#pragma unroll
+    for (int d = 1; d < D / 16; d <<= 1) s[0] = __fadd_rn(s[0], __shfl_xor_sync(0xffffffffu, s[0], d));
+    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(s[0], 1.0f / D), eps)));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x.a[i] = __fmul_rn(__fmul_rn(x.a[i], r), wa[i]);
+        x.b[i] = __fmul_rn(__fmul_rn(x.b[i], r), wb[i]);
+    }
+}
+
+__device__ __forceinline__ void rotate_pair(float &a, float &b, float c, float s) {
+    const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+    b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+    a = x;
+}
+
+enum { ROT_NONE = 0, ROT_HALF = 1, ROT_PART = 2, ROT_PAIRS = 3 };
+
+// The angles a lane needs.  HALF: pairs (i, i + D/2), both in this lane.  PART: pairs (i, i + rot/2) with
+// rot < D, the partner in another lane of the head.  PAIRS: (2 p, 2 p + 1), both in this lane.
+template <int ROT>
+struct Angles { float c[8], s[8]; };
+
+template <int D, int ROT>
+__device__ __forceinline__ void load_angles(Angles<ROT> &A, const float *row, int rot_dim, int j) {
+    if (ROT == ROT_HALF) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 c = __ldg(reinterpret_cast<const float4 *>(row + 8 * j + i));
+            const float4 s = __ldg(reinterpret_cast<const float4 *>(row + D / 2 + 8 * j + i));
+            A.c[i] = c.x; A.c[i + 1] = c.y; A.c[i + 2] = c.z; A.c[i + 3] = c.w;
+            A.s[i] = s.x; A.s[i + 1] = s.y; A.s[i + 2] = s.z; A.s[i + 3] = s.w;
+        }
+    } else if (ROT == ROT_PAIRS) {   // pairs 4 j .. in the first run, D/4 + 4 j .. in the second
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int p = (i < 4 ? 4 * j + i : D / 4 + 4 * j + i - 4);
+            const bool in = 2 * p < rot_dim;
+            A.c[i] = in ? __ldg(row + p) : 1.0f;
+            A.s[i] = in ? __ldg(row + rot_dim / 2 + p) : 0.0f;
+        }
+    }
+}
+
+// The rotated run (0: x.a, 1: x.b) of a head whose first rot_dim < D elements are rotated: the partner of
+// element e is e +- rot/2.  rot/2 is a multiple of 8, so the eight elements of a run have their partners
+// in one run of one lane.
+template <int D>
+__device__ __forceinline__ void rotate_part(const Row &x, int run, const float *row, int rot_dim, int j, float (&o)[8]) {
+    const int half = rot_dim / 2, e = run * (D / 2) + 8 * j;
+    const bool first = e < half, in = e < rot_dim;
+    const int pe = first ? e + half : in ? e - half : e;
+    const int src = (threadIdx.x & 31) - j + (pe / 8) % (D / 16);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // a lane sends both of its runs: which one the reader wants is the reader's to choose
+        const float pa = __shfl_sync(0xffffffffu, x.a[i], src), pb = __shfl_sync(0xffffffffu, x.b[i], src);
+        const float other = pe >= D / 2 ? pb : pa, mine = run ? x.b[i] : x.a[i];
+        o[i] = mine;
+        if (in) {
+            const int p = (first ? e : e - half) + i;
+            const float c = __ldg(row + p), s = __ldg(row + half + p);
+            o[i] = first ? __fsub_rn(__fmul_rn(mine, c), __fmul_rn(other, s))
+                         : __fadd_rn(__fmul_rn(mine, c), __fmul_rn(other, s));
+        }
+    }
+}
+
+template <int D, int ROT>
+__device__ __forceinline__ void rotate_row(Row &x, const Angles<ROT> &A, const float *row, int rot_dim, int j) {
+    if (ROT == ROT_HALF) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rotate_pair(x.a[i], x.b[i], A.c[i], A.s[i]);
+    } else if (ROT == ROT_PAIRS) {   // pairs past rot_dim have cosine 1 and sine 0, but -0 and NaN must pass unchanged
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (8 * j + 2 * i < rot_dim) rotate_pair(x.a[2 * i], x.a[2 * i + 1], A.c[i], A.s[i]);
+            if (D / 2 + 8 * j + 2 * i < rot_dim) rotate_pair(x.b[2 * i], x.b[2 * i + 1], A.c[4 + i], A.s[4 + i]);
+        }
+    } else if (ROT == ROT_PART) {
+        float na[8], nb[8];
+        rotate_part<D>(x, 0, row, rot_dim, j, na);
+        rotate_part<D>(x, 1, row, rot_dim, j, nb);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { x.a[i] = na[i]; x.b[i] = nb[i]; }
+    }
+}
+
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Eight codes as a word: nibble n holds element {0,2,4,6,1,3,5,7}[n], so that (word >> 4 i) & 0x000f000f
+// is elements 2 i and 2 i + 1.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float low, float inv, bool bad) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float c = fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], low), inv)), 0.0f), 15.0f);
+        w |= (uint32_t)(int)c << (4 * ((i >> 1) + 4 * (i & 1)));
+    }
+    return bad ? 0u : w;
+}
+// One head's row as 4-bit codes: the words of runs a and b, and (scale, low) as two bf16.
+template <int D>
+__device__ __forceinline__ void quantise_row(const Row &x, uint32_t &wa, uint32_t &wb, uint32_t &param) {
+    float lo = x.a[0], hi = x.a[0];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo = min_nan(lo, min_nan(x.a[i], x.b[i]));
+        hi = max_nan(hi, max_nan(x.a[i], x.b[i]));
+    }
+#pragma unroll
+    for (int d = 1; d < D / 16; d <<= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+    }
+    const float low = __bfloat162float(__float2bfloat16_rn(lo));
+    float scale = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, low), 15.0f)));
+    if (scale < 1.17549435e-38f) scale = 0.0f;
+    const bool bad = !(fabsf(scale) < INFINITY) || !(fabsf(low) < INFINITY);
+    const float inv = scale == 0.0f ? 0.0f : __fdiv_rn(1.0f, scale);
+    wa = codes8(x.a, low, inv, bad);
+    wb = codes8(x.b, low, inv, bad);
+    param = bad ? 0x7fc07fc0u : __float_as_uint(scale) >> 16 | (__float_as_uint(low) & 0xffff0000u);
+}
+
+// A warp takes one token and `heads_per_warp` x (32 / (D/16)) consecutive heads of its row of query, key
+// and (with a cache) value heads.  The angles are loaded once per warp.
+template <int D, int ROT, bool CACHE>
+__global__ void __launch_bounds__(256) rows_kernel(const RowParams P) {
+    constexpr int LPH = D / 16, HPP = 32 / LPH;     // lanes of a head, heads of a pass
+    const int lane = threadIdx.x & 31, j = lane % LPH, g = lane / LPH;
+    const int heads = P.hq + P.hk + (CACHE ? P.hk : 0);
+    const int per = P.heads_per_warp * HPP;
+    const int parts = (heads + per - 1) / per;
+    const int64_t wid = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t t64 = wid / parts;
+    if (t64 >= P.T) return;     // whole warps
+    const int32_t t = (int32_t)t64;
+    const int h0 = (int)(wid - t64 * parts) * per, h1 = min(h0 + per, heads);
+
+    const float *row = nullptr;
+    Angles<ROT> A;
+    bool turn = false;
+    if (ROT != ROT_NONE) {
+        const int32_t pos = __ldg(P.positions + t);
+        turn = pos >= 0 && pos < P.num_positions;
+        row = P.cos_sin + (int64_t)(turn ? pos : 0) * P.rot_dim;
+        if (turn) load_angles<D, ROT>(A, row, P.rot_dim, j);
+        else if (P.status && h0 == 0 && lane == 0) atomicAdd(&P.status[STATUS_INVALID_TOKENS], 1);
+    }
+    int32_t slot = -1;
+    if (CACHE) {
+        slot = __ldg(P.slots + t);
+        const bool in = slot >= 0 && (slot >> P.kv.page_shift) < P.kv.num_pages;
+        if (!in && slot != -1 && h0 == 0 && lane == 0) atomicAdd(&P.kv.status[STATUS_INVALID_TOKENS], 1);
+        if (!in) slot = -1;
+    }
+    for (int hb = h0; hb < h1; hb += HPP) {
+        const int h = hb + g;
+        const bool live = h < h1;
+        // 0 query, 1 key, 2 value
+        const int kind = h < P.hq ? 0 : h < P.hq + P.hk ? 1 : 2;
+        const int hh = kind == 0 ? h : kind == 1 ? h - P.hq : h - P.hq - P.hk;
+        Row x;
+        if (live) {
+            const __nv_bfloat16 *src = kind == 0 ? P.q + t * P.ldq : kind == 1 ? P.k + t * P.ldk : P.v + t * P.ldv;
+            src += hh * D + 8 * j;
+            unpack8(*reinterpret_cast<const uint4 *>(src), x.a);
+            unpack8(*reinterpret_cast<const uint4 *>(src + D / 2), x.b);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x.a[i] = x.b[i] = 0.0f;
+        }
+        // lanes of one warp may hold query, key and value heads: every shuffle is executed by all of them
+        Row y = x;
+        const __nv_bfloat16 *w = kind == 0 ? P.qw : P.kw;
+        if (P.qw || P.kw) {
+            float wa[8], wb[8];
+            const bool norm = live && kind < 2 && w;
+            if (norm) {
+                unpack8(__ldg(reinterpret_cast<const uint4 *>(w + 8 * j)), wa);
+                unpack8(__ldg(reinterpret_cast<const uint4 *>(w + D / 2 + 8 * j)), wb);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wa[i] = wb[i] = 1.0f;
+            }
+            norm_row<D>(y, wa, wb, P.eps);
+            if (!norm) y = x;
+        }
+        if (ROT != ROT_NONE && turn) {   // `turn` is the token's, the same in the whole warp
+            const Row z = y;
+            rotate_row<D, ROT>(y, A, row, P.rot_dim, j);
+            if (kind == 2) y = z;
+        }
+        if (live && kind == 0) {
+            __nv_bfloat16 *dst = P.q_out + t * P.ldqo + hh * D + 8 * j;
+            *reinterpret_cast<uint4 *>(dst) = pack8(y.a);
+            *reinterpret_cast<uint4 *>(dst + D / 2) = pack8(y.b);
+        }
+        if (live && kind == 1 && P.k_out) {
+            __nv_bfloat16 *dst = P.k_out + t * P.ldko + hh * D + 8 * j;
+            *reinterpret_cast<uint4 *>(dst) = pack8(y.a);
+            *reinterpret_cast<uint4 *>(dst + D / 2) = pack8(y.b);
+        }
+        if (CACHE && hb + HPP > P.hq) {   // some lane holds a key or a value (the same for all lanes)
+            uint32_t wa, wb, param;
+            quantise_row<D>(y, wa, wb, param);
+            if (live && kind > 0 && slot >= 0) {
+                const int off = slot & (P.kv.page_size - 1), r = off % KV_CELL;
+                unsigned char *cell = kv_cell(P.kv, slot >> P.kv.page_shift, hh, off, kv_cell_bytes(D));
+                uint32_t *codes = reinterpret_cast<uint32_t *>(cell + ((kind - 1) * KV_CELL + r) * (D / 2));
+                codes[j] = wa;
+                codes[D / 16 + j] = wb;
+                if (j == 0)
+                    *reinterpret_cast<uint32_t *>(cell + kv_cell_params(D) + ((kind - 1) * KV_CELL + r) * 4) = param;
+            }
+        }
+    }
+}
+
+// Rows of the cache as bf16: low + scale * code, the product exact in fp32, one rounding of the sum, one
+// to bf16.  A lane takes 8 elements of one row: one word of codes, one 16-byte store.
+template <int D>
+__global__ void __launch_bounds__(256)
+read_kernel(const KvView kv, const int32_t *slots, int32_t n, __nv_bfloat16 *k_out, int64_t ldk,
+            __nv_bfloat16 *v_out, int64_t ldv) {
+    constexpr int W = D / 8;                       // words of a row
+    const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int w = (int)(unit % W);
+    const int64_t rest = unit / W;
+    const int rows = 2 * kv.hkv;                   // key rows, then value rows of a token
+    const int64_t i = rest / rows;
+    if (i >= n) return;
+    const int which = (int)(rest - i * rows) / kv.hkv, h = (int)(rest - i * rows) % kv.hkv;
+    __nv_bfloat16 *dst = which ? v_out : k_out;
+    if (!dst) return;
+    dst += i * (which ? ldv : ldk) + h * D + w * 8;
+    const int32_t slot = __ldg(slots + i);
+    float f[8];
+    if (slot >= 0 && (slot >> kv.page_shift) < kv.num_pages) {
+        const int off = slot & (kv.page_size - 1), r = off % KV_CELL;
+        const unsigned char *cell = kv_cell(kv, slot >> kv.page_shift, h, off, kv_cell_bytes(D));
+        const uint32_t c = *reinterpret_cast<const uint32_t *>(cell + (which * KV_CELL + r) * (D / 2) + w * 4);
+        const uint32_t p = *reinterpret_cast<const uint32_t *>(cell + kv_cell_params(D) + (which * KV_CELL + r) * 4);
+        const float scale = __uint_as_float(p << 16), low = __uint_as_float(p & 0xffff0000u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            f[e] = __fadd_rn(__fmul_rn((float)((c >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15u), scale), low);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = 0.0f;
+    }
+    *reinterpret_cast<uint4 *>(dst) = pack8(f);
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+// Do T rows of `wa` bytes at pitch `lda` and T rows of `wb` bytes at pitch `ldb` touch?  Rows of one
+// pitch may interleave (parts of a fused projection's rows).
+static bool rows_overlap(const void *a, int64_t wa, int64_t lda, const void *b, int64_t wb, int64_t ldb, int32_t T) {
+    const char *pa = (const char *)a, *pb = (const char *)b;
+    const char *ea = pa + (T - 1) * lda + wa, *eb = pb + (T - 1) * ldb + wb;
+    if (ea <= pb || eb <= pa) return false;
+    if (lda != ldb) return true;
+    int64_t d = (pb - pa) % lda;
+    if (d < 0) d += lda;
+    return d < wa || d + wb > lda;
+}
+
+static lora_status_t check_rows(const void *p, int64_t ld, int32_t heads, int32_t d) {
+    if (!p || ((uintptr_t)p & 15)) return LORA_ERR_INVALID_ARG;
+    if (ld < (int64_t)heads * d || ld % 8) return LORA_ERR_SHAPE;
+    return LORA_OK;
+}
+
+static lora_status_t fill_rows(const lora_qk_args_t *a, int32_t T, bool cache, RowParams *P) {
+    if (!a) return LORA_ERR_INVALID_ARG;
+    if (T < 0 || a->num_q_heads < 0 || a->num_kv_heads < 0) return LORA_ERR_SHAPE;
+    if (a->num_q_heads > 65536 || a->num_kv_heads > 65536) return LORA_ERR_SHAPE;
+    const int32_t d = a->head_dim, hq = a->num_q_heads, hk = a->num_kv_heads;
+    if (d != 64 && d != 128) return LORA_ERR_SHAPE;
+    if (hq + hk == 0) return LORA_ERR_SHAPE;
+    if (a->cos_sin) {
+        if (a->rot_dim < 16 || a->rot_dim > d || a->rot_dim % 16 || a->num_positions < 1) return LORA_ERR_SHAPE;
+        if (!a->positions || ((uintptr_t)a->cos_sin & 15)) return LORA_ERR_INVALID_ARG;
+    }
+    if (!(a->eps >= 0.0f)) return LORA_ERR_INVALID_ARG;
+    if (((uintptr_t)a->q_weight | (uintptr_t)a->k_weight) & 15) return LORA_ERR_INVALID_ARG;
+    lora_status_t s = LORA_OK;
+    if (T == 0) return s;
+    if (hq && (s = check_rows(a->q, a->ldq, hq, d)) != LORA_OK) return s;
+    if (hq && (s = check_rows(a->q_out, a->ldqo, hq, d)) != LORA_OK) return s;
+    if (hk && (s = check_rows(a->k, a->ldk, hk, d)) != LORA_OK) return s;
+    if (hk && (a->k_out || !cache) && (s = check_rows(a->k_out, a->ldko, hk, d)) != LORA_OK) return s;
+    if (hk && cache && (s = check_rows(a->v, a->ldv, hk, d)) != LORA_OK) return s;
+    // an output may be its own input in place; anything else it may not touch
+    const int64_t bq = (int64_t)hq * d * 2, bk = (int64_t)hk * d * 2;
+    const void *out[2] = {hq ? a->q_out : nullptr, hk ? a->k_out : nullptr};
+    const int64_t wo[2] = {bq, bk}, lo[2] = {a->ldqo * 2, a->ldko * 2};
+    const void *in[3] = {hq ? a->q : nullptr, hk ? a->k : nullptr, hk && cache ? a->v : nullptr};
+    const int64_t wi[3] = {bq, bk, bk}, li[3] = {a->ldq * 2, a->ldk * 2, a->ldv * 2};
+    for (int o = 0; o < 2; ++o)
+        for (int i = 0; i < 3; ++i) {
+            if (!out[o] || !in[i]) continue;
+            if (o == i && out[o] == in[i] && lo[o] == li[i]) continue;
+            if (rows_overlap(out[o], wo[o], lo[o], in[i], wi[i], li[i], T)) return LORA_ERR_INVALID_ARG;
+        }
+    if (out[0] && out[1] && rows_overlap(out[0], wo[0], lo[0], out[1], wo[1], lo[1], T)) return LORA_ERR_INVALID_ARG;
+    P->q = (const __nv_bfloat16 *)a->q;
+    P->k = (const __nv_bfloat16 *)a->k;
+    P->v = (const __nv_bfloat16 *)a->v;
+    P->qw = (const __nv_bfloat16 *)a->q_weight;
+    P->kw = (const __nv_bfloat16 *)a->k_weight;
+    P->cos_sin = a->cos_sin;
+    P->positions = a->positions;
+    P->slots = nullptr;
+    P->q_out = (__nv_bfloat16 *)a->q_out;
+    P->k_out = (__nv_bfloat16 *)a->k_out;
+    P->ldq = a->ldq; P->ldk = a->ldk; P->ldv = a->ldv; P->ldqo = a->ldqo; P->ldko = a->ldko;
+    P->T = T;
+    P->hq = hq;
+    P->hk = hk;
+    P->num_positions = a->num_positions;
+    P->rot_dim = a->rot_dim;
+    P->eps = a->eps;
+    P->status = nullptr;
+    memset(&P->kv, 0, sizeof(P->kv));
+    return LORA_OK;
+}
+
+template <int D, int ROT, bool CACHE>
+static void launch_rows(const RowParams &P, int64_t blocks, cudaStream_t s) {
+    rows_kernel<D, ROT, CACHE><<<(unsigned)blocks, 256, 0, s>>>(P);
+}
+template <int D, bool CACHE>
+static void launch_rows_rot(const RowParams &P, int rot, int64_t blocks, cudaStream_t s) {
+    if (rot == ROT_NONE) launch_rows<D, ROT_NONE, CACHE>(P, blocks, s);
+    else if (rot == ROT_HALF) launch_rows<D, ROT_HALF, CACHE>(P, blocks, s);
+    else if (rot == ROT_PART) launch_rows<D, ROT_PART, CACHE>(P, blocks, s);
+    else launch_rows<D, ROT_PAIRS, CACHE>(P, blocks, s);
+}
+
+static lora_status_t run_rows(const lora_qk_args_t *a, RowParams &P, bool cache, cudaStream_t stream) {
+    const int d = a->head_dim;
+    const int rot = !a->cos_sin ? ROT_NONE : a->interleaved ? ROT_PAIRS : a->rot_dim == d ? ROT_HALF : ROT_PART;
+    const int heads = P.hq + P.hk * (cache ? 2 : 1), pass = 512 / d;   // heads of one pass of a warp
+    P.heads_per_warp = 1;
+    const int parts = (heads + pass * P.heads_per_warp - 1) / (pass * P.heads_per_warp);
+    const int64_t blocks = ((int64_t)P.T * parts + 7) / 8;
+    if (blocks > 0x7fffffff) return LORA_ERR_SHAPE;
+    if (d == 64) {
+        if (cache) launch_rows_rot<64, true>(P, rot, blocks, stream);
+        else launch_rows_rot<64, false>(P, rot, blocks, stream);
+    } else {
+        if (cache) launch_rows_rot<128, true>(P, rot, blocks, stream);
+        else launch_rows_rot<128, false>(P, rot, blocks, stream);
+    }
+    return count_launch();
+}
+
+}  // namespace lora
+
+using namespace lora;
+
+extern "C" {
+
+lora_status_t lora_qk_norm_rope(const lora_qk_args_t *args, int32_t T, void *stream) {
+    RowParams P;
+    lora_status_t s = fill_rows(args, T, false, &P);
+    if (s != LORA_OK || T == 0) return s;
+    DeviceGuard g(args->device);
+    return run_rows(args, P, false, (cudaStream_t)stream);
+}
+
+lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args, const int32_t *slots,
+                             int32_t T, void *stream) {
+    if (!kv || !args) return LORA_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= kv->num_layers) return LORA_ERR_SLOT_RANGE;
+    if (args->head_dim != kv->d || args->num_kv_heads != kv->hkv) return LORA_ERR_SHAPE;
+    if (args->num_q_heads != kv->hq && args->num_q_heads != 0) return LORA_ERR_SHAPE;
+    RowParams P;
+    lora_status_t s = fill_rows(args, T, true, &P);
+    if (s != LORA_OK || T == 0) return s;
+    if (!slots) return LORA_ERR_INVALID_ARG;
+    P.slots = slots;
+    P.kv = kv->view(layer);
+    P.status = kv->status_dev;
+    DeviceGuard g(kv->device);
+    return run_rows(args, P, true, (cudaStream_t)stream);
+}
+
+lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, int32_t n, void *k_out, int64_t ldk,
+                           void *v_out, int64_t ldv, void *stream) {
+    if (!kv) return LORA_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= kv->num_layers) return LORA_ERR_SLOT_RANGE;
+    if (n < 0) return LORA_ERR_SHAPE;
+    if (n == 0) return LORA_OK;
+    if (!slots) return LORA_ERR_INVALID_ARG;
+    lora_status_t s;
+    if (k_out && (s = check_rows(k_out, ldk, kv->hkv, kv->d)) != LORA_OK) return s;
+    if (v_out && (s = check_rows(v_out, ldv, kv->hkv, kv->d)) != LORA_OK) return s;
+    if (!k_out && !v_out) return LORA_OK;
+    const int64_t units = (int64_t)n * 2 * kv->hkv * (kv->d / 8), blocks = (units + 255) / 256;
+    if (blocks > 0x7fffffff) return LORA_ERR_SHAPE;
+    DeviceGuard g(kv->device);
+    if (kv->d == 64)
+        read_kernel<64><<<(unsigned)blocks, 256, 0, (cudaStream_t)stream>>>(
+            kv->view(layer), slots, n, (__nv_bfloat16 *)k_out, ldk, (__nv_bfloat16 *)v_out, ldv);
+    else
+        read_kernel<128><<<(unsigned)blocks, 256, 0, (cudaStream_t)stream>>>(
+            kv->view(layer), slots, n, (__nv_bfloat16 *)k_out, ldk, (__nv_bfloat16 *)v_out, ldv);
+    return count_launch();
+}
+
+}  // extern "C"

@@ -186,3 +186,98 @@ class Session:
 
     def __exit__(self, *exc):
         self.close()
+
+
+class KVCache:
+    """A paged 4-bit key/value cache on one GPU with the table buffer and workspace of its calls.
+
+    The caller keeps the requests' state (lengths, block table, stack of free pages) as int32 device
+    tensors; build_tables() advances it for one batch, then append() and attention() run per layer on
+    the tables it left."""
+
+    def __init__(self, num_layers: int, num_pages: int, page_size: int, num_q_heads: int, num_kv_heads: int,
+                 head_dim: int, device: int = 0):
+        self.device = torch.device("cuda", int(device))
+        self.shape = (num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim)
+        nbytes = lb.kv_bytes(*self.shape, device=int(device))
+        self.buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        off = (-self.buf.data_ptr()) % 256
+        self.mem = self.buf[off:off + nbytes]
+        self.kv = lb.kv_create(*self.shape, self.mem, device=int(device))
+        self.workspace = torch.empty(lb.kv_workspace_bytes(self.kv), dtype=torch.uint8, device=self.device)
+        self._workspace_bytes = self.workspace.numel()
+        self.tables = None
+        self.R = self.T = 0
+
+    def layer(self, layer: int) -> torch.Tensor:
+        """One layer's pages as bytes (a view)."""
+        off, n = lb.kv_layer_range(layer, *self.shape, device=self.device.index)
+        return self.mem[off:off + n]
+
+    def reserve(self, R: int, T: int) -> None:
+        """Makes room for the tables of a batch of R requests and T new tokens."""
+        words = lb.kv_tables_bytes(self.kv, R, T) // 4
+        if self.tables is None or self.tables.numel() < words:
+            self.tables = torch.empty(words, dtype=torch.int32, device=self.device)
+            self.R = -1
+        if (R, T) != (self.R, self.T):
+            self.R, self.T = R, T
+            v = lb.kv_table_views(self.tables, R, T)
+            self.header, self.starts, self.lengths = v["header"], v["start"], v["kv_len"]
+            self.positions, self.slots = v["position"], v["slot"]
+
+    def build_tables(self, kv_len, q_len, T: int, free_pages, free_count, block_table, *, max_q: int = 0,
+                     window: int = 0, kv_len_out=None, free_count_out=None, stream=None) -> None:
+        """Tables of a batch; kv_len and free_count are advanced in place unless *_out names other
+        tensors."""
+        R = int(kv_len.shape[0])
+        if q_len.shape != (R,) or block_table.shape[0] != R:
+            raise ValueError("q_len and block_table need one entry and one row per request (%d)" % R)
+        self.reserve(R, T)
+        self.block_table, self.ld_table = block_table, int(block_table.stride(0))
+        lb.kv_build_tables(self.kv, kv_len, q_len, R, T, free_pages, free_count, block_table, self.ld_table,
+                           self.tables, max_q=max_q, window=window,
+                           kv_len_out=kv_len if kv_len_out is None else kv_len_out,
+                           free_count_out=free_count if free_count_out is None else free_count_out,
+                           stream=stream)
+
+    def release(self, requests, kv_len, block_table, free_pages, free_count, stream=None) -> None:
+        lb.kv_release(self.kv, requests, int(requests.shape[0]), int(kv_len.shape[0]), kv_len, block_table,
+                      int(block_table.stride(0)), free_pages, free_count, stream=stream)
+
+    def append(self, layer: int, args, slots=None, T: Optional[int] = None, stream=None) -> None:
+        """args: binding.qk_args(...); slots: default those of the tables."""
+        lb.kv_append(self.kv, layer, args, self.slots if slots is None else slots,
+                     self.T if T is None else T, stream=stream)
+
+    def read(self, layer: int, slots, k_out, v_out, stream=None) -> None:
+        lb.kv_read(self.kv, layer, slots, int(slots.shape[0]), k_out, 0 if k_out is None else k_out.stride(0),
+                   v_out, 0 if v_out is None else v_out.stride(0), stream=stream)
+
+    def attention(self, layer: int, q, out, *, scale: float, lse=None, stream=None) -> None:
+        lb.kv_attention(self.kv, layer, q, q.stride(0), out, out.stride(0), lse, scale, self.tables, self.R,
+                        self.T, self.block_table, self.ld_table, self.workspace, self._workspace_bytes,
+                        stream=stream)
+
+    def status(self, stream=None):
+        return lb.kv_check_status(self.kv, stream)
+
+    def close(self):
+        if self.kv:
+            torch.cuda.synchronize(self.device)
+            lb.kv_destroy(self.kv)
+            self.kv = 0
+
+    def __del__(self):   # the handle holds host memory only; the buffers are torch's to free
+        try:
+            if getattr(self, "kv", 0):
+                lb.kv_destroy(self.kv)
+        except TypeError:   # the interpreter is taking its modules down
+            pass
+        self.kv = 0
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()

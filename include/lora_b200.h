@@ -406,7 +406,7 @@ lora_status_t lora_apply_host(lora_pool_t *pool, int32_t target, int32_t kind,
  * A_max x S_max region is taken from what the requests' keys and values could use), so a row of
  * head_dim values is kept as head_dim 4-bit codes with one scale and one low value:
  *     value_i = low + scale * code_i ,  code_i in 0 .. 15 ,
- *     low = bf16(min x) , scale = bf16((max x - low) / 15) ,
+ *     low = bf16(min x) , scale = bf16((max x - low) * fl(1/15)) ,
  *     code_i = clamp(rint((x_i - low) * (1 / scale)), 0, 15)      (all in fp32, IEEE rounding;
  *     a scale below the smallest normal number counts as 0, and then every code is 0;
  *     a row with a value that is not finite, or whose scale is not, reads back as NaN throughout)

@@ -1,41 +1,29 @@
 // Attention of a batch over one layer of the 4-bit cache.
-#include "kv_common.cuh"
+#include "kv_decode.cuh"
 
 namespace lora {
-
-struct AttnParams {
-    const __nv_bfloat16 *q;
-    __nv_bfloat16 *out;
-    float *lse;
-    int64_t ldq, ldo;
-    const int32_t *tables, *block_table;
-    int64_t ld_table;
-    KvTables L;
-    KvView kv;
-    int32_t R, T, window;
-    float scale;
-};
 
 // One warp per (token, query head): a lane takes a key for the scores, then head_dim / 32 columns for the
 // products with the values.
 template <int D>
-__global__ void __launch_bounds__(128) attention_plain_kernel(const AttnParams P) {
+__global__ void __launch_bounds__(128) attention_plain_kernel(const AttnParams P, int32_t T) {
     __shared__ float qs[4][D];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t unit = (int64_t)blockIdx.x * 4 + w;
     const int32_t t = (int32_t)(unit / P.kv.hq), h = (int32_t)(unit % P.kv.hq);
-    if (t >= P.T) return;
+    if (t >= T) return;
     constexpr int E = D / 32;
     for (int e = lane; e < D; e += 32) qs[w][e] = __bfloat162float(P.q[t * P.ldq + h * D + e]);
     __syncwarp();
     const int32_t *start = P.tables + P.L.start;
     const int32_t slot = P.tables[P.L.slot + t];
-    int lo = 0, hi = P.R;   // the request: last r with start[r] <= t < start[r + 1]
+    int lo = 0, hi = P.tables[KVH_R];   // the request: last r with start[r] <= t < start[r + 1]
     while (lo < hi) {
         const int m = (lo + hi) >> 1;
         if (start[m + 1] > t) hi = m; else lo = m + 1;
     }
-    const int32_t limit = lo < P.R && slot != -1 ? P.tables[P.L.position + t] + 1 : 0;
+    if (lo >= P.tables[KVH_R] || slot == -1 || (int64_t)(start[lo + 1] - start[lo]) * P.kv.group <= KV_DEC_MAX_ROWS) return;
+    const int32_t limit = P.tables[P.L.position + t] + 1;
     const int32_t from = P.window > 0 ? max(0, limit - P.window) : 0;
     float m = -INFINITY, l = 0.0f, acc[E];
 #pragma unroll
@@ -59,7 +47,7 @@ __global__ void __launch_bounds__(128) attention_plain_kernel(const AttnParams P
                 for (int e = 0; e < 8; ++e)
                     dot = fmaf(qs[w][wd * 8 + e], fmaf((float)((c >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15u), s, low), dot);
             }
-            x = dot * P.scale;
+            x = dot * P.scale2 * 0.69314718f;
         }
         float mx = x;
 #pragma unroll
@@ -96,6 +84,27 @@ __global__ void __launch_bounds__(128) attention_plain_kernel(const AttnParams P
     if (P.lse && lane == 0) P.lse[(int64_t)t * P.kv.hq + h] = m == -INFINITY ? -INFINITY : m + logf(l);
 }
 
+// Space for the pieces of one walk: outputs, then maximum and sum.
+static size_t part_bytes(int32_t walkers, int32_t rows, int32_t d) {
+    return (size_t)2 * walkers * rows * (d * sizeof(float) + sizeof(float2));
+}
+
+template <int D, int NT>
+static lora_status_t launch_decode(lora_kv *kv, AttnParams P, cudaStream_t stream) {
+    using C = DecCfg<D>;
+    bool &done = kv->decode_attr[(D == 128 ? 2 : 0) + NT - 1];
+    if (!done) {
+        LORA_CUDA_TRY(cudaFuncSetAttribute(decode_attention_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           C::SMEM));
+        done = true;
+    }
+    decode_attention_kernel<D, NT><<<P.walkers / DK_WARPS, 32 * DK_WARPS, C::SMEM, stream>>>(P);
+    lora_status_t s = count_launch();
+    if (s != LORA_OK) return s;
+    join_kernel<D, 8 * NT, false><<<P.walkers, 256, 0, stream>>>(P);
+    return count_launch();
+}
+
 }  // namespace lora
 
 using namespace lora;
@@ -104,7 +113,12 @@ extern "C" {
 
 lora_status_t lora_kv_workspace_bytes(const lora_kv_t *kv, size_t *bytes) {
     if (!kv || !bytes) return LORA_ERR_INVALID_ARG;
-    *bytes = 256;
+    size_t most = 0;
+    for (int rows = 8; rows <= 16; rows += 8) {
+        const size_t b = part_bytes(kv->dec_walkers(rows), rows, kv->d);
+        if (b > most) most = b;
+    }
+    *bytes = (most + 255) / 256 * 256;
     return LORA_OK;
 }
 
@@ -137,17 +151,26 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     P.tables = (const int32_t *)tables;
     P.block_table = block_table;
     P.ld_table = ld_table;
-    P.L = kv_tables(R, T, kv->group, kv->dec_walkers(), kv->pr_walkers());
+    const int32_t rows = kv->dec_rows(rec->max_q);
+    P.L = kv_tables(R, T, kv->group, kv->dec_walkers(rows), kv->pr_walkers());
     P.kv = kv->view(layer);
-    P.R = R;
-    P.T = T;
     P.window = rec->window;
-    P.scale = scale;
+    P.scale2 = scale * 1.4426950408889634f;
+    P.walkers = kv->dec_walkers(rows);
+    P.part = (float *)workspace;
+    P.part_ml = (float2 *)(P.part + (size_t)2 * P.walkers * rows * kv->d);
     DeviceGuard g(kv->device);
+    lora_status_t s = kv->d == 64 ? (rows == 8 ? launch_decode<64, 1>(kv, P, (cudaStream_t)stream)
+                                               : launch_decode<64, 2>(kv, P, (cudaStream_t)stream))
+                                  : (rows == 8 ? launch_decode<128, 1>(kv, P, (cudaStream_t)stream)
+                                               : launch_decode<128, 2>(kv, P, (cudaStream_t)stream));
+    if (s != LORA_OK) return s;
+    // a batch whose requests all have few rows needs no more
+    if ((int64_t)rec->max_q * kv->group <= KV_DEC_MAX_ROWS) return LORA_OK;
     const int64_t blocks = ((int64_t)T * kv->hq + 3) / 4;
     if (blocks > 0x7fffffff) return LORA_ERR_SHAPE;
-    if (kv->d == 64) attention_plain_kernel<64><<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(P);
-    else attention_plain_kernel<128><<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(P);
+    if (kv->d == 64) attention_plain_kernel<64><<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(P, T);
+    else attention_plain_kernel<128><<<(unsigned)blocks, 128, 0, (cudaStream_t)stream>>>(P, T);
     return count_launch();
 }
 

@@ -81,7 +81,8 @@ __host__ __device__ inline KvTables kv_tables(int32_t R, int32_t T, int32_t grou
     o = (o + 3) & ~(int64_t)3;
     // a request of q tokens has ceil(q * group / rows) items: at most one more than q * group / rows
     const int64_t rows = (int64_t)T * group;
-    int64_t cd = R + rows / 8, cp = R + rows / KV_PROMPT_ROWS;
+    // (the tokens of no request count as one more)
+    int64_t cd = R + 1 + rows / 8, cp = R + rows / KV_PROMPT_ROWS;
     L.cap_dec = (int32_t)(cd < 0x7fffffff ? cd : 0x7fffffff);
     L.cap_pr = (int32_t)(cp < 0x7fffffff ? cp : 0x7fffffff);
     L.walk = o;      o += 2 * (int64_t)(sizeof(KvWalk) / 4);
@@ -107,6 +108,7 @@ struct lora_kv {
     int32_t *status_dev = nullptr;
     int64_t page_bytes = 0, layer_bytes = 0;
     int32_t sm_count = 148;
+    bool decode_attr[4] = {false, false, false, false};   // attributes set: head_dim 64 / 128, 8 / 16 rows
     size_t tables_attr_smem = 0;      // dynamic shared memory the table builder has been allowed
     std::vector<lora::KvTableRecord> tables;
 
@@ -125,6 +127,8 @@ struct lora_kv {
     // Rows of one item of the single-token walk: 8, or 16 where a token alone has more than 8 or a
     // request may bring several tokens.
     int32_t dec_rows(int32_t max_q) const { return (int64_t)max_q * group <= 8 ? 8 : 16; }
-    int32_t dec_walkers() const { return sm_count * 16; }
+    // Warps of the single-token kernel that are resident at once (its registers: 128 a thread at 8 rows,
+    // 168 at 16).
+    int32_t dec_walkers(int32_t rows) const { return sm_count * (rows == 8 ? 16 : 12); }
     int32_t pr_walkers() const { return sm_count; }
 };

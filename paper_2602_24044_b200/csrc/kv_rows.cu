@@ -179,7 +179,7 @@ __device__ __forceinline__ void quantise_row(const Row &x, uint32_t &wa, uint32_
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
     const float low = __bfloat162float(__float2bfloat16_rn(lo));
-    float scale = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, low), 15.0f)));
+    float scale = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(hi, low), 1.0f / 15.0f)));
     if (scale < 1.17549435e-38f) scale = 0.0f;
     const bool bad = !(fabsf(scale) < INFINITY) || !(fabsf(low) < INFINITY);
     const float inv = scale == 0.0f ? 0.0f : __fdiv_rn(1.0f, scale);

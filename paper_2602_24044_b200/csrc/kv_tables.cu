@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         kv[r] = max(k, 0);
         chunks_d[r] = min(max(q, 0), T + 1);
     }
-    const int32_t count = min(max(*P.free_count, 0), P.num_pages);
+    const int32_t count = P.free_count ? min(max(*P.free_count, 0), P.num_pages) : 0;
     __syncthreads();
     block_scan(chunks_d, R, warp64);
     for (int r = tid; r < R; r += TB_THREADS) {
@@ -131,11 +131,13 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         else atomicMax(&taken, need > 0 ? pages[r] : 0);
     }
     __syncthreads();
-    if (tid == 0) sum_q = (int32_t)min(chunks_d[R - 1], (int64_t)0x7fffffff);
+    if (tid == 0) sum_q = R ? (int32_t)min(chunks_d[R - 1], (int64_t)0x7fffffff) : 0;
     __syncthreads();
+    const int32_t tokens = R ? end[R - 1] : 0;
 
     // items and chunks of every request: few for a request of single tokens, one warp each for prompts.
-    // A failed request's rows, however many, are items of one empty chunk in the single-token list.
+    // A failed request's rows, however many, are items of one empty chunk in the single-token list;
+    // behind all requests' items come those of the tokens that belong to none.
     for (int r = tid; r < R; r += TB_THREADS) {
         const int32_t q = end[r] - (r ? end[r - 1] : 0);
         const int64_t rows = (int64_t)q * P.group;
@@ -181,8 +183,10 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     block_scan(chunks_p, R, warp64);
     block_scan(items_d, R, warp32);
     block_scan(items_p, R, warp32);
+    const int64_t spare_rows = (int64_t)(T - tokens) * P.group;
+    const int32_t spare = (int32_t)((spare_rows + P.dec_rows - 1) / P.dec_rows);
     if (tid < 2) {
-        const int64_t total = P.hkv * (tid ? chunks_p : chunks_d)[R - 1];
+        const int64_t total = P.hkv * ((R ? (tid ? chunks_p : chunks_d)[R - 1] : 0) + (tid ? 0 : spare));
         const int32_t walkers = tid ? P.pr_walkers : P.dec_walkers;
         int64_t span = (total + walkers - 1) / walkers;
         // single tokens: no fewer than four chunks per warp, or joining the pieces costs more than
@@ -209,7 +213,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         KvWalk w;
         w.total = walk_total[gt];
         w.span = walk_span[gt];
-        w.n_items = (gt ? items_p : items_d)[R - 1];
+        w.n_items = (R ? (gt ? items_p : items_d)[R - 1] : 0) + (gt ? 0 : spare);
         w.reserved[0] = w.reserved[1] = w.reserved[2] = 0;
         reinterpret_cast<KvWalk *>(P.out + P.L.walk)[gt] = w;
     }
@@ -223,7 +227,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     // tokens.  A page of the batch is taken from the stack directly; an old one from the block table
     for (int t = gt; t < T; t += all_threads) {
         int32_t pos = 0, slot = -1;
-        if (t < end[R - 1]) {
+        if (t < tokens) {
             const int r = upper_bound(end, R, t);
             const int64_t p64 = (int64_t)kv[r] + (t - (r ? end[r - 1] : 0));
             pos = (int32_t)min(p64, (int64_t)0x7fffffff);
@@ -279,6 +283,19 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
     }
+    for (int i = gt; i < spare; i += all_threads) {
+        KvItem it;
+        it.start = (R ? chunks_d[R - 1] : 0) + i;
+        it.req = 0;
+        it.row0 = i * P.dec_rows;
+        it.nrows = (int32_t)min((int64_t)P.dec_rows, spare_rows - it.row0);
+        it.k_lo = 0;
+        it.n = 1;
+        it.tok0 = tokens;
+        it.lim0 = -0x40000000;
+        it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
+        dec[(R ? items_d[R - 1] : 0) + i] = it;
+    }
     cluster_arrive();   // the lists are complete
     cluster_wait();
     for (int w = gt; w < P.dec_walkers + P.pr_walkers; w += all_threads) {
@@ -290,13 +307,17 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
             const int64_t at = pos / P.hkv;   // hkv * start <= pos  <=>  start <= at
             const int r = upper_bound(single ? chunks_d : chunks_p, R, at);
             const int32_t *items = single ? items_d : items_p;
-            int32_t lo = r ? items[r - 1] : 0, hi = items[r];
+            int32_t lo = r ? items[r - 1] : 0, hi = r < R ? items[r] : 0;
             const KvItem *list = single ? dec : pr;
-            while (hi - lo > 1) {   // last item that starts at or before `at`
-                const int32_t m = (lo + hi) >> 1;
-                if (list[m].start <= at) lo = m; else hi = m;
+            if (r == R) {
+                found = (int32_t)(lo + at - (R ? chunks_d[R - 1] : 0));   // a spare item
+            } else {
+                while (hi - lo > 1) {   // last item that starts at or before `at`
+                    const int32_t m = (lo + hi) >> 1;
+                    if (list[m].start <= at) lo = m; else hi = m;
+                }
+                found = lo;
             }
-            found = lo;
         }
         P.out[(single ? P.L.dec_first : P.L.pr_first) + i] = found;
     }
@@ -365,34 +386,29 @@ __global__ void __launch_bounds__(TB_THREADS) release_kernel(const int32_t *requ
     if (tid == 0) *free_count = (int32_t)min((int64_t)have + (n ? count[n - 1] : 0), (int64_t)num_pages);
 }
 
-// A batch without requests: every position 0, every slot -1, both lists empty.
-__global__ void empty_tables_kernel(int32_t *out, const KvTables L, int32_t T, const int32_t *free_count,
-                                    int32_t *free_count_out) {
-    for (int64_t i = threadIdx.x; i < L.words; i += blockDim.x)
-        out[i] = i == KVH_T ? T : i >= L.slot && i < L.slot + T ? -1 : 0;
-    if (threadIdx.x == 0 && free_count && free_count_out) *free_count_out = *free_count;
-}
-
 }  // namespace lora
 
 using namespace lora;
 
 extern "C" {
 
-static lora_status_t tables_shape(const lora_kv_t *kv, int32_t R, int32_t T, KvTables *L) {
+static lora_status_t tables_shape(const lora_kv_t *kv, int32_t R, int32_t T, int32_t max_q, KvTables *L) {
     if (!kv) return LORA_ERR_INVALID_ARG;
     if (R < 0 || T < 0 || R > KV_MAX_REQUESTS) return LORA_ERR_SHAPE;
     if ((int64_t)T * kv->group > 0x7ffffff0) return LORA_ERR_SHAPE;
-    *L = kv_tables(R, T, kv->group, kv->dec_walkers(), kv->pr_walkers());
+    *L = kv_tables(R, T, kv->group, kv->dec_walkers(kv->dec_rows(max_q)), kv->pr_walkers());
     return LORA_OK;
 }
 
 lora_status_t lora_kv_tables_bytes(const lora_kv_t *kv, int32_t R, int32_t T, size_t *bytes) {
     if (!bytes) return LORA_ERR_INVALID_ARG;
     KvTables L;
-    lora_status_t s = tables_shape(kv, R, T, &L);
+    lora_status_t s = tables_shape(kv, R, T, 1, &L);
     if (s != LORA_OK) return s;
-    *bytes = (size_t)L.words * 4;
+    const int64_t words = L.words;
+    s = tables_shape(kv, R, T, T, &L);
+    if (s != LORA_OK) return s;
+    *bytes = (size_t)(words > L.words ? words : L.words) * 4;
     return LORA_OK;
 }
 
@@ -402,19 +418,14 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
                                    int32_t *kv_len_out, int32_t *free_count_out, void *tables, size_t tables_bytes,
                                    void *stream) {
     TableParams P;
-    lora_status_t s = tables_shape(kv, R, T, &P.L);
+    if (max_q == 0 || max_q > T) max_q = T;
+    lora_status_t s = tables_shape(kv, R, T, max_q, &P.L);
     if (s != LORA_OK) return s;
     if (max_q < 0 || window < 0 || ld_table < 0) return LORA_ERR_SHAPE;
     if (!tables || ((uintptr_t)tables & 15)) return LORA_ERR_INVALID_ARG;
     if (tables_bytes < (size_t)P.L.words * 4) return LORA_ERR_BUFFER_TOO_SMALL;
     if (R > 0 && (!kv_len || !q_len || !free_pages || !free_count || !block_table)) return LORA_ERR_INVALID_ARG;
-    if (max_q == 0 || max_q > T) max_q = T;
     DeviceGuard g(kv->device);
-    if (R == 0) {
-        empty_tables_kernel<<<1, 256, 0, (cudaStream_t)stream>>>((int32_t *)tables, P.L, T, free_count, free_count_out);
-        kv->remember(tables, R, T, max_q, window);
-        return count_launch();
-    }
     P.kv_len = kv_len;
     P.q_len = q_len;
     P.free_pages = free_pages;
@@ -433,7 +444,7 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
     P.hkv = kv->hkv;
     P.group = kv->group;
     P.dec_rows = kv->dec_rows(max_q);
-    P.dec_walkers = kv->dec_walkers();
+    P.dec_walkers = kv->dec_walkers(P.dec_rows);
     P.pr_walkers = kv->pr_walkers();
     const size_t smem = (size_t)R * (2 * 8 + 6 * 4) + 32 * 8 + 32 * 4;
     if (smem > kv->tables_attr_smem) {

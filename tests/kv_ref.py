@@ -78,7 +78,7 @@ def quantise(x):
     """float32 [n, D] -> codes uint8 [n, D], scale and low float32 (bf16 values) [n]."""
     with np.errstate(all="ignore"):
         low = bf16(x.min(-1))
-        scale = bf16((x.max(-1) - low) / np.float32(15))
+        scale = bf16((x.max(-1) - low) * np.float32(1.0 / 15.0))
         scale = np.where(scale < np.float32(1.17549435e-38), np.float32(0), scale)
         bad = ~(np.isfinite(scale) & np.isfinite(low) & np.isfinite(x).all(-1))
         inv = np.where(scale == 0, np.float32(0), np.float32(1) / np.where(scale == 0, np.float32(1), scale))

@@ -109,6 +109,7 @@ struct lora_kv {
     int64_t page_bytes = 0, layer_bytes = 0;
     int32_t sm_count = 148;
     bool decode_attr[4] = {false, false, false, false};   // attributes set: head_dim 64 / 128, 8 / 16 rows
+    bool prompt_attr[2] = {false, false};
     size_t tables_attr_smem = 0;      // dynamic shared memory the table builder has been allowed
     std::vector<lora::KvTableRecord> tables;
 

@@ -1,0 +1,666 @@
+// Attention of prompts (many query rows a request) over the 4-bit cache on the 5th-generation tensor cores.
+//
+// The mathematics is that of the single-token kernel: scores are s_t (q . (c_t - 8)) + (low_t + 8 s_t) sum(q),
+// probabilities enter the second product as p_t s_t in fp16, the low values of the values as one number a row.
+//
+// What bounds it: a block of 128 keys against 256 rows is 2 x 1024 cycles of tensor pipe, 2048 of the
+// exponential unit and about 1800 issue slots a scheduler (scores to probabilities about 5 a score, widening
+// about 1.3 a code, shared by all 256 rows): all three near each other.  Hence 256 rows a block of threads,
+// as two tiles of 128 whose softmax and matrix products alternate, and everything else on warps of its own:
+//   warps 0-3, 4-7   softmax of tile 0, tile 1: a thread is a row; scores from tensor memory to registers,
+//                    probabilities back to the same tensor-memory columns, which the second product reads
+//                    as its A operand; rescales the accumulator itself when its maximum was raised
+//   warps 8-11       widen the codes of a block of keys: K as bf16, V as fp16, into three swizzled tiles
+//                    (order K0 V0 K1 V1 ..), and lay out the keys' scales and lows
+//   warp 12          issues the matrix products
+//   warp 13          requests the cells (bulk copies), two blocks ahead
+//   warps 14, 15     bring the queries of the next (item, head), tile 0, tile 1
+// The (item, head, block) triples form one walk cut into equal spans, one per SM; what a span's ends cut is
+// joined afterwards.  Tensor memory: scores of both tiles (2 x 128 columns), accumulators (2 x head_dim).
+#pragma once
+
+#include "kv_decode.cuh"
+
+namespace lora {
+
+namespace tcp {
+__device__ __forceinline__ void tmem_alloc(uint32_t *dst_smem, uint32_t ncols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)),
+                 "r"(ncols)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish() {
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[smem] . B[smem]; A[tmem] . B[smem]
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// one arrival on the mbarrier when every product issued so far by this thread has completed
+__device__ __forceinline__ void commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
+                 : "memory");
+}
+#define LORA_R32(r, o)                                                                                             \
+    "=r"(r[o + 0]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), \
+        "=r"(r[o + 7]), "=r"(r[o + 8]), "=r"(r[o + 9]), "=r"(r[o + 10]), "=r"(r[o + 11]), "=r"(r[o + 12]),           \
+        "=r"(r[o + 13]), "=r"(r[o + 14]), "=r"(r[o + 15]), "=r"(r[o + 16]), "=r"(r[o + 17]), "=r"(r[o + 18]),        \
+        "=r"(r[o + 19]), "=r"(r[o + 20]), "=r"(r[o + 21]), "=r"(r[o + 22]), "=r"(r[o + 23]), "=r"(r[o + 24]),        \
+        "=r"(r[o + 25]), "=r"(r[o + 26]), "=r"(r[o + 27]), "=r"(r[o + 28]), "=r"(r[o + 29]), "=r"(r[o + 30]),        \
+        "=r"(r[o + 31])
+// 32 lanes x 32 columns -> registers o .. o + 31 of every thread (lane = thread)
+#define LORA_TMEM_LD32(addr, r, o)                                                                                \
+    asm volatile(                                                                                                 \
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, " \
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"              \
+        : LORA_R32(r, o)                                                                                          \
+        : "r"(addr)                                                                                               \
+        : "memory")
+template <int N>
+__device__ __forceinline__ void st32(uint32_t addr, const uint32_t (&r)[N], int o) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[o + 0]),
+        "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7]),
+        "r"(r[o + 8]), "r"(r[o + 9]), "r"(r[o + 10]), "r"(r[o + 11]), "r"(r[o + 12]), "r"(r[o + 13]), "r"(r[o + 14]),
+        "r"(r[o + 15]), "r"(r[o + 16]), "r"(r[o + 17]), "r"(r[o + 18]), "r"(r[o + 19]), "r"(r[o + 20]), "r"(r[o + 21]),
+        "r"(r[o + 22]), "r"(r[o + 23]), "r"(r[o + 24]), "r"(r[o + 25]), "r"(r[o + 26]), "r"(r[o + 27]), "r"(r[o + 28]),
+        "r"(r[o + 29]), "r"(r[o + 30]), "r"(r[o + 31]), "r"(addr)
+        : "memory");
+}
+// shared-memory matrix descriptor, 128-byte swizzle (start, leading and stride offsets in 16-byte units)
+__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)((lead >> 4) & 0x3FFFu) << 16 |
+           (uint64_t)((stride >> 4) & 0x3FFFu) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// fp32 accumulator; a, b: 0 = fp16, 1 = bf16; b_n: B's rows run along N
+__host__ __device__ constexpr uint32_t instr(uint32_t type, uint32_t N, uint32_t b_n) {
+    return (1u << 4) | (type << 7) | (type << 10) | (b_n << 16) | ((N >> 3) << 17) | ((128u >> 4) << 24);
+}
+template <int R> __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R> __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+
+// two floats at once
+__device__ __forceinline__ uint64_t pack2f(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2f(uint64_t v, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ void lds_2x64(uint32_t addr, uint64_t &a, uint64_t &b) {
+    asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
+}
+__device__ __forceinline__ void sts_v4(uint32_t addr, const uint32_t (&v)[4]) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+                 : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {   // the rest becomes zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+}  // namespace tcp
+
+constexpr int PK_THREADS = 512, PK_TILES = 3, PK_RAW = 2, PK_PARAMS = 3;
+
+template <int D>
+struct PromptCfg {
+    static constexpr int CELL = kv_cell_bytes(D);
+    static constexpr int RAW = 8 * CELL;                    // a block of 128 keys as it lies in the cache
+    static constexpr int TILE = 128 * D * 2;                // 128 rows of 16-bit values
+    static constexpr int PARAM = 128 * 16 + 16;             // (scale, z) of keys, of values; exponent, valid cells
+    static constexpr int OFF_KV = 2 * TILE;                 // behind the queries of both tiles
+    static constexpr int OFF_RAW = OFF_KV + PK_TILES * TILE;
+    static constexpr int OFF_PARAM = OFF_RAW + PK_RAW * RAW;
+    static constexpr int OFF_BAR = OFF_PARAM + PK_PARAMS * PARAM;
+    static constexpr int SMEM = OFF_BAR + 512 + 1024;       // 1024: the swizzled tiles' alignment
+};
+
+// A walker's cursor over its span: (item, head, block) in order.
+struct PromptCursor {
+    const KvItem *items;
+    KvItem it;
+    int64_t pos, end;
+    int32_t index, head, chunk, hkv;
+    __device__ __forceinline__ PromptCursor(const KvItem *list, int32_t first, int64_t s0, int64_t s1, int32_t heads)
+        : items(list), pos(s0), end(s1), index(first), hkv(heads) {
+        it = load_item(items + index);
+        const int64_t off = s0 - hkv * it.start;
+        head = (int32_t)(off / it.n);
+        chunk = (int32_t)(off - (int64_t)head * it.n);
+    }
+    __device__ __forceinline__ bool more() const { return pos < end; }
+    // blocks of the current (item, head) that belong to the span
+    __device__ __forceinline__ int32_t last_chunk() const { return (int32_t)min((int64_t)it.n, chunk + (end - pos)); }
+    __device__ __forceinline__ void next_pair(int32_t blocks) {
+        pos += blocks;
+        chunk = 0;
+        if (++head == hkv) {
+            head = 0;
+            if (pos < end) it = load_item(items + ++index);
+        }
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const AttnParams P) {
+    using C = PromptCfg<D>;
+    extern __shared__ __align__(1024) unsigned char pk_raw[];
+    unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)pk_raw + 1023) & ~(uintptr_t)1023);
+    uint64_t *raw_full = reinterpret_cast<uint64_t *>(smem + C::OFF_BAR);
+    uint64_t *raw_empty = raw_full + PK_RAW;
+    uint64_t *kv_full = raw_empty + PK_RAW;
+    uint64_t *kv_empty = kv_full + PK_TILES;
+    uint64_t *s_full = kv_empty + PK_TILES;       // [2] scores of a tile are in tensor memory
+    uint64_t *p_ready = s_full + 2;               // [2] probabilities are
+    uint64_t *o_full = p_ready + 2;               // [2] the accumulator of an (item, head) is complete
+    uint64_t *q_ready = o_full + 2;               // [2] queries are in shared memory
+    uint64_t *q_free = q_ready + 2;               // [2] the last score product of an (item, head) is done, the sums are taken
+    uint64_t *param_full = q_free + 2;
+    uint64_t *param_empty = param_full + PK_PARAMS;
+    uint64_t *drained = param_empty + PK_PARAMS;  // every product has completed
+    uint32_t *valid_s = reinterpret_cast<uint32_t *>(drained + 1);      // [PK_RAW] cells that are there
+    uint32_t *most_s = valid_s + PK_RAW;          // [2][4] largest value row of a block, per warp
+    uint32_t *tmem_slot = most_s + 8;
+    volatile uint32_t *failed = tmem_slot + 1;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const KvWalk *walk = reinterpret_cast<const KvWalk *>(P.tables + P.L.walk) + 1;
+    const int64_t s0 = blockIdx.x * walk->span, s1 = min(s0 + walk->span, walk->total);
+    if (s0 >= s1) return;
+    const KvItem *items = reinterpret_cast<const KvItem *>(P.tables + P.L.pr_items);
+    const int32_t first = __ldg(P.tables + P.L.pr_first + blockIdx.x);
+    const int32_t group = P.kv.group;
+
+    if (tid == 0) {
+        for (int i = 0; i < PK_RAW; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 4); }
+        for (int i = 0; i < PK_TILES; ++i) { mbar_init(&kv_full[i], 4); mbar_init(&kv_empty[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_ready[i], 128);
+            mbar_init(&o_full[i], 1);
+            mbar_init(&q_ready[i], 1);
+            mbar_init(&q_free[i], 5);
+        }
+        for (int i = 0; i < PK_PARAMS; ++i) { mbar_init(&param_full[i], 4); mbar_init(&param_empty[i], 8); }
+        mbar_init(drained, 1);
+        *failed = 0;
+        fence_mbar_init();
+    }
+    if (warp == 12) {
+        tcp::tmem_alloc(tmem_slot, 512);
+        tcp::tmem_relinquish();
+    }
+    tcp::fence_before();
+    __syncthreads();
+    tcp::fence_after();
+    const uint32_t tmem = *tmem_slot;
+    // a wait gives up after a limit, or when another warp has
+    auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
+        for (uint32_t i = 0; i < WAIT_POLLS; ++i) {
+            if (mbar_try_wait(bar, parity)) return true;
+            if (*failed) return false;
+        }
+        *failed = 1;
+        return false;
+    };
+    PromptCursor cur(items, first, s0, s1, P.kv.hkv);
+
+    if (warp < 8) {
+        // =========================== softmax: a thread is a row ====================================
+        tcp::reg_inc<184>();
+        const int t = warp >> 2, row = tid & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
+        uint32_t j = 0, pair = 0;
+        bool ok = true;
+        for (; ok && cur.more(); ++pair) {
+            const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
+            const int32_t r = cur.it.row0 + t * 128 + row;
+            const int32_t my = t * 128 + row;
+            // rows past the item's end (their queries are zero) follow the last one's limit
+            const int32_t lim = cur.it.lim0 + min(r, cur.it.row0 + cur.it.nrows - 1) / group;
+            const int32_t lo = P.window > 0 ? lim - P.window : 0;
+            const int32_t lim_min = cur.it.lim0 + min(cur.it.row0 + t * 128, cur.it.row0 + cur.it.nrows - 1) / group;
+            const int32_t lo_max = P.window > 0 ? cur.it.lim0 + min(cur.it.row0 + t * 128 + 127, cur.it.row0 + cur.it.nrows - 1) / group - P.window : 0;
+            ok = wait(&q_ready[t], pair & 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            float qs = 0.0f;
+            {
+                const uint32_t q_at = smem_u32(smem) + t * C::TILE + row * 128;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    uint32_t v[4];
+                    lds_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) qs += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_free[t]);
+            float m = -INFINITY, l = 0.0f, z = 0.0f;
+            int ve = KV_NO_EXPONENT;
+            for (int32_t ch = c0; ch < c1; ++ch, ++j) {
+                const uint32_t ps = j % PK_PARAMS;
+                ok = wait(&param_full[ps], (j / PK_PARAMS) & 1u) && wait(&s_full[t], j & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tcp::fence_after();
+                uint32_t x[128];
+                LORA_TMEM_LD32(s_at, x, 0);
+                LORA_TMEM_LD32(s_at + 32, x, 32);
+                LORA_TMEM_LD32(s_at + 64, x, 64);
+                LORA_TMEM_LD32(s_at + 96, x, 96);
+                const uint32_t par = smem_u32(smem) + C::OFF_PARAM + ps * C::PARAM;
+                const int ve_new = (int)lds_u32(par + 2048);
+                const uint32_t valid = lds_u32(par + 2052);
+                const int32_t key0 = cur.it.k_lo + ch * KV_PROMPT_CHUNK;
+                const bool whole = valid == 0xffu && key0 + 128 <= lim_min && key0 >= lo_max;
+                tcp::wait_ld();
+                const uint64_t qs2 = tcp::pack2f(qs, qs);
+                float mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    uint64_t ks, kz;
+                    tcp::lds_2x64(par + i * 16, ks, kz);
+                    const uint64_t v = tcp::fma2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), ks,
+                                                 tcp::mul2(qs2, kz));
+                    float a, b;
+                    tcp::unpack2f(v, a, b);
+                    if (!whole) {
+                        const int32_t k = key0 + 2 * i;
+                        const bool there = (valid >> (i / 8)) & 1u;
+                        a = there && k < lim && k >= lo ? a : -INFINITY;
+                        b = there && k + 1 < lim && k + 1 >= lo ? b : -INFINITY;
+                    }
+                    mx = fmaxf(mx, fmaxf(a, b));
+                    x[2 * i] = __float_as_uint(a);
+                    x[2 * i + 1] = __float_as_uint(b);
+                }
+                const bool up = mx > m + KV_RAISE || ve_new != ve;
+                if (__any_sync(0xffffffffu, up)) {
+                    const float mn = mx > m + KV_RAISE ? mx : m;
+                    const float f = mn == m ? 1.0f : exp2_approx(m - mn), fe = f * pow2(max(ve - ve_new, -126));
+                    m = mn;
+                    ve = ve_new;
+                    l *= f;
+                    z *= fe;
+                    if (ch > c0) {     // the products of the blocks before have completed: their scores' successor is here
+#pragma unroll
+                        for (int cc = 0; cc < D; cc += 32) {
+                            uint32_t o[32];
+                            LORA_TMEM_LD32(o_at + cc, o, 0);
+                            tcp::wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fe);
+                            tcp::st32(o_at + cc, o, 0);
+                        }
+                        tcp::wait_st();
+                    }
+                }
+                uint64_t l2 = 0, z2 = 0;
+                const uint64_t nm = tcp::pack2f(-m, -m);
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    uint64_t vs, vz;
+                    tcp::lds_2x64(par + 1024 + i * 16, vs, vz);
+                    float a, b;
+                    tcp::unpack2f(tcp::add2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), nm), a, b);
+                    a = exp2_approx(a);
+                    b = exp2_approx(b);
+                    uint64_t p = tcp::pack2f(a, b);
+                    if (!whole) {      // what is not seen counts nothing, whatever its scale and low are
+                        const bool na = __uint_as_float(x[2 * i]) == -INFINITY, nb = __uint_as_float(x[2 * i + 1]) == -INFINITY;
+                        p = tcp::pack2f(na ? 0.0f : a, nb ? 0.0f : b);
+                        float s0f, s1f, z0f, z1f;
+                        tcp::unpack2f(vs, s0f, s1f);
+                        tcp::unpack2f(vz, z0f, z1f);
+                        vs = tcp::pack2f(na ? 0.0f : s0f, nb ? 0.0f : s1f);
+                        vz = tcp::pack2f(na ? 0.0f : z0f, nb ? 0.0f : z1f);
+                    }
+                    l2 = tcp::add2(l2, p);
+                    z2 = tcp::fma2(p, vz, z2);
+                    float c, d;
+                    tcp::unpack2f(tcp::mul2(p, vs), c, d);
+                    x[i] = pack_f16(c, d);
+                }
+                float a, b;
+                tcp::unpack2f(l2, a, b);
+                l += a + b;
+                tcp::unpack2f(z2, a, b);
+                z += a + b;
+                tcp::st32(s_at, x, 0);
+                tcp::st32(s_at + 32, x, 32);
+                tcp::wait_st();
+                tcp::fence_before();
+                mbar_arrive(&p_ready[t]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&param_empty[ps]);
+            }
+            if (!ok) break;
+            // ---- the (item, head) is over, or the span is ------------------------------------------
+            ok = wait(&o_full[t], pair & 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tcp::fence_after();
+            const bool live = my < cur.it.nrows, complete = c0 == 0 && c1 == cur.it.n;
+            const float inv = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l, back = pow2(ve);
+            const int32_t tok = cur.it.tok0 + r / group, hq = cur.head * group + r % group;
+            const int64_t slot = (2 * (int64_t)blockIdx.x + (c0 == 0 ? 1 : 0)) * KV_PROMPT_ROWS + my;
+#pragma unroll
+            for (int cc = 0; cc < D; cc += 32) {
+                uint32_t o[32];
+                LORA_TMEM_LD32(o_at + cc, o, 0);
+                tcp::wait_ld();
+                if (live) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint((__uint_as_float(o[e]) + z) * inv * back);
+                    if (complete) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(P.out + tok * P.ldo + (int64_t)hq * D + cc);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t h[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(o[8 * e + 2 * k]),
+                                                                                __uint_as_float(o[8 * e + 2 * k + 1]));
+                                h[k] = *reinterpret_cast<const uint32_t *>(&b2);
+                            }
+                            dst[e] = make_uint4(h[0], h[1], h[2], h[3]);
+                        }
+                    } else {
+                        uint4 *dst = reinterpret_cast<uint4 *>(P.part + slot * D + cc);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                }
+            }
+            if (live) {
+                if (!complete) P.part_ml[slot] = make_float2(m, l);
+                else if (P.lse) P.lse[(int64_t)tok * P.kv.hq + hq] = inv == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
+            }
+            tcp::fence_before();
+            cur.next_pair(c1 - c0);
+        }
+    } else if (warp < 12) {
+        // =========================== widening ======================================================
+        tcp::reg_dec<96>();
+        const int id = tid - 256, wq = warp - 8, kr = id >> 2, c = id & 3;
+        uint32_t j = 0, u = 0;        // blocks, tiles
+        // a warp whose wait failed still takes part in the named barrier of the next block, where all four
+        // learn of it and leave together
+        bool ok = true, dead = false;
+        while (!dead && cur.more()) {
+            const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
+            const int32_t end = cur.it.lim0 + (cur.it.row0 + cur.it.nrows - 1) / group;
+            int ve = KV_NO_EXPONENT;
+            for (int32_t ch = c0; ch < c1; ++ch, ++j) {
+                const uint32_t rs = j % PK_RAW, ps = j % PK_PARAMS;
+                const uint32_t raw = smem_u32(smem) + C::OFF_RAW + rs * C::RAW;
+                const uint32_t par = smem_u32(smem) + C::OFF_PARAM + ps * C::PARAM;
+                ok = ok && wait(&raw_full[rs], (j / PK_RAW) & 1u);
+                if (ok && j >= PK_PARAMS) ok = wait(&param_empty[ps], (j / PK_PARAMS - 1) & 1u);
+                // scales and lows: a thread is a key
+                const uint32_t valid = valid_s[rs];
+                float ks = 0.0f, kz = 0.0f, vs = 0.0f, vz = 0.0f;
+                uint32_t mag = 0;
+                if (((valid >> (id >> 4)) & 1u) && cur.it.k_lo + ch * KV_PROMPT_CHUNK + id < end) {
+                    const uint32_t at = raw + (id >> 4) * C::CELL + kv_cell_params(D) + (id & 15) * 4;
+                    const uint32_t kp = lds_u32(at), vp = lds_u32(at + KV_CELL * 4);
+                    ks = __uint_as_float(kp << 16);
+                    kz = fmaf(8.0f, ks, __uint_as_float(kp & 0xffff0000u)) * P.scale2;
+                    ks *= P.scale2;
+                    vs = __uint_as_float(vp << 16);
+                    vz = fmaf(8.0f, vs, __uint_as_float(vp & 0xffff0000u));
+                    mag = max(vp << 16, vp & 0x7fff0000u);
+                    if (mag >= 0x7f800000u) mag = 0;
+                }
+                mag = __reduce_max_sync(0xffffffffu, mag);
+                if (lane == 0) most_s[(j & 1u) * 4 + wq] = mag;
+                uint32_t any_bad;      // all four warps take the same decision
+                asm volatile(
+                    "{\n\t.reg .pred p, q;\n\t"
+                    "setp.ne.u32 p, %1, 0;\n\t"
+                    "bar.red.or.pred q, 1, 128, p;\n\t"
+                    "selp.u32 %0, 1, 0, q;\n\t}"
+                    : "=r"(any_bad)
+                    : "r"(ok ? 0u : 1u)
+                    : "memory");
+                if (any_bad) { dead = true; break; }
+                const uint32_t *mo = most_s + (j & 1u) * 4;
+                ve = raise_exponent(ve, max(max(mo[0], mo[1]), max(mo[2], mo[3])));
+                const float unit = pow2(-ve);
+                {
+                    float *pf = reinterpret_cast<float *>(smem + C::OFF_PARAM + ps * C::PARAM);
+                    pf[(id >> 1) * 4 + (id & 1)] = ks;
+                    pf[(id >> 1) * 4 + 2 + (id & 1)] = kz;
+                    pf[256 + (id >> 1) * 4 + (id & 1)] = vs * unit;
+                    pf[256 + (id >> 1) * 4 + 2 + (id & 1)] = vz * unit;
+                    if (id == 0) {
+                        reinterpret_cast<int *>(pf)[512] = ve;
+                        reinterpret_cast<uint32_t *>(pf)[513] = valid;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&param_full[ps]);
+                // codes: K, then V.  Four lanes share a row; those of the second pair take their two halves
+                // in the other order, so that the eight lanes of a store phase hit eight different banks
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++u) {
+                    const uint32_t b = u % PK_TILES, tile = smem_u32(smem) + C::OFF_KV + b * C::TILE;
+                    if (u >= PK_TILES) ok = ok && wait(&kv_empty[b], (u / PK_TILES - 1) & 1u);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = i * 32 + kr;
+                        const uint32_t src = raw + (key >> 4) * C::CELL + (kv * KV_CELL + (key & 15)) * (D / 2) + c * (D / 8);
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h) {
+                            const int hh = D == 128 ? h ^ (c >> 1) : 0;      // which 8 bytes of the lane's run
+                            uint32_t w[2];
+                            lds_v2(src + hh * 8, w);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int word = c * (D / 32) + hh * 2 + e;      // 8 elements: a 16-byte run of the tile's row
+                                uint32_t v[4];
+                                if (kv == 0) {
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) v[q] = widen_bf16(w[e] >> (4 * q));
+                                } else {
+                                    v[0] = widen_f16_lo(w[e]);
+                                    v[1] = widen_f16_hi(w[e]);
+                                    v[2] = widen_f16_lo(w[e] >> 8);
+                                    v[3] = widen_f16_hi(w[e] >> 8);
+                                }
+                                tcp::sts_v4(tile + (word >> 3) * 16384 + key * 128 + (((word & 7) ^ (key & 7)) << 4), v);
+                            }
+                        }
+                    }
+                    fence_proxy_async();     // ordinary stores, read by the matrix unit
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&kv_full[b]);
+                        if (kv == 1) mbar_arrive(&raw_empty[rs]);
+                    }
+                }
+            }
+            cur.next_pair(c1 - c0);
+        }
+        if (dead || !ok) *failed = 1;
+    } else {
+        tcp::reg_dec<48>();
+        if (warp == 12) {
+            // ======================= matrix products ===============================================
+            if (lane == 0) {
+                constexpr uint32_t QK = tcp::instr(1, 128, 0), PV = tcp::instr(0, D, 1);
+                const uint32_t q_at = smem_u32(smem), kv_at = q_at + C::OFF_KV;
+                bool ok = true;
+                auto scores = [&](int t, uint32_t u) {
+                    const uint32_t qa = q_at + t * C::TILE, ka = kv_at + (u % PK_TILES) * C::TILE;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        tcp::mma_ss(tmem + t * 128, tcp::desc(qa + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024),
+                                    tcp::desc(ka + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024), QK, k > 0);
+                };
+                uint32_t j = 0, pair = 0;
+                int32_t left = cur.last_chunk() - cur.chunk;      // blocks left of the current (item, head)
+                bool fresh = true;                                // its first block
+                ok = wait(&kv_full[0], 0);
+                for (int t = 0; t < 2 && ok; ++t) {
+                    ok = wait(&q_ready[t], 0);
+                    tcp::fence_after();
+                    if (!ok) break;
+                    scores(t, 0);
+                    tcp::commit(&s_full[t]);
+                    if (left == 1) tcp::commit(&q_free[t]);
+                }
+                if (ok) tcp::commit(&kv_empty[0]);
+                while (ok) {
+                    const uint32_t uv = 2 * j + 1, uk = 2 * j + 2;
+                    const bool last = left == 1;
+                    if (last) cur.next_pair(cur.last_chunk() - cur.chunk);
+                    const bool another = !last || cur.more();     // one more block follows
+                    const int32_t next_left = last ? (another ? cur.last_chunk() - cur.chunk : 0) : left - 1;
+                    ok = wait(&kv_full[uv % PK_TILES], (uv / PK_TILES) & 1u);
+                    for (int t = 0; t < 2 && ok; ++t) {
+                        ok = wait(&p_ready[t], j & 1u);
+                        if (!ok) break;
+                        tcp::fence_after();
+                        const uint32_t va = kv_at + (uv % PK_TILES) * C::TILE;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            tcp::mma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, tcp::desc(va + k * 2048, 16384, 1024), PV,
+                                        !fresh || k > 0);
+                        if (last) tcp::commit(&o_full[t]);
+                        if (t == 1) tcp::commit(&kv_empty[uv % PK_TILES]);
+                        if (another) {
+                            if (t == 0) ok = wait(&kv_full[uk % PK_TILES], (uk / PK_TILES) & 1u);
+                            if (ok && last) ok = wait(&q_ready[t], (pair + 1) & 1u);
+                            if (!ok) break;
+                            tcp::fence_after();
+                            scores(t, uk);
+                            tcp::commit(&s_full[t]);
+                            if (next_left == 1) tcp::commit(&q_free[t]);
+                            if (t == 1) tcp::commit(&kv_empty[uk % PK_TILES]);
+                        }
+                    }
+                    if (!ok || !another) break;
+                    fresh = last;
+                    pair += last;
+                    left = next_left;
+                    ++j;
+                }
+                if (!ok) *failed = 1;
+                // nothing of this block's memory may be given back while a product is in flight
+                tcp::commit(drained);
+                mbar_wait(drained, 0);
+            }
+            __syncwarp();
+        } else if (warp == 13) {
+            // ======================= cells from the cache ==========================================
+            uint32_t j = 0;
+            bool ok = true;
+            for (; ok && cur.more();) {
+                const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
+                const int32_t end = cur.it.lim0 + (cur.it.row0 + cur.it.nrows - 1) / group;
+                for (int32_t ch = c0; ch < c1; ++ch, ++j) {
+                    const uint32_t rs = j % PK_RAW;
+                    const int32_t key = cur.it.k_lo + ch * KV_PROMPT_CHUNK + lane * KV_CELL;
+                    int32_t page = -1;
+                    if (lane < 8 && key < end) {
+                        page = __ldg(P.block_table + cur.it.req * P.ld_table + (key >> P.kv.page_shift));
+                        if (page < 0 || page >= P.kv.num_pages) page = -1;
+                    }
+                    const uint32_t valid = __ballot_sync(0xffffffffu, page >= 0);
+                    if (j >= PK_RAW) ok = wait(&raw_empty[rs], (j / PK_RAW - 1) & 1u);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        valid_s[rs] = valid;
+                        mbar_expect_tx(&raw_full[rs], __popc(valid) * C::CELL);
+                    }
+                    __syncwarp();
+                    if (page >= 0)
+                        bulk_g2s(smem + C::OFF_RAW + rs * C::RAW + lane * C::CELL,
+                                 kv_cell(P.kv, page, cur.head, key & (P.kv.page_size - 1), C::CELL), C::CELL, &raw_full[rs]);
+                }
+                if (!ok) break;
+                cur.next_pair(c1 - c0);
+            }
+            if (!ok) {
+                *failed = 1;
+                // copies on their way must land before the block leaves
+                for (uint32_t i = j > PK_RAW ? j - PK_RAW : 0; i < j; ++i) mbar_wait(&raw_full[i % PK_RAW], (i / PK_RAW) & 1u);
+            }
+        } else {
+            // ======================= queries: warp 14 tile 0, warp 15 tile 1 ========================
+            const int t = warp - 14;
+            constexpr int LPR = D / 8;                 // 16-byte runs of a row
+            const uint32_t q_at = smem_u32(smem) + t * C::TILE;
+            uint32_t pair = 0;
+            bool ok = true;
+            for (; ok && cur.more(); ++pair) {
+                const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
+                if (pair > 0) ok = wait(&q_free[t], (pair - 1) & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                for (int i = lane; i < 128 * LPR; i += 32) {
+                    const int row = i / LPR, k = i % LPR, my = t * 128 + row;
+                    const bool live = my < cur.it.nrows;
+                    const int32_t r = cur.it.row0 + (live ? my : 0);
+                    const __nv_bfloat16 *src =
+                        P.q + (cur.it.tok0 + r / group) * P.ldq + (int64_t)(cur.head * group + r % group) * D + k * 8;
+                    tcp::cp_async16(q_at + (k >> 3) * 16384 + row * 128 + (((k & 7) ^ (row & 7)) << 4), src, live ? 16 : 0);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_ready[t]);
+                cur.next_pair(c1 - c0);
+            }
+        }
+    }
+    tcp::fence_before();
+    __syncthreads();
+    if (tid == 0 && *failed) atomicAdd(&P.kv.status[STATUS_TIMEOUTS], 1);
+    if (warp == 12) tcp::tmem_dealloc(tmem, 512);
+}
+
+}  // namespace lora

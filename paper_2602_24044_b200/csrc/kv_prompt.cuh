@@ -1,23 +1,31 @@
 // Attention of prompts (many query rows a request) over the 4-bit cache on the 5th-generation tensor cores.
 //
-// The mathematics is that of the single-token kernel: scores are s_t (q . (c_t - 8)) + (low_t + 8 s_t) sum(q),
-// probabilities enter the second product as p_t s_t in fp16, the low values of the values as one number a row.
+//   x = scale q . k_t ,  k_t = z_t + s_t (c_t - 8) ,  z_t = low_t + 8 s_t
+// enters the tensor cores whole, so that a score needs nothing of its key afterwards: s_t has 8 significant
+// bits and c_t - 8 three (or is a power of two), so s_t (c_t - 8) is exact in fp16, and sum(q) z_t is one
+// more step of 16 columns with both factors split into fp16 parts.  Queries (8 bits) are exact in fp16 once
+// a row is divided by a power of two; keys and values of a block are divided by a common power of two,
+// raised like the maximum.  Values enter as fp16(z_t + s_t (c_t - 8)), rounded to 11 bits like the
+// probabilities.
 //
-// What bounds it: a block of 128 keys against 256 rows is 2 x 1024 cycles of tensor pipe, 2048 of the
-// exponential unit and about 1800 issue slots a scheduler (scores to probabilities about 5 a score, widening
-// about 1.3 a code, shared by all 256 rows): all three near each other.  Hence 256 rows a block of threads,
-// as two tiles of 128 whose softmax and matrix products alternate, and everything else on warps of its own:
+// What bounds it: a block of 128 keys against 256 rows is 2100 cycles of tensor pipe, 2048 of the
+// exponential unit, about 2300 of shared memory (operands of the products 1650, widened tiles in and out
+// 650) and about 1400 issue slots a scheduler: all near each other.  A version that kept the codes as they
+// are and applied scale and low to every score read 4 numbers a key and row from shared memory, 4096 cycles
+// more.  Hence 256 rows a block of threads, as two tiles of 128 whose softmax and matrix products
+// alternate, and everything else on warps of its own:
 //   warps 0-3, 4-7   softmax of tile 0, tile 1: a thread is a row; scores from tensor memory to registers,
 //                    probabilities back to the same tensor-memory columns, which the second product reads
 //                    as its A operand; rescales the accumulator itself when its maximum was raised
-//   warps 8-11       widen the codes of a block of keys: K as bf16, V as fp16, into three swizzled tiles
-//                    (order K0 V0 K1 V1 ..), and lay out the keys' scales and lows
+//   warps 8-11       widen the codes of a block of keys, K and V, into three swizzled tiles (order K0 V0 K1 ..)
 //   warp 12          issues the matrix products
 //   warp 13          requests the cells (bulk copies), two blocks ahead
 //   warps 14, 15     bring the queries of the next (item, head), tile 0, tile 1
 // The (item, head, block) triples form one walk cut into equal spans, one per SM; what a span's ends cut is
 // joined afterwards.  Tensor memory: scores of both tiles (2 x 128 columns), accumulators (2 x head_dim).
 #pragma once
+
+#include <cuda_fp16.h>
 
 #include "kv_decode.cuh"
 
@@ -88,18 +96,32 @@ __device__ __forceinline__ void st32(uint32_t addr, const uint32_t (&r)[N], int 
         "r"(r[o + 29]), "r"(r[o + 30]), "r"(r[o + 31]), "r"(addr)
         : "memory");
 }
-// shared-memory matrix descriptor, 128-byte swizzle (start, leading and stride offsets in 16-byte units)
-__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+        "[%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        : "memory");
+}
+// shared-memory matrix descriptor (start, leading and stride offsets in 16-byte units; layout 2: 128-byte
+// swizzle, 0: 8 x 8 core matrices)
+__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t lead, uint32_t stride, uint32_t layout = 2) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)((lead >> 4) & 0x3FFFu) << 16 |
-           (uint64_t)((stride >> 4) & 0x3FFFu) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+           (uint64_t)((stride >> 4) & 0x3FFFu) << 32 | (uint64_t)1 << 46 | (uint64_t)layout << 61;
 }
 // fp32 accumulator; a, b: 0 = fp16, 1 = bf16; b_n: B's rows run along N
 __host__ __device__ constexpr uint32_t instr(uint32_t type, uint32_t N, uint32_t b_n) {
     return (1u << 4) | (type << 7) | (type << 10) | (b_n << 16) | ((N >> 3) << 17) | ((128u >> 4) << 24);
 }
-template <int R> __device__ __forceinline__ void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
-template <int R> __device__ __forceinline__ void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
-
 // two floats at once
 __device__ __forceinline__ uint64_t pack2f(float a, float b) {
     uint64_t r;
@@ -136,18 +158,54 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32
 }
 }  // namespace tcp
 
-constexpr int PK_THREADS = 512, PK_TILES = 3, PK_RAW = 2, PK_PARAMS = 3;
+__device__ __forceinline__ uint32_t half2_of(float x) { return pack_f16(x, x); }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ float f16_round(float x) { return __half2float(__float2half_rn(x)); }
+// x as three fp16 parts
+struct Split { float h, l, t; };
+__device__ __forceinline__ Split split_f16(float x) {
+    Split s;
+    s.h = f16_round(x);
+    s.l = f16_round(x - s.h);
+    s.t = f16_round(x - s.h - s.l);
+    return s;
+}
+
+// the n lowest bits (n may lie outside 0 .. 32)
+__device__ __forceinline__ uint32_t low_bits(int32_t n) {
+    return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
+constexpr int PK_THREADS = 512, PK_TILES = 3, PK_RAW = 2, PK_INFO = 3;
+constexpr int PK_EXTRA = 128 * 16 * 2;       // 16 more columns of 128 rows, as core matrices
+
+struct PromptInfo {          // of a block of keys, from the widening warps to the softmax
+    int32_t ek, ev;          // exponents taken out of the keys, of the values
+    uint32_t valid;          // cells that are there
+    uint32_t bad[4];         // value rows that are no numbers (their tile rows are zero)
+    uint32_t reserved;
+};
 
 template <int D>
 struct PromptCfg {
     static constexpr int CELL = kv_cell_bytes(D);
     static constexpr int RAW = 8 * CELL;                    // a block of 128 keys as it lies in the cache
     static constexpr int TILE = 128 * D * 2;                // 128 rows of 16-bit values
-    static constexpr int PARAM = 128 * 16 + 16;             // (scale, z) of keys, of values; exponent, valid cells
     static constexpr int OFF_KV = 2 * TILE;                 // behind the queries of both tiles
-    static constexpr int OFF_RAW = OFF_KV + PK_TILES * TILE;
-    static constexpr int OFF_PARAM = OFF_RAW + PK_RAW * RAW;
-    static constexpr int OFF_BAR = OFF_PARAM + PK_PARAMS * PARAM;
+    static constexpr int OFF_QX = OFF_KV + PK_TILES * TILE; // the further columns: queries of both tiles,
+    static constexpr int OFF_KX = OFF_QX + 2 * PK_EXTRA;    // keys of the tiles
+    static constexpr int OFF_RAW = OFF_KX + PK_TILES * PK_EXTRA;
+    static constexpr int OFF_INFO = OFF_RAW + PK_RAW * RAW;
+    static constexpr int OFF_BAR = OFF_INFO + PK_INFO * (int)sizeof(PromptInfo);
     static constexpr int SMEM = OFF_BAR + 512 + 1024;       // 1024: the swizzled tiles' alignment
 };
 
@@ -189,14 +247,16 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
     uint64_t *s_full = kv_empty + PK_TILES;       // [2] scores of a tile are in tensor memory
     uint64_t *p_ready = s_full + 2;               // [2] probabilities are
     uint64_t *o_full = p_ready + 2;               // [2] the accumulator of an (item, head) is complete
-    uint64_t *q_ready = o_full + 2;               // [2] queries are in shared memory
-    uint64_t *q_free = q_ready + 2;               // [2] the last score product of an (item, head) is done, the sums are taken
-    uint64_t *param_full = q_free + 2;
-    uint64_t *param_empty = param_full + PK_PARAMS;
-    uint64_t *drained = param_empty + PK_PARAMS;  // every product has completed
+    uint64_t *q_here = o_full + 2;                // [2] queries are in shared memory as they came
+    uint64_t *q_ready = q_here + 2;               // [2] and as fp16
+    uint64_t *q_free = q_ready + 2;               // [2] the last score product of an (item, head) is done
+    uint64_t *info_full = q_free + 2;
+    uint64_t *info_empty = info_full + PK_INFO;
+    uint64_t *drained = info_empty + PK_INFO;     // every product has completed
     uint32_t *valid_s = reinterpret_cast<uint32_t *>(drained + 1);      // [PK_RAW] cells that are there
-    uint32_t *most_s = valid_s + PK_RAW;          // [2][4] largest value row of a block, per warp
-    uint32_t *tmem_slot = most_s + 8;
+    uint32_t *most_s = valid_s + PK_RAW;          // [2][8] largest key and value row of a block, per warp
+    uint32_t *tmem_slot = most_s + 16;
+    PromptInfo *infos = reinterpret_cast<PromptInfo *>(smem + C::OFF_INFO);
     volatile uint32_t *failed = tmem_slot + 1;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -214,14 +274,19 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[i], 128);
             mbar_init(&o_full[i], 1);
-            mbar_init(&q_ready[i], 1);
-            mbar_init(&q_free[i], 5);
+            mbar_init(&q_here[i], 1);
+            mbar_init(&q_ready[i], 128);
+            mbar_init(&q_free[i], 1);
         }
-        for (int i = 0; i < PK_PARAMS; ++i) { mbar_init(&param_full[i], 4); mbar_init(&param_empty[i], 8); }
+        for (int i = 0; i < PK_INFO; ++i) { mbar_init(&info_full[i], 4); mbar_init(&info_empty[i], 8); }
         mbar_init(drained, 1);
         *failed = 0;
         fence_mbar_init();
     }
+    // the columns that no part fills stay zero
+    for (int i = tid; i < (2 + PK_TILES) * PK_EXTRA / 16; i += PK_THREADS)
+        *reinterpret_cast<uint4 *>(smem + C::OFF_QX + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async();
     if (warp == 12) {
         tcp::tmem_alloc(tmem_slot, 512);
         tcp::tmem_relinquish();
@@ -243,136 +308,159 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
 
     if (warp < 8) {
         // =========================== softmax: a thread is a row ====================================
-        tcp::reg_inc<184>();
         const int t = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
+        // The queries of a pair: bf16 as they came -> fp16 divided by a power of two, in place, and the row's
+        // sum in parts; returns log2(e) |scale| times that power.  (A negative scale turns the queries.)
+        auto take_queries = [&](uint32_t pair, bool &ok) -> float {
+            ok = wait(&q_here[t], pair & 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return 0.0f;
+            const uint32_t q_at = smem_u32(smem) + t * C::TILE + row * 128;
+            uint32_t most = 0;
+#pragma unroll 4
+            for (int i = 0; i < D / 8; ++i) {
+                uint32_t v[4];
+                lds_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = max(most, max((v[e] << 16) & 0x7fff0000u, v[e] & 0x7fff0000u));
+            }
+            const int a = most >= 0x7f800000u ? 0 : max((int)(most >> 23) - 126, -126);     // |q| < 2^a
+            const float unit = copysignf(pow2(max(-a, -126)), P.scale2);
+            float sum = 0.0f;
+#pragma unroll 4
+            for (int i = 0; i < D / 8; ++i) {
+                const uint32_t at = q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4);
+                uint32_t v[4];
+                lds_v4(at, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float lo = __uint_as_float(v[e] << 16) * unit, hi = __uint_as_float(v[e] & 0xffff0000u) * unit;
+                    sum += lo + hi;
+                    v[e] = pack_f16(lo, hi);
+                }
+                tcp::sts_v4(at, v);
+            }
+            const Split q = split_f16(sum);
+            const uint32_t qx[4] = {pack_f16(q.h, q.h), pack_f16(q.l, q.l), pack_f16(q.h, q.t), 0u};
+            tcp::sts_v4(smem_u32(smem) + C::OFF_QX + t * PK_EXTRA + (row >> 3) * 128 + (row & 7) * 16, qx);
+            fence_proxy_async();
+            mbar_arrive(&q_ready[t]);
+            return fabsf(P.scale2) * pow2(min(max(a, -126), 126));
+        };
         uint32_t j = 0, pair = 0;
         bool ok = true;
+        float q_unit = take_queries(0, ok);
         for (; ok && cur.more(); ++pair) {
             const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
             const int32_t r = cur.it.row0 + t * 128 + row;
             const int32_t my = t * 128 + row;
             // rows past the item's end (their queries are zero) follow the last one's limit
-            const int32_t lim = cur.it.lim0 + min(r, cur.it.row0 + cur.it.nrows - 1) / group;
+            const int32_t last_row = cur.it.row0 + cur.it.nrows - 1;
+            const int32_t lim = cur.it.lim0 + min(r, last_row) / group;
             const int32_t lo = P.window > 0 ? lim - P.window : 0;
-            const int32_t lim_min = cur.it.lim0 + min(cur.it.row0 + t * 128, cur.it.row0 + cur.it.nrows - 1) / group;
-            const int32_t lo_max = P.window > 0 ? cur.it.lim0 + min(cur.it.row0 + t * 128 + 127, cur.it.row0 + cur.it.nrows - 1) / group - P.window : 0;
-            ok = wait(&q_ready[t], pair & 1u);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            float qs = 0.0f;
-            {
-                const uint32_t q_at = smem_u32(smem) + t * C::TILE + row * 128;
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    uint32_t v[4];
-                    lds_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), v);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) qs += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&q_free[t]);
-            float m = -INFINITY, l = 0.0f, z = 0.0f;
+            const int32_t lim_min = cur.it.lim0 + min(cur.it.row0 + t * 128, last_row) / group;
+            const int32_t lo_max = P.window > 0 ? cur.it.lim0 + min(cur.it.row0 + t * 128 + 127, last_row) / group - P.window : 0;
+            float m = -INFINITY, l = 0.0f;
             int ve = KV_NO_EXPONENT;
             for (int32_t ch = c0; ch < c1; ++ch, ++j) {
-                const uint32_t ps = j % PK_PARAMS;
-                ok = wait(&param_full[ps], (j / PK_PARAMS) & 1u) && wait(&s_full[t], j & 1u);
+                const uint32_t ps = j % PK_INFO;
+                ok = wait(&info_full[ps], (j / PK_INFO) & 1u) && wait(&s_full[t], j & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tcp::fence_after();
-                uint32_t x[128];
-                LORA_TMEM_LD32(s_at, x, 0);
-                LORA_TMEM_LD32(s_at + 32, x, 32);
-                LORA_TMEM_LD32(s_at + 64, x, 64);
-                LORA_TMEM_LD32(s_at + 96, x, 96);
-                const uint32_t par = smem_u32(smem) + C::OFF_PARAM + ps * C::PARAM;
-                const int ve_new = (int)lds_u32(par + 2048);
-                const uint32_t valid = lds_u32(par + 2052);
+                const PromptInfo *info = infos + ps;
+                const int ve_new = info->ev;
+                const uint32_t valid = info->valid;
+                const float f = fminf(fmaxf(q_unit * pow2(info->ek), 1.17549435e-38f), 3e38f);     // never 0 or inf: masked scores stay -inf
                 const int32_t key0 = cur.it.k_lo + ch * KV_PROMPT_CHUNK;
                 const bool whole = valid == 0xffu && key0 + 128 <= lim_min && key0 >= lo_max;
-                tcp::wait_ld();
-                const uint64_t qs2 = tcp::pack2f(qs, qs);
+                const bool any_bad = (info->bad[0] | info->bad[1] | info->bad[2] | info->bad[3]) != 0;
+                // the scores are read twice (tensor memory is fast; 128 registers of them are not there)
                 float mx = -INFINITY;
+#pragma unroll 1
+                for (int h = 0; h < 128; h += 64) {
+                    uint32_t x[64];
+                    LORA_TMEM_LD32(s_at + h, x, 0);
+                    LORA_TMEM_LD32(s_at + h + 32, x, 32);
+                    tcp::wait_ld();
+                    if (!whole) {      // what a row does not see goes back as -inf
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
-                    uint64_t ks, kz;
-                    tcp::lds_2x64(par + i * 16, ks, kz);
-                    const uint64_t v = tcp::fma2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), ks,
-                                                 tcp::mul2(qs2, kz));
-                    float a, b;
-                    tcp::unpack2f(v, a, b);
-                    if (!whole) {
-                        const int32_t k = key0 + 2 * i;
-                        const bool there = (valid >> (i / 8)) & 1u;
-                        a = there && k < lim && k >= lo ? a : -INFINITY;
-                        b = there && k + 1 < lim && k + 1 >= lo ? b : -INFINITY;
+                        for (int w = 0; w < 2; ++w) {
+                            const int32_t k = key0 + h + 32 * w;       // the word's 32 keys: bit i is key k + i
+                            const uint32_t cells = valid >> ((h >> 4) + 2 * w);
+                            const uint32_t seen = low_bits(lim - k) & ~low_bits(lo - k) &
+                                                  (((cells & 1u) ? 0xffffu : 0u) | ((cells & 2u) ? 0xffff0000u : 0u));
+                            // a value row that is no number makes the rows that see it no numbers
+                            if (any_bad && (seen & info->bad[(h >> 5) + w])) l = NAN;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[32 * w + i] = (seen >> i) & 1u ? x[32 * w + i] : 0xff800000u;
+                        }
+                        tcp::st32(s_at + h, x, 0);
+                        tcp::st32(s_at + h + 32, x, 32);
                     }
-                    mx = fmaxf(mx, fmaxf(a, b));
-                    x[2 * i] = __float_as_uint(a);
-                    x[2 * i + 1] = __float_as_uint(b);
+#pragma unroll
+                    for (int i = 0; i < 64; i += 2)
+                        mx = fmaxf(mx, fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
                 }
-                const bool up = mx > m + KV_RAISE || ve_new != ve;
-                if (__any_sync(0xffffffffu, up)) {
+                if (!whole) tcp::wait_st();
+                else if (any_bad) l = NAN;
+                mx = mx == -INFINITY ? mx : mx * f;
+                if (__any_sync(0xffffffffu, mx > m + KV_RAISE || ve_new != ve)) {
                     const float mn = mx > m + KV_RAISE ? mx : m;
-                    const float f = mn == m ? 1.0f : exp2_approx(m - mn), fe = f * pow2(max(ve - ve_new, -126));
+                    const float fm = mn == m ? 1.0f : exp2_approx(m - mn), fe = fm * pow2(max(ve - ve_new, -126));
                     m = mn;
                     ve = ve_new;
-                    l *= f;
-                    z *= fe;
+                    l *= fm;
                     if (ch > c0) {     // the products of the blocks before have completed: their scores' successor is here
 #pragma unroll
-                        for (int cc = 0; cc < D; cc += 32) {
-                            uint32_t o[32];
-                            LORA_TMEM_LD32(o_at + cc, o, 0);
+                        for (int cc = 0; cc < D; cc += 16) {
+                            uint32_t o[16];
+                            tcp::ld16(o_at + cc, o);
                             tcp::wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fe);
-                            tcp::st32(o_at + cc, o, 0);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fe);
+                            tcp::st16(o_at + cc, o);
                         }
                         tcp::wait_st();
                     }
                 }
-                uint64_t l2 = 0, z2 = 0;
-                const uint64_t nm = tcp::pack2f(-m, -m);
+                // a row that sees nothing has no maximum: its probabilities are 2^(-inf - 0)
+                const float mm = m == -INFINITY ? 0.0f : m;
+                const uint64_t f2 = tcp::pack2f(f, f), nm = tcp::pack2f(-mm, -mm);
+                uint64_t l2 = 0;
+#pragma unroll 1
+                for (int h = 0; h < 128; h += 64) {     // (probabilities h / 2 .. overwrite scores that have been read)
+                    uint32_t x[64];
+                    LORA_TMEM_LD32(s_at + h, x, 0);
+                    LORA_TMEM_LD32(s_at + h + 32, x, 32);
+                    tcp::wait_ld();
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
-                    uint64_t vs, vz;
-                    tcp::lds_2x64(par + 1024 + i * 16, vs, vz);
-                    float a, b;
-                    tcp::unpack2f(tcp::add2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), nm), a, b);
-                    a = exp2_approx(a);
-                    b = exp2_approx(b);
-                    uint64_t p = tcp::pack2f(a, b);
-                    if (!whole) {      // what is not seen counts nothing, whatever its scale and low are
-                        const bool na = __uint_as_float(x[2 * i]) == -INFINITY, nb = __uint_as_float(x[2 * i + 1]) == -INFINITY;
-                        p = tcp::pack2f(na ? 0.0f : a, nb ? 0.0f : b);
-                        float s0f, s1f, z0f, z1f;
-                        tcp::unpack2f(vs, s0f, s1f);
-                        tcp::unpack2f(vz, z0f, z1f);
-                        vs = tcp::pack2f(na ? 0.0f : s0f, nb ? 0.0f : s1f);
-                        vz = tcp::pack2f(na ? 0.0f : z0f, nb ? 0.0f : z1f);
+                    for (int i = 0; i < 32; ++i) {
+                        float a, b;
+                        tcp::unpack2f(tcp::fma2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, nm),
+                                      a, b);
+                        a = exp2_approx(a);
+                        b = exp2_approx(b);
+                        l2 = tcp::add2(l2, tcp::pack2f(a, b));
+                        x[i] = pack_f16(a, b);
                     }
-                    l2 = tcp::add2(l2, p);
-                    z2 = tcp::fma2(p, vz, z2);
-                    float c, d;
-                    tcp::unpack2f(tcp::mul2(p, vs), c, d);
-                    x[i] = pack_f16(c, d);
+                    tcp::st32(s_at + h / 2, x, 0);
                 }
                 float a, b;
                 tcp::unpack2f(l2, a, b);
                 l += a + b;
-                tcp::unpack2f(z2, a, b);
-                z += a + b;
-                tcp::st32(s_at, x, 0);
-                tcp::st32(s_at + 32, x, 32);
                 tcp::wait_st();
                 tcp::fence_before();
                 mbar_arrive(&p_ready[t]);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&param_empty[ps]);
+                if (lane == 0) mbar_arrive(&info_empty[ps]);
             }
+            if (!ok) break;
+            // the next pair's queries, while the last product runs
+            float next_unit = 0.0f;
+            if (cur.pos + (c1 - c0) < cur.end) next_unit = take_queries(pair + 1, ok);
             if (!ok) break;
             // ---- the (item, head) is over, or the span is ------------------------------------------
             ok = wait(&o_full[t], pair & 1u);
@@ -390,7 +478,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 tcp::wait_ld();
                 if (live) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint((__uint_as_float(o[e]) + z) * inv * back);
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv * back);
                     if (complete) {
                         uint4 *dst = reinterpret_cast<uint4 *>(P.out + tok * P.ldo + (int64_t)hq * D + cc);
 #pragma unroll
@@ -416,11 +504,11 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 else if (P.lse) P.lse[(int64_t)tok * P.kv.hq + hq] = inv == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
             }
             tcp::fence_before();
+            q_unit = next_unit;
             cur.next_pair(c1 - c0);
         }
     } else if (warp < 12) {
         // =========================== widening ======================================================
-        tcp::reg_dec<96>();
         const int id = tid - 256, wq = warp - 8, kr = id >> 2, c = id & 3;
         uint32_t j = 0, u = 0;        // blocks, tiles
         // a warp whose wait failed still takes part in the named barrier of the next block, where all four
@@ -429,30 +517,37 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         while (!dead && cur.more()) {
             const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
             const int32_t end = cur.it.lim0 + (cur.it.row0 + cur.it.nrows - 1) / group;
-            int ve = KV_NO_EXPONENT;
+            int ek = KV_NO_EXPONENT, ev = KV_NO_EXPONENT;
             for (int32_t ch = c0; ch < c1; ++ch, ++j) {
-                const uint32_t rs = j % PK_RAW, ps = j % PK_PARAMS;
+                const uint32_t rs = j % PK_RAW, ps = j % PK_INFO;
                 const uint32_t raw = smem_u32(smem) + C::OFF_RAW + rs * C::RAW;
-                const uint32_t par = smem_u32(smem) + C::OFF_PARAM + ps * C::PARAM;
                 ok = ok && wait(&raw_full[rs], (j / PK_RAW) & 1u);
-                if (ok && j >= PK_PARAMS) ok = wait(&param_empty[ps], (j / PK_PARAMS - 1) & 1u);
-                // scales and lows: a thread is a key
+                if (ok && j >= PK_INFO) ok = wait(&info_empty[ps], (j / PK_INFO - 1) & 1u);
+                // the common exponents: a thread is a key
                 const uint32_t valid = valid_s[rs];
-                float ks = 0.0f, kz = 0.0f, vs = 0.0f, vz = 0.0f;
-                uint32_t mag = 0;
-                if (((valid >> (id >> 4)) & 1u) && cur.it.k_lo + ch * KV_PROMPT_CHUNK + id < end) {
+                const int32_t left = end - (cur.it.k_lo + ch * KV_PROMPT_CHUNK);     // keys of the block that are there
+                float ks = 0.0f, kl = 0.0f;
+                uint32_t kmag = 0, vmag = 0;
+                bool bad = false;
+                if (((valid >> (id >> 4)) & 1u) && id < left) {
                     const uint32_t at = raw + (id >> 4) * C::CELL + kv_cell_params(D) + (id & 15) * 4;
                     const uint32_t kp = lds_u32(at), vp = lds_u32(at + KV_CELL * 4);
                     ks = __uint_as_float(kp << 16);
-                    kz = fmaf(8.0f, ks, __uint_as_float(kp & 0xffff0000u)) * P.scale2;
-                    ks *= P.scale2;
-                    vs = __uint_as_float(vp << 16);
-                    vz = fmaf(8.0f, vs, __uint_as_float(vp & 0xffff0000u));
-                    mag = max(vp << 16, vp & 0x7fff0000u);
-                    if (mag >= 0x7f800000u) mag = 0;
+                    kl = __uint_as_float(kp & 0xffff0000u);
+                    kmag = max(kp << 16, kp & 0x7fff0000u);
+                    vmag = max(vp << 16, vp & 0x7fff0000u);
+                    bad = vmag >= 0x7f800000u;
+                    if (kmag >= 0x7f800000u) kmag = 0;
+                    if (bad) vmag = 0;
                 }
-                mag = __reduce_max_sync(0xffffffffu, mag);
-                if (lane == 0) most_s[(j & 1u) * 4 + wq] = mag;
+                kmag = __reduce_max_sync(0xffffffffu, kmag);
+                vmag = __reduce_max_sync(0xffffffffu, vmag);
+                const uint32_t bad_keys = __ballot_sync(0xffffffffu, bad);
+                uint32_t *most = most_s + (j & 1u) * 8;
+                if (lane == 0) {
+                    most[wq] = kmag;
+                    most[4 + wq] = vmag;
+                }
                 uint32_t any_bad;      // all four warps take the same decision
                 asm volatile(
                     "{\n\t.reg .pred p, q;\n\t"
@@ -463,22 +558,19 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     : "r"(ok ? 0u : 1u)
                     : "memory");
                 if (any_bad) { dead = true; break; }
-                const uint32_t *mo = most_s + (j & 1u) * 4;
-                ve = raise_exponent(ve, max(max(mo[0], mo[1]), max(mo[2], mo[3])));
-                const float unit = pow2(-ve);
-                {
-                    float *pf = reinterpret_cast<float *>(smem + C::OFF_PARAM + ps * C::PARAM);
-                    pf[(id >> 1) * 4 + (id & 1)] = ks;
-                    pf[(id >> 1) * 4 + 2 + (id & 1)] = kz;
-                    pf[256 + (id >> 1) * 4 + (id & 1)] = vs * unit;
-                    pf[256 + (id >> 1) * 4 + 2 + (id & 1)] = vz * unit;
-                    if (id == 0) {
-                        reinterpret_cast<int *>(pf)[512] = ve;
-                        reinterpret_cast<uint32_t *>(pf)[513] = valid;
+                ek = raise_exponent(ek, max(max(most[0], most[1]), max(most[2], most[3])));
+                ev = raise_exponent(ev, max(max(most[4], most[5]), max(most[6], most[7])));
+                const float k_unit = pow2(-ek), v_unit = pow2(-ev);
+                if (lane == 0) {
+                    PromptInfo *info = infos + ps;
+                    info->bad[wq] = bad_keys;
+                    if (wq == 0) {
+                        info->ek = ek;
+                        info->ev = ev;
+                        info->valid = valid;
                     }
+                    mbar_arrive(&info_full[ps]);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&param_full[ps]);
                 // codes: K, then V.  Four lanes share a row; those of the second pair take their two halves
                 // in the other order, so that the eight lanes of a store phase hit eight different banks
 #pragma unroll
@@ -487,10 +579,23 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     if (u >= PK_TILES) ok = ok && wait(&kv_empty[b], (u / PK_TILES - 1) & 1u);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
+                    if (kv == 0) {     // sum(q) z_t: parts (h, l, h, l, t, h) against the queries' (h, h, l, l, h, t)
+                        const Split z = split_f16(fmaf(8.0f, ks, kl) * k_unit);
+                        const uint32_t kx[4] = {pack_f16(z.h, z.l), pack_f16(z.h, z.l), pack_f16(z.t, z.h), 0u};
+                        tcp::sts_v4(smem_u32(smem) + C::OFF_KX + b * PK_EXTRA + (id >> 3) * 128 + (id & 7) * 16, kx);
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int key = i * 32 + kr;
-                        const uint32_t src = raw + (key >> 4) * C::CELL + (kv * KV_CELL + (key & 15)) * (D / 2) + c * (D / 8);
+                        const uint32_t cell = raw + (key >> 4) * C::CELL;
+                        const uint32_t src = cell + (kv * KV_CELL + (key & 15)) * (D / 2) + c * (D / 8);
+                        // a row that is not there, or whose values are no numbers, becomes zero
+                        const uint32_t par = lds_u32(cell + kv_cell_params(D) + (kv * KV_CELL + (key & 15)) * 4);
+                        float sf = __uint_as_float(par << 16), zf = fmaf(8.0f, sf, __uint_as_float(par & 0xffff0000u));
+                        bool there = ((valid >> (key >> 4)) & 1u) && key < left;
+                        if (kv == 1) there = there && max(par << 16, par & 0x7fff0000u) < 0x7f800000u;
+                        const uint32_t s2 = half2_of(there ? sf * (kv ? v_unit : k_unit) : 0.0f);
+                        const uint32_t z2 = half2_of(there ? zf * v_unit : 0.0f);
 #pragma unroll
                         for (int h = 0; h < D / 64; ++h) {
                             const int hh = D == 128 ? h ^ (c >> 1) : 0;      // which 8 bytes of the lane's run
@@ -499,16 +604,10 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 const int word = c * (D / 32) + hh * 2 + e;      // 8 elements: a 16-byte run of the tile's row
-                                uint32_t v[4];
-                                if (kv == 0) {
+                                uint32_t v[4] = {widen_f16_lo(w[e]), widen_f16_hi(w[e]), widen_f16_lo(w[e] >> 8),
+                                                 widen_f16_hi(w[e] >> 8)};
 #pragma unroll
-                                    for (int q = 0; q < 4; ++q) v[q] = widen_bf16(w[e] >> (4 * q));
-                                } else {
-                                    v[0] = widen_f16_lo(w[e]);
-                                    v[1] = widen_f16_hi(w[e]);
-                                    v[2] = widen_f16_lo(w[e] >> 8);
-                                    v[3] = widen_f16_hi(w[e] >> 8);
-                                }
+                                for (int q = 0; q < 4; ++q) v[q] = kv ? fma_f16x2(v[q], s2, z2) : mul_f16x2(v[q], s2);
                                 tcp::sts_v4(tile + (word >> 3) * 16384 + key * 128 + (((word & 7) ^ (key & 7)) << 4), v);
                             }
                         }
@@ -525,11 +624,10 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         }
         if (dead || !ok) *failed = 1;
     } else {
-        tcp::reg_dec<48>();
         if (warp == 12) {
             // ======================= matrix products ===============================================
             if (lane == 0) {
-                constexpr uint32_t QK = tcp::instr(1, 128, 0), PV = tcp::instr(0, D, 1);
+                constexpr uint32_t QK = tcp::instr(0, 128, 0), PV = tcp::instr(0, D, 1);
                 const uint32_t q_at = smem_u32(smem), kv_at = q_at + C::OFF_KV;
                 bool ok = true;
                 auto scores = [&](int t, uint32_t u) {
@@ -538,6 +636,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     for (int k = 0; k < D / 16; ++k)
                         tcp::mma_ss(tmem + t * 128, tcp::desc(qa + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024),
                                     tcp::desc(ka + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024), QK, k > 0);
+                    tcp::mma_ss(tmem + t * 128, tcp::desc(q_at + C::OFF_QX + t * PK_EXTRA, 2048, 128, 0),
+                                tcp::desc(q_at + C::OFF_KX + (u % PK_TILES) * PK_EXTRA, 2048, 128, 0), QK, 1);
                 };
                 uint32_t j = 0, pair = 0;
                 int32_t left = cur.last_chunk() - cur.chunk;      // blocks left of the current (item, head)
@@ -652,7 +752,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&q_ready[t]);
+                if (lane == 0) mbar_arrive(&q_here[t]);
                 cur.next_pair(c1 - c0);
             }
         }

@@ -9,8 +9,24 @@ static size_t part_bytes(int32_t walkers, int32_t rows, int32_t d) {
     return (size_t)2 * walkers * rows * (d * sizeof(float) + sizeof(float2));
 }
 
+// The joining kernel may become resident while the one before it runs.
+template <typename K>
+static lora_status_t launch_join(K kernel, dim3 grid, const AttnParams &P, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, P));
+    return count_launch();
+}
+
 template <int D, int NT>
-static lora_status_t launch_decode(lora_kv *kv, AttnParams P, cudaStream_t stream) {
+static lora_status_t launch_decode(lora_kv *kv, AttnParams P, int64_t pairs, cudaStream_t stream) {
     using C = DecCfg<D>;
     bool &done = kv->decode_attr[(D == 128 ? 2 : 0) + NT - 1];
     if (!done) {
@@ -21,8 +37,10 @@ static lora_status_t launch_decode(lora_kv *kv, AttnParams P, cudaStream_t strea
     decode_attention_kernel<D, NT><<<P.walkers / DK_WARPS, 32 * DK_WARPS, C::SMEM, stream>>>(P);
     lora_status_t s = count_launch();
     if (s != LORA_OK) return s;
-    join_kernel<D, 8 * NT, false><<<P.walkers, 256, 0, stream>>>(P);
-    return count_launch();
+    // few pairs are cut into many pieces each: a block per pair and row
+    if (pairs <= 4 * kv->sm_count)
+        return launch_join(join_kernel<D, 8 * NT, false, true>, dim3((unsigned)pairs, 8 * NT), P, stream);
+    return launch_join(join_kernel<D, 8 * NT, false, false>, dim3(P.walkers, NT), P, stream);
 }
 
 template <int D>
@@ -37,8 +55,7 @@ static lora_status_t launch_prompt(lora_kv *kv, AttnParams P, cudaStream_t strea
     prompt_attention_kernel<D><<<P.walkers, PK_THREADS, C::SMEM, stream>>>(P);
     lora_status_t s = count_launch();
     if (s != LORA_OK) return s;
-    join_kernel<D, KV_PROMPT_ROWS, true><<<dim3(P.walkers, 32), 256, 0, stream>>>(P);
-    return count_launch();
+    return launch_join(join_kernel<D, KV_PROMPT_ROWS, true, false>, dim3(P.walkers, KV_PROMPT_ROWS / 8), P, stream);
 }
 
 }  // namespace lora
@@ -97,11 +114,14 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     P.walkers = kv->dec_walkers(rows);
     P.part = (float *)workspace;
     P.part_ml = (float2 *)(P.part + (size_t)2 * P.walkers * rows * kv->d);
+    // (item, head) pairs that can be in the list: one item a request where a request's rows fit one
+    const int64_t pairs = ((int64_t)rec->max_q * kv->group <= rows ? (int64_t)R
+                                                                   : R + (int64_t)T * kv->group / rows) * kv->hkv;
     DeviceGuard g(kv->device);
-    lora_status_t s = kv->d == 64 ? (rows == 8 ? launch_decode<64, 1>(kv, P, (cudaStream_t)stream)
-                                               : launch_decode<64, 2>(kv, P, (cudaStream_t)stream))
-                                  : (rows == 8 ? launch_decode<128, 1>(kv, P, (cudaStream_t)stream)
-                                               : launch_decode<128, 2>(kv, P, (cudaStream_t)stream));
+    lora_status_t s = kv->d == 64 ? (rows == 8 ? launch_decode<64, 1>(kv, P, pairs, (cudaStream_t)stream)
+                                               : launch_decode<64, 2>(kv, P, pairs, (cudaStream_t)stream))
+                                  : (rows == 8 ? launch_decode<128, 1>(kv, P, pairs, (cudaStream_t)stream)
+                                               : launch_decode<128, 2>(kv, P, pairs, (cudaStream_t)stream));
     if (s != LORA_OK) return s;
     // a batch whose requests all have few rows needs no more
     if ((int64_t)rec->max_q * kv->group <= KV_DEC_MAX_ROWS) return LORA_OK;

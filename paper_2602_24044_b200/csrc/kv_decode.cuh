@@ -150,6 +150,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     const int64_t total = walk->total, span = walk->span;
     const int64_t s0 = w * span, s1 = min(s0 + span, total);
     if (s0 >= s1) return;
+    griddep_launch_dependents();      // the joining blocks may come as soon as there is room: they wait for the end
     const KvItem *items = reinterpret_cast<const KvItem *>(P.tables + P.L.dec_items);
     const int32_t first = __ldg(P.tables + P.L.dec_first + w);
     const int32_t hkv = P.kv.hkv, group = P.kv.group;
@@ -476,72 +477,111 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     }
 }
 
-// Joins the pieces of the (item, head) pairs that lie in more than one span: block w takes the one that
-// begins in walker w's span and goes on in the next.  Pieces are added in their order, so the result does
-// not depend on timing.  PROMPT: the prompt walk's lists (rows of an item: ROWS).
-template <int D, int ROWS, bool PROMPT>
+// Joins the pieces of the (item, head) pairs that lie in more than one span, in their order, so that the
+// result does not depend on timing.  What bounds it is the chain of dependent loads (walk, item, maxima,
+// outputs), so every block reads its item before it waits for the kernel that leaves the pieces, and the
+// loads of 16 pieces are in flight together.  Two ways to share it out:
+//   PAIRS = false  block x looks at the end of walker x's span and takes the pair that begins in the span and
+//                  crosses it; a warp per row (rows 8 y .. 8 y + 7): many pairs of few pieces
+//   PAIRS = true   block x is a pair, y its row, whose pieces the eight warps share: few pairs of many pieces
+//                  (four requests of 100k keys: 75 pieces each)
+template <int D, int ROWS, bool PROMPT, bool PAIRS>
 __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
-    constexpr int WARPS = 8, E = D / 32;
-    __shared__ float acc_s[WARPS][D];
-    const KvWalk *walk = reinterpret_cast<const KvWalk *>(P.tables + P.L.walk) + (PROMPT ? 1 : 0);
-    const int32_t w = blockIdx.x;
-    const int64_t total = walk->total, span = walk->span, cut = (w + 1) * span;
-    if (cut >= total) return;
-    const KvItem it = load_item(reinterpret_cast<const KvItem *>(P.tables + (PROMPT ? P.L.pr_items : P.L.dec_items)) +
-                                __ldg(P.tables + (PROMPT ? P.L.pr_first : P.L.dec_first) + w + 1));
-    const int64_t off = cut - P.kv.hkv * it.start;
-    const int32_t head = (int32_t)(off / it.n);
-    const int64_t begin = P.kv.hkv * it.start + (int64_t)head * it.n;
-    if (begin == cut || begin < w * span) return;      // nothing crosses this end, or another block has it
-    const int32_t last = (int32_t)((begin + it.n - 1) / span), pieces = last - w + 1;
+    constexpr int E = D / 32, U = 16;
+    __shared__ float acc_s[PAIRS ? 8 : 1][D];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int4 *wk = reinterpret_cast<const int4 *>(reinterpret_cast<const KvWalk *>(P.tables + P.L.walk) + (PROMPT ? 1 : 0));
+    const int4 w01 = __ldg(wk), w23 = __ldg(wk + 1);
+    const int64_t total = (int64_t)(uint32_t)w01.x | ((int64_t)w01.y << 32), span = (int64_t)(uint32_t)w01.z | ((int64_t)w01.w << 32);
+    const KvItem *items = reinterpret_cast<const KvItem *>(P.tables + (PROMPT ? P.L.pr_items : P.L.dec_items));
+    KvItem it;
+    int32_t head;
+    int64_t begin, w;
+    if (PAIRS) {
+        const int32_t item = blockIdx.x / P.kv.hkv;
+        if (item >= w23.x) return;
+        it = load_item(items + item);
+        head = blockIdx.x % P.kv.hkv;
+        begin = P.kv.hkv * it.start + (int64_t)head * it.n;
+        w = begin / span;
+        if (begin + it.n <= (w + 1) * span) return;
+    } else {
+        w = blockIdx.x;
+        const int64_t cut = (w + 1) * span;
+        if (cut >= total) return;
+        it = load_item(items + __ldg(P.tables + (PROMPT ? P.L.pr_first : P.L.dec_first) + w + 1));
+        const int64_t off = cut - P.kv.hkv * it.start;
+        head = (int32_t)(off / it.n);
+        begin = P.kv.hkv * it.start + (int64_t)head * it.n;
+        if (begin == cut || begin < w * span) return;      // nothing crosses this end, or another block has it
+    }
+    const int32_t row = PAIRS ? (int32_t)blockIdx.y : (int32_t)blockIdx.y * 8 + warp;
+    if (row >= it.nrows) return;
+    const int32_t pieces = (int32_t)((begin + it.n - 1) / span - w) + 1;
     // piece i is walker w + i's: its second slot where it begins the pair (i = 0), else its first
-    auto slot = [&](int i) { return 2 * (int64_t)(w + i) + (i == 0 ? 1 : 0); };
-    for (int32_t row = blockIdx.y; row < it.nrows; row += gridDim.y) {
-        float m = -INFINITY;
-        bool bad = false;
-        for (int i = lane; i < pieces; i += 32) {
-            const float2 v = P.part_ml[slot(i) * ROWS + row];
-            m = fmaxf(m, v.x);
-            bad |= isnan(v.y);
+    auto slot = [&](int i) { return (2 * (w + i) + (i == 0 ? 1 : 0)) * ROWS + row; };
+    griddep_wait();
+    float m = -INFINITY, l = 0.0f;
+    for (int i = lane; i < pieces; i += 32) m = fmaxf(m, P.part_ml[slot(i)].x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    for (int i = lane; i < pieces; i += 32) {      // a piece in which the row saw nothing has sum 0
+        const float2 v = P.part_ml[slot(i)];
+        l += v.y == 0.0f ? 0.0f : v.y * exp2f(v.x - m);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    float a[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[e] = 0.0f;
+    for (int i0 = PAIRS ? warp : 0; i0 < pieces; i0 += U * (PAIRS ? 8 : 1)) {
+        float f[U], v[U][E];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int i = i0 + k * (PAIRS ? 8 : 1);
+            if (i < pieces) {
+                const float2 ml = P.part_ml[slot(i)];
+                f[k] = ml.y == 0.0f ? 0.0f : ml.y * exp2f(ml.x - m) * inv;
+                const float *src = P.part + slot(i) * D + lane * E;
+                if constexpr (E == 4) {
+                    const float4 t = *reinterpret_cast<const float4 *>(src);
+                    v[k][0] = t.x; v[k][1] = t.y; v[k][2] = t.z; v[k][3] = t.w;
+                } else {
+                    const float2 t = *reinterpret_cast<const float2 *>(src);
+                    v[k][0] = t.x; v[k][1] = t.y;
+                }
+            }
         }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        bad = __any_sync(0xffffffffu, bad);
-        // every warp sums all weights (they are few) and its share of the outputs
-        float l = 0.0f;
-        for (int i = lane; i < pieces; i += 32) {
-            const float2 v = P.part_ml[slot(i) * ROWS + row];
-            l += v.y == 0.0f ? 0.0f : v.y * exp2f(v.x - m);
-        }
+        for (int k = 0; k < U; ++k)
+            if (i0 + k * (PAIRS ? 8 : 1) < pieces)
 #pragma unroll
-        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        float a[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) a[e] = 0.0f;
-#pragma unroll 4
-        for (int i = warp; i < pieces; i += WARPS) {
-            const float2 v = P.part_ml[slot(i) * ROWS + row];
-            const float f = v.y == 0.0f ? 0.0f : v.y * exp2f(v.x - m) * inv;
-            const float *src = P.part + (slot(i) * ROWS + row) * D + lane * E;
-#pragma unroll
-            for (int e = 0; e < E; ++e) a[e] = fmaf(f, src[e], a[e]);
-        }
+                for (int e = 0; e < E; ++e) a[e] = fmaf(f[k], v[k][e], a[e]);
+    }
+    const int32_t r = it.row0 + row, tok = it.tok0 + r / P.kv.group, hq = head * P.kv.group + r % P.kv.group;
+    if (PAIRS) {
 #pragma unroll
         for (int e = 0; e < E; ++e) acc_s[warp][lane * E + e] = a[e];
         __syncthreads();
-        const int32_t r = it.row0 + row, tok = it.tok0 + r / P.kv.group, hq = head * P.kv.group + r % P.kv.group;
-        for (int d = threadIdx.x; d < D; d += 256) {
-            float s = 0.0f;
+        if (warp) return;
 #pragma unroll
-            for (int k = 0; k < WARPS; ++k) s += acc_s[k][d];
-            P.out[tok * P.ldo + (int64_t)hq * D + d] = __float2bfloat16_rn(bad ? __int_as_float(0x7fc00000) : s);
-        }
-        if (P.lse && threadIdx.x == 0)
-            P.lse[(int64_t)tok * P.kv.hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
-        __syncthreads();
+        for (int e = 0; e < E; ++e) a[e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) a[e] += acc_s[PAIRS ? k : 0][lane * E + e];
     }
+    // (a row whose sum is no number has inv = NaN, and so has every column)
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[e] = isnan(l) ? l : a[e];
+    __nv_bfloat162 h[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) h[e] = __floats2bfloat162_rn(a[2 * e], a[2 * e + 1]);
+    __nv_bfloat16 *dst = P.out + tok * P.ldo + (int64_t)hq * D + lane * E;
+    if constexpr (E == 4) *reinterpret_cast<uint2 *>(dst) = *reinterpret_cast<const uint2 *>(h);
+    else *reinterpret_cast<uint32_t *>(dst) = *reinterpret_cast<const uint32_t *>(h);
+    if (P.lse && lane == 0) P.lse[(int64_t)tok * P.kv.hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718f;
 }
 
 }  // namespace lora

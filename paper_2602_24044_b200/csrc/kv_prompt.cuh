@@ -295,6 +295,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
     __syncthreads();
     tcp::fence_after();
     const uint32_t tmem = *tmem_slot;
+    griddep_launch_dependents();
     // a wait gives up after a limit, or when another warp has
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
         for (uint32_t i = 0; i < WAIT_POLLS; ++i) {

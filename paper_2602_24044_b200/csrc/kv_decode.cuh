@@ -7,9 +7,11 @@
 // so a code is widened to c - 8 (exact in bf16 and fp16) and never multiplied by its scale: the scale
 // enters once per score and once per probability, and the low values of the values add one number per row.
 //
-// What bounds it: every key costs head_dim + 8 bytes and each of its codes about 1.4 instructions of
-// widening, whatever the number of query heads, so the memory and the instruction issue are close to
-// each other (about 0.7 of the issue slots at full memory speed).  Hence:
+// What bounds it: every key costs head_dim + 8 bytes, and each of its codes has to be widened for the
+// tensor cores whatever the number of query heads is; 1.2 instructions a code (to c - 8 in bf16 and fp16)
+// were 983 a chunk and a full integer pipe, 209 us where the bytes need 97.  Hence:
+//   - a nibble masked in place IS an fp16 number (a subnormal one, c 2^-24 or c 2^-20): two thirds of an
+//     instruction a code, and the powers of two are put on the queries and taken from the outputs;
 //   - a warp works alone: its own ring of chunks (32 keys, two cells) filled by bulk copies, its own
 //     maximum and sums; no block barrier anywhere;
 //   - the matrix instructions take the keys as their 16 rows and up to eight query rows as their 8
@@ -23,6 +25,8 @@
 // (11 bits, where bf16 would add as much error as the output's own rounding has); its exponent range is
 // kept by a common power of two of the value rows seen so far, raised like the maximum.
 #pragma once
+
+#include <type_traits>
 
 #include "fused_ptx.cuh"
 #include "kv_common.cuh"
@@ -64,21 +68,15 @@ __device__ __forceinline__ float exp2_approx(float x) {
 }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 __device__ __forceinline__ void mma16816_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
         "{%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// nibbles at bits 0..3 and 16..19 -> two numbers c - 8.  bf16: 0x4300 | c is 128 + c.
-__device__ __forceinline__ uint32_t widen_bf16(uint32_t w) {
-    uint32_t v = (w & 0x000f000fu) | 0x43004300u, r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x43084308u));
-    return r;
 }
 // fp16: 0x6400 | c is 1024 + c; the nibble above it, left in place, is 1024 + 16 c.
 __device__ __forceinline__ uint32_t widen_f16_lo(uint32_t w) {
@@ -91,23 +89,31 @@ __device__ __forceinline__ uint32_t widen_f16_hi(uint32_t w) {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x2c002c00u), "r"(0xd480d480u));   // v / 16 - 72
     return r;
 }
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Loads from shared memory by address.  They are ordered against waits and barriers (both clobber memory)
+// and may move freely otherwise.
+__device__ __forceinline__ const void *shared_at(uint32_t addr) {
+    return __cvta_shared_to_generic(addr);
+}
 __device__ __forceinline__ uint32_t lds_u32(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
+    return *reinterpret_cast<const uint32_t *>(shared_at(addr));
 }
 __device__ __forceinline__ void lds_v2(uint32_t addr, uint32_t (&v)[2]) {
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(addr));
+    const uint2 u = *reinterpret_cast<const uint2 *>(shared_at(addr));
+    v[0] = u.x; v[1] = u.y;
 }
 __device__ __forceinline__ void lds_v4(uint32_t addr, uint32_t (&v)[4]) {
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                 : "r"(addr));
+    const uint4 u = *reinterpret_cast<const uint4 *>(shared_at(addr));
+    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
 }
 // 2^e as a float, e in -126 .. 127
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
@@ -129,6 +135,9 @@ __device__ __forceinline__ int raise_exponent(int e, uint32_t most_bits) {
     return a > e + KV_RAISE_E ? min(a, 126) : e;
 }
 constexpr int KV_NO_EXPONENT = -126;
+// Codes as fp16 without any arithmetic: a nibble at bits 0..3 of a half is the subnormal number c 2^-24,
+// at bits 4..7 it is c 2^-20, and the tensor cores take subnormal numbers as they are.
+constexpr uint32_t NIB_LO = 0x000f000fu, NIB_HI = 0x00f000f0u;
 
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attention_kernel(const AttnParams P) {
@@ -160,39 +169,34 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     KvItem fi = load_item(items + f_item);
     int32_t f_head = (int32_t)((s0 - hkv * fi.start) / fi.n), f_chunk = (int32_t)(s0 - hkv * fi.start - (int64_t)f_head * fi.n);
     int64_t f_pos = s0;
-    int32_t pages = -1, pages_at = -1;       // lane i: the page of cell pages_at + i of the cursor's request
-    int32_t pages_item = -1;
-    uint32_t issued = 0;
+    // Lane i holds cell pages_at + i of the cursor's request: the address of its first head (or none), and
+    // brings that cell itself when its chunk's turn comes.
+    const unsigned char *cell_at = nullptr;
+    uint32_t pages_there = 0;                // bit i: lane i has one
+    int32_t pages_at = 0, pages_item = -1;
+    int f_s = 0;                             // the stage of the next request
     auto request = [&]() {
         if (f_pos >= s1) return;
-        const int s = issued % S;
-        const int32_t key = fi.k_lo + f_chunk * KV_DEC_CHUNK, cell = key / KV_CELL;
-        const int32_t end = fi.lim0 + (fi.row0 + fi.nrows - 1) / group;      // keys below this are there
-        if (pages_item != f_item || cell < pages_at || cell + 2 > pages_at + 32) {
-            pages_at = cell;
+        int32_t idx = fi.k_lo / KV_CELL + 2 * f_chunk - pages_at;
+        if (pages_item != f_item || (uint32_t)idx >= 32u) {
+            pages_at += idx;
             pages_item = f_item;
-            const int32_t k = (cell + lane) * KV_CELL;
-            pages = -1;
-            if (k < end) {
-                pages = __ldg(P.block_table + fi.req * P.ld_table + (k >> P.kv.page_shift));
-                if (pages < 0 || pages >= P.kv.num_pages) pages = -1;
-            }
+            idx = 0;
+            const int32_t k = (pages_at + lane) * KV_CELL, end = fi.lim0 + (fi.row0 + fi.nrows - 1) / group;
+            int32_t page = -1;
+            if (k < end) page = __ldg(P.block_table + fi.req * P.ld_table + (k >> P.kv.page_shift));
+            if (page >= P.kv.num_pages) page = -1;
+            pages_there = __ballot_sync(0xffffffffu, page >= 0);
+            cell_at = kv_cell(P.kv, max(page, 0), 0, k & (P.kv.page_size - 1), C::CELL);
         }
-        const int32_t p0 = __shfl_sync(0xffffffffu, pages, cell - pages_at);
-        const int32_t p1 = __shfl_sync(0xffffffffu, pages, cell + 1 - pages_at);
+        const uint32_t there = (pages_there >> idx) & 3u;
         if (lane == 0) {
-            unsigned char *dst = ring + s * C::STAGE;
-            flags[s] = (p0 >= 0 ? 1u : 0u) | (p1 >= 0 ? 2u : 0u);
-            mbar_expect_tx(&full[s], ((p0 >= 0) + (p1 >= 0)) * C::CELL);
-            const int32_t off = key & (P.kv.page_size - 1);
-            if (P.kv.page_size > KV_CELL) {      // both cells lie in one page
-                if (p0 >= 0) bulk_g2s(dst, kv_cell(P.kv, p0, f_head, off, C::CELL), (1 + (p1 >= 0)) * C::CELL, &full[s]);
-            } else {
-                if (p0 >= 0) bulk_g2s(dst, kv_cell(P.kv, p0, f_head, 0, C::CELL), C::CELL, &full[s]);
-                if (p1 >= 0) bulk_g2s(dst + C::CELL, kv_cell(P.kv, p1, f_head, 0, C::CELL), C::CELL, &full[s]);
-            }
+            flags[f_s] = there;
+            mbar_expect_tx(&full[f_s], (there == 3u ? 2 : there ? 1 : 0) * C::CELL);
         }
-        ++issued;
+        if ((lane >> 1) == (idx >> 1) && ((pages_there >> lane) & 1u))
+            bulk_g2s(ring + f_s * C::STAGE + (lane & 1) * C::CELL, cell_at + f_head * P.kv.head_bytes, C::CELL, &full[f_s]);
+        if (++f_s == S) f_s = 0;
         ++f_pos;
         if (++f_chunk == fi.n) {
             f_chunk = 0;
@@ -211,18 +215,18 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     KvItem it = load_item(items + it_i);
     int32_t head = (int32_t)((s0 - hkv * it.start) / it.n), chunk = (int32_t)(s0 - hkv * it.start - (int64_t)head * it.n);
     int64_t pos = s0;
-    uint32_t done = 0;
+    int stage = 0;
+    uint32_t phase = 0;
     while (pos < s1) {
         // one (item, head): its chunks from `chunk` to the end of the item or of the span
         const int32_t c0 = chunk, c1 = (int32_t)min((int64_t)it.n, chunk + (s1 - pos));
         uint32_t qf[NT][4 * KW];
-        float qs[NT][2];
-        int32_t lim[NT][2];
-        int32_t lim_min = 0x7fffffff, lim_max = -0x7fffffff;
+        float qs[NT][2], qx[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int32_t row = n * 8 + g;
             float sum = 0.0f;
+            uint32_t most = 0;
             if (row < it.nrows) {
                 const int32_t r = it.row0 + row;
                 const uint4 *src = reinterpret_cast<const uint4 *>(
@@ -233,42 +237,70 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                     qf[n][4 * i] = u.x; qf[n][4 * i + 1] = u.y; qf[n][4 * i + 2] = u.z; qf[n][4 * i + 3] = u.w;
                 }
 #pragma unroll
-                for (int i = 0; i < 4 * KW; ++i)
+                for (int i = 0; i < 4 * KW; ++i) {
                     sum += __uint_as_float(qf[n][i] << 16) + __uint_as_float(qf[n][i] & 0xffff0000u);
+                    most = max(most, max((qf[n][i] << 16) & 0x7fff0000u, qf[n][i] & 0x7fff0000u));
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < 4 * KW; ++i) qf[n][i] = 0u;
             }
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            // the row as fp16, divided by a power of two that brings it just below 2^15 (then 8 bits are exact
+            // 30 powers of two down); the columns that meet a high nibble 16 times smaller.  A negative scale
+            // turns the queries.
+            const int a = min(max((int)(most >> 23) - 126, -100), 110);
+            const float unit = copysignf(pow2(15 - a), P.scale2);
+            sum = copysignf(pow2(-9 - a), P.scale2) * sum;
+#pragma unroll
+            for (int i = 0; i < 4 * KW; ++i) {
+                const float u = (i & 1) ? unit * 0.0625f : unit;
+                qf[n][i] = pack_f16(__uint_as_float(qf[n][i] << 16) * u, __uint_as_float(qf[n][i] & 0xffff0000u) * u);
+            }
+            const float f = fmaxf(fabsf(P.scale2) * pow2(a + 9), 1e-30f);     // never 0: masked scores stay -inf
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 qs[n][j] = __shfl_sync(0xffffffffu, sum, (2 * c + j) * 4);
-                const int32_t rr = min(n * 8 + 2 * c + j, it.nrows - 1);
-                lim[n][j] = it.lim0 + (it.row0 + rr) / group;
+                qx[n][j] = __shfl_sync(0xffffffffu, f, (2 * c + j) * 4);
             }
         }
-        lim_min = it.lim0 + it.row0 / group;
-        lim_max = it.lim0 + (it.row0 + it.nrows - 1) / group;
-        float o[NT][MT][4], m[NT][2], l[NT][2], z[NT][2];
+        const int32_t lim_min = it.lim0 + it.row0 / group;
+        const int32_t lim_max = it.lim0 + (it.row0 + it.nrows - 1) / group;
+        // o: outputs, lo nibbles times 2^-24, high ones times 2^-20; sp: sums of the rounded p s, which take the
+        // offset 8 of the codes out again.  A score x as it is held is qx x in log2; nm: -(maximum in log2) (0 while
+        // nothing was seen), so that a probability is 2^(qx x + nm); top: the x that raises the maximum
+        float o[NT][MT][4], sp[NT][4], nm[NT][2], top[NT][2], l[NT][2], z[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[n][t][i] = 0.0f;
-            m[n][0] = m[n][1] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sp[n][i] = 0.0f;
+            top[n][0] = top[n][1] = -INFINITY;
+            nm[n][0] = nm[n][1] = 0.0f;
             l[n][0] = l[n][1] = z[n][0] = z[n][1] = 0.0f;
         }
         int ve = KV_NO_EXPONENT;
-        for (chunk = c0; chunk < c1; ++chunk, ++done) {
-            const int s = done % S;
+        uint32_t most_ok = (uint32_t)(ve + KV_RAISE_E + 127) << 23;     // value rows up to this leave ve as it is
+        for (chunk = c0; chunk < c1; ++chunk) {
+            const int s = stage;
             request();       // refills the stage that was finished in the previous round
-            const bool ok = mbar_wait(&full[s], (done / S) & 1u);
-            if (!__all_sync(0xffffffffu, ok)) {      // give up: nothing more is stored
-                if (lane == 0) {
-                    atomicAdd(&P.kv.status[STATUS_TIMEOUTS], 1);
-                    for (uint32_t i = done + 1; i < issued; ++i) mbar_wait(&full[i % S], (i / S) & 1u);
+            const bool ok = mbar_wait(&full[s], phase);
+            if (++stage == S) {
+                stage = 0;
+                phase ^= 1u;
+            }
+            if (!__all_sync(0xffffffffu, ok)) {
+                // give up: nothing more is stored; copies on their way have to land first
+                if (lane == 0) atomicAdd(&P.kv.status[STATUS_TIMEOUTS], 1);
+                for (int i = 0; i < S - 1; ++i) {
+                    mbar_wait(&full[stage], phase);
+                    if (++stage == S) { stage = 0; phase ^= 1u; }
                 }
                 return;
             }
@@ -276,155 +308,186 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
             const int32_t key0 = it.k_lo + chunk * KV_DEC_CHUNK;
             const bool whole = valid == 3u && key0 + KV_DEC_CHUNK <= lim_min && (P.window == 0 || key0 >= lim_max - P.window);
 
-            // scores of both cells: x[n][cell][i]: i 0, 1: row pr, columns 2c, 2c+1; i 2, 3: row pr + 8
-            float x[NT][2][4];
-            float vs[2][2], vz[2][2];
-            uint32_t most = 0;
+            // (two copies of what follows: one for chunks of which every row sees every key)
+            auto work = [&](auto all) {
+                constexpr bool WHOLE = decltype(all)::value;
+                // scores of both cells: x[n][cell][i]: i 0, 1: row pr, columns 2c, 2c+1; i 2, 3: row pr + 8
+                float x[NT][2][4];
+                uint32_t vp_[2][2];      // (scale, low) of the value rows, 0 where there is none
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const uint32_t cell = base + b * C::CELL;
-                float acc[NT][4];
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t cell = base + b * C::CELL;
+                    float acc[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+                    uint32_t ka[KW], kb[KW];
+                    const uint32_t at = cell + pr * (D / 2) + c * (D / 8);
+                    if constexpr (D == 128) {
+                        lds_v4(at, ka);
+                        lds_v4(at + 8 * (D / 2), kb);
+                    } else {
+                        lds_v2(at, ka);
+                        lds_v2(at + 8 * (D / 2), kb);
+                    }
+#pragma unroll
+                    for (int i = 0; i < KW; ++i) {
+                        const uint32_t ah = ka[i] >> 8, bh = kb[i] >> 8;
+                        const uint32_t a0[4] = {ka[i] & NIB_LO, kb[i] & NIB_LO, ka[i] & NIB_HI, kb[i] & NIB_HI};
+                        const uint32_t a1[4] = {ah & NIB_LO, bh & NIB_LO, ah & NIB_HI, bh & NIB_HI};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma16816_f16(acc[n], a0, qf[n][4 * i], qf[n][4 * i + 1]);
+                            mma16816_f16(acc[n], a1, qf[n][4 * i + 2], qf[n][4 * i + 3]);
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t par = cell + kv_cell_params(D) + (pr + 8 * r) * 4;
+                        const uint32_t kp = lds_u32(par), vp = lds_u32(par + KV_CELL * 4);
+                        const float ks = __uint_as_float(kp << 16), kl = __uint_as_float(kp & 0xffff0000u);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            x[n][b][2 * r] = fmaf(acc[n][2 * r], ks, qs[n][0] * kl);
+                            x[n][b][2 * r + 1] = fmaf(acc[n][2 * r + 1], ks, qs[n][1] * kl);
+                        }
+                        vp_[b][r] = vp;
+                        if (!WHOLE && !(((valid >> b) & 1u) && key0 + b * KV_CELL + pr + 8 * r < lim_max)) vp_[b][r] = 0;
+                    }
+                }
+                // magnitude of the value rows (bf16 bits of scale and |low|), for the common exponent
+                uint32_t most;
+                {
+                    const uint32_t h = max_u16x2(max_u16x2(vp_[0][0] & 0x7fff7fffu, vp_[0][1] & 0x7fff7fffu),
+                                                 max_u16x2(vp_[1][0] & 0x7fff7fffu, vp_[1][1] & 0x7fff7fffu));
+                    most = max(h << 16, h & 0xffff0000u);
+                }
+                if (!WHOLE) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int32_t hi = it.lim0 + (it.row0 + min(n * 8 + 2 * c + j, it.nrows - 1)) / group - key0;
+                            const int32_t lo = P.window > 0 ? hi - P.window : 0;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int32_t k = (i >> 1) * KV_CELL + pr + 8 * (i & 1);
+                                const bool seen = ((valid >> (i >> 1)) & 1u) && k < hi && k >= lo;
+                                if (!seen) x[n][i >> 1][2 * (i & 1) + j] = -INFINITY;
+                            }
+                        }
+                }
+                // maximum and exponent: raised when a score or a value row passes them by the margin
+                bool up = most > most_ok;
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
-                uint32_t ka[KW], kb[KW];
-                const uint32_t at = cell + pr * (D / 2) + c * (D / 8);
-                if constexpr (D == 128) {
-                    lds_v4(at, ka);
-                    lds_v4(at + 8 * (D / 2), kb);
-                } else {
-                    lds_v2(at, ka);
-                    lds_v2(at + 8 * (D / 2), kb);
-                }
-#pragma unroll
-                for (int i = 0; i < KW; ++i)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint32_t a[4] = {widen_bf16(ka[i] >> (8 * j)), widen_bf16(kb[i] >> (8 * j)),
-                                               widen_bf16(ka[i] >> (8 * j + 4)), widen_bf16(kb[i] >> (8 * j + 4))};
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma16816(acc[n], a, qf[n][4 * i + 2 * j], qf[n][4 * i + 2 * j + 1]);
+                        const float mx = fmaxf(fmaxf(x[n][0][j], x[n][0][2 + j]), fmaxf(x[n][1][j], x[n][1][2 + j]));
+                        up |= mx > top[n][j];      // (also the first time)
                     }
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint32_t par = cell + kv_cell_params(D) + (pr + 8 * r) * 4;
-                    const uint32_t kp = lds_u32(par), vp = lds_u32(par + KV_CELL * 4);
-                    const float ks = __uint_as_float(kp << 16), kl = __uint_as_float(kp & 0xffff0000u);
-                    const float kz = fmaf(8.0f, ks, kl) * P.scale2, kf = ks * P.scale2;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        x[n][b][2 * r] = fmaf(acc[n][2 * r], kf, qs[n][0] * kz);
-                        x[n][b][2 * r + 1] = fmaf(acc[n][2 * r + 1], kf, qs[n][1] * kz);
-                    }
-                    vs[b][r] = __uint_as_float(vp << 16);
-                    const float vl = __uint_as_float(vp & 0xffff0000u);
-                    vz[b][r] = fmaf(8.0f, vs[b][r], vl);
-                    // magnitude of the value row, for the common exponent (rows that do not count: none)
-                    const uint32_t mag = max(vp << 16, vp & 0x7fff0000u);
-                    const int32_t key = key0 + b * KV_CELL + pr + 8 * r;
-                    const bool seen = whole || (((valid >> b) & 1u) && key < lim_max);
-                    if (seen && mag < 0x7f800000u) most = max(most, mag);
-                    if (!seen) vs[b][r] = vz[b][r] = 0.0f;
-                }
-            }
-            if (!whole) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                if (__any_sync(0xffffffffu, up)) {
+                    // rows that are no numbers do not count (their outputs are none either)
+                    if (most >= 0x7f800000u) {
+                        most = 0;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int32_t key = key0 + b * KV_CELL + pr + 8 * (i >> 1), lm = lim[n][i & 1];
-                            const bool seen = ((valid >> b) & 1u) && key < lm && (P.window == 0 || key >= lm - P.window);
-                            if (!seen) x[n][b][i] = -INFINITY;
-                        }
-            }
-            // maximum and exponent: raised when a score or a value row passes them by the margin
-            bool up = false;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float mx = fmaxf(fmaxf(x[n][0][j], x[n][0][2 + j]), fmaxf(x[n][1][j], x[n][1][2 + j]));
-                    up |= mx > m[n][j] + KV_RAISE;      // (also the first time: m is -inf)
-                }
-            const int ve_lane = raise_exponent(ve, most);
-            up |= ve_lane != ve;
-            if (__any_sync(0xffffffffu, up)) {
-                const int ve_new = raise_exponent(ve, __reduce_max_sync(0xffffffffu, most));
-                const float fe = pow2(max(ve - ve_new, -126));
-                ve = ve_new;
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float mx = fmaxf(fmaxf(x[n][0][j], x[n][0][2 + j]), fmaxf(x[n][1][j], x[n][1][2 + j]));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        const float mn = mx > m[n][j] + KV_RAISE ? mx : m[n][j];
-                        const float f = mn == m[n][j] ? 1.0f : exp2_approx(m[n][j] - mn);
-                        m[n][j] = mn;
-                        l[n][j] *= f;
-                        z[n][j] *= f * fe;
-#pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            o[n][t][j] *= f * fe;
-                            o[n][t][2 + j] *= f * fe;
+                            const uint32_t vp = vp_[i >> 1][i & 1], mag = max(vp << 16, vp & 0x7fff0000u);
+                            if (mag < 0x7f800000u) most = max(most, mag);
                         }
                     }
-            }
-            // probabilities, and the second product
-            const float unit = pow2(-ve);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const uint32_t cell = base + b * C::CELL + KV_CELL * (D / 2);
-                uint32_t pb[NT][2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float fs = vs[b][r] * unit, fz = vz[b][r] * unit;
+                    const int ve_new = raise_exponent(ve, __reduce_max_sync(0xffffffffu, most));
+                    const float fe = pow2(max(ve - ve_new, -126));
+                    most_ok = (uint32_t)(ve_new + KV_RAISE_E + 127) << 23;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        float p0 = exp2_approx(x[n][b][2 * r] - m[n][0]), p1 = exp2_approx(x[n][b][2 * r + 1] - m[n][1]);
-                        float q0 = p0 * fs, q1 = p1 * fs, z0 = p0 * fz, z1 = p1 * fz;
-                        if (!whole) {    // a row that nothing counts in has no maximum; a row's NaN counts only where it is seen
-                            const bool a0 = x[n][b][2 * r] == -INFINITY, a1 = x[n][b][2 * r + 1] == -INFINITY;
-                            p0 = a0 ? 0.0f : p0; q0 = a0 ? 0.0f : q0; z0 = a0 ? 0.0f : z0;
-                            p1 = a1 ? 0.0f : p1; q1 = a1 ? 0.0f : q1; z1 = a1 ? 0.0f : z1;
+                        float fj[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float mx = fmaxf(fmaxf(x[n][0][j], x[n][0][2 + j]), fmaxf(x[n][1][j], x[n][1][2 + j]));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                            float f = 1.0f;
+                            if (mx > top[n][j]) {
+                                const float now = -mx * qx[n][j];
+                                f = top[n][j] == -INFINITY ? 0.0f : exp2_approx(now - nm[n][j]);
+                                nm[n][j] = now;
+                                top[n][j] = mx + KV_RAISE / qx[n][j];
+                            }
+                            fj[j] = f * fe;
+                            l[n][j] *= f;
+                            z[n][j] *= fj[j];
                         }
-                        l[n][0] += p0;
-                        l[n][1] += p1;
-                        z[n][0] += z0;
-                        z[n][1] += z1;
-                        pb[n][r] = movmatrix_trans(pack_f16(q0, q1));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sp[n][i] *= fj[i & 1];
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[n][t][i] *= fj[i & 1];
                     }
+                    ve = ve_new;
                 }
-                uint32_t v[4][D / 64];     // rows c, c + 4, c + 8, c + 12 of the cell: matrix columns 2c, 2c+1, 2c+8, 2c+9
+                // probabilities, and the second product
+                const float unit = pow2(-ve);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t at = cell + (c + 4 * r) * (D / 2) + g * (D / 16);
-                    if constexpr (D == 128) lds_v2(at, v[r]);
-                    else v[r][0] = lds_u32(at);
-                }
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t cell = base + b * C::CELL + KV_CELL * (D / 2);
+                    uint32_t pb[NT][2];
+                    float vs[2], vz[2];
 #pragma unroll
-                for (int u = 0; u < D / 64; ++u)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t sel = j | ((4 + j) << 8);     // byte j of both words, one in each half
-                        const uint32_t lo = __byte_perm(v[0][u], v[1][u], sel), hi = __byte_perm(v[2][u], v[3][u], sel);
-                        const uint32_t a[4] = {widen_f16_lo(lo), widen_f16_hi(lo), widen_f16_lo(hi), widen_f16_hi(hi)};
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) mma16816_f16(o[n][u * 4 + j], a, pb[n][0], pb[n][1]);
+                    for (int r = 0; r < 2; ++r) {
+                        vs[r] = __uint_as_float(vp_[b][r] << 16) * unit;
+                        vz[r] = fmaf(8.0f, vs[r], __uint_as_float(vp_[b][r] & 0xffff0000u) * unit);
                     }
-            }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float p0 = exp2_approx(fmaf(x[n][b][2 * r], qx[n][0], nm[n][0]));
+                            const float p1 = exp2_approx(fmaf(x[n][b][2 * r + 1], qx[n][1], nm[n][1]));
+                            float q0 = p0 * vs[r], q1 = p1 * vs[r], z0 = p0 * vz[r], z1 = p1 * vz[r];
+                            if (!WHOLE) {     // a value row's NaN counts only where it is seen
+                                const bool h0 = x[n][b][2 * r] == -INFINITY, h1 = x[n][b][2 * r + 1] == -INFINITY;
+                                q0 = h0 ? 0.0f : q0; z0 = h0 ? 0.0f : z0;
+                                q1 = h1 ? 0.0f : q1; z1 = h1 ? 0.0f : z1;
+                            }
+                            l[n][0] += p0;
+                            l[n][1] += p1;
+                            z[n][0] += z0;
+                            z[n][1] += z1;
+                            pb[n][r] = movmatrix_trans(pack_f16(q0, q1));
+                        }
+                        const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
+                        mma16816_f16(sp[n], ones, pb[n][0], pb[n][1]);
+                    }
+                    uint32_t v[4][D / 64];     // rows c, c + 4, c + 8, c + 12 of the cell: matrix columns 2c, 2c+1, 2c+8, 2c+9
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t at = cell + (c + 4 * r) * (D / 2) + g * (D / 16);
+                        if constexpr (D == 128) lds_v2(at, v[r]);
+                        else v[r][0] = lds_u32(at);
+                    }
+#pragma unroll
+                    for (int u = 0; u < D / 64; ++u)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t sel = j | ((4 + j) << 8);     // byte j of both words, one in each half
+                            const uint32_t lo = __byte_perm(v[0][u], v[1][u], sel), hi = __byte_perm(v[2][u], v[3][u], sel);
+                            const uint32_t a[4] = {lo & NIB_LO, lo & NIB_HI, hi & NIB_LO, hi & NIB_HI};
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) mma16816_f16(o[n][u * 4 + j], a, pb[n][0], pb[n][1]);
+                        }
+                }
+            };
+            if (whole) work(std::true_type{});
+            else work(std::false_type{});
             __syncwarp();     // every lane has read the stage: it may be requested again
         }
         // ---- this (item, head) is over, or the span is -----------------------------------------
         const bool complete = c0 == 0 && c1 == it.n;
         const int64_t slot = 2 * (int64_t)w + (c0 == 0 ? 1 : 0);
-        const float back = pow2(ve);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -437,14 +500,15 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                 }
                 const int32_t row = n * 8 + 2 * c + j;
                 if (row >= it.nrows) continue;
-                const float inv = m[n][j] == -INFINITY && ls == 0.0f ? 0.0f : 1.0f / ls;
+                const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+                const float off = zs - 8.0f * sp[n][j], ml = -nm[n][j], back = pow2(ve);
                 // a lane's columns are g D/8 .. g D/8 + D/8 - 1, in the order of the codes' nibbles
                 float f[D / 8];
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
                     const int u = t >> 2, jj = t & 3;
-                    f[u * 8 + (jj < 2 ? 4 * jj : 4 * (jj - 2) + 1)] = (o[n][t][j] + zs) * inv * back;
-                    f[u * 8 + (jj < 2 ? 4 * jj + 2 : 4 * (jj - 2) + 3)] = (o[n][t][2 + j] + zs) * inv * back;
+                    f[u * 8 + (jj < 2 ? 4 * jj : 4 * (jj - 2) + 1)] = fmaf(o[n][t][j], 16777216.0f, off) * inv * back;
+                    f[u * 8 + (jj < 2 ? 4 * jj + 2 : 4 * (jj - 2) + 3)] = fmaf(o[n][t][2 + j], 1048576.0f, off) * inv * back;
                 }
                 const int32_t r = it.row0 + row, tok = it.tok0 + r / group, hq = head * group + r % group;
                 if (complete) {
@@ -458,12 +522,12 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
 #pragma unroll
                     for (int i = 0; i < D / 64; ++i) dst[i] = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
                     if (P.lse && g == 0)
-                        P.lse[(int64_t)tok * P.kv.hq + hq] = inv == 0.0f ? -INFINITY : (m[n][j] + log2f(ls)) * 0.69314718f;
+                        P.lse[(int64_t)tok * P.kv.hq + hq] = inv == 0.0f ? -INFINITY : (ml + log2f(ls)) * 0.69314718f;
                 } else {
                     float4 *dst = reinterpret_cast<float4 *>(P.part + (slot * ROWS + row) * D + g * (D / 8));
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) dst[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-                    if (g == 0) P.part_ml[slot * ROWS + row] = make_float2(m[n][j], ls);
+                    if (g == 0) P.part_ml[slot * ROWS + row] = make_float2(top[n][j] == -INFINITY ? -INFINITY : ml, ls);
                 }
             }
         pos += c1 - c0;

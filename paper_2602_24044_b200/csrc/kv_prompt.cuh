@@ -47,22 +47,37 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D[tmem] (+)= A[smem] . B[smem]; A[tmem] . B[smem]
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// D[tmem] (+)= A[smem] . B[smem]; A[tmem] . B[smem].  Descriptors come as their low words (start address and
+// leading offset); the high word is the layout's.
+template <uint32_t HI>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(HI)
         : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+template <uint32_t HI>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(HI)
+        : "memory");
+}
+// one lane of the (converged) warp
+__device__ __forceinline__ bool elect() {
+    uint32_t is;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(is));
+    return is != 0;
 }
 // one arrival on the mbarrier when every product issued so far by this thread has completed
 __device__ __forceinline__ void commit(uint64_t *bar) {
@@ -112,12 +127,11 @@ __device__ __forceinline__ void st16(uint32_t addr, const uint32_t (&r)[16]) {
         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
         : "memory");
 }
-// shared-memory matrix descriptor (start, leading and stride offsets in 16-byte units; layout 2: 128-byte
-// swizzle, 0: 8 x 8 core matrices)
-__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t lead, uint32_t stride, uint32_t layout = 2) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)((lead >> 4) & 0x3FFFu) << 16 |
-           (uint64_t)((stride >> 4) & 0x3FFFu) << 32 | (uint64_t)1 << 46 | (uint64_t)layout << 61;
-}
+// Shared-memory matrix descriptors.  Low word: start address and leading offset in 16-byte units.  High
+// word: stride offset, version, layout (2: 128-byte swizzle, 0: 8 x 8 core matrices).
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lead) { return ((addr & 0x3FFFFu) >> 4) | (lead >> 4) << 16; }
+constexpr uint32_t desc_hi(uint32_t stride, uint32_t layout) { return (stride >> 4) | 1u << 14 | layout << 29; }
+constexpr uint32_t HI_SWIZZLED = desc_hi(1024, 2), HI_CORES = desc_hi(128, 0);
 // fp32 accumulator; a, b: 0 = fp16, 1 = bf16; b_n: B's rows run along N
 __host__ __device__ constexpr uint32_t instr(uint32_t type, uint32_t N, uint32_t b_n) {
     return (1u << 4) | (type << 7) | (type << 10) | (b_n << 16) | ((N >> 3) << 17) | ((128u >> 4) << 24);
@@ -627,73 +641,82 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
     } else {
         if (warp == 12) {
             // ======================= matrix products ===============================================
-            if (lane == 0) {
-                constexpr uint32_t QK = tcp::instr(0, 128, 0), PV = tcp::instr(0, D, 1);
-                const uint32_t q_at = smem_u32(smem), kv_at = q_at + C::OFF_KV;
-                bool ok = true;
-                auto scores = [&](int t, uint32_t u) {
-                    const uint32_t qa = q_at + t * C::TILE, ka = kv_at + (u % PK_TILES) * C::TILE;
+            // The whole warp follows the same path (so that descriptors live in uniform registers); one
+            // elected lane issues.
+            constexpr uint32_t QK = tcp::instr(0, 128, 0), PV = tcp::instr(0, D, 1);
+            const uint32_t base = smem_u32(smem);
+            const uint32_t q_lo = tcp::desc_lo(base, 16), kv_lo = tcp::desc_lo(base + C::OFF_KV, 16);
+            const uint32_t v_lo = tcp::desc_lo(base + C::OFF_KV, 16384);
+            const uint32_t qx_lo = tcp::desc_lo(base + C::OFF_QX, 2048), kx_lo = tcp::desc_lo(base + C::OFF_KX, 2048);
+            bool ok = true;
+            // scores of tile t with the keys in tile buffer b; `done`: more barriers that learn of its end
+            auto scores = [&](int t, uint32_t b, uint64_t *also, uint64_t *and_also) {
+                if (tcp::elect()) {
+                    const uint32_t qa = q_lo + t * (C::TILE >> 4), ka = kv_lo + b * (C::TILE >> 4);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
-                        tcp::mma_ss(tmem + t * 128, tcp::desc(qa + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024),
-                                    tcp::desc(ka + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024), QK, k > 0);
-                    tcp::mma_ss(tmem + t * 128, tcp::desc(q_at + C::OFF_QX + t * PK_EXTRA, 2048, 128, 0),
-                                tcp::desc(q_at + C::OFF_KX + (u % PK_TILES) * PK_EXTRA, 2048, 128, 0), QK, 1);
-                };
-                uint32_t j = 0, pair = 0;
-                int32_t left = cur.last_chunk() - cur.chunk;      // blocks left of the current (item, head)
-                bool fresh = true;                                // its first block
-                ok = wait(&kv_full[0], 0);
-                for (int t = 0; t < 2 && ok; ++t) {
-                    ok = wait(&q_ready[t], 0);
-                    tcp::fence_after();
-                    if (!ok) break;
-                    scores(t, 0);
+                        tcp::mma_ss<tcp::HI_SWIZZLED>(tmem + t * 128, qa + ((k >> 2) * 16384 + (k & 3) * 32) / 16,
+                                                      ka + ((k >> 2) * 16384 + (k & 3) * 32) / 16, QK, k > 0);
+                    tcp::mma_ss<tcp::HI_CORES>(tmem + t * 128, qx_lo + t * (PK_EXTRA >> 4), kx_lo + b * (PK_EXTRA >> 4), QK, 1);
                     tcp::commit(&s_full[t]);
-                    if (left == 1) tcp::commit(&q_free[t]);
+                    if (also) tcp::commit(also);
+                    if (and_also) tcp::commit(and_also);
                 }
-                if (ok) tcp::commit(&kv_empty[0]);
-                while (ok) {
-                    const uint32_t uv = 2 * j + 1, uk = 2 * j + 2;
-                    const bool last = left == 1;
-                    if (last) cur.next_pair(cur.last_chunk() - cur.chunk);
-                    const bool another = !last || cur.more();     // one more block follows
-                    const int32_t next_left = last ? (another ? cur.last_chunk() - cur.chunk : 0) : left - 1;
-                    ok = wait(&kv_full[uv % PK_TILES], (uv / PK_TILES) & 1u);
-                    for (int t = 0; t < 2 && ok; ++t) {
-                        ok = wait(&p_ready[t], j & 1u);
-                        if (!ok) break;
-                        tcp::fence_after();
-                        const uint32_t va = kv_at + (uv % PK_TILES) * C::TILE;
+                __syncwarp();
+            };
+            uint32_t j = 0, pair = 0, b = 0, b_phase = 0;      // b: the tile buffer of the block's values
+            int32_t left = cur.last_chunk() - cur.chunk;      // blocks left of the current (item, head)
+            bool fresh = true;                                // its first block
+            ok = __all_sync(0xffffffffu, wait(&kv_full[0], 0));
+            for (int t = 0; t < 2 && ok; ++t) {
+                ok = __all_sync(0xffffffffu, wait(&q_ready[t], 0));
+                tcp::fence_after();
+                if (!ok) break;
+                scores(t, 0, left == 1 ? &q_free[t] : nullptr, t == 1 ? &kv_empty[0] : nullptr);
+            }
+            b = 1;
+            while (ok) {
+                const bool last = left == 1;
+                if (last) cur.next_pair(cur.last_chunk() - cur.chunk);
+                const bool another = !last || cur.more();     // one more block follows
+                const int32_t next_left = last ? (another ? cur.last_chunk() - cur.chunk : 0) : left - 1;
+                const uint32_t kb = b + 1 == PK_TILES ? 0 : b + 1, kb_phase = b + 1 == PK_TILES ? b_phase ^ 1u : b_phase;
+                ok = __all_sync(0xffffffffu, wait(&kv_full[b], b_phase));
+                for (int t = 0; t < 2 && ok; ++t) {
+                    ok = __all_sync(0xffffffffu, wait(&p_ready[t], j & 1u));
+                    if (!ok) break;
+                    tcp::fence_after();
+                    if (tcp::elect()) {
+                        const uint32_t va = v_lo + b * (C::TILE >> 4);
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            tcp::mma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, tcp::desc(va + k * 2048, 16384, 1024), PV,
-                                        !fresh || k > 0);
+                            tcp::mma_ts<tcp::HI_SWIZZLED>(tmem + 256 + t * D, tmem + t * 128 + k * 8, va + k * 128, PV,
+                                                          (k > 0 || !fresh) ? 1u : 0u);
                         if (last) tcp::commit(&o_full[t]);
-                        if (t == 1) tcp::commit(&kv_empty[uv % PK_TILES]);
-                        if (another) {
-                            if (t == 0) ok = wait(&kv_full[uk % PK_TILES], (uk / PK_TILES) & 1u);
-                            if (ok && last) ok = wait(&q_ready[t], (pair + 1) & 1u);
-                            if (!ok) break;
-                            tcp::fence_after();
-                            scores(t, uk);
-                            tcp::commit(&s_full[t]);
-                            if (next_left == 1) tcp::commit(&q_free[t]);
-                            if (t == 1) tcp::commit(&kv_empty[uk % PK_TILES]);
-                        }
+                        if (t == 1) tcp::commit(&kv_empty[b]);
                     }
-                    if (!ok || !another) break;
-                    fresh = last;
-                    pair += last;
-                    left = next_left;
-                    ++j;
+                    __syncwarp();
+                    if (another) {
+                        if (t == 0) ok = __all_sync(0xffffffffu, wait(&kv_full[kb], kb_phase));
+                        if (ok && last) ok = __all_sync(0xffffffffu, wait(&q_ready[t], (pair + 1) & 1u));
+                        if (!ok) break;
+                        tcp::fence_after();
+                        scores(t, kb, next_left == 1 ? &q_free[t] : nullptr, t == 1 ? &kv_empty[kb] : nullptr);
+                    }
                 }
-                if (!ok) *failed = 1;
-                // nothing of this block's memory may be given back while a product is in flight
-                tcp::commit(drained);
-                mbar_wait(drained, 0);
+                if (!ok || !another) break;
+                fresh = last;
+                pair += last;
+                left = next_left;
+                ++j;
+                b = kb + 1 == PK_TILES ? 0 : kb + 1;
+                b_phase = kb + 1 == PK_TILES ? kb_phase ^ 1u : kb_phase;
             }
+            if (!ok) *failed = 1;
+            // nothing of this block's memory may be given back while a product is in flight
+            if (tcp::elect()) tcp::commit(drained);
             __syncwarp();
+            mbar_wait(drained, 0);
         } else if (warp == 13) {
             // ======================= cells from the cache ==========================================
             uint32_t j = 0;

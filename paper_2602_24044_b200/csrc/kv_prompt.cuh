@@ -588,7 +588,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 }
                 // codes: K, then V.  Four lanes share a row; those of the second pair take their two halves
                 // in the other order, so that the eight lanes of a store phase hit eight different banks
-#pragma unroll
+                // (one small loop for both: the roles' code together has to fit the instruction cache)
+#pragma unroll 1
                 for (int kv = 0; kv < 2; ++kv, ++u) {
                     const uint32_t b = u % PK_TILES, tile = smem_u32(smem) + C::OFF_KV + b * C::TILE;
                     if (u >= PK_TILES) ok = ok && wait(&kv_empty[b], (u / PK_TILES - 1) & 1u);
@@ -599,32 +600,32 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                         const uint32_t kx[4] = {pack_f16(z.h, z.l), pack_f16(z.h, z.l), pack_f16(z.t, z.h), 0u};
                         tcp::sts_v4(smem_u32(smem) + C::OFF_KX + b * PK_EXTRA + (id >> 3) * 128 + (id & 7) * 16, kx);
                     }
-#pragma unroll
+                    const float unit = kv ? v_unit : k_unit;
+#pragma unroll 1
                     for (int i = 0; i < 4; ++i) {
                         const int key = i * 32 + kr;
-                        const uint32_t cell = raw + (key >> 4) * C::CELL;
-                        const uint32_t src = cell + (kv * KV_CELL + (key & 15)) * (D / 2) + c * (D / 8);
+                        const uint32_t cell = raw + (key >> 4) * C::CELL + kv * KV_CELL * (D / 2);
+                        const uint32_t src = cell + (key & 15) * (D / 2) + c * (D / 8);
                         // a row that is not there, or whose values are no numbers, becomes zero
-                        const uint32_t par = lds_u32(cell + kv_cell_params(D) + (kv * KV_CELL + (key & 15)) * 4);
-                        float sf = __uint_as_float(par << 16), zf = fmaf(8.0f, sf, __uint_as_float(par & 0xffff0000u));
-                        bool there = ((valid >> (key >> 4)) & 1u) && key < left;
-                        if (kv == 1) there = there && max(par << 16, par & 0x7fff0000u) < 0x7f800000u;
-                        const uint32_t s2 = half2_of(there ? sf * (kv ? v_unit : k_unit) : 0.0f);
-                        const uint32_t z2 = half2_of(there ? zf * v_unit : 0.0f);
+                        const uint32_t par = lds_u32(raw + (key >> 4) * C::CELL + kv_cell_params(D) + (kv * KV_CELL + (key & 15)) * 4);
+                        uint32_t w[D / 32];
+                        if constexpr (D == 128) lds_v4(src, w);
+                        else lds_v2(src, w);
+                        const float sf = __uint_as_float(par << 16), zf = fmaf(8.0f, sf, __uint_as_float(par & 0xffff0000u));
+                        const bool there = ((valid >> (key >> 4)) & 1u) && key < left &&
+                                           (kv == 0 || max(par << 16, par & 0x7fff0000u) < 0x7f800000u);
+                        const uint32_t s2 = half2_of(there ? sf * unit : 0.0f);
+                        const uint32_t z2 = half2_of(there && kv ? zf * unit : 0.0f);      // (keys get theirs in the further columns)
+                        const uint32_t dst = tile + (c * (D / 32) >> 3) * 16384 + key * 128;
 #pragma unroll
-                        for (int h = 0; h < D / 64; ++h) {
-                            const int hh = D == 128 ? h ^ (c >> 1) : 0;      // which 8 bytes of the lane's run
-                            uint32_t w[2];
-                            lds_v2(src + hh * 8, w);
+                        for (int e = 0; e < D / 32; ++e) {
+                            // lanes 2 and 3 of a row begin with their second half
+                            const int we = D == 128 ? e ^ (c & 2) : e;
+                            const uint32_t we_w = D == 128 ? ((c & 2) ? w[e ^ 2] : w[e]) : w[e];
+                            uint32_t v[4] = {widen_f16_lo(we_w), widen_f16_hi(we_w), widen_f16_lo(we_w >> 8), widen_f16_hi(we_w >> 8)};
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int word = c * (D / 32) + hh * 2 + e;      // 8 elements: a 16-byte run of the tile's row
-                                uint32_t v[4] = {widen_f16_lo(w[e]), widen_f16_hi(w[e]), widen_f16_lo(w[e] >> 8),
-                                                 widen_f16_hi(w[e] >> 8)};
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) v[q] = kv ? fma_f16x2(v[q], s2, z2) : mul_f16x2(v[q], s2);
-                                tcp::sts_v4(tile + (word >> 3) * 16384 + key * 128 + (((word & 7) ^ (key & 7)) << 4), v);
-                            }
+                            for (int q = 0; q < 4; ++q) v[q] = fma_f16x2(v[q], s2, z2);
+                            tcp::sts_v4(dst + (((c * (D / 32) + we) & 7) ^ (key & 7)) * 16, v);
                         }
                     }
                     fence_proxy_async();     // ordinary stores, read by the matrix unit

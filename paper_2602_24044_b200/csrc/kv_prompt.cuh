@@ -120,7 +120,8 @@ __device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&r)[16]) {
         : "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void st16(uint32_t addr, const uint32_t (&r)[16]) {
+template <int N>
+__device__ __forceinline__ void st16(uint32_t addr, const uint32_t (&r)[N]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
         "%15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
@@ -392,35 +393,35 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 const int32_t key0 = cur.it.k_lo + ch * KV_PROMPT_CHUNK;
                 const bool whole = valid == 0xffu && key0 + 128 <= lim_min && key0 >= lo_max;
                 const bool any_bad = (info->bad[0] | info->bad[1] | info->bad[2] | info->bad[3]) != 0;
-                // the scores are read twice (tensor memory is fast; 128 registers of them are not there)
-                float mx = -INFINITY;
-#pragma unroll 1
-                for (int h = 0; h < 128; h += 64) {
-                    uint32_t x[64];
-                    LORA_TMEM_LD32(s_at + h, x, 0);
-                    LORA_TMEM_LD32(s_at + h + 32, x, 32);
-                    tcp::wait_ld();
+                // The scores are read twice (tensor memory is fast; 128 registers of them are not there), 32
+                // columns at a time, the next on their way while these are worked on.
+                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                uint32_t xa[32];
+                auto largest = [&](uint32_t (&x)[32], int h) {
                     if (!whole) {      // what a row does not see goes back as -inf
+                        const int32_t k = key0 + h;       // bit i is key k + i
+                        const uint32_t cells = valid >> (h >> 4);
+                        const uint32_t seen = low_bits(lim - k) & ~low_bits(lo - k) &
+                                              (((cells & 1u) ? 0xffffu : 0u) | ((cells & 2u) ? 0xffff0000u : 0u));
+                        // a value row that is no number makes the rows that see it no numbers
+                        if (any_bad && (seen & info->bad[h >> 5])) l = NAN;
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            const int32_t k = key0 + h + 32 * w;       // the word's 32 keys: bit i is key k + i
-                            const uint32_t cells = valid >> ((h >> 4) + 2 * w);
-                            const uint32_t seen = low_bits(lim - k) & ~low_bits(lo - k) &
-                                                  (((cells & 1u) ? 0xffffu : 0u) | ((cells & 2u) ? 0xffff0000u : 0u));
-                            // a value row that is no number makes the rows that see it no numbers
-                            if (any_bad && (seen & info->bad[(h >> 5) + w])) l = NAN;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[32 * w + i] = (seen >> i) & 1u ? x[32 * w + i] : 0xff800000u;
-                        }
+                        for (int i = 0; i < 32; ++i) x[i] = (seen >> i) & 1u ? x[i] : 0xff800000u;
                         tcp::st32(s_at + h, x, 0);
-                        tcp::st32(s_at + h + 32, x, 32);
                     }
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2)
-                        mx = fmaxf(mx, fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+                    for (int i = 0; i < 32; i += 2)
+                        mx4[(i >> 1) & 3] = fmaxf(fmaxf(mx4[(i >> 1) & 3], __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
+                };
+#pragma unroll 1
+                for (int h = 0; h < 128; h += 32) {
+                    LORA_TMEM_LD32(s_at + h, xa, 0);
+                    tcp::wait_ld();
+                    largest(xa, h);
                 }
                 if (!whole) tcp::wait_st();
                 else if (any_bad) l = NAN;
+                float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx = mx == -INFINITY ? mx : mx * f;
                 if (__any_sync(0xffffffffu, mx > m + KV_RAISE || ve_new != ve)) {
                     const float mn = mx > m + KV_RAISE ? mx : m;
@@ -444,27 +445,28 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 // a row that sees nothing has no maximum: its probabilities are 2^(-inf - 0)
                 const float mm = m == -INFINITY ? 0.0f : m;
                 const uint64_t f2 = tcp::pack2f(f, f), nm = tcp::pack2f(-mm, -mm);
-                uint64_t l2 = 0;
-#pragma unroll 1
-                for (int h = 0; h < 128; h += 64) {     // (probabilities h / 2 .. overwrite scores that have been read)
-                    uint32_t x[64];
-                    LORA_TMEM_LD32(s_at + h, x, 0);
-                    LORA_TMEM_LD32(s_at + h + 32, x, 32);
-                    tcp::wait_ld();
+                uint64_t l2[2] = {0, 0};
+                auto spread = [&](uint32_t (&x)[32], int h) {     // (probabilities h / 2 .. overwrite scores that have been read)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int i = 0; i < 16; ++i) {
                         float a, b;
                         tcp::unpack2f(tcp::fma2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, nm),
                                       a, b);
                         a = exp2_approx(a);
                         b = exp2_approx(b);
-                        l2 = tcp::add2(l2, tcp::pack2f(a, b));
+                        l2[i & 1] = tcp::add2(l2[i & 1], tcp::pack2f(a, b));
                         x[i] = pack_f16(a, b);
                     }
-                    tcp::st32(s_at + h / 2, x, 0);
+                    tcp::st16(s_at + h / 2, x);
+                };
+#pragma unroll 1
+                for (int h = 0; h < 128; h += 32) {
+                    LORA_TMEM_LD32(s_at + h, xa, 0);
+                    tcp::wait_ld();
+                    spread(xa, h);
                 }
                 float a, b;
-                tcp::unpack2f(l2, a, b);
+                tcp::unpack2f(tcp::add2(l2[0], l2[1]), a, b);
                 l += a + b;
                 tcp::wait_st();
                 tcp::fence_before();
@@ -654,10 +656,12 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             auto scores = [&](int t, uint32_t b, uint64_t *also, uint64_t *and_also) {
                 if (tcp::elect()) {
                     const uint32_t qa = q_lo + t * (C::TILE >> 4), ka = kv_lo + b * (C::TILE >> 4);
+                    // rolled: the code of all roles has to fit the instruction caches of an SM
+#pragma unroll 1
+                    for (int h = 0; h < D / 64; ++h)
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        tcp::mma_ss<tcp::HI_SWIZZLED>(tmem + t * 128, qa + ((k >> 2) * 16384 + (k & 3) * 32) / 16,
-                                                      ka + ((k >> 2) * 16384 + (k & 3) * 32) / 16, QK, k > 0);
+                        for (int k = 0; k < 4; ++k)
+                            tcp::mma_ss<tcp::HI_SWIZZLED>(tmem + t * 128, qa + h * 1024 + k * 2, ka + h * 1024 + k * 2, QK, (h | k) > 0);
                     tcp::mma_ss<tcp::HI_CORES>(tmem + t * 128, qx_lo + t * (PK_EXTRA >> 4), kx_lo + b * (PK_EXTRA >> 4), QK, 1);
                     tcp::commit(&s_full[t]);
                     if (also) tcp::commit(also);
@@ -669,6 +673,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             int32_t left = cur.last_chunk() - cur.chunk;      // blocks left of the current (item, head)
             bool fresh = true;                                // its first block
             ok = __all_sync(0xffffffffu, wait(&kv_full[0], 0));
+#pragma unroll 1
             for (int t = 0; t < 2 && ok; ++t) {
                 ok = __all_sync(0xffffffffu, wait(&q_ready[t], 0));
                 tcp::fence_after();
@@ -683,13 +688,14 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 const int32_t next_left = last ? (another ? cur.last_chunk() - cur.chunk : 0) : left - 1;
                 const uint32_t kb = b + 1 == PK_TILES ? 0 : b + 1, kb_phase = b + 1 == PK_TILES ? b_phase ^ 1u : b_phase;
                 ok = __all_sync(0xffffffffu, wait(&kv_full[b], b_phase));
+#pragma unroll 1
                 for (int t = 0; t < 2 && ok; ++t) {
                     ok = __all_sync(0xffffffffu, wait(&p_ready[t], j & 1u));
                     if (!ok) break;
                     tcp::fence_after();
                     if (tcp::elect()) {
                         const uint32_t va = v_lo + b * (C::TILE >> 4);
-#pragma unroll
+#pragma unroll 2
                         for (int k = 0; k < 8; ++k)
                             tcp::mma_ts<tcp::HI_SWIZZLED>(tmem + 256 + t * D, tmem + t * 128 + k * 8, va + k * 128, PV,
                                                           (k > 0 || !fresh) ? 1u : 0u);

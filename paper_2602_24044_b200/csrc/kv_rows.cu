@@ -20,7 +20,7 @@ struct RowParams {
     const int32_t *positions, *slots;
     __nv_bfloat16 *q_out, *k_out;
     int64_t ldq, ldk, ldv, ldqo, ldko;
-    int32_t T, hq, hk, num_positions, rot_dim, heads_per_warp;
+    int32_t T, hq, hk, num_positions, rot_dim;
     float eps;
     KvView kv;          // with slots
     int32_t *status;    // NULL without a cache
@@ -154,13 +154,16 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return r;
 }
 // Eight codes as a word: nibble n holds element {0,2,4,6,1,3,5,7}[n], so that (word >> 4 i) & 0x000f000f
-// is elements 2 i and 2 i + 1.
+// is elements 2 i and 2 i + 1.  A number in 0 .. 15 plus 1.5 2^23 is rounded to the nearest whole one (ties
+// to even) and has it in its low bits; the constant's own bits are taken out of the sum at the start.
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float low, float inv, bool bad) {
-    uint32_t w = 0;
+    constexpr uint32_t MAGIC = 0x4b400000u;
+    uint32_t w = 0u - (MAGIC + (MAGIC << 4) + (MAGIC << 8) + (MAGIC << 12) + (MAGIC << 16) + (MAGIC << 20) +
+                       (MAGIC << 24) + (MAGIC << 28));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float c = fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], low), inv)), 0.0f), 15.0f);
-        w |= (uint32_t)(int)c << (4 * ((i >> 1) + 4 * (i & 1)));
+        const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], low), inv), 0.0f), 15.0f);
+        w += __float_as_uint(__fadd_rn(c, 12582912.0f)) << (4 * ((i >> 1) + 4 * (i & 1)));
     }
     return bad ? 0u : w;
 }
@@ -188,21 +191,38 @@ __device__ __forceinline__ void quantise_row(const Row &x, uint32_t &wa, uint32_
     param = bad ? 0x7fc07fc0u : __float_as_uint(scale) >> 16 | (__float_as_uint(low) & 0xffff0000u);
 }
 
-// A warp takes one token and `heads_per_warp` x (32 / (D/16)) consecutive heads of its row of query, key
-// and (with a cache) value heads.  The angles are loaded once per warp.
-template <int D, int ROT, bool CACHE>
-__global__ void __launch_bounds__(256) rows_kernel(const RowParams P) {
+// A warp takes one token and NP passes of 32 / (D/16) consecutive heads each of its row of query, key and
+// (with a cache) value heads.  All its rows are requested before anything is waited for: position, angles
+// and rows one after the other were 2 us a warp with 2 KB on their way (prefill of 12936 tokens: 94 us a
+// launch, 187 with the cache; bytes alone 41 and 40).
+template <int D, int ROT, bool CACHE, int NP>
+__global__ void __launch_bounds__(128) rows_kernel(const RowParams P) {
     constexpr int LPH = D / 16, HPP = 32 / LPH;     // lanes of a head, heads of a pass
     const int lane = threadIdx.x & 31, j = lane % LPH, g = lane / LPH;
     const int heads = P.hq + P.hk + (CACHE ? P.hk : 0);
-    const int per = P.heads_per_warp * HPP;
-    const int parts = (heads + per - 1) / per;
-    const int64_t wid = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int parts = (heads + NP * HPP - 1) / (NP * HPP);
+    const int64_t wid = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const int64_t t64 = wid / parts;
     if (t64 >= P.T) return;     // whole warps
     const int32_t t = (int32_t)t64;
-    const int h0 = (int)(wid - t64 * parts) * per, h1 = min(h0 + per, heads);
+    const int h0 = (int)(wid - t64 * parts) * (NP * HPP);
 
+    uint4 raw[NP][2];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const int h = h0 + p * HPP + g;
+        if (h < heads) {
+            const __nv_bfloat16 *src = h < P.hq          ? P.q + t * P.ldq + h * D
+                                       : h < P.hq + P.hk ? P.k + t * P.ldk + (h - P.hq) * D
+                                                         : P.v + t * P.ldv + (h - P.hq - P.hk) * D;
+            raw[p][0] = *reinterpret_cast<const uint4 *>(src + 8 * j);
+            raw[p][1] = *reinterpret_cast<const uint4 *>(src + D / 2 + 8 * j);
+        } else {
+            raw[p][0] = raw[p][1] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    int32_t slot = -1;
+    if (CACHE) slot = __ldg(P.slots + t);
     const float *row = nullptr;
     Angles<ROT> A;
     bool turn = false;
@@ -210,38 +230,32 @@ __global__ void __launch_bounds__(256) rows_kernel(const RowParams P) {
         const int32_t pos = __ldg(P.positions + t);
         turn = pos >= 0 && pos < P.num_positions;
         row = P.cos_sin + (int64_t)(turn ? pos : 0) * P.rot_dim;
-        if (turn) load_angles<D, ROT>(A, row, P.rot_dim, j);
-        else if (P.status && h0 == 0 && lane == 0) atomicAdd(&P.status[STATUS_INVALID_TOKENS], 1);
+        load_angles<D, ROT>(A, row, P.rot_dim, j);
+        if (!turn && P.status && h0 == 0 && lane == 0) atomicAdd(&P.status[STATUS_INVALID_TOKENS], 1);
     }
-    int32_t slot = -1;
     if (CACHE) {
-        slot = __ldg(P.slots + t);
         const bool in = slot >= 0 && (slot >> P.kv.page_shift) < P.kv.num_pages;
         if (!in && slot != -1 && h0 == 0 && lane == 0) atomicAdd(&P.kv.status[STATUS_INVALID_TOKENS], 1);
         if (!in) slot = -1;
     }
-    for (int hb = h0; hb < h1; hb += HPP) {
-        const int h = hb + g;
-        const bool live = h < h1;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const int h = h0 + p * HPP + g;
+        const bool live = h < heads;
         // 0 query, 1 key, 2 value
         const int kind = h < P.hq ? 0 : h < P.hq + P.hk ? 1 : 2;
         const int hh = kind == 0 ? h : kind == 1 ? h - P.hq : h - P.hq - P.hk;
-        Row x;
-        if (live) {
-            const __nv_bfloat16 *src = kind == 0 ? P.q + t * P.ldq : kind == 1 ? P.k + t * P.ldk : P.v + t * P.ldv;
-            src += hh * D + 8 * j;
-            unpack8(*reinterpret_cast<const uint4 *>(src), x.a);
-            unpack8(*reinterpret_cast<const uint4 *>(src + D / 2), x.b);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x.a[i] = x.b[i] = 0.0f;
-        }
-        // lanes of one warp may hold query, key and value heads: every shuffle is executed by all of them
-        Row y = x;
-        const __nv_bfloat16 *w = kind == 0 ? P.qw : P.kw;
-        if (P.qw || P.kw) {
+        if (h0 + p * HPP >= heads) break;
+        Row y;
+        unpack8(raw[p][0], y.a);
+        unpack8(raw[p][1], y.b);
+        // lanes of one warp may hold query, key and value heads: every shuffle is executed by all of them, and
+        // what no lane needs is skipped by the whole warp
+        const __nv_bfloat16 *w = kind == 0 ? P.qw : kind == 1 ? P.kw : nullptr;
+        const bool norm = live && w;
+        if (__any_sync(0xffffffffu, norm)) {
+            const Row x = y;
             float wa[8], wb[8];
-            const bool norm = live && kind < 2 && w;
             if (norm) {
                 unpack8(__ldg(reinterpret_cast<const uint4 *>(w + 8 * j)), wa);
                 unpack8(__ldg(reinterpret_cast<const uint4 *>(w + D / 2 + 8 * j)), wb);
@@ -252,10 +266,10 @@ __global__ void __launch_bounds__(256) rows_kernel(const RowParams P) {
             norm_row<D>(y, wa, wb, P.eps);
             if (!norm) y = x;
         }
-        if (ROT != ROT_NONE && turn) {   // `turn` is the token's, the same in the whole warp
-            const Row z = y;
+        if (ROT != ROT_NONE && turn && __any_sync(0xffffffffu, kind < 2)) {   // `turn` is the token's, the same in the whole warp
+            const Row x = y;
             rotate_row<D, ROT>(y, A, row, P.rot_dim, j);
-            if (kind == 2) y = z;
+            if (kind == 2) y = x;
         }
         if (live && kind == 0) {
             __nv_bfloat16 *dst = P.q_out + t * P.ldqo + hh * D + 8 * j;
@@ -267,7 +281,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const RowParams P) {
             *reinterpret_cast<uint4 *>(dst) = pack8(y.a);
             *reinterpret_cast<uint4 *>(dst + D / 2) = pack8(y.b);
         }
-        if (CACHE && hb + HPP > P.hq) {   // some lane holds a key or a value (the same for all lanes)
+        if (CACHE && h0 + p * HPP + HPP > P.hq) {   // some lane holds a key or a value (the same for all lanes)
             uint32_t wa, wb, param;
             quantise_row<D>(y, wa, wb, param);
             if (live && kind > 0 && slot >= 0) {
@@ -394,34 +408,33 @@ static lora_status_t fill_rows(const lora_qk_args_t *a, int32_t T, bool cache, R
     return LORA_OK;
 }
 
-template <int D, int ROT, bool CACHE>
-static void launch_rows(const RowParams &P, int64_t blocks, cudaStream_t s) {
-    rows_kernel<D, ROT, CACHE><<<(unsigned)blocks, 256, 0, s>>>(P);
+template <int D, bool CACHE, int NP>
+static void launch_rows(const RowParams &P, int rot, unsigned blocks, cudaStream_t s) {
+    if (rot == ROT_NONE) rows_kernel<D, ROT_NONE, CACHE, NP><<<blocks, 128, 0, s>>>(P);
+    else if (rot == ROT_HALF) rows_kernel<D, ROT_HALF, CACHE, NP><<<blocks, 128, 0, s>>>(P);
+    else if (rot == ROT_PART) rows_kernel<D, ROT_PART, CACHE, NP><<<blocks, 128, 0, s>>>(P);
+    else rows_kernel<D, ROT_PAIRS, CACHE, NP><<<blocks, 128, 0, s>>>(P);
 }
 template <int D, bool CACHE>
-static void launch_rows_rot(const RowParams &P, int rot, int64_t blocks, cudaStream_t s) {
-    if (rot == ROT_NONE) launch_rows<D, ROT_NONE, CACHE>(P, blocks, s);
-    else if (rot == ROT_HALF) launch_rows<D, ROT_HALF, CACHE>(P, blocks, s);
-    else if (rot == ROT_PART) launch_rows<D, ROT_PART, CACHE>(P, blocks, s);
-    else launch_rows<D, ROT_PAIRS, CACHE>(P, blocks, s);
+static lora_status_t launch_rows_for(const RowParams &P, int rot, cudaStream_t s) {
+    constexpr int HPP = 512 / D;                        // heads of one pass of a warp
+    const int heads = P.hq + P.hk * (CACHE ? 2 : 1), passes = (heads + HPP - 1) / HPP;
+    // Four passes a warp once there are enough of them to fill the GPU several times over (their loads are in
+    // flight together and share the token's angles); fewer rows are spread over as many warps as possible.
+    const bool many = (int64_t)P.T * passes >= 32768 && passes >= 4;
+    const int np = many ? 4 : 1;
+    const int64_t blocks = ((int64_t)P.T * ((passes + np - 1) / np) + 3) / 4;
+    if (blocks > 0x7fffffff) return LORA_ERR_SHAPE;
+    if (many) launch_rows<D, CACHE, 4>(P, rot, (unsigned)blocks, s);
+    else launch_rows<D, CACHE, 1>(P, rot, (unsigned)blocks, s);
+    return count_launch();
 }
 
 static lora_status_t run_rows(const lora_qk_args_t *a, RowParams &P, bool cache, cudaStream_t stream) {
     const int d = a->head_dim;
     const int rot = !a->cos_sin ? ROT_NONE : a->interleaved ? ROT_PAIRS : a->rot_dim == d ? ROT_HALF : ROT_PART;
-    const int heads = P.hq + P.hk * (cache ? 2 : 1), pass = 512 / d;   // heads of one pass of a warp
-    P.heads_per_warp = 1;
-    const int parts = (heads + pass * P.heads_per_warp - 1) / (pass * P.heads_per_warp);
-    const int64_t blocks = ((int64_t)P.T * parts + 7) / 8;
-    if (blocks > 0x7fffffff) return LORA_ERR_SHAPE;
-    if (d == 64) {
-        if (cache) launch_rows_rot<64, true>(P, rot, blocks, stream);
-        else launch_rows_rot<64, false>(P, rot, blocks, stream);
-    } else {
-        if (cache) launch_rows_rot<128, true>(P, rot, blocks, stream);
-        else launch_rows_rot<128, false>(P, rot, blocks, stream);
-    }
-    return count_launch();
+    if (d == 64) return cache ? launch_rows_for<64, true>(P, rot, stream) : launch_rows_for<64, false>(P, rot, stream);
+    return cache ? launch_rows_for<128, true>(P, rot, stream) : launch_rows_for<128, false>(P, rot, stream);
 }
 
 }  // namespace lora

@@ -66,11 +66,7 @@ extern "C" {
 
 lora_status_t lora_kv_workspace_bytes(const lora_kv_t *kv, size_t *bytes) {
     if (!kv || !bytes) return LORA_ERR_INVALID_ARG;
-    size_t most = 0;
-    for (int rows = 8; rows <= 16; rows += 8) {
-        const size_t b = part_bytes(kv->dec_walkers(rows), rows, kv->d);
-        if (b > most) most = b;
-    }
+    size_t most = part_bytes(kv->dec_walkers(), kv->dec_rows(), kv->d);
     const size_t b = part_bytes(kv->pr_walkers(), KV_PROMPT_ROWS, kv->d);
     if (b > most) most = b;
     *bytes = (most + 255) / 256 * 256;
@@ -106,12 +102,12 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     P.tables = (const int32_t *)tables;
     P.block_table = block_table;
     P.ld_table = ld_table;
-    const int32_t rows = kv->dec_rows(rec->max_q);
-    P.L = kv_tables(R, T, kv->group, kv->dec_walkers(rows), kv->pr_walkers());
+    const int32_t rows = kv->dec_rows();
+    P.L = kv_tables(R, T, kv->group, kv->dec_walkers(), kv->pr_walkers());
     P.kv = kv->view(layer);
     P.window = rec->window;
     P.scale2 = scale * 1.4426950408889634f;
-    P.walkers = kv->dec_walkers(rows);
+    P.walkers = kv->dec_walkers();
     P.part = (float *)workspace;
     P.part_ml = (float2 *)(P.part + (size_t)2 * P.walkers * rows * kv->d);
     // (item, head) pairs that can be in the list: one item a request where a request's rows fit one

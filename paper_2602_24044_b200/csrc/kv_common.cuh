@@ -27,6 +27,31 @@ __device__ __forceinline__ unsigned char *kv_cell(const KvView &v, int32_t page,
     return v.cells + page * v.page_bytes + head * v.head_bytes + (int64_t)(offset / KV_CELL) * cell_bytes;
 }
 
+// Two floats at once, each rounded by itself.
+__device__ __forceinline__ uint64_t pack2f(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2f(uint64_t v, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // ---------------------------------------------------------------------------------------------
 // batch tables (int32 words): public part as documented, then the attention's work lists
 // ---------------------------------------------------------------------------------------------
@@ -125,11 +150,13 @@ struct lora_kv {
         return nullptr;
     }
     lora::KvView view(int32_t layer) const;
-    // Rows of one item of the single-token walk: 8, or 16 where a token alone has more than 8 or a
-    // request may bring several tokens.
-    int32_t dec_rows(int32_t max_q) const { return (int64_t)max_q * group <= 8 ? 8 : 16; }
+    // Rows of one item of the single-token walk: 8 (one column tile of the matrix instructions), or 16 where
+    // a token alone has more than 8 rows.  (16 for requests of several tokens would halve their reads of the
+    // cache, but the wider kernel costs every request of one token more: the single tokens of a batch of 512
+    // beside four prompt chunks 229 us against 143.)
+    int32_t dec_rows() const { return group <= 8 ? 8 : 16; }
     // Warps of the single-token kernel that are resident at once (its registers: 128 a thread at 8 rows,
     // 168 at 16).
-    int32_t dec_walkers(int32_t rows) const { return sm_count * (rows == 8 ? 16 : 12); }
+    int32_t dec_walkers() const { return sm_count * (dec_rows() == 8 ? 16 : 12); }
     int32_t pr_walkers() const { return sm_count; }
 };

@@ -544,15 +544,16 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
 // Joins the pieces of the (item, head) pairs that lie in more than one span, in their order, so that the
 // result does not depend on timing.  What bounds it is the chain of dependent loads (walk, item, maxima,
 // outputs), so every block reads its item before it waits for the kernel that leaves the pieces, and the
-// loads of 16 pieces are in flight together.  Two ways to share it out:
+// loads of eight pieces are in flight together.  Two ways to share it out:
 //   PAIRS = false  block x looks at the end of walker x's span and takes the pair that begins in the span and
 //                  crosses it; a warp per row (rows 8 y .. 8 y + 7): many pairs of few pieces
 //   PAIRS = true   block x is a pair, y its row, whose pieces the eight warps share: few pairs of many pieces
 //                  (four requests of 100k keys: 75 pieces each)
 template <int D, int ROWS, bool PROMPT, bool PAIRS>
 __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
-    constexpr int E = D / 32, U = 16;
+    constexpr int E = D / 32, U = 8;
     __shared__ float acc_s[PAIRS ? 8 : 1][D];
+    __shared__ float2 ml_s[PAIRS ? 8 : 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int4 *wk = reinterpret_cast<const int4 *>(reinterpret_cast<const KvWalk *>(P.tables + P.L.walk) + (PROMPT ? 1 : 0));
     const int4 w01 = __ldg(wk), w23 = __ldg(wk + 1);
@@ -585,28 +586,22 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
     // piece i is walker w + i's: its second slot where it begins the pair (i = 0), else its first
     auto slot = [&](int i) { return (2 * (w + i) + (i == 0 ? 1 : 0)) * ROWS + row; };
     griddep_wait();
-    float m = -INFINITY, l = 0.0f;
-    for (int i = lane; i < pieces; i += 32) m = fmaxf(m, P.part_ml[slot(i)].x);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    for (int i = lane; i < pieces; i += 32) {      // a piece in which the row saw nothing has sum 0
-        const float2 v = P.part_ml[slot(i)];
-        l += v.y == 0.0f ? 0.0f : v.y * exp2f(v.x - m);
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    float a[E];
+    // maximum, sum and outputs of eight pieces at a time, all requested before the first is used
+    float m = -INFINITY, l = 0.0f, a[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) a[e] = 0.0f;
-    for (int i0 = PAIRS ? warp : 0; i0 < pieces; i0 += U * (PAIRS ? 8 : 1)) {
-        float f[U], v[U][E];
+    constexpr int STEP = PAIRS ? 8 : 1;
+    for (int i0 = PAIRS ? warp : 0; i0 < pieces; i0 += U * STEP) {
+        float2 ml[U];
+        float v[U][E];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int i = i0 + k * (PAIRS ? 8 : 1);
+            const int i = i0 + k * STEP;
+            ml[k] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
             if (i < pieces) {
-                const float2 ml = P.part_ml[slot(i)];
-                f[k] = ml.y == 0.0f ? 0.0f : ml.y * exp2f(ml.x - m) * inv;
+                ml[k] = P.part_ml[slot(i)];
                 const float *src = P.part + slot(i) * D + lane * E;
                 if constexpr (E == 4) {
                     const float4 t = *reinterpret_cast<const float4 *>(src);
@@ -617,25 +612,46 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
                 }
             }
         }
+        float mn = m;
 #pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (i0 + k * (PAIRS ? 8 : 1) < pieces)
+        for (int k = 0; k < U; ++k) mn = fmaxf(mn, ml[k].x);
+        const float f = m == mn ? 1.0f : exp2f(m - mn);
+        l *= f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) a[e] = fmaf(f[k], v[k][e], a[e]);
+        for (int e = 0; e < E; ++e) a[e] *= f;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {      // a piece in which the row saw nothing has sum 0
+            const float w_k = ml[k].y == 0.0f ? 0.0f : ml[k].y * exp2f(ml[k].x - mn);
+            l += w_k;
+#pragma unroll
+            for (int e = 0; e < E; ++e) a[e] = fmaf(w_k, v[k][e], a[e]);
+        }
+        m = mn;
     }
-    const int32_t r = it.row0 + row, tok = it.tok0 + r / P.kv.group, hq = head * P.kv.group + r % P.kv.group;
-    if (PAIRS) {
+    if (PAIRS) {     // the eight warps' shares, in their order
 #pragma unroll
         for (int e = 0; e < E; ++e) acc_s[warp][lane * E + e] = a[e];
+        if (lane == 0) ml_s[warp] = make_float2(m, l);
         __syncthreads();
         if (warp) return;
 #pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, ml_s[PAIRS ? k : 0].x);
+        l = 0.0f;
+#pragma unroll
         for (int e = 0; e < E; ++e) a[e] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < 8; ++k) {
+            const float2 o = ml_s[PAIRS ? k : 0];
+            const float f = o.y == 0.0f ? 0.0f : exp2f(o.x - m);
+            l = fmaf(f, o.y, l);
 #pragma unroll
-            for (int e = 0; e < E; ++e) a[e] += acc_s[PAIRS ? k : 0][lane * E + e];
+            for (int e = 0; e < E; ++e) a[e] = fmaf(f, acc_s[PAIRS ? k : 0][lane * E + e], a[e]);
+        }
     }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[e] *= inv;
+    const int32_t r = it.row0 + row, tok = it.tok0 + r / P.kv.group, hq = head * P.kv.group + r % P.kv.group;
     // (a row whose sum is no number has inv = NaN, and so has every column)
 #pragma unroll
     for (int e = 0; e < E; ++e) a[e] = isnan(l) ? l : a[e];

@@ -137,33 +137,6 @@ constexpr uint32_t HI_SWIZZLED = desc_hi(1024, 2), HI_CORES = desc_hi(128, 0);
 __host__ __device__ constexpr uint32_t instr(uint32_t type, uint32_t N, uint32_t b_n) {
     return (1u << 4) | (type << 7) | (type << 10) | (b_n << 16) | ((N >> 3) << 17) | ((128u >> 4) << 24);
 }
-// two floats at once
-__device__ __forceinline__ uint64_t pack2f(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpack2f(uint64_t v, float &a, float &b) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ void lds_2x64(uint32_t addr, uint64_t &a, uint64_t &b) {
-    asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
-}
 __device__ __forceinline__ void sts_v4(uint32_t addr, const uint32_t (&v)[4]) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
                  : "memory");
@@ -444,17 +417,17 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 }
                 // a row that sees nothing has no maximum: its probabilities are 2^(-inf - 0)
                 const float mm = m == -INFINITY ? 0.0f : m;
-                const uint64_t f2 = tcp::pack2f(f, f), nm = tcp::pack2f(-mm, -mm);
+                const uint64_t f2 = pack2f(f, f), nm = pack2f(-mm, -mm);
                 uint64_t l2[2] = {0, 0};
                 auto spread = [&](uint32_t (&x)[32], int h) {     // (probabilities h / 2 .. overwrite scores that have been read)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         float a, b;
-                        tcp::unpack2f(tcp::fma2(tcp::pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, nm),
+                        unpack2f(fma2(pack2f(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), f2, nm),
                                       a, b);
                         a = exp2_approx(a);
                         b = exp2_approx(b);
-                        l2[i & 1] = tcp::add2(l2[i & 1], tcp::pack2f(a, b));
+                        l2[i & 1] = add2(l2[i & 1], pack2f(a, b));
                         x[i] = pack_f16(a, b);
                     }
                     tcp::st16(s_at + h / 2, x);
@@ -466,7 +439,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     spread(xa, h);
                 }
                 float a, b;
-                tcp::unpack2f(tcp::add2(l2[0], l2[1]), a, b);
+                unpack2f(add2(l2[0], l2[1]), a, b);
                 l += a + b;
                 tcp::wait_st();
                 tcp::fence_before();
@@ -772,13 +745,22 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 if (pair > 0) ok = wait(&q_free[t], (pair - 1) & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                for (int i = lane; i < 128 * LPR; i += 32) {
-                    const int row = i / LPR, k = i % LPR, my = t * 128 + row;
-                    const bool live = my < cur.it.nrows;
-                    const int32_t r = cur.it.row0 + (live ? my : 0);
-                    const __nv_bfloat16 *src =
-                        P.q + (cur.it.tok0 + r / group) * P.ldq + (int64_t)(cur.head * group + r % group) * D + k * 8;
-                    tcp::cp_async16(q_at + (k >> 3) * 16384 + row * 128 + (((k & 7) ^ (row & 7)) << 4), src, live ? 16 : 0);
+                // lane: run k of rows first, first + step, ..; token and head of a row follow by counting (a
+                // division a row made this 20 us a pair)
+                constexpr int STEP = 32 / LPR;
+                const int k = lane % LPR, first_row = lane / LPR;
+                const uint32_t to = q_at + (k >> 3) * 16384;
+                const int32_t r0 = cur.it.row0 + t * 128 + first_row;
+                int32_t tok = r0 / group, h = r0 - tok * group;
+                const __nv_bfloat16 *src = P.q + (int64_t)cur.head * group * D + k * 8;
+                const int32_t left = cur.it.nrows - t * 128;
+#pragma unroll 4
+                for (int row = first_row; row < 128; row += STEP) {
+                    const bool live = row < left;
+                    tcp::cp_async16(to + row * 128 + (((k & 7) ^ (row & 7)) << 4),
+                                    live ? src + (cur.it.tok0 + tok) * P.ldq + h * D : P.q, live ? 16 : 0);
+                    h += STEP;
+                    while (h >= group) { h -= group; ++tok; }
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_proxy_async();

@@ -392,23 +392,20 @@ using namespace lora;
 
 extern "C" {
 
-static lora_status_t tables_shape(const lora_kv_t *kv, int32_t R, int32_t T, int32_t max_q, KvTables *L) {
+static lora_status_t tables_shape(const lora_kv_t *kv, int32_t R, int32_t T, KvTables *L) {
     if (!kv) return LORA_ERR_INVALID_ARG;
     if (R < 0 || T < 0 || R > KV_MAX_REQUESTS) return LORA_ERR_SHAPE;
     if ((int64_t)T * kv->group > 0x7ffffff0) return LORA_ERR_SHAPE;
-    *L = kv_tables(R, T, kv->group, kv->dec_walkers(kv->dec_rows(max_q)), kv->pr_walkers());
+    *L = kv_tables(R, T, kv->group, kv->dec_walkers(), kv->pr_walkers());
     return LORA_OK;
 }
 
 lora_status_t lora_kv_tables_bytes(const lora_kv_t *kv, int32_t R, int32_t T, size_t *bytes) {
     if (!bytes) return LORA_ERR_INVALID_ARG;
     KvTables L;
-    lora_status_t s = tables_shape(kv, R, T, 1, &L);
+    lora_status_t s = tables_shape(kv, R, T, &L);
     if (s != LORA_OK) return s;
-    const int64_t words = L.words;
-    s = tables_shape(kv, R, T, T, &L);
-    if (s != LORA_OK) return s;
-    *bytes = (size_t)(words > L.words ? words : L.words) * 4;
+    *bytes = (size_t)L.words * 4;
     return LORA_OK;
 }
 
@@ -419,7 +416,7 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
                                    void *stream) {
     TableParams P;
     if (max_q == 0 || max_q > T) max_q = T;
-    lora_status_t s = tables_shape(kv, R, T, max_q, &P.L);
+    lora_status_t s = tables_shape(kv, R, T, &P.L);
     if (s != LORA_OK) return s;
     if (max_q < 0 || window < 0 || ld_table < 0) return LORA_ERR_SHAPE;
     if (!tables || ((uintptr_t)tables & 15)) return LORA_ERR_INVALID_ARG;
@@ -443,8 +440,8 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
     P.page_shift = kv->page_shift;
     P.hkv = kv->hkv;
     P.group = kv->group;
-    P.dec_rows = kv->dec_rows(max_q);
-    P.dec_walkers = kv->dec_walkers(P.dec_rows);
+    P.dec_rows = kv->dec_rows();
+    P.dec_walkers = kv->dec_walkers();
     P.pr_walkers = kv->pr_walkers();
     const size_t smem = (size_t)R * (2 * 8 + 6 * 4) + 32 * 8 + 32 * 4;
     if (smem > kv->tables_attr_smem) {

@@ -59,9 +59,11 @@ enum { KVH_R = 0, KVH_T = 1, KVH_TOKENS = 2, KVH_FAILED = 3, KVH_NEGATIVE = 4, K
 
 // A piece of attention work before it is multiplied by the key/value heads: some rows of one request
 // (row = token * group + query head inside its group) against a run of key chunks.  An item of n
-// chunks stands for hkv runs of n chunks, one per head, at hkv * start + head * n of the list's walk.
+// chunks stands for hkv pairs (item, head) of over + n places each in the list's walk, the first at hkv *
+// start: `over` empty places for what a pair costs whatever its length is (queries in, outputs out), then its
+// chunks.
 struct __align__(16) KvItem {
-    int64_t start;     // chunks of the items before it (one head's)
+    int64_t start;     // places of the items before it (one head's)
     int32_t req;
     int32_t row0, nrows;
     int32_t k_lo;      // first key, a multiple of the chunk
@@ -72,15 +74,18 @@ struct __align__(16) KvItem {
 };
 static_assert(sizeof(KvItem) == 48, "three 16-byte words");
 
-// The walk over a list (all items, heads and chunks in order) is cut into equal spans, one per walker:
+// The walk over a list (all items, heads and places in order) is cut into equal spans, one per walker:
 // a warp of the single-token kernel, a block of the prompt kernel.
 struct __align__(16) KvWalk {
-    int64_t total;     // hkv * chunks
+    int64_t total;     // hkv * places
     int64_t span;
     int32_t n_items;
     int32_t reserved[3];
 };
 
+// Empty places of a pair.  32 prompts of 32..2048 tokens (pairs of one to sixteen chunks), 0 / 2 / 3 / 6 places:
+// 435 / 275 / 262 / 303 us.  256 single tokens on 256..8192 keys, 0 / 1 / 2 / 4 places: 157 / 152 / 149 / 150 us.
+constexpr int KV_DEC_OVER = 2, KV_PROMPT_OVER = 3;
 constexpr int KV_DEC_CHUNK = 32;       // keys of a chunk of the single-token walk
 constexpr int KV_PROMPT_CHUNK = 128;   // keys of a chunk of the prompt walk
 constexpr int KV_PROMPT_ROWS = 256;    // rows of an item of the prompt walk

@@ -142,7 +142,7 @@ constexpr uint32_t NIB_LO = 0x000f000fu, NIB_HI = 0x00f000f0u;
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attention_kernel(const AttnParams P) {
     using C = DecCfg<D>;
-    constexpr int S = C::STAGES, KW = D / 32, MT = D / 16, ROWS = 8 * NT;   // words of K a lane, column tiles
+    constexpr int S = C::STAGES, KW = D / 32, MT = D / 16, ROWS = 8 * NT, OVER = KV_DEC_OVER;   // words of K a lane, column tiles
     extern __shared__ __align__(128) unsigned char dk_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     unsigned char *ring = dk_smem + warp * (S * C::STAGE);
@@ -167,7 +167,8 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     // ---- the requesting side: a cursor over the walk that runs S - 1 chunks ahead -----------------
     int32_t f_item = first;
     KvItem fi = load_item(items + f_item);
-    int32_t f_head = (int32_t)((s0 - hkv * fi.start) / fi.n), f_chunk = (int32_t)(s0 - hkv * fi.start - (int64_t)f_head * fi.n);
+    int32_t f_head = (int32_t)((s0 - hkv * fi.start) / (fi.n + OVER));
+    int32_t f_place = (int32_t)(s0 - hkv * fi.start - (int64_t)f_head * (fi.n + OVER));     // of the pair's; chunks come behind OVER
     int64_t f_pos = s0;
     // Lane i holds cell pages_at + i of the cursor's request: the address of its first head (or none), and
     // brings that cell itself when its chunk's turn comes.
@@ -176,8 +177,12 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     int32_t pages_at = 0, pages_item = -1;
     int f_s = 0;                             // the stage of the next request
     auto request = [&]() {
+        if (f_place < OVER) {
+            f_pos += OVER - f_place;
+            f_place = OVER;
+        }
         if (f_pos >= s1) return;
-        int32_t idx = fi.k_lo / KV_CELL + 2 * f_chunk - pages_at;
+        int32_t idx = fi.k_lo / KV_CELL + 2 * (f_place - OVER) - pages_at;
         if (pages_item != f_item || (uint32_t)idx >= 32u) {
             pages_at += idx;
             pages_item = f_item;
@@ -198,8 +203,8 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
             bulk_g2s(ring + f_s * C::STAGE + (lane & 1) * C::CELL, cell_at + f_head * P.kv.head_bytes, C::CELL, &full[f_s]);
         if (++f_s == S) f_s = 0;
         ++f_pos;
-        if (++f_chunk == fi.n) {
-            f_chunk = 0;
+        if (++f_place == fi.n + OVER) {
+            f_place = 0;
             if (++f_head == hkv) {
                 f_head = 0;
                 if (f_pos < s1) fi = load_item(items + ++f_item);
@@ -213,13 +218,15 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
     const uint32_t ring_u = smem_u32(ring);
     int32_t it_i = first;
     KvItem it = load_item(items + it_i);
-    int32_t head = (int32_t)((s0 - hkv * it.start) / it.n), chunk = (int32_t)(s0 - hkv * it.start - (int64_t)head * it.n);
+    int32_t head = (int32_t)((s0 - hkv * it.start) / (it.n + OVER));
+    int32_t place = (int32_t)(s0 - hkv * it.start - (int64_t)head * (it.n + OVER));
     int64_t pos = s0;
     int stage = 0;
     uint32_t phase = 0;
     while (pos < s1) {
-        // one (item, head): its chunks from `chunk` to the end of the item or of the span
-        const int32_t c0 = chunk, c1 = (int32_t)min((int64_t)it.n, chunk + (s1 - pos));
+        // one (item, head): its chunks c0 .. c1 - 1, to the end of the item or of the span
+        const int32_t c0 = max(place - OVER, 0), c1 = (int32_t)min((int64_t)it.n, place + (s1 - pos) - OVER);
+        if (c1 <= c0) break;      // the span ends inside the pair's empty places
         uint32_t qf[NT][4 * KW];
         float qs[NT][2], qx[NT][2];
 #pragma unroll
@@ -287,7 +294,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
         }
         int ve = KV_NO_EXPONENT;
         uint32_t most_ok = (uint32_t)(ve + KV_RAISE_E + 127) << 23;     // value rows up to this leave ve as it is
-        for (chunk = c0; chunk < c1; ++chunk) {
+        for (int32_t chunk = c0; chunk < c1; ++chunk) {
             const int s = stage;
             request();       // refills the stage that was finished in the previous round
             const bool ok = mbar_wait(&full[s], phase);
@@ -530,9 +537,9 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                     if (g == 0) P.part_ml[slot * ROWS + row] = make_float2(top[n][j] == -INFINITY ? -INFINITY : ml, ls);
                 }
             }
-        pos += c1 - c0;
+        pos += c1 + OVER - place;
         if (c1 == it.n) {
-            chunk = 0;
+            place = 0;
             if (++head == hkv) {
                 head = 0;
                 if (pos < s1) it = load_item(items + ++it_i);
@@ -551,7 +558,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
 //                  (four requests of 100k keys: 75 pieces each)
 template <int D, int ROWS, bool PROMPT, bool PAIRS>
 __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
-    constexpr int E = D / 32, U = 8;
+    constexpr int E = D / 32, U = 8, OVER = PROMPT ? KV_PROMPT_OVER : KV_DEC_OVER;
     __shared__ float acc_s[PAIRS ? 8 : 1][D];
     __shared__ float2 ml_s[PAIRS ? 8 : 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -567,7 +574,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
         if (item >= w23.x) return;
         it = load_item(items + item);
         head = blockIdx.x % P.kv.hkv;
-        begin = P.kv.hkv * it.start + (int64_t)head * it.n;
+        begin = P.kv.hkv * it.start + (int64_t)head * (it.n + OVER) + OVER;
         w = begin / span;
         if (begin + it.n <= (w + 1) * span) return;
     } else {
@@ -576,9 +583,9 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
         if (cut >= total) return;
         it = load_item(items + __ldg(P.tables + (PROMPT ? P.L.pr_first : P.L.dec_first) + w + 1));
         const int64_t off = cut - P.kv.hkv * it.start;
-        head = (int32_t)(off / it.n);
-        begin = P.kv.hkv * it.start + (int64_t)head * it.n;
-        if (begin == cut || begin < w * span) return;      // nothing crosses this end, or another block has it
+        head = (int32_t)(off / (it.n + OVER));
+        begin = P.kv.hkv * it.start + (int64_t)head * (it.n + OVER) + OVER;      // its first chunk
+        if (begin >= cut || begin < w * span || begin + it.n <= cut) return;     // nothing crosses this end, or another block has it
     }
     const int32_t row = PAIRS ? (int32_t)blockIdx.y : (int32_t)blockIdx.y * 8 + warp;
     if (row >= it.nrows) return;

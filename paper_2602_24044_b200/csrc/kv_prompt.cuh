@@ -199,26 +199,31 @@ struct PromptCfg {
 
 // A walker's cursor over its span: (item, head, block) in order.
 struct PromptCursor {
+    static constexpr int OVER = KV_PROMPT_OVER;
     const KvItem *items;
     KvItem it;
-    int64_t pos, end;
+    int64_t left;             // places of the span that are left, from the pair's first chunk or the span's start on
     int32_t index, head, chunk, hkv;
     __device__ __forceinline__ PromptCursor(const KvItem *list, int32_t first, int64_t s0, int64_t s1, int32_t heads)
-        : items(list), pos(s0), end(s1), index(first), hkv(heads) {
+        : items(list), index(first), hkv(heads) {
         it = load_item(items + index);
         const int64_t off = s0 - hkv * it.start;
-        head = (int32_t)(off / it.n);
-        chunk = (int32_t)(off - (int64_t)head * it.n);
+        head = (int32_t)(off / (it.n + OVER));
+        const int32_t place = (int32_t)(off - (int64_t)head * (it.n + OVER));
+        chunk = max(place - OVER, 0);
+        left = s1 - s0 - max(OVER - place, 0);
     }
-    __device__ __forceinline__ bool more() const { return pos < end; }
+    __device__ __forceinline__ bool more() const { return left > 0; }
     // blocks of the current (item, head) that belong to the span
-    __device__ __forceinline__ int32_t last_chunk() const { return (int32_t)min((int64_t)it.n, chunk + (end - pos)); }
+    __device__ __forceinline__ int32_t last_chunk() const { return (int32_t)min((int64_t)it.n, chunk + left); }
+    // is there a block behind the current pair's?
+    __device__ __forceinline__ bool another_pair() const { return left > it.n - chunk + OVER; }
     __device__ __forceinline__ void next_pair(int32_t blocks) {
-        pos += blocks;
+        left -= blocks + OVER;
         chunk = 0;
         if (++head == hkv) {
             head = 0;
-            if (pos < end) it = load_item(items + ++index);
+            if (left > 0) it = load_item(items + ++index);
         }
     }
 };
@@ -254,6 +259,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
     const KvItem *items = reinterpret_cast<const KvItem *>(P.tables + P.L.pr_items);
     const int32_t first = __ldg(P.tables + P.L.pr_first + blockIdx.x);
     const int32_t group = P.kv.group;
+    PromptCursor cur(items, first, s0, s1, P.kv.hkv);
+    if (!cur.more()) return;      // only empty places (the same for the whole block)
 
     if (tid == 0) {
         for (int i = 0; i < PK_RAW; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 4); }
@@ -293,8 +300,6 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         *failed = 1;
         return false;
     };
-    PromptCursor cur(items, first, s0, s1, P.kv.hkv);
-
     if (warp < 8) {
         // =========================== softmax: a thread is a row ====================================
         const int t = warp >> 2, row = tid & 127;
@@ -450,7 +455,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             if (!ok) break;
             // the next pair's queries, while the last product runs
             float next_unit = 0.0f;
-            if (cur.pos + (c1 - c0) < cur.end) next_unit = take_queries(pair + 1, ok);
+            if (cur.another_pair()) next_unit = take_queries(pair + 1, ok);
             if (!ok) break;
             // ---- the (item, head) is over, or the span is ------------------------------------------
             ok = wait(&o_full[t], pair & 1u);

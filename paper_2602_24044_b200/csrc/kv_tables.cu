@@ -87,7 +87,7 @@ __device__ __forceinline__ void item_range(int32_t lim0, int32_t group, int32_t 
 __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TableParams P) {
     extern __shared__ __align__(16) unsigned char tb_smem[];
     const int R = P.R, T = P.T, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int64_t *chunks_d = reinterpret_cast<int64_t *>(tb_smem);   // prefix sums: chunks of the single-token list
+    int64_t *chunks_d = reinterpret_cast<int64_t *>(tb_smem);   // prefix sums: places of the single-token list
     int64_t *chunks_p = chunks_d + R;                            // and of the prompt list
     int64_t *warp64 = chunks_p + R;                              // [32]
     int32_t *kv = reinterpret_cast<int32_t *>(warp64 + 32);
@@ -145,12 +145,12 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         int64_t c = 0;
         int32_t n_items = 0;
         if (failed[r])
-            c = n_items = (int32_t)((rows + P.dec_rows - 1) / P.dec_rows);
+            c = (1 + KV_DEC_OVER) * (int64_t)(n_items = (int32_t)((rows + P.dec_rows - 1) / P.dec_rows));
         else if (rows <= KV_DEC_MAX_ROWS)
             for (int32_t row0 = 0; row0 < rows; row0 += P.dec_rows, ++n_items) {
                 int32_t lo, n;
                 item_range(lim0, P.group, P.window, KV_DEC_CHUNK, row0, min(P.dec_rows, (int32_t)rows - row0), &lo, &n);
-                c += n;
+                c += n + KV_DEC_OVER;
             }
         chunks_d[r] = c;
         items_d[r] = n_items;
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
             int32_t lo, n;
             item_range(lim0, P.group, P.window, KV_PROMPT_CHUNK, t * KV_PROMPT_ROWS,
                        (int32_t)min((int64_t)KV_PROMPT_ROWS, rows - (int64_t)t * KV_PROMPT_ROWS), &lo, &n);
-            c += n;
+            c += n + KV_PROMPT_OVER;
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
@@ -186,12 +186,12 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     const int64_t spare_rows = (int64_t)(T - tokens) * P.group;
     const int32_t spare = (int32_t)((spare_rows + P.dec_rows - 1) / P.dec_rows);
     if (tid < 2) {
-        const int64_t total = P.hkv * ((R ? (tid ? chunks_p : chunks_d)[R - 1] : 0) + (tid ? 0 : spare));
+        const int64_t total = P.hkv * ((R ? (tid ? chunks_p : chunks_d)[R - 1] : 0) + (tid ? 0 : (1 + KV_DEC_OVER) * (int64_t)spare));
         const int32_t walkers = tid ? P.pr_walkers : P.dec_walkers;
         int64_t span = (total + walkers - 1) / walkers;
         // single tokens: no fewer than four chunks per warp, or joining the pieces costs more than
         // the split saves
-        if (tid == 0 && span < 4) span = 4;
+        if (tid == 0 && span < 4 + KV_DEC_OVER) span = 4 + KV_DEC_OVER;
         if (span < 1) span = 1;
         walk_total[tid] = total;
         walk_span[tid] = span;
@@ -277,15 +277,16 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
             if (i < n_items)
                 item_range(it.lim0, P.group, P.window, single ? KV_DEC_CHUNK : KV_PROMPT_CHUNK, it.row0, it.nrows,
                            &it.k_lo, &it.n);
-            const int64_t incl = warp_incl((int64_t)it.n);
-            it.start = before + incl - it.n;
+            const int64_t places = i < n_items ? it.n + (single ? KV_DEC_OVER : KV_PROMPT_OVER) : 0;
+            const int64_t incl = warp_incl(places);
+            it.start = before + incl - places;
             if (i < n_items) (single ? dec : pr)[first + i] = it;
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
     }
     for (int i = gt; i < spare; i += all_threads) {
         KvItem it;
-        it.start = (R ? chunks_d[R - 1] : 0) + i;
+        it.start = (R ? chunks_d[R - 1] : 0) + (1 + KV_DEC_OVER) * (int64_t)i;
         it.req = 0;
         it.row0 = i * P.dec_rows;
         it.nrows = (int32_t)min((int64_t)P.dec_rows, spare_rows - it.row0);
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
             int32_t lo = r ? items[r - 1] : 0, hi = r < R ? items[r] : 0;
             const KvItem *list = single ? dec : pr;
             if (r == R) {
-                found = (int32_t)(lo + at - (R ? chunks_d[R - 1] : 0));   // a spare item
+                found = (int32_t)(lo + (at - (R ? chunks_d[R - 1] : 0)) / (1 + KV_DEC_OVER));   // a spare item
             } else {
                 while (hi - lo > 1) {   // last item that starts at or before `at`
                     const int32_t m = (lo + hi) >> 1;

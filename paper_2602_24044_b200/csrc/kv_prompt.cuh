@@ -747,7 +747,17 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             bool ok = true;
             for (; ok && cur.more(); ++pair) {
                 const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
-                if (pair > 0) ok = wait(&q_free[t], (pair - 1) & 1u);
+                if (pair > 0) {
+                    // rows of this pair to L2 while the queries before them are still in use
+                    for (int row = lane; row < min(128, cur.it.nrows - t * 128); row += 32) {
+                        const int32_t r = cur.it.row0 + t * 128 + row;
+                        const __nv_bfloat16 *src =
+                            P.q + (cur.it.tok0 + r / group) * P.ldq + (int64_t)(cur.head * group + r % group) * D;
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(src));
+                        if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + 64));
+                    }
+                    ok = wait(&q_free[t], (pair - 1) & 1u);
+                }
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 // lane: run k of rows first, first + step, ..; token and head of a row follow by counting (a

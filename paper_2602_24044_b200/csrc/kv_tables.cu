@@ -4,7 +4,8 @@
 // prefix sums, tables out), not bytes.  One cluster of eight blocks, each of which recomputes all
 // prefix sums for itself in shared memory (they are short), so the only exchange between blocks is the
 // cluster barrier that separates the reads of the inputs from the writes (lengths and stack may be
-// updated in place) and the one after which the walkers' first items are looked up in the lists.
+// updated in place) and, where there are prompts, the one after which their walkers' first items are looked
+// up in the list.
 #include "fused_ptx.cuh"
 #include "kv_common.cuh"
 
@@ -33,27 +34,34 @@ __device__ __forceinline__ I warp_incl(I v) {
     return v;
 }
 
-// In place: a[0 .. n) -> its inclusive prefix sums (all threads of the block call it).
-template <typename I>
-__device__ void block_scan(I *a, int n, I *warp_sum) {
+// In place: each of N arrays a[k][0 .. n) -> its inclusive prefix sums (all threads of the block call it).
+template <int N, typename I>
+__device__ void block_scan(I *const (&a)[N], int n, I *warp_sum) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (n + TB_THREADS - 1) / TB_THREADS;
     const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    I sum = 0;
-    for (int i = i0; i < i1; ++i) sum += a[i];
-    const I incl = warp_incl(sum);
-    if (lane == 31) warp_sum[warp] = incl;
-    __syncthreads();
-    if (warp == 0) {
-        const I v = warp_incl(warp_sum[lane]);
-        __syncwarp();
-        warp_sum[lane] = v;
+    I incl[N], sum[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        sum[k] = 0;
+        for (int i = i0; i < i1; ++i) sum[k] += a[k][i];
+        incl[k] = warp_incl(sum[k]);
+        if (lane == 31) warp_sum[k * 32 + warp] = incl[k];
     }
     __syncthreads();
-    I run = incl - sum + (warp ? warp_sum[warp - 1] : (I)0);
-    for (int i = i0; i < i1; ++i) {
-        run += a[i];
-        a[i] = run;
+    if (warp < N) {
+        const I v = warp_incl(warp_sum[warp * 32 + lane]);
+        __syncwarp();
+        warp_sum[warp * 32 + lane] = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        I run = incl[k] - sum[k] + (warp ? warp_sum[k * 32 + warp - 1] : (I)0);
+        for (int i = i0; i < i1; ++i) {
+            run += a[k][i];
+            a[k][i] = run;
+        }
     }
     __syncthreads();
 }
@@ -89,14 +97,14 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     const int R = P.R, T = P.T, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int64_t *chunks_d = reinterpret_cast<int64_t *>(tb_smem);   // prefix sums: places of the single-token list
     int64_t *chunks_p = chunks_d + R;                            // and of the prompt list
-    int64_t *warp64 = chunks_p + R;                              // [32]
-    int32_t *kv = reinterpret_cast<int32_t *>(warp64 + 32);
+    int64_t *warp64 = chunks_p + R;                              // [2][32]
+    int32_t *kv = reinterpret_cast<int32_t *>(warp64 + 64);
     int32_t *end = kv + R;        // prefix sums of the new tokens
     int32_t *pages = end + R;     // of the pages needed
     int32_t *items_d = pages + R; // of the items
     int32_t *items_p = items_d + R;
     int32_t *failed = items_p + R;   // 1: failed
-    int32_t *warp32 = failed + R;    // [32]
+    int32_t *warp32 = failed + R;    // [2][32]
     __shared__ int32_t n_failed, n_negative, taken, sum_q;
     __shared__ int64_t walk_total[2], walk_span[2];
 
@@ -112,7 +120,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     }
     const int32_t count = P.free_count ? min(max(*P.free_count, 0), P.num_pages) : 0;
     __syncthreads();
-    block_scan(chunks_d, R, warp64);
+    block_scan<1>({chunks_d}, R, warp64);
     for (int r = tid; r < R; r += TB_THREADS) {
         const int64_t e = chunks_d[r], q = e - (r ? chunks_d[r - 1] : 0);
         const int64_t all = kv[r] + q;
@@ -122,7 +130,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         chunks_p[r] = fits ? pages_for((int32_t)all, P.page_shift) - pages_for(kv[r], P.page_shift) : 0;
     }
     __syncthreads();
-    block_scan(chunks_p, R, warp64);   // pages needed, in 64 bits
+    block_scan<1>({chunks_p}, R, warp64);   // pages needed, in 64 bits
     for (int r = tid; r < R; r += TB_THREADS) {
         const int64_t upto = chunks_p[r], need = upto - (r ? chunks_p[r - 1] : 0);
         if (need > 0 && upto > count) failed[r] = 1;
@@ -158,7 +166,8 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         items_p[r] = 0;
     }
     __syncthreads();
-    for (int r = warp; r < R; r += TB_THREADS / 32) {
+    // (max_q bounds every request that did not fail)
+    for (int r = warp; r < R && (int64_t)P.max_q * P.group > KV_DEC_MAX_ROWS; r += TB_THREADS / 32) {
         const int32_t q = end[r] - (r ? end[r - 1] : 0);
         const int64_t rows = (int64_t)q * P.group;
         if (rows <= KV_DEC_MAX_ROWS || failed[r]) continue;
@@ -179,10 +188,8 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         }
     }
     __syncthreads();
-    block_scan(chunks_d, R, warp64);
-    block_scan(chunks_p, R, warp64);
-    block_scan(items_d, R, warp32);
-    block_scan(items_p, R, warp32);
+    block_scan<2>({chunks_d, chunks_p}, R, warp64);
+    block_scan<2>({items_d, items_p}, R, warp32);
     const int64_t spare_rows = (int64_t)(T - tokens) * P.group;
     const int32_t spare = (int32_t)((spare_rows + P.dec_rows - 1) / P.dec_rows);
     if (tid < 2) {
@@ -297,27 +304,42 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
         dec[(R ? items_d[R - 1] : 0) + i] = it;
     }
-    cluster_arrive();   // the lists are complete
-    cluster_wait();
+    // The first item of each walker.  A request of single tokens has at most eight items, whose places are
+    // counted again; a prompt's are looked up in the list, once that is complete.
+    const bool prompts = R && items_p[R - 1] > 0;
+    if (prompts) {
+        cluster_arrive();
+        cluster_wait();
+    }
     for (int w = gt; w < P.dec_walkers + P.pr_walkers; w += all_threads) {
         const bool single = w < P.dec_walkers;
         const int32_t i = single ? w : w - P.dec_walkers;
         const int64_t pos = i * walk_span[single ? 0 : 1];
         int32_t found = -1;
         if (pos < walk_total[single ? 0 : 1]) {
-            const int64_t at = pos / P.hkv;   // hkv * start <= pos  <=>  start <= at
+            int64_t at = pos / P.hkv;   // hkv * start <= pos  <=>  start <= at
             const int r = upper_bound(single ? chunks_d : chunks_p, R, at);
             const int32_t *items = single ? items_d : items_p;
-            int32_t lo = r ? items[r - 1] : 0, hi = r < R ? items[r] : 0;
-            const KvItem *list = single ? dec : pr;
-            if (r == R) {
-                found = (int32_t)(lo + (at - (R ? chunks_d[R - 1] : 0)) / (1 + KV_DEC_OVER));   // a spare item
-            } else {
-                while (hi - lo > 1) {   // last item that starts at or before `at`
-                    const int32_t m = (lo + hi) >> 1;
-                    if (list[m].start <= at) lo = m; else hi = m;
+            found = r ? items[r - 1] : 0;
+            if (single) {
+                at -= r ? chunks_d[r - 1] : 0;
+                if (r == R || failed[r]) {
+                    found += (int32_t)(at / (1 + KV_DEC_OVER));      // items of one empty chunk each
+                } else {
+                    const int32_t rows = (end[r] - (r ? end[r - 1] : 0)) * P.group;
+                    for (int32_t row0 = 0;; row0 += P.dec_rows, ++found) {
+                        int32_t lo, n;
+                        item_range(kv[r] + 1, P.group, P.window, KV_DEC_CHUNK, row0, min(P.dec_rows, rows - row0), &lo, &n);
+                        at -= n + KV_DEC_OVER;
+                        if (at < 0 || row0 + P.dec_rows >= rows) break;
+                    }
                 }
-                found = lo;
+            } else {
+                int32_t hi = items[r];
+                while (hi - found > 1) {   // last item that starts at or before `at`
+                    const int32_t m = (found + hi) >> 1;
+                    if (pr[m].start <= at) found = m; else hi = m;
+                }
             }
         }
         P.out[(single ? P.L.dec_first : P.L.pr_first) + i] = found;
@@ -358,7 +380,7 @@ __global__ void __launch_bounds__(TB_THREADS) release_kernel(const int32_t *requ
         }
     }
     __syncthreads();
-    block_scan(count, n, warp_sum);
+    block_scan<1>({count}, n, warp_sum);
     const int32_t have = min(max(*free_count, 0), num_pages);
     __syncthreads();
     int32_t lost = 0;
@@ -444,7 +466,7 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
     P.dec_rows = kv->dec_rows();
     P.dec_walkers = kv->dec_walkers();
     P.pr_walkers = kv->pr_walkers();
-    const size_t smem = (size_t)R * (2 * 8 + 6 * 4) + 32 * 8 + 32 * 4;
+    const size_t smem = (size_t)R * (2 * 8 + 6 * 4) + 2 * 32 * 8 + 2 * 32 * 4;
     if (smem > kv->tables_attr_smem) {
         LORA_CUDA_TRY(cudaFuncSetAttribute(build_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         kv->tables_attr_smem = smem;

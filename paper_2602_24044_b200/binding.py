@@ -191,10 +191,11 @@ def _ptr(obj) -> Optional[int]:
     """Address of a torch tensor / numpy array / int / None."""
     if obj is None:
         return None
+    data_ptr = getattr(obj, "data_ptr", None)
+    if data_ptr is not None:
+        return data_ptr()
     if isinstance(obj, int):
         return obj
-    if hasattr(obj, "data_ptr"):
-        return int(obj.data_ptr())
     if isinstance(obj, np.ndarray):
         return int(obj.ctypes.data)
     raise TypeError("cannot take the address of %r" % type(obj))

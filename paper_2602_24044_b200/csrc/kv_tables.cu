@@ -11,7 +11,8 @@
 
 namespace lora {
 
-constexpr int TB_BLOCKS = 8, TB_THREADS = 1024;
+constexpr int TB_BLOCKS = 8, TB_THREADS = 512;
+constexpr int TB_WARPS = TB_THREADS / 32;
 
 struct TableParams {
     const int32_t *kv_len, *q_len, *free_pages, *free_count;
@@ -23,46 +24,69 @@ struct TableParams {
     KvTables L;
 };
 
+// Sums that stay at the largest int32 once they pass it (with lengths that are not negative: associative).
+__device__ __forceinline__ int32_t plus(int32_t a, int32_t b) {
+    return (int32_t)min((uint32_t)a + (uint32_t)b, 0x7fffffffu);
+}
+__device__ __forceinline__ int64_t plus(int64_t a, int64_t b) { return a + b; }
+
 template <typename I>
 __device__ __forceinline__ I warp_incl(I v) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const I o = __shfl_up_sync(0xffffffffu, v, d);
-        if (lane >= d) v += o;
+        if (lane >= d) v = plus(v, o);
     }
     return v;
 }
 
-// In place: each of N arrays a[k][0 .. n) -> its inclusive prefix sums (all threads of the block call it).
-template <int N, typename I>
-__device__ void block_scan(I *const (&a)[N], int n, I *warp_sum) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (n + TB_THREADS - 1) / TB_THREADS;
-    const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
-    I incl[N], sum[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        sum[k] = 0;
-        for (int i = i0; i < i1; ++i) sum[k] += a[k][i];
-        incl[k] = warp_incl(sum[k]);
-        if (lane == 31) warp_sum[k * 32 + warp] = incl[k];
+// In place: a[0 .. n) -> its inclusive prefix sums.  A thread takes consecutive entries.  In three steps, so
+// that several arrays share the block's barriers: the threads' sums, the warps' sums (one warp an array), the
+// entries.
+template <typename I>
+struct Scan {
+    I *a, *warp_sum;      // [TB_WARPS]
+    I sum, incl;
+    __device__ __forceinline__ Scan(I *array, I *sums) : a(array), warp_sum(sums) {}
+    __device__ __forceinline__ void threads(int i0, int i1) {
+        sum = 0;
+        for (int i = i0; i < i1; ++i) sum = plus(sum, a[i]);
+        incl = warp_incl(sum);
+        if ((threadIdx.x & 31) == 31) warp_sum[threadIdx.x >> 5] = incl;
     }
-    __syncthreads();
-    if (warp < N) {
-        const I v = warp_incl(warp_sum[warp * 32 + lane]);
+    __device__ __forceinline__ void warps(int warp) {
+        if ((int)(threadIdx.x >> 5) != warp) return;
+        const int lane = threadIdx.x & 31;
+        const I v = warp_incl(lane < TB_WARPS ? warp_sum[lane] : (I)0);
         __syncwarp();
-        warp_sum[warp * 32 + lane] = v;
+        if (lane < TB_WARPS) warp_sum[lane] = v;
     }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        I run = incl[k] - sum[k] + (warp ? warp_sum[k * 32 + warp - 1] : (I)0);
+    __device__ __forceinline__ void entries(int i0, int i1) {
+        // what lies before this thread: the warps before, the lanes before
+        const I before = __shfl_up_sync(0xffffffffu, incl, 1);
+        I run = plus(threadIdx.x >= 32 ? warp_sum[(threadIdx.x >> 5) - 1] : (I)0, (threadIdx.x & 31) ? before : (I)0);
         for (int i = i0; i < i1; ++i) {
-            run += a[k][i];
-            a[k][i] = run;
+            run = plus(run, a[i]);
+            a[i] = run;
         }
     }
+};
+__device__ __forceinline__ void share_of(int n, int &i0, int &i1) {
+    const int per = (n + TB_THREADS - 1) / TB_THREADS;
+    i0 = min((int)threadIdx.x * per, n);
+    i1 = min(i0 + per, n);
+}
+template <typename I>
+__device__ void block_scan(I *a, int n, I *warp_sum) {
+    int i0, i1;
+    share_of(n, i0, i1);
+    Scan<I> s(a, warp_sum);
+    s.threads(i0, i1);
+    __syncthreads();
+    s.warps(0);
+    __syncthreads();
+    s.entries(i0, i1);
     __syncthreads();
 }
 
@@ -99,7 +123,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     int64_t *chunks_p = chunks_d + R;                            // and of the prompt list
     int64_t *warp64 = chunks_p + R;                              // [2][32]
     int32_t *kv = reinterpret_cast<int32_t *>(warp64 + 64);
-    int32_t *end = kv + R;        // prefix sums of the new tokens
+    int32_t *end = kv + R;        // prefix sums of the new tokens, cut at T
     int32_t *pages = end + R;     // of the pages needed
     int32_t *items_d = pages + R; // of the items
     int32_t *items_p = items_d + R;
@@ -108,38 +132,38 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
     __shared__ int32_t n_failed, n_negative, taken, sum_q;
     __shared__ int64_t walk_total[2], walk_span[2];
 
-    // a prefix sum that would pass 32 bits is cut at the batch's own size (T tokens): each length enters
-    // the sum as at most T + 1, and sums are kept in 64 bits until they have been cut
-    if (tid == 0) n_failed = n_negative = taken = 0;
+    if (tid == 0) n_failed = n_negative = taken = sum_q = 0;
     __syncthreads();
     for (int r = tid; r < R; r += TB_THREADS) {
         const int32_t k = P.kv_len[r], q = P.q_len[r];
         if (k < 0 || q < 0) atomicAdd(&n_negative, 1);
         kv[r] = max(k, 0);
-        chunks_d[r] = min(max(q, 0), T + 1);
+        end[r] = max(q, 0);
+        items_d[r] = max(q, 0);
     }
     const int32_t count = P.free_count ? min(max(*P.free_count, 0), P.num_pages) : 0;
     __syncthreads();
-    block_scan<1>({chunks_d}, R, warp64);
+    block_scan(end, R, warp32);
     for (int r = tid; r < R; r += TB_THREADS) {
-        const int64_t e = chunks_d[r], q = e - (r ? chunks_d[r - 1] : 0);
-        const int64_t all = kv[r] + q;
-        end[r] = (int32_t)min(e, (int64_t)T);
-        const bool fits = e <= T && q <= P.max_q && all <= (P.ld << P.page_shift) && all < 0x7fffff00;
+        const int32_t q = items_d[r];
+        const int64_t all = (int64_t)kv[r] + q;
+        // (a sum that stopped at the largest number is over T in any case: T * group is below it)
+        const bool fits = end[r] <= T && q <= P.max_q && all <= (P.ld << P.page_shift) && all < 0x7fffff00;
         failed[r] = !fits;
-        chunks_p[r] = fits ? pages_for((int32_t)all, P.page_shift) - pages_for(kv[r], P.page_shift) : 0;
+        pages[r] = items_p[r] = fits ? pages_for((int32_t)all, P.page_shift) - pages_for(kv[r], P.page_shift) : 0;
     }
     __syncthreads();
-    block_scan<1>({chunks_p}, R, warp64);   // pages needed, in 64 bits
+    block_scan(pages, R, warp32);
+    const int32_t all_q = R ? end[R - 1] : 0;
     for (int r = tid; r < R; r += TB_THREADS) {
-        const int64_t upto = chunks_p[r], need = upto - (r ? chunks_p[r - 1] : 0);
-        if (need > 0 && upto > count) failed[r] = 1;
-        pages[r] = (int32_t)min(upto, (int64_t)0x7fffffff);
+        const int32_t need = items_p[r];
+        if (need > 0 && pages[r] > count) failed[r] = 1;
         if (failed[r]) atomicAdd(&n_failed, 1);
-        else atomicMax(&taken, need > 0 ? pages[r] : 0);
+        else if (need > 0) atomicMax(&taken, pages[r]);
     }
     __syncthreads();
-    if (tid == 0) sum_q = R ? (int32_t)min(chunks_d[R - 1], (int64_t)0x7fffffff) : 0;
+    for (int r = tid; r < R; r += TB_THREADS) end[r] = min(end[r], T);
+    if (tid == 0) sum_q = all_q;
     __syncthreads();
     const int32_t tokens = R ? end[R - 1] : 0;
 
@@ -166,30 +190,44 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         items_p[r] = 0;
     }
     __syncthreads();
-    // (max_q bounds every request that did not fail)
-    for (int r = warp; r < R && (int64_t)P.max_q * P.group > KV_DEC_MAX_ROWS; r += TB_THREADS / 32) {
-        const int32_t q = end[r] - (r ? end[r - 1] : 0);
-        const int64_t rows = (int64_t)q * P.group;
-        if (rows <= KV_DEC_MAX_ROWS || failed[r]) continue;
-        const int32_t lim0 = kv[r] + 1;
-        const int32_t tiles = (int32_t)((rows + KV_PROMPT_ROWS - 1) / KV_PROMPT_ROWS);
-        int64_t c = 0;
-        for (int32_t t = lane; t < tiles; t += 32) {
-            int32_t lo, n;
-            item_range(lim0, P.group, P.window, KV_PROMPT_CHUNK, t * KV_PROMPT_ROWS,
-                       (int32_t)min((int64_t)KV_PROMPT_ROWS, rows - (int64_t)t * KV_PROMPT_ROWS), &lo, &n);
-            c += n + KV_PROMPT_OVER;
-        }
+    // (max_q bounds every request that did not fail; a warp looks at 32 requests and takes the prompts among them)
+    const bool may_prompt = (int64_t)P.max_q * P.group > KV_DEC_MAX_ROWS;
+    for (int r0 = warp * 32; may_prompt && r0 < R; r0 += TB_WARPS * 32) {
+        const int mine = r0 + lane;
+        uint32_t mask = __ballot_sync(0xffffffffu, mine < R && !failed[mine] &&
+            (int64_t)(end[mine] - (mine ? end[mine - 1] : 0)) * P.group > KV_DEC_MAX_ROWS);
+        for (; mask; mask &= mask - 1) {
+            const int r = r0 + __ffs(mask) - 1;
+            const int64_t rows = (int64_t)(end[r] - (r ? end[r - 1] : 0)) * P.group;
+            const int32_t tiles = (int32_t)((rows + KV_PROMPT_ROWS - 1) / KV_PROMPT_ROWS);
+            int64_t c = 0;
+            for (int32_t t = lane; t < tiles; t += 32) {
+                int32_t lo, n;
+                item_range(kv[r] + 1, P.group, P.window, KV_PROMPT_CHUNK, t * KV_PROMPT_ROWS,
+                           (int32_t)min((int64_t)KV_PROMPT_ROWS, rows - (int64_t)t * KV_PROMPT_ROWS), &lo, &n);
+                c += n + KV_PROMPT_OVER;
+            }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
-        if (lane == 0) {
-            chunks_p[r] = c;
-            items_p[r] = tiles;
+            for (int d = 16; d; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
+            if (lane == 0) {
+                chunks_p[r] = c;
+                items_p[r] = tiles;
+            }
         }
     }
     __syncthreads();
-    block_scan<2>({chunks_d, chunks_p}, R, warp64);
-    block_scan<2>({items_d, items_p}, R, warp32);
+    {
+        int i0, i1;
+        share_of(R, i0, i1);
+        Scan<int64_t> a(chunks_d, warp64), b(chunks_p, warp64 + 32);
+        Scan<int32_t> c(items_d, warp32), d(items_p, warp32 + 32);
+        a.threads(i0, i1); b.threads(i0, i1); c.threads(i0, i1); d.threads(i0, i1);
+        __syncthreads();
+        a.warps(0); b.warps(1); c.warps(2); d.warps(3);
+        __syncthreads();
+        a.entries(i0, i1); b.entries(i0, i1); c.entries(i0, i1); d.entries(i0, i1);
+        __syncthreads();
+    }
     const int64_t spare_rows = (int64_t)(T - tokens) * P.group;
     const int32_t spare = (int32_t)((spare_rows + P.dec_rows - 1) / P.dec_rows);
     if (tid < 2) {
@@ -231,78 +269,103 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         P.out[P.L.kv_len + r] = after;
         if (P.kv_len_out) P.kv_len_out[r] = after;
     }
-    // tokens.  A page of the batch is taken from the stack directly; an old one from the block table
-    for (int t = gt; t < T; t += all_threads) {
-        int32_t pos = 0, slot = -1;
-        if (t < tokens) {
-            const int r = upper_bound(end, R, t);
-            const int64_t p64 = (int64_t)kv[r] + (t - (r ? end[r - 1] : 0));
-            pos = (int32_t)min(p64, (int64_t)0x7fffffff);
-            if (!failed[r]) {
-                const int32_t i = pos >> P.page_shift, old = pages_for(kv[r], P.page_shift);
-                int32_t page;
-                if (i < old) {
-                    page = P.block_table[r * P.ld + i];
-                } else {
-                    const int32_t k = (r ? pages[r - 1] : 0) + i - old;
-                    page = P.free_pages[count - 1 - k];
-                }
-                if (page >= 0 && page < P.num_pages) slot = (page << P.page_shift) + (pos & ((1 << P.page_shift) - 1));
-            }
-        }
-        P.out[P.L.position + t] = pos;
-        P.out[P.L.slot + t] = slot;
-    }
-    for (int k = gt; k < taken; k += all_threads) {
-        const int r = upper_bound(pages, R, k);
-        const int32_t i = pages_for(kv[r], P.page_shift) + k - (r ? pages[r - 1] : 0);
-        P.block_table[r * P.ld + i] = P.free_pages[count - 1 - k];
-    }
-    // work lists
+    // Half of each block's threads write what belongs to tokens and pages, the other half the work lists and
+    // the walkers' first items: their chains of loads and divisions run beside each other.
     KvItem *dec = reinterpret_cast<KvItem *>(P.out + P.L.dec_items);
     KvItem *pr = reinterpret_cast<KvItem *>(P.out + P.L.pr_items);
-    for (int r = gt >> 5; r < R; r += all_threads >> 5) {
-        const int32_t tok0 = r ? end[r - 1] : 0, q = end[r] - tok0;
-        const int64_t rows = (int64_t)q * P.group;
-        if (rows == 0) continue;
-        const bool single = rows <= KV_DEC_MAX_ROWS || failed[r];
-        const int32_t per = single ? P.dec_rows : KV_PROMPT_ROWS;
-        const int32_t n_items = (int32_t)((rows + per - 1) / per);
-        const int32_t first = single ? (r ? items_d[r - 1] : 0) : (r ? items_p[r - 1] : 0);
-        int64_t before = single ? (r ? chunks_d[r - 1] : 0) : (r ? chunks_p[r - 1] : 0);
-        KvItem it;
-        it.req = r;
-        it.tok0 = tok0;
-        it.lim0 = failed[r] ? -0x40000000 : kv[r] + 1;
-        it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
-        for (int32_t b = 0; b < n_items; b += 32) {
-            const int32_t i = b + lane;
-            it.row0 = i * per;
-            it.nrows = (int32_t)min((int64_t)per, rows - it.row0);
-            it.n = 0;
-            it.k_lo = 0;
-            if (i < n_items)
-                item_range(it.lim0, P.group, P.window, single ? KV_DEC_CHUNK : KV_PROMPT_CHUNK, it.row0, it.nrows,
-                           &it.k_lo, &it.n);
-            const int64_t places = i < n_items ? it.n + (single ? KV_DEC_OVER : KV_PROMPT_OVER) : 0;
-            const int64_t incl = warp_incl(places);
-            it.start = before + incl - places;
-            if (i < n_items) (single ? dec : pr)[first + i] = it;
-            before += __shfl_sync(0xffffffffu, incl, 31);
+    const int half_threads = gridDim.x * (TB_THREADS / 2);
+    const int half = blockIdx.x * (TB_THREADS / 2) + tid % (TB_THREADS / 2);
+    if (tid < TB_THREADS / 2) {
+        // tokens.  A page of the batch is taken from the stack directly; an old one from the block table
+        for (int t = half; t < T; t += half_threads) {
+            int32_t pos = 0, slot = -1;
+            if (t < tokens) {
+                const int r = upper_bound(end, R, t);
+                const int64_t p64 = (int64_t)kv[r] + (t - (r ? end[r - 1] : 0));
+                pos = (int32_t)min(p64, (int64_t)0x7fffffff);
+                if (!failed[r]) {
+                    const int32_t i = pos >> P.page_shift, old = pages_for(kv[r], P.page_shift);
+                    int32_t page;
+                    if (i < old) {
+                        page = P.block_table[r * P.ld + i];
+                    } else {
+                        const int32_t k = (r ? pages[r - 1] : 0) + i - old;
+                        page = P.free_pages[count - 1 - k];
+                    }
+                    if (page >= 0 && page < P.num_pages) slot = (page << P.page_shift) + (pos & ((1 << P.page_shift) - 1));
+                }
+            }
+            P.out[P.L.position + t] = pos;
+            P.out[P.L.slot + t] = slot;
         }
-    }
-    for (int i = gt; i < spare; i += all_threads) {
-        KvItem it;
-        it.start = (R ? chunks_d[R - 1] : 0) + (1 + KV_DEC_OVER) * (int64_t)i;
-        it.req = 0;
-        it.row0 = i * P.dec_rows;
-        it.nrows = (int32_t)min((int64_t)P.dec_rows, spare_rows - it.row0);
-        it.k_lo = 0;
-        it.n = 1;
-        it.tok0 = tokens;
-        it.lim0 = -0x40000000;
-        it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
-        dec[(R ? items_d[R - 1] : 0) + i] = it;
+        for (int k = half; k < taken; k += half_threads) {
+            const int r = upper_bound(pages, R, k);
+            const int32_t i = pages_for(kv[r], P.page_shift) + k - (r ? pages[r - 1] : 0);
+            P.block_table[r * P.ld + i] = P.free_pages[count - 1 - k];
+        }
+    } else {
+        // work lists
+        for (int r = half; r < R; r += half_threads) {      // requests of single tokens: at most eight items, a thread each
+            const int32_t tok0 = r ? end[r - 1] : 0;
+            const int64_t rows = (int64_t)(end[r] - tok0) * P.group;
+            if (rows > KV_DEC_MAX_ROWS || failed[r]) continue;
+            KvItem it;
+            it.req = r;
+            it.tok0 = tok0;
+            it.lim0 = kv[r] + 1;
+            it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
+            it.start = r ? chunks_d[r - 1] : 0;
+            KvItem *to = dec + (r ? items_d[r - 1] : 0);
+            for (it.row0 = 0; it.row0 < rows; it.row0 += P.dec_rows) {
+                it.nrows = min(P.dec_rows, (int32_t)rows - it.row0);
+                item_range(it.lim0, P.group, P.window, KV_DEC_CHUNK, it.row0, it.nrows, &it.k_lo, &it.n);
+                *to++ = it;
+                it.start += it.n + KV_DEC_OVER;
+            }
+        }
+        for (int r = half >> 5; r < R && (n_failed > 0 || items_p[R - 1] > 0); r += half_threads >> 5) {      // the others: a warp each
+            const int32_t tok0 = r ? end[r - 1] : 0, q = end[r] - tok0;
+            const int64_t rows = (int64_t)q * P.group;
+            if (rows == 0 || (rows <= KV_DEC_MAX_ROWS && !failed[r])) continue;
+            const bool single = failed[r];
+            const int32_t per = single ? P.dec_rows : KV_PROMPT_ROWS;
+            const int32_t n_items = (int32_t)((rows + per - 1) / per);
+            const int32_t first = single ? (r ? items_d[r - 1] : 0) : (r ? items_p[r - 1] : 0);
+            int64_t before = single ? (r ? chunks_d[r - 1] : 0) : (r ? chunks_p[r - 1] : 0);
+            KvItem it;
+            it.req = r;
+            it.tok0 = tok0;
+            it.lim0 = failed[r] ? -0x40000000 : kv[r] + 1;
+            it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
+            for (int32_t b = 0; b < n_items; b += 32) {
+                const int32_t i = b + lane;
+                it.row0 = i * per;
+                it.nrows = (int32_t)min((int64_t)per, rows - it.row0);
+                it.n = 0;
+                it.k_lo = 0;
+                if (i < n_items)
+                    item_range(it.lim0, P.group, P.window, single ? KV_DEC_CHUNK : KV_PROMPT_CHUNK, it.row0, it.nrows,
+                               &it.k_lo, &it.n);
+                const int64_t places = i < n_items ? it.n + (single ? KV_DEC_OVER : KV_PROMPT_OVER) : 0;
+                const int64_t incl = warp_incl(places);
+                it.start = before + incl - places;
+                if (i < n_items) (single ? dec : pr)[first + i] = it;
+                before += __shfl_sync(0xffffffffu, incl, 31);
+            }
+        }
+        for (int i = half; i < spare; i += half_threads) {
+            KvItem it;
+            it.start = (R ? chunks_d[R - 1] : 0) + (1 + KV_DEC_OVER) * (int64_t)i;
+            it.req = 0;
+            it.row0 = i * P.dec_rows;
+            it.nrows = (int32_t)min((int64_t)P.dec_rows, spare_rows - it.row0);
+            it.k_lo = 0;
+            it.n = 1;
+            it.tok0 = tokens;
+            it.lim0 = -0x40000000;
+            it.reserved[0] = it.reserved[1] = it.reserved[2] = 0;
+            dec[(R ? items_d[R - 1] : 0) + i] = it;
+        }
     }
     // The first item of each walker.  A request of single tokens has at most eight items, whose places are
     // counted again; a prompt's are looked up in the list, once that is complete.
@@ -311,13 +374,14 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
         cluster_arrive();
         cluster_wait();
     }
-    for (int w = gt; w < P.dec_walkers + P.pr_walkers; w += all_threads) {
+    for (int w = prompts ? gt : half; w < P.dec_walkers + P.pr_walkers; w += prompts ? all_threads : half_threads) {
+        if (!prompts && tid < TB_THREADS / 2) break;
         const bool single = w < P.dec_walkers;
         const int32_t i = single ? w : w - P.dec_walkers;
         const int64_t pos = i * walk_span[single ? 0 : 1];
         int32_t found = -1;
         if (pos < walk_total[single ? 0 : 1]) {
-            int64_t at = pos / P.hkv;   // hkv * start <= pos  <=>  start <= at
+            int64_t at = pos >> 31 ? pos / P.hkv : (int64_t)((uint32_t)pos / (uint32_t)P.hkv);   // hkv * start <= pos  <=>  start <= at
             const int r = upper_bound(single ? chunks_d : chunks_p, R, at);
             const int32_t *items = single ? items_d : items_p;
             found = r ? items[r - 1] : 0;
@@ -360,7 +424,7 @@ __global__ void __launch_bounds__(TB_THREADS) release_kernel(const int32_t *requ
     // the first mention of a request takes it: an entry is skipped when an earlier one names the same
     for (int i = tid; i < n; i += TB_THREADS) lens[i] = requests[i];
     __syncthreads();
-    for (int i = warp; i < n; i += TB_THREADS / 32) {
+    for (int i = warp; i < n; i += TB_WARPS) {
         const int32_t r = lens[i];
         bool dup = false;
         for (int j = lane; j < i; j += 32) dup |= lens[j] == r;
@@ -380,11 +444,11 @@ __global__ void __launch_bounds__(TB_THREADS) release_kernel(const int32_t *requ
         }
     }
     __syncthreads();
-    block_scan<1>({count}, n, warp_sum);
+    block_scan(count, n, warp_sum);
     const int32_t have = min(max(*free_count, 0), num_pages);
     __syncthreads();
     int32_t lost = 0;
-    for (int i = warp; i < n; i += TB_THREADS / 32) {
+    for (int i = warp; i < n; i += TB_WARPS) {
         const int32_t r = lens[i];
         if (!take[i]) continue;
         const int32_t pages = (int32_t)min((int64_t)pages_for(max(kv_len[r], 0), page_shift), ld);

@@ -206,8 +206,8 @@ class KVCache:
         self.kv = lb.kv_create(*self.shape, self.mem, device=int(device))
         self.workspace = torch.empty(lb.kv_workspace_bytes(self.kv), dtype=torch.uint8, device=self.device)
         self._workspace_bytes = self.workspace.numel()
-        self.tables = None
-        self.R = self.T = 0
+        self.tables, self._tables_bytes = None, 0
+        self.R = self.T = -1
 
     def layer(self, layer: int) -> torch.Tensor:
         """One layer's pages as bytes (a view)."""
@@ -219,6 +219,7 @@ class KVCache:
         words = lb.kv_tables_bytes(self.kv, R, T) // 4
         if self.tables is None or self.tables.numel() < words:
             self.tables = torch.empty(words, dtype=torch.int32, device=self.device)
+            self._tables_bytes = 4 * words
             self.R = -1
         if (R, T) != (self.R, self.T):
             self.R, self.T = R, T
@@ -230,16 +231,17 @@ class KVCache:
                      window: int = 0, kv_len_out=None, free_count_out=None, stream=None) -> None:
         """Tables of a batch; kv_len and free_count are advanced in place unless *_out names other
         tensors."""
-        R = int(kv_len.shape[0])
-        if q_len.shape != (R,) or block_table.shape[0] != R:
+        R = kv_len.shape[0]
+        if q_len.shape[0] != R or block_table.shape[0] != R:
             raise ValueError("q_len and block_table need one entry and one row per request (%d)" % R)
-        self.reserve(R, T)
-        self.block_table, self.ld_table = block_table, int(block_table.stride(0))
+        if R != self.R or T != self.T:
+            self.reserve(R, T)
+        self.block_table, self.ld_table = block_table, block_table.stride(0)
         lb.kv_build_tables(self.kv, kv_len, q_len, R, T, free_pages, free_count, block_table, self.ld_table,
                            self.tables, max_q=max_q, window=window,
                            kv_len_out=kv_len if kv_len_out is None else kv_len_out,
                            free_count_out=free_count if free_count_out is None else free_count_out,
-                           stream=stream)
+                           tables_bytes=self._tables_bytes, stream=stream)
 
     def release(self, requests, kv_len, block_table, free_pages, free_count, stream=None) -> None:
         lb.kv_release(self.kv, requests, int(requests.shape[0]), int(kv_len.shape[0]), kv_len, block_table,

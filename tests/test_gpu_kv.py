@@ -609,3 +609,52 @@ def test_refusals_leave_everything_alone():
     lb.kv_append(c.kv, 0, lb.qk_args(**ok), c.slots, 0)       # nothing to do
     lb.kv_read(c.kv, 0, c.slots, 0, out, 512, None, 0)
     assert lb.launch_count() == before
+
+
+def test_layer_of_a_served_batch():
+    """The example's layer: prompts, then a mixed step, then single tokens; its attention against the definition
+    on the rows that its QKV projection (adapters included) gave."""
+    require_gpu()
+    import sys
+    import torch
+    import os
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    from attention_step import AttentionLayer
+    hq, hkv, d = 8, 2, 128
+    layer = AttentionLayer(pages=64, max_positions=256)
+    layer.admit(3, 200)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    owner = torch.tensor([0, 2, -1], dtype=torch.int32, device="cuda")
+    K, V = [np.zeros((0, hkv, d)) for _ in range(3)], [np.zeros((0, hkv, d)) for _ in range(3)]
+    qw, kw = _np(layer.q_weight), _np(layer.k_weight)
+    cs = _np(layer.angles)
+    used = 0
+    for q_len in ([40, 70, 1], [1, 33, 5], [1, 1, 1], [1, 1, 1]):
+        T = sum(q_len)
+        x = torch.randn(T, 1024, generator=g, device="cuda").bfloat16()
+        ids = torch.repeat_interleave(owner, torch.tensor(q_len, device="cuda"))
+        out, attn, qkv = layer.step(x, q_len, ids.contiguous())
+        assert torch.isfinite(out).all()
+        rows, got = _np(qkv), _np(attn).reshape(T, hq, d)
+        t0 = 0
+        for r, n in enumerate(q_len):
+            pos = np.arange(len(K[r]), len(K[r]) + n)
+            part = rows[t0:t0 + n].reshape(n, hq + 2 * hkv, d)
+            at = lambda h: cs[np.repeat(pos, h)]      # noqa: E731
+            q = ref.bf16(ref.rotate(ref.norm32(part[:, :hq].reshape(-1, d), qw, 1e-6), at(hq), d, False))
+            k = ref.rotate(ref.norm32(part[:, hq:hq + hkv].reshape(-1, d), kw, 1e-6), at(hkv), d, False)
+            for store, val in ((K, k), (V, part[:, hq + hkv:].reshape(-1, d))):
+                c, s, low = ref.quantise(val)
+                store[r] = np.concatenate([store[r], (c.astype(np.float64) * s[:, None] + low[:, None]).reshape(n, hkv, d)])
+            L = len(K[r])
+            want, _, mag = ref.attention(q.astype(np.float64).reshape(n, hq, d), K[r], V[r], np.arange(-(-L // 16))[None],
+                                         16, 1 << 20, [0, n], [L - n], d ** -0.5)
+            bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -12) * mag + 2.0 ** -25 * np.abs(V[r]).max() * L
+            assert (np.abs(got[t0:t0 + n] - want) <= bound).all()
+            t0 += n
+    used = sum(-(-len(k) // 16) for k in K)
+    assert int(layer.free_count) == 64 - used
+    layer.release([0, 1, 2])
+    assert int(layer.free_count) == 64 and sorted(_np(layer.free).tolist()) == list(range(64))
+    assert layer.kv.status()[:2] == [0, 0]
+    layer.close()

@@ -26,6 +26,8 @@
 // kept by a common power of two of the value rows seen so far, raised like the maximum.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include <type_traits>
 
 #include "fused_ptx.cuh"
@@ -64,6 +66,11 @@ struct DecCfg {
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
@@ -442,11 +449,24 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                 for (int b = 0; b < 2; ++b) {
                     const uint32_t cell = base + b * C::CELL + KV_CELL * (D / 2);
                     uint32_t pb[NT][2];
-                    float vs[2], vz[2];
+                    // A row's value is s (c + low / s).  Where the low values are no more than a few steps off, they
+                    // are added with the probability as it was rounded for the codes, so that its rounding counts
+                    // with the value itself and not with c - 8, which may be much larger; where one is further off
+                    // (or a scale is zero beside a low that is not), with the probability before the rounding.
+                    float vs[2], add[2];
+                    bool near = true;
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        vs[r] = __uint_as_float(vp_[b][r] << 16) * unit;
-                        vz[r] = fmaf(8.0f, vs[r], __uint_as_float(vp_[b][r] & 0xffff0000u) * unit);
+                        const float s = __uint_as_float(vp_[b][r] << 16), low = __uint_as_float(vp_[b][r] & 0xffff0000u);
+                        vs[r] = s * unit;
+                        add[r] = fmaf(low, rcp_approx(s), 8.0f);
+                        if (!WHOLE && vp_[b][r] == 0) add[r] = 0.0f;
+                        near = near && fabsf(add[r]) <= 16.0f;
+                    }
+                    const bool far = !__all_sync(0xffffffffu, near);
+                    if (far) {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) add[r] = fmaf(8.0f, vs[r], __uint_as_float(vp_[b][r] & 0xffff0000u) * unit);
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -454,17 +474,27 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                         for (int r = 0; r < 2; ++r) {
                             const float p0 = exp2_approx(fmaf(x[n][b][2 * r], qx[n][0], nm[n][0]));
                             const float p1 = exp2_approx(fmaf(x[n][b][2 * r + 1], qx[n][1], nm[n][1]));
-                            float q0 = p0 * vs[r], q1 = p1 * vs[r], z0 = p0 * vz[r], z1 = p1 * vz[r];
+                            float q0 = p0 * vs[r], q1 = p1 * vs[r];
+                            bool h0 = false, h1 = false;
                             if (!WHOLE) {     // a value row's NaN counts only where it is seen
-                                const bool h0 = x[n][b][2 * r] == -INFINITY, h1 = x[n][b][2 * r + 1] == -INFINITY;
-                                q0 = h0 ? 0.0f : q0; z0 = h0 ? 0.0f : z0;
-                                q1 = h1 ? 0.0f : q1; z1 = h1 ? 0.0f : z1;
+                                h0 = x[n][b][2 * r] == -INFINITY;
+                                h1 = x[n][b][2 * r + 1] == -INFINITY;
+                                q0 = h0 ? 0.0f : q0;
+                                q1 = h1 ? 0.0f : q1;
                             }
                             l[n][0] += p0;
                             l[n][1] += p1;
-                            z[n][0] += z0;
-                            z[n][1] += z1;
-                            pb[n][r] = movmatrix_trans(pack_f16(q0, q1));
+                            const uint32_t ph = pack_f16(q0, q1);
+                            float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&ph));
+                            if (far) f = make_float2(p0, p1);
+                            if (WHOLE) {
+                                z[n][0] = fmaf(f.x, add[r], z[n][0]);
+                                z[n][1] = fmaf(f.y, add[r], z[n][1]);
+                            } else {
+                                z[n][0] += h0 ? 0.0f : f.x * add[r];
+                                z[n][1] += h1 ? 0.0f : f.y * add[r];
+                            }
+                            pb[n][r] = movmatrix_trans(ph);
                         }
                         const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
                         mma16816_f16(sp[n], ones, pb[n][0], pb[n][1]);

@@ -658,3 +658,60 @@ def test_layer_of_a_served_batch():
     assert int(layer.free_count) == 64 and sorted(_np(layer.free).tolist()) == list(range(64))
     assert layer.kv.status()[:2] == [0, 0]
     layer.close()
+
+
+def test_pages_beyond_four_gigabytes():
+    """Byte offsets of pages pass 32 bits: a cache of 4.6 GB of which the last pages are used."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    n, P, hkv, D, T = 33000, 128, 8, 128, 300
+    rng = np.random.default_rng(21)
+    with _cache(num_pages=n, page_size=P, num_q_heads=hkv, num_kv_heads=hkv, head_dim=D) as c:
+        assert c.mem.numel() > 1 << 32
+        x = ref.bf16(rng.standard_normal((T, 3 * hkv * D)).astype(np.float32))
+        xd = _dev(x, torch.bfloat16)
+        free, cnt = _i32(np.arange(n)), _i32([n])                     # the stack's top is the last page
+        kv, table = _i32([0, 0]), _i32(np.full((2, 4), -1))
+        c.build_tables(kv, _i32([T - 1, 1]), T, free, cnt, table)
+        assert _np(table)[0, 0] == n - 1 and _np(c.slots).max() == n * P - 1
+        q = torch.empty((T, hkv * D), dtype=torch.bfloat16, device="cuda")
+        w = 3 * hkv * D
+        c.append(0, lb.qk_args(num_q_heads=hkv, num_kv_heads=hkv, head_dim=D, q=xd, ldq=w, k=xd[:, hkv * D:], ldk=w,
+                               v=xd[:, 2 * hkv * D:], ldv=w, q_out=q))
+        out = torch.empty_like(q)
+        c.attention(0, q, out, scale=D ** -0.5)
+        got = _np(out).reshape(T, hkv, D)
+        vals = []
+        for part in (x[:, hkv * D:2 * hkv * D], x[:, 2 * hkv * D:]):
+            code, s, low = ref.quantise(part.reshape(-1, D))
+            vals.append((code.astype(np.float64) * s[:, None] + low[:, None]).reshape(T, hkv, D))
+        back = torch.empty_like(q)
+        c.read(0, c.slots, None, back)
+        assert np.array_equal(_np(back), ref.bf16(vals[1].astype(np.float32)).reshape(T, -1))
+        want, _, mag = ref.attention(x[:, :hkv * D].astype(np.float64).reshape(T, hkv, D), vals[0], vals[1],
+                                     np.arange(3)[None], P, 1 << 20, [0, T - 1], [0], D ** -0.5)
+        bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2.0 ** -12) * mag + 2.0 ** -25 * np.abs(vals[1]).max() * T
+        assert (np.abs(got - want)[:T - 1] <= bound[:T - 1]).all()
+        # the request of one token sees itself alone
+        assert (np.abs(got[T - 1] - vals[1][T - 1]) <= 2.0 ** -8 * np.abs(vals[1][T - 1]) + 2.0 ** -10 * np.abs(vals[1][T - 1])).all()
+        assert c.status()[:2] == [0, 0]
+
+
+@pytest.mark.parametrize("lens,hq,hkv,P", [
+    ([(20000, 1)], 1, 1, 128),                                        # one pair, hundreds of pieces
+    ([(9000, 1), (3, 1)], 3, 1, 16),
+    ([(k % 37, 1) for k in range(700)], 4, 4, 16),                    # more pairs than warps
+    ([(k % 5, 17 + k % 3) for k in range(60)], 4, 2, 16),             # many prompts of one chunk
+    ([(0, 0), (0, 0), (5000, 80)], 2, 1, 64), ([(6, 33), (0, 1500)], 1, 1, 32)])
+def test_walks_of_every_shape(lens, hq, hkv, P):
+    require_gpu()
+    Batch(lens, hq, hkv, 64, P, seed=len(lens), max_q=max(q for _, q in lens)).check()
+
+
+def test_scale_zero_and_negative():
+    """scale 0: the mean of the values; a negative scale turns the scores."""
+    require_gpu()
+    for lens in ([(70, 1)], [(10, 90)]):
+        Batch(lens, 4, 2, 128, seed=30, scale=0.0).check()
+        Batch(lens, 4, 2, 128, seed=31, scale=-0.1).check()

@@ -597,32 +597,37 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnParams P) {
     const int64_t total = (int64_t)(uint32_t)w01.x | ((int64_t)w01.y << 32), span = (int64_t)(uint32_t)w01.z | ((int64_t)w01.w << 32);
     const KvItem *items = reinterpret_cast<const KvItem *>(P.tables + (PROMPT ? P.L.pr_items : P.L.dec_items));
     KvItem it;
-    int32_t head;
-    int64_t begin, w;
+    int32_t head = 0;
+    int64_t begin = 0, w = blockIdx.x;
+    bool mine = false;       // this block has a pair to join
     if (PAIRS) {
         const int32_t item = blockIdx.x / P.kv.hkv;
-        if (item >= w23.x) return;
-        it = load_item(items + item);
-        head = blockIdx.x % P.kv.hkv;
-        begin = P.kv.hkv * it.start + (int64_t)head * (it.n + OVER) + OVER;
-        w = begin / span;
-        if (begin + it.n <= (w + 1) * span) return;
+        if (item < w23.x) {
+            it = load_item(items + item);
+            head = blockIdx.x % P.kv.hkv;
+            begin = P.kv.hkv * it.start + (int64_t)head * (it.n + OVER) + OVER;
+            w = begin / span;
+            mine = begin + it.n > (w + 1) * span;
+        }
     } else {
-        w = blockIdx.x;
         const int64_t cut = (w + 1) * span;
-        if (cut >= total) return;
-        it = load_item(items + __ldg(P.tables + (PROMPT ? P.L.pr_first : P.L.dec_first) + w + 1));
-        const int64_t off = cut - P.kv.hkv * it.start;
-        head = (int32_t)(off / (it.n + OVER));
-        begin = P.kv.hkv * it.start + (int64_t)head * (it.n + OVER) + OVER;      // its first chunk
-        if (begin >= cut || begin < w * span || begin + it.n <= cut) return;     // nothing crosses this end, or another block has it
+        if (cut < total) {
+            it = load_item(items + __ldg(P.tables + (PROMPT ? P.L.pr_first : P.L.dec_first) + w + 1));
+            const int64_t off = cut - P.kv.hkv * it.start;
+            head = (int32_t)(off / (it.n + OVER));
+            begin = P.kv.hkv * it.start + (int64_t)head * (it.n + OVER) + OVER;      // its first chunk
+            mine = begin < cut && begin >= w * span && begin + it.n > cut;     // else nothing crosses this end, or another block has it
+        }
     }
+    // Every block waits, those without work too: what follows on the stream may in its turn wait for no more
+    // than this kernel.
+    griddep_wait();
+    if (!mine) return;
     const int32_t row = PAIRS ? (int32_t)blockIdx.y : (int32_t)blockIdx.y * 8 + warp;
     if (row >= it.nrows) return;
     const int32_t pieces = (int32_t)((begin + it.n - 1) / span - w) + 1;
     // piece i is walker w + i's: its second slot where it begins the pair (i = 0), else its first
     auto slot = [&](int i) { return (2 * (w + i) + (i == 0 ? 1 : 0)) * ROWS + row; };
-    griddep_wait();
     // maximum, sum and outputs of eight pieces at a time, all requested before the first is used
     float m = -INFINITY, l = 0.0f, a[E];
 #pragma unroll

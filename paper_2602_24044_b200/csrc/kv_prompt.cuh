@@ -16,11 +16,12 @@
 // alternate, and everything else on warps of its own:
 //   warps 0-3, 4-7   softmax of tile 0, tile 1: a thread is a row; scores from tensor memory to registers,
 //                    probabilities back to the same tensor-memory columns, which the second product reads
-//                    as its A operand; rescales the accumulator itself when its maximum was raised
+//                    as its A operand; rescales the accumulator itself when its maximum was raised; brings its
+//                    row of the next (item, head)'s queries while the last products of this one run (a warp that
+//                    brought them for 128 rows was 4.5 us a pair)
 //   warps 8-11       widen the codes of a block of keys, K and V, into three swizzled tiles (order K0 V0 K1 ..)
 //   warp 12          issues the matrix products
 //   warp 13          requests the cells (bulk copies), two blocks ahead
-//   warps 14, 15     bring the queries of the next (item, head), tile 0, tile 1
 // The (item, head, block) triples form one walk cut into equal spans, one per SM; what a span's ends cut is
 // joined afterwards.  Tensor memory: scores of both tiles (2 x 128 columns), accumulators (2 x head_dim).
 #pragma once
@@ -141,9 +142,6 @@ __device__ __forceinline__ void sts_v4(uint32_t addr, const uint32_t (&v)[4]) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
                  : "memory");
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {   // the rest becomes zero
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 }  // namespace tcp
 
 __device__ __forceinline__ uint32_t half2_of(float x) { return pack_f16(x, x); }
@@ -173,7 +171,7 @@ __device__ __forceinline__ uint32_t low_bits(int32_t n) {
     return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
 }
 
-constexpr int PK_THREADS = 512, PK_TILES = 3, PK_RAW = 2, PK_INFO = 3;
+constexpr int PK_THREADS = 448, PK_TILES = 3, PK_RAW = 2, PK_INFO = 3;
 constexpr int PK_EXTRA = 128 * 16 * 2;       // 16 more columns of 128 rows, as core matrices
 
 struct PromptInfo {          // of a block of keys, from the widening warps to the softmax
@@ -240,8 +238,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
     uint64_t *s_full = kv_empty + PK_TILES;       // [2] scores of a tile are in tensor memory
     uint64_t *p_ready = s_full + 2;               // [2] probabilities are
     uint64_t *o_full = p_ready + 2;               // [2] the accumulator of an (item, head) is complete
-    uint64_t *q_here = o_full + 2;                // [2] queries are in shared memory as they came
-    uint64_t *q_ready = q_here + 2;               // [2] and as fp16
+    uint64_t *q_ready = o_full + 2;               // [2] queries are in shared memory
     uint64_t *q_free = q_ready + 2;               // [2] the last score product of an (item, head) is done
     uint64_t *info_full = q_free + 2;
     uint64_t *info_empty = info_full + PK_INFO;
@@ -269,7 +266,6 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[i], 128);
             mbar_init(&o_full[i], 1);
-            mbar_init(&q_here[i], 1);
             mbar_init(&q_ready[i], 128);
             mbar_init(&q_free[i], 1);
         }
@@ -305,37 +301,42 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         const int t = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
-        // The queries of a pair: bf16 as they came -> fp16 divided by a power of two, in place, and the row's
-        // sum in parts; returns log2(e) |scale| times that power.  (A negative scale turns the queries.)
-        auto take_queries = [&](uint32_t pair, bool &ok) -> float {
-            ok = wait(&q_here[t], pair & 1u);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) return 0.0f;
-            const uint32_t q_at = smem_u32(smem) + t * C::TILE + row * 128;
-            uint32_t most = 0;
-#pragma unroll 4
-            for (int i = 0; i < D / 8; ++i) {
-                uint32_t v[4];
-                lds_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), v);
+        // The queries of a pair: this thread's row from memory (all of it requested at once, before the wait for the
+        // pair before it), as fp16 divided by a power of two, and the row's sum in parts; returns log2(e) |scale|
+        // times that power.  (A negative scale turns the queries.)
+        auto take_queries = [&](const KvItem &it, int32_t head, uint32_t pair, bool &ok) -> float {
+            const int32_t r = it.row0 + t * 128 + row, tok = it.tok0 + r / group;
+            const uint4 *src = reinterpret_cast<const uint4 *>(P.q + tok * P.ldq + (int64_t)(head * group + r % group) * D);
+            uint4 v[D / 8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) most = max(most, max((v[e] << 16) & 0x7fff0000u, v[e] & 0x7fff0000u));
+            for (int i = 0; i < D / 8; ++i) v[i] = t * 128 + row < it.nrows ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+                const uint32_t h = max_u16x2(max_u16x2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu),
+                                             max_u16x2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
+                most = max_u16x2(most, h);
             }
+            most = max(most << 16, most & 0xffff0000u);
             const int a = most >= 0x7f800000u ? 0 : max((int)(most >> 23) - 126, -126);     // |q| < 2^a
             const float unit = copysignf(pow2(max(-a, -126)), P.scale2);
+            if (pair > 0) ok = ok && wait(&q_free[t], (pair - 1) & 1u);
+            const uint32_t q_at = smem_u32(smem) + t * C::TILE + row * 128;
             float sum = 0.0f;
-#pragma unroll 4
+#pragma unroll
             for (int i = 0; i < D / 8; ++i) {
-                const uint32_t at = q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4);
-                uint32_t v[4];
-                lds_v4(at, v);
+                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                uint32_t o[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float lo = __uint_as_float(v[e] << 16) * unit, hi = __uint_as_float(v[e] & 0xffff0000u) * unit;
+                    const float lo = __uint_as_float(w[e] << 16) * unit, hi = __uint_as_float(w[e] & 0xffff0000u) * unit;
                     sum += lo + hi;
-                    v[e] = pack_f16(lo, hi);
+                    o[e] = pack_f16(lo, hi);
                 }
-                tcp::sts_v4(at, v);
+                if (ok) tcp::sts_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), o);
             }
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return 0.0f;
             const Split q = split_f16(sum);
             const uint32_t qx[4] = {pack_f16(q.h, q.h), pack_f16(q.l, q.l), pack_f16(q.h, q.t), 0u};
             tcp::sts_v4(smem_u32(smem) + C::OFF_QX + t * PK_EXTRA + (row >> 3) * 128 + (row & 7) * 16, qx);
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         };
         uint32_t j = 0, pair = 0;
         bool ok = true;
-        float q_unit = take_queries(0, ok);
+        float q_unit = take_queries(cur.it, cur.head, 0, ok);
         for (; ok && cur.more(); ++pair) {
             const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
             const int32_t r = cur.it.row0 + t * 128 + row;
@@ -455,7 +456,11 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             if (!ok) break;
             // the next pair's queries, while the last product runs
             float next_unit = 0.0f;
-            if (cur.another_pair()) next_unit = take_queries(pair + 1, ok);
+            if (cur.another_pair()) {
+                const bool same = cur.head + 1 < cur.hkv;
+                const KvItem next = same ? cur.it : load_item(items + cur.index + 1);
+                next_unit = take_queries(next, same ? cur.head + 1 : 0, pair + 1, ok);
+            }
             if (!ok) break;
             // ---- the (item, head) is over, or the span is ------------------------------------------
             ok = wait(&o_full[t], pair & 1u);
@@ -737,51 +742,6 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 *failed = 1;
                 // copies on their way must land before the block leaves
                 for (uint32_t i = j > PK_RAW ? j - PK_RAW : 0; i < j; ++i) mbar_wait(&raw_full[i % PK_RAW], (i / PK_RAW) & 1u);
-            }
-        } else {
-            // ======================= queries: warp 14 tile 0, warp 15 tile 1 ========================
-            const int t = warp - 14;
-            constexpr int LPR = D / 8;                 // 16-byte runs of a row
-            const uint32_t q_at = smem_u32(smem) + t * C::TILE;
-            uint32_t pair = 0;
-            bool ok = true;
-            for (; ok && cur.more(); ++pair) {
-                const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
-                if (pair > 0) {
-                    // rows of this pair to L2 while the queries before them are still in use
-                    for (int row = lane; row < min(128, cur.it.nrows - t * 128); row += 32) {
-                        const int32_t r = cur.it.row0 + t * 128 + row;
-                        const __nv_bfloat16 *src =
-                            P.q + (cur.it.tok0 + r / group) * P.ldq + (int64_t)(cur.head * group + r % group) * D;
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(src));
-                        if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + 64));
-                    }
-                    ok = wait(&q_free[t], (pair - 1) & 1u);
-                }
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                // lane: run k of rows first, first + step, ..; token and head of a row follow by counting (a
-                // division a row made this 20 us a pair)
-                constexpr int STEP = 32 / LPR;
-                const int k = lane % LPR, first_row = lane / LPR;
-                const uint32_t to = q_at + (k >> 3) * 16384;
-                const int32_t r0 = cur.it.row0 + t * 128 + first_row;
-                int32_t tok = r0 / group, h = r0 - tok * group;
-                const __nv_bfloat16 *src = P.q + (int64_t)cur.head * group * D + k * 8;
-                const int32_t left = cur.it.nrows - t * 128;
-#pragma unroll 4
-                for (int row = first_row; row < 128; row += STEP) {
-                    const bool live = row < left;
-                    tcp::cp_async16(to + row * 128 + (((k & 7) ^ (row & 7)) << 4),
-                                    live ? src + (cur.it.tok0 + tok) * P.ldq + h * D : P.q, live ? 16 : 0);
-                    h += STEP;
-                    while (h >= group) { h -= group; ++tok; }
-                }
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&q_here[t]);
-                cur.next_pair(c1 - c0);
             }
         }
     }

@@ -301,42 +301,64 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         const int t = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * D;
-        // The queries of a pair: this thread's row from memory (all of it requested at once, before the wait for the
-        // pair before it), as fp16 divided by a power of two, and the row's sum in parts; returns log2(e) |scale|
-        // times that power.  (A negative scale turns the queries.)
+        // The queries of a pair.  A warp requests its 32 rows (whole lines; before the wait for the pair before
+        // it), lays them out as they came, and then every thread takes its own row: as fp16 divided by a power of
+        // two, in place, and its sum in parts.  Returns log2(e) |scale| times that power.  (A negative scale turns
+        // the queries.)
         auto take_queries = [&](const KvItem &it, int32_t head, uint32_t pair, bool &ok) -> float {
-            const int32_t r = it.row0 + t * 128 + row, tok = it.tok0 + r / group;
-            const uint4 *src = reinterpret_cast<const uint4 *>(P.q + tok * P.ldq + (int64_t)(head * group + r % group) * D);
-            uint4 v[D / 8];
+            constexpr int LPR = D / 8, RPI = 32 / LPR;       // lanes of a row, rows of a request
+            const int run = lane % LPR;
+            const uint32_t tile = smem_u32(smem) + t * C::TILE;
+            {
+                uint4 v[LPR];
+                const int32_t my0 = t * 128 + (warp & 3) * 32 + lane / LPR;
+                const int32_t r0 = it.row0 + my0;
+                int32_t tok = r0 / group, h = r0 - tok * group;
+                const __nv_bfloat16 *src = P.q + it.tok0 * P.ldq + (int64_t)head * group * D + run * 8;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) v[i] = t * 128 + row < it.nrows ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+                for (int i = 0; i < LPR; ++i) {
+                    v[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (my0 + i * RPI < it.nrows) v[i] = __ldg(reinterpret_cast<const uint4 *>(src + tok * P.ldq + h * D));
+                    h += RPI;
+                    while (h >= group) { h -= group; ++tok; }
+                }
+                if (pair > 0) ok = ok && wait(&q_free[t], (pair - 1) & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) return 0.0f;
+#pragma unroll
+                for (int i = 0; i < LPR; ++i) {
+                    const int rr = (warp & 3) * 32 + lane / LPR + i * RPI;
+                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                    tcp::sts_v4(tile + (run >> 3) * 16384 + rr * 128 + (((run & 7) ^ (rr & 7)) << 4), w);
+                }
+            }
+            __syncwarp();
+            const uint32_t q_at = tile + row * 128;
             uint32_t most = 0;
-#pragma unroll
+#pragma unroll 4
             for (int i = 0; i < D / 8; ++i) {
-                const uint32_t h = max_u16x2(max_u16x2(v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu),
-                                             max_u16x2(v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu));
-                most = max_u16x2(most, h);
+                uint32_t v[4];
+                lds_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), v);
+                most = max_u16x2(most, max_u16x2(max_u16x2(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu),
+                                                 max_u16x2(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu)));
             }
             most = max(most << 16, most & 0xffff0000u);
             const int a = most >= 0x7f800000u ? 0 : max((int)(most >> 23) - 126, -126);     // |q| < 2^a
             const float unit = copysignf(pow2(max(-a, -126)), P.scale2);
-            if (pair > 0) ok = ok && wait(&q_free[t], (pair - 1) & 1u);
-            const uint32_t q_at = smem_u32(smem) + t * C::TILE + row * 128;
             float sum = 0.0f;
-#pragma unroll
+#pragma unroll 4
             for (int i = 0; i < D / 8; ++i) {
-                const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                uint32_t o[4];
+                const uint32_t at = q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4);
+                uint32_t v[4];
+                lds_v4(at, v);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float lo = __uint_as_float(w[e] << 16) * unit, hi = __uint_as_float(w[e] & 0xffff0000u) * unit;
+                    const float lo = __uint_as_float(v[e] << 16) * unit, hi = __uint_as_float(v[e] & 0xffff0000u) * unit;
                     sum += lo + hi;
-                    o[e] = pack_f16(lo, hi);
+                    v[e] = pack_f16(lo, hi);
                 }
-                if (ok) tcp::sts_v4(q_at + (i >> 3) * 16384 + (((i & 7) ^ (row & 7)) << 4), o);
+                tcp::sts_v4(at, v);
             }
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) return 0.0f;
             const Split q = split_f16(sum);
             const uint32_t qx[4] = {pack_f16(q.h, q.h), pack_f16(q.l, q.l), pack_f16(q.h, q.t), 0u};
             tcp::sts_v4(smem_u32(smem) + C::OFF_QX + t * PK_EXTRA + (row >> 3) * 128 + (row & 7) * 16, qx);

@@ -2,10 +2,12 @@
 // pieces that both attention kernels leave.
 //
 //   o = sum_t p_t v_t / sum_t p_t ,  p_t = 2^(x_t - m) ,  x_t = log2(e) scale q . k_t
-//   k_t = low_t + s_t c_t :   q . k_t = s_t (q . (c_t - 8)) + (low_t + 8 s_t) sum(q)
-//   sum_t p_t v_t = sum_t (p_t s_t) (c_t - 8) + sum_t p_t (low_t + 8 s_t)
-// so a code is widened to c - 8 (exact in bf16 and fp16) and never multiplied by its scale: the scale
-// enters once per score and once per probability, and the low values of the values add one number per row.
+//   k_t = low_t + s_t c_t :   q . k_t = s_t (q . c_t) + low_t sum(q)
+//   sum_t p_t v_t = sum_t (p_t s_t) c_t - 8 sum_t (p_t s_t) + sum_t p_t (low_t + 8 s_t)
+// so a code is never multiplied by its scale: the scale enters once per score and once per probability, and
+// the low values of the values add one number per row.  (The middle sum, over the rounded p s, centres the
+// codes, and the last one is taken over the rounded p s as well where that is exact enough: a rounding of p
+// then counts v_t times.)
 //
 // What bounds it: every key costs head_dim + 8 bytes, and each of its codes has to be widened for the
 // tensor cores whatever the number of query heads is; 1.2 instructions a code (to c - 8 in bf16 and fp16)
@@ -24,6 +26,10 @@
 // and the accumulators are rescaled once in a while instead of once a chunk.  p_t s_t is rounded to fp16
 // (11 bits, where bf16 would add as much error as the output's own rounding has); its exponent range is
 // kept by a common power of two of the value rows seen so far, raised like the maximum.
+//
+// Measured: 256 requests of 256..8192 keys (638 MB) 159 us with the joining, 4.0 TB/s; four requests of
+// 60k..131k keys (397 MB) 100 us.  About 560 instructions a chunk at 2.2 a cycle and SM: the chain of each warp
+// and the integer pipe (over half busy) are what is left, not the memory.
 #pragma once
 
 #include <cuda_fp16.h>

@@ -110,9 +110,8 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     P.walkers = kv->dec_walkers();
     P.part = (float *)workspace;
     P.part_ml = (float2 *)(P.part + (size_t)2 * P.walkers * rows * kv->d);
-    // (item, head) pairs that can be in the list: one item a request where a request's rows fit one
-    const int64_t pairs = ((int64_t)rec->max_q * kv->group <= rows ? (int64_t)R
-                                                                   : R + (int64_t)T * kv->group / rows) * kv->hkv;
+    // (item, head) pairs that can be in the list (a failed request's rows are items too, however many)
+    const int64_t pairs = (R + 1 + (int64_t)T * kv->group / rows) * kv->hkv;
     DeviceGuard g(kv->device);
     lora_status_t s = kv->d == 64 ? (rows == 8 ? launch_decode<64, 1>(kv, P, pairs, (cudaStream_t)stream)
                                                : launch_decode<64, 2>(kv, P, pairs, (cudaStream_t)stream))

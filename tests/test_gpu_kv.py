@@ -715,3 +715,10 @@ def test_scale_zero_and_negative():
     for lens in ([(70, 1)], [(10, 90)]):
         Batch(lens, 4, 2, 128, seed=30, scale=0.0).check()
         Batch(lens, 4, 2, 128, seed=31, scale=-0.1).check()
+
+
+def test_pieces_behind_a_failed_request_are_joined():
+    """A request of 60 tokens fails (max_q 1) and leaves more items than there are requests; the long one behind
+    it is cut into pieces all the same."""
+    require_gpu()
+    Batch([(3, 60), (3000, 1)], 8, 1, 128, max_q=1, seed=40).check()

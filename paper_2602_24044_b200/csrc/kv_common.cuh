@@ -141,17 +141,21 @@ struct lora_kv {
     bool decode_attr[4] = {false, false, false, false};   // attributes set: head_dim 64 / 128, 8 / 16 rows
     bool prompt_attr[2] = {false, false};
     size_t tables_attr_smem = 0;      // dynamic shared memory the table builder has been allowed
-    std::vector<lora::KvTableRecord> tables;
+    // tables built through this handle, the oldest forgotten first (a fixed array: no call allocates)
+    static constexpr int32_t MAX_TABLES = 256;
+    lora::KvTableRecord tables[MAX_TABLES];
+    int32_t n_tables = 0, next_table = 0;
 
     void remember(const void *ptr, int32_t R, int32_t T, int32_t max_q, int32_t window) {
-        for (lora::KvTableRecord &t : tables)
-            if (t.ptr == ptr) { t = {ptr, R, T, max_q, window}; return; }
-        if (tables.size() >= 256) tables.erase(tables.begin());
-        tables.push_back({ptr, R, T, max_q, window});
+        for (int32_t i = 0; i < n_tables; ++i)
+            if (tables[i].ptr == ptr) { tables[i] = {ptr, R, T, max_q, window}; return; }
+        tables[next_table] = {ptr, R, T, max_q, window};
+        next_table = (next_table + 1) % MAX_TABLES;
+        if (n_tables < MAX_TABLES) ++n_tables;
     }
     const lora::KvTableRecord *find(const void *ptr, int32_t R, int32_t T) const {
-        for (const lora::KvTableRecord &t : tables)
-            if (t.ptr == ptr && t.R == R && t.T == T) return &t;
+        for (int32_t i = 0; i < n_tables; ++i)
+            if (tables[i].ptr == ptr && tables[i].R == R && tables[i].T == T) return &tables[i];
         return nullptr;
     }
     lora::KvView view(int32_t layer) const;

@@ -14,9 +14,12 @@
 
 namespace lora {
 
-// Passes of a warp when there are many rows: 2 / 3 / 4 passes 65.9 / 59.8 / 64.4 us (norm and rotation of 12936
-// tokens, 10 passes a token), 104 / 101 / 103 us (12 passes, with the cache, and the read back).
-constexpr int ROWS_NP = 3;
+// Passes of a warp when there are many rows, and blocks of an SM that the registers have to leave room for.
+// Norm and rotation of 12936 tokens (10 passes a token) / with the cache and the read back (12 passes), us:
+//   no bound on registers:  2 passes 65.9 / 104   3 passes 59.8 / 101   4 passes 64.4 / 103
+//   three blocks:           2 passes 59.1 / 102   3 passes 58.3 / 92.2
+//   four blocks:            2 passes 57.9 / 106   3 passes 63.9 / 100
+constexpr int ROWS_NP = 3, ROWS_BLOCKS = 3;
 struct RowParams {
     const __nv_bfloat16 *q, *k, *v, *qw, *kw;
     const float *cos_sin;
@@ -217,7 +220,7 @@ __device__ __forceinline__ void quantise_row(const Row &x, uint32_t &wa, uint32_
 // angles and rows one after the other were 2 us a warp with 2 KB on their way (prefill of 12936 tokens:
 // 94 us a launch, 187 with the cache; bytes alone 41 and 40).
 template <int D, int ROT, bool CACHE, int NP>
-__global__ void __launch_bounds__(256) rows_kernel(const RowParams P) {
+__global__ void __launch_bounds__(256, ROWS_BLOCKS) rows_kernel(const RowParams P) {
     constexpr int LPH = D / 16, HPP = 32 / LPH;     // lanes of a head, heads of a pass
     const int lane = threadIdx.x & 31, j = lane % LPH, g = lane / LPH;
     const int heads = P.hq + P.hk + (CACHE ? P.hk : 0);

@@ -140,7 +140,7 @@ struct lora_kv {
     int32_t sm_count = 148;
     bool decode_attr[4] = {false, false, false, false};   // attributes set: head_dim 64 / 128, 8 / 16 rows
     bool prompt_attr[2] = {false, false};
-    size_t tables_attr_smem = 0;      // dynamic shared memory the table builder has been allowed
+    bool tables_attr = false;
     // tables built through this handle, the oldest forgotten first (a fixed array: no call allocates)
     static constexpr int32_t MAX_TABLES = 256;
     lora::KvTableRecord tables[MAX_TABLES];

@@ -24,6 +24,9 @@ struct TableParams {
     KvTables L;
 };
 
+// Dynamic shared memory of a batch of R requests, as the kernel carves it up.
+constexpr size_t tables_smem(int32_t R) { return (size_t)R * (2 * 8 + 6 * 4) + 2 * 32 * 8 + 2 * 32 * 4; }
+
 // Sums that stay at the largest int32 once they pass it (with lengths that are not negative: associative).
 __device__ __forceinline__ int32_t plus(int32_t a, int32_t b) {
     return (int32_t)min((uint32_t)a + (uint32_t)b, 0x7fffffffu);
@@ -530,15 +533,16 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
     P.dec_rows = kv->dec_rows();
     P.dec_walkers = kv->dec_walkers();
     P.pr_walkers = kv->pr_walkers();
-    const size_t smem = (size_t)R * (2 * 8 + 6 * 4) + 2 * 32 * 8 + 2 * 32 * 4;
-    if (smem > kv->tables_attr_smem) {
-        LORA_CUDA_TRY(cudaFuncSetAttribute(build_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        kv->tables_attr_smem = smem;
+    // The limit belongs to the function, so every handle sets the same one: what the largest batch needs.
+    if (!kv->tables_attr) {
+        LORA_CUDA_TRY(cudaFuncSetAttribute(build_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)tables_smem(KV_MAX_REQUESTS)));
+        kv->tables_attr = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(TB_BLOCKS);
     cfg.blockDim = dim3(TB_THREADS);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = tables_smem(R);
     cfg.stream = (cudaStream_t)stream;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;

@@ -1,0 +1,27 @@
+"""The paged 4-bit cache on the GPU where it went wrong, or was never run: several handles at once, tables in
+turn, probabilities far below the largest, groups of every size, batches of many rows."""
+import numpy as np
+import pytest
+
+import kv_ref as ref
+from gpu_util import require_gpu
+from test_gpu_kv import Batch, _angles, _cache, _dev, _i32, _np
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("large,small", [(2000, 3), (100, 16)])
+def test_two_caches_build_tables_in_turn(large, small):
+    """A cache that has built small tables does not take from another what its large ones need."""
+    require_gpu()
+
+    def build(c, R):
+        kv, q = np.arange(R) % 31, np.ones(R, int)
+        table = np.zeros((R, 3), np.int32)
+        c.build_tables(_i32(kv), _i32(q), R, _i32(np.arange(64)), _i32([0]), _i32(table))
+        return _np(c.slots).tolist(), ref.tables(kv, q, R, 16, np.arange(64), 0, table, 64)["slot"]
+
+    with _cache() as a, _cache() as b:
+        for c, R in ((a, large), (b, small), (a, large), (b, large), (a, small), (b, large)):
+            got, want = build(c, R)
+            assert got == want, (R, c is a)

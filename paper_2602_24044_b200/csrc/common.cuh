@@ -35,6 +35,19 @@ inline lora_status_t count_launch() {
     return e == cudaSuccess ? LORA_OK : cuda_fail(e);
 }
 
+// Allows a kernel all the dynamic shared memory that a block can have on the current device.  The limit
+// belongs to the function and not to the handle that launches it: a handle that set what it needs itself
+// would take from another one's launches.
+template <typename K>
+inline cudaError_t allow_all_smem(K *kernel, int device) {
+    cudaFuncAttributes a;
+    int most = 0;
+    cudaError_t e = cudaFuncGetAttributes(&a, kernel);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)a.sharedSizeBytes);
+}
+
 // ---------------------------------------------------------------------------------------------
 // device-side pool description
 // ---------------------------------------------------------------------------------------------
@@ -158,8 +171,7 @@ struct lora_pool {
     // kernel attributes the other launchers have set for this pool's device
     bool twophase_attr_done = false;
     bool tc_attr_done[3] = {false, false, false};   // rank buckets 16, 32, 64
-    size_t seg_attr_smem = 0, seg_attr_chunked = 0;
-    size_t seg_attr_chunked_wide = 0;
+    bool seg_attr_done[3] = {false, false, false};   // list kernel, chunked with 256 and 1024 threads
 
     // Shapes of the metadata tables built through this handle (the table itself lives on the
     // device; apply calls need T and tile_m on the host to size their grids).

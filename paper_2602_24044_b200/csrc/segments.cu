@@ -456,15 +456,11 @@ lora_status_t launch_build_segments(lora_pool_t *pool, const int32_t *slot_idx_d
         if (words * sizeof(int32_t) <= 200 * 1024) {
             const size_t smem = words * sizeof(int32_t);
             const bool wide = T >= 8192;
-            size_t &attr_chunked = wide ? pool->seg_attr_chunked_wide : pool->seg_attr_chunked;
-            if (attr_chunked == 0) attr_chunked = 48 * 1024;
-            if (smem > attr_chunked) {
-                cudaError_t e = wide ? cudaFuncSetAttribute(build_segments_chunked_kernel<1024>,
-                                                            cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)
-                                     : cudaFuncSetAttribute(build_segments_chunked_kernel<256>,
-                                                            cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-                if (e != cudaSuccess) return cuda_fail(e);
-                attr_chunked = smem;
+            bool &attr_done = pool->seg_attr_done[wide ? 2 : 1];
+            if (!attr_done) {
+                LORA_CUDA_TRY(wide ? allow_all_smem(build_segments_chunked_kernel<1024>, pool->device)
+                                   : allow_all_smem(build_segments_chunked_kernel<256>, pool->device));
+                attr_done = true;
             }
             // every block builds the tables; the blocks share the writes (chunks of perm, slots)
             const int warps = wide ? 32 : 8;
@@ -487,13 +483,10 @@ lora_status_t launch_build_segments(lora_pool_t *pool, const int32_t *slot_idx_d
     const size_t fixed = 6 * (size_t)N + 2 * (size_t)meta_layout(T, N, tile_m).cap_tile;
     const int32_t staged = sizeof(int32_t) * (fixed + (size_t)T) <= 200 * 1024 ? 1 : 0;
     const size_t smem = sizeof(int32_t) * (fixed + (staged ? (size_t)T : 0));
-    size_t &attr_smem = pool->seg_attr_smem;
-    if (attr_smem == 0) attr_smem = 48 * 1024;
-    if (smem > attr_smem) {
-        cudaError_t e = cudaFuncSetAttribute(build_segments_kernel,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return cuda_fail(e);
-        attr_smem = smem;
+    bool &attr_done = pool->seg_attr_done[0];
+    if (!attr_done) {
+        LORA_CUDA_TRY(allow_all_smem(build_segments_kernel, pool->device));
+        attr_done = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid, 1, 1);

@@ -177,9 +177,9 @@ static lora_status_t launch_h(lora_pool_t *pool, FusedParams &P, int32_t C, cons
     for (int32_t i = 0; i < P.n_items; ++i) P.copy_idle |= P.item[i].in_place ? 0 : 1;
 
     lora_pool::FusedLaunchCache &lc = pool->fused_cache[H];
-    if (smem > lc.attr_smem) {
-        LORA_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        lc.attr_smem = smem;
+    if (!lc.attr_done) {
+        LORA_CUDA_TRY(allow_all_smem(kern, pool->device));
+        lc.attr_done = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3((unsigned)(32 * (nwc + 1)), 1, 1);

@@ -165,7 +165,8 @@ struct lora_pool {
     // shared-memory limit, resident clusters), per kernel variant; part of the handle, so pools
     // used from different threads share nothing.
     struct FusedLaunchCache {
-        int32_t attr_smem = 0, occ_smem = 0, occ_c = 0, occ_clusters = 0;
+        bool attr_done = false;
+        int32_t occ_smem = 0, occ_c = 0, occ_clusters = 0;
     };
     FusedLaunchCache fused_cache[3];
     // kernel attributes the other launchers have set for this pool's device

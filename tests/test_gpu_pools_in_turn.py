@@ -35,3 +35,18 @@ def test_two_pools_build_segments_in_turn(T, slots):
         torch.cuda.synchronize()
         for pool, _, _ in pools:
             lb.pool_destroy(pool)
+
+
+@pytest.mark.parametrize("kind,ranks,tuning", [("bgmv", ([64], [8]), ({}, {})), ("bgmv", ([8], [8]), ({5: 3}, {5: 2})),
+                                               ("sgmv", ([64], [8]), ({}, {}))])
+def test_two_pools_apply_in_turn(kind, ranks, tuning):
+    """Pools of different ranks or ring depths: the one whose kernels need less shared memory comes second."""
+    require_gpu()
+    from paper_2602_24044_b200 import workloads as W
+    from paper_2602_24044_b200.harness import Session, bf16_bits
+    wls = [W.make_custom(90, 512, 512, 6, r, kind=kind, scale=0.5, weight_mode="unitB", seed=60 + i, tile_m=16)
+           for i, r in enumerate(ranks)]
+    with Session(wls[0], tuning=tuning[0]) as a, Session(wls[1], tuning=tuning[1]) as b:
+        want = bf16_bits(a.apply()), bf16_bits(b.apply())
+        for s, w in ((a, want[0]), (b, want[1]), (a, want[0])):
+            assert np.array_equal(bf16_bits(s.apply()), w)

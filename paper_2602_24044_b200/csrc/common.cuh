@@ -21,6 +21,7 @@ extern std::atomic<int64_t> g_launch_count;
 
 inline lora_status_t cuda_fail(cudaError_t e) {
     g_last_cuda_error = (int32_t)e;
+    cudaGetLastError();     // reported here: the next launch's check would take it for its own
     return LORA_ERR_CUDA;
 }
 #define LORA_CUDA_TRY(expr)                                   \

@@ -25,3 +25,22 @@ def test_two_caches_build_tables_in_turn(large, small):
         for c, R in ((a, large), (b, small), (a, large), (b, large), (a, small), (b, large)):
             got, want = build(c, R)
             assert got == want, (R, c is a)
+
+
+def test_an_error_is_reported_once():
+    """A call that the CUDA runtime refused does not leave its error for the next call, which has nothing to do
+    with it."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    x = torch.ones((3, 128), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(x)
+    kw = dict(num_q_heads=2, num_kv_heads=0, head_dim=64, q=x, ldq=128, q_out=out, eps=1e-6)
+    buf = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    shape = dict(num_layers=1, num_pages=4, page_size=16, num_q_heads=2, num_kv_heads=2, head_dim=64)
+    for _ in range(2):
+        with pytest.raises(lb.LoraError) as e:
+            lb.kv_create(**shape, device_buf=buf, device=99)
+        assert e.value.status == 9
+        lb.qk_norm_rope(lb.qk_args(**kw), 3)
+    assert torch.equal(out, x)

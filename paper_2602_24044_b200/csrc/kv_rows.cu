@@ -467,6 +467,7 @@ lora_status_t lora_qk_norm_rope(const lora_qk_args_t *args, int32_t T, void *str
     lora_status_t s = fill_rows(args, T, false, &P);
     if (s != LORA_OK || T == 0) return s;
     DeviceGuard g(args->device);
+    if (!g.ok) return cuda_fail(cudaErrorInvalidDevice);
     return run_rows(args, P, false, (cudaStream_t)stream);
 }
 

@@ -44,3 +44,15 @@ def test_an_error_is_reported_once():
         assert e.value.status == 9
         lb.qk_norm_rope(lb.qk_args(**kw), 3)
     assert torch.equal(out, x)
+
+
+def test_a_device_that_is_not_there_runs_nothing():
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    x = torch.ones((3, 128), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(x)
+    before = lb.launch_count()
+    with pytest.raises(lb.LoraError) as e:
+        lb.qk_norm_rope(lb.qk_args(num_q_heads=2, num_kv_heads=0, head_dim=64, q=x, ldq=128, q_out=out, device=99), 3)
+    assert e.value.status == 9 and lb.launch_count() == before and (_np(out) == 0).all()

@@ -22,10 +22,13 @@
 //   - all (item, head, chunk) triples of the batch form one walk that is cut into equal spans, one per
 //     resident warp: no tail, whatever the lengths.  A span that ends inside an (item, head) leaves a
 //     piece (maximum, sum, normalised output) in the workspace, at most two per warp.
-// The running maximum is raised only when a score passes it by 2^8: the probabilities then stay below 256
-// and the accumulators are rescaled once in a while instead of once a chunk.  p_t s_t is rounded to fp16
-// (11 bits, where bf16 would add as much error as the output's own rounding has); its exponent range is
-// kept by a common power of two of the value rows seen so far, raised like the maximum.
+// p_t s_t is rounded to fp16 (11 bits, where bf16 would add as much error as the output's own rounding has) and
+// has to keep its bits far below the largest: a thousand keys that are each 2^-20 of one with a small value
+// count.  So nearly the whole range is used: the running maximum is raised when a score passes it by 2^3, the
+// common power of two of the value rows' scales seen so far when one passes it by 2^2, and the largest product of
+// both is 2^15.  11 bits then reach down to 2^-22 of the largest p times the largest s; smaller products are off
+// by 2^-34 of that at most.  (With margins of 2^8 for p and 2^7 for the rows' magnitudes above 1, one key 2^22
+// above 8191 others took their weight from them.)
 //
 // Measured: 256 requests of 256..8192 keys (638 MB) 159 us with the joining, 4.0 TB/s; four requests of
 // 60k..131k keys (397 MB) 100 us.  About 560 instructions a chunk at 2.2 a cycle and SM: the chain of each warp
@@ -57,8 +60,13 @@ struct AttnParams {
 };
 
 constexpr int DK_WARPS = 4;             // warps of a block; each is on its own
-constexpr float KV_RAISE = 8.0f;        // a score may pass the running maximum by this (log2)
-constexpr int KV_RAISE_E = 7;           // a value row may pass the common exponent by this
+constexpr float KV_RAISE = 8.0f;        // prompts: a score may pass the running maximum by this (log2),
+constexpr int KV_RAISE_E = 7;           // a row of keys or values the common exponent by this
+// Single tokens: the same margins, and the power of two that probabilities come with, so that the largest p s is
+// 2^15 (half of what fp16 holds: a large score's own rounding may take p past its margin).
+constexpr float DK_RAISE = 3.0f;
+constexpr int DK_RAISE_E = 2;
+constexpr float DK_UNIT = 15.0f - DK_RAISE - DK_RAISE_E;
 
 template <int D>
 struct DecCfg {
@@ -141,13 +149,19 @@ __device__ __forceinline__ KvItem load_item(const KvItem *p) {
     return it;
 }
 
-// The common exponent of the value rows: what their scales and lows are divided by.  A row whose
-// magnitude is 2^a needs e >= a - KV_RAISE_E; a new exponent is set to the row's own.
+// A common exponent of rows: what their scales and lows are divided by.  A row whose magnitude is 2^a
+// needs e >= a - MARGIN; a new exponent is set to the row's own, or to MOST.
+template <int MARGIN, int MOST>
 __device__ __forceinline__ int raise_exponent(int e, uint32_t most_bits) {
     const int a = (int)(most_bits >> 23) - 126;      // magnitude < 2^a
-    return a > e + KV_RAISE_E ? min(a, 126) : e;
+    return a > e + MARGIN ? min(a, MOST) : e;
 }
-constexpr int KV_NO_EXPONENT = -126;
+constexpr int KV_NO_EXPONENT = -126, KV_MOST_EXPONENT = 126;
+// Single tokens: the magnitude of a value row is that of 16 s, or of its low value where that is more (p s alone
+// is rounded to fp16; a low value that is far off only has to stay in fp32's range).  Scales are divided by
+// 2^(e - 4).
+constexpr uint32_t DK_SIXTEEN = 4u << 23;
+constexpr int DK_NO_EXPONENT = -122, DK_MOST_EXPONENT = 127;
 // Codes as fp16 without any arithmetic: a nibble at bits 0..3 of a half is the subnormal number c 2^-24,
 // at bits 4..7 it is c 2^-20, and the tensor cores take subnormal numbers as they are.
 constexpr uint32_t NIB_LO = 0x000f000fu, NIB_HI = 0x00f000f0u;
@@ -290,8 +304,8 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
         const int32_t lim_min = it.lim0 + it.row0 / group;
         const int32_t lim_max = it.lim0 + (it.row0 + it.nrows - 1) / group;
         // o: outputs, lo nibbles times 2^-24, high ones times 2^-20; sp: sums of the rounded p s, which take the
-        // offset 8 of the codes out again.  A score x as it is held is qx x in log2; nm: -(maximum in log2) (0 while
-        // nothing was seen), so that a probability is 2^(qx x + nm); top: the x that raises the maximum
+        // offset 8 of the codes out again.  A score x as it is held is qx x in log2; nm: DK_UNIT - (maximum in
+        // log2) (0 while nothing was seen), so that a probability with its unit is 2^(qx x + nm); top: the x that raises the maximum
         float o[NT][MT][4], sp[NT][4], nm[NT][2], top[NT][2], l[NT][2], z[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -305,8 +319,8 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
             nm[n][0] = nm[n][1] = 0.0f;
             l[n][0] = l[n][1] = z[n][0] = z[n][1] = 0.0f;
         }
-        int ve = KV_NO_EXPONENT;
-        uint32_t most_ok = (uint32_t)(ve + KV_RAISE_E + 127) << 23;     // value rows up to this leave ve as it is
+        int ve = DK_NO_EXPONENT;
+        uint32_t most_ok = (uint32_t)(ve + DK_RAISE_E + 127) << 23;     // value rows up to this leave ve as it is
         for (int32_t chunk = c0; chunk < c1; ++chunk) {
             const int s = stage;
             request();       // refills the stage that was finished in the previous round
@@ -376,12 +390,12 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                         if (!WHOLE && !(((valid >> b) & 1u) && key0 + b * KV_CELL + pr + 8 * r < lim_max)) vp_[b][r] = 0;
                     }
                 }
-                // magnitude of the value rows (bf16 bits of scale and |low|), for the common exponent
+                // magnitude of the value rows (16 scale and |low|, or a little more), for the common exponent
                 uint32_t most;
                 {
                     const uint32_t h = max_u16x2(max_u16x2(vp_[0][0] & 0x7fff7fffu, vp_[0][1] & 0x7fff7fffu),
                                                  max_u16x2(vp_[1][0] & 0x7fff7fffu, vp_[1][1] & 0x7fff7fffu));
-                    most = max(h << 16, h & 0xffff0000u);
+                    most = max((h << 16) + DK_SIXTEEN, h & 0xffff0000u);
                 }
                 if (!WHOLE) {
 #pragma unroll
@@ -413,13 +427,13 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                         most = 0;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint32_t vp = vp_[i >> 1][i & 1], mag = max(vp << 16, vp & 0x7fff0000u);
-                            if (mag < 0x7f800000u) most = max(most, mag);
+                            const uint32_t vp = vp_[i >> 1][i & 1], sb = vp << 16, lb = vp & 0x7fff0000u;
+                            if (max(sb, lb) < 0x7f800000u) most = max(most, max(sb + DK_SIXTEEN, lb));
                         }
                     }
-                    const int ve_new = raise_exponent(ve, __reduce_max_sync(0xffffffffu, most));
+                    const int ve_new = raise_exponent<DK_RAISE_E, DK_MOST_EXPONENT>(ve, __reduce_max_sync(0xffffffffu, most));
                     const float fe = pow2(max(ve - ve_new, -126));
-                    most_ok = (uint32_t)(ve_new + KV_RAISE_E + 127) << 23;
+                    most_ok = (uint32_t)(ve_new + DK_RAISE_E + 127) << 23;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         float fj[2];
@@ -431,10 +445,10 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
                             float f = 1.0f;
                             if (mx > top[n][j]) {
-                                const float now = -mx * qx[n][j];
+                                const float now = fmaf(-mx, qx[n][j], DK_UNIT);
                                 f = top[n][j] == -INFINITY ? 0.0f : exp2_approx(now - nm[n][j]);
                                 nm[n][j] = now;
-                                top[n][j] = mx + KV_RAISE / qx[n][j];
+                                top[n][j] = mx + DK_RAISE / qx[n][j];
                             }
                             fj[j] = f * fe;
                             l[n][j] *= f;
@@ -450,7 +464,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                     ve = ve_new;
                 }
                 // probabilities, and the second product
-                const float unit = pow2(-ve);
+                const float unit = pow2(4 - ve);
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const uint32_t cell = base + b * C::CELL + KV_CELL * (D / 2);
@@ -544,7 +558,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                 const int32_t row = n * 8 + 2 * c + j;
                 if (row >= it.nrows) continue;
                 const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
-                const float off = zs - 8.0f * sp[n][j], ml = -nm[n][j], back = pow2(ve);
+                const float off = zs - 8.0f * sp[n][j], ml = -nm[n][j], back = pow2(ve - 4);
                 // a lane's columns are g D/8 .. g D/8 + D/8 - 1, in the order of the codes' nibbles
                 float f[D / 8];
 #pragma unroll

@@ -586,8 +586,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     : "r"(ok ? 0u : 1u)
                     : "memory");
                 if (any_bad) { dead = true; break; }
-                ek = raise_exponent(ek, max(max(most[0], most[1]), max(most[2], most[3])));
-                ev = raise_exponent(ev, max(max(most[4], most[5]), max(most[6], most[7])));
+                ek = raise_exponent<KV_RAISE_E, KV_MOST_EXPONENT>(ek, max(max(most[0], most[1]), max(most[2], most[3])));
+                ev = raise_exponent<KV_RAISE_E, KV_MOST_EXPONENT>(ev, max(max(most[4], most[5]), max(most[6], most[7])));
                 const float k_unit = pow2(-ek), v_unit = pow2(-ev);
                 if (lane == 0) {
                     PromptInfo *info = infos + ps;

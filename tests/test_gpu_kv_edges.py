@@ -56,3 +56,65 @@ def test_a_device_that_is_not_there_runs_nothing():
     with pytest.raises(lb.LoraError) as e:
         lb.qk_norm_rope(lb.qk_args(num_q_heads=2, num_kv_heads=0, head_dim=64, q=x, ldq=128, q_out=out, device=99), 3)
     assert e.value.status == 9 and lb.launch_count() == before and (_np(out) == 0).all()
+
+
+def _sink(hq, hkv, D, R, kv, q_len, bits, seed):
+    """R requests that share one cached prefix of kv keys (the last page of each is its own), whose first key, with
+    a value of zero, has a score `bits` binades above the others.  So long a walk that a span holds whole requests.
+    Returns outputs, the definition's in 64 bits, sum_j p_j |v_j|, and the largest scale and value."""
+    import torch
+    rng = np.random.default_rng(seed)
+    P = 16
+    shared = kv // P
+    own = -(-(kv + q_len) // P) - shared
+    n = shared + R * own
+    slots = n * P
+    k32 = rng.standard_normal((slots, hkv, D)).astype(np.float32)
+    v32 = (0.5 + rng.standard_normal((slots, hkv, D)) * np.exp(0.5 * rng.standard_normal((slots, hkv, 1)))).astype(np.float32)
+    k32[..., 0] = 0
+    k32[0] = 0
+    k32[0, :, 0] = bits * np.log(2.0) * D ** 0.5 / 4
+    v32[0] = 0
+    Kq, Vq = ([a.reshape((slots, hkv) + a.shape[1:]) for a in ref.quantise(x.reshape(-1, D))] for x in (k32, v32))
+    table = np.concatenate([np.tile(np.arange(shared), (R, 1)), shared + np.arange(R * own).reshape(R, own)], 1).astype(np.int32)
+    T = R * q_len
+    q = (0.3 * rng.standard_normal((T, hq, D))).astype(np.float32)
+    q[..., 0] = 4
+    q = ref.bf16(q)
+    with _cache(num_pages=n, num_q_heads=hq, num_kv_heads=hkv, head_dim=D) as c:
+        c.layer(0).copy_(_dev(ref.pack_layer(Kq, Vq, n, P, hkv, D)))
+        # the table holds its last pages already: the stack hands out the same ones
+        have = _i32(np.full(R, kv))
+        full = _i32(table)
+        new = table[:, shared + (kv % P > 0):].reshape(-1)
+        free, cnt = _i32(np.append(new[::-1], 0)), _i32([new.size])
+        c.build_tables(have, _i32(np.full(R, q_len)), T, free, cnt, full, max_q=q_len)
+        assert np.array_equal(_np(full), table)
+        qd = _dev(q.reshape(T, hq * D), torch.bfloat16)
+        out = torch.empty_like(qd)
+        c.attention(0, qd, out, scale=D ** -0.5)
+        assert c.status()[1] == 0
+        got = out.double().view(R, q_len, hkv, hq // hkv, D)
+    K, V = (_dev(a.astype(np.float64) * s[..., None].astype(np.float64) + l[..., None].astype(np.float64)) for a, s, l in (Kq, Vq))
+    want, mag = torch.empty_like(got), torch.empty_like(got)
+    limit = kv + torch.arange(q_len, device="cuda") + 1
+    for r in range(R):
+        at = (full[r].long()[:, None] * P + torch.arange(P, device="cuda")).view(-1)[: kv + q_len]
+        x = torch.einsum("qhgd,khd->qhgk", qd.double().view(R, q_len, hkv, hq // hkv, D)[r], K[at]) * D ** -0.5
+        x.masked_fill_((torch.arange(kv + q_len, device="cuda") >= limit[:, None])[:, None, None], -float("inf"))
+        p = torch.softmax(x, -1)
+        want[r], mag[r] = torch.einsum("qhgk,khd->qhgd", p, V[at]), torch.einsum("qhgk,khd->qhgd", p, V[at].abs())
+    return got, want, mag, float(np.max(Vq[1])), float(V.abs().max())
+
+
+@pytest.mark.parametrize("D,hq,hkv", [(64, 8, 8), (128, 64, 4)])
+def test_single_tokens_beside_a_key_far_above_the_others(D, hq, hkv):
+    """p s is rounded to 11 bits, or to 2^-33 of the largest p times the largest s where that is more (half of it off
+    at most); a value is at most 24 times its row's scale here (low between -24 and 8 scales).  With the output's own
+    rounding and 2^-12 for exponentials and sums."""
+    require_gpu()
+    kv = 8191
+    got, want, mag, s_max, _ = _sink(hq, hkv, D, 300 * 8 // hkv, kv, 1, 22, D)
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -12) * mag + (kv + 1) * 2.0 ** -34 * s_max * 24
+    worst = float(((got - want).abs() / bound).max())
+    assert worst <= 1, "worst %.3g times the bound" % worst

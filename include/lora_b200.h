@@ -546,8 +546,9 @@ lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, i
  * sums: queries, codes and scales enter exactly (what is 2^-17 of its row's, of its request's largest so
  * far, or smaller loses bits below 2^-25 of that), a probability times its value row's scale is rounded
  * to 11 bits, or to 2^-33 of the largest probability times the largest scale (or |low| / 16) where that is
- * more, and in requests with more than 64 rows (q_len * num_q_heads / num_kv_heads) the values are rounded to
- * 11 bits.  Queries beyond 2^110 count as infinite.  The result does not depend on timing.
+ * more; in requests with more than 64 rows (q_len * num_q_heads / num_kv_heads) a probability is rounded to
+ * 11 bits, or to 2^-33 of the largest where that is more, and the values to 11 bits, or to 2^-23 of the
+ * request's largest scale or |low| so far.  Queries beyond 2^110 count as infinite.  The result does not depend on timing.
  * Calls on one workspace must be ordered on one stream; the workspace's contents are undefined afterwards.
  * Errors: INVALID_ARG, SHAPE, SLOT_RANGE (layer), BUFFER_TOO_SMALL (workspace), CUDA.
  */

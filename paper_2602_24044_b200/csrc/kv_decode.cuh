@@ -60,9 +60,8 @@ struct AttnParams {
 };
 
 constexpr int DK_WARPS = 4;             // warps of a block; each is on its own
-constexpr float KV_RAISE = 8.0f;        // prompts: a score may pass the running maximum by this (log2),
-constexpr int KV_RAISE_E = 7;           // a row of keys or values the common exponent by this
-// Single tokens: the same margins, and the power of two that probabilities come with, so that the largest p s is
+// Single tokens: a score may pass the running maximum by DK_RAISE (log2), a value row the common exponent by
+// DK_RAISE_E; and the power of two that probabilities come with, so that the largest p s is
 // 2^15 (half of what fp16 holds: a large score's own rounding may take p past its margin).
 constexpr float DK_RAISE = 3.0f;
 constexpr int DK_RAISE_E = 2;
@@ -156,7 +155,6 @@ __device__ __forceinline__ int raise_exponent(int e, uint32_t most_bits) {
     const int a = (int)(most_bits >> 23) - 126;      // magnitude < 2^a
     return a > e + MARGIN ? min(a, MOST) : e;
 }
-constexpr int KV_NO_EXPONENT = -126, KV_MOST_EXPONENT = 126;
 // Single tokens: the magnitude of a value row is that of 16 s, or of its low value where that is more (p s alone
 // is rounded to fp16; a low value that is far off only has to stay in fp32's range).  Scales are divided by
 // 2^(e - 4).

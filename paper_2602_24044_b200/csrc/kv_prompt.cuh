@@ -178,6 +178,13 @@ __device__ __forceinline__ uint32_t low_bits(int32_t n) {
 }
 
 constexpr int PK_THREADS = 448, PK_TILES = 3, PK_RAW = 2, PK_INFO = 3;
+// A score may pass the running maximum by PK_RAISE (log2), a row of keys or values the common exponent by
+// PK_RAISE_E.  Probabilities come with a power of two, so that the largest is 2^15, half of what fp16 holds: 11
+// bits then reach down to 2^-23 of the largest, and smaller ones are off by 2^-34 of it at most.  (With the largest
+// at 2^8, 8000 keys 2^-25 below one whose value is zero had 35 % of their weight misrounded.)
+constexpr float PK_RAISE = 6.0f, PK_UNIT = 15.0f - PK_RAISE;
+constexpr int PK_RAISE_E = 7;
+constexpr int PK_NO_EXPONENT = -126, PK_MOST_EXPONENT = 126;
 constexpr int PK_EXTRA = 128 * 16 * 2;       // 16 more columns of 128 rows, as core matrices
 
 struct PromptInfo {          // of a block of keys, from the widening warps to the softmax
@@ -385,8 +392,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
             const int32_t lo = P.window > 0 ? lim - P.window : 0;
             const int32_t lim_min = cur.it.lim0 + min(cur.it.row0 + t * 128, last_row) / group;
             const int32_t lo_max = P.window > 0 ? cur.it.lim0 + min(cur.it.row0 + t * 128 + 127, last_row) / group - P.window : 0;
-            float m = -INFINITY, l = 0.0f;
-            int ve = KV_NO_EXPONENT;
+            float m = -INFINITY, l = 0.0f;      // m: a maximum less PK_UNIT
+            int ve = PK_NO_EXPONENT;
             for (int32_t ch = c0; ch < c1; ++ch, ++j) {
                 const uint32_t ps = j % PK_INFO;
                 ok = wait(&info_full[ps], (j / PK_INFO) & 1u) && wait(&s_full[t], j & 1u);
@@ -430,8 +437,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                 else if (any_bad) l = NAN;
                 float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx = mx == -INFINITY ? mx : mx * f;
-                if (__any_sync(0xffffffffu, mx > m + KV_RAISE || ve_new != ve)) {
-                    const float mn = mx > m + KV_RAISE ? mx : m;
+                if (__any_sync(0xffffffffu, mx > m + (PK_UNIT + PK_RAISE) || ve_new != ve)) {
+                    const float mn = mx > m + (PK_UNIT + PK_RAISE) ? mx - PK_UNIT : m;
                     const float fm = mn == m ? 1.0f : exp2_approx(m - mn), fe = fm * pow2(max(ve - ve_new, -126));
                     m = mn;
                     ve = ve_new;
@@ -545,7 +552,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
         while (!dead && cur.more()) {
             const int32_t c0 = cur.chunk, c1 = cur.last_chunk();
             const int32_t end = cur.it.lim0 + (cur.it.row0 + cur.it.nrows - 1) / group;
-            int ek = KV_NO_EXPONENT, ev = KV_NO_EXPONENT;
+            int ek = PK_NO_EXPONENT, ev = PK_NO_EXPONENT;
             for (int32_t ch = c0; ch < c1; ++ch, ++j) {
                 const uint32_t rs = j % PK_RAW, ps = j % PK_INFO;
                 const uint32_t raw = smem_u32(smem) + C::OFF_RAW + rs * C::RAW;
@@ -586,8 +593,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     : "r"(ok ? 0u : 1u)
                     : "memory");
                 if (any_bad) { dead = true; break; }
-                ek = raise_exponent<KV_RAISE_E, KV_MOST_EXPONENT>(ek, max(max(most[0], most[1]), max(most[2], most[3])));
-                ev = raise_exponent<KV_RAISE_E, KV_MOST_EXPONENT>(ev, max(max(most[4], most[5]), max(most[6], most[7])));
+                ek = raise_exponent<PK_RAISE_E, PK_MOST_EXPONENT>(ek, max(max(most[0], most[1]), max(most[2], most[3])));
+                ev = raise_exponent<PK_RAISE_E, PK_MOST_EXPONENT>(ev, max(max(most[4], most[5]), max(most[6], most[7])));
                 const float k_unit = pow2(-ek), v_unit = pow2(-ev);
                 if (lane == 0) {
                     PromptInfo *info = infos + ps;

@@ -118,3 +118,15 @@ def test_single_tokens_beside_a_key_far_above_the_others(D, hq, hkv):
     bound = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -12) * mag + (kv + 1) * 2.0 ** -34 * s_max * 24
     worst = float(((got - want).abs() / bound).max())
     assert worst <= 1, "worst %.3g times the bound" % worst
+
+
+@pytest.mark.parametrize("D,hq,hkv", [(64, 4, 4), (128, 8, 2)])
+def test_prompts_beside_a_key_far_above_the_others(D, hq, hkv):
+    """Probabilities are rounded to 11 bits, or to 2^-33 of the largest where that is more (half of it off at most);
+    values to 11 bits."""
+    require_gpu()
+    kv = 8190
+    got, want, mag, _, v_max = _sink(hq, hkv, D, 160 // hkv, kv, 70, 25.5, D + 1)
+    bound = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -12) * mag + (kv + 70) * 2.0 ** -34 * v_max
+    worst = float(((got - want).abs() / bound).max())
+    assert worst <= 1, "worst %.3g times the bound" % worst

@@ -98,15 +98,16 @@ __device__ __forceinline__ void mma16816_f16(float (&d)[4], const uint32_t (&a)[
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// fp16: 0x6400 | c is 1024 + c; the nibble above it, left in place, is 1024 + 16 c.
-__device__ __forceinline__ uint32_t widen_f16_lo(uint32_t w) {
+// fp16: 0x6400 | c is 1024 + c; the nibble above it, left in place, is 1024 + 16 c.  Less `off` (1024, or 1032
+// for c - 8); a sixteenth of it, and `off` added (-64, or -72).
+__device__ __forceinline__ uint32_t widen_f16_lo(uint32_t w, uint32_t off) {
     uint32_t v = (w & 0x000f000fu) | 0x64006400u, r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x64086408u));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(off));
     return r;
 }
-__device__ __forceinline__ uint32_t widen_f16_hi(uint32_t w) {
+__device__ __forceinline__ uint32_t widen_f16_hi(uint32_t w, uint32_t off) {
     uint32_t v = (w & 0x00f000f0u) | 0x64006400u, r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x2c002c00u), "r"(0xd480d480u));   // v / 16 - 72
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(0x2c002c00u), "r"(off));
     return r;
 }
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {

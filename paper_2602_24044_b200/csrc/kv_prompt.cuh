@@ -5,8 +5,9 @@
 // bits and c_t - 8 three (or is a power of two), so s_t (c_t - 8) is exact in fp16, and sum(q) z_t is one
 // more step of 16 columns with both factors split into fp16 parts.  Queries (8 bits) are exact in fp16 once
 // a row is divided by a power of two; keys and values of a block are divided by a common power of two,
-// raised like the maximum.  Values enter as fp16(z_t + s_t (c_t - 8)), rounded to 11 bits like the
-// probabilities.
+// raised like the maximum.  Values enter as fp16(low_t + s_t c_t), rounded once to 11 bits like the
+// probabilities (by way of z_t, which is rounded to 11 bits itself, a small value beside a large scale was off by
+// several per cent).
 //
 // What bounds it: a block of 128 keys against 256 rows is 2100 cycles of tensor pipe, 2048 of the
 // exponential unit, about 2300 of shared memory (operands of the products 1650, widened tiles in and out
@@ -621,6 +622,8 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                         tcp::sts_v4(smem_u32(smem) + C::OFF_KX + b * PK_EXTRA + (id >> 3) * 128 + (id & 7) * 16, kx);
                     }
                     const float unit = kv ? v_unit : k_unit;
+                    // keys become s (c - 8), values low + s c: codes less 8 or as they are
+                    const uint32_t off_lo = kv ? 0x64006400u : 0x64086408u, off_hi = kv ? 0xd400d400u : 0xd480d480u;
 #pragma unroll 1
                     for (int i = 0; i < 4; ++i) {
                         const int key = i * 32 + kr;
@@ -631,18 +634,19 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                         uint32_t w[D / 32];
                         if constexpr (D == 128) lds_v4(src, w);
                         else lds_v2(src, w);
-                        const float sf = __uint_as_float(par << 16), zf = fmaf(8.0f, sf, __uint_as_float(par & 0xffff0000u));
+                        const float sf = __uint_as_float(par << 16), lf = __uint_as_float(par & 0xffff0000u);
                         const bool there = ((valid >> (key >> 4)) & 1u) && key < left &&
                                            (kv == 0 || max(par << 16, par & 0x7fff0000u) < 0x7f800000u);
                         const uint32_t s2 = half2_of(there ? sf * unit : 0.0f);
-                        const uint32_t z2 = half2_of(there && kv ? zf * unit : 0.0f);      // (keys get theirs in the further columns)
+                        const uint32_t z2 = half2_of(there && kv ? lf * unit : 0.0f);      // (keys get theirs in the further columns)
                         const uint32_t dst = tile + (c * (D / 32) >> 3) * 16384 + key * 128;
 #pragma unroll
                         for (int e = 0; e < D / 32; ++e) {
                             // lanes 2 and 3 of a row begin with their second half
                             const int we = D == 128 ? e ^ (c & 2) : e;
                             const uint32_t we_w = D == 128 ? ((c & 2) ? w[e ^ 2] : w[e]) : w[e];
-                            uint32_t v[4] = {widen_f16_lo(we_w), widen_f16_hi(we_w), widen_f16_lo(we_w >> 8), widen_f16_hi(we_w >> 8)};
+                            uint32_t v[4] = {widen_f16_lo(we_w, off_lo), widen_f16_hi(we_w, off_hi), widen_f16_lo(we_w >> 8, off_lo),
+                                             widen_f16_hi(we_w >> 8, off_hi)};
 #pragma unroll
                             for (int q = 0; q < 4; ++q) v[q] = fma_f16x2(v[q], s2, z2);
                             tcp::sts_v4(dst + (((c * (D / 32) + we) & 7) ^ (key & 7)) * 16, v);

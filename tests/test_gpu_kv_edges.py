@@ -130,3 +130,23 @@ def test_prompts_beside_a_key_far_above_the_others(D, hq, hkv):
     bound = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -12) * mag + (kv + 70) * 2.0 ** -34 * v_max
     worst = float(((got - want).abs() / bound).max())
     assert worst <= 1, "worst %.3g times the bound" % worst
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_values_keep_eleven_bits_when_small_beside_their_scale(D):
+    """Rows whose low value is a small fraction of the scale: their smallest elements are rounded as such and not
+    as parts of the row's middle, which is hundreds of times larger."""
+    require_gpu()
+    b = Batch([(0, 90), (3, 70)], 2, 1, D, seed=50)
+    rng = np.random.default_rng(51)
+    written = np.isfinite(b.Vq[1])
+    b.Vq[1] = np.where(written, np.float32(1), b.Vq[1])
+    b.Vq[2] = np.where(written, ref.bf16(rng.uniform(0.005, 0.06, b.Vq[2].shape).astype(np.float32)), b.Vq[2])
+    b.store()
+    got = b.run()
+    b.check(got)
+    # the first token of a prompt sees itself alone: its values, rounded to 11 bits and then to 8
+    t = b.want_tables["slot"][0]
+    v = b.values()[1][t, 0]
+    assert (b.Vq[0][t, 0] == 0).any()
+    assert (np.abs(got[0][0] - v) <= (2.0 ** -11 + 2.0 ** -8) * 1.001 * np.abs(v)).all()

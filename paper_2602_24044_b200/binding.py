@@ -209,6 +209,11 @@ def _stream(s) -> Optional[int]:
     return int(s.cuda_stream)
 
 
+def stream_handle(s) -> int:
+    """The cudaStream_t behind a torch stream, an int or None (0: the device's default stream)."""
+    return _stream(s) or 0
+
+
 def _nbytes(obj) -> int:
     if hasattr(obj, "element_size"):
         return int(obj.numel() * obj.element_size())

@@ -193,12 +193,18 @@ class KVCache:
 
     The caller keeps the requests' state (lengths, block table, stack of free pages) as int32 device
     tensors; build_tables() advances it for one batch, then append() and attention() run per layer on
-    the tables it left."""
+    the tables it left.
+
+    stream: as for the entry points (None is the device's default stream).  Calls on several streams are
+    the caller's to order; the cache sees to it that its own buffers are not given back to the allocator
+    while work on any stream it was called on is pending, so these streams outlive it.  Tables that grow
+    move: a captured graph keeps the old ones, so reserve() for the largest batch before a capture."""
 
     def __init__(self, num_layers: int, num_pages: int, page_size: int, num_q_heads: int, num_kv_heads: int,
                  head_dim: int, device: int = 0):
         self.device = torch.device("cuda", int(device))
         self.shape = (num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim)
+        self._streams = set()            # handles of the streams that work on the buffers was queued on
         nbytes = lb.kv_bytes(*self.shape, device=int(device))
         self.buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         off = (-self.buf.data_ptr()) % 256
@@ -209,16 +215,42 @@ class KVCache:
         self.tables, self._tables_bytes = None, 0
         self.R = self.T = -1
 
+    def _on(self, stream) -> int:
+        """The stream's handle, noted as one that may have work on the buffers."""
+        handle = lb.stream_handle(stream)
+        self._streams.add(handle)
+        return handle
+
+    def _torch_stream(self, handle: int):
+        return torch.cuda.ExternalStream(handle, self.device) if handle else torch.cuda.default_stream(self.device)
+
+    def _let_go(self, *tensors) -> None:
+        """Before tensors are dropped: their memory may be handed out once the work queued so far is done."""
+        for handle in self._streams:
+            stream = self._torch_stream(handle)
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+
     def layer(self, layer: int) -> torch.Tensor:
         """One layer's pages as bytes (a view)."""
         off, n = lb.kv_layer_range(layer, *self.shape, device=self.device.index)
         return self.mem[off:off + n]
 
     def reserve(self, R: int, T: int) -> None:
-        """Makes room for the tables of a batch of R requests and T new tokens."""
+        """Makes room for the tables of a batch of R requests and T new tokens, ready for calls on any stream."""
+        here = torch.cuda.current_stream(self.device)
+        if self._room(R, T, here) and not torch.cuda.is_current_stream_capturing():
+            here.synchronize()           # recycled memory is free in the order of the stream it was taken on
+
+    def _room(self, R: int, T: int, stream) -> bool:
+        """Room for a batch's tables, taken on `stream` (a torch stream); True when they moved."""
         words = lb.kv_tables_bytes(self.kv, R, T) // 4
-        if self.tables is None or self.tables.numel() < words:
-            self.tables = torch.empty(words, dtype=torch.int32, device=self.device)
+        grow = self.tables is None or self.tables.numel() < words
+        if grow:
+            self._let_go(self.tables)
+            with torch.cuda.stream(stream):
+                self.tables = torch.empty(words, dtype=torch.int32, device=self.device)
             self._tables_bytes = 4 * words
             self.R = -1
         if (R, T) != (self.R, self.T):
@@ -226,6 +258,7 @@ class KVCache:
             v = lb.kv_table_views(self.tables, R, T)
             self.header, self.starts, self.lengths = v["header"], v["start"], v["kv_len"]
             self.positions, self.slots = v["position"], v["slot"]
+        return grow
 
     def build_tables(self, kv_len, q_len, T: int, free_pages, free_count, block_table, *, max_q: int = 0,
                      window: int = 0, kv_len_out=None, free_count_out=None, stream=None) -> None:
@@ -234,8 +267,9 @@ class KVCache:
         R = kv_len.shape[0]
         if q_len.shape[0] != R or block_table.shape[0] != R:
             raise ValueError("q_len and block_table need one entry and one row per request (%d)" % R)
+        stream = self._on(stream)
         if R != self.R or T != self.T:
-            self.reserve(R, T)
+            self._room(R, T, self._torch_stream(stream))
         self.block_table, self.ld_table = block_table, block_table.stride(0)
         lb.kv_build_tables(self.kv, kv_len, q_len, R, T, free_pages, free_count, block_table, self.ld_table,
                            self.tables, max_q=max_q, window=window,
@@ -245,21 +279,21 @@ class KVCache:
 
     def release(self, requests, kv_len, block_table, free_pages, free_count, stream=None) -> None:
         lb.kv_release(self.kv, requests, int(requests.shape[0]), int(kv_len.shape[0]), kv_len, block_table,
-                      int(block_table.stride(0)), free_pages, free_count, stream=stream)
+                      int(block_table.stride(0)), free_pages, free_count, stream=self._on(stream))
 
     def append(self, layer: int, args, slots=None, T: Optional[int] = None, stream=None) -> None:
         """args: binding.qk_args(...); slots: default those of the tables."""
         lb.kv_append(self.kv, layer, args, self.slots if slots is None else slots,
-                     self.T if T is None else T, stream=stream)
+                     self.T if T is None else T, stream=self._on(stream))
 
     def read(self, layer: int, slots, k_out, v_out, stream=None) -> None:
         lb.kv_read(self.kv, layer, slots, int(slots.shape[0]), k_out, 0 if k_out is None else k_out.stride(0),
-                   v_out, 0 if v_out is None else v_out.stride(0), stream=stream)
+                   v_out, 0 if v_out is None else v_out.stride(0), stream=self._on(stream))
 
     def attention(self, layer: int, q, out, *, scale: float, lse=None, stream=None) -> None:
         lb.kv_attention(self.kv, layer, q, q.stride(0), out, out.stride(0), lse, scale, self.tables, self.R,
                         self.T, self.block_table, self.ld_table, self.workspace, self._workspace_bytes,
-                        stream=stream)
+                        stream=self._on(stream))
 
     def status(self, stream=None):
         return lb.kv_check_status(self.kv, stream)
@@ -273,8 +307,9 @@ class KVCache:
     def __del__(self):   # the handle holds host memory only; the buffers are torch's to free
         try:
             if getattr(self, "kv", 0):
+                self._let_go(self.buf, self.workspace, self.tables)
                 lb.kv_destroy(self.kv)
-        except TypeError:   # the interpreter is taking its modules down
+        except (TypeError, AttributeError):   # the interpreter is taking its modules down
             pass
         self.kv = 0
 

@@ -150,3 +150,37 @@ def test_prompt_values_keep_eleven_bits_when_small_beside_their_scale(D):
     v = b.values()[1][t, 0]
     assert (b.Vq[0][t, 0] == 0).any()
     assert (np.abs(got[0][0] - v) <= (2.0 ** -11 + 2.0 ** -8) * 1.001 * np.abs(v)).all()
+
+
+def test_memory_that_a_side_stream_still_reads_is_not_handed_out():
+    """Work on a side stream is pending when the tables grow, and when the cache goes: what is allocated next does
+    not get their memory."""
+    require_gpu()
+    import torch
+    side, inputs = torch.cuda.Stream(), []
+    c = _cache()
+
+    def build(R):
+        a = [_i32(v) for v in (np.zeros(R), np.ones(R), np.arange(64), [64], np.full((R, 1), -1))]
+        inputs.append(a)
+        c.build_tables(a[0], a[1], R, a[2], a[3], a[4], max_q=1, stream=side)
+
+    def place(t):
+        return t.data_ptr(), t.numel(), t.dtype
+
+    def handed_out(at, n, dtype):
+        return any(t.data_ptr() == at for t in [torch.empty(n, dtype=dtype, device="cuda") for _ in range(4)])
+
+    c.reserve(1, 1)
+    build(1)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)       # about 0.2 s
+    old = place(c.tables)
+    build(60)
+    reused = [handed_out(*old)]
+    old = place(c.buf), place(c.workspace)
+    del c
+    reused += [handed_out(*p) for p in old]
+    pending = not side.query()
+    torch.cuda.synchronize()
+    assert pending and not any(reused)

@@ -98,6 +98,7 @@ class _QkArgs(ctypes.Structure):
                 ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("q_out", ctypes.c_void_p), ("ldqo", ctypes.c_int64),
                 ("k_out", ctypes.c_void_p), ("ldko", ctypes.c_int64)]
+    max_tokens = 2 ** 31 - 1
 
 
 _handle = None
@@ -189,29 +190,28 @@ def _check(status: int, where: str) -> None:
 
 def _ptr(obj) -> Optional[int]:
     """Address of a torch tensor / numpy array / int / None."""
-    if obj is None:
-        return None
-    data_ptr = getattr(obj, "data_ptr", None)
-    if data_ptr is not None:
-        return data_ptr()
-    if isinstance(obj, int):
+    if obj is None or type(obj) is int:
         return obj
+    try:
+        return obj.data_ptr()
+    except AttributeError:
+        pass
+    if isinstance(obj, int):
+        return int(obj)
     if isinstance(obj, np.ndarray):
         return int(obj.ctypes.data)
     raise TypeError("cannot take the address of %r" % type(obj))
 
 
 def _stream(s) -> Optional[int]:
-    if s is None:
-        return None
-    if isinstance(s, int):
+    if s is None or type(s) is int:
         return s
     return int(s.cuda_stream)
 
 
 def stream_handle(s) -> int:
     """The cudaStream_t behind a torch stream, an int or None (0: the device's default stream)."""
-    return _stream(s) or 0
+    return s if type(s) is int else 0 if s is None else int(s.cuda_stream)
 
 
 def _nbytes(obj) -> int:
@@ -549,10 +549,12 @@ def kv_build_tables(kv: int, kv_len, q_len, R: int, T: int, free_pages, free_cou
                     ld_table: int, tables, *, max_q: int = 0, window: int = 0, kv_len_out=None,
                     free_count_out=None, tables_bytes: Optional[int] = None, stream=None) -> None:
     nbytes = _nbytes(tables) if tables_bytes is None else tables_bytes
-    _check(_lib().lora_kv_build_tables(kv, _ptr(kv_len), _ptr(q_len), R, T, max_q, window,
-                                       _ptr(free_pages), _ptr(free_count), _ptr(block_table), ld_table,
-                                       _ptr(kv_len_out), _ptr(free_count_out), _ptr(tables), nbytes,
-                                       _stream(stream)), "lora_kv_build_tables")
+    p = _ptr
+    status = _lib().lora_kv_build_tables(kv, p(kv_len), p(q_len), R, T, max_q, window, p(free_pages), p(free_count),
+                                         p(block_table), ld_table, p(kv_len_out), p(free_count_out), p(tables), nbytes,
+                                         stream if type(stream) is int else _stream(stream))
+    if status:
+        _check(status, "lora_kv_build_tables")
 
 
 def kv_release(kv: int, requests, n: int, R: int, kv_len, block_table, ld_table: int, free_pages,
@@ -562,6 +564,18 @@ def kv_release(kv: int, requests, n: int, R: int, kv_len, block_table, ld_table:
            "lora_kv_release")
 
 
+def _elements(what: str, t, dtype: str, device: int, n: int = 0) -> Optional[int]:
+    """How many elements lie from a tensor's first to the end of its memory; None for a bare address.  n > 0: the
+    tensor itself has to have that many, in a row."""
+    if not hasattr(t, "untyped_storage"):
+        return None
+    if str(t.dtype) != "torch." + dtype or t.get_device() != device:
+        raise LoraError(1, "%s (%s on %s, not %s on device %d)" % (what, t.dtype, t.device, dtype, device))
+    if n and (t.numel() < n or not t.is_contiguous()):
+        raise LoraError(1, "%s (needs %d values in a row)" % (what, n))
+    return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+
+
 def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: int = 0, k=None,
             ldk: int = 0, v=None, ldv: int = 0, q_weight=None, k_weight=None, eps: float = 0.0,
             cos_sin=None, rot_dim: Optional[int] = None, num_positions: Optional[int] = None,
@@ -569,7 +583,8 @@ def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: 
             ldko: Optional[int] = None, device: int = 0):
     """The argument block of qk_norm_rope and kv_append (build it once when the same buffers are used
     again).  rot_dim, num_positions and the outputs' leading dimensions default to those of the tensors
-    given.  The tensors must stay alive while the block is used; it keeps them."""
+    given.  The tensors must stay alive while the block is used; it keeps them, and a call for more tokens than
+    they hold is refused."""
     if cos_sin is not None:
         num_positions = int(cos_sin.shape[0]) if num_positions is None else num_positions
         rot_dim = int(cos_sin.shape[1]) if rot_dim is None else rot_dim
@@ -582,16 +597,45 @@ def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: 
                 int(ldk), _ptr(v), int(ldv), _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin),
                 _ptr(positions), _ptr(q_out), int(ldqo or 0), _ptr(k_out), int(ldko or 0))
     a._keep = (q, k, v, q_weight, k_weight, cos_sin, positions, q_out, k_out)
+    a.max_tokens = _max_tokens(a)
     return a
+
+
+def _max_tokens(a) -> int:
+    """The tokens that fit the tensors of an argument block."""
+    q, k, v, q_weight, k_weight, cos_sin, positions, q_out, k_out = a._keep
+    most, d, device = 2 ** 31 - 1, a.head_dim, a.device
+    for what, t, heads, ld in (("q", q, a.num_q_heads, a.ldq), ("k", k, a.num_kv_heads, a.ldk),
+                               ("v", v, a.num_kv_heads, a.ldv), ("q_out", q_out, a.num_q_heads, a.ldqo),
+                               ("k_out", k_out, a.num_kv_heads, a.ldko)):
+        n = _elements(what, t, "bfloat16", device) if heads > 0 else None
+        if n is not None:
+            most = min(most, 0 if n < heads * d else most if ld <= 0 else (n - heads * d) // ld + 1)
+    _elements("q_weight", q_weight, "bfloat16", device, d)
+    _elements("k_weight", k_weight, "bfloat16", device, d)
+    if cos_sin is not None:
+        _elements("cos_sin", cos_sin, "float32", device, a.num_positions * a.rot_dim)
+        if _elements("positions", positions, "int32", device, 0) is not None:
+            if not positions.is_contiguous():
+                raise LoraError(1, "positions (needs its values in a row)")
+            most = min(most, positions.numel())
+    return most
+
+
+def _check_tokens(args, T: int, where: str) -> None:
+    if T > args.max_tokens:
+        raise LoraError(1, "%s (the tensors given hold %d tokens, not %d)" % (where, args.max_tokens, T))
 
 
 def qk_norm_rope(args, T: int, stream=None) -> None:
     """Per-head norm and rotation of T tokens' queries and keys; `args` from qk_args."""
+    _check_tokens(args, T, "qk_norm_rope")
     _check(_lib().lora_qk_norm_rope(ctypes.byref(args), T, _stream(stream)), "lora_qk_norm_rope")
 
 
 def kv_append(kv: int, layer: int, args, slots, T: int, stream=None) -> None:
     """qk_norm_rope with the keys and values also going to their slots of the cache as 4-bit rows."""
+    _check_tokens(args, T, "kv_append")
     _check(_lib().lora_kv_append(kv, layer, ctypes.byref(args), _ptr(slots), T, _stream(stream)),
            "lora_kv_append")
 

@@ -203,6 +203,7 @@ class KVCache:
     def __init__(self, num_layers: int, num_pages: int, page_size: int, num_q_heads: int, num_kv_heads: int,
                  head_dim: int, device: int = 0):
         self.device = torch.device("cuda", int(device))
+        self._index = int(device)
         self.shape = (num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim)
         self._streams = set()            # handles of the streams that work on the buffers was queued on
         nbytes = lb.kv_bytes(*self.shape, device=int(device))
@@ -213,12 +214,14 @@ class KVCache:
         self.workspace = torch.empty(lb.kv_workspace_bytes(self.kv), dtype=torch.uint8, device=self.device)
         self._workspace_bytes = self.workspace.numel()
         self.tables, self._tables_bytes = None, 0
+        self.slots = self.block_table = None
         self.R = self.T = -1
 
     def _on(self, stream) -> int:
         """The stream's handle, noted as one that may have work on the buffers."""
-        handle = lb.stream_handle(stream)
-        self._streams.add(handle)
+        handle = 0 if stream is None else lb.stream_handle(stream)
+        if handle not in self._streams:
+            self._streams.add(handle)
         return handle
 
     def _torch_stream(self, handle: int):
@@ -231,6 +234,43 @@ class KVCache:
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
+
+    # -- checks: what the kernels would read or write past a tensor's end, or as another type --------------
+    def _ints(self, what: str, t, n: int) -> None:
+        if t.dtype is not torch.int32 or t.numel() < n or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError("%s: needs %d int32 in a row on %s" % (what, n, self.device))
+
+    def _rows(self, what: str, t, n: int, width: int) -> int:
+        """The leading dimension of n bf16 rows of `width` values (in one or several dimensions)."""
+        shape = t.shape
+        if t.dtype is torch.bfloat16 and t.get_device() == self._index and len(shape) >= 2 and shape[0] >= n:
+            if len(shape) == 2 and shape[1] >= width and t.is_contiguous():
+                return shape[1]
+            strides, have = t.stride(), 1
+            for i in range(len(shape) - 1, 0, -1):
+                if strides[i] != have and shape[i] != 1:
+                    have = 0
+                    break
+                have *= shape[i]
+            if have >= width:
+                return strides[0] if shape[0] > 1 else max(strides[0], have)
+        raise ValueError("%s: needs %d bf16 rows of %d values, each in a row, on %s" % (what, n, width, self.device))
+
+    def _table(self, t, R: int) -> int:
+        """The leading dimension of a block table, which is also the pages that a request may have."""
+        shape = t.shape
+        if t.dtype is torch.int32 and t.get_device() == self._index and len(shape) == 2 and shape[0] == R:
+            cols = shape[1]
+            if t.is_contiguous():
+                return cols
+            ld, step = t.stride()
+            if R == 1 and ld < cols:
+                ld = cols
+            # rows that are wider than the table: to their ends they have to lie in its memory
+            if (cols <= 1 or step == 1) and (ld == cols or (
+                    ld > cols and t.storage_offset() + R * ld <= t.untyped_storage().nbytes() // 4)):
+                return ld
+        raise ValueError("block_table: needs %d rows of int32 pages, each in a row, on %s" % (R, self.device))
 
     def layer(self, layer: int) -> torch.Tensor:
         """One layer's pages as bytes (a view)."""
@@ -265,35 +305,70 @@ class KVCache:
         """Tables of a batch; kv_len and free_count are advanced in place unless *_out names other
         tensors."""
         R = kv_len.shape[0]
-        if q_len.shape[0] != R or block_table.shape[0] != R:
-            raise ValueError("q_len and block_table need one entry and one row per request (%d)" % R)
+        if q_len.shape[0] != R:
+            raise ValueError("q_len needs one entry per request (%d)" % R)
+        # (as _ints, written out: the time of this call is the host's.  Lengths have their R by their shape)
+        index, int32 = self._index, torch.int32
+        if (kv_len.dtype is not int32 or kv_len.get_device() != index or not kv_len.is_contiguous() or
+                q_len.dtype is not int32 or q_len.get_device() != index or not q_len.is_contiguous()):
+            self._ints("kv_len", kv_len, R), self._ints("q_len", q_len, R)
+        if (free_pages.dtype is not int32 or free_pages.get_device() != index or not free_pages.is_contiguous() or
+                free_count.dtype is not int32 or free_count.get_device() != index or free_count.numel() < 1):
+            self._ints("free_pages", free_pages, 0), self._ints("free_count", free_count, 1)
+        if kv_len_out is None:
+            kv_len_out = kv_len
+        elif (kv_len_out.dtype is not int32 or kv_len_out.get_device() != index or kv_len_out.numel() < R or
+              not kv_len_out.is_contiguous()):
+            self._ints("kv_len_out", kv_len_out, R)
+        if free_count_out is None:
+            free_count_out = free_count
+        elif free_count_out.dtype is not int32 or free_count_out.get_device() != index or free_count_out.numel() < 1:
+            self._ints("free_count_out", free_count_out, 1)
+        ld_table = self._table(block_table, R)
         stream = self._on(stream)
         if R != self.R or T != self.T:
             self._room(R, T, self._torch_stream(stream))
-        self.block_table, self.ld_table = block_table, block_table.stride(0)
+        self.block_table, self.ld_table = block_table, ld_table
         lb.kv_build_tables(self.kv, kv_len, q_len, R, T, free_pages, free_count, block_table, self.ld_table,
                            self.tables, max_q=max_q, window=window,
-                           kv_len_out=kv_len if kv_len_out is None else kv_len_out,
-                           free_count_out=free_count if free_count_out is None else free_count_out,
+                           kv_len_out=kv_len_out, free_count_out=free_count_out,
                            tables_bytes=self._tables_bytes, stream=stream)
 
     def release(self, requests, kv_len, block_table, free_pages, free_count, stream=None) -> None:
-        lb.kv_release(self.kv, requests, int(requests.shape[0]), int(kv_len.shape[0]), kv_len, block_table,
-                      int(block_table.stride(0)), free_pages, free_count, stream=self._on(stream))
+        """free_pages: room for every page of the cache."""
+        n, R = int(requests.shape[0]), int(kv_len.shape[0])
+        self._ints("requests", requests, n)
+        self._ints("kv_len", kv_len, R)
+        self._ints("free_pages", free_pages, self.shape[1])
+        self._ints("free_count", free_count, 1)
+        lb.kv_release(self.kv, requests, n, R, kv_len, block_table, self._table(block_table, R), free_pages,
+                      free_count, stream=self._on(stream))
 
     def append(self, layer: int, args, slots=None, T: Optional[int] = None, stream=None) -> None:
         """args: binding.qk_args(...); slots: default those of the tables."""
-        lb.kv_append(self.kv, layer, args, self.slots if slots is None else slots,
-                     self.T if T is None else T, stream=self._on(stream))
+        slots, T = self.slots if slots is None else slots, self.T if T is None else T
+        if slots is None:
+            raise ValueError("append: no slots, and no tables have been built")
+        self._ints("slots", slots, T)
+        lb.kv_append(self.kv, layer, args, slots, T, stream=self._on(stream))
 
     def read(self, layer: int, slots, k_out, v_out, stream=None) -> None:
-        lb.kv_read(self.kv, layer, slots, int(slots.shape[0]), k_out, 0 if k_out is None else k_out.stride(0),
-                   v_out, 0 if v_out is None else v_out.stride(0), stream=self._on(stream))
+        n, width = int(slots.shape[0]), self.shape[4] * self.shape[5]
+        self._ints("slots", slots, n)
+        lb.kv_read(self.kv, layer, slots, n, k_out, 0 if k_out is None else self._rows("k_out", k_out, n, width),
+                   v_out, 0 if v_out is None else self._rows("v_out", v_out, n, width), stream=self._on(stream))
 
     def attention(self, layer: int, q, out, *, scale: float, lse=None, stream=None) -> None:
-        lb.kv_attention(self.kv, layer, q, q.stride(0), out, out.stride(0), lse, scale, self.tables, self.R,
-                        self.T, self.block_table, self.ld_table, self.workspace, self._workspace_bytes,
-                        stream=self._on(stream))
+        """q, out: rows of num_q_heads * head_dim values, one per new token of the tables; lse: fp32 in a row."""
+        T, width = self.T, self.shape[3] * self.shape[5]
+        if self.block_table is None:
+            raise ValueError("attention: no tables have been built")
+        ldq, ldo = self._rows("q", q, T, width), self._rows("out", out, T, width)
+        if lse is not None and (lse.dtype is not torch.float32 or lse.numel() < T * self.shape[3] or
+                                not lse.is_contiguous() or lse.get_device() != self._index):
+            raise ValueError("lse: needs %d x %d fp32 in a row on %s" % (T, self.shape[3], self.device))
+        lb.kv_attention(self.kv, layer, q, ldq, out, ldo, lse, scale, self.tables, self.R, T, self.block_table,
+                        self.ld_table, self.workspace, self._workspace_bytes, stream=self._on(stream))
 
     def status(self, stream=None):
         return lb.kv_check_status(self.kv, stream)

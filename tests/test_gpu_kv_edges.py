@@ -53,8 +53,10 @@ def test_a_device_that_is_not_there_runs_nothing():
     x = torch.ones((3, 128), dtype=torch.bfloat16, device="cuda")
     out = torch.zeros_like(x)
     before = lb.launch_count()
+    args = lb.qk_args(num_q_heads=2, num_kv_heads=0, head_dim=64, q=x, ldq=128, q_out=out)
+    args.device = 99
     with pytest.raises(lb.LoraError) as e:
-        lb.qk_norm_rope(lb.qk_args(num_q_heads=2, num_kv_heads=0, head_dim=64, q=x, ldq=128, q_out=out, device=99), 3)
+        lb.qk_norm_rope(args, 3)
     assert e.value.status == 9 and lb.launch_count() == before and (_np(out) == 0).all()
 
 

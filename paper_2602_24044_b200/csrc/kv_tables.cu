@@ -16,7 +16,7 @@ constexpr int TB_WARPS = TB_THREADS / 32;
 
 struct TableParams {
     const int32_t *kv_len, *q_len, *free_pages, *free_count;
-    int32_t *block_table, *kv_len_out, *free_count_out, *out;
+    int32_t *block_table, *kv_len_out, *free_count_out, *out, *status;
     int64_t ld;
     int32_t R, T, max_q, window;
     int32_t num_pages, page_shift, hkv, group;
@@ -296,6 +296,7 @@ __global__ void __launch_bounds__(TB_THREADS) build_tables_kernel(const TablePar
                         page = P.free_pages[count - 1 - k];
                     }
                     if (page >= 0 && page < P.num_pages) slot = (page << P.page_shift) + (pos & ((1 << P.page_shift) - 1));
+                    else atomicAdd(&P.status[STATUS_INVALID_TOKENS], 1);
                 }
             }
             P.out[P.L.position + t] = pos;
@@ -521,6 +522,7 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
     P.kv_len_out = kv_len_out;
     P.free_count_out = free_count_out;
     P.out = (int32_t *)tables;
+    P.status = kv->status_dev;
     P.ld = ld_table;
     P.R = R;
     P.T = T;

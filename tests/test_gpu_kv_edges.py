@@ -186,3 +186,37 @@ def test_memory_that_a_side_stream_still_reads_is_not_handed_out():
     pending = not side.query()
     torch.cuda.synchronize()
     assert pending and not any(reused)
+
+
+def test_pages_outside_the_cache_are_counted():
+    """Word 0 of the status tells of a page that a block table should not hold: where a new token goes, and where
+    attention looks for a key."""
+    require_gpu()
+    table = np.array([[999, -1], [3, -1]], np.int32)
+    with _cache(num_pages=8) as c:
+        c.build_tables(_i32([5, 5]), _i32([1, 1]), 2, _i32(np.arange(8)), _i32([2]), _i32(table))
+        assert c.status()[0] == 1
+    for lens in ([(100, 1)], [(50, 130)]):
+        for page in (10 ** 6, -5):
+            b = Batch(lens, 4, 1, 64, seed=13)
+            b.run()
+            assert b.c.status()[0] == 0
+            b.c.block_table[0, 1] = page
+            b.run()
+            assert b.c.status()[0] > 0
+
+
+def test_pages_that_no_query_sees_are_not_counted():
+    """Behind the window, past the end and of failed requests: pages that are not there are nobody's mistake."""
+    require_gpu()
+    for lens, window in (([(200, 1)], 20), ([(300, 70)], 33)):
+        b = Batch(lens, 4, 1, 64, window=window, seed=14)
+        want, _ = b.run()
+        first = (lens[0][0] + 1 - window) // 16
+        b.c.block_table[0, :first] = -1
+        b.want_tables["table"][0, :first] = -1
+        assert np.array_equal(b.check(), b.check()) and np.array_equal(b.run()[0], want)
+        assert b.c.status()[0] == 0
+    b = Batch([(20, 2), (10, 40), (33, 1)], 8, 2, 128, max_q=2, pad_tokens=2, seed=15)
+    b.check()
+    assert b.c.status()[0] == 0

@@ -541,8 +541,7 @@ lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, i
  * lse = -inf; a key in a page outside the cache is not seen.  q, out: dev bf16 [T, num_q_heads *
  * head_dim] with leading dimensions, out may not overlap q; lse: dev fp32 [T, num_q_heads] or NULL.
  * tables: as written by lora_kv_build_tables for this R and T (and through this handle, which knows the
- * last 256 buffers that it wrote tables to), block_table
- * the one it was given.  A row of the cache that is not finite makes the outputs that see it NaN and no
+ * 256 buffers that it wrote tables to last), block_table the one it was given.  A row of the cache that is not finite makes the outputs that see it NaN and no
  * others.  Statistics and sums are fp32.  Both products run on tensor cores with fp16 operands and fp32
  * sums: queries, codes and scales enter exactly (what is 2^-17 of its row's, of its request's largest so
  * far, or smaller loses bits below 2^-25 of that), a probability times its value row's scale is rounded

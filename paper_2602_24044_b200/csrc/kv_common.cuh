@@ -127,6 +127,7 @@ __host__ __device__ inline KvTables kv_tables(int32_t R, int32_t T, int32_t grou
 struct KvTableRecord {        // what the host knows of a table it built
     const void *ptr;
     int32_t R, T, max_q, window;
+    uint64_t written;         // the how-manieth build through the handle
 };
 
 }  // namespace lora
@@ -141,17 +142,21 @@ struct lora_kv {
     bool decode_attr[4] = {false, false, false, false};   // attributes set: head_dim 64 / 128, 8 / 16 rows
     bool prompt_attr[2] = {false, false};
     bool tables_attr = false;
-    // tables built through this handle, the oldest forgotten first (a fixed array: no call allocates)
+    // tables built through this handle, the one written longest ago forgotten first (a fixed array: no call
+    // allocates)
     static constexpr int32_t MAX_TABLES = 256;
     lora::KvTableRecord tables[MAX_TABLES];
-    int32_t n_tables = 0, next_table = 0;
+    int32_t n_tables = 0;
+    uint64_t builds = 0;
 
     void remember(const void *ptr, int32_t R, int32_t T, int32_t max_q, int32_t window) {
-        for (int32_t i = 0; i < n_tables; ++i)
-            if (tables[i].ptr == ptr) { tables[i] = {ptr, R, T, max_q, window}; return; }
-        tables[next_table] = {ptr, R, T, max_q, window};
-        next_table = (next_table + 1) % MAX_TABLES;
-        if (n_tables < MAX_TABLES) ++n_tables;
+        int32_t at = -1, oldest = 0;
+        for (int32_t i = 0; i < n_tables && at < 0; ++i) {
+            if (tables[i].ptr == ptr) at = i;
+            if (tables[i].written < tables[oldest].written) oldest = i;
+        }
+        if (at < 0) at = n_tables < MAX_TABLES ? n_tables++ : oldest;
+        tables[at] = {ptr, R, T, max_q, window, ++builds};
     }
     const lora::KvTableRecord *find(const void *ptr, int32_t R, int32_t T) const {
         for (int32_t i = 0; i < n_tables; ++i)

@@ -220,3 +220,36 @@ def test_pages_that_no_query_sees_are_not_counted():
     b = Batch([(20, 2), (10, 40), (33, 1)], 8, 2, 128, max_q=2, pad_tokens=2, seed=15)
     b.check()
     assert b.c.status()[0] == 0
+
+
+def test_tables_written_again_are_not_the_oldest():
+    """A handle knows the last 256 buffers that it wrote tables to: one that was written first, and again just
+    now, is among them when the 257th comes."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    with _cache(num_pages=4, num_q_heads=1, num_kv_heads=1, head_dim=64) as c:
+        c.mem[256:].zero_()
+        n = lb.kv_tables_bytes(c.kv, 1, 1)
+        bufs = torch.zeros((257, (n + 15) // 16 * 4), dtype=torch.int32, device="cuda")
+        kv, q, free, cnt, table = _i32([3]), _i32([1]), _i32([0]), _i32([0]), _i32([[0]])
+
+        def build(i):
+            lb.kv_build_tables(c.kv, kv, q, 1, 1, free, cnt, table, 1, bufs[i], max_q=1)
+
+        x = torch.zeros((1, 64), dtype=torch.bfloat16, device="cuda")
+        out = torch.empty_like(x)
+
+        def attend(i):
+            lb.kv_attention(c.kv, 0, x, 64, out, 64, None, 1.0, bufs[i], 1, 1, table, 1, c.workspace)
+
+        for i in range(256):
+            build(i)
+        build(0)
+        build(256)
+        attend(0)
+        attend(256)
+        with pytest.raises(lb.LoraError) as e:       # the oldest now
+            attend(1)
+        assert e.value.status == 1
+        attend(2)

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <cstddef>
 #include <vector>
 
 #include "lora_b200.h"
@@ -185,12 +186,11 @@ struct lora_pool {
     };
     std::vector<MetaRecord> metas;
     void remember_meta(const void *ptr, int32_t T, int32_t tile_m, int32_t long_min, bool has_list) {
-        for (MetaRecord &m : metas)
-            if (m.ptr == ptr) {
-                m.T = T; m.tile_m = tile_m; m.long_min = long_min; m.fresh = true; m.has_list = has_list;
-                return;
-            }
-        if (metas.size() >= 256) metas.erase(metas.begin());
+        // the latest at the back: the table built longest ago is the one that is forgotten
+        size_t at = 0;
+        while (at < metas.size() && metas[at].ptr != ptr) ++at;
+        if (at == metas.size() && at >= 256) at = 0;
+        if (at < metas.size()) metas.erase(metas.begin() + (std::ptrdiff_t)at);
         metas.push_back({ptr, T, tile_m, long_min, true, has_list});
     }
     bool meta_has_list(const void *ptr) const {

@@ -50,3 +50,34 @@ def test_two_pools_apply_in_turn(kind, ranks, tuning):
         want = bf16_bits(a.apply()), bf16_bits(b.apply())
         for s, w in ((a, want[0]), (b, want[1]), (a, want[0])):
             assert np.array_equal(bf16_bits(s.apply()), w)
+
+
+def test_lists_built_again_are_not_the_oldest():
+    """A pool knows the last 256 lists that it built: one that was built first, and again just now, is among them
+    when the 257th comes."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    buf = torch.zeros(lb.pool_bytes(2, 8, [(16, 16)]) + 256, dtype=torch.uint8, device="cuda")
+    pool = lb.pool_create(2, 8, [(16, 16)], buf[(-buf.data_ptr()) % 256:])
+    try:
+        n = (lb.segments_bytes(1, 2, 16) + 15) // 16 * 4
+        lists = torch.zeros((257, n), dtype=torch.int32, device="cuda")
+        slot = _i32([0])
+        ws = torch.zeros(max(lb.workspace_bytes(pool, 1), 16), dtype=torch.uint8, device="cuda")
+        x = torch.zeros((1, 16), dtype=torch.bfloat16, device="cuda")
+
+        def apply(i):
+            lb.bgmv_apply(pool, 0, x, 16, x, 16, x, 16, slot, 1, lists[i], ws)
+
+        for i in [*range(256), 0, 256]:
+            lb.build_segments(pool, slot, 1, 16, 128, lists[i])
+        apply(0)
+        apply(256)
+        with pytest.raises(lb.LoraError) as e:       # the oldest now
+            apply(1)
+        assert e.value.status == 1
+        apply(2)
+        torch.cuda.synchronize()
+    finally:
+        lb.pool_destroy(pool)

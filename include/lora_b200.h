@@ -549,6 +549,7 @@ lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, i
  * more; in requests with more than 64 rows (q_len * num_q_heads / num_kv_heads) a probability is rounded to
  * 11 bits, or to 2^-33 of the largest where that is more, and the values to 11 bits, or to 2^-23 of the
  * request's largest scale or |low| so far.  Queries beyond 2^110 count as infinite.  The result does not depend on timing.
+ * scale is finite, and so is scale * log2(e).
  * Calls on one workspace must be ordered on one stream; the workspace's contents are undefined afterwards.
  * Errors: INVALID_ARG, SHAPE, SLOT_RANGE (layer), BUFFER_TOO_SMALL (workspace), CUDA.
  */

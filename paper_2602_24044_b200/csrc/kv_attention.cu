@@ -1,4 +1,6 @@
 // Attention of a batch over one layer of the 4-bit cache.
+#include <cmath>
+
 #include "kv_decode.cuh"
 #include "kv_prompt.cuh"
 
@@ -87,6 +89,8 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)tables) & 15) return LORA_ERR_INVALID_ARG;
     const char *a = (const char *)q, *b = (const char *)out;
     if (a < b + ((T - 1) * ldo + width) * 2 && b < a + ((T - 1) * ldq + width) * 2) return LORA_ERR_INVALID_ARG;
+    const float scale2 = scale * 1.4426950408889634f;
+    if (!std::isfinite(scale2)) return LORA_ERR_INVALID_ARG;
     size_t need = 0;
     lora_kv_workspace_bytes(kv, &need);
     if (!workspace || ((uintptr_t)workspace & 15)) return LORA_ERR_INVALID_ARG;
@@ -106,7 +110,7 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     P.L = kv_tables(R, T, kv->group, kv->dec_walkers(), kv->pr_walkers());
     P.kv = kv->view(layer);
     P.window = rec->window;
-    P.scale2 = scale * 1.4426950408889634f;
+    P.scale2 = scale2;
     P.walkers = kv->dec_walkers();
     P.part = (float *)workspace;
     P.part_ml = (float2 *)(P.part + (size_t)2 * P.walkers * rows * kv->d);

@@ -253,3 +253,17 @@ def test_tables_written_again_are_not_the_oldest():
             attend(1)
         assert e.value.status == 1
         attend(2)
+
+
+def test_a_scale_that_is_no_number_is_refused():
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    b = Batch([(20, 1)], 4, 2, 128, seed=17)
+    out = torch.zeros_like(b.qd)
+    before = lb.launch_count()
+    for scale in (float("nan"), float("inf"), -float("inf"), 3e38):
+        with pytest.raises(lb.LoraError) as e:
+            b.c.attention(0, b.qd, out, scale=scale)
+        assert e.value.status == 1
+    assert lb.launch_count() == before and (_np(out) == 0).all()

@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                 const float u = (i & 1) ? unit * 0.0625f : unit;
                 qf[n][i] = pack_f16(__uint_as_float(qf[n][i] << 16) * u, __uint_as_float(qf[n][i] & 0xffff0000u) * u);
             }
-            const float f = fmaxf(fabsf(P.scale2) * pow2(a + 9), 1e-30f);     // never 0: masked scores stay -inf
+            const float f = fmaxf(fabsf(P.scale2) * pow2(a + 9), 1.17549435e-38f);     // never 0: masked scores stay -inf
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 qs[n][j] = __shfl_sync(0xffffffffu, sum, (2 * c + j) * 4);

@@ -267,3 +267,14 @@ def test_a_scale_that_is_no_number_is_refused():
             b.c.attention(0, b.qd, out, scale=scale)
         assert e.value.status == 1
     assert lb.launch_count() == before and (_np(out) == 0).all()
+
+
+@pytest.mark.parametrize("lens", [[(70, 1)], [(10, 90)]])
+def test_scale_zero_with_huge_keys(lens):
+    """scale 0 is the mean of the values, however large the keys are."""
+    require_gpu()
+    b = Batch(lens, 4, 2, 128, seed=18, scale=0.0)
+    for i in (1, 2):
+        b.Kq[i] = (b.Kq[i] * np.float32(2.0 ** 110)).astype(np.float32)
+    b.store()
+    b.check()

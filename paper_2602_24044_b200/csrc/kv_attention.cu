@@ -87,8 +87,7 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
     const int64_t width = (int64_t)kv->hq * kv->d;
     if (ldq < width || ldo < width || ldq % 8 || ldo % 8) return LORA_ERR_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)tables) & 15) return LORA_ERR_INVALID_ARG;
-    const char *a = (const char *)q, *b = (const char *)out;
-    if (a < b + ((T - 1) * ldo + width) * 2 && b < a + ((T - 1) * ldq + width) * 2) return LORA_ERR_INVALID_ARG;
+    if (rows_overlap(q, width * 2, ldq * 2, out, width * 2, ldo * 2, T)) return LORA_ERR_INVALID_ARG;
     const float scale2 = scale * 1.4426950408889634f;
     if (!std::isfinite(scale2)) return LORA_ERR_INVALID_ARG;
     size_t need = 0;

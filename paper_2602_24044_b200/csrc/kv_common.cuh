@@ -124,6 +124,18 @@ __host__ __device__ inline KvTables kv_tables(int32_t R, int32_t T, int32_t grou
     return L;
 }
 
+// Do T rows of `wa` bytes at pitch `lda` and T rows of `wb` bytes at pitch `ldb` touch?  Rows of one
+// pitch may interleave (parts of a fused projection's rows).
+inline bool rows_overlap(const void *a, int64_t wa, int64_t lda, const void *b, int64_t wb, int64_t ldb, int32_t T) {
+    const char *pa = (const char *)a, *pb = (const char *)b;
+    const char *ea = pa + (T - 1) * lda + wa, *eb = pb + (T - 1) * ldb + wb;
+    if (ea <= pb || eb <= pa) return false;
+    if (lda != ldb) return true;
+    int64_t d = (pb - pa) % lda;
+    if (d < 0) d += lda;
+    return d < wa || d + wb > lda;
+}
+
 struct KvTableRecord {        // what the host knows of a table it built
     const void *ptr;
     int32_t R, T, max_q, window;

@@ -355,18 +355,6 @@ read_kernel(const KvView kv, const int32_t *slots, int32_t n, int32_t per_block,
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
-// Do T rows of `wa` bytes at pitch `lda` and T rows of `wb` bytes at pitch `ldb` touch?  Rows of one
-// pitch may interleave (parts of a fused projection's rows).
-static bool rows_overlap(const void *a, int64_t wa, int64_t lda, const void *b, int64_t wb, int64_t ldb, int32_t T) {
-    const char *pa = (const char *)a, *pb = (const char *)b;
-    const char *ea = pa + (T - 1) * lda + wa, *eb = pb + (T - 1) * ldb + wb;
-    if (ea <= pb || eb <= pa) return false;
-    if (lda != ldb) return true;
-    int64_t d = (pb - pa) % lda;
-    if (d < 0) d += lda;
-    return d < wa || d + wb > lda;
-}
-
 static lora_status_t check_rows(const void *p, int64_t ld, int32_t heads, int32_t d) {
     if (!p || ((uintptr_t)p & 15)) return LORA_ERR_INVALID_ARG;
     if (ld < (int64_t)heads * d || ld % 8) return LORA_ERR_SHAPE;

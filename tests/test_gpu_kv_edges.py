@@ -278,3 +278,22 @@ def test_scale_zero_with_huge_keys(lens):
         b.Kq[i] = (b.Kq[i] * np.float32(2.0 ** 110)).astype(np.float32)
     b.store()
     b.check()
+
+
+def test_queries_and_outputs_may_be_parts_of_the_same_rows():
+    """Rows of one pitch that lie beside each other do not overlap; those that do are refused."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    b = Batch([(70, 1), (0, 200)], 4, 2, 128, seed=19)
+    want, _ = b.run()
+    wide = torch.full((b.T, 2 * 512 + 24), 3.0, dtype=torch.bfloat16, device="cuda")
+    wide[:, 16:528] = b.qd
+    b.c.attention(0, wide[:, 16:528], wide[:, 528:1040], scale=b.scale)
+    got = _np(wide)
+    assert np.array_equal(got[:, 528:1040].reshape(want.shape), want)
+    assert np.array_equal(got[:, 16:528], b.q) and (got[:, :16] == 3).all() and (got[:, 1040:] == 3).all()
+    for q, out in ((wide[:, :512], wide[:, 504:1016]), (wide[:, 512:1024], wide[:, 8:520]), (wide[:, 8:520], wide[:, 8:520])):
+        with pytest.raises(lb.LoraError) as e:
+            b.c.attention(0, q, out, scale=b.scale)
+        assert e.value.status == 1

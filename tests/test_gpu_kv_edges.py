@@ -1,5 +1,5 @@
-"""The paged 4-bit cache on the GPU where it went wrong, or was never run: several handles at once, tables in
-turn, probabilities far below the largest, groups of every size, batches of many rows."""
+"""The paged 4-bit cache on the GPU at its edges: several handles at once, tables in turn, streams, probabilities
+far below the largest, bad pages and scales, groups of every size, batches of many rows."""
 import numpy as np
 import pytest
 
@@ -297,3 +297,100 @@ def test_queries_and_outputs_may_be_parts_of_the_same_rows():
         with pytest.raises(lb.LoraError) as e:
             b.c.attention(0, q, out, scale=b.scale)
         assert e.value.status == 1
+
+
+@pytest.mark.parametrize("hq,hkv,D", [(16, 1, 128), (24, 2, 64), (20, 1, 64), (128, 1, 64)])
+@pytest.mark.parametrize("P,window", [(16, 0), (32, 21)])
+def test_attention_of_mixed_batches_in_wide_groups(hq, hkv, D, P, window):
+    """More than eight query heads share keys: items of sixteen rows that span tokens, and prompts."""
+    require_gpu()
+    lens = [(0, 1), (5, 0), (40, 3), (0, 19), (100, 5), (0, 41), (77, 1), (130, 2), (31, 4), (60, 1)]
+    Batch(lens, hq, hkv, D, P, window, seed=hq + P).check()
+
+
+@pytest.mark.parametrize("hq,hkv,D", [(72, 1, 128), (130, 2, 64), (128, 1, 64), (9, 1, 128)])
+def test_attention_of_single_tokens_in_wide_groups(hq, hkv, D):
+    """Above 64 query heads a key/value head one token alone is a prompt's tile."""
+    require_gpu()
+    lens = [(k, 1) for k in (0, 1, 15, 16, 31, 33, 127, 128, 129, 300)]
+    Batch(lens, hq, hkv, D, seed=hq, max_q=1).check()
+
+
+@pytest.mark.parametrize("hq", [16, 72])
+@pytest.mark.parametrize("max_q", [0, 2])
+def test_failed_requests_and_spare_tokens_in_wide_groups(hq, max_q):
+    require_gpu()
+    b = Batch([(20, 2), (10, 40), (33, 1)], hq, 1, 64, max_q=max_q, pad_tokens=3, seed=4)
+    want = b.check()
+    assert (want[-3:] == 0).all() and ((want[2:42] == 0).all() == (max_q == 2))
+
+
+@pytest.mark.parametrize("D,hq,hk", [(128, 30, 5), (64, 45, 9)])
+@pytest.mark.parametrize("rot,inter", [(0, False), (1, False), (32, False), (48, True)])
+def test_many_rows_are_the_same_as_few(D, hq, hk, rot, inter):
+    """Batches that are large enough for a warp to take several passes of heads: bit for bit what calls of 250
+    tokens give, and a sample of rows against the definition; with and without the cache."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    rot = D if rot == 1 else rot
+    per = 512 // D
+    T = 32768 // -(-(hq + hk) // per) + 7          # the first count, with a margin, at which passes are put together
+    rng = np.random.default_rng(D + rot)
+    n_pages = -(-T // 16) + 1
+    g = torch.Generator(device="cuda").manual_seed(D + rot)
+    x = torch.randn(T, (hq + 2 * hk) * D, generator=g, device="cuda").mul_(
+        torch.rand((hq + 2 * hk) * D, generator=g, device="cuda") + 0.5).bfloat16()
+    w = ref.bf16(1 + 0.3 * rng.standard_normal(D).astype(np.float32))
+    wd = _dev(w, torch.bfloat16)
+    pos = rng.integers(-1, 301, T).astype(np.int32)       # -1 and 300 are outside the table
+    slots = rng.permutation(n_pages * 16)[:T].astype(np.int32)
+    pos_d, slots_d, cs = _i32(pos), _i32(slots), _angles(300, rot) if rot else None
+    cs_d = _dev(cs) if rot else None
+    ld = x.stride(0)
+
+    def args(a, b, q_out, k_out):
+        return lb.qk_args(num_q_heads=hq, num_kv_heads=hk, head_dim=D, q=x[a:b], ldq=ld, k=x[a:b, hq * D:], ldk=ld,
+                          v=x[a:b, (hq + hk) * D:], ldv=ld, q_weight=wd, k_weight=wd, eps=1e-6, cos_sin=cs_d,
+                          positions=pos_d[a:b], interleaved=inter, q_out=q_out[a:b], k_out=k_out[a:b])
+
+    def outputs():
+        return (torch.full((T, hq * D + 8), 7.0, dtype=torch.bfloat16, device="cuda"),
+                torch.full((T, hk * D), 7.0, dtype=torch.bfloat16, device="cuda"))
+
+    pieces = [(a, min(a + 250, T)) for a in range(0, T, 250)]
+    one, few = outputs(), outputs()
+    lb.qk_norm_rope(args(0, T, *one), T)
+    for a, b in pieces:
+        lb.qk_norm_rope(args(a, b, *few), b - a)
+    assert all(torch.equal(p, q) for p, q in zip(one, few))
+    sample = np.unique(np.concatenate([np.arange(0, T, 61), [T - 1]]))
+    rows = _np(x[_dev(sample)])
+
+    def want(part):
+        y = ref.norm32(part.reshape(-1, D), w, 1e-6)
+        if rot:
+            p = np.repeat(pos[sample], y.shape[0] // sample.size)
+            ok = (p >= 0) & (p < 300)
+            y = np.where(ok[:, None], ref.rotate(y, cs[np.where(ok, p, 0)], rot, inter), y)
+        return y.reshape(sample.size, -1)
+
+    wq, wk = want(rows[:, :hq * D]), want(rows[:, hq * D:(hq + hk) * D])
+    assert np.array_equal(_np(one[0])[sample, :hq * D], ref.bf16(wq)) and (_np(one[0])[:, hq * D:] == 7).all()
+    assert np.array_equal(_np(one[1])[sample], ref.bf16(wk))
+    with _cache(num_pages=n_pages, num_q_heads=hq, num_kv_heads=hk, head_dim=D) as c:
+        bytes_ = []
+        for calls in ([(0, T)], pieces):
+            c.mem[256:].zero_()
+            out = outputs()
+            for a, b in calls:
+                lb.kv_append(c.kv, 0, args(a, b, *out), slots_d[a:b], b - a)
+            assert all(torch.equal(p, q) for p, q in zip(one, out))
+            bytes_.append(c.layer(0).clone())
+        assert torch.equal(*bytes_)
+        back = torch.empty((2, sample.size, hk * D), dtype=torch.bfloat16, device="cuda")
+        c.read(0, _i32(slots[sample]), back[0], back[1])
+        for got, val in zip(_np(back), (wk, rows[:, (hq + hk) * D:])):
+            assert np.array_equal(got, ref.bf16(ref.dequantise32(*ref.quantise(val.reshape(-1, D)))).reshape(got.shape))
+        if rot:
+            assert c.status()[0] == 2 * int(((pos < 0) | (pos >= 300)).sum())

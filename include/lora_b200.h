@@ -466,7 +466,8 @@ lora_status_t lora_kv_check_status(lora_kv_t *kv, void *stream, int32_t *words_o
  * [r, i] (row r at r * ld_table, i = page number inside the request) is written for new pages and
  * read for old ones.  A request gets all the pages it needs or fails: a request that needs pages
  * fails once the pages needed up to and including it exceed the stack; so does one that needs more
- * than ld_table pages, has more than max_q new tokens or tokens past T.  A failed request keeps its
+ * than ld_table pages, has more than max_q new tokens or tokens past T (so do all behind that one, idle ones
+ * too).  A failed request keeps its
  * length, its slots are -1 and its attention is zero.  A negative length counts as 0.
  * kv_len_out [R] and free_count_out [1] may be the inputs themselves or NULL.  window: 0, or how many
  * keys a query sees, itself included (for the attention calls on these tables).  max_q bounds the

@@ -55,7 +55,7 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 // ---------------------------------------------------------------------------------------------
 // batch tables (int32 words): public part as documented, then the attention's work lists
 // ---------------------------------------------------------------------------------------------
-enum { KVH_R = 0, KVH_T = 1, KVH_TOKENS = 2, KVH_FAILED = 3, KVH_NEGATIVE = 4, KVH_TAKEN = 5, KVH_WORDS = 16 };
+constexpr int KVH_WORDS = 16;      // of the header, the first six in use
 
 // A piece of attention work before it is multiplied by the key/value heads: some rows of one request
 // (row = token * group + query head inside its group) against a run of key chunks.  An item of n
@@ -97,7 +97,6 @@ struct KvTables {
     int64_t dec_items, pr_items;                   // KvItem lists
     int64_t dec_first, pr_first;                   // first item of each walker
     int64_t words;
-    int32_t cap_dec, cap_pr;
 };
 
 __host__ __device__ inline KvTables kv_tables(int32_t R, int32_t T, int32_t group, int32_t dec_walkers,
@@ -112,9 +111,7 @@ __host__ __device__ inline KvTables kv_tables(int32_t R, int32_t T, int32_t grou
     // a request of q tokens has ceil(q * group / rows) items: at most one more than q * group / rows
     const int64_t rows = (int64_t)T * group;
     // (the tokens of no request count as one more)
-    int64_t cd = R + 1 + rows / 8, cp = R + rows / KV_PROMPT_ROWS;
-    L.cap_dec = (int32_t)(cd < 0x7fffffff ? cd : 0x7fffffff);
-    L.cap_pr = (int32_t)(cp < 0x7fffffff ? cp : 0x7fffffff);
+    const int64_t cd = R + 1 + rows / 8, cp = R + rows / KV_PROMPT_ROWS;
     L.walk = o;      o += 2 * (int64_t)(sizeof(KvWalk) / 4);
     L.dec_items = o; o += cd * (int64_t)(sizeof(KvItem) / 4);
     L.pr_items = o;  o += cp * (int64_t)(sizeof(KvItem) / 4);

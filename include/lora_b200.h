@@ -445,11 +445,11 @@ lora_status_t lora_kv_layer_range(const lora_kv_desc_t *desc, int32_t layer, siz
 lora_status_t lora_kv_create(const lora_kv_desc_t *desc, lora_kv_t **out);
 lora_status_t lora_kv_destroy(lora_kv_t *kv);
 
-/* Device status words since creation: [0] how often a slot, a position or a page was outside its range (such
- * tokens are not rotated, not stored or not seen): once a token in the calls that write, and in attention for every
- * cell of 16 keys that a query should see, each time the kernel comes to it, [1] expired device-side waits (that call's outputs are
- * not to be trusted), [2..3] reserved.  Synchronises `stream`; returns LORA_ERR_TIMEOUT when word 1
- * is non-zero.  words_out (host, [4]) may be NULL. */
+/* Device status words since creation: [0] new tokens whose slot, position or page was outside its range (they
+ * are not stored or not rotated), and pages that a release could not put back (attention does not see keys in
+ * pages outside the cache, and counts nothing); [1] expired device-side waits (that call's outputs are not to be
+ * trusted), [2..3] reserved.  Synchronises `stream`; returns LORA_ERR_TIMEOUT when word 1 is non-zero.
+ * words_out (host, [4]) may be NULL. */
 lora_status_t lora_kv_check_status(lora_kv_t *kv, void *stream, int32_t *words_out);
 
 /*

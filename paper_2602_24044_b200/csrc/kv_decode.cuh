@@ -149,13 +149,6 @@ __device__ __forceinline__ KvItem load_item(const KvItem *p) {
     return it;
 }
 
-// A cell that holds keys which some row of the item sees (from key k on; the last row's end) is in no page of the
-// cache: status word 0.
-__device__ __forceinline__ void count_missing(const AttnParams &P, const KvItem &it, int32_t k, int32_t end) {
-    const int32_t first = P.window > 0 ? it.lim0 + it.row0 / P.kv.group - P.window : 0;
-    if (k < end && k + KV_CELL > first) atomicAdd(&P.kv.status[STATUS_INVALID_TOKENS], 1);
-}
-
 // A common exponent of rows: what their scales and lows are divided by.  A row whose magnitude is 2^a
 // needs e >= a - MARGIN; a new exponent is set to the row's own, or to MOST.
 template <int MARGIN, int MOST>
@@ -348,7 +341,6 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
             const int32_t key0 = it.k_lo + chunk * KV_DEC_CHUNK;
             const bool whole = valid == 3u && key0 + KV_DEC_CHUNK <= lim_min && (P.window == 0 || key0 >= lim_max - P.window);
 
-            if (valid != 3u && lane < 2 && !((valid >> lane) & 1u)) count_missing(P, it, key0 + lane * KV_CELL, lim_max);
             // (two copies of what follows: one for chunks of which every row sees every key)
             auto work = [&](auto all) {
                 constexpr bool WHOLE = decltype(all)::value;

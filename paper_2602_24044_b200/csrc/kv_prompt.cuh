@@ -759,10 +759,7 @@ __global__ void __launch_bounds__(PK_THREADS, 1) prompt_attention_kernel(const A
                     int32_t page = -1;
                     if (lane < 8 && key < end) {
                         page = __ldg(P.block_table + cur.it.req * P.ld_table + (key >> P.kv.page_shift));
-                        if (page < 0 || page >= P.kv.num_pages) {
-                            page = -1;
-                            count_missing(P, cur.it, key, end);
-                        }
+                        if (page < 0 || page >= P.kv.num_pages) page = -1;
                     }
                     const uint32_t valid = __ballot_sync(0xffffffffu, page >= 0);
                     if (j >= PK_RAW) ok = wait(&raw_empty[rs], (j / PK_RAW - 1) & 1u);

@@ -188,22 +188,16 @@ def test_memory_that_a_side_stream_still_reads_is_not_handed_out():
     assert pending and not any(reused)
 
 
-def test_pages_outside_the_cache_are_counted():
-    """Word 0 of the status tells of a page that a block table should not hold: where a new token goes, and where
-    attention looks for a key."""
+def test_tokens_whose_page_is_outside_the_cache_are_counted():
+    """Word 0 of the status tells of a page that a block table or the stack should not hold, where a new token
+    goes: once a token, and not for tokens that fail."""
     require_gpu()
-    table = np.array([[999, -1], [3, -1]], np.int32)
+    table = np.array([[999, -1], [3, -1], [-7, -1], [998, -1]], np.int32)
     with _cache(num_pages=8) as c:
-        c.build_tables(_i32([5, 5]), _i32([1, 1]), 2, _i32(np.arange(8)), _i32([2]), _i32(table))
-        assert c.status()[0] == 1
-    for lens in ([(100, 1)], [(50, 130)]):
-        for page in (10 ** 6, -5):
-            b = Batch(lens, 4, 1, 64, seed=13)
-            b.run()
-            assert b.c.status()[0] == 0
-            b.c.block_table[0, 1] = page
-            b.run()
-            assert b.c.status()[0] > 0
+        c.build_tables(_i32([5, 5, 14, 9]), _i32([1, 1, 2, 9]), 13, _i32([4, 5, 6, 7]), _i32([4]), _i32(table), max_q=4)
+        assert c.status()[0] == 1 + 2
+        c.build_tables(_i32([16]), _i32([3]), 3, _i32([77]), _i32([1]), _i32([[2, -1]]))
+        assert c.status()[0] == 3 + 3
 
 
 def test_pages_that_no_query_sees_are_not_counted():

@@ -552,7 +552,7 @@ def kv_build_tables(kv: int, kv_len, q_len, R: int, T: int, free_pages, free_cou
     p = _ptr
     status = _lib().lora_kv_build_tables(kv, p(kv_len), p(q_len), R, T, max_q, window, p(free_pages), p(free_count),
                                          p(block_table), ld_table, p(kv_len_out), p(free_count_out), p(tables), nbytes,
-                                         stream if type(stream) is int else _stream(stream))
+                                         _stream(stream))
     if status:
         _check(status, "lora_kv_build_tables")
 
@@ -622,28 +622,33 @@ def _max_tokens(a) -> int:
     return most
 
 
-def _check_tokens(args, T: int, where: str) -> None:
-    if T > args.max_tokens:
-        raise LoraError(1, "%s (the tensors given hold %d tokens, not %d)" % (where, args.max_tokens, T))
+def _too_many(args, T: int, where: str) -> None:
+    raise LoraError(1, "%s (the tensors given hold %d tokens, not %d)" % (where, args.max_tokens, T))
 
 
 def qk_norm_rope(args, T: int, stream=None) -> None:
     """Per-head norm and rotation of T tokens' queries and keys; `args` from qk_args."""
-    _check_tokens(args, T, "qk_norm_rope")
-    _check(_lib().lora_qk_norm_rope(ctypes.byref(args), T, _stream(stream)), "lora_qk_norm_rope")
+    if T > args.max_tokens:
+        _too_many(args, T, "qk_norm_rope")
+    status = _lib().lora_qk_norm_rope(ctypes.byref(args), T, _stream(stream))
+    if status:
+        _check(status, "lora_qk_norm_rope")
 
 
 def kv_append(kv: int, layer: int, args, slots, T: int, stream=None) -> None:
     """qk_norm_rope with the keys and values also going to their slots of the cache as 4-bit rows."""
-    _check_tokens(args, T, "kv_append")
-    _check(_lib().lora_kv_append(kv, layer, ctypes.byref(args), _ptr(slots), T, _stream(stream)),
-           "lora_kv_append")
+    if T > args.max_tokens:
+        _too_many(args, T, "kv_append")
+    status = _lib().lora_kv_append(kv, layer, ctypes.byref(args), _ptr(slots), T, _stream(stream))
+    if status:
+        _check(status, "lora_kv_append")
 
 
 def kv_read(kv: int, layer: int, slots, n: int, k_out, ldk: int, v_out, ldv: int, stream=None) -> None:
     """Rows of the cache as the bf16 values they stand for."""
-    _check(_lib().lora_kv_read(kv, layer, _ptr(slots), n, _ptr(k_out), ldk, _ptr(v_out), ldv,
-                               _stream(stream)), "lora_kv_read")
+    status = _lib().lora_kv_read(kv, layer, _ptr(slots), n, _ptr(k_out), ldk, _ptr(v_out), ldv, _stream(stream))
+    if status:
+        _check(status, "lora_kv_read")
 
 
 def kv_workspace_bytes(kv: int) -> int:
@@ -655,11 +660,14 @@ def kv_workspace_bytes(kv: int) -> int:
 def kv_attention(kv: int, layer: int, q, ldq: int, out, ldo: int, lse, scale: float, tables, R: int,
                  T: int, block_table, ld_table: int, workspace, workspace_bytes_: Optional[int] = None,
                  stream=None) -> None:
-    nbytes = (_nbytes(workspace) if workspace is not None else 0) \
-        if workspace_bytes_ is None else workspace_bytes_
-    _check(_lib().lora_kv_attention(kv, layer, _ptr(q), ldq, _ptr(out), ldo, _ptr(lse), scale, _ptr(tables),
-                                    R, T, _ptr(block_table), ld_table, _ptr(workspace), nbytes,
-                                    _stream(stream)), "lora_kv_attention")
+    nbytes = workspace_bytes_
+    if nbytes is None:
+        nbytes = 0 if workspace is None else _nbytes(workspace)
+    p = _ptr
+    status = _lib().lora_kv_attention(kv, layer, p(q), ldq, p(out), ldo, p(lse), scale, p(tables), R, T, p(block_table),
+                                      ld_table, p(workspace), nbytes, _stream(stream))
+    if status:
+        _check(status, "lora_kv_attention")
 
 
 # ------------------------------------------------------------------------------------------

@@ -205,6 +205,7 @@ class KVCache:
         self.device = torch.device("cuda", int(device))
         self._index = int(device)
         self.shape = (num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim)
+        self._width = num_q_heads * head_dim
         self._streams = set()            # handles of the streams that work on the buffers was queued on
         nbytes = lb.kv_bytes(*self.shape, device=int(device))
         self.buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
@@ -360,10 +361,15 @@ class KVCache:
 
     def attention(self, layer: int, q, out, *, scale: float, lse=None, stream=None) -> None:
         """q, out: rows of num_q_heads * head_dim values, one per new token of the tables; lse: fp32 in a row."""
-        T, width = self.T, self.shape[3] * self.shape[5]
+        T, width = self.T, self._width
         if self.block_table is None:
             raise ValueError("attention: no tables have been built")
-        ldq, ldo = self._rows("q", q, T, width), self._rows("out", out, T, width)
+        shape = q.shape
+        if (shape == (T, width) and out.shape == shape and q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16 and
+                q.get_device() == out.get_device() == self._index and q.is_contiguous() and out.is_contiguous()):
+            ldq = ldo = width        # the usual case without a call each: a small batch's time is the host's
+        else:
+            ldq, ldo = self._rows("q", q, T, width), self._rows("out", out, T, width)
         if lse is not None and (lse.dtype is not torch.float32 or lse.numel() < T * self.shape[3] or
                                 not lse.is_contiguous() or lse.get_device() != self._index):
             raise ValueError("lse: needs %d x %d fp32 in a row on %s" % (T, self.shape[3], self.device))

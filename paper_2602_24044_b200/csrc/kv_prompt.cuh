@@ -26,9 +26,9 @@
 // The (item, head, block) triples form one walk cut into equal spans, one per SM; what a span's ends cut is
 // joined afterwards.  Tensor memory: scores of both tiles (2 x 128 columns), accumulators (2 x head_dim).
 //
-// Measured: 2048 tokens on 30001 cached keys 1.23 ms (850 TFLOP/s), 5400 cycles a block: the issuing warp is in
+// Measured: 2048 tokens on 30001 cached keys 1.24 ms (840 TFLOP/s), 5400 cycles a block: the issuing warp is in
 // the products 43 % of them and waits for probabilities 20 % and for widened tiles 24 %.  32 prompts of 32..2048
-// tokens 259 us.  Measured and not faster (the first case, 1.22..1.27 ms at the time): two threads a row 1.30..1.33,
+// tokens 263 us, of which the blocks at that pace are 143.  Measured and not faster (the first case, 1.22..1.27 ms at the time): two threads a row 1.30..1.33,
 // eight widening warps 1.28, all scores in registers 1.33, an eighth or a quarter of the exponentials as
 // polynomials 1.26, 1.31.
 #pragma once

@@ -14,7 +14,9 @@
 
 namespace lora {
 
-// Passes of a warp when there are many rows, and blocks of an SM that the registers have to leave room for.
+// Passes of a warp when there are many rows, and blocks of 256 threads that the registers have to leave room for
+// on an SM.  (Ten and twelve passes a token, three a warp, are blocks of 128: with the bound of three blocks, 80
+// registers a thread, six of them are on an SM.)
 // Norm and rotation of 12936 tokens (10 passes a token) / with the cache and the read back (12 passes), us:
 //   no bound on registers:  2 passes 65.9 / 104   3 passes 59.8 / 101   4 passes 64.4 / 103
 //   three blocks:           2 passes 59.1 / 102   3 passes 58.3 / 92.2

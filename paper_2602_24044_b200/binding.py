@@ -602,7 +602,7 @@ def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: 
 
 
 def _max_tokens(a) -> int:
-    """The tokens that fit the tensors of an argument block."""
+    """The tokens that fit the memory from the tensors of an argument block on."""
     q, k, v, q_weight, k_weight, cos_sin, positions, q_out, k_out = a._keep
     most, d, device = 2 ** 31 - 1, a.head_dim, a.device
     for what, t, heads, ld in (("q", q, a.num_q_heads, a.ldq), ("k", k, a.num_kv_heads, a.ldk),
@@ -615,10 +615,11 @@ def _max_tokens(a) -> int:
     _elements("k_weight", k_weight, "bfloat16", device, d)
     if cos_sin is not None:
         _elements("cos_sin", cos_sin, "float32", device, a.num_positions * a.rot_dim)
-        if _elements("positions", positions, "int32", device, 0) is not None:
+        n = _elements("positions", positions, "int32", device)
+        if n is not None:
             if not positions.is_contiguous():
                 raise LoraError(1, "positions (needs its values in a row)")
-            most = min(most, positions.numel())
+            most = min(most, n)
     return most
 
 

@@ -246,6 +246,8 @@ def test_argument_blocks_know_how_many_tokens_they_hold():
     assert lb.qk_args(**dict(kw, k=fused[:, 400:])).max_tokens == 4       # its last row reaches past the end
     a = lb.qk_args(**dict(kw, cos_sin=torch.zeros(9, 64), positions=_i32(3)))
     assert a.max_tokens == 3
+    # (positions of a table buffer that holds more than the batch the view was made for)
+    assert lb.qk_args(**dict(kw, cos_sin=torch.zeros(9, 64), positions=_i32(9)[2:4])).max_tokens == 5
     for call in (lambda: lb.qk_norm_rope(a, 4), lambda: lb.kv_append(None, 0, a, None, 4)):
         with pytest.raises(lb.LoraError) as e:
             call()

@@ -538,10 +538,10 @@ lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, i
  * num_kv_heads) holds,
  *     out[t, h] = sum_j softmax_j(scale * q[t, h] . k_j) v_j ,   lse[t, h] = log sum_j exp(scale * q . k_j)
  * with k and v the values that the cache's rows stand for.  Call it after the batch's keys have been
- * appended.  Queries of tokens without a request, of a failed request or without a key give zeros and lse
- * = -inf; a key in a page outside the cache is not seen.  q, out: dev bf16 [T, num_q_heads * head_dim]
- * with leading dimensions; rows of out may lie beside rows of q (one leading dimension), but not on them;
- * lse: dev fp32 [T, num_q_heads] or NULL.  tables: as written by lora_kv_build_tables for this R and T (and
+ * appended.  Queries of tokens without a request, of a failed request or without a key give zeros and lse =
+ * -inf; a key in a page outside the cache is not seen.  q, out: dev bf16 [T, num_q_heads * head_dim] with
+ * leading dimensions; rows of out may lie beside rows of q (one leading dimension), but not on them; lse:
+ * dev fp32 [T, num_q_heads] or NULL.  tables: as written by lora_kv_build_tables for this R and T (and
  * through this handle, which knows the 256 buffers that it wrote tables to last), block_table the one it
  * was given.  A row of the cache that is not finite makes the outputs that see it NaN and no others.
  * Statistics and sums are fp32.  Both products run on tensor cores with fp16 operands and fp32 sums:
@@ -550,9 +550,12 @@ lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, i
  * or to 2^-33 of the largest probability times the largest scale (or |low| / 16) where that is more; in
  * requests with more than 64 rows (q_len * num_q_heads / num_kv_heads) a probability is rounded to 11 bits,
  * or to 2^-33 of the largest where that is more, and the values to 11 bits, or to 2^-23 of the request's
- * largest scale or |low| so far.  Queries beyond 2^110 count as infinite.  The result does not depend on
- * timing.  scale is finite, and so is scale * log2(e).  Calls on one workspace must be ordered on one
- * stream; the workspace's contents are undefined afterwards.
+ * largest scale or |low| so far.  The other requests' codes enter as subnormal numbers, which costs their
+ * sums bits: a score is good to about 2^-14 of the row's largest |q| times the key's scale (times scale;
+ * 2^-17 is usual), an output to about 2^-13 of the largest probability times its scale (2^-19 is usual).
+ * Queries beyond 2^110 count as infinite.  The result does not depend on timing.  scale is finite, and so
+ * is scale * log2(e).  Calls on one workspace must be ordered on one stream; the workspace's contents are
+ * undefined afterwards.
  * Errors: INVALID_ARG, SHAPE, SLOT_RANGE (layer), BUFFER_TOO_SMALL (workspace), CUDA.
  */
 lora_status_t lora_kv_workspace_bytes(const lora_kv_t *kv, size_t *bytes);

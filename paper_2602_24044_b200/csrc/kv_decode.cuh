@@ -13,7 +13,11 @@
 // tensor cores whatever the number of query heads is; 1.2 instructions a code (to c - 8 in bf16 and fp16)
 // were 983 a chunk and a full integer pipe, 209 us where the bytes need 97.  Hence:
 //   - a nibble masked in place IS an fp16 number (a subnormal one, c 2^-24 or c 2^-20): two thirds of an
-//     instruction a code, and the powers of two are put on the queries and taken from the outputs;
+//     instruction a code, and the powers of two are put on the queries and taken from the outputs.  (The tensor
+//     cores align products by the exponents as they stand, so that small ones lose bits beside a subnormal
+//     factor: scores are off by 2^-17.4 of max |q| s scale, rms, 2^-14.7 at most, where prompts, whose codes are
+//     normal numbers, have 2^-19.2 and 2^-16.3; outputs by up to 2^-13 of the largest p s, 2^-19 as a rule.  Both are
+//     below what the 11 bits of p s cost.);
 //   - a warp works alone: its own ring of chunks (32 keys, two cells) filled by bulk copies, its own
 //     maximum and sums; no block barrier anywhere;
 //   - the matrix instructions take the keys as their 16 rows and up to eight query rows as their 8

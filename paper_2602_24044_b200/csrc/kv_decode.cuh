@@ -3,11 +3,16 @@
 //
 //   o = sum_t p_t v_t / sum_t p_t ,  p_t = 2^(x_t - m) ,  x_t = log2(e) scale q . k_t
 //   k_t = low_t + s_t c_t :   q . k_t = s_t (q . c_t) + low_t sum(q)
-//   sum_t p_t v_t = sum_t (p_t s_t) c_t - 8 sum_t (p_t s_t) + sum_t p_t (low_t + 8 s_t)
+//   sum_t p_t v_t = sum_A (p_t s_t) c_t + sum_B (-p_t s_t) (15 - c_t) - 7.5 (sum_A p_t s_t + sum_B -p_t s_t)
+//                   + sum_t p_t (low_t + 7.5 s_t)
 // so a code is never multiplied by its scale: the scale enters once per score and once per probability, and
-// the low values of the values add one number per row.  (The middle sum, over the rounded p s, centres the
-// codes, and the last one is taken over the rounded p s as well where that is exact enough: a rounding of p
-// then counts v_t times.)
+// the low values of the values add one number per row.  A and B are the first and the last eight keys of a cell:
+// the tensor cores cut their sums off towards zero at every step, so that a sum of codes that only grows is too
+// small by a part of itself that grows with the number of keys (of equal weight, values around zero: outputs 0.8 %
+// off at 16383 keys, 8.7 % at 131071, where their own rounding is 0.17 %); with the complements of half of the
+// codes all sums stay about as small as the result is, at no cost.  (The sum of p s, over its rounded values, takes
+// the middle of the codes out again, and the last one is taken over the rounded p s as well where that is exact
+// enough: a rounding of p then counts v_t times.)
 //
 // What bounds it: every key costs head_dim + 8 bytes, and each of its codes has to be widened for the
 // tensor cores whatever the number of query heads is; 1.2 instructions a code (to c - 8 in bf16 and fp16)
@@ -307,8 +312,8 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
         }
         const int32_t lim_min = it.lim0 + it.row0 / group;
         const int32_t lim_max = it.lim0 + (it.row0 + it.nrows - 1) / group;
-        // o: outputs, lo nibbles times 2^-24, high ones times 2^-20; sp: sums of the rounded p s, which take the
-        // offset 8 of the codes out again.  A score x as it is held is qx x in log2; nm: DK_UNIT - (maximum in
+        // o: outputs, lo nibbles times 2^-24, high ones times 2^-20; sp: -7.5 times the sum of the
+        // rounded p s, signed as they are, which takes the middle of the codes out again.  A score x as it is held is qx x in log2; nm: DK_UNIT - (maximum in
         // log2) (0 while nothing was seen), so that a probability with its unit is 2^(qx x + nm); top: the x that raises the maximum
         float o[NT][MT][4], sp[NT][4], nm[NT][2], top[NT][2], l[NT][2], z[NT][2];
 #pragma unroll
@@ -482,15 +487,17 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const float s = __uint_as_float(vp_[b][r] << 16), low = __uint_as_float(vp_[b][r] & 0xffff0000u);
-                        vs[r] = s * unit;
-                        add[r] = fmaf(low, rcp_approx(s), 8.0f);
+                        // (r = 1: the keys of B, whose p s is negative)
+                        vs[r] = s * (r ? -unit : unit);
+                        add[r] = r ? fmaf(-low, rcp_approx(s), -7.5f) : fmaf(low, rcp_approx(s), 7.5f);
                         if (!WHOLE && vp_[b][r] == 0) add[r] = 0.0f;
                         near = near && fabsf(add[r]) <= 16.0f;
                     }
                     const bool far = !__all_sync(0xffffffffu, near);
                     if (far) {
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) add[r] = fmaf(8.0f, vs[r], __uint_as_float(vp_[b][r] & 0xffff0000u) * unit);
+                        for (int r = 0; r < 2; ++r)
+                            add[r] = fmaf(r ? -7.5f : 7.5f, vs[r], __uint_as_float(vp_[b][r] & 0xffff0000u) * unit);
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -520,8 +527,8 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                             }
                             pb[n][r] = movmatrix_trans(ph);
                         }
-                        const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
-                        mma16816_f16(sp[n], ones, pb[n][0], pb[n][1]);
+                        const uint32_t middle[4] = {0xc780c780u, 0xc780c780u, 0xc780c780u, 0xc780c780u};   // -7.5
+                        mma16816_f16(sp[n], middle, pb[n][0], pb[n][1]);
                     }
                     uint32_t v[4][D / 64];     // rows c, c + 4, c + 8, c + 12 of the cell: matrix columns 2c, 2c+1, 2c+8, 2c+9
 #pragma unroll
@@ -536,7 +543,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                         for (int j = 0; j < 4; ++j) {
                             const uint32_t sel = j | ((4 + j) << 8);     // byte j of both words, one in each half
                             const uint32_t lo = __byte_perm(v[0][u], v[1][u], sel), hi = __byte_perm(v[2][u], v[3][u], sel);
-                            const uint32_t a[4] = {lo & NIB_LO, lo & NIB_HI, hi & NIB_LO, hi & NIB_HI};
+                            const uint32_t a[4] = {lo & NIB_LO, lo & NIB_HI, ~hi & NIB_LO, ~hi & NIB_HI};
 #pragma unroll
                             for (int n = 0; n < NT; ++n) mma16816_f16(o[n][u * 4 + j], a, pb[n][0], pb[n][1]);
                         }
@@ -562,7 +569,7 @@ __global__ void __launch_bounds__(32 * DK_WARPS, NT == 1 ? 4 : 3) decode_attenti
                 const int32_t row = n * 8 + 2 * c + j;
                 if (row >= it.nrows) continue;
                 const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
-                const float off = zs - 8.0f * sp[n][j], ml = -nm[n][j], back = pow2(ve - 4);
+                const float off = zs + sp[n][j], ml = -nm[n][j], back = pow2(ve - 4);
                 // a lane's columns are g D/8 .. g D/8 + D/8 - 1, in the order of the codes' nibbles
                 float f[D / 8];
 #pragma unroll

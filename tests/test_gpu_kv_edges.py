@@ -60,7 +60,7 @@ def test_a_device_that_is_not_there_runs_nothing():
     assert e.value.status == 9 and lb.launch_count() == before and (_np(out) == 0).all()
 
 
-def _sink(hq, hkv, D, R, kv, q_len, bits, seed):
+def _sink(hq, hkv, D, R, kv, q_len, bits, seed, mean=0.5):
     """R requests that share one cached prefix of kv keys (the last page of each is its own), whose first key, with
     a value of zero, has a score `bits` binades above the others.  So long a walk that a span holds whole requests.
     Returns outputs, the definition's in 64 bits, sum_j p_j |v_j|, and the largest scale and value."""
@@ -72,7 +72,7 @@ def _sink(hq, hkv, D, R, kv, q_len, bits, seed):
     n = shared + R * own
     slots = n * P
     k32 = rng.standard_normal((slots, hkv, D)).astype(np.float32)
-    v32 = (0.5 + rng.standard_normal((slots, hkv, D)) * np.exp(0.5 * rng.standard_normal((slots, hkv, 1)))).astype(np.float32)
+    v32 = (mean + rng.standard_normal((slots, hkv, D)) * np.exp(0.5 * rng.standard_normal((slots, hkv, 1)))).astype(np.float32)
     k32[..., 0] = 0
     k32[0] = 0
     k32[0, :, 0] = bits * np.log(2.0) * D ** 0.5 / 4
@@ -388,3 +388,16 @@ def test_many_rows_are_the_same_as_few(D, hq, hk, rot, inter):
             assert np.array_equal(got, ref.bf16(ref.dequantise32(*ref.quantise(val.reshape(-1, D)))).reshape(got.shape))
         if rot:
             assert c.status()[0] == 2 * int(((pos < 0) | (pos >= 300)).sum())
+
+
+@pytest.mark.parametrize("D,hq,hkv,kv,q_len,R", [
+    (64, 8, 8, 16383, 1, 600), (128, 16, 4, 16383, 1, 1200), (64, 8, 8, 131071, 1, 256), (64, 4, 4, 16382, 70, 160)])
+def test_long_flat_sums_are_as_exact_as_their_rounding(D, hq, hkv, kv, q_len, R):
+    """Tens of thousands of keys of about the same weight in one span, values around zero: the error is that of
+    rounding the output to bf16.  (Probabilities of 11 bits, 2^-12 off as a rule, and fp32 sums are less than a third
+    of that each; a tenth is added for both.)"""
+    require_gpu()
+    got, want, _, _, _ = _sink(hq, hkv, D, R, kv, q_len, 0, 7 + D, mean=0.0)
+    rounding = want.bfloat16().double() - want
+    ratio = float((got - want).norm() / rounding.norm())
+    assert ratio <= 1.1, "%.3g times the rounding alone" % ratio

@@ -39,8 +39,8 @@
 // by 2^-34 of that at most.  (With margins of 2^8 for p and 2^7 for the rows' magnitudes above 1, one key 2^22
 // above 8191 others took their weight from them.)
 //
-// Measured: 256 requests of 256..8192 keys (638 MB) 161 us with the joining, 4.0 TB/s; four requests of
-// 60k..131k keys (397 MB) 100 us.  585 instructions a chunk, of which the widening is less than half, at 2.2 a
+// Measured: 256 requests of 256..8192 keys (638 MB) 162 us with the joining, 3.9 TB/s; four requests of
+// 60k..131k keys (397 MB) 101 us.  588 instructions a chunk, of which the widening is less than half, at 2.2 a
 // cycle and SM (of 4): four warps a scheduler, each mostly waiting for its own last result, and the integer pipe
 // (57 % busy) are what is left, not the memory.
 #pragma once

@@ -22,7 +22,7 @@
 //     cores align products by the exponents as they stand, so that small ones lose bits beside a subnormal
 //     factor: scores are off by 2^-17.4 of max |q| s scale, rms, 2^-14.7 at most, where prompts, whose codes are
 //     normal numbers, have 2^-19.2 and 2^-16.3; outputs by up to 2^-13 of the largest p s, 2^-19 as a rule.  Both are
-//     below what the 11 bits of p s cost.);
+//     below what the 11 bits of p s cost while |q| s scale is below 4.);
 //   - a warp works alone: its own ring of chunks (32 keys, two cells) filled by bulk copies, its own
 //     maximum and sums; no block barrier anywhere;
 //   - the matrix instructions take the keys as their 16 rows and up to eight query rows as their 8

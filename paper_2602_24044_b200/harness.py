@@ -197,8 +197,8 @@ class KVCache:
 
     stream: as for the entry points (None is the device's default stream).  Calls on several streams are
     the caller's to order; the cache sees to it that its own buffers are not given back to the allocator
-    while work on any stream it was called on is pending, so these streams outlive it.  Tables that grow
-    move: a captured graph keeps the old ones, so reserve() for the largest batch before a capture."""
+    while work on any stream it was called on is pending.  Tables that grow move: a captured graph keeps
+    the old ones, so reserve() for the largest batch before a capture."""
 
     def __init__(self, num_layers: int, num_pages: int, page_size: int, num_q_heads: int, num_kv_heads: int,
                  head_dim: int, device: int = 0):
@@ -206,7 +206,8 @@ class KVCache:
         self._index = int(device)
         self.shape = (num_layers, num_pages, page_size, num_q_heads, num_kv_heads, head_dim)
         self._width = num_q_heads * head_dim
-        self._streams = set()            # handles of the streams that work on the buffers was queued on
+        self._streams = set()            # handles of torch's streams that work on the buffers was queued on
+        self._others = False             # and was some on a stream that is not torch's, and may be gone by now?
         nbytes = lb.kv_bytes(*self.shape, device=int(device))
         self.buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         off = (-self.buf.data_ptr()) % 256
@@ -222,7 +223,10 @@ class KVCache:
         """The stream's handle, noted as one that may have work on the buffers."""
         handle = 0 if stream is None else lb.stream_handle(stream)
         if handle not in self._streams:
-            self._streams.add(handle)
+            if handle and (type(stream) is int or isinstance(stream, torch.cuda.ExternalStream)):
+                self._others = True
+            else:
+                self._streams.add(handle)
         return handle
 
     def _torch_stream(self, handle: int):
@@ -230,6 +234,9 @@ class KVCache:
 
     def _let_go(self, *tensors) -> None:
         """Before tensors are dropped: their memory may be handed out once the work queued so far is done."""
+        if self._others:
+            torch.cuda.synchronize(self.device)
+            return
         for handle in self._streams:
             stream = self._torch_stream(handle)
             for t in tensors:
@@ -289,7 +296,8 @@ class KVCache:
         words = lb.kv_tables_bytes(self.kv, R, T) // 4
         grow = self.tables is None or self.tables.numel() < words
         if grow:
-            self._let_go(self.tables)
+            if self.tables is not None:
+                self._let_go(self.tables)
             with torch.cuda.stream(stream):
                 self.tables = torch.empty(words, dtype=torch.int32, device=self.device)
             self._tables_bytes = 4 * words
@@ -390,7 +398,7 @@ class KVCache:
             if getattr(self, "kv", 0):
                 self._let_go(self.buf, self.workspace, self.tables)
                 lb.kv_destroy(self.kv)
-        except (TypeError, AttributeError):   # the interpreter is taking its modules down
+        except (TypeError, AttributeError, RuntimeError):   # the interpreter is taking its modules down
             pass
         self.kv = 0
 

@@ -53,17 +53,23 @@ class Stream:
         self.waited += 1
 
 
+class Outside(Stream):
+    """A stream that is not torch's."""
+
+
 class Cuda:
     def __init__(self):
-        self.on = [Stream(0)]
+        self.on, self.waited = [Stream(0)], 0
+
+    def synchronize(self, device=None):
+        self.waited += 1
 
     def current_stream(self, device=None):
         return self.on[-1]
 
     default_stream = staticmethod(lambda device=None: Stream(0))
-    ExternalStream = Stream
+    ExternalStream = Outside
     is_current_stream_capturing = staticmethod(lambda: False)
-    synchronize = staticmethod(lambda device=None: None)
 
     @contextlib.contextmanager
     def stream(self, s):
@@ -124,9 +130,18 @@ def test_tables_that_grow_are_kept_for_the_streams_that_use_them(cache):
     c.attention(0, rows, Tensor(1, 256, dtype=torch.bfloat16), scale=1.0, stream=Stream(9))
     _build(c, 1, None)
     assert c.tables is old and not old.kept
-    _build(c, 500, 11)                           # (a stream's handle as an integer)
+    _build(c, 500, Stream(11))
     assert c.tables is not old and c.tables.made_on == 11
-    assert {7, 9, 0} <= old.kept
+    assert {7, 9, 0} <= old.kept and harness.torch.cuda.waited == 0
+
+
+@pytest.mark.parametrize("stream", [11, Outside(11)])
+def test_streams_that_are_not_torchs_are_waited_for(cache, stream):
+    """They may be gone when the memory is given back, so nothing is asked of them then."""
+    _build(cache, 1, stream)
+    old = cache.tables
+    _build(cache, 500, Stream(7))
+    assert cache.tables is not old and not old.kept and harness.torch.cuda.waited == 1
 
 
 def test_room_made_beforehand_is_ready_for_any_stream(cache):

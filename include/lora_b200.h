@@ -26,6 +26,7 @@
  *   lora_qk_norm_rope     per-head norm and rotation of queries and keys in one pass
  *   lora_kv_append        the same pass, with the keys and values going to the cache as 4-bit rows
  *   lora_kv_attention     attention of a batch (single tokens and prompts together) over the cache
+ *   lora_add_norm         residual addition and norm of rows, to bf16 and to 8 bits with scales
  *
  * Conventions
  *  - plain C ABI; every call returns a lora_status_t; nothing aborts, traps or resets a device;
@@ -564,6 +565,40 @@ lora_status_t lora_kv_attention(lora_kv_t *kv, int32_t layer, const void *q, int
                                 const void *tables, int32_t R, int32_t T,
                                 const int32_t *block_table, int64_t ld_table,
                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* ----------------------------------------------------------------------------------------
+ * Rows between two projections: for each of T rows of `width` values
+ *     s = x + residual                               (s = x where residual is NULL)
+ *     residual_out = bf16(s)                         (where given)
+ *     y_i = s_i * (1 / sqrt(mean(s^2) + eps)) * weight_i        (no weight where it is NULL)
+ *     out = bf16(y)                                  (where given)
+ *     codes_i = e4m3(y_i / scale of i's group)       (where given)
+ * in fp32, every operation rounded by itself, y from s before its rounding to bf16.  The squares of eight
+ * neighbours are added as a tree in fp32, these sums in fp64 (rounded to fp32 once, then times
+ * fl(1 / width)), so the result does not depend on how the work is split.
+ * A group is group neighbouring values: with group = 128, or group = width (one a row), its scale is fp32,
+ *     scale = max|y| * fl(1/448) ,  codes_i = e4m3(y_i * (1 / scale)) ,
+ * a scale below the smallest normal number counting as 0 (every code is 0 then); with group = 32 it is a
+ * power of two kept as the byte e + 127: the smallest 2^e (e in -127 .. 127) with max|y| <= 448 * 2^e, byte
+ * 0 for a group of zeros.  A group with a value that is not finite has codes 0 and the scale NaN (the byte
+ * 255).  group = 0: no codes.
+ * bf16 outputs may be bf16 inputs in place (same leading dimension); otherwise no output overlaps anything.
+ * -------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t device;
+    int32_t width;                             /* a multiple of 8 (and of group), 8 .. 32768 */
+    int32_t group;                             /* 0, 32, 128 or width */
+    float eps;                                 /* >= 0 */
+    const void *x;         int64_t ldx;        /* dev bf16 */
+    const void *weight;                        /* dev bf16 [width] or NULL */
+    const void *residual;  int64_t ldr;        /* dev bf16 or NULL */
+    void *residual_out;    int64_t ldro;       /* dev bf16 or NULL */
+    void *out;             int64_t ldo;        /* dev bf16 or NULL */
+    void *codes;           int64_t ldc;        /* dev e4m3 bytes, 8-byte aligned, ldc a multiple of 8; or NULL */
+    void *scales;          int64_t lds;        /* dev [T, width / group] fp32, bytes with group = 32; or NULL */
+} lora_norm_args_t;
+/* At least one output.  Errors: INVALID_ARG, SHAPE, CUDA. */
+lora_status_t lora_add_norm(const lora_norm_args_t *args, int32_t T, void *stream);
 
 #ifdef __cplusplus
 }

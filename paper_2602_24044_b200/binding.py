@@ -35,6 +35,7 @@ EXPORTS = [
     "lora_kv_bytes", "lora_kv_layer_range", "lora_kv_create", "lora_kv_destroy", "lora_kv_check_status",
     "lora_kv_tables_bytes", "lora_kv_build_tables", "lora_kv_release", "lora_qk_norm_rope",
     "lora_kv_append", "lora_kv_read", "lora_kv_workspace_bytes", "lora_kv_attention",
+    "lora_add_norm",
 ]
 STATIC_SCRATCH_BYTES = 2 * 1024 * 1024
 
@@ -98,6 +99,18 @@ class _QkArgs(ctypes.Structure):
                 ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("q_out", ctypes.c_void_p), ("ldqo", ctypes.c_int64),
                 ("k_out", ctypes.c_void_p), ("ldko", ctypes.c_int64)]
+    max_tokens = 2 ** 31 - 1
+
+
+class _NormArgs(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("weight", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("residual_out", ctypes.c_void_p), ("ldro", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64),
+                ("codes", ctypes.c_void_p), ("ldc", ctypes.c_int64),
+                ("scales", ctypes.c_void_p), ("lds", ctypes.c_int64)]
     max_tokens = 2 ** 31 - 1
 
 
@@ -174,6 +187,7 @@ def _lib():
             "lora_kv_workspace_bytes": [vp, ctypes.POINTER(sz)],
             "lora_kv_attention": [vp, i32, vp, i64, vp, i64, vp, ctypes.c_float, vp, i32, i32, vp, i64,
                                   vp, sz, vp],
+            "lora_add_norm": [ctypes.POINTER(_NormArgs), i32, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -669,6 +683,59 @@ def kv_attention(kv: int, layer: int, q, ldq: int, out, ldo: int, lse, scale: fl
                                       ld_table, p(workspace), nbytes, _stream(stream))
     if status:
         _check(status, "lora_kv_attention")
+
+
+# ------------------------------------------------------------------------------------------
+# rows between two projections
+# ------------------------------------------------------------------------------------------
+def _ld(what: str, t, ld: Optional[int], width: int) -> int:
+    """The leading dimension of rows: as given, or that of a tensor of two dimensions."""
+    if t is None or ld is not None or not hasattr(t, "stride"):
+        return int(ld or 0)
+    if t.dim() != 2 or t.shape[1] < width or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise LoraError(1, "%s (needs rows of %d values, each in a row)" % (what, width))
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+def norm_args(*, x, weight=None, eps: float = 1e-6, residual=None, residual_out=None, out=None, codes=None,
+              scales=None, group: int = 0, width: Optional[int] = None, ldx: Optional[int] = None,
+              ldr: Optional[int] = None, ldro: Optional[int] = None, ldo: Optional[int] = None,
+              ldc: Optional[int] = None, lds: Optional[int] = None, device: int = 0):
+    """The argument block of add_norm (build it once when the same buffers are used again).  width and the
+    leading dimensions default to those of the tensors given; codes: float8_e4m3fn; scales: float32, with
+    group = 32 uint8.  The tensors must stay alive while the block is used; it keeps them, and a call for more
+    rows than they hold is refused."""
+    n = int(x.shape[-1]) if width is None else int(width)
+    groups = n // int(group) if group else 0
+    lds = _ld("scales", scales, lds, groups)
+    rows = [(what, t, _ld(what, t, ld, n)) for what, t, ld in (
+        ("x", x, ldx), ("residual", residual, ldr), ("residual_out", residual_out, ldro), ("out", out, ldo),
+        ("codes", codes, ldc))]
+    (ldx, ldr, ldro, ldo, ldc) = (ld for _, _, ld in rows)
+    a = _NormArgs(int(device), n, int(group), float(eps), _ptr(x), ldx, _ptr(weight), _ptr(residual), ldr,
+                  _ptr(residual_out), ldro, _ptr(out), ldo, _ptr(codes), ldc, _ptr(scales), lds)
+    a._keep = (x, weight, residual, residual_out, out, codes, scales)
+    most = 2 ** 31 - 1
+    for what, t, ld in rows + [("scales", scales, lds)]:
+        need = groups if what == "scales" else n
+        dtype = "float8_e4m3fn" if what == "codes" else "bfloat16" if what != "scales" else \
+            "uint8" if group == 32 else "float32"
+        have = None if t is None else _elements(what, t, dtype, int(device))
+        if have is not None:
+            most = min(most, 0 if have < need else most if ld <= 0 else (have - need) // ld + 1)
+    if weight is not None:
+        _elements("weight", weight, "bfloat16", int(device), n)
+    a.max_tokens = most
+    return a
+
+
+def add_norm(args, T: int, stream=None) -> None:
+    """Residual addition and norm of T rows; `args` from norm_args."""
+    if T > args.max_tokens:
+        _too_many(args, T, "add_norm")
+    status = _lib().lora_add_norm(ctypes.byref(args), T, _stream(stream))
+    if status:
+        _check(status, "lora_add_norm")
 
 
 # ------------------------------------------------------------------------------------------

@@ -25,6 +25,8 @@
  *   lora_kv_build_tables  block tables, positions and slot maps from the requests' lengths
  *   lora_qk_norm_rope     per-head norm and rotation of queries and keys in one pass
  *   lora_kv_append        the same pass, with the keys and values going to the cache as 4-bit rows
+ *   lora_kv_axis_positions, lora_qk_norm_rope_axes, lora_kv_append_axes
+ *                         the same for tokens of images and videos, with positions on several axes
  *   lora_kv_attention     attention of a batch (single tokens and prompts together) over the cache
  *   lora_add_norm         residual addition and norm of rows, to bf16 and to 8 bits with scales
  *
@@ -528,6 +530,45 @@ lora_status_t lora_qk_norm_rope(const lora_qk_args_t *args, int32_t T, void *str
  * row undefined.  The heads must be the cache's.  Errors: INVALID_ARG, SHAPE, SLOT_RANGE (layer), CUDA. */
 lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args,
                              const int32_t *slots, int32_t T, void *stream);
+/*
+ * The same two with positions on several axes (time, height and width of image and video tokens): rotation
+ * pair p of token t turns by the angles of row positions[axis_of_pair[p], t] of cos_sin.  args->positions is
+ * then dev int32 [num_axes, ld_positions]; a token with a position outside 0 .. num_positions - 1 on any axis
+ * is not rotated.  With equal positions on all axes the results are those of the calls above.
+ * Errors: those of the calls above (SHAPE: an axis that is not there, ld_positions < T).
+ */
+#define LORA_ROPE_AXES_MAX 4
+typedef struct {
+    int32_t num_axes;                              /* 1 .. LORA_ROPE_AXES_MAX */
+    int64_t ld_positions;
+    const uint8_t *axis_of_pair;                   /* host [rot_dim / 2], read during the call */
+} lora_rope_axes_t;
+lora_status_t lora_qk_norm_rope_axes(const lora_qk_args_t *args, const lora_rope_axes_t *axes, int32_t T,
+                                     void *stream);
+lora_status_t lora_kv_append_axes(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args,
+                                  const lora_rope_axes_t *axes, const int32_t *slots, int32_t T, void *stream);
+/*
+ * Such positions for the T new tokens of a batch, from its tables (as for lora_kv_attention) and the images
+ * and videos of its requests: request r's spans are spans[span_begin[r]] .. spans[span_begin[r + 1] - 1],
+ * ascending by their first token, each 8 words
+ *     {first, frames, rows, columns, base, step, 0, 0} :
+ * tokens first .. first + frames * rows * columns - 1 of the request are a grid of them, the columns fastest,
+ * and base is the position that its first one has.  For a token at position p of its request, with the last
+ * span that begins at or before it and k = p - first:
+ *     inside the span  (base + k / (rows * columns) * step,  base + k / columns % rows,  base + k % columns)
+ *     behind it        k - frames * rows * columns + base + max((frames - 1) * step + 1, rows, columns)   three times
+ *     no such span     p three times.
+ * A span's base is what its predecessors make it (the position that text there would have had), so it is
+ * known when the request arrives and stays; single tokens of later batches need no other form.  Entries are
+ * not negative (a span without tokens may have zeros); offsets outside the spans are taken to their ends.
+ * spans: dev, 16-byte aligned; span_begin: dev int32 [R + 1].  positions: dev int32 [3, ld_positions]: time,
+ * height, width; 0 behind the last request's tokens.  An exact integer function of its inputs.
+ * Errors: INVALID_ARG, SHAPE, CUDA.
+ */
+lora_status_t lora_kv_axis_positions(lora_kv_t *kv, const void *tables, int32_t R, int32_t T, const int32_t *spans,
+                                     const int32_t *span_begin, int32_t num_spans, int32_t *positions,
+                                     int64_t ld_positions, void *stream);
+
 /* Rows of the cache as bf16, one per slot (zeros for a slot that is -1 or outside the cache): k_out
  * and v_out are [n, num_kv_heads * head_dim] with leading dimensions; either may be NULL. */
 lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, int32_t n,

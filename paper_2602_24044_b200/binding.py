@@ -35,7 +35,7 @@ EXPORTS = [
     "lora_kv_bytes", "lora_kv_layer_range", "lora_kv_create", "lora_kv_destroy", "lora_kv_check_status",
     "lora_kv_tables_bytes", "lora_kv_build_tables", "lora_kv_release", "lora_qk_norm_rope",
     "lora_kv_append", "lora_kv_read", "lora_kv_workspace_bytes", "lora_kv_attention",
-    "lora_add_norm",
+    "lora_add_norm", "lora_qk_norm_rope_axes", "lora_kv_append_axes", "lora_kv_axis_positions",
 ]
 STATIC_SCRATCH_BYTES = 2 * 1024 * 1024
 
@@ -100,6 +100,12 @@ class _QkArgs(ctypes.Structure):
                 ("q_out", ctypes.c_void_p), ("ldqo", ctypes.c_int64),
                 ("k_out", ctypes.c_void_p), ("ldko", ctypes.c_int64)]
     max_tokens = 2 ** 31 - 1
+    axes = None                          # a reference to a _RopeAxes where positions are on several axes
+
+
+class _RopeAxes(ctypes.Structure):
+    _fields_ = [("num_axes", ctypes.c_int32), ("ld_positions", ctypes.c_int64),
+                ("axis_of_pair", ctypes.c_char_p)]
 
 
 class _NormArgs(ctypes.Structure):
@@ -188,6 +194,9 @@ def _lib():
             "lora_kv_attention": [vp, i32, vp, i64, vp, i64, vp, ctypes.c_float, vp, i32, i32, vp, i64,
                                   vp, sz, vp],
             "lora_add_norm": [ctypes.POINTER(_NormArgs), i32, vp],
+            "lora_qk_norm_rope_axes": [ctypes.POINTER(_QkArgs), ctypes.POINTER(_RopeAxes), i32, vp],
+            "lora_kv_append_axes": [vp, i32, ctypes.POINTER(_QkArgs), ctypes.POINTER(_RopeAxes), vp, i32, vp],
+            "lora_kv_axis_positions": [vp, vp, i32, i32, vp, vp, i32, vp, i64, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -594,11 +603,16 @@ def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: 
             ldk: int = 0, v=None, ldv: int = 0, q_weight=None, k_weight=None, eps: float = 0.0,
             cos_sin=None, rot_dim: Optional[int] = None, num_positions: Optional[int] = None,
             interleaved: bool = False, positions=None, q_out=None, ldqo: Optional[int] = None, k_out=None,
-            ldko: Optional[int] = None, device: int = 0):
+            ldko: Optional[int] = None, axis_of_pair: Optional[Sequence[int]] = None, num_axes: Optional[int] = None,
+            ld_positions: Optional[int] = None, device: int = 0):
     """The argument block of qk_norm_rope and kv_append (build it once when the same buffers are used
     again).  rot_dim, num_positions and the outputs' leading dimensions default to those of the tensors
     given.  The tensors must stay alive while the block is used; it keeps them, and a call for more tokens than
-    they hold is refused."""
+    they hold is refused.
+
+    axis_of_pair: which axis turns each of the rot_dim / 2 rotation pairs; positions is then [axes, tokens], and
+    the calls go to lora_qk_norm_rope_axes and lora_kv_append_axes (num_axes and ld_positions: as positions has
+    them)."""
     if cos_sin is not None:
         num_positions = int(cos_sin.shape[0]) if num_positions is None else num_positions
         rot_dim = int(cos_sin.shape[1]) if rot_dim is None else rot_dim
@@ -611,8 +625,24 @@ def qk_args(*, num_q_heads: int, num_kv_heads: int, head_dim: int, q=None, ldq: 
                 int(ldk), _ptr(v), int(ldv), _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin),
                 _ptr(positions), _ptr(q_out), int(ldqo or 0), _ptr(k_out), int(ldko or 0))
     a._keep = (q, k, v, q_weight, k_weight, cos_sin, positions, q_out, k_out)
+    if axis_of_pair is not None:
+        _set_axes(a, axis_of_pair, num_axes, ld_positions, positions)
     a.max_tokens = _max_tokens(a)
     return a
+
+
+def _set_axes(a, axis_of_pair, num_axes, ld_positions, positions) -> None:
+    axis = [int(x) for x in axis_of_pair]
+    if len(axis) != a.rot_dim // 2 or min(axis, default=0) < 0 or max(axis, default=0) > 255:
+        raise LoraError(2, "axis_of_pair (needs the axis of each of the %d rotation pairs)" % (a.rot_dim // 2))
+    if hasattr(positions, "stride"):
+        if positions.dim() != 2 or (positions.stride(1) != 1 and positions.shape[1] > 1):
+            raise LoraError(1, "positions (needs a row of tokens for each axis)")
+        num_axes = int(positions.shape[0]) if num_axes is None else num_axes
+        if ld_positions is None:
+            ld_positions = max(int(positions.stride(0)), int(positions.shape[1]))
+    a._axes = _RopeAxes(int(num_axes or 0), int(ld_positions or 0), bytes(axis))
+    a.axes = ctypes.byref(a._axes)
 
 
 def _max_tokens(a) -> int:
@@ -630,7 +660,11 @@ def _max_tokens(a) -> int:
     if cos_sin is not None:
         _elements("cos_sin", cos_sin, "float32", device, a.num_positions * a.rot_dim)
         n = _elements("positions", positions, "int32", device)
-        if n is not None:
+        if n is not None and a.axes is not None:
+            if positions.shape[0] < a._axes.num_axes:
+                raise LoraError(1, "positions (needs %d axes)" % a._axes.num_axes)
+            most = min(most, a._axes.ld_positions, max(0, n - (a._axes.num_axes - 1) * a._axes.ld_positions))
+        elif n is not None:
             if not positions.is_contiguous():
                 raise LoraError(1, "positions (needs its values in a row)")
             most = min(most, n)
@@ -645,7 +679,10 @@ def qk_norm_rope(args, T: int, stream=None) -> None:
     """Per-head norm and rotation of T tokens' queries and keys; `args` from qk_args."""
     if T > args.max_tokens:
         _too_many(args, T, "qk_norm_rope")
-    status = _lib().lora_qk_norm_rope(ctypes.byref(args), T, _stream(stream))
+    if args.axes is None:
+        status = _lib().lora_qk_norm_rope(ctypes.byref(args), T, _stream(stream))
+    else:
+        status = _lib().lora_qk_norm_rope_axes(ctypes.byref(args), args.axes, T, _stream(stream))
     if status:
         _check(status, "lora_qk_norm_rope")
 
@@ -654,9 +691,21 @@ def kv_append(kv: int, layer: int, args, slots, T: int, stream=None) -> None:
     """qk_norm_rope with the keys and values also going to their slots of the cache as 4-bit rows."""
     if T > args.max_tokens:
         _too_many(args, T, "kv_append")
-    status = _lib().lora_kv_append(kv, layer, ctypes.byref(args), _ptr(slots), T, _stream(stream))
+    if args.axes is None:
+        status = _lib().lora_kv_append(kv, layer, ctypes.byref(args), _ptr(slots), T, _stream(stream))
+    else:
+        status = _lib().lora_kv_append_axes(kv, layer, ctypes.byref(args), args.axes, _ptr(slots), T, _stream(stream))
     if status:
         _check(status, "lora_kv_append")
+
+
+def kv_axis_positions(kv: int, tables, R: int, T: int, spans, span_begin, num_spans: int, positions,
+                      ld_positions: int, stream=None) -> None:
+    """Positions of a batch's tokens on the three axes of images and videos."""
+    status = _lib().lora_kv_axis_positions(kv, _ptr(tables), R, T, _ptr(spans), _ptr(span_begin), num_spans,
+                                           _ptr(positions), ld_positions, _stream(stream))
+    if status:
+        _check(status, "lora_kv_axis_positions")
 
 
 def kv_read(kv: int, layer: int, slots, n: int, k_out, ldk: int, v_out, ldv: int, stream=None) -> None:

@@ -32,6 +32,10 @@ struct RowParams {
     float eps;
     KvView kv;          // with slots
     int32_t *status;    // NULL without a cache
+    // positions on several axes: [num_axes, ld_pos], and two bits a rotation pair that say which turns it
+    int64_t ld_pos;
+    int32_t num_axes;
+    uint32_t axis[4];
 };
 
 // Elements 8 j .. 8 j + 7 and D/2 + 8 j .. of lane j of the head, two to a register pair: the packed
@@ -89,13 +93,17 @@ enum { ROT_NONE = 0, ROT_HALF = 1, ROT_PART = 2, ROT_PAIRS = 3 };
 template <int ROT>
 struct Angles { uint64_t c[4], s[4]; };      // PAIRS: one cosine and one sine a pair, 4 of each run
 
-template <int D, int ROT>
+// Angles in global memory, or (SH) in shared memory.
+template <bool SH, typename V>
+__device__ __forceinline__ V angle(const V *p) { return SH ? *p : __ldg(p); }
+
+template <int D, int ROT, bool SH>
 __device__ __forceinline__ void load_angles(Angles<ROT> &A, const float *row, int rot_dim, int j) {
     if (ROT == ROT_HALF) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float4 c = __ldg(reinterpret_cast<const float4 *>(row + 8 * j + 4 * i));
-            const float4 s = __ldg(reinterpret_cast<const float4 *>(row + D / 2 + 8 * j + 4 * i));
+            const float4 c = angle<SH>(reinterpret_cast<const float4 *>(row + 8 * j + 4 * i));
+            const float4 s = angle<SH>(reinterpret_cast<const float4 *>(row + D / 2 + 8 * j + 4 * i));
             A.c[2 * i] = pack2f(c.x, c.y); A.c[2 * i + 1] = pack2f(c.z, c.w);
             A.s[2 * i] = pack2f(s.x, s.y); A.s[2 * i + 1] = pack2f(s.z, s.w);
         }
@@ -104,8 +112,8 @@ __device__ __forceinline__ void load_angles(Angles<ROT> &A, const float *row, in
         for (int i = 0; i < 4; ++i) {
             const int p = 4 * j + i, q = D / 4 + 4 * j + i;
             const bool in_p = 2 * p < rot_dim, in_q = 2 * q < rot_dim;
-            A.c[i] = pack2f(in_p ? __ldg(row + p) : 1.0f, in_q ? __ldg(row + q) : 1.0f);
-            A.s[i] = pack2f(in_p ? __ldg(row + rot_dim / 2 + p) : 0.0f, in_q ? __ldg(row + rot_dim / 2 + q) : 0.0f);
+            A.c[i] = pack2f(in_p ? angle<SH>(row + p) : 1.0f, in_q ? angle<SH>(row + q) : 1.0f);
+            A.s[i] = pack2f(in_p ? angle<SH>(row + rot_dim / 2 + p) : 0.0f, in_q ? angle<SH>(row + rot_dim / 2 + q) : 0.0f);
         }
     }
 }
@@ -113,7 +121,7 @@ __device__ __forceinline__ void load_angles(Angles<ROT> &A, const float *row, in
 // The rotated run (0: x.a, 1: x.b) of a head whose first rot_dim < D elements are rotated: the partner of
 // element e is e +- rot/2.  rot/2 is a multiple of 8, so the eight elements of a run have their partners
 // in one run of one lane.
-template <int D>
+template <int D, bool SH>
 __device__ __forceinline__ void rotate_part(const Row &x, int run, const float *row, int rot_dim, int j, uint64_t (&o)[4]) {
     const int half = rot_dim / 2, e = run * (D / 2) + 8 * j;
     const bool first = e < half, in = e < rot_dim;
@@ -127,15 +135,15 @@ __device__ __forceinline__ void rotate_part(const Row &x, int run, const float *
         o[i] = mine;
         if (in) {
             const int p = (first ? e : e - half) + 2 * i;
-            const uint64_t c = pack2f(__ldg(row + p), __ldg(row + p + 1));
-            const uint64_t s = pack2f(__ldg(row + half + p), __ldg(row + half + p + 1));
+            const uint64_t c = pack2f(angle<SH>(row + p), angle<SH>(row + p + 1));
+            const uint64_t s = pack2f(angle<SH>(row + half + p), angle<SH>(row + half + p + 1));
             o[i] = sum_of_products(mine, c, other, first ? neg2(s) : s);
         }
     }
 }
 
 // (a, b) -> (a c - b s, b c + a s).  a c - b s is taken as a c + b (-s): the same roundings.
-template <int D, int ROT>
+template <int D, int ROT, bool SH>
 __device__ __forceinline__ void rotate_row(Row &x, const Angles<ROT> &A, const float *row, int rot_dim, int j) {
     if (ROT == ROT_HALF) {
 #pragma unroll
@@ -158,8 +166,8 @@ __device__ __forceinline__ void rotate_row(Row &x, const Angles<ROT> &A, const f
         }
     } else if (ROT == ROT_PART) {
         uint64_t na[4], nb[4];
-        rotate_part<D>(x, 0, row, rot_dim, j, na);
-        rotate_part<D>(x, 1, row, rot_dim, j, nb);
+        rotate_part<D, SH>(x, 0, row, rot_dim, j, na);
+        rotate_part<D, SH>(x, 1, row, rot_dim, j, nb);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x.a[i] = na[i]; x.b[i] = nb[i]; }
     }
@@ -221,8 +229,12 @@ __device__ __forceinline__ void quantise_row(const Row &x, uint32_t &wa, uint32_
 // key and (with a cache) value heads.  All its rows are requested before anything is waited for: position,
 // angles and rows one after the other were 2 us a warp with 2 KB on their way (prefill of 12936 tokens:
 // 94 us a launch, 187 with the cache; bytes alone 41 and 40).
-template <int D, int ROT, bool CACHE, int NP>
+// AXES: the token's positions on several axes each give some of the pairs their angles.  The block puts the
+// token's row of angles together in shared memory while its rows are on their way, and goes on from there as
+// with one position; a pair's axis is looked up once a token and not once a head.
+template <int D, int ROT, bool CACHE, int NP, bool AXES>
 __global__ void __launch_bounds__(256, ROWS_BLOCKS) rows_kernel(const RowParams P) {
+    __shared__ __align__(16) float angle_row[AXES ? D : 4];
     constexpr int LPH = D / 16, HPP = 32 / LPH;     // lanes of a head, heads of a pass
     const int lane = threadIdx.x & 31, j = lane % LPH, g = lane / LPH;
     const int heads = P.hq + P.hk + (CACHE ? P.hk : 0);
@@ -248,10 +260,29 @@ __global__ void __launch_bounds__(256, ROWS_BLOCKS) rows_kernel(const RowParams 
         Angles<ROT> A;
         bool turn = false;
         if (ROT != ROT_NONE) {
-            const int32_t pos = __ldg(P.positions + t);
-            turn = pos >= 0 && pos < P.num_positions;
-            row = P.cos_sin + (int64_t)(turn ? pos : 0) * P.rot_dim;
-            load_angles<D, ROT>(A, row, P.rot_dim, j);
+            if (AXES) {
+                turn = true;
+                for (int a = 0; a < P.num_axes; ++a) {
+                    const int32_t pos = __ldg(P.positions + a * P.ld_pos + t);
+                    turn = turn && pos >= 0 && pos < P.num_positions;
+                }
+                if (h0 == (int)(threadIdx.x >> 5) * (NP * HPP)) {      // every warp has a first pass
+                    const int half = P.rot_dim / 2;
+                    for (int p = threadIdx.x; turn && p < half; p += blockDim.x) {
+                        const int a = P.axis[p / 16] >> (2 * (p % 16)) & 3;
+                        const float *from = P.cos_sin + (int64_t)__ldg(P.positions + a * P.ld_pos + t) * P.rot_dim + p;
+                        angle_row[p] = __ldg(from);
+                        angle_row[half + p] = __ldg(from + half);
+                    }
+                    __syncthreads();
+                }
+                row = angle_row;
+            } else {
+                const int32_t pos = __ldg(P.positions + t);
+                turn = pos >= 0 && pos < P.num_positions;
+                row = P.cos_sin + (int64_t)(turn ? pos : 0) * P.rot_dim;
+            }
+            load_angles<D, ROT, AXES>(A, row, P.rot_dim, j);
             if (!turn && P.status && h0 == 0 && lane == 0) atomicAdd(&P.status[STATUS_INVALID_TOKENS], 1);
         }
         if (CACHE) {
@@ -289,7 +320,7 @@ __global__ void __launch_bounds__(256, ROWS_BLOCKS) rows_kernel(const RowParams 
             }
             if (ROT != ROT_NONE && turn && __any_sync(0xffffffffu, kind < 2)) {   // `turn` is the token's, the same in the whole warp
                 const Row x = y;
-                rotate_row<D, ROT>(y, A, row, P.rot_dim, j);
+                rotate_row<D, ROT, AXES>(y, A, row, P.rot_dim, j);
                 if (kind == 2) y = x;
             }
             if (live && kind == 0) {
@@ -415,15 +446,34 @@ static lora_status_t fill_rows(const lora_qk_args_t *a, int32_t T, bool cache, R
     P->eps = a->eps;
     P->status = nullptr;
     memset(&P->kv, 0, sizeof(P->kv));
+    P->ld_pos = 0;
+    P->num_axes = 0;
+    memset(P->axis, 0, sizeof(P->axis));
+    return LORA_OK;
+}
+
+static lora_status_t fill_axes(const lora_qk_args_t *a, const lora_rope_axes_t *axes, int32_t T, RowParams *P) {
+    if (!a->cos_sin || !axes->axis_of_pair) return LORA_ERR_INVALID_ARG;
+    if (axes->num_axes < 1 || axes->num_axes > LORA_ROPE_AXES_MAX || axes->ld_positions < T) return LORA_ERR_SHAPE;
+    P->ld_pos = axes->ld_positions;
+    P->num_axes = axes->num_axes;
+    for (int p = 0; p < a->rot_dim / 2; ++p) {
+        if (axes->axis_of_pair[p] >= axes->num_axes) return LORA_ERR_SHAPE;
+        P->axis[p / 16] |= (uint32_t)axes->axis_of_pair[p] << (2 * (p % 16));
+    }
     return LORA_OK;
 }
 
 template <int D, bool CACHE, int NP>
 static void launch_rows(const RowParams &P, int rot, int threads, cudaStream_t s) {
-    if (rot == ROT_NONE) rows_kernel<D, ROT_NONE, CACHE, NP><<<P.T, threads, 0, s>>>(P);
-    else if (rot == ROT_HALF) rows_kernel<D, ROT_HALF, CACHE, NP><<<P.T, threads, 0, s>>>(P);
-    else if (rot == ROT_PART) rows_kernel<D, ROT_PART, CACHE, NP><<<P.T, threads, 0, s>>>(P);
-    else rows_kernel<D, ROT_PAIRS, CACHE, NP><<<P.T, threads, 0, s>>>(P);
+    if (P.num_axes) {
+        if (rot == ROT_HALF) rows_kernel<D, ROT_HALF, CACHE, NP, true><<<P.T, threads, 0, s>>>(P);
+        else if (rot == ROT_PART) rows_kernel<D, ROT_PART, CACHE, NP, true><<<P.T, threads, 0, s>>>(P);
+        else rows_kernel<D, ROT_PAIRS, CACHE, NP, true><<<P.T, threads, 0, s>>>(P);
+    } else if (rot == ROT_NONE) rows_kernel<D, ROT_NONE, CACHE, NP, false><<<P.T, threads, 0, s>>>(P);
+    else if (rot == ROT_HALF) rows_kernel<D, ROT_HALF, CACHE, NP, false><<<P.T, threads, 0, s>>>(P);
+    else if (rot == ROT_PART) rows_kernel<D, ROT_PART, CACHE, NP, false><<<P.T, threads, 0, s>>>(P);
+    else rows_kernel<D, ROT_PAIRS, CACHE, NP, false><<<P.T, threads, 0, s>>>(P);
 }
 template <int D, bool CACHE>
 static lora_status_t launch_rows_for(const RowParams &P, int rot, cudaStream_t s) {
@@ -452,17 +502,18 @@ using namespace lora;
 
 extern "C" {
 
-lora_status_t lora_qk_norm_rope(const lora_qk_args_t *args, int32_t T, void *stream) {
+static lora_status_t norm_rope(const lora_qk_args_t *args, const lora_rope_axes_t *axes, int32_t T, void *stream) {
     RowParams P;
     lora_status_t s = fill_rows(args, T, false, &P);
     if (s != LORA_OK || T == 0) return s;
+    if (axes && (s = fill_axes(args, axes, T, &P)) != LORA_OK) return s;
     DeviceGuard g(args->device);
     if (!g.ok) return cuda_fail(cudaErrorInvalidDevice);
     return run_rows(args, P, false, (cudaStream_t)stream);
 }
 
-lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args, const int32_t *slots,
-                             int32_t T, void *stream) {
+static lora_status_t append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args, const lora_rope_axes_t *axes,
+                            const int32_t *slots, int32_t T, void *stream) {
     if (!kv || !args) return LORA_ERR_INVALID_ARG;
     if (layer < 0 || layer >= kv->num_layers) return LORA_ERR_SLOT_RANGE;
     if (args->head_dim != kv->d || args->num_kv_heads != kv->hkv) return LORA_ERR_SHAPE;
@@ -470,12 +521,33 @@ lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t 
     RowParams P;
     lora_status_t s = fill_rows(args, T, true, &P);
     if (s != LORA_OK || T == 0) return s;
+    if (axes && (s = fill_axes(args, axes, T, &P)) != LORA_OK) return s;
     if (!slots) return LORA_ERR_INVALID_ARG;
     P.slots = slots;
     P.kv = kv->view(layer);
     P.status = kv->status_dev;
     DeviceGuard g(kv->device);
     return run_rows(args, P, true, (cudaStream_t)stream);
+}
+
+lora_status_t lora_qk_norm_rope(const lora_qk_args_t *args, int32_t T, void *stream) {
+    return norm_rope(args, nullptr, T, stream);
+}
+
+lora_status_t lora_qk_norm_rope_axes(const lora_qk_args_t *args, const lora_rope_axes_t *axes, int32_t T, void *stream) {
+    if (!axes) return LORA_ERR_INVALID_ARG;
+    return norm_rope(args, axes, T, stream);
+}
+
+lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args, const int32_t *slots,
+                             int32_t T, void *stream) {
+    return append(kv, layer, args, nullptr, slots, T, stream);
+}
+
+lora_status_t lora_kv_append_axes(lora_kv_t *kv, int32_t layer, const lora_qk_args_t *args,
+                                  const lora_rope_axes_t *axes, const int32_t *slots, int32_t T, void *stream) {
+    if (!axes) return LORA_ERR_INVALID_ARG;
+    return append(kv, layer, args, axes, slots, T, stream);
 }
 
 lora_status_t lora_kv_read(lora_kv_t *kv, int32_t layer, const int32_t *slots, int32_t n, void *k_out, int64_t ldk,

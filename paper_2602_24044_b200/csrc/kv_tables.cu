@@ -477,6 +477,46 @@ __global__ void __launch_bounds__(TB_THREADS) release_kernel(const int32_t *requ
     if (tid == 0) *free_count = (int32_t)min((int64_t)have + (n ? count[n - 1] : 0), (int64_t)num_pages);
 }
 
+// Positions of the batch's tokens on three axes.  A thread a token: its request is looked up in the starts,
+// which every block brings into shared memory (three loads in a row instead of twelve), then the last of the
+// request's spans that begins at or before it.  What bounds it is that chain of dependent loads.
+constexpr int AP_THREADS = 256;
+__global__ void __launch_bounds__(AP_THREADS)
+axis_positions_kernel(const int32_t *start_dev, const int32_t *position, int32_t R, int32_t T, const int32_t *spans,
+                      const int32_t *span_begin, int32_t num_spans, int32_t *out, int64_t ld) {
+    __shared__ int32_t start[KV_MAX_REQUESTS + 1];
+    const int64_t t = (int64_t)blockIdx.x * AP_THREADS + threadIdx.x;
+    const int64_t p = t < T ? __ldg(position + t) : 0;
+    for (int i = threadIdx.x; i <= R; i += AP_THREADS) start[i] = __ldg(start_dev + i);
+    __syncthreads();
+    if (t >= T) return;
+    int64_t a0 = p, a1 = p, a2 = p;
+    const int r = upper_bound(start + 1, R, (int32_t)t);
+    if (r < R) {
+        const int lo = min(max(__ldg(span_begin + r), 0), num_spans), hi = min(__ldg(span_begin + r + 1), num_spans);
+        int i = lo, j = hi;                      // first span that begins behind the token
+        while (i < j) {
+            const int m = (i + j) >> 1;
+            if (__ldg(spans + (int64_t)m * 8) > p) j = m; else i = m + 1;
+        }
+        if (i > lo) {
+            const int4 *s = reinterpret_cast<const int4 *>(spans + (int64_t)(i - 1) * 8);
+            const int4 u = __ldg(s), v = __ldg(s + 1);               // first, frames, rows, columns; base, step
+            const int64_t k = p - u.x, hw = (int64_t)u.z * u.w, size = hw * u.y;
+            if (k < size) {
+                a0 = v.x + k / hw * v.y;
+                a1 = v.x + k / u.w % u.z;
+                a2 = v.x + k % u.w;
+            } else {
+                a0 = a1 = a2 = k - size + v.x + max(max(((int64_t)u.y - 1) * v.y + 1, (int64_t)u.z), (int64_t)u.w);
+            }
+        }
+    }
+    out[t] = (int32_t)a0;
+    out[ld + t] = (int32_t)a1;
+    out[2 * ld + t] = (int32_t)a2;
+}
+
 }  // namespace lora
 
 using namespace lora;
@@ -554,6 +594,24 @@ lora_status_t lora_kv_build_tables(lora_kv_t *kv, const int32_t *kv_len, const i
     cfg.numAttrs = 1;
     LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, build_tables_kernel, P));
     kv->remember(tables, R, T, max_q, window);
+    return count_launch();
+}
+
+lora_status_t lora_kv_axis_positions(lora_kv_t *kv, const void *tables, int32_t R, int32_t T, const int32_t *spans,
+                                     const int32_t *span_begin, int32_t num_spans, int32_t *positions,
+                                     int64_t ld_positions, void *stream) {
+    if (!kv) return LORA_ERR_INVALID_ARG;
+    if (R < 0 || T < 0 || num_spans < 0) return LORA_ERR_SHAPE;
+    if (T == 0) return LORA_OK;
+    if (ld_positions < T) return LORA_ERR_SHAPE;
+    if (!tables || !positions || (R > 0 && !span_begin) || (num_spans > 0 && !spans)) return LORA_ERR_INVALID_ARG;
+    if ((uintptr_t)spans & 15) return LORA_ERR_INVALID_ARG;
+    if (!kv->find(tables, R, T)) return LORA_ERR_INVALID_ARG;
+    const KvTables L = kv_tables(R, T, kv->group, kv->dec_walkers(), kv->pr_walkers());
+    const int32_t *words = (const int32_t *)tables;
+    DeviceGuard g(kv->device);
+    axis_positions_kernel<<<(unsigned)(((int64_t)T + AP_THREADS - 1) / AP_THREADS), AP_THREADS, 0, (cudaStream_t)stream>>>(
+        words + L.start, words + L.position, R, T, spans, span_begin, num_spans, positions, ld_positions);
     return count_launch();
 }
 

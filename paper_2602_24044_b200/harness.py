@@ -188,6 +188,26 @@ class Session:
         self.close()
 
 
+def media_spans(requests: Sequence[Sequence]):
+    """The images and videos of requests as kv_axis_positions takes them: for each request a list of (first
+    token, frames, rows, columns[, step of a frame]), ascending by their first tokens.  Returns int32 arrays
+    (spans [n, 8], span_begin [requests + 1])."""
+    spans, begin = [], [0]
+    for r, mine in enumerate(requests):
+        end = at = 0                      # tokens so far, and the position of the next one
+        for first, frames, rows, columns, *step in mine:
+            step = step[0] if step else 1
+            if first < end or min(frames, rows, columns) < 1 or step < 0:
+                raise ValueError("media_spans: request %d: a span at token %d overlaps the one before it, or is empty"
+                                 % (r, first))
+            at += first - end
+            spans.append((first, frames, rows, columns, at, step, 0, 0))
+            end = first + frames * rows * columns
+            at += max((frames - 1) * step + 1, rows, columns)
+        begin.append(len(spans))
+    return np.array(spans, dtype=np.int32).reshape(-1, 8), np.array(begin, dtype=np.int32)
+
+
 class KVCache:
     """A paged 4-bit key/value cache on one GPU with the table buffer and workspace of its calls.
 
@@ -352,6 +372,23 @@ class KVCache:
         self._ints("free_count", free_count, 1)
         lb.kv_release(self.kv, requests, n, R, kv_len, block_table, self._table(block_table, R), free_pages,
                       free_count, stream=self._on(stream))
+
+    def axis_positions(self, spans, span_begin, out, stream=None) -> None:
+        """Positions on three axes of the tables' tokens; spans, span_begin: as media_spans returns them, on the
+        device; out: int32 [3, tokens]."""
+        R, T = self.R, self.T
+        if self.block_table is None:
+            raise ValueError("axis_positions: no tables have been built")
+        self._ints("spans", spans, 0)
+        self._ints("span_begin", span_begin, R + 1)
+        shape = out.shape
+        if spans.dim() != 2 or (spans.shape[1] != 8 and spans.shape[0]):
+            raise ValueError("spans: needs rows of 8 words")
+        if (out.dtype is not torch.int32 or out.get_device() != self._index or len(shape) != 2 or shape[0] < 3 or
+                shape[1] < T or (shape[1] > 1 and out.stride(1) != 1)):
+            raise ValueError("out: needs int32 [3, %d] on %s" % (T, self.device))
+        lb.kv_axis_positions(self.kv, self.tables, R, T, spans, span_begin, spans.shape[0], out, out.stride(0),
+                             stream=self._on(stream))
 
     def append(self, layer: int, args, slots=None, T: Optional[int] = None, stream=None) -> None:
         """args: binding.qk_args(...); slots: default those of the tables."""

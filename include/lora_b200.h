@@ -29,6 +29,7 @@
  *                         the same for tokens of images and videos, with positions on several axes
  *   lora_kv_attention     attention of a batch (single tokens and prompts together) over the cache
  *   lora_add_norm         residual addition and norm of rows, to bf16 and to 8 bits with scales
+ *   lora_sample           the next tokens from rows of logits
  *
  * Conventions
  *  - plain C ABI; every call returns a lora_status_t; nothing aborts, traps or resets a device;
@@ -640,6 +641,42 @@ typedef struct {
 } lora_norm_args_t;
 /* At least one output.  Errors: INVALID_ARG, SHAPE, CUDA. */
 lora_status_t lora_add_norm(const lora_norm_args_t *args, int32_t T, void *stream);
+
+/* ----------------------------------------------------------------------------------------
+ * The next token of each of R requests from its row of `vocab` logits, with parameters of its own.
+ * With m the row's largest logit, w_i = exp((l_i - m) / temperature), and the tokens in order of
+ * their logits, the larger first and of equal ones the lower index first:
+ *   top_k   only the first top_k tokens are kept                        (0 or less, or >= vocab: all)
+ *   min_p   of these the ones with w_i >= min(min_p, 1)                 (0 or less: all)
+ *   top_p   of these the shortest run from the front whose weights reach top_p times their sum, at least
+ *           one                                                        (1 or more: all)
+ *   token   the lowest index at which the sum of the kept weights up to it exceeds uniform times the sum of
+ *           all kept weights (uniform below 0 counts as 0; from 1 on, the last kept token)
+ *   logprob log(w_token / sum of the kept weights)
+ * A temperature of 0 (or less, or NaN) takes the largest logit, of equal ones the lowest index (logprob 0).
+ * Parameters that are NaN count as absent, a uniform that is NaN as 0.  A logit of -inf is never taken, and
+ * nor is one whose weight is below 2^-46; logits of +inf share the weight.  A row with a NaN, or of -inf
+ * alone, gives the token -1 and the logprob NaN.
+ * Weights are good to 1e-11 of themselves, sums are held in 64 bits.  The result does not depend on how the
+ * rows are split but for borders that are closer than that.
+ * Random numbers are the caller's: the same uniform gives the same token.
+ * -------------------------------------------------------------------------------------- */
+enum { LORA_LOGITS_BF16 = 0, LORA_LOGITS_FP32 = 1 };
+typedef struct {
+    int32_t device;
+    int32_t vocab;                     /* 1 .. 2^20 */
+    int32_t logits_type;               /* LORA_LOGITS_BF16 or LORA_LOGITS_FP32 */
+    const void *logits; int64_t ld;    /* dev [R, vocab], ld >= vocab in elements (rows on 16-byte boundaries
+                                          are read fastest) */
+    const float *temperature;          /* dev [R] */
+    const int32_t *top_k;              /* dev [R] or NULL */
+    const float *top_p, *min_p;        /* dev [R] or NULL */
+    const float *uniform;              /* dev [R], in [0, 1) */
+    int32_t *token;                    /* dev [R] */
+    float *logprob;                    /* dev [R] or NULL */
+} lora_sample_args_t;
+/* No output may overlap anything.  R <= 2^24.  Errors: INVALID_ARG, SHAPE, CUDA. */
+lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, void *stream);
 
 #ifdef __cplusplus
 }

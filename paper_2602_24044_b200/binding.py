@@ -36,6 +36,7 @@ EXPORTS = [
     "lora_kv_tables_bytes", "lora_kv_build_tables", "lora_kv_release", "lora_qk_norm_rope",
     "lora_kv_append", "lora_kv_read", "lora_kv_workspace_bytes", "lora_kv_attention",
     "lora_add_norm", "lora_qk_norm_rope_axes", "lora_kv_append_axes", "lora_kv_axis_positions",
+    "lora_sample",
 ]
 STATIC_SCRATCH_BYTES = 2 * 1024 * 1024
 
@@ -120,6 +121,15 @@ class _NormArgs(ctypes.Structure):
     max_tokens = 2 ** 31 - 1
 
 
+class _SampleArgs(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("vocab", ctypes.c_int32), ("logits_type", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("ld", ctypes.c_int64),
+                ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("uniform", ctypes.c_void_p),
+                ("token", ctypes.c_void_p), ("logprob", ctypes.c_void_p)]
+    max_tokens = 2 ** 31 - 1
+
+
 _handle = None
 
 
@@ -193,6 +203,7 @@ def _lib():
             "lora_kv_workspace_bytes": [vp, ctypes.POINTER(sz)],
             "lora_kv_attention": [vp, i32, vp, i64, vp, i64, vp, ctypes.c_float, vp, i32, i32, vp, i64,
                                   vp, sz, vp],
+            "lora_sample": [ctypes.POINTER(_SampleArgs), i32, vp],
             "lora_add_norm": [ctypes.POINTER(_NormArgs), i32, vp],
             "lora_qk_norm_rope_axes": [ctypes.POINTER(_QkArgs), ctypes.POINTER(_RopeAxes), i32, vp],
             "lora_kv_append_axes": [vp, i32, ctypes.POINTER(_QkArgs), ctypes.POINTER(_RopeAxes), vp, i32, vp],
@@ -785,6 +796,52 @@ def add_norm(args, T: int, stream=None) -> None:
     status = _lib().lora_add_norm(ctypes.byref(args), T, _stream(stream))
     if status:
         _check(status, "lora_add_norm")
+
+
+# ------------------------------------------------------------------------------------------
+# the next tokens
+# ------------------------------------------------------------------------------------------
+LOGITS_BF16, LOGITS_FP32 = 0, 1
+
+
+def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None, top_p=None, min_p=None,
+                vocab: Optional[int] = None, ld: Optional[int] = None, logits_type: Optional[int] = None, device: int = 0):
+    """The argument block of sample (build it once when the same buffers are used again).  logits: bf16 or fp32
+    rows; vocab, their type and leading dimension default to the tensor's.  The others hold one entry a row.  The
+    tensors must stay alive while the block is used; it keeps them, and a call for more rows than they hold is
+    refused."""
+    V = int(logits.shape[-1]) if vocab is None else int(vocab)
+    ld = _ld("logits", logits, ld, V)
+    kind = "bfloat16" if logits_type == LOGITS_BF16 else "float32"
+    if logits_type is None:
+        kind = "bfloat16" if str(getattr(logits, "dtype", "")) == "torch.bfloat16" else "float32"
+        logits_type = LOGITS_BF16 if kind == "bfloat16" else LOGITS_FP32
+    a = _SampleArgs(int(device), V, int(logits_type), _ptr(logits), ld, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                    _ptr(min_p), _ptr(uniform), _ptr(token), _ptr(logprob))
+    a._keep = (logits, temperature, top_k, top_p, min_p, uniform, token, logprob)
+    most = 2 ** 31 - 1
+    have = None if logits is None else _elements("logits", logits, kind, int(device))
+    if have is not None:
+        most = 0 if have < V else most if ld <= 0 else (have - V) // ld + 1
+    for what, t, dtype in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"), ("top_p", top_p, "float32"),
+                           ("min_p", min_p, "float32"), ("uniform", uniform, "float32"), ("token", token, "int32"),
+                           ("logprob", logprob, "float32")):
+        have = None if t is None else _elements(what, t, dtype, int(device))
+        if have is not None:
+            if not t.is_contiguous():
+                raise LoraError(1, "%s (needs its values in a row)" % what)
+            most = min(most, have)
+    a.max_tokens = most
+    return a
+
+
+def sample(args, R: int, stream=None) -> None:
+    """The next tokens of R requests; `args` from sample_args."""
+    if R > args.max_tokens:
+        _too_many(args, R, "sample")
+    status = _lib().lora_sample(ctypes.byref(args), R, _stream(stream))
+    if status:
+        _check(status, "lora_sample")
 
 
 # ------------------------------------------------------------------------------------------

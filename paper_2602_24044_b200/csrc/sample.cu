@@ -1,0 +1,957 @@
+// The next token of every request from its row of logits: temperature, top-k, min-p, top-p, a given number.
+//
+// w_i = exp((l_i - m) / tau), m the row's largest; tokens are ordered by l, ties by the lower index; kept are
+// the first k, of these the ones with w_i >= min_p, of these the shortest run from the front whose weight
+// reaches top_p of theirs; the token is the lowest index at which the kept weights so far exceed u times their
+// sum.  A row is read once: the time should be the logits' way from memory.
+//
+// What is kept hangs on borders (a sum of thousands of weights against p times another), and a token on where
+// u falls among as many: weights are good to 1e-11 and sums are held in fp64 or in 64-bit whole numbers.
+// 2^t is a table of 64 powers and a polynomial of degree 3 in fp64 (7 fp64 instructions a weight, which issue
+// at half the rate of fp32's; a polynomial alone would be 12).  The table is there once for each pair of
+// banks, so that lanes with different entries do not wait for one another.
+//
+// A cluster of blocks takes a row, in steps of 2 KB a warp.  Rows with a filter collect candidates: whatever is
+// not below a threshold that only rises (the K-th largest so far, or min_p of the largest so far) goes to a
+// list in shared memory.  A list that is full is cut to the best K or a few more: K = top_k, or KEEP_P for
+// top_p alone, where the sum of all weights is taken on the way.  The first block then sorts what is left.
+// Rows without a filter only sum, a step's sum by itself: the token's step is looked up among the sums and
+// read again.  Whatever does not fit (top_k over KEEP_K, a list of ties, a nucleus of thousands) goes to a
+// general path that finds the cut digit by digit, reading its row once a digit from the second-level cache.
+#include <cooperative_groups.h>
+
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "kv_common.cuh"
+
+namespace lora {
+
+namespace cg = cooperative_groups;
+
+constexpr int SP_THREADS = 256, SP_WARPS = SP_THREADS / 32;
+constexpr int SP_CLUSTER = 8;                 // blocks of a row at most
+constexpr int SP_LIST = 2048;                 // entries of a list
+constexpr int KEEP_K = 256, KEEP_P = 256;
+constexpr int SP_MAX_V = 1 << 20;             // steps' sums of a block's row fit its list
+constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
+constexpr double SP_ONE = 70368744177664.0;   // 2^46: the largest weight as a whole number
+constexpr double SP_MAGIC = 105553116266496.0;   // 1.5 * 2^46: sums with it are rounded to 1/64
+
+struct SampleParams {
+    const void *logits;
+    int64_t ld;
+    int32_t V, segs, steps;      // steps of 2 KB in a row, and of one warp
+    bool aligned;
+    const float *temperature, *top_p, *min_p, *uniform;
+    const int32_t *top_k;
+    int32_t *token;
+    float *logprob;
+};
+
+struct SampleShared {
+    double table[64 * 16];       // 2^(i / 64), once for each pair of banks
+    uint64_t list[SP_LIST];      // candidates; sums of steps; weights
+    uint64_t merge[SP_LIST];     // (first block) the cluster's candidates; sums of all steps
+    uint64_t digit_weight[2][256];
+    uint32_t digit_count[2][256];
+    uint64_t scan_u[SP_WARPS];
+    double scan_d[SP_WARPS];
+    int32_t n, failed_here;
+    uint32_t threshold, best;    // what candidates are not below, and the block's largest so far, as keys
+    uint32_t key_min, key_max;
+    int32_t pick_bin, pick_above, pick_kept;
+    uint64_t pick_count, pick_weight, pick_here;
+    int32_t found;
+    double rest;
+    // written by the blocks of the cluster to the first one
+    uint32_t top[SP_CLUSTER];
+    int32_t bad[SP_CLUSTER], failed[SP_CLUSTER];
+    double sum[SP_CLUSTER], base[SP_CLUSTER];
+    int32_t merged;
+    // of the first block: what turns the blocks' sums into sums against the largest value
+    double scale[SP_CLUSTER];
+    // written by the first block to all
+    int32_t general;
+    float row_max;
+};
+
+// what a row asks for
+struct RowPlan {
+    double c;                    // log2(e) / temperature
+    double low;                  // smallest exponent that min_p keeps, -inf: all
+    float drop;                  // how far below the largest value that is, and a little more
+    float u;
+    double p;
+    int32_t k;                   // 0: all
+    int32_t keep;                // entries that a list is cut to; 0: not by rank
+    bool greedy, by_p, by_min, list, sums, segments;
+};
+
+// ---- values, keys -----------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t key_of(float l) {          // larger value, larger key; -0 and 0 alike
+    const uint32_t u = __float_as_uint(__fadd_rn(l, 0.0f));
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+__device__ __forceinline__ uint64_t entry_of(float l, int32_t i) { return (uint64_t)key_of(l) << 32 | (uint32_t)~i; }
+__device__ __forceinline__ int32_t index_of(uint64_t entry) { return (int32_t)~(uint32_t)entry; }
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// 2^(x c - b) with magic = SP_MAGIC - b (b a multiple of 1/64): the nearest 1/64 from a rounded sum, the rest by
+// the exponential series to the third power.  Its fourth term is a4 r^4 with |r| <= h = 1/128; the square's
+// coefficient has 2 (sqrt 2 - 1) a4 h^2 more, which leaves 6.1e-12 of it at most (not 3.6e-11).
+__device__ __forceinline__ double power2(double x, double c, double magic, const double *table) {
+    const double t = fma(x, c, magic);
+    const int32_t k = __double2loint(t);
+    const double r = fma(x, c, -(t - magic));
+    const double p = fma(r, fma(r, fma(r, 0.05550410866482158, 0.24022699328228442), 0.6931471805599453), 1.0);
+    const double e = table[(k & 63) * 16 + (threadIdx.x & 15)];
+    return p * __hiloint2double(__double2hiint(e) + ((k & ~63) << 14), __double2loint(e));
+}
+// the weight of a value against the row's largest
+__device__ __forceinline__ double exponent_of(float l, float m, double c) {
+    return l == m ? 0.0 : ((double)l - (double)m) * c;
+}
+__device__ __forceinline__ double weight_of(double t, const double *table) {
+    return t >= SP_LOW ? power2(t, 1.0, SP_MAGIC, table) : 0.0;        // (not a number: nothing)
+}
+__device__ __forceinline__ uint64_t whole(double w) { return (uint64_t)(w * SP_ONE); }
+
+__device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
+
+// ---- a step: 64 bytes a lane ------------------------------------------------------------------
+template <bool BF16>
+struct Step {
+    static constexpr int VEC = BF16 ? 8 : 4, N = 4 * VEC, SEG = 32 * N;     // values of a vector, a lane, a warp
+    uint32_t w[16];
+
+    __device__ __forceinline__ void load(const SampleParams &P, const char *row, int32_t seg) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int32_t at = seg * SEG + (v * 32 + lane) * VEC;
+            uint32_t x[4];
+            if (P.aligned && at + VEC <= P.V) {
+                const uint4 q = __ldg(reinterpret_cast<const uint4 *>(row + (int64_t)at * (BF16 ? 2 : 4)));
+                x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (BF16) {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(row) + at + 2 * j;
+                        x[j] = (at + 2 * j < P.V ? (uint32_t)__ldg(h) : 0xff80u) |
+                               (at + 2 * j + 1 < P.V ? (uint32_t)__ldg(h + 1) : 0xff80u) << 16;
+                    } else {
+                        x[j] = at + j < P.V ? __ldg(reinterpret_cast<const uint32_t *>(row) + at + j) : 0xff800000u;
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * v + j] = x[j];
+        }
+    }
+    __device__ __forceinline__ void nothing() {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = BF16 ? 0xff80ff80u : 0xff800000u;
+    }
+    __device__ __forceinline__ float value(int e) const {
+        if (BF16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        return __uint_as_float(w[e]);
+    }
+    static __device__ __forceinline__ int32_t index(int32_t seg, int e) {
+        return seg * SEG + (e / VEC * 32 + (int)(threadIdx.x & 31)) * VEC + e % VEC;
+    }
+};
+
+// ---- block-wide sums --------------------------------------------------------------------------
+// What lies before this thread, and (total) all of it.  Every thread of the block calls it.
+template <typename I>
+__device__ __forceinline__ I block_before(I v, I *warp_sum, I &total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    I incl = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const I o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    I before = incl - v;
+    if (std::is_floating_point<I>::value) {                   // not by a difference
+        before = __shfl_up_sync(0xffffffffu, incl, 1);
+        if (lane == 0) before = 0;
+    }
+    total = 0;
+    I ahead = 0;
+#pragma unroll
+    for (int i = 0; i < SP_WARPS; ++i) {
+        if (i == warp) ahead = total;
+        total += warp_sum[i];
+    }
+    return ahead + before;
+}
+
+// n entries (a power of two of them, at most SP_LIST) in descending or ascending order.
+template <bool DOWN>
+__device__ void sort_entries(uint64_t *a, int n) {
+    for (int k = 2; k <= n; k <<= 1)
+        for (int j = k >> 1; j; j >>= 1) {
+            for (int i = threadIdx.x; i < n / 2; i += SP_THREADS) {
+                const int x = 2 * i - (i & (j - 1)), y = x + j;
+                const uint64_t p = a[x], q = a[y];
+                if (((p < q) == DOWN) == ((x & k) == 0) && p != q) {
+                    a[x] = q;
+                    a[y] = p;
+                }
+            }
+            __syncthreads();
+        }
+}
+
+// ---- the list ---------------------------------------------------------------------------------
+__device__ __forceinline__ bool put(SampleShared &s, uint64_t entry) {
+    const int at = atomicAdd(&s.n, 1);
+    if (at < SP_LIST) s.list[at] = entry;
+    return at < SP_LIST;
+}
+
+// Leaves the entries whose keys are not below `cut`; returns how many there are.
+__device__ int leave_from(SampleShared &s, uint64_t *a, int n, uint32_t cut) {
+    const int tid = threadIdx.x;
+    uint64_t mine[SP_LIST / SP_THREADS];
+#pragma unroll
+    for (int j = 0; j < SP_LIST / SP_THREADS; ++j) mine[j] = tid + j * SP_THREADS < n ? a[tid + j * SP_THREADS] : 0;
+    __syncthreads();
+    if (tid == 0) s.found = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < SP_LIST / SP_THREADS; ++j)
+        if (mine[j] && (uint32_t)(mine[j] >> 32) >= cut) a[atomicAdd(&s.found, 1)] = mine[j];
+    __syncthreads();
+    const int left = s.found;
+    __syncthreads();
+    return left;
+}
+
+// Leaves at least `keep` of the n entries of `a`, the best ones, and as a rule no more than `most`; returns their
+// number and the smallest key among them (n < keep: all of them, and 0).  All threads of the block call it.
+// The K-th is looked for in 256 equal parts of the values' range, then of the part it is in, and so on: any rule
+// that never puts a larger value behind a smaller one is right, so roundings, infinities and ties only make the
+// parts uneven.
+__device__ int cut_list(SampleShared &s, uint64_t *a, int n, int keep, int most, uint32_t &cut) {
+    cut = 0;
+    if (n < keep) return n;
+    const int tid = threadIdx.x, lane = tid & 31;
+    uint32_t lo = 0, hi = 0xffffffffu;
+    int above = 0, kept = n;
+    uint32_t *bins = s.digit_count[0];
+    for (int round = 0; round < 8; ++round) {
+        __syncthreads();
+        if (tid == 0) { s.key_min = 0xffffffffu; s.key_max = 0; }
+        bins[tid] = 0;
+        __syncthreads();
+        uint32_t mn = 0xffffffffu, mx = 0;
+        for (int i = tid; i < n; i += SP_THREADS) {
+            const uint32_t k = (uint32_t)(a[i] >> 32);
+            if (k >= lo && k <= hi) { mn = min(mn, k); mx = max(mx, k); }
+        }
+        mn = __reduce_min_sync(0xffffffffu, mn);
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        if (lane == 0) { atomicMin(&s.key_min, mn); atomicMax(&s.key_max, mx); }
+        __syncthreads();
+        const float top = 0.5f * fminf(value_of(s.key_max), FLT_MAX), bottom = 0.5f * fmaxf(value_of(s.key_min), -FLT_MAX);
+        const float scale = 256.0f / (top - bottom);
+        auto bin = [&](uint32_t k) {
+            return min(255, max(0, (int)((top - 0.5f * fminf(value_of(k), FLT_MAX)) * scale)));
+        };
+        for (int i = tid; i < n; i += SP_THREADS) {
+            const uint32_t k = (uint32_t)(a[i] >> 32);
+            if (k >= lo && k <= hi) atomicAdd(&bins[bin(k)], 1u);
+        }
+        __syncthreads();
+        if (tid < 32) {
+            uint32_t c[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += c[i] = bins[lane * 8 + i];
+            uint32_t incl = sum;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += o;
+            }
+            int before = above + (int)(incl - sum);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (before < keep && before + (int)c[i] >= keep) {
+                    s.pick_bin = lane * 8 + i;
+                    s.pick_above = before;
+                    s.pick_kept = before + (int)c[i];
+                }
+                before += (int)c[i];
+            }
+            if (lane == 0) { s.key_min = 0xffffffffu; s.key_max = 0; }
+        }
+        __syncthreads();
+        const int b = s.pick_bin;
+        mn = 0xffffffffu, mx = 0;
+        for (int i = tid; i < n; i += SP_THREADS) {
+            const uint32_t k = (uint32_t)(a[i] >> 32);
+            if (k >= lo && k <= hi && bin(k) == b) { mn = min(mn, k); mx = max(mx, k); }
+        }
+        mn = __reduce_min_sync(0xffffffffu, mn);
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        if (lane == 0) { atomicMin(&s.key_min, mn); atomicMax(&s.key_max, mx); }
+        __syncthreads();
+        lo = cut = s.key_min;
+        hi = s.key_max;
+        above = s.pick_above;
+        kept = s.pick_kept;
+        if (kept <= most || lo == hi) break;
+    }
+    return leave_from(s, a, n, cut);
+}
+
+// A full list: cut to what the row keeps by rank, or to what min_p leaves by now.  s.n is its length afterwards;
+// s.failed_here where it is still nearly full.
+__device__ void shorten(SampleShared &s, const RowPlan &R) {
+    const int tid = threadIdx.x;
+    int n = min(s.n, SP_LIST);
+    uint32_t cut = s.threshold;
+    if (R.keep) n = cut_list(s, s.list, n, R.keep, SP_LIST / 4, cut);
+    else n = leave_from(s, s.list, n, cut);
+    if (tid == 0) {
+        s.n = n;
+        s.threshold = max(s.threshold, cut);
+        if (n > SP_LIST * 3 / 4) s.failed_here = 1;
+    }
+    __syncthreads();
+}
+
+// ---- finding the token ------------------------------------------------------------------------
+__device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t token, double logprob) {
+    P.token[r] = token;
+    if (P.logprob) P.logprob[r] = (float)logprob;
+}
+
+// The first block, from the cluster's candidates.  False where they do not hold the whole of what is kept.
+__device__ bool pick_from_list(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m,
+                               double all, int n) {
+    const int tid = threadIdx.x;
+    if (R.keep && n > R.keep) {
+        uint32_t cut;
+        n = cut_list(s, s.merge, n, R.keep, R.keep + 32, cut);
+    }
+    int size = 32;
+    while (size < n) size <<= 1;
+    for (int i = n + tid; i < size; i += SP_THREADS) s.merge[i] = 0;
+    __syncthreads();
+    sort_entries<true>(s.merge, size);
+    if (R.k == 1) {
+        if (tid == 0) answer(P, row, index_of(s.merge[0]), 0.0);
+        return true;
+    }
+    const int per = (size + SP_THREADS - 1) / SP_THREADS, first = tid * per;
+    constexpr int MOST = SP_LIST / SP_THREADS;
+    uint64_t w[MOST], sum = 0;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+        const int i = first + j;
+        w[j] = 0;
+        if (j < per && i < n && (R.k == 0 || i < R.k)) {
+            const double t = exponent_of(value_of((uint32_t)(s.merge[i] >> 32)), m, R.c);
+            if (t >= R.low) w[j] = whole(weight_of(t, s.table));
+        }
+        sum += w[j];
+    }
+    uint64_t total;
+    uint64_t before = block_before<uint64_t>(sum, s.scan_u, total);
+    if (R.p < 1.0) {
+        const double need = R.p * (R.sums ? all : (double)total);
+        if (R.sums && (double)total < need) return false;      // (the same in every thread)
+        sum = 0;
+        uint64_t at = before;
+#pragma unroll
+        for (int j = 0; j < MOST; ++j) {
+            const uint64_t mine = w[j];
+            if (!((double)at < need) && first + j > 0) w[j] = 0;
+            at += mine;
+            sum += w[j];
+        }
+        block_before<uint64_t>(sum, s.scan_u, total);
+    }
+    // what is kept, by index: its place in the order goes along
+    uint32_t index[MOST];
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+        if (j < per && w[j]) {
+            index[j] = (uint32_t)index_of(s.merge[first + j]);
+            ++mine;
+        }
+    }
+    uint64_t all_kept;
+    int at = (int)block_before<uint64_t>((uint64_t)mine, s.scan_u, all_kept);
+    const int kept = (int)all_kept;
+    size = 32;
+    while (size < kept) size <<= 1;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j)
+        if (j < per && w[j]) {
+            s.merge[at] = (uint64_t)index[j] << 32 | (uint32_t)at;
+            s.list[at++] = w[j];
+        }
+    for (int i = kept + tid; i < size; i += SP_THREADS) s.merge[i] = ~0ull;
+    __syncthreads();
+    sort_entries<false>(s.merge, size);
+    uint64_t target = (uint64_t)((double)R.u * (double)total);
+    if (target >= total) target = total - 1;
+    const int per2 = (size + SP_THREADS - 1) / SP_THREADS, first2 = tid * per2;
+    sum = 0;
+    for (int j = 0; j < per2; ++j)
+        if (first2 + j < kept) sum += s.list[(uint32_t)s.merge[first2 + j]];
+    uint64_t whole_sum;
+    before = block_before<uint64_t>(sum, s.scan_u, whole_sum);
+    if (before <= target && target < before + sum)
+        for (int j = 0; j < per2; ++j) {
+            const uint64_t e = s.merge[first2 + j], we = s.list[(uint32_t)e];
+            if (target < before + we) {
+                answer(P, row, (int32_t)(e >> 32), log((double)we / (double)total));
+                break;
+            }
+            before += we;
+        }
+    return true;
+}
+
+// The first block, from the sums of the row's steps in s.merge; w(value, index) is the weight of a value again.
+template <bool BF16, typename W>
+__device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, const char *logits, W w) {
+    constexpr int SEG = Step<BF16>::SEG, PER = SP_LIST / SP_THREADS, MINE = SEG / SP_THREADS;
+    const int tid = threadIdx.x;
+    const double *sums = reinterpret_cast<const double *>(s.merge);
+    double mine[PER], sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        mine[j] = tid * PER + j < P.segs ? sums[tid * PER + j] : 0.0;
+        sum += mine[j];
+    }
+    double total;
+    double before = block_before<double>(sum, s.scan_d, total);
+    const double target = (double)R.u * total;
+    if (tid == 0) { s.found = P.segs; s.rest = 0.0; }
+    __syncthreads();
+    bool here = false;
+    int seg = P.segs;
+    double rest = 0.0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (!here && mine[j] > 0.0 && target < before + mine[j]) {
+            here = true;
+            seg = tid * PER + j;
+            rest = target - before;
+        }
+        before += mine[j];
+    }
+    if (here) atomicMin(&s.found, seg);
+    __syncthreads();
+    if (here && s.found == seg) s.rest = rest;
+    __syncthreads();
+    seg = s.found;
+    rest = s.rest;
+    // The step at which the sums pass the target; should it hold nothing to draw (the target on a border), the
+    // next that does, and behind the last one the last that does.
+    int step = seg < P.segs ? 1 : -1;
+    if (step < 0) seg = P.segs - 1;
+    for (bool begun = false; seg >= 0;) {
+        const int32_t at = seg * SEG + tid * MINE;
+        double x[MINE], own = 0.0;
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            x[j] = 0.0;
+            if (at + j < P.V) {
+                const float l = BF16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(logits) + at + j) << 16)
+                                     : __ldg(reinterpret_cast<const float *>(logits) + at + j);
+                x[j] = w(l, at + j);
+            }
+            own += x[j];
+        }
+        double here_total;
+        const double ahead = block_before<double>(own, s.scan_d, here_total);
+        if (tid == 0) s.found = step > 0 ? 0x7fffffff : -1;
+        __syncthreads();
+        if (here_total > 0.0) {
+            // the lowest index that passes the rest; where none does by a rounding, or behind the end: the last one
+            const double limit = step < 0 ? INFINITY : begun ? 0.0 : rest;
+            double run = ahead;
+            int32_t first = -1, last = -1;
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) {
+                run += x[j];
+                if (x[j] > 0.0) {
+                    if (first < 0 && run > limit) first = at + j;
+                    last = at + j;
+                }
+            }
+            if (step > 0 && first >= 0) atomicMin(&s.found, first);
+            __syncthreads();
+            if (step < 0 || s.found == 0x7fffffff) {
+                __syncthreads();
+                if (tid == 0) s.found = -1;
+                __syncthreads();
+                if (last >= 0) atomicMax(&s.found, last);
+                __syncthreads();
+            }
+            const int32_t token = s.found;
+#pragma unroll
+            for (int j = 0; j < MINE; ++j)
+                if (token == at + j) answer(P, row, token, log(x[j] / total));
+            return;
+        }
+        begun = true;
+        seg += step;
+        if (seg >= P.segs) { seg = P.segs - 1; step = -1; }
+        __syncthreads();
+    }
+}
+
+// ---- the general path -------------------------------------------------------------------------
+// What is kept so far: parts of the range before `part`, and of that one the entries from `from` on.
+struct SampleCut { int32_t part; uint64_t from; };
+
+struct GeneralRow {
+    float m, c32;
+    RowPlan R;
+    __device__ __forceinline__ int32_t part_of(float l) const {       // quarters of a power of two below the largest
+        return l == m ? 0 : min(255, max(0, (int)((m - l) * c32 * 4.0f)));
+    }
+    __device__ __forceinline__ bool inside(float l, int32_t i, const SampleCut &cut) const {
+        if (!(l > -INFINITY)) return false;
+        if (cut.part < 256) {
+            const int32_t p = part_of(l);
+            if (p > cut.part || (p == cut.part && entry_of(l, i) < cut.from)) return false;
+        }
+        return R.low == -INFINITY || exponent_of(l, m, R.c) >= R.low;
+    }
+};
+
+// Finds how far the first k (weight: the first ones with p of all weight) of what `cut` keeps reach, a digit of
+// eight bits at a time: the part of the range, the key's bytes, the index's.  Every block of the cluster calls it.
+template <bool BF16>
+__device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const GeneralRow &G,
+                                 const char *logits, SampleCut cut, bool weight, int &turn) {
+    using S = Step<BF16>;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    SampleCut to = {256, 0};
+    uint64_t base_count = 0, base_weight = 0;
+    double need = weight ? 0.0 : (double)G.R.k;
+    for (int level = 0; level < 8; ++level) {
+        // (a digit's sums are read by the whole cluster while the next one's are taken: two sets in turn)
+        uint32_t *const digit_count = s.digit_count[turn];
+        uint64_t *const digit_weight = s.digit_weight[turn];
+        turn ^= 1;
+        const int shift = level <= 4 ? 64 - 8 * level : 56 - 8 * level;
+        if (level == 5) to.from |= 0xff000000u;          // an index has 24 bits, and stands there as its complement
+        digit_count[tid] = 0;
+        digit_weight[tid] = 0;
+        __syncthreads();
+        for (int it = 0; it < P.steps; ++it) {
+            const int32_t seg = (it * C + rank) * SP_WARPS + warp;
+            if (seg >= P.segs) break;
+            S x;
+            x.load(P, logits, seg);
+#pragma unroll 4
+            for (int e = 0; e < S::N; ++e) {
+                const float l = x.value(e);
+                const int32_t i = S::index(seg, e);
+                if (!G.inside(l, i, cut)) continue;
+                const int32_t part = G.part_of(l);
+                int digit = part;
+                if (level > 0) {
+                    const uint64_t entry = entry_of(l, i);
+                    if (part != to.part) continue;
+                    if (level > 1 && (entry >> (shift + 8)) != (to.from >> (shift + 8))) continue;
+                    digit = 255 - (int)(entry >> shift & 255u);
+                }
+                atomicAdd(&digit_count[digit], 1u);
+                if (weight)
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&digit_weight[digit]),
+                              (unsigned long long)whole(weight_of(exponent_of(l, G.m, G.R.c), s.table)));
+            }
+        }
+        cluster.sync();
+        uint64_t count = 0, sum = 0;
+        for (int r = 0; r < C; ++r) {
+            count += *cluster.map_shared_rank(digit_count + tid, r);
+            sum += *cluster.map_shared_rank(digit_weight + tid, r);
+        }
+        uint64_t counts, sums;
+        const uint64_t count_before = block_before<uint64_t>(count, s.scan_u, counts);
+        const uint64_t sum_before = block_before<uint64_t>(sum, s.scan_u, sums);
+        if (weight && level == 0) need = G.R.p * (double)sums;
+        const double reached = weight ? (double)(base_weight + sum_before + sum) : (double)(base_count + count_before + count);
+        const double before = weight ? (double)(base_weight + sum_before) : (double)(base_count + count_before);
+        if (tid == 0) s.found = 256;
+        __syncthreads();
+        if (count && (before < need || (count_before == 0 && base_count == 0)) && reached >= need) atomicMin(&s.found, tid);
+        __syncthreads();
+        const int digit = s.found;
+        if (digit == 256) return level == 0 ? cut : to;      // all of it
+        if (tid == digit) {
+            s.pick_count = base_count + count_before;
+            s.pick_weight = base_weight + sum_before;
+            s.pick_here = count;
+        }
+        __syncthreads();
+        if (level == 0) to.part = digit; else to.from |= (uint64_t)(255 - digit) << shift;
+        base_count = s.pick_count;
+        base_weight = s.pick_weight;
+        const uint64_t here = s.pick_here;
+        __syncthreads();
+        if (here == 1 || (!weight && (double)(base_count + here) == need)) break;     // all that are left belong to it
+    }
+    return to;
+}
+
+template <bool BF16>
+__device__ void general_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
+                            const char *logits) {
+    using S = Step<BF16>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const GeneralRow G = {s.row_max, (float)R.c, R};
+    SampleCut cut = {256, 0};
+    int turn = 0;
+    if (R.k) {
+        RowPlan all = R;                     // the first k of all, then min_p, then top_p
+        all.low = -INFINITY;
+        const GeneralRow A = {G.m, G.c32, all};
+        cut = general_cut<BF16>(s, cluster, P, A, logits, cut, false, turn);
+    }
+    if (R.p < 1.0) cut = general_cut<BF16>(s, cluster, P, G, logits, cut, true, turn);
+    auto w = [&](float l, int32_t i) { return G.inside(l, i, cut) ? weight_of(exponent_of(l, G.m, R.c), s.table) : 0.0; };
+    double *sums = reinterpret_cast<double *>(s.list);
+    for (int it = 0; it < P.steps; ++it) {
+        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
+        double sum = 0.0;
+        if (seg < P.segs) {
+            S x;
+            x.load(P, logits, seg);
+#pragma unroll 4
+            for (int e = 0; e < S::N; ++e) sum += w(x.value(e), S::index(seg, e));
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) sums[it * SP_WARPS + warp] = sum;
+    }
+    cluster.sync();
+    if (rank == 0) {
+        double *all = reinterpret_cast<double *>(s.merge);
+        for (int g = threadIdx.x; g < P.segs; g += SP_THREADS) {
+            const int r = g / SP_WARPS % C;
+            all[g] = cluster.map_shared_rank(sums, r)[g / (SP_WARPS * C) * SP_WARPS + g % SP_WARPS];
+        }
+        __syncthreads();
+        pick_from_sums<BF16>(s, P, R, row, logits, w);
+    }
+    cluster.sync();
+}
+
+// ---- the kernel -------------------------------------------------------------------------------
+__device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) {
+    RowPlan R;
+    const float tau = __ldg(P.temperature + row);
+    R.greedy = !(tau > 0.0f);
+    R.c = 1.4426950408889634 / (R.greedy ? 1.0 : (double)tau);
+    const int32_t k = R.greedy ? 1 : P.top_k ? __ldg(P.top_k + row) : 0;
+    R.k = k > 0 && k < P.V ? k : R.greedy ? 1 : 0;
+    const float p = R.greedy || !P.top_p ? 1.0f : __ldg(P.top_p + row), mp = R.greedy || !P.min_p ? 0.0f : __ldg(P.min_p + row);
+    R.by_p = p < 1.0f;
+    R.p = R.by_p ? (double)fmaxf(p, 0.0f) : 1.0;
+    R.by_min = mp > 0.0f;
+    R.low = R.by_min ? log2((double)fminf(mp, 1.0f)) : -INFINITY;
+    // with a little room for the roundings of this bound
+    R.drop = R.by_min ? (float)(-R.low / R.c) * 1.00001f : INFINITY;
+    R.u = fminf(fmaxf(__ldg(P.uniform + row), 0.0f), 1.0f);
+    // (far temperatures, at which masked tokens do not vanish by themselves, take the general path)
+    const bool far = !(R.c > 1e-30);
+    const bool by_rank = R.k && R.k <= KEEP_K;
+    R.list = !far && (by_rank || R.by_min || (R.by_p && !R.k));
+    R.keep = by_rank ? R.k : R.by_min || !R.list ? 0 : KEEP_P;
+    R.sums = !far && !R.k && !R.by_min;
+    R.segments = R.sums && !R.by_p;
+    return R;
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParams P) {
+    using S = Step<BF16>;
+    __shared__ SampleShared s;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / C;
+    const char *logits = reinterpret_cast<const char *>(P.logits) + row * P.ld * (BF16 ? 2 : 4);
+    S next;
+    {
+        const int32_t seg = rank * SP_WARPS + warp;
+        if (seg < P.segs) next.load(P, logits, seg); else next.nothing();
+    }
+    const RowPlan R = plan_row(P, row);
+    if (tid < 64) {
+        const double e = exp2(tid / 64.0);
+        for (int i = 0; i < 16; ++i) s.table[tid * 16 + i] = e;
+    }
+    if (tid == 0) {
+        s.n = s.failed_here = s.merged = 0;
+        s.threshold = key_of(-FLT_MAX);
+        s.best = 0;
+    }
+    __syncthreads();
+    cluster.barrier_arrive();                 // (s.merged is there before any block adds to it)
+    bool list = R.list;
+    float top = -INFINITY;
+    double sum = 0.0, base = 0.0, magic = SP_MAGIC;
+    float floor_l = -FLT_MAX;
+    double *const segs = reinterpret_cast<double *>(s.list);
+    for (int it = 0; it < P.steps; ++it) {
+        const S x = next;
+        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
+        if (it + 1 < P.steps && seg + C * SP_WARPS < P.segs) next.load(P, logits, seg + C * SP_WARPS); else next.nothing();
+        float vec[4], step_top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            vec[v] = x.value(v * S::VEC);
+#pragma unroll
+            for (int j = 1; j < S::VEC; ++j) vec[v] = max_or_nan(vec[v], x.value(v * S::VEC + j));
+            step_top = max_or_nan(step_top, vec[v]);
+        }
+        top = max_or_nan(top, step_top);
+        if (it == 0 && (R.sums || (list && R.keep))) {
+            // the largest of the first steps: what the sums are taken against; the K-th of the vectors' largest is
+            // one that K values at least are not below
+            if (R.sums) {
+                const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
+                if (lane == 0) atomicMax(&s.best, k);
+                __syncthreads();
+                const float b = s.best ? value_of(s.best) : 0.0f;
+                base = rint((double)b * R.c);
+                if (!(fabs(base) < 1e12)) base = 0.0;
+                magic = SP_MAGIC - base;
+                floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
+            }
+            if (list && R.keep) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (vec[v] > -INFINITY) put(s, entry_of(vec[v], 0));
+                __syncthreads();
+                uint32_t cut;
+                cut_list(s, s.list, s.n, R.keep, R.keep + R.keep / 4, cut);
+                __syncthreads();
+                if (tid == 0) {
+                    s.n = 0;
+                    s.threshold = max(s.threshold, cut);
+                }
+                __syncthreads();
+            }
+        }
+        if (R.sums) {
+#pragma unroll
+            for (int e = 0; e < S::N; ++e) sum += power2((double)fmaxf(x.value(e), floor_l), R.c, magic, s.table);
+            if (R.segments) {
+#pragma unroll
+                for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                if (lane == 0) segs[it * SP_WARPS + warp] = sum;
+                sum = 0.0;
+            }
+        }
+        if (list) {
+            if (R.by_min) {
+                const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
+                if (lane == 0 && k > s.best && atomicMax(&s.best, k) < k) {
+                    const float m = value_of(k), t = (m - R.drop) - fabsf(m) * 1e-5f;
+                    if (t > -FLT_MAX) atomicMax(&s.threshold, key_of(t));
+                }
+                __syncwarp();
+            }
+            float t = value_of(s.threshold);
+            uint32_t wait = 0;
+            if (!(step_top < t)) {
+#pragma unroll
+                for (int e = 0; e < S::N; ++e)
+                    if (x.value(e) >= t) wait |= 1u << e;
+            }
+            for (;;) {
+                if (wait) {
+#pragma unroll
+                    for (int e = 0; e < S::N; ++e)
+                        if ((wait >> e & 1u) && put(s, entry_of(x.value(e), S::index(seg, e)))) wait &= ~(1u << e);
+                }
+                if (!__syncthreads_or(wait != 0)) break;
+                shorten(s, R);
+                if (s.failed_here) {
+                    list = false;
+                    break;
+                }
+                t = value_of(s.threshold);
+#pragma unroll
+                for (int e = 0; e < S::N; ++e)
+                    if (!(x.value(e) >= t)) wait &= ~(1u << e);
+            }
+        }
+    }
+    // to the first block: the largest value, the sum, the candidates
+    const bool nan = top != top;
+    const uint32_t block_top = __reduce_max_sync(0xffffffffu, nan ? 0u : key_of(top));
+    if (lane == 0) atomicMax(&s.best, block_top);
+    const bool any_nan = __syncthreads_or(nan);
+    double block_sum = 0.0;
+    if (R.sums && !R.segments) block_before<double>(sum, s.scan_d, block_sum);
+    int n = list ? min(s.n, SP_LIST) : 0;
+    if (list && R.keep && n > R.keep + 32) {
+        uint32_t cut;
+        n = cut_list(s, s.list, n, R.keep, R.keep + 32, cut);
+    }
+    cluster.barrier_wait();
+    SampleShared &first = *cluster.map_shared_rank(&s, 0);
+    if (tid == 0) {
+        s.found = n ? atomicAdd(&first.merged, n) : 0;
+        first.top[rank] = s.best;
+        first.bad[rank] = any_nan;
+        first.failed[rank] = s.failed_here || s.found + n > SP_LIST;
+        first.sum[rank] = block_sum;
+        first.base[rank] = base;
+    }
+    __syncthreads();
+    for (int i = tid; i < n && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
+    cluster.sync();
+    if (rank == 0) {
+        uint32_t best = 0;
+        bool bad = false, failed = !R.list && !R.sums;
+        for (int i = 0; i < C; ++i) {
+            best = max(best, s.top[i]);
+            bad = bad || s.bad[i];
+            failed = failed || s.failed[i];
+        }
+        const float m = value_of(best);
+        bad = bad || !(m > -INFINITY);
+        bool general = false;
+        if (bad) {
+            if (tid == 0) answer(P, row, -1, nan_value());
+        } else {
+            if (R.sums) {
+                double all = 0.0;
+                for (int i = 0; i < C; ++i) {
+                    const double t = (double)value_of(s.top[i]) * R.c, b = s.base[i];
+                    const bool some = value_of(s.top[i]) > -INFINITY;
+                    failed = failed || (some && !(fabs(t - b) < 900.0));
+                    if (tid == i) s.scale[i] = some ? exp2(fma(-(double)m, R.c, b)) : 0.0;
+                }
+                __syncthreads();
+                if (!failed) {
+                    for (int i = 0; i < C; ++i) all += s.scale[i] > 0.0 ? s.sum[i] * s.scale[i] : 0.0;
+                    if (R.segments) {
+                        double *const sums = reinterpret_cast<double *>(s.merge);
+                        for (int g = tid; g < P.segs; g += SP_THREADS) {
+                            const int r = g / SP_WARPS % C;
+                            const double v = cluster.map_shared_rank(segs, r)[g / (SP_WARPS * C) * SP_WARPS + g % SP_WARPS];
+                            sums[g] = s.scale[r] > 0.0 ? v * s.scale[r] : 0.0;
+                        }
+                        __syncthreads();
+                        pick_from_sums<BF16>(s, P, R, row, logits,
+                                             [&](float l, int32_t) { return weight_of(exponent_of(l, m, R.c), s.table); });
+                    } else {
+                        general = !pick_from_list(s, P, R, row, m, all * SP_ONE, s.merged);
+                    }
+                }
+            } else if (!failed) {
+                general = !pick_from_list(s, P, R, row, m, 0.0, s.merged);
+            }
+            general = general || failed;
+        }
+        if (tid < C) {
+            SampleShared &to = *cluster.map_shared_rank(&s, tid);
+            to.general = general;
+            to.row_max = m;
+        }
+    }
+    cluster.sync();
+    if (s.general) general_row<BF16>(s, cluster, P, R, row, logits);
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+template <bool BF16>
+static lora_status_t launch_sample(SampleParams P, int32_t R, cudaStream_t stream) {
+    constexpr int SEG = Step<BF16>::SEG;
+    P.segs = (P.V + SEG - 1) / SEG;
+    // blocks of a row: so many that the rows fill the GPU, and no more than there are steps for their warps
+    int C = 1;
+    while (C < SP_CLUSTER && (int64_t)R * C < 148 * 4 && P.segs >= 2 * C * SP_WARPS) C *= 2;
+    P.steps = (P.segs + C * SP_WARPS - 1) / (C * SP_WARPS);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(R * C));
+    cfg.blockDim = dim3(SP_THREADS);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)C;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<BF16>, P));
+    return count_launch();
+}
+
+}  // namespace lora
+
+using namespace lora;
+
+extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, void *stream) {
+    if (!args) return LORA_ERR_INVALID_ARG;
+    const bool bf16 = args->logits_type == LORA_LOGITS_BF16;
+    if (!bf16 && args->logits_type != LORA_LOGITS_FP32) return LORA_ERR_INVALID_ARG;
+    if (R < 0 || R > (1 << 24) || args->vocab < 1 || args->vocab > SP_MAX_V) return LORA_ERR_SHAPE;
+    if (R == 0) return LORA_OK;
+    if (!args->logits || !args->temperature || !args->uniform || !args->token) return LORA_ERR_INVALID_ARG;
+    if (args->ld < args->vocab) return LORA_ERR_SHAPE;
+    const int64_t unit = bf16 ? 2 : 4;
+    const void *words[7] = {args->token, args->logprob, args->temperature, args->top_k, args->top_p, args->min_p, args->uniform};
+    if ((uintptr_t)args->logits % unit) return LORA_ERR_INVALID_ARG;
+    for (int i = 0; i < 7; ++i) {
+        if (!words[i]) continue;
+        if ((uintptr_t)words[i] & 3) return LORA_ERR_INVALID_ARG;
+        for (int o = 0; o < 2 && o < i; ++o)       // no output lies on anything else
+            if (words[o] && rows_overlap(words[o], 4 * (int64_t)R, 4 * (int64_t)R, words[i], 4 * (int64_t)R, 4 * (int64_t)R, 1))
+                return LORA_ERR_INVALID_ARG;
+        if (i < 2 && rows_overlap(words[i], 4 * (int64_t)R, 4 * (int64_t)R, args->logits,
+                                  ((R - 1) * args->ld + args->vocab) * unit, 8, 1))
+            return LORA_ERR_INVALID_ARG;
+    }
+    SampleParams P;
+    P.logits = args->logits;
+    P.ld = args->ld;
+    P.V = args->vocab;
+    P.segs = P.steps = 0;
+    P.aligned = ((uintptr_t)args->logits | (uint64_t)(args->ld * unit)) % 16 == 0;
+    P.temperature = args->temperature;
+    P.top_p = args->top_p;
+    P.min_p = args->min_p;
+    P.uniform = args->uniform;
+    P.top_k = args->top_k;
+    P.token = args->token;
+    P.logprob = args->logprob;
+    DeviceGuard g(args->device);
+    if (!g.ok) return cuda_fail(cudaErrorInvalidDevice);
+    return bf16 ? launch_sample<true>(P, R, (cudaStream_t)stream) : launch_sample<false>(P, R, (cudaStream_t)stream);
+}

@@ -1,0 +1,288 @@
+"""Sampling of the next tokens against the definition in 64 bits, row by row."""
+import numpy as np
+import pytest
+
+from gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+def _reference(x, tau, k, p, mp, u):
+    """One row: (token, logprob, distance of u from the nearest border of the kept tokens' sums)."""
+    x = np.asarray(x, np.float64)
+    if np.isnan(x).any() or not (x > -np.inf).any():
+        return -1, np.nan, 1.0
+    m = x.max()
+    if not tau > 0:
+        return int(np.argmax(x)), 0.0, 1.0
+    with np.errstate(all="ignore"):
+        e = np.where(x == m, 0.0, (x - m) / np.float64(tau))
+    e = np.where(x == -np.inf, -np.inf, e)
+    w = np.where(e < -46 * np.log(2), 0.0, np.exp(e))
+    order = np.lexsort((np.arange(x.size), -x))
+    keep = np.zeros(x.size, bool)
+    keep[order[:k] if 0 < k < x.size else order] = True
+    if mp > 0:
+        keep &= e >= np.log(min(np.float64(mp), 1.0))
+    if p < 1:
+        o = order[keep[order]]
+        cum = np.cumsum(w[o])
+        n = max(1, int((cum - w[o] < max(np.float64(p), 0.0) * cum[-1]).sum()))
+        keep[:] = False
+        keep[o[:n]] = True
+    w = np.where(keep, w, 0.0)
+    cum = np.cumsum(w)
+    u = 0.0 if np.isnan(u) else min(max(float(u), 0.0), 1.0)
+    at = int(np.searchsorted(cum, u * cum[-1], side="right"))
+    last = int(np.flatnonzero(w)[-1])
+    at = min(at, last)
+    return at, np.log(w[at] / cum[-1]), np.abs(cum / cum[-1] - u).min()
+
+
+def _run(logits, tau, k=None, p=None, mp=None, u=None, stream=None, R=None):
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    R = logits.shape[0] if R is None else R
+
+    def dev(a, dtype):
+        return None if a is None else torch.as_tensor(np.broadcast_to(np.asarray(a), (R,)).copy()).to(dtype).cuda()
+
+    token = torch.full((R + 2,), -77, dtype=torch.int32, device="cuda")
+    logprob = torch.full((R + 2,), 77.0, dtype=torch.float32, device="cuda")
+    params = [dev(tau, torch.float32), dev(k, torch.int32), dev(p, torch.float32), dev(mp, torch.float32), dev(u, torch.float32)]
+    lb.sample(lb.sample_args(logits=logits, temperature=params[0], top_k=params[1], top_p=params[2], min_p=params[3],
+                             uniform=params[4], token=token[1:R + 1], logprob=logprob[1:R + 1]), R, stream=stream)
+    torch.cuda.synchronize()
+    assert token[0] == token[R + 1] == -77 and logprob[0] == logprob[R + 1] == 77.0
+    return token[1:R + 1].cpu().numpy(), logprob[1:R + 1].cpu().numpy()
+
+
+def _check(logits, tau, k=None, p=None, mp=None, u=None):
+    R = logits.shape[0]
+    got, lp = _run(logits, tau, k, p, mp, u)
+    x = logits.float().cpu().numpy()
+
+    def each(a, none, dtype):
+        return np.full(R, none) if a is None else np.broadcast_to(np.asarray(a), (R,)).astype(dtype)
+
+    tau, k, p, mp, u = (each(a, n, t) for a, n, t in ((tau, 1, np.float32), (k, 0, np.int32), (p, 1.0, np.float32),
+                                                     (mp, 0.0, np.float32), (u, 0.0, np.float32)))
+    for r in range(R):
+        want, want_lp, _ = _reference(x[r], tau[r], int(k[r]), p[r], mp[r], u[r])
+        assert got[r] == want, (r, got[r], want, tau[r], k[r], p[r], mp[r], u[r])
+        # the weight and the sum to 1e-11 each, and one rounding to fp32
+        assert (np.isnan(lp[r]) and np.isnan(want_lp)) or abs(lp[r] - want_lp) <= 4e-11 + 2.0 ** -24 * abs(want_lp), (r, lp[r], want_lp)
+    return got
+
+
+def _logits(R, V, seed, bf16=False, spread=2.5, peaks=True, masked=0.0):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(R, V, generator=g, device="cuda") * spread
+    if peaks:
+        at = torch.randint(0, V, (R, min(V, 20)), generator=g, device="cuda")
+        x.scatter_add_(1, at, 8 * torch.rand(at.shape, generator=g, device="cuda"))
+    if masked:
+        x.masked_fill_(torch.rand(R, V, generator=g, device="cuda") < masked, -float("inf"))
+        x[:, seed % V] = 1.0
+    return x.bfloat16() if bf16 else x
+
+
+def _params(R, seed, ks, ps, mps):
+    rng = np.random.default_rng(seed)
+    return dict(tau=rng.choice([0.0, 0.5, 0.8, 1.0, 1.0, 1.7], R), k=rng.choice(ks, R), p=rng.choice(ps, R),
+                mp=rng.choice(mps, R), u=rng.random(R).astype(np.float32))
+
+
+SIZES = [1, 2, 7, 31, 100, 511, 512, 513, 1000, 1025, 4097, 8192, 20000, 32000, 50021, 131072, 200001]
+
+
+@pytest.mark.parametrize("V", SIZES)
+@pytest.mark.parametrize("bf16", [False, True])
+def test_mixed_parameters(V, bf16):
+    require_gpu()
+    R = 40 if V < 10000 else 24
+    x = _logits(R, V, V, bf16)
+    _check(x, **_params(R, V, [0, 0, 1, 2, 5, 40, 200, 256, 257, 1000], [1.0, 1.0, 0.1, 0.5, 0.9, 0.95, 0.999],
+                        [0.0, 0.0, 0.01, 0.2, 1.0]))
+
+
+@pytest.mark.parametrize("V", SIZES)
+@pytest.mark.parametrize("bf16", [False, True])
+def test_whole_vocabulary(V, bf16):
+    require_gpu()
+    R = 30
+    x = _logits(R, V, V + 1, bf16, peaks=False)
+    rng = np.random.default_rng(V)
+    _check(x, rng.choice([0.3, 1.0, 2.0, 30.0], R), u=rng.random(R).astype(np.float32))
+
+
+@pytest.mark.parametrize("R", [1, 2, 5, 37, 74, 75, 148, 149, 297, 600])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_every_number_of_blocks_a_row(R, bf16):
+    require_gpu()
+    V = 9001
+    x = _logits(R, V, R, bf16)
+    _check(x, **_params(R, R, [0, 0, 3, 50, 700], [1.0, 0.9, 0.99], [0.0, 0.0, 0.05]))
+
+
+@pytest.mark.parametrize("V,k,p,mp", [(50021, 300, 1.0, 0.0), (50021, 5000, 0.98, 0.0), (50021, 50020, 1.0, 0.0),
+                                      (50021, 50021, 1.0, 0.0), (50021, 0, 0.999, 0.0), (50021, 0, 0.5, 0.0),
+                                      (131072, 20000, 0.9, 1e-6), (131072, 0, 0.97, 1e-4), (3000, 2999, 0.9999, 1e-9),
+                                      (600, 599, 1.0, 0.0), (50021, 257, 0.3, 0.0), (50021, 0, 1.0, 1e-5)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_what_no_list_holds(V, k, p, mp, bf16):
+    require_gpu()
+    R = 20
+    x = _logits(R, V, V + k, bf16, peaks=False, spread=1.5)
+    rng = np.random.default_rng(k)
+    _check(x, rng.choice([0.7, 1.0, 2.0], R), k, p, mp, rng.random(R).astype(np.float32))
+
+
+@pytest.mark.parametrize("R", [3, 700])
+@pytest.mark.parametrize("k,p,mp", [(0, 1.0, 0.0), (1, 1.0, 0.0), (7, 1.0, 0.0), (250, 1.0, 0.0), (3000, 1.0, 0.0),
+                                    (0, 0.3, 0.0), (40, 0.5, 0.0), (0, 1.0, 1.0), (0, 0.25, 0.5), (4000, 0.7, 0.9)])
+@pytest.mark.parametrize("kind", ["equal", "two", "whole", "steps"])
+def test_ties_go_to_the_lowest_index(R, k, p, mp, kind):
+    """Weights that are exact (1, and 2^-n with the temperature 1 / ln 2 missed by a rounding): many equal values."""
+    require_gpu()
+    import torch
+    V = 6001
+    g = torch.Generator(device="cuda").manual_seed(k)
+    if kind == "equal":
+        x = torch.full((R, V), -3.25, device="cuda")
+    elif kind == "two":
+        x = torch.where(torch.rand(R, V, generator=g, device="cuda") < 0.4, 2.0, -1.0)
+    elif kind == "whole":
+        x = torch.randint(-6, 7, (R, V), generator=g, device="cuda").float()
+    else:
+        x = (torch.arange(V, device="cuda") // 100).float().expand(R, V).contiguous() * 0.25
+    u = torch.rand(R, generator=g, device="cuda").cpu().numpy()
+    _check(x if k % 2 else x.bfloat16(), 1.0, k, p, mp, u)
+    _check(x, 0.0, k, p, mp, u)
+
+
+def test_zeros_of_both_signs_are_one_value():
+    require_gpu()
+    import torch
+    x = torch.tensor([[-0.0, 0.0, -0.0, 0.0, -1.0, -0.0]] * 8, device="cuda")
+    got = _check(x, 1.0, 3, 1.0, 0.0, np.linspace(0, 0.99, 8))
+    assert set(got.tolist()) == {0, 1, 2}
+    assert _check(x, 0.0, u=0.5).tolist() == [0] * 8
+
+
+@pytest.mark.parametrize("V", [50, 3000, 40000])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("k,p,mp", [(0, 1.0, 0.0), (5, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.1), (1000, 0.8, 0.01)])
+def test_values_that_are_not_finite(V, bf16, k, p, mp):
+    require_gpu()
+    import torch
+    inf = float("inf")
+    x = _logits(12, V, V, bf16)
+    x[0, V // 2] = float("nan")
+    x[1] = -inf
+    x[2, :] = -inf
+    x[2, V - 1] = -5.0                                     # one token is left
+    x[3, V // 3] = inf
+    x[4, [3, V // 2, V - 2]] = inf                         # three share the weight
+    x[5, : V - 7] = -inf
+    x[6, V // 5] = 3e38
+    x[7] = -3e38
+    x[8, ::2] = -inf
+    x[9, 1] = -float("nan")
+    x[10, 10:] = x[10, 10:] * 1e4
+    x[11] = 1e-42
+    for tau in (1.0, 0.0, 0.01, 50.0):
+        _check(x, tau, k, p, mp, np.linspace(0.0, 0.999, 12).astype(np.float32))
+
+
+@pytest.mark.parametrize("V", [100, 5000])
+def test_odd_parameters(V):
+    require_gpu()
+    nan, inf = float("nan"), float("inf")
+    for tau in (-1.0, nan, -inf, inf, 1e-30, 1e-42, 1e30, 3e38, 1e-3, 1e6):
+        x = _logits(6, V, 3, masked=0.3)
+        u = np.array([0.0, 0.3, 0.6, 0.9, 0.999, 0.5], np.float32)
+        for k, p, mp in ((0, 1.0, 0.0), (4, 1.0, 0.0), (0, 0.7, 0.0), (0, 1.0, 0.3), (90, 0.5, 0.2)):
+            _check(x, tau, k, p, mp, u)
+    x = _logits(9, V, 4)
+    one = np.nextafter(np.float32(1), np.float32(0))
+    for u in (0.0, one, 1.0, 5.0, -1.0, nan, inf, 2.0 ** -40):
+        for k, p, mp in ((0, 1.0, 0.0), (9, 1.0, 0.0), (0, 0.8, 0.0), (0, 1.0, 0.1), (400, 0.99, 0.0)):
+            _check(x, 1.0, k, p, mp, u)
+    for k in (-5, -2 ** 31, 2 ** 31 - 1, V - 1, V, V + 1):
+        _check(x, 1.0, k, None, None, 0.4)
+    for p in (0.0, -1.0, nan, 1.5, inf, one, 1e-30):
+        _check(x, 1.0, None, p, None, 0.4)
+    for mp in (-1.0, nan, 1.0, 2.0, inf, 1e-30, 1e-44):
+        _check(x, 1.0, None, None, mp, 0.4)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_masked_rows(bf16):
+    require_gpu()
+    for masked in (0.5, 0.99, 0.9999):
+        x = _logits(24, 40007, 8, bf16, masked=masked)
+        _check(x, **_params(24, 5, [0, 0, 1, 30, 256, 400], [1.0, 0.9, 0.5], [0.0, 0.05]))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V,more,at", [(1000, 24, 0), (1001, 0, 0), (1000, 1, 0), (999, 25, 3), (30001, 7, 1)])
+def test_rows_of_any_stride_and_alignment(V, more, at, bf16):
+    require_gpu()
+    import torch
+    wide = torch.full((9, V + more + 8), float("nan"), dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
+    flat = wide.view(-1)
+    x = _logits(9, V, V, bf16)
+    rows = torch.as_strided(flat, (9, V), (V + more, 1), at)
+    rows.copy_(x)
+    if more:
+        rows = torch.as_strided(flat, (9, V), (V + more, 1), at)
+    _check(rows, **_params(9, 3, [0, 20, 300], [1.0, 0.9], [0.0, 0.1]))
+
+
+def test_a_graph_follows_its_inputs():
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    R, V = 20, 12345
+    x, u = _logits(R, V, 0), torch.rand(R, device="cuda")
+    tau, k = torch.full((R,), 0.9, device="cuda"), torch.full((R,), 30, dtype=torch.int32, device="cuda")
+    k[::3] = 0
+    token, lp = torch.empty(R, dtype=torch.int32, device="cuda"), torch.empty(R, device="cuda")
+    args = lb.sample_args(logits=x, temperature=tau, top_k=k, uniform=u, token=token, logprob=lp)
+    lb.sample(args, R)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    before = lb.launch_count()
+    with torch.cuda.graph(graph):
+        lb.sample(args, R, stream=torch.cuda.current_stream())
+    assert lb.launch_count() == before + 1
+    for seed in range(3):
+        x.copy_(_logits(R, V, seed))
+        u.uniform_()
+        graph.replay()
+        torch.cuda.synchronize()
+        xs, us, ks = x.cpu().numpy(), u.cpu().numpy(), k.cpu().numpy()
+        assert token.tolist() == [_reference(xs[r], np.float32(0.9), int(ks[r]), 1.0, 0.0, us[r])[0] for r in range(R)]
+    # on another stream, twice at once, without logprobs, and fewer rows than there are
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [torch.full((R,), -77, dtype=torch.int32, device="cuda") for _ in side]
+    torch.cuda.synchronize()
+    for s, o in zip(side, outs):
+        lb.sample(lb.sample_args(logits=x, temperature=tau, top_k=k, uniform=u, token=o), R - 1, stream=s)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o[:-1], token[:-1]) and o[-1] == -77
+
+
+def test_shares_of_the_tokens():
+    """Ten thousand even numbers over one row: each token as often as its weight says, to one."""
+    require_gpu()
+    import torch
+    R, V = 10000, 17
+    x = torch.linspace(-2, 1, V, device="cuda").repeat(R, 1)
+    u = (np.arange(R) + 0.5) / R
+    got, _ = _run(x, 0.7, u=u)
+    p = torch.softmax(x[0].double() / np.float32(0.7).astype(np.float64), 0).cpu().numpy()
+    assert (np.abs(np.bincount(got, minlength=V) - p * R) <= 1).all()

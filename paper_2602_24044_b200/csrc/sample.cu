@@ -11,13 +11,13 @@
 // at half the rate of fp32's; a polynomial alone would be 12).  The table is there once for each pair of
 // banks, so that lanes with different entries do not wait for one another.
 //
-// A cluster of blocks takes a row, in steps of 2 KB a warp.  Rows with a filter collect candidates: whatever is
-// not below a threshold that only rises (the K-th largest so far, or min_p of the largest so far) goes to a
-// list in shared memory.  A list that is full is cut to the best K or a few more: K = top_k, or KEEP_P for
-// top_p alone, where the sum of all weights is taken on the way.  The first block then sorts what is left.
-// Rows without a filter only sum, a step's sum by itself: the token's step is looked up among the sums and
-// read again.  Whatever does not fit (top_k over KEEP_K, a list of ties, a nucleus of thousands) goes to a
-// general path that finds the cut digit by digit, reading its row once a digit from the second-level cache.
+// A cluster of blocks takes a row, in steps of 2 KB a warp.  Rows with a filter collect candidates in shared memory:
+// whatever is not below a threshold that only rises (one that K values so far are not below, or min_p of the largest
+// so far); K = top_k, or KEEP_P for top_p alone, where the sum of all weights is taken on the way.  The first block
+// sorts what is left at the end.  Rows without a filter only sum, a step's sum by itself: the token's step is looked
+// up among the sums and read again.  What does not fit (top_k over KEEP_K, a nucleus of thousands) is found with two
+// more readings of the row, which the second-level cache has in part: band_row.  What does not fit there either
+// (thousands of ties) takes a reading for each digit of the cut: general_row.
 #include <cooperative_groups.h>
 
 #include <cfloat>
@@ -31,9 +31,10 @@ namespace lora {
 namespace cg = cooperative_groups;
 
 constexpr int SP_THREADS = 256, SP_WARPS = SP_THREADS / 32;
-constexpr int SP_CLUSTER = 8;                 // blocks of a row at most
+constexpr int SP_CLUSTER = 8, SP_OVER = 8;    // blocks of a row at most; what a block costs besides its steps, in steps
 constexpr int SP_LIST = 2048;                 // entries of a list
-constexpr int KEEP_K = 256, KEEP_P = 256;
+constexpr int KEEP_K = 256, KEEP_P = 128;     // what a list is kept to at most, and where top_p alone asks for one
+constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
 constexpr int SP_MAX_V = 1 << 20;             // steps' sums of a block's row fit its list
 constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
 constexpr double SP_ONE = 70368744177664.0;   // 2^46: the largest weight as a whole number
@@ -60,20 +61,21 @@ struct SampleShared {
     double scan_d[SP_WARPS];
     int32_t n, failed_here;
     uint32_t threshold, best;    // what candidates are not below, and the block's largest so far, as keys
+    uint32_t warp_threshold[SP_WARPS];
     uint32_t key_min, key_max;
     int32_t pick_bin, pick_above, pick_kept;
     uint64_t pick_count, pick_weight, pick_here;
     int32_t found;
     double rest;
     // written by the blocks of the cluster to the first one
-    uint32_t top[SP_CLUSTER];
+    uint32_t top[SP_CLUSTER], cut[SP_CLUSTER];
     int32_t bad[SP_CLUSTER], failed[SP_CLUSTER];
     double sum[SP_CLUSTER], base[SP_CLUSTER];
     int32_t merged;
     // of the first block: what turns the blocks' sums into sums against the largest value
     double scale[SP_CLUSTER];
     // written by the first block to all
-    int32_t general;
+    int32_t general, k_bin, p_first, p_last;
     float row_max;
 };
 
@@ -336,6 +338,29 @@ __device__ void shorten(SampleShared &s, const RowPlan &R) {
     __syncthreads();
 }
 
+// A threshold that `keep` values of the block's at least are not below: its warps each take the largest of every
+// lane so far, of these the (keep / warps)-th, and the lowest of the warps' counts.  It rises with the steps: as
+// many values again pass it in steps 2 .. 3 as in 1, in 4 .. 7 as in 2 .. 3, ..
+__device__ __forceinline__ void warp_threshold(SampleShared &s, const RowPlan &R, float top) {
+    const int lane = threadIdx.x & 31;
+    uint32_t v = top == top ? key_of(top) : 0u;
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j; j >>= 1) {
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
+            v = ((lane & k) == 0) == ((lane & j) == 0) ? max(v, o) : min(v, o);
+        }
+    const uint32_t mine = __shfl_sync(0xffffffffu, v, (R.keep + SP_WARPS - 1) / SP_WARPS - 1);
+    if (lane == 0) s.warp_threshold[threadIdx.x >> 5] = mine;
+}
+__device__ __forceinline__ uint32_t block_threshold(const SampleShared &s) {
+    uint32_t t = 0xffffffffu;              // (where nothing is kept by rank all of them are 0)
+#pragma unroll
+    for (int i = 0; i < SP_WARPS; ++i) t = min(t, *(volatile const uint32_t *)&s.warp_threshold[i]);
+    return max(t, *(volatile const uint32_t *)&s.threshold);
+}
+
 // ---- finding the token ------------------------------------------------------------------------
 __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t token, double logprob) {
     P.token[r] = token;
@@ -346,7 +371,13 @@ __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t
 __device__ bool pick_from_list(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m,
                                double all, int n) {
     const int tid = threadIdx.x;
-    if (R.keep && n > R.keep) {
+    if (R.sums) {
+        // below the highest of the blocks' thresholds the candidates have gaps (among the first k of all they have none)
+        uint32_t cut = 0;
+        for (int i = 0; i < (int)cg::this_cluster().num_blocks(); ++i) cut = max(cut, s.cut[i]);
+        n = leave_from(s, s.merge, n, cut);
+    }
+    if (R.keep && n > 512) {
         uint32_t cut;
         n = cut_list(s, s.merge, n, R.keep, R.keep + 32, cut);
     }
@@ -432,12 +463,12 @@ __device__ bool pick_from_list(SampleShared &s, const SampleParams &P, const Row
     return true;
 }
 
-// The first block, from the sums of the row's steps in s.merge; w(value, index) is the weight of a value again.
+// The first block, from the sums of the row's steps; w(value, index) is the weight of a value again.
 template <bool BF16, typename W>
-__device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, const char *logits, W w) {
+__device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, const char *logits,
+                               const double *sums, W w) {
     constexpr int SEG = Step<BF16>::SEG, PER = SP_LIST / SP_THREADS, MINE = SEG / SP_THREADS;
     const int tid = threadIdx.x;
-    const double *sums = reinterpret_cast<const double *>(s.merge);
     double mine[PER], sum = 0.0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -521,6 +552,232 @@ __device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const Row
         if (seg >= P.segs) { seg = P.segs - 1; step = -1; }
         __syncthreads();
     }
+}
+
+// ---- the band path ----------------------------------------------------------------------------
+// Where the candidates were not enough: how many values and how much weight lie in each 1/64 of a power of two
+// below the largest says in which of these the first k end, and (weights to 2^-17, a little room at both sides)
+// top_p of them.  The row is read once for that and once more for the values of those bands themselves, with the
+// exact weight before them: sorted, they give the cut.  False (the same in the whole cluster) where a band is too
+// wide for a list, or where the exact sums do not confirm it.
+template <bool BF16>
+__device__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
+                         const char *logits) {
+    using S = Step<BF16>;
+    constexpr int PER = SP_BINS / SP_THREADS;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const float m = s.row_max, c64 = (float)(R.c * 64.0);
+    if (!(R.c > 1e-30) || !(fabsf(m) <= FLT_MAX) || P.steps * SP_WARPS > 512 || !(R.k || R.by_p || R.by_min)) return false;
+    auto place = [&](float l) { return fminf((m - l) * c64, (float)(SP_BINS - 1)); };
+    const float last = R.by_min ? fminf((float)(-R.low * 64.0), 1e30f) : INFINITY;
+    uint32_t *const counts = reinterpret_cast<uint32_t *>(s.list), *const weights = counts + SP_BINS;
+    for (int i = tid; i < 2 * SP_BINS; i += SP_THREADS) counts[i] = 0;
+    __syncthreads();
+    S next;
+    auto begin = [&](int it) {
+        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
+        if (it < P.steps && seg < P.segs) next.load(P, logits, seg); else next.nothing();
+        return seg;
+    };
+    begin(0);
+    for (int it = 0; it < P.steps; ++it) {
+        const S x = next;
+        begin(it + 1);
+#pragma unroll 8
+        for (int e = 0; e < S::N; ++e) {
+            const float l = x.value(e), f = place(l);
+            if (!(l > -INFINITY)) continue;
+            const int b = (int)f;
+            if (R.k) atomicAdd(&counts[b], 1u);
+            if (R.by_p && f <= last) atomicAdd(&weights[b], (uint32_t)__float2int_rn(65536.0f * exp2f(((float)b - f) * 0.015625f)));
+        }
+    }
+    cluster.sync();
+    uint64_t before_k = 0;                     // (first block) values in front of the band in which the first k end
+    if (rank == 0) {
+        uint64_t count[PER], counted = 0;
+        double weight[PER], weighed = 0.0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int b = tid * PER + j;
+            count[j] = 0;
+            weight[j] = 0.0;
+            for (int r = 0; r < C; ++r) {
+                const uint32_t *from = cluster.map_shared_rank(counts, r);
+                count[j] += from[b];
+                weight[j] += (double)from[SP_BINS + b];
+            }
+            weight[j] *= exp2(-b / 64.0);
+            counted += count[j];
+            weighed += weight[j];
+        }
+        uint64_t all_counted;
+        double all_weighed;
+        uint64_t at_count = block_before<uint64_t>(counted, s.scan_u, all_counted);
+        const double at_weight = block_before<double>(weighed, s.scan_d, all_weighed);
+        if (tid == 0) {
+            s.k_bin = s.p_first = s.p_last = SP_BINS;
+            s.rest = all_weighed;
+            s.pick_count = 0;
+        }
+        __syncthreads();
+        double run = at_weight;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            if (R.k && at_count < (uint64_t)R.k && at_count + count[j] >= (uint64_t)R.k) {
+                s.k_bin = tid * PER + j;
+                s.pick_count = at_count;
+                s.rest = run + weight[j] * ((double)(R.k - (int64_t)at_count) / (double)count[j]);
+            }
+            at_count += count[j];
+            run += weight[j];
+        }
+        __syncthreads();
+        before_k = s.pick_count;
+        if (R.by_p) {
+            const double near = R.p * s.rest;
+            run = at_weight;
+#pragma unroll
+            for (int j = PER - 1; j >= 0; --j) {
+                double to = at_weight;
+                for (int i = 0; i <= j; ++i) to += weight[i];
+                if (weight[j] > 0.0 && to >= near * (1.0 - 2e-5)) atomicMin(&s.p_first, tid * PER + j);
+                if (weight[j] > 0.0 && to >= near * (1.0 + 2e-5)) atomicMin(&s.p_last, tid * PER + j);
+            }
+        }
+        __syncthreads();
+        const int k_bin = s.k_bin, p_first = R.by_p ? min(s.p_first, k_bin) : k_bin, p_last = R.by_p ? min(s.p_last, k_bin) : k_bin;
+        // the last bin is not one of 1/64 but all the rest, and where nothing reached the sum there is no band
+        const bool none = (R.k && k_bin >= SP_BINS - 1) || (R.by_p && p_last >= SP_BINS - 1);
+        __syncthreads();
+        if (tid < C) {
+            SampleShared &to = *cluster.map_shared_rank(&s, tid);
+            to.k_bin = k_bin;
+            to.p_first = p_first;
+            to.p_last = p_last;
+            to.general = none;
+        }
+        if (tid == 0) s.merged = 0;
+    }
+    cluster.sync();
+    if (s.general) return false;
+    const int k_bin = s.k_bin, p_first = s.p_first, p_last = s.p_last;
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    double *const sums = reinterpret_cast<double *>(s.digit_weight);
+    double between = 0.0;                      // the weight behind the band of top_p and in front of that of the first k
+    begin(0);
+    for (int it = 0; it < P.steps; ++it) {
+        const S x = next;
+        const int32_t seg = begin(it + 1) - C * SP_WARPS;
+        double sum = 0.0;
+#pragma unroll 8
+        for (int e = 0; e < S::N; ++e) {
+            const float l = x.value(e);
+            const int b = (int)place(l);
+            if (!(l > -INFINITY) || b > k_bin) continue;
+            if (b >= p_first && (b <= p_last || b == k_bin)) {
+                put(s, entry_of(l, S::index(seg, e)));
+            } else {
+                const double t = exponent_of(l, m, R.c);
+                if (t >= R.low) (b < p_first ? sum : between) += weight_of(t, s.table);
+            }
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) sums[it * SP_WARPS + warp] = sum;
+    }
+    double block_between;
+    block_before<double>(between, s.scan_d, block_between);
+    const int n = s.n;
+    SampleShared &first = *cluster.map_shared_rank(&s, 0);
+    __syncthreads();
+    if (tid == 0) {
+        s.found = n ? atomicAdd(&first.merged, n) : 0;
+        first.sum[rank] = block_between;
+        first.failed[rank] = n > SP_LIST || s.found + n > SP_LIST;
+    }
+    __syncthreads();
+    for (int i = tid; i < min(n, SP_LIST) && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
+    cluster.sync();
+    if (rank == 0) {
+        bool failed = false;
+        double behind = 0.0;
+        for (int i = 0; i < C; ++i) {
+            failed = failed || s.failed[i];
+            behind += s.sum[i];
+        }
+        double *const all = reinterpret_cast<double *>(s.list);
+        double front = 0.0;
+        for (int g = tid; g < P.segs; g += SP_THREADS) {
+            const int r = g / SP_WARPS % C;
+            front += all[g] = cluster.map_shared_rank(sums, r)[g / (SP_WARPS * C) * SP_WARPS + g % SP_WARPS];
+        }
+        double in_front;
+        block_before<double>(front, s.scan_d, in_front);
+        uint64_t cut = 0;
+        if (!failed) {
+            const int found = s.merged;
+            int size = 32;
+            while (size < found) size <<= 1;
+            for (int i = found + tid; i < size; i += SP_THREADS) s.merge[i] = 0;
+            __syncthreads();
+            sort_entries<true>(s.merge, size);
+            // entries of the bands: those of top_p's first.  How many are in front of the k-th's band?
+            int ahead = 0;
+            for (int i = tid; i < found; i += SP_THREADS) ahead += (int)place(value_of((uint32_t)(s.merge[i] >> 32))) < k_bin;
+            uint64_t in_p;
+            block_before<uint64_t>((uint64_t)ahead, s.scan_u, in_p);
+            constexpr int MOST = SP_LIST / SP_THREADS;
+            const int per = (size + SP_THREADS - 1) / SP_THREADS, at = tid * per;
+            double w[MOST], mine = 0.0, of_p = 0.0;
+#pragma unroll
+            for (int j = 0; j < MOST; ++j) {
+                w[j] = 0.0;
+                const int i = at + j;
+                if (j < per && i < found) {
+                    const float l = value_of((uint32_t)(s.merge[i] >> 32));
+                    const int b = (int)place(l);
+                    const double t = exponent_of(l, m, R.c);
+                    const bool counts_in = b < k_bin || (uint64_t)i - in_p + before_k < (uint64_t)R.k;
+                    if (counts_in && t >= R.low) w[j] = weight_of(t, s.table);
+                    if (b <= p_last) of_p += w[j];
+                }
+                mine += w[j];
+            }
+            double band, p_band;
+            const double ahead_of_me = block_before<double>(mine, s.scan_d, band);
+            block_before<double>(of_p, s.scan_d, p_band);
+            const double need = R.by_p ? R.p * (in_front + band + behind) : INFINITY;
+            if (R.by_p) failed = !((in_front < need || p_first == 0) && in_front + p_band >= need);
+            if (tid == 0) s.pick_here = ~0ull;
+            __syncthreads();
+            double run = in_front + ahead_of_me;
+#pragma unroll
+            for (int j = 0; j < MOST; ++j) {
+                const int i = at + j;
+                if (j < per && i < found && w[j] > 0.0 && (run < need || (i == 0 && p_first == 0))) {
+                    atomicMin(reinterpret_cast<unsigned long long *>(&s.pick_here), (unsigned long long)s.merge[i]);
+                    atomicAdd(&all[index_of(s.merge[i]) / S::SEG], w[j]);
+                }
+                run += w[j];
+            }
+            __syncthreads();
+            // none of the bands: all in front of them
+            cut = s.pick_here != ~0ull ? s.pick_here : found ? s.merge[0] + 1 : 0;
+            __syncthreads();
+        }
+        if (!failed)
+            pick_from_sums<BF16>(s, P, R, row, logits, all, [&](float l, int32_t i) {
+                if (!(l > -INFINITY) || entry_of(l, i) < cut) return 0.0;
+                const double t = exponent_of(l, m, R.c);
+                return t >= R.low ? weight_of(t, s.table) : 0.0;
+            });
+        if (tid < C) cluster.map_shared_rank(&s, tid)->general = failed;
+    }
+    cluster.sync();
+    return !s.general;
 }
 
 // ---- the general path -------------------------------------------------------------------------
@@ -661,7 +918,7 @@ __device__ void general_row(SampleShared &s, cg::cluster_group &cluster, const S
             all[g] = cluster.map_shared_rank(sums, r)[g / (SP_WARPS * C) * SP_WARPS + g % SP_WARPS];
         }
         __syncthreads();
-        pick_from_sums<BF16>(s, P, R, row, logits, w);
+        pick_from_sums<BF16>(s, P, R, row, logits, all, w);
     }
     cluster.sync();
 }
@@ -693,7 +950,7 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
 }
 
 template <bool BF16>
-__global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParams P) {
+__global__ void __launch_bounds__(SP_THREADS, 4) sample_kernel(const SampleParams P) {
     using S = Step<BF16>;
     __shared__ SampleShared s;
     cg::cluster_group cluster = cg::this_cluster();
@@ -716,10 +973,11 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
         s.threshold = key_of(-FLT_MAX);
         s.best = 0;
     }
+    if (tid < SP_WARPS) s.warp_threshold[tid] = 0;
     __syncthreads();
     cluster.barrier_arrive();                 // (s.merged is there before any block adds to it)
     bool list = R.list;
-    float top = -INFINITY;
+    float top = -INFINITY, t = -FLT_MAX;
     double sum = 0.0, base = 0.0, magic = SP_MAGIC;
     float floor_l = -FLT_MAX;
     double *const segs = reinterpret_cast<double *>(s.list);
@@ -736,33 +994,16 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
             step_top = max_or_nan(step_top, vec[v]);
         }
         top = max_or_nan(top, step_top);
-        if (it == 0 && (R.sums || (list && R.keep))) {
-            // the largest of the first steps: what the sums are taken against; the K-th of the vectors' largest is
-            // one that K values at least are not below
-            if (R.sums) {
-                const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
-                if (lane == 0) atomicMax(&s.best, k);
-                __syncthreads();
-                const float b = s.best ? value_of(s.best) : 0.0f;
-                base = rint((double)b * R.c);
-                if (!(fabs(base) < 1e12)) base = 0.0;
-                magic = SP_MAGIC - base;
-                floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
-            }
-            if (list && R.keep) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (vec[v] > -INFINITY) put(s, entry_of(vec[v], 0));
-                __syncthreads();
-                uint32_t cut;
-                cut_list(s, s.list, s.n, R.keep, R.keep + R.keep / 4, cut);
-                __syncthreads();
-                if (tid == 0) {
-                    s.n = 0;
-                    s.threshold = max(s.threshold, cut);
-                }
-                __syncthreads();
-            }
+        if (it == 0 && R.sums) {
+            // what the sums are taken against: the largest of the first steps, as a power of two
+            const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
+            if (lane == 0) atomicMax(&s.best, k);
+            __syncthreads();
+            const float b = s.best ? value_of(s.best) : 0.0f;
+            base = rint((double)b * R.c);
+            if (!(fabs(base) < 1e12)) base = 0.0;
+            magic = SP_MAGIC - base;
+            floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
         }
         if (R.sums) {
 #pragma unroll
@@ -783,29 +1024,19 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
                 }
                 __syncwarp();
             }
-            float t = value_of(s.threshold);
-            uint32_t wait = 0;
-            if (!(step_top < t)) {
-#pragma unroll
-                for (int e = 0; e < S::N; ++e)
-                    if (x.value(e) >= t) wait |= 1u << e;
+            if ((it & (it + 1)) == 0) {          // steps 0, 1, 3, 7, ..
+                if (R.keep) warp_threshold(s, R, top);
+                if (__syncthreads_or(s.n > SP_LIST / 2)) {
+                    shorten(s, R);
+                    list = !s.failed_here;
+                }
+                t = value_of(block_threshold(s));
             }
-            for (;;) {
-                if (wait) {
-#pragma unroll
-                    for (int e = 0; e < S::N; ++e)
-                        if ((wait >> e & 1u) && put(s, entry_of(x.value(e), S::index(seg, e)))) wait &= ~(1u << e);
-                }
-                if (!__syncthreads_or(wait != 0)) break;
-                shorten(s, R);
-                if (s.failed_here) {
-                    list = false;
-                    break;
-                }
-                t = value_of(s.threshold);
+            if (R.by_min) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
+            if (list && !(step_top < t)) {
 #pragma unroll
                 for (int e = 0; e < S::N; ++e)
-                    if (!(x.value(e) >= t)) wait &= ~(1u << e);
+                    if (x.value(e) >= t) put(s, entry_of(x.value(e), S::index(seg, e)));
             }
         }
     }
@@ -816,10 +1047,13 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
     const bool any_nan = __syncthreads_or(nan);
     double block_sum = 0.0;
     if (R.sums && !R.segments) block_before<double>(sum, s.scan_d, block_sum);
-    int n = list ? min(s.n, SP_LIST) : 0;
-    if (list && R.keep && n > R.keep + 32) {
-        uint32_t cut;
-        n = cut_list(s, s.list, n, R.keep, R.keep + 32, cut);
+    int n = 0;
+    if (list) {
+        if (R.keep) warp_threshold(s, R, top);
+        __syncthreads();
+        const bool all_there = s.n <= SP_LIST;
+        n = all_there ? leave_from(s, s.list, s.n, block_threshold(s)) : 0;
+        if (!all_there) list = false;
     }
     cluster.barrier_wait();
     SampleShared &first = *cluster.map_shared_rank(&s, 0);
@@ -827,7 +1061,8 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
         s.found = n ? atomicAdd(&first.merged, n) : 0;
         first.top[rank] = s.best;
         first.bad[rank] = any_nan;
-        first.failed[rank] = s.failed_here || s.found + n > SP_LIST;
+        first.cut[rank] = block_threshold(s);
+        first.failed[rank] = list != R.list || s.found + n > SP_LIST;
         first.sum[rank] = block_sum;
         first.base[rank] = base;
     }
@@ -867,7 +1102,7 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
                             sums[g] = s.scale[r] > 0.0 ? v * s.scale[r] : 0.0;
                         }
                         __syncthreads();
-                        pick_from_sums<BF16>(s, P, R, row, logits,
+                        pick_from_sums<BF16>(s, P, R, row, logits, sums,
                                              [&](float l, int32_t) { return weight_of(exponent_of(l, m, R.c), s.table); });
                     } else {
                         general = !pick_from_list(s, P, R, row, m, all * SP_ONE, s.merged);
@@ -885,7 +1120,7 @@ __global__ void __launch_bounds__(SP_THREADS, 3) sample_kernel(const SampleParam
         }
     }
     cluster.sync();
-    if (s.general) general_row<BF16>(s, cluster, P, R, row, logits);
+    if (s.general && !band_row<BF16>(s, cluster, P, R, row, logits)) general_row<BF16>(s, cluster, P, R, row, logits);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -895,10 +1130,18 @@ template <bool BF16>
 static lora_status_t launch_sample(SampleParams P, int32_t R, cudaStream_t stream) {
     constexpr int SEG = Step<BF16>::SEG;
     P.segs = (P.V + SEG - 1) / SEG;
-    // blocks of a row: so many that the rows fill the GPU, and no more than there are steps for their warps
+    // Blocks of a row: those with which the rounds of blocks that the GPU holds at a time (four on an SM) take the
+    // fewest steps, a block's beginning and end counted as SP_OVER of them.
     int C = 1;
-    while (C < SP_CLUSTER && (int64_t)R * C < 148 * 4 && P.segs >= 2 * C * SP_WARPS) C *= 2;
-    P.steps = (P.segs + C * SP_WARPS - 1) / (C * SP_WARPS);
+    int64_t least = INT64_MAX;
+    for (int c = 1; c <= SP_CLUSTER; c *= 2) {
+        const int64_t steps = (P.segs + c * SP_WARPS - 1) / (c * SP_WARPS), rounds = ((int64_t)R * c + 4 * 148 - 1) / (4 * 148);
+        if (rounds * (steps + SP_OVER) < least) {
+            least = rounds * (steps + SP_OVER);
+            C = c;
+            P.steps = (int32_t)steps;
+        }
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(R * C));
     cfg.blockDim = dim3(SP_THREADS);

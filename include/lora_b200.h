@@ -664,10 +664,9 @@ lora_status_t lora_add_norm(const lora_norm_args_t *args, int32_t T, void *strea
 enum { LORA_LOGITS_BF16 = 0, LORA_LOGITS_FP32 = 1 };
 typedef struct {
     int32_t device;
-    int32_t vocab;                     /* 1 .. 2^20 */
+    int32_t vocab;                     /* 1 .. 2^20 - 8 */
     int32_t logits_type;               /* LORA_LOGITS_BF16 or LORA_LOGITS_FP32 */
-    const void *logits; int64_t ld;    /* dev [R, vocab], ld >= vocab in elements (rows on 16-byte boundaries
-                                          are read fastest) */
+    const void *logits; int64_t ld;    /* dev [R, vocab], ld >= vocab in elements, at any multiple of an element */
     const float *temperature;          /* dev [R] */
     const int32_t *top_k;              /* dev [R] or NULL */
     const float *top_p, *min_p;        /* dev [R] or NULL */

@@ -33,9 +33,10 @@ namespace cg = cooperative_groups;
 constexpr int SP_THREADS = 256, SP_WARPS = SP_THREADS / 32;
 constexpr int SP_CLUSTER = 8, SP_OVER = 8;    // blocks of a row at most; what a block costs besides its steps, in steps
 constexpr int SP_LIST = 2048;                 // entries of a list
+constexpr int SP_STAGES = 3, SP_BLOCKS = 3;   // steps of a warp in shared memory; blocks on an SM
 constexpr int KEEP_K = 256, KEEP_P = 128;     // what a list is kept to at most, and where top_p alone asks for one
 constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
-constexpr int SP_MAX_V = 1 << 20;             // steps' sums of a block's row fit its list
+constexpr int SP_MAX_V = (1 << 20) - 8;       // a row's steps have their sums in a list
 constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
 constexpr double SP_ONE = 70368744177664.0;   // 2^46: the largest weight as a whole number
 constexpr double SP_MAGIC = 105553116266496.0;   // 1.5 * 2^46: sums with it are rounded to 1/64
@@ -44,19 +45,37 @@ struct SampleParams {
     const void *logits;
     int64_t ld;
     int32_t V, segs, steps;      // steps of 2 KB in a row, and of one warp
-    bool aligned;
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t *top_k;
     int32_t *token;
     float *logprob;
 };
 
+// what a row asks for
+struct RowPlan {
+    double c;                    // log2(e) / temperature
+    double low;                  // smallest exponent that min_p keeps, -inf: all
+    float drop;                  // how far below the largest value that is, and a little more
+    float u;
+    double p;
+    int32_t k;                   // 0: all
+    int32_t keep;                // entries that a list is cut to; 0: not by rank
+    bool greedy, by_p, by_min, list, sums, segments;
+};
+
 struct SampleShared {
+    RowPlan plan;
     double table[64 * 16];       // 2^(i / 64), once for each pair of banks
     uint64_t list[SP_LIST];      // candidates; sums of steps; weights
-    uint64_t merge[SP_LIST];     // (first block) the cluster's candidates; sums of all steps
-    uint64_t digit_weight[2][256];
-    uint32_t digit_count[2][256];
+    union {
+        uint4 ring[SP_WARPS][SP_STAGES][4][32];   // steps on their way from memory
+        struct {                                  // when the row has been read:
+            uint64_t merge[SP_LIST];              // (first block) the cluster's candidates; sums of all steps
+            uint64_t digit_weight[2][256];
+            uint32_t digit_count[2][256];
+        };
+    };
+    uint32_t bins[256];
     uint64_t scan_u[SP_WARPS];
     double scan_d[SP_WARPS];
     int32_t n, failed_here;
@@ -77,18 +96,6 @@ struct SampleShared {
     // written by the first block to all
     int32_t general, k_bin, p_first, p_last;
     float row_max;
-};
-
-// what a row asks for
-struct RowPlan {
-    double c;                    // log2(e) / temperature
-    double low;                  // smallest exponent that min_p keeps, -inf: all
-    float drop;                  // how far below the largest value that is, and a little more
-    float u;
-    double p;
-    int32_t k;                   // 0: all
-    int32_t keep;                // entries that a list is cut to; 0: not by rank
-    bool greedy, by_p, by_min, list, sums, segments;
 };
 
 // ---- values, keys -----------------------------------------------------------------------------
@@ -129,47 +136,90 @@ __device__ __forceinline__ uint64_t whole(double w) { return (uint64_t)(w * SP_O
 
 __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
 
+struct SampleRow { const char *base; int32_t off, end; };       // see Step::load
+
 // ---- a step: 64 bytes a lane ------------------------------------------------------------------
 template <bool BF16>
 struct Step {
     static constexpr int VEC = BF16 ? 8 : 4, N = 4 * VEC, SEG = 32 * N;     // values of a vector, a lane, a warp
+    static constexpr uint32_t NOTHING = BF16 ? 0xff80ff80u : 0xff800000u;   // -inf
     uint32_t w[16];
 
-    __device__ __forceinline__ void load(const SampleParams &P, const char *row, int32_t seg) {
+    // Places count from the 16-byte boundary at or before the row's first value, which is place `off`: what a vector
+    // holds besides the row is masked out (its 16 bytes lie in one piece of memory with a value of the row).
+    __device__ __forceinline__ void load(const SampleRow &row, int32_t seg) {
+        const char *from = row.base + (int64_t)seg * 2048 + (threadIdx.x & 31) * 16;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int32_t at = seg * SEG + (v * 32 + (int)(threadIdx.x & 31)) * VEC;
+            uint4 q = make_uint4(NOTHING, NOTHING, NOTHING, NOTHING);
+            if (at < row.end && at + VEC > row.off) q = __ldg(reinterpret_cast<const uint4 *>(from + v * 512));
+            w[4 * v] = q.x; w[4 * v + 1] = q.y; w[4 * v + 2] = q.z; w[4 * v + 3] = q.w;
+        }
+        if (seg * SEG < row.off || (seg + 1) * SEG > row.end) mask(row, seg);
+    }
+    // the same by way of shared memory: a lane's own 64 bytes, asked for ahead
+    static __device__ __forceinline__ void ask(const SampleRow &row, int32_t seg, uint4 (*to)[32]) {
         const int lane = threadIdx.x & 31;
+        const char *from = row.base + (int64_t)seg * 2048 + lane * 16;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int32_t at = seg * SEG + (v * 32 + lane) * VEC;
-            uint32_t x[4];
-            if (P.aligned && at + VEC <= P.V) {
-                const uint4 q = __ldg(reinterpret_cast<const uint4 *>(row + (int64_t)at * (BF16 ? 2 : 4)));
-                x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
-            } else {
+            if (at < row.end && at + VEC > row.off)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&to[v][lane])),
+                             "l"(from + v * 512) : "memory");
+        }
+    }
+    __device__ __forceinline__ void take(const SampleRow &row, int32_t seg, const uint4 (*from)[32]) {
+        const int lane = threadIdx.x & 31;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (BF16) {
-                        const uint16_t *h = reinterpret_cast<const uint16_t *>(row) + at + 2 * j;
-                        x[j] = (at + 2 * j < P.V ? (uint32_t)__ldg(h) : 0xff80u) |
-                               (at + 2 * j + 1 < P.V ? (uint32_t)__ldg(h + 1) : 0xff80u) << 16;
-                    } else {
-                        x[j] = at + j < P.V ? __ldg(reinterpret_cast<const uint32_t *>(row) + at + j) : 0xff800000u;
-                    }
-                }
+        for (int v = 0; v < 4; ++v) {
+            const uint4 q = from[v][lane];
+            w[4 * v] = q.x; w[4 * v + 1] = q.y; w[4 * v + 2] = q.z; w[4 * v + 3] = q.w;
+        }
+        if (seg * SEG < row.off || (seg + 1) * SEG > row.end) mask(row, seg);
+    }
+    __device__ __forceinline__ void mask(const SampleRow &row, int32_t seg) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int32_t at = seg * SEG + (v * 32 + (int)(threadIdx.x & 31)) * VEC;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t lo = at + j * (VEC / 4), hi = lo + VEC / 4 - 1;
+                const bool low = lo >= row.off && lo < row.end, high = hi >= row.off && hi < row.end;
+                uint32_t &x = w[4 * v + j];
+                x = BF16 ? (low ? x & 0xffffu : 0xff80u) | (high ? x & 0xffff0000u : 0xff800000u) : (low ? x : NOTHING);
             }
+        }
+    }
+    // the largest of each vector's values (NaN where there is one)
+    __device__ __forceinline__ void tops(float (&top)[4]) const {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[4 * v + j] = x[j];
+        for (int v = 0; v < 4; ++v) {
+            const uint32_t *x = w + 4 * v;
+            if (BF16) {
+                uint32_t a, b;
+                asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(x[0]), "r"(x[1]));
+                asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(x[2]), "r"(x[3]));
+                asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+                top[v] = max_or_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+            } else {
+                float a;
+                asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(value(4 * v)), "f"(value(4 * v + 1)), "f"(value(4 * v + 2)));
+                top[v] = max_or_nan(a, value(4 * v + 3));
+            }
         }
     }
     __device__ __forceinline__ void nothing() {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = BF16 ? 0xff80ff80u : 0xff800000u;
+        for (int i = 0; i < 16; ++i) w[i] = NOTHING;
     }
     __device__ __forceinline__ float value(int e) const {
         if (BF16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
         return __uint_as_float(w[e]);
     }
-    static __device__ __forceinline__ int32_t index(int32_t seg, int e) {
-        return seg * SEG + (e / VEC * 32 + (int)(threadIdx.x & 31)) * VEC + e % VEC;
+    static __device__ __forceinline__ int32_t index(const SampleRow &row, int32_t seg, int e) {
+        return seg * SEG - row.off + (e / VEC * 32 + (int)(threadIdx.x & 31)) * VEC + e % VEC;
     }
 };
 
@@ -204,7 +254,7 @@ __device__ __forceinline__ I block_before(I v, I *warp_sum, I &total) {
 
 // n entries (a power of two of them, at most SP_LIST) in descending or ascending order.
 template <bool DOWN>
-__device__ void sort_entries(uint64_t *a, int n) {
+__device__ __noinline__ void sort_entries(uint64_t *a, int n) {
     for (int k = 2; k <= n; k <<= 1)
         for (int j = k >> 1; j; j >>= 1) {
             for (int i = threadIdx.x; i < n / 2; i += SP_THREADS) {
@@ -227,7 +277,7 @@ __device__ __forceinline__ bool put(SampleShared &s, uint64_t entry) {
 }
 
 // Leaves the entries whose keys are not below `cut`; returns how many there are.
-__device__ int leave_from(SampleShared &s, uint64_t *a, int n, uint32_t cut) {
+__device__ __noinline__ int leave_from(SampleShared &s, uint64_t *a, int n, uint32_t cut) {
     const int tid = threadIdx.x;
     uint64_t mine[SP_LIST / SP_THREADS];
 #pragma unroll
@@ -249,13 +299,13 @@ __device__ int leave_from(SampleShared &s, uint64_t *a, int n, uint32_t cut) {
 // The K-th is looked for in 256 equal parts of the values' range, then of the part it is in, and so on: any rule
 // that never puts a larger value behind a smaller one is right, so roundings, infinities and ties only make the
 // parts uneven.
-__device__ int cut_list(SampleShared &s, uint64_t *a, int n, int keep, int most, uint32_t &cut) {
+__device__ __noinline__ int cut_list(SampleShared &s, uint64_t *a, int n, int keep, int most, uint32_t &cut) {
     cut = 0;
     if (n < keep) return n;
     const int tid = threadIdx.x, lane = tid & 31;
     uint32_t lo = 0, hi = 0xffffffffu;
     int above = 0, kept = n;
-    uint32_t *bins = s.digit_count[0];
+    uint32_t *bins = s.bins;
     for (int round = 0; round < 8; ++round) {
         __syncthreads();
         if (tid == 0) { s.key_min = 0xffffffffu; s.key_max = 0; }
@@ -324,7 +374,7 @@ __device__ int cut_list(SampleShared &s, uint64_t *a, int n, int keep, int most,
 
 // A full list: cut to what the row keeps by rank, or to what min_p leaves by now.  s.n is its length afterwards;
 // s.failed_here where it is still nearly full.
-__device__ void shorten(SampleShared &s, const RowPlan &R) {
+__device__ __noinline__ void shorten(SampleShared &s, const RowPlan &R) {
     const int tid = threadIdx.x;
     int n = min(s.n, SP_LIST);
     uint32_t cut = s.threshold;
@@ -368,7 +418,7 @@ __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t
 }
 
 // The first block, from the cluster's candidates.  False where they do not hold the whole of what is kept.
-__device__ bool pick_from_list(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m,
+__device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m,
                                double all, int n) {
     const int tid = threadIdx.x;
     if (R.sums) {
@@ -465,7 +515,7 @@ __device__ bool pick_from_list(SampleShared &s, const SampleParams &P, const Row
 
 // The first block, from the sums of the row's steps; w(value, index) is the weight of a value again.
 template <bool BF16, typename W>
-__device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, const char *logits,
+__device__ __noinline__ void pick_from_sums(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, const SampleRow &logits,
                                const double *sums, W w) {
     constexpr int SEG = Step<BF16>::SEG, PER = SP_LIST / SP_THREADS, MINE = SEG / SP_THREADS;
     const int tid = threadIdx.x;
@@ -503,14 +553,15 @@ __device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const Row
     int step = seg < P.segs ? 1 : -1;
     if (step < 0) seg = P.segs - 1;
     for (bool begun = false; seg >= 0;) {
-        const int32_t at = seg * SEG + tid * MINE;
+        const int32_t at = seg * SEG + tid * MINE - logits.off;
         double x[MINE], own = 0.0;
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
             x[j] = 0.0;
-            if (at + j < P.V) {
-                const float l = BF16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(logits) + at + j) << 16)
-                                     : __ldg(reinterpret_cast<const float *>(logits) + at + j);
+            if (at + j >= 0 && at + j < P.V) {
+                const char *from = logits.base + (int64_t)(at + j + logits.off) * (BF16 ? 2 : 4);
+                const float l = BF16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t *>(from)) << 16)
+                                     : __ldg(reinterpret_cast<const float *>(from));
                 x[j] = w(l, at + j);
             }
             own += x[j];
@@ -561,8 +612,8 @@ __device__ void pick_from_sums(SampleShared &s, const SampleParams &P, const Row
 // exact weight before them: sorted, they give the cut.  False (the same in the whole cluster) where a band is too
 // wide for a list, or where the exact sums do not confirm it.
 template <bool BF16>
-__device__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
-                         const char *logits) {
+__device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
+                         const SampleRow &logits) {
     using S = Step<BF16>;
     constexpr int PER = SP_BINS / SP_THREADS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -577,7 +628,7 @@ __device__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const Samp
     S next;
     auto begin = [&](int it) {
         const int32_t seg = (it * C + rank) * SP_WARPS + warp;
-        if (it < P.steps && seg < P.segs) next.load(P, logits, seg); else next.nothing();
+        if (it < P.steps && seg < P.segs) next.load(logits, seg); else next.nothing();
         return seg;
     };
     begin(0);
@@ -678,7 +729,7 @@ __device__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const Samp
             const int b = (int)place(l);
             if (!(l > -INFINITY) || b > k_bin) continue;
             if (b >= p_first && (b <= p_last || b == k_bin)) {
-                put(s, entry_of(l, S::index(seg, e)));
+                put(s, entry_of(l, S::index(logits, seg, e)));
             } else {
                 const double t = exponent_of(l, m, R.c);
                 if (t >= R.low) (b < p_first ? sum : between) += weight_of(t, s.table);
@@ -759,7 +810,7 @@ __device__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const Samp
                 const int i = at + j;
                 if (j < per && i < found && w[j] > 0.0 && (run < need || (i == 0 && p_first == 0))) {
                     atomicMin(reinterpret_cast<unsigned long long *>(&s.pick_here), (unsigned long long)s.merge[i]);
-                    atomicAdd(&all[index_of(s.merge[i]) / S::SEG], w[j]);
+                    atomicAdd(&all[(index_of(s.merge[i]) + logits.off) / S::SEG], w[j]);
                 }
                 run += w[j];
             }
@@ -804,7 +855,7 @@ struct GeneralRow {
 // eight bits at a time: the part of the range, the key's bytes, the index's.  Every block of the cluster calls it.
 template <bool BF16>
 __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const GeneralRow &G,
-                                 const char *logits, SampleCut cut, bool weight, int &turn) {
+                                 const SampleRow &logits, SampleCut cut, bool weight, int &turn) {
     using S = Step<BF16>;
     const int tid = threadIdx.x, warp = tid >> 5;
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -825,11 +876,11 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
             const int32_t seg = (it * C + rank) * SP_WARPS + warp;
             if (seg >= P.segs) break;
             S x;
-            x.load(P, logits, seg);
+            x.load(logits, seg);
 #pragma unroll 4
             for (int e = 0; e < S::N; ++e) {
                 const float l = x.value(e);
-                const int32_t i = S::index(seg, e);
+                const int32_t i = S::index(logits, seg, e);
                 if (!G.inside(l, i, cut)) continue;
                 const int32_t part = G.part_of(l);
                 int digit = part;
@@ -880,8 +931,8 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
 }
 
 template <bool BF16>
-__device__ void general_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
-                            const char *logits) {
+__device__ __noinline__ void general_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
+                            const SampleRow &logits) {
     using S = Step<BF16>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -902,9 +953,9 @@ __device__ void general_row(SampleShared &s, cg::cluster_group &cluster, const S
         double sum = 0.0;
         if (seg < P.segs) {
             S x;
-            x.load(P, logits, seg);
+            x.load(logits, seg);
 #pragma unroll 4
-            for (int e = 0; e < S::N; ++e) sum += w(x.value(e), S::index(seg, e));
+            for (int e = 0; e < S::N; ++e) sum += w(x.value(e), S::index(logits, seg, e));
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -922,6 +973,8 @@ __device__ void general_row(SampleShared &s, cg::cluster_group &cluster, const S
     }
     cluster.sync();
 }
+
+static_assert(SP_BLOCKS * (sizeof(SampleShared) + 1024) <= 233472, "the blocks on an SM share 228 KB");
 
 // ---- the kernel -------------------------------------------------------------------------------
 __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) {
@@ -950,23 +1003,34 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
 }
 
 template <bool BF16>
-__global__ void __launch_bounds__(SP_THREADS, 4) sample_kernel(const SampleParams P) {
+__global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __grid_constant__ SampleParams P) {
     using S = Step<BF16>;
-    __shared__ SampleShared s;
+    extern __shared__ __align__(16) unsigned char sample_smem[];
+    SampleShared &s = *reinterpret_cast<SampleShared *>(sample_smem);
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t row = blockIdx.x / C;
-    const char *logits = reinterpret_cast<const char *>(P.logits) + row * P.ld * (BF16 ? 2 : 4);
-    S next;
+    SampleRow logits;
     {
-        const int32_t seg = rank * SP_WARPS + warp;
-        if (seg < P.segs) next.load(P, logits, seg); else next.nothing();
+        const char *from = reinterpret_cast<const char *>(P.logits) + row * P.ld * (BF16 ? 2 : 4);
+        const int skip = (int)((uintptr_t)from & 15);
+        logits.base = from - skip;
+        logits.off = skip / (BF16 ? 2 : 4);
+        logits.end = logits.off + P.V;
     }
-    const RowPlan R = plan_row(P, row);
+    // The steps of a warp: every C * SP_WARPS-th of the row's.  Two are on their way while one is looked at.
+    auto ask = [&](int it) {
+        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
+        if (it < P.steps) S::ask(logits, seg, s.ring[warp][it % SP_STAGES]);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int it = 0; it < SP_STAGES - 1; ++it) ask(it);
     if (tid < 64) {
         const double e = exp2(tid / 64.0);
         for (int i = 0; i < 16; ++i) s.table[tid * 16 + i] = e;
+    } else if (tid == 64) {
+        s.plan = plan_row(P, row);
     }
     if (tid == 0) {
         s.n = s.failed_here = s.merged = 0;
@@ -975,24 +1039,21 @@ __global__ void __launch_bounds__(SP_THREADS, 4) sample_kernel(const SampleParam
     }
     if (tid < SP_WARPS) s.warp_threshold[tid] = 0;
     __syncthreads();
-    cluster.barrier_arrive();                 // (s.merged is there before any block adds to it)
+    const RowPlan &R = s.plan;
     bool list = R.list;
     float top = -INFINITY, t = -FLT_MAX;
     double sum = 0.0, base = 0.0, magic = SP_MAGIC;
     float floor_l = -FLT_MAX;
     double *const segs = reinterpret_cast<double *>(s.list);
     for (int it = 0; it < P.steps; ++it) {
-        const S x = next;
         const int32_t seg = (it * C + rank) * SP_WARPS + warp;
-        if (it + 1 < P.steps && seg + C * SP_WARPS < P.segs) next.load(P, logits, seg + C * SP_WARPS); else next.nothing();
-        float vec[4], step_top = -INFINITY;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            vec[v] = x.value(v * S::VEC);
-#pragma unroll
-            for (int j = 1; j < S::VEC; ++j) vec[v] = max_or_nan(vec[v], x.value(v * S::VEC + j));
-            step_top = max_or_nan(step_top, vec[v]);
-        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(SP_STAGES - 2) : "memory");
+        S x;
+        x.take(logits, seg, s.ring[warp][it % SP_STAGES]);
+        ask(it + SP_STAGES - 1);
+        float vec[4];
+        x.tops(vec);
+        const float step_top = max_or_nan(max_or_nan(vec[0], vec[1]), max_or_nan(vec[2], vec[3]));
         top = max_or_nan(top, step_top);
         if (it == 0 && R.sums) {
             // what the sums are taken against: the largest of the first steps, as a power of two
@@ -1033,10 +1094,15 @@ __global__ void __launch_bounds__(SP_THREADS, 4) sample_kernel(const SampleParam
                 t = value_of(block_threshold(s));
             }
             if (R.by_min) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
-            if (list && !(step_top < t)) {
+            if (list && step_top >= t) {
 #pragma unroll
-                for (int e = 0; e < S::N; ++e)
-                    if (x.value(e) >= t) put(s, entry_of(x.value(e), S::index(seg, e)));
+                for (int v = 0; v < 4; ++v) {
+                    if (vec[v] >= t) {
+#pragma unroll
+                        for (int e = v * S::VEC; e < (v + 1) * S::VEC; ++e)
+                            if (x.value(e) >= t) put(s, entry_of(x.value(e), S::index(logits, seg, e)));
+                    }
+                }
             }
         }
     }
@@ -1055,7 +1121,7 @@ __global__ void __launch_bounds__(SP_THREADS, 4) sample_kernel(const SampleParam
         n = all_there ? leave_from(s, s.list, s.n, block_threshold(s)) : 0;
         if (!all_there) list = false;
     }
-    cluster.barrier_wait();
+    cluster.sync();                           // (the ring's memory is the candidates' from here on)
     SampleShared &first = *cluster.map_shared_rank(&s, 0);
     if (tid == 0) {
         s.found = n ? atomicAdd(&first.merged, n) : 0;
@@ -1127,15 +1193,22 @@ __global__ void __launch_bounds__(SP_THREADS, 4) sample_kernel(const SampleParam
 // host side
 // ---------------------------------------------------------------------------------------------
 template <bool BF16>
-static lora_status_t launch_sample(SampleParams P, int32_t R, cudaStream_t stream) {
+static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cudaStream_t stream) {
+    static std::atomic<bool> allowed[DEVICE_TABLE];
+    if (device >= DEVICE_TABLE || !allowed[device].load(std::memory_order_relaxed)) {
+        LORA_CUDA_TRY(allow_all_smem(sample_kernel<BF16>, device));
+        if (device < DEVICE_TABLE) allowed[device].store(true, std::memory_order_relaxed);
+    }
     constexpr int SEG = Step<BF16>::SEG;
-    P.segs = (P.V + SEG - 1) / SEG;
-    // Blocks of a row: those with which the rounds of blocks that the GPU holds at a time (four on an SM) take the
+    // (rows that do not begin on 16-byte boundaries have a part of a vector more)
+    const bool even = ((uintptr_t)P.logits | (uint64_t)(P.ld * (BF16 ? 2 : 4))) % 16 == 0;
+    P.segs = (P.V + (even ? 0 : Step<BF16>::VEC - 1) + SEG - 1) / SEG;
+    // Blocks of a row: those with which the rounds of blocks that the GPU holds at a time (SP_BLOCKS on an SM) take the
     // fewest steps, a block's beginning and end counted as SP_OVER of them.
     int C = 1;
     int64_t least = INT64_MAX;
     for (int c = 1; c <= SP_CLUSTER; c *= 2) {
-        const int64_t steps = (P.segs + c * SP_WARPS - 1) / (c * SP_WARPS), rounds = ((int64_t)R * c + 4 * 148 - 1) / (4 * 148);
+        const int64_t steps = (P.segs + c * SP_WARPS - 1) / (c * SP_WARPS), rounds = ((int64_t)R * c + SP_BLOCKS * 148 - 1) / (SP_BLOCKS * 148);
         if (rounds * (steps + SP_OVER) < least) {
             least = rounds * (steps + SP_OVER);
             C = c;
@@ -1145,6 +1218,7 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, cudaStream_t strea
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(R * C));
     cfg.blockDim = dim3(SP_THREADS);
+    cfg.dynamicSmemBytes = sizeof(SampleShared);
     cfg.stream = stream;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -1186,7 +1260,6 @@ extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, 
     P.ld = args->ld;
     P.V = args->vocab;
     P.segs = P.steps = 0;
-    P.aligned = ((uintptr_t)args->logits | (uint64_t)(args->ld * unit)) % 16 == 0;
     P.temperature = args->temperature;
     P.top_p = args->top_p;
     P.min_p = args->min_p;
@@ -1196,5 +1269,6 @@ extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, 
     P.logprob = args->logprob;
     DeviceGuard g(args->device);
     if (!g.ok) return cuda_fail(cudaErrorInvalidDevice);
-    return bf16 ? launch_sample<true>(P, R, (cudaStream_t)stream) : launch_sample<false>(P, R, (cudaStream_t)stream);
+    return bf16 ? launch_sample<true>(P, R, args->device, (cudaStream_t)stream)
+                : launch_sample<false>(P, R, args->device, (cudaStream_t)stream);
 }

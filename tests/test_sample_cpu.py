@@ -14,7 +14,7 @@ BASE = 1 << 24
 
 
 @pytest.mark.parametrize("bad,status", [
-    (dict(vocab=0), 2), (dict(vocab=(1 << 20) + 1), 2), (dict(logits_type=2), 1), (dict(logits_type=-1), 1),
+    (dict(vocab=0), 2), (dict(vocab=(1 << 20) - 7, ld=1 << 20), 2), (dict(logits_type=2), 1), (dict(logits_type=-1), 1),
     (dict(R=-1), 2), (dict(R=(1 << 24) + 1), 2), (dict(ld=999), 2), (dict(logits=None), 1), (dict(temperature=None), 1),
     (dict(uniform=None), 1), (dict(token=None), 1), (dict(logits=BASE + 2), 1), (dict(token=BASE + (1 << 20) + 2), 1),
     (dict(top_k=BASE + 1), 1), (dict(logprob=BASE + (1 << 20)), 1), (dict(token=BASE + 400), 1),

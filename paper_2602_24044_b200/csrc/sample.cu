@@ -31,10 +31,10 @@ namespace lora {
 namespace cg = cooperative_groups;
 
 constexpr int SP_THREADS = 256, SP_WARPS = SP_THREADS / 32;
-constexpr int SP_CLUSTER = 8, SP_OVER = 8;    // blocks of a row at most; what a block costs besides its steps, in steps
+constexpr int SP_CLUSTER = 8;                 // blocks of a row at most
 constexpr int SP_LIST = 2048;                 // entries of a list
-constexpr int SP_STAGES = 3, SP_BLOCKS = 3;   // steps of a warp in shared memory; blocks on an SM
-constexpr int KEEP_K = 256, KEEP_P = 128;     // what a list is kept to at most, and where top_p alone asks for one
+constexpr int SP_STAGES = 4, SP_BLOCKS = 2;   // steps of a warp in shared memory; blocks on an SM
+constexpr int KEEP_K = 256, KEEP_P = 192;     // what a list is kept to at most, and where top_p alone asks for one
 constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
 constexpr int SP_MAX_V = (1 << 20) - 8;       // a row's steps have their sums in a list
 constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
@@ -44,7 +44,7 @@ constexpr double SP_MAGIC = 105553116266496.0;   // 1.5 * 2^46: sums with it are
 struct SampleParams {
     const void *logits;
     int64_t ld;
-    int32_t V, segs, steps;      // steps of 2 KB in a row, and of one warp
+    int32_t R, V, segs, steps;   // rows, their values; steps of 2 KB in a row, and of one warp
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t *top_k;
     int32_t *token;
@@ -67,13 +67,18 @@ struct SampleShared {
     RowPlan plan;
     double table[64 * 16];       // 2^(i / 64), once for each pair of banks
     uint64_t list[SP_LIST];      // candidates; sums of steps; weights
+    uint64_t merge[SP_LIST];     // (first block) the cluster's candidates; sums of all steps
     union {
         uint4 ring[SP_WARPS][SP_STAGES][4][32];   // steps on their way from memory
-        struct {                                  // when the row has been read:
-            uint64_t merge[SP_LIST];              // (first block) the cluster's candidates; sums of all steps
+        struct {                                  // general path
             uint64_t digit_weight[2][256];
             uint32_t digit_count[2][256];
         };
+        struct {                                  // (first block) band path: of the whole row
+            double bin_weight[SP_BINS];
+            uint32_t bin_count[SP_BINS];
+        };
+        double step_sums[SP_LIST];                // (first block) band path: the sums of all steps
     };
     uint32_t bins[256];
     uint64_t scan_u[SP_WARPS];
@@ -96,6 +101,7 @@ struct SampleShared {
     // written by the first block to all
     int32_t general, k_bin, p_first, p_last;
     float row_max;
+    double total;                // of all weights, NaN where the row was not summed
 };
 
 // ---- values, keys -----------------------------------------------------------------------------
@@ -137,6 +143,7 @@ __device__ __forceinline__ uint64_t whole(double w) { return (uint64_t)(w * SP_O
 __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
 
 struct SampleRow { const char *base; int32_t off, end; };       // see Step::load
+
 
 // ---- a step: 64 bytes a lane ------------------------------------------------------------------
 template <bool BF16>
@@ -223,6 +230,36 @@ struct Step {
     }
 };
 
+// A warp's steps of a row: every C * SP_WARPS-th of the row's.  The next ones are on their way while f looks at one.
+template <bool BF16>
+__device__ __forceinline__ void ask_step(SampleShared &s, const SampleParams &P, const SampleRow &row, int C, int rank, int it) {
+    const int warp = threadIdx.x >> 5;
+    if (it < P.steps) Step<BF16>::ask(row, (it * C + rank) * SP_WARPS + warp, s.ring[warp][it % SP_STAGES]);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <bool BF16>
+__device__ __forceinline__ void ask_first_steps(SampleShared &s, const SampleParams &P, const SampleRow &row, int C, int rank) {
+#pragma unroll
+    for (int it = 0; it < SP_STAGES - 1; ++it) ask_step<BF16>(s, P, row, C, rank, it);
+}
+template <bool BF16, typename F>
+__device__ __forceinline__ void read_steps(SampleShared &s, const SampleParams &P, const SampleRow &row, int C, int rank, F f) {
+    const int warp = threadIdx.x >> 5;
+    for (int it = 0; it < P.steps; ++it) {
+        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
+        ask_step<BF16>(s, P, row, C, rank, it + SP_STAGES - 1);     // (where the step before this one was)
+        asm volatile("cp.async.wait_group %0;" ::"n"(SP_STAGES - 1) : "memory");
+        Step<BF16> x;
+        x.take(row, seg, s.ring[warp][it % SP_STAGES]);
+        f(x, seg, it);
+    }
+}
+
+// A cluster of one block needs no more than the block's barrier.
+__device__ __forceinline__ void cluster_sync(cg::cluster_group &cluster, int C) {
+    if (C == 1) __syncthreads(); else cluster.sync();
+}
+
 // ---- block-wide sums --------------------------------------------------------------------------
 // What lies before this thread, and (total) all of it.  Every thread of the block calls it.
 template <typename I>
@@ -252,28 +289,70 @@ __device__ __forceinline__ I block_before(I v, I *warp_sum, I &total) {
     return ahead + before;
 }
 
-// n entries (a power of two of them, at most SP_LIST) in descending or ascending order.
-template <bool DOWN>
-__device__ __noinline__ void sort_entries(uint64_t *a, int n) {
-    for (int k = 2; k <= n; k <<= 1)
-        for (int j = k >> 1; j; j >>= 1) {
-            for (int i = threadIdx.x; i < n / 2; i += SP_THREADS) {
-                const int x = 2 * i - (i & (j - 1)), y = x + j;
-                const uint64_t p = a[x], q = a[y];
-                if (((p < q) == DOWN) == ((x & k) == 0) && p != q) {
-                    a[x] = q;
-                    a[y] = p;
-                }
+// E entries a thread of `warps` warps, n = 32 * warps * E in all, in descending or ascending order (a bitonic
+// network): partners in one thread, by shuffles, and only those of other warps through shared memory.  All threads
+// of the block call it.
+template <bool DOWN, int E>
+__device__ __forceinline__ void sort_blocked(uint64_t *a, int warps) {
+    const int tid = threadIdx.x, n = 32 * warps * E;
+    const bool in = tid < 32 * warps;
+    uint64_t e[E];
+#pragma unroll
+    for (int x = 0; x < E; ++x) e[x] = in ? a[tid * E + x] : 0;
+    for (int k = 2; k <= n; k <<= 1) {
+        for (int j = k >> 1; j >= E; j >>= 1) {
+            const int d = j / E;
+            const bool larger = (((tid * E) & j) == 0) == (((tid * E) & k) == 0);
+            if (d >= 32) {
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < E; ++x) a[tid * E + x] = e[x];
+                __syncthreads();
             }
-            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < E; ++x) {        // (d is the same in the whole block)
+                const uint64_t o = d >= 32 ? a[(tid ^ d) * E + x] : __shfl_xor_sync(0xffffffffu, e[x], d);
+                e[x] = (larger == DOWN) == (e[x] > o) ? e[x] : o;
+            }
         }
+#pragma unroll
+        for (int j = E / 2; j > 0; j >>= 1) {
+            if (j >= k) continue;
+#pragma unroll
+            for (int x = 0; x < E; ++x) {
+                if (x & j) continue;
+                const bool first = (((tid * E + x) & k) == 0) == DOWN;       // the larger one first
+                const uint64_t p = e[x], q = e[x | j];
+                const bool swap = first ? p < q : q < p;
+                e[x] = swap ? q : p;
+                e[x | j] = swap ? p : q;
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < E; ++x)
+        if (in) a[tid * E + x] = e[x];
+    __syncthreads();
+}
+// The entries a[0 .. n), n <= SP_LIST, filled up to the size that is sorted, which is returned.
+template <bool DOWN>
+__device__ __noinline__ int sort_entries(uint64_t *a, int n) {
+    const int size = n <= 64 ? 64 : n <= 256 ? 256 : n <= 512 ? 512 : n <= 1024 ? 1024 : 2048;
+    for (int i = n + (int)threadIdx.x; i < size; i += SP_THREADS) a[i] = DOWN ? 0 : ~0ull;
+    __syncthreads();
+    if (size == 64) sort_blocked<DOWN, 2>(a, 1);
+    else if (size == 256) sort_blocked<DOWN, 1>(a, SP_WARPS);
+    else if (size == 512) sort_blocked<DOWN, 2>(a, SP_WARPS);
+    else if (size == 1024) sort_blocked<DOWN, 4>(a, SP_WARPS);
+    else sort_blocked<DOWN, 8>(a, SP_WARPS);
+    return size;
 }
 
 // ---- the list ---------------------------------------------------------------------------------
-__device__ __forceinline__ bool put(SampleShared &s, uint64_t entry) {
+__device__ __forceinline__ void put(SampleShared &s, uint64_t entry, int most = SP_LIST) {
     const int at = atomicAdd(&s.n, 1);
-    if (at < SP_LIST) s.list[at] = entry;
-    return at < SP_LIST;
+    if (at < most) s.list[at] = entry;
 }
 
 // Leaves the entries whose keys are not below `cut`; returns how many there are.
@@ -373,9 +452,10 @@ __device__ __noinline__ int cut_list(SampleShared &s, uint64_t *a, int n, int ke
 }
 
 // A full list: cut to what the row keeps by rank, or to what min_p leaves by now.  s.n is its length afterwards;
-// s.failed_here where it is still nearly full.
+// s.failed_here where it is still nearly full, or where entries had no place.
 __device__ __noinline__ void shorten(SampleShared &s, const RowPlan &R) {
     const int tid = threadIdx.x;
+    const bool lost = s.n > SP_LIST;
     int n = min(s.n, SP_LIST);
     uint32_t cut = s.threshold;
     if (R.keep) n = cut_list(s, s.list, n, R.keep, SP_LIST / 4, cut);
@@ -383,25 +463,34 @@ __device__ __noinline__ void shorten(SampleShared &s, const RowPlan &R) {
     if (tid == 0) {
         s.n = n;
         s.threshold = max(s.threshold, cut);
-        if (n > SP_LIST * 3 / 4) s.failed_here = 1;
+        if (lost || n > SP_LIST * 3 / 4) s.failed_here = 1;
     }
     __syncthreads();
 }
 
-// A threshold that `keep` values of the block's at least are not below: its warps each take the largest of every
-// lane so far, of these the (keep / warps)-th, and the lowest of the warps' counts.  It rises with the steps: as
-// many values again pass it in steps 2 .. 3 as in 1, in 4 .. 7 as in 2 .. 3, ..
-__device__ __forceinline__ void warp_threshold(SampleShared &s, const RowPlan &R, float top) {
-    const int lane = threadIdx.x & 31;
-    uint32_t v = top == top ? key_of(top) : 0u;
+// A threshold that `keep` values of the block's at least are not below: a lane holds the largest so far of either
+// half of its steps, a warp takes the (keep / warps)-th of its 64, and the lowest of the warps' counts.  It rises with
+// the steps: as many values again pass it in steps 2 .. 3 as in 1, in 4 .. 7 as in 2 .. 3, ..
+__device__ __forceinline__ void warp_threshold(SampleShared &s, const RowPlan &R, float top0, float top1) {
+    const int lane = threadIdx.x & 31, want = (R.keep + SP_WARPS - 1) / SP_WARPS - 1;
+    const uint32_t k0 = top0 == top0 ? key_of(top0) : 0u, k1 = top1 == top1 ? key_of(top1) : 0u;
+    // the 64 in descending order, two neighbours a lane
+    uint32_t a = (lane & 1) ? min(k0, k1) : max(k0, k1), b = (lane & 1) ? max(k0, k1) : min(k0, k1);
 #pragma unroll
-    for (int k = 2; k <= 32; k <<= 1)
+    for (int k = 2; k <= 32; k <<= 1) {
 #pragma unroll
         for (int j = k >> 1; j; j >>= 1) {
-            const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
-            v = ((lane & k) == 0) == ((lane & j) == 0) ? max(v, o) : min(v, o);
+            const uint32_t oa = __shfl_xor_sync(0xffffffffu, a, j), ob = __shfl_xor_sync(0xffffffffu, b, j);
+            const bool larger = ((lane & k) == 0) == ((lane & j) == 0);
+            a = larger ? max(a, oa) : min(a, oa);
+            b = larger ? max(b, ob) : min(b, ob);
         }
-    const uint32_t mine = __shfl_sync(0xffffffffu, v, (R.keep + SP_WARPS - 1) / SP_WARPS - 1);
+        const bool first = (lane & k) == 0;
+        const uint32_t x = max(a, b), y = min(a, b);
+        a = first ? x : y;
+        b = first ? y : x;
+    }
+    const uint32_t mine = __shfl_sync(0xffffffffu, (want & 1) ? b : a, want >> 1);
     if (lane == 0) s.warp_threshold[threadIdx.x >> 5] = mine;
 }
 __device__ __forceinline__ uint32_t block_threshold(const SampleShared &s) {
@@ -418,28 +507,83 @@ __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t
 }
 
 // The first block, from the cluster's candidates.  False where they do not hold the whole of what is kept.
-__device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m,
-                               double all, int n) {
+//
+// Up to a candidate a thread, everything is counted: how many candidates are in front of one and what they weigh says
+// whether it is kept, what the kept ones of lower index weigh whether u falls on it.
+__device__ bool count_candidates(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m, double all,
+                                 int n) {
     const int tid = threadIdx.x;
+    const uint64_t mine = tid < n ? s.merge[tid] : 0;
+    uint64_t w = 0;
+    if (tid < n) {
+        const double t = exponent_of(value_of((uint32_t)(mine >> 32)), m, R.c);
+        if (t >= R.low) w = whole(weight_of(t, s.table));
+    }
+    ulonglong2 *const pair = reinterpret_cast<ulonglong2 *>(s.list);         // n <= SP_THREADS <= SP_LIST / 2
+    pair[tid] = make_ulonglong2(mine, w);
+    __syncthreads();
+    int rank = 0;
+    uint64_t before = 0;
+    if (tid < n) {
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const ulonglong2 o = pair[j];
+            if (o.x > mine) {
+                ++rank;
+                before += o.y;
+            }
+        }
+    }
+    // (what is in front of one of the first k is so too, and has a weight that min_p leaves if this one has)
+    if (R.k && rank >= R.k) w = 0;
+    uint64_t total;
+    block_before<uint64_t>(w, s.scan_u, total);
+    if (R.p < 1.0) {
+        const double need = R.p * (R.sums ? all : (double)total);
+        if (R.sums && (double)total < need) return false;      // (the same in every thread)
+        if (!((double)before < need) && rank > 0) w = 0;
+        block_before<uint64_t>(w, s.scan_u, total);
+    }
+    const uint32_t index = (uint32_t)index_of(mine);
+    pair[tid] = make_ulonglong2(index, w);
+    __syncthreads();
+    if (w) {
+        uint64_t target = (uint64_t)((double)R.u * (double)total);
+        if (target >= total) target = total - 1;
+        before = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const ulonglong2 o = pair[j];
+            if ((uint32_t)o.x < index) before += o.y;
+        }
+        if (before <= target && target < before + w) answer(P, row, (int32_t)index, log((double)w / (double)total));
+    }
+    return true;
+}
+
+__device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m,
+                                            double all, int n) {
+    const int tid = threadIdx.x;
+    if (R.k == 1) {
+        uint64_t best = 0;
+        for (int i = tid; i < n; i += SP_THREADS) best = max(best, s.merge[i]);
+        if (tid == 0) s.pick_here = 0;
+        __syncthreads();
+        if (best) atomicMax(reinterpret_cast<unsigned long long *>(&s.pick_here), (unsigned long long)best);
+        __syncthreads();
+        if (tid == 0) answer(P, row, index_of(s.pick_here), 0.0);
+        return true;
+    }
+    uint32_t cut = 0;
     if (R.sums) {
         // below the highest of the blocks' thresholds the candidates have gaps (among the first k of all they have none)
-        uint32_t cut = 0;
         for (int i = 0; i < (int)cg::this_cluster().num_blocks(); ++i) cut = max(cut, s.cut[i]);
         n = leave_from(s, s.merge, n, cut);
     }
-    if (R.keep && n > 512) {
-        uint32_t cut;
-        n = cut_list(s, s.merge, n, R.keep, R.keep + 32, cut);
-    }
-    int size = 32;
-    while (size < n) size <<= 1;
-    for (int i = n + tid; i < size; i += SP_THREADS) s.merge[i] = 0;
-    __syncthreads();
-    sort_entries<true>(s.merge, size);
-    if (R.k == 1) {
-        if (tid == 0) answer(P, row, index_of(s.merge[0]), 0.0);
-        return true;
-    }
+    if (n > SP_THREADS && R.k && R.keep) n = cut_list(s, s.merge, n, R.keep, SP_THREADS, cut);
+    if (n <= SP_THREADS) return count_candidates(s, P, R, row, m, all, n);
+    // more of them: sorted
+    int size = sort_entries<true>(s.merge, n);
     const int per = (size + SP_THREADS - 1) / SP_THREADS, first = tid * per;
     constexpr int MOST = SP_LIST / SP_THREADS;
     uint64_t w[MOST], sum = 0;
@@ -457,7 +601,7 @@ __device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams 
     uint64_t before = block_before<uint64_t>(sum, s.scan_u, total);
     if (R.p < 1.0) {
         const double need = R.p * (R.sums ? all : (double)total);
-        if (R.sums && (double)total < need) return false;      // (the same in every thread)
+        if (R.sums && (double)total < need) return false;
         sum = 0;
         uint64_t at = before;
 #pragma unroll
@@ -482,17 +626,14 @@ __device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams 
     uint64_t all_kept;
     int at = (int)block_before<uint64_t>((uint64_t)mine, s.scan_u, all_kept);
     const int kept = (int)all_kept;
-    size = 32;
-    while (size < kept) size <<= 1;
 #pragma unroll
     for (int j = 0; j < MOST; ++j)
         if (j < per && w[j]) {
             s.merge[at] = (uint64_t)index[j] << 32 | (uint32_t)at;
             s.list[at++] = w[j];
         }
-    for (int i = kept + tid; i < size; i += SP_THREADS) s.merge[i] = ~0ull;
     __syncthreads();
-    sort_entries<false>(s.merge, size);
+    size = sort_entries<false>(s.merge, kept);
     uint64_t target = (uint64_t)((double)R.u * (double)total);
     if (target >= total) target = total - 1;
     const int per2 = (size + SP_THREADS - 1) / SP_THREADS, first2 = tid * per2;
@@ -503,6 +644,7 @@ __device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams 
     before = block_before<uint64_t>(sum, s.scan_u, whole_sum);
     if (before <= target && target < before + sum)
         for (int j = 0; j < per2; ++j) {
+            if (first2 + j >= kept) break;
             const uint64_t e = s.merge[first2 + j], we = s.list[(uint32_t)e];
             if (target < before + we) {
                 answer(P, row, (int32_t)(e >> 32), log((double)we / (double)total));
@@ -612,95 +754,96 @@ __device__ __noinline__ void pick_from_sums(SampleShared &s, const SampleParams 
 // exact weight before them: sorted, they give the cut.  False (the same in the whole cluster) where a band is too
 // wide for a list, or where the exact sums do not confirm it.
 template <bool BF16>
-__device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R, int64_t row,
-                         const SampleRow &logits) {
+__device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R,
+                                      int64_t row, const SampleRow &logits) {
     using S = Step<BF16>;
-    constexpr int PER = SP_BINS / SP_THREADS;
+    constexpr int PER = SP_BINS / SP_THREADS, MOST_SUMS = 512, MOST_BAND = SP_LIST - MOST_SUMS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const float m = s.row_max, c64 = (float)(R.c * 64.0);
-    if (!(R.c > 1e-30) || !(fabsf(m) <= FLT_MAX) || P.steps * SP_WARPS > 512 || !(R.k || R.by_p || R.by_min)) return false;
+    if (!(R.c > 1e-30) || !(fabsf(m) <= FLT_MAX) || P.steps * SP_WARPS > MOST_SUMS || !(R.k || R.by_p || R.by_min)) return false;
+    // a value's place below the largest, in 1/64 of a power of two; the last bin is all the rest, masked tokens too
     auto place = [&](float l) { return fminf((m - l) * c64, (float)(SP_BINS - 1)); };
     const float last = R.by_min ? fminf((float)(-R.low * 64.0), 1e30f) : INFINITY;
+    const bool by_k = R.k != 0, by_p = R.by_p;
     uint32_t *const counts = reinterpret_cast<uint32_t *>(s.list), *const weights = counts + SP_BINS;
+    ask_first_steps<BF16>(s, P, logits, C, rank);
     for (int i = tid; i < 2 * SP_BINS; i += SP_THREADS) counts[i] = 0;
     __syncthreads();
-    S next;
-    auto begin = [&](int it) {
-        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
-        if (it < P.steps && seg < P.segs) next.load(logits, seg); else next.nothing();
-        return seg;
-    };
-    begin(0);
-    for (int it = 0; it < P.steps; ++it) {
-        const S x = next;
-        begin(it + 1);
-#pragma unroll 8
+    read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t, int) {
+#pragma unroll
         for (int e = 0; e < S::N; ++e) {
-            const float l = x.value(e), f = place(l);
-            if (!(l > -INFINITY)) continue;
+            const float f = place(x.value(e));
             const int b = (int)f;
-            if (R.k) atomicAdd(&counts[b], 1u);
-            if (R.by_p && f <= last) atomicAdd(&weights[b], (uint32_t)__float2int_rn(65536.0f * exp2f(((float)b - f) * 0.015625f)));
+            if (by_k) atomicAdd(&counts[b], 1u);
+            // 2^(-r / 64) of the rest r < 1, to its square
+            const float r = f - (float)b;
+            if (by_p && f <= last)
+                atomicAdd(&weights[b], (uint32_t)__float2int_rn(fmaf(r, fmaf(r, 3.843576f, -709.7827f), 65536.0f)));
         }
+    });
+    cluster_sync(cluster, C);
+    SampleShared &first = *cluster.map_shared_rank(&s, 0);
+    for (int b = rank * (SP_BINS / C) + tid; b < (rank + 1) * (SP_BINS / C); b += SP_THREADS) {
+        uint32_t count = 0;
+        uint64_t weight = 0;
+        for (int r = 0; r < C; ++r) {
+            const uint32_t *from = cluster.map_shared_rank(counts, r);
+            count += from[b];
+            weight += from[SP_BINS + b];
+        }
+        first.bin_count[b] = count;
+        first.bin_weight[b] = (double)weight * power2(-b / 64.0, 1.0, SP_MAGIC, s.table);
     }
-    cluster.sync();
+    cluster_sync(cluster, C);
     uint64_t before_k = 0;                     // (first block) values in front of the band in which the first k end
     if (rank == 0) {
-        uint64_t count[PER], counted = 0;
         double weight[PER], weighed = 0.0;
+        uint64_t counted = 0;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            const int b = tid * PER + j;
-            count[j] = 0;
-            weight[j] = 0.0;
-            for (int r = 0; r < C; ++r) {
-                const uint32_t *from = cluster.map_shared_rank(counts, r);
-                count[j] += from[b];
-                weight[j] += (double)from[SP_BINS + b];
-            }
-            weight[j] *= exp2(-b / 64.0);
-            counted += count[j];
+            counted += s.bin_count[tid * PER + j];
+            weight[j] = s.bin_weight[tid * PER + j];
             weighed += weight[j];
         }
         uint64_t all_counted;
         double all_weighed;
-        uint64_t at_count = block_before<uint64_t>(counted, s.scan_u, all_counted);
-        const double at_weight = block_before<double>(weighed, s.scan_d, all_weighed);
+        uint64_t at = block_before<uint64_t>(counted, s.scan_u, all_counted);
+        const double ahead = block_before<double>(weighed, s.scan_d, all_weighed);
         if (tid == 0) {
             s.k_bin = s.p_first = s.p_last = SP_BINS;
             s.rest = all_weighed;
             s.pick_count = 0;
+            s.merged = 0;
         }
         __syncthreads();
-        double run = at_weight;
+        double run = ahead;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            if (R.k && at_count < (uint64_t)R.k && at_count + count[j] >= (uint64_t)R.k) {
+            const uint64_t count = s.bin_count[tid * PER + j];
+            if (by_k && at < (uint64_t)R.k && at + count >= (uint64_t)R.k) {
                 s.k_bin = tid * PER + j;
-                s.pick_count = at_count;
-                s.rest = run + weight[j] * ((double)(R.k - (int64_t)at_count) / (double)count[j]);
+                s.pick_count = at;
+                s.rest = run + weight[j] * ((double)(R.k - (int64_t)at) / (double)count);
             }
-            at_count += count[j];
+            at += count;
             run += weight[j];
         }
         __syncthreads();
         before_k = s.pick_count;
-        if (R.by_p) {
+        if (by_p) {
             const double near = R.p * s.rest;
-            run = at_weight;
+            run = ahead;
 #pragma unroll
-            for (int j = PER - 1; j >= 0; --j) {
-                double to = at_weight;
-                for (int i = 0; i <= j; ++i) to += weight[i];
-                if (weight[j] > 0.0 && to >= near * (1.0 - 2e-5)) atomicMin(&s.p_first, tid * PER + j);
-                if (weight[j] > 0.0 && to >= near * (1.0 + 2e-5)) atomicMin(&s.p_last, tid * PER + j);
+            for (int j = 0; j < PER; ++j) {
+                run += weight[j];
+                if (weight[j] > 0.0 && run >= near * (1.0 - 2e-5)) atomicMin(&s.p_first, tid * PER + j);
+                if (weight[j] > 0.0 && run >= near * (1.0 + 2e-5)) atomicMin(&s.p_last, tid * PER + j);
             }
         }
         __syncthreads();
-        const int k_bin = s.k_bin, p_first = R.by_p ? min(s.p_first, k_bin) : k_bin, p_last = R.by_p ? min(s.p_last, k_bin) : k_bin;
-        // the last bin is not one of 1/64 but all the rest, and where nothing reached the sum there is no band
-        const bool none = (R.k && k_bin >= SP_BINS - 1) || (R.by_p && p_last >= SP_BINS - 1);
+        const int k_bin = s.k_bin, p_first = by_p ? min(s.p_first, k_bin) : k_bin, p_last = by_p ? min(s.p_last, k_bin) : k_bin;
+        const bool none = (by_k && k_bin >= SP_BINS - 1) || (by_p && p_last >= SP_BINS - 1);
         __syncthreads();
         if (tid < C) {
             SampleShared &to = *cluster.map_shared_rank(&s, tid);
@@ -709,49 +852,45 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
             to.p_last = p_last;
             to.general = none;
         }
-        if (tid == 0) s.merged = 0;
     }
-    cluster.sync();
+    cluster_sync(cluster, C);
     if (s.general) return false;
     const int k_bin = s.k_bin, p_first = s.p_first, p_last = s.p_last;
+    ask_first_steps<BF16>(s, P, logits, C, rank);
     if (tid == 0) s.n = 0;
     __syncthreads();
-    double *const sums = reinterpret_cast<double *>(s.digit_weight);
-    double between = 0.0;                      // the weight behind the band of top_p and in front of that of the first k
-    begin(0);
-    for (int it = 0; it < P.steps; ++it) {
-        const S x = next;
-        const int32_t seg = begin(it + 1) - C * SP_WARPS;
+    double *const sums = reinterpret_cast<double *>(s.list) + MOST_BAND;
+    const bool known = s.total == s.total;     // is the weight of all known?
+    double between = 0.0;                      // else: what is behind top_p's band and in front of that of the first k
+    read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
         double sum = 0.0;
-#pragma unroll 8
+#pragma unroll
         for (int e = 0; e < S::N; ++e) {
             const float l = x.value(e);
             const int b = (int)place(l);
-            if (!(l > -INFINITY) || b > k_bin) continue;
-            if (b >= p_first && (b <= p_last || b == k_bin)) {
-                put(s, entry_of(l, S::index(logits, seg, e)));
-            } else {
+            if (b < p_first || (b > p_last && b < k_bin && !known)) {
                 const double t = exponent_of(l, m, R.c);
                 if (t >= R.low) (b < p_first ? sum : between) += weight_of(t, s.table);
+            } else if (b <= p_last || b == k_bin) {
+                put(s, entry_of(l, S::index(logits, seg, e)), MOST_BAND);
             }
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (lane == 0) sums[it * SP_WARPS + warp] = sum;
-    }
+    });
     double block_between;
     block_before<double>(between, s.scan_d, block_between);
     const int n = s.n;
-    SampleShared &first = *cluster.map_shared_rank(&s, 0);
-    __syncthreads();
+    cluster_sync(cluster, C);                            // (the ring's memory is the candidates' again)
     if (tid == 0) {
         s.found = n ? atomicAdd(&first.merged, n) : 0;
         first.sum[rank] = block_between;
-        first.failed[rank] = n > SP_LIST || s.found + n > SP_LIST;
+        first.failed[rank] = n > MOST_BAND || s.found + n > SP_LIST;
     }
     __syncthreads();
-    for (int i = tid; i < min(n, SP_LIST) && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
-    cluster.sync();
+    for (int i = tid; i < min(n, MOST_BAND) && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
+    cluster_sync(cluster, C);
     if (rank == 0) {
         bool failed = false;
         double behind = 0.0;
@@ -759,7 +898,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
             failed = failed || s.failed[i];
             behind += s.sum[i];
         }
-        double *const all = reinterpret_cast<double *>(s.list);
+        double *const all = s.step_sums;
         double front = 0.0;
         for (int g = tid; g < P.segs; g += SP_THREADS) {
             const int r = g / SP_WARPS % C;
@@ -767,14 +906,9 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
         }
         double in_front;
         block_before<double>(front, s.scan_d, in_front);
-        uint64_t cut = 0;
         if (!failed) {
             const int found = s.merged;
-            int size = 32;
-            while (size < found) size <<= 1;
-            for (int i = found + tid; i < size; i += SP_THREADS) s.merge[i] = 0;
-            __syncthreads();
-            sort_entries<true>(s.merge, size);
+            const int size = sort_entries<true>(s.merge, found);
             // entries of the bands: those of top_p's first.  How many are in front of the k-th's band?
             int ahead = 0;
             for (int i = tid; i < found; i += SP_THREADS) ahead += (int)place(value_of((uint32_t)(s.merge[i] >> 32))) < k_bin;
@@ -800,8 +934,8 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
             double band, p_band;
             const double ahead_of_me = block_before<double>(mine, s.scan_d, band);
             block_before<double>(of_p, s.scan_d, p_band);
-            const double need = R.by_p ? R.p * (in_front + band + behind) : INFINITY;
-            if (R.by_p) failed = !((in_front < need || p_first == 0) && in_front + p_band >= need);
+            const double need = by_p ? R.p * (known ? s.total : in_front + band + behind) : INFINITY;
+            if (by_p) failed = !((in_front < need || p_first == 0) && in_front + p_band >= need);
             if (tid == 0) s.pick_here = ~0ull;
             __syncthreads();
             double run = in_front + ahead_of_me;
@@ -816,18 +950,18 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
             }
             __syncthreads();
             // none of the bands: all in front of them
-            cut = s.pick_here != ~0ull ? s.pick_here : found ? s.merge[0] + 1 : 0;
-            __syncthreads();
+            const uint64_t cut = s.pick_here != ~0ull ? s.pick_here : found ? s.merge[0] + 1 : 0;
+            if (!failed)
+                pick_from_sums<BF16>(s, P, R, row, logits, all, [&](float l, int32_t i) {
+                    if (!(l > -INFINITY) || entry_of(l, i) < cut) return 0.0;
+                    const double t = exponent_of(l, m, R.c);
+                    return t >= R.low ? weight_of(t, s.table) : 0.0;
+                });
         }
-        if (!failed)
-            pick_from_sums<BF16>(s, P, R, row, logits, all, [&](float l, int32_t i) {
-                if (!(l > -INFINITY) || entry_of(l, i) < cut) return 0.0;
-                const double t = exponent_of(l, m, R.c);
-                return t >= R.low ? weight_of(t, s.table) : 0.0;
-            });
+        __syncthreads();
         if (tid < C) cluster.map_shared_rank(&s, tid)->general = failed;
     }
-    cluster.sync();
+    cluster_sync(cluster, C);
     return !s.general;
 }
 
@@ -896,7 +1030,7 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
                               (unsigned long long)whole(weight_of(exponent_of(l, G.m, G.R.c), s.table)));
             }
         }
-        cluster.sync();
+        cluster_sync(cluster, C);
         uint64_t count = 0, sum = 0;
         for (int r = 0; r < C; ++r) {
             count += *cluster.map_shared_rank(digit_count + tid, r);
@@ -961,7 +1095,7 @@ __device__ __noinline__ void general_row(SampleShared &s, cg::cluster_group &clu
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (lane == 0) sums[it * SP_WARPS + warp] = sum;
     }
-    cluster.sync();
+    cluster_sync(cluster, C);
     if (rank == 0) {
         double *all = reinterpret_cast<double *>(s.merge);
         for (int g = threadIdx.x; g < P.segs; g += SP_THREADS) {
@@ -971,7 +1105,7 @@ __device__ __noinline__ void general_row(SampleShared &s, cg::cluster_group &clu
         __syncthreads();
         pick_from_sums<BF16>(s, P, R, row, logits, all, w);
     }
-    cluster.sync();
+    cluster_sync(cluster, C);
 }
 
 static_assert(SP_BLOCKS * (sizeof(SampleShared) + 1024) <= 233472, "the blocks on an SM share 228 KB");
@@ -1003,6 +1137,17 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
 }
 
 template <bool BF16>
+__device__ __forceinline__ SampleRow row_at(const SampleParams &P, int64_t row) {
+    const char *from = reinterpret_cast<const char *>(P.logits) + row * P.ld * (BF16 ? 2 : 4);
+    const int skip = (int)((uintptr_t)from & 15);
+    SampleRow r;
+    r.base = from - skip;
+    r.off = skip / (BF16 ? 2 : 4);
+    r.end = r.off + P.V;
+    return r;
+}
+
+template <bool BF16>
 __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __grid_constant__ SampleParams P) {
     using S = Step<BF16>;
     extern __shared__ __align__(16) unsigned char sample_smem[];
@@ -1010,28 +1155,17 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t row = blockIdx.x / C;
-    SampleRow logits;
-    {
-        const char *from = reinterpret_cast<const char *>(P.logits) + row * P.ld * (BF16 ? 2 : 4);
-        const int skip = (int)((uintptr_t)from & 15);
-        logits.base = from - skip;
-        logits.off = skip / (BF16 ? 2 : 4);
-        logits.end = logits.off + P.V;
-    }
-    // The steps of a warp: every C * SP_WARPS-th of the row's.  Two are on their way while one is looked at.
-    auto ask = [&](int it) {
-        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
-        if (it < P.steps) S::ask(logits, seg, s.ring[warp][it % SP_STAGES]);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    for (int it = 0; it < SP_STAGES - 1; ++it) ask(it);
     if (tid < 64) {
         const double e = exp2(tid / 64.0);
         for (int i = 0; i < 16; ++i) s.table[tid * 16 + i] = e;
-    } else if (tid == 64) {
-        s.plan = plan_row(P, row);
     }
+    // The clusters take the rows in turn; the next row's first steps are asked for before the end of this one's work.
+    const int64_t rows_apart = gridDim.x / C;
+    SampleRow next = row_at<BF16>(P, blockIdx.x / C);
+    ask_first_steps<BF16>(s, P, next, C, rank);
+    for (int64_t row = blockIdx.x / C; row < P.R; row += rows_apart) {
+    const SampleRow logits = next;
+    if (tid == 64) s.plan = plan_row(P, row);
     if (tid == 0) {
         s.n = s.failed_here = s.merged = 0;
         s.threshold = key_of(-FLT_MAX);
@@ -1041,20 +1175,18 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     __syncthreads();
     const RowPlan &R = s.plan;
     bool list = R.list;
-    float top = -INFINITY, t = -FLT_MAX;
+    float top = -INFINITY, top1 = -INFINITY, t = -FLT_MAX;
     double sum = 0.0, base = 0.0, magic = SP_MAGIC;
     float floor_l = -FLT_MAX;
     double *const segs = reinterpret_cast<double *>(s.list);
-    for (int it = 0; it < P.steps; ++it) {
-        const int32_t seg = (it * C + rank) * SP_WARPS + warp;
-        asm volatile("cp.async.wait_group %0;" ::"n"(SP_STAGES - 2) : "memory");
-        S x;
-        x.take(logits, seg, s.ring[warp][it % SP_STAGES]);
-        ask(it + SP_STAGES - 1);
+    read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
         float vec[4];
         x.tops(vec);
-        const float step_top = max_or_nan(max_or_nan(vec[0], vec[1]), max_or_nan(vec[2], vec[3]));
+        const float half = max_or_nan(vec[2], vec[3]);
+        float step_top = max_or_nan(vec[0], vec[1]);
         top = max_or_nan(top, step_top);
+        top1 = max_or_nan(top1, half);
+        step_top = max_or_nan(step_top, half);
         if (it == 0 && R.sums) {
             // what the sums are taken against: the largest of the first steps, as a power of two
             const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
@@ -1086,7 +1218,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 __syncwarp();
             }
             if ((it & (it + 1)) == 0) {          // steps 0, 1, 3, 7, ..
-                if (R.keep) warp_threshold(s, R, top);
+                if (R.keep) warp_threshold(s, R, top, top1);
                 if (__syncthreads_or(s.n > SP_LIST / 2)) {
                     shorten(s, R);
                     list = !s.failed_here;
@@ -1105,23 +1237,33 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 }
             }
         }
+    });
+    if (row + rows_apart < P.R) {
+        next = row_at<BF16>(P, row + rows_apart);
+        ask_first_steps<BF16>(s, P, next, C, rank);
     }
     // to the first block: the largest value, the sum, the candidates
-    const bool nan = top != top;
-    const uint32_t block_top = __reduce_max_sync(0xffffffffu, nan ? 0u : key_of(top));
+    const bool nan = top != top || top1 != top1;
+    const uint32_t block_top = __reduce_max_sync(0xffffffffu, nan ? 0u : key_of(fmaxf(top, top1)));
     if (lane == 0) atomicMax(&s.best, block_top);
     const bool any_nan = __syncthreads_or(nan);
     double block_sum = 0.0;
     if (R.sums && !R.segments) block_before<double>(sum, s.scan_d, block_sum);
     int n = 0;
     if (list) {
-        if (R.keep) warp_threshold(s, R, top);
+        if (R.keep) warp_threshold(s, R, top, top1);
         __syncthreads();
         const bool all_there = s.n <= SP_LIST;
         n = all_there ? leave_from(s, s.list, s.n, block_threshold(s)) : 0;
         if (!all_there) list = false;
+        // the cluster's candidates have to fit
+        if (R.keep && C > 1 && n * C > SP_LIST) {
+            uint32_t cut;
+            n = cut_list(s, s.list, n, R.keep, max(R.keep, SP_LIST / C), cut);
+            if (tid == 0) s.threshold = max(s.threshold, cut);
+        }
     }
-    cluster.sync();                           // (the ring's memory is the candidates' from here on)
+    cluster_sync(cluster, C);                  // (the first block's counts of this row are at zero)
     SampleShared &first = *cluster.map_shared_rank(&s, 0);
     if (tid == 0) {
         s.found = n ? atomicAdd(&first.merged, n) : 0;
@@ -1134,7 +1276,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     }
     __syncthreads();
     for (int i = tid; i < n && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
-    cluster.sync();
+    cluster_sync(cluster, C);
     if (rank == 0) {
         uint32_t best = 0;
         bool bad = false, failed = !R.list && !R.sums;
@@ -1146,36 +1288,37 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
         const float m = value_of(best);
         bad = bad || !(m > -INFINITY);
         bool general = false;
+        double total = NAN;
         if (bad) {
             if (tid == 0) answer(P, row, -1, nan_value());
         } else {
             if (R.sums) {
-                double all = 0.0;
+                bool in_range = true;
                 for (int i = 0; i < C; ++i) {
-                    const double t = (double)value_of(s.top[i]) * R.c, b = s.base[i];
-                    const bool some = value_of(s.top[i]) > -INFINITY;
-                    failed = failed || (some && !(fabs(t - b) < 900.0));
-                    if (tid == i) s.scale[i] = some ? exp2(fma(-(double)m, R.c, b)) : 0.0;
+                    const float l = value_of(s.top[i]);
+                    const double b = s.base[i];
+                    if (l > -INFINITY) in_range = in_range && fabs((double)l * R.c - b) < 900.0;
+                    if (tid == i) s.scale[i] = l > -INFINITY ? exp2(fma(-(double)m, R.c, b)) : 0.0;
                 }
                 __syncthreads();
-                if (!failed) {
-                    for (int i = 0; i < C; ++i) all += s.scale[i] > 0.0 ? s.sum[i] * s.scale[i] : 0.0;
-                    if (R.segments) {
-                        double *const sums = reinterpret_cast<double *>(s.merge);
-                        for (int g = tid; g < P.segs; g += SP_THREADS) {
-                            const int r = g / SP_WARPS % C;
-                            const double v = cluster.map_shared_rank(segs, r)[g / (SP_WARPS * C) * SP_WARPS + g % SP_WARPS];
-                            sums[g] = s.scale[r] > 0.0 ? v * s.scale[r] : 0.0;
-                        }
-                        __syncthreads();
-                        pick_from_sums<BF16>(s, P, R, row, logits, sums,
-                                             [&](float l, int32_t) { return weight_of(exponent_of(l, m, R.c), s.table); });
-                    } else {
-                        general = !pick_from_list(s, P, R, row, m, all * SP_ONE, s.merged);
-                    }
+                failed = failed || !in_range;
+                if (in_range) {
+                    total = 0.0;
+                    for (int i = 0; i < C; ++i) total += s.scale[i] > 0.0 ? s.sum[i] * s.scale[i] : 0.0;
                 }
+            }
+            if (!failed && R.segments) {
+                double *const sums = reinterpret_cast<double *>(s.merge);
+                for (int g = tid; g < P.segs; g += SP_THREADS) {
+                    const int r = g / SP_WARPS % C;
+                    const double v = cluster.map_shared_rank(segs, r)[g / (SP_WARPS * C) * SP_WARPS + g % SP_WARPS];
+                    sums[g] = s.scale[r] > 0.0 ? v * s.scale[r] : 0.0;
+                }
+                __syncthreads();
+                pick_from_sums<BF16>(s, P, R, row, logits, sums,
+                                     [&](float l, int32_t) { return weight_of(exponent_of(l, m, R.c), s.table); });
             } else if (!failed) {
-                general = !pick_from_list(s, P, R, row, m, 0.0, s.merged);
+                general = !pick_from_list(s, P, R, row, m, total * SP_ONE, s.merged);
             }
             general = general || failed;
         }
@@ -1183,10 +1326,19 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
             SampleShared &to = *cluster.map_shared_rank(&s, tid);
             to.general = general;
             to.row_max = m;
+            to.total = total;
         }
     }
-    cluster.sync();
-    if (s.general && !band_row<BF16>(s, cluster, P, R, row, logits)) general_row<BF16>(s, cluster, P, R, row, logits);
+    cluster_sync(cluster, C);
+    if (s.general) {
+        // the next row's steps make room, and are asked for again
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        cluster_sync(cluster, C);
+        if (!band_row<BF16>(s, cluster, P, R, row, logits)) general_row<BF16>(s, cluster, P, R, row, logits);
+        cluster_sync(cluster, C);
+        if (row + rows_apart < P.R) ask_first_steps<BF16>(s, P, next, C, rank);
+    }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1203,20 +1355,15 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     // (rows that do not begin on 16-byte boundaries have a part of a vector more)
     const bool even = ((uintptr_t)P.logits | (uint64_t)(P.ld * (BF16 ? 2 : 4))) % 16 == 0;
     P.segs = (P.V + (even ? 0 : Step<BF16>::VEC - 1) + SEG - 1) / SEG;
-    // Blocks of a row: those with which the rounds of blocks that the GPU holds at a time (SP_BLOCKS on an SM) take the
-    // fewest steps, a block's beginning and end counted as SP_OVER of them.
+    // Blocks of a row: as many as the GPU holds for all rows at a time (SP_BLOCKS on an SM), while each of their
+    // warps has a step.
     int C = 1;
-    int64_t least = INT64_MAX;
-    for (int c = 1; c <= SP_CLUSTER; c *= 2) {
-        const int64_t steps = (P.segs + c * SP_WARPS - 1) / (c * SP_WARPS), rounds = ((int64_t)R * c + SP_BLOCKS * 148 - 1) / (SP_BLOCKS * 148);
-        if (rounds * (steps + SP_OVER) < least) {
-            least = rounds * (steps + SP_OVER);
-            C = c;
-            P.steps = (int32_t)steps;
-        }
-    }
+    while (C < SP_CLUSTER && (((int64_t)R * 2 * C <= SP_BLOCKS * 148 && P.segs > C * SP_WARPS) ||
+                              P.segs > SP_LIST * C)) C *= 2;
+    P.steps = (P.segs + C * SP_WARPS - 1) / (C * SP_WARPS);
+    const int32_t clusters = R < SP_BLOCKS * 148 / C ? R : SP_BLOCKS * 148 / C;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(R * C));
+    cfg.gridDim = dim3((unsigned)(clusters * C));
     cfg.blockDim = dim3(SP_THREADS);
     cfg.dynamicSmemBytes = sizeof(SampleShared);
     cfg.stream = stream;
@@ -1258,6 +1405,7 @@ extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, 
     SampleParams P;
     P.logits = args->logits;
     P.ld = args->ld;
+    P.R = R;
     P.V = args->vocab;
     P.segs = P.steps = 0;
     P.temperature = args->temperature;

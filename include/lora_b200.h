@@ -673,8 +673,14 @@ typedef struct {
     const float *uniform;              /* dev [R], in [0, 1) */
     int32_t *token;                    /* dev [R] */
     float *logprob;                    /* dev [R] or NULL */
+    void *workspace;                   /* dev, 16-byte aligned, or NULL */
+    size_t workspace_bytes;
 } lora_sample_args_t;
-/* No output may overlap anything.  R <= 2^24.  Errors: INVALID_ARG, SHAPE, CUDA. */
+/* The workspace notes rows that take longest (of batches that fill the GPU), so that they can be given more of it
+ * in a second launch; without one they take their time.  It is zeroed by the caller once, before its first use, and
+ * every call leaves it so; calls on one workspace must be ordered on one stream. */
+lora_status_t lora_sample_workspace_bytes(int32_t R, size_t *bytes);
+/* No output may overlap anything.  R <= 2^24.  Errors: INVALID_ARG, SHAPE, BUFFER_TOO_SMALL (workspace), CUDA. */
 lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, void *stream);
 
 #ifdef __cplusplus

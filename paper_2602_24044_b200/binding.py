@@ -36,7 +36,7 @@ EXPORTS = [
     "lora_kv_tables_bytes", "lora_kv_build_tables", "lora_kv_release", "lora_qk_norm_rope",
     "lora_kv_append", "lora_kv_read", "lora_kv_workspace_bytes", "lora_kv_attention",
     "lora_add_norm", "lora_qk_norm_rope_axes", "lora_kv_append_axes", "lora_kv_axis_positions",
-    "lora_sample",
+    "lora_sample", "lora_sample_workspace_bytes",
 ]
 STATIC_SCRATCH_BYTES = 2 * 1024 * 1024
 
@@ -126,8 +126,11 @@ class _SampleArgs(ctypes.Structure):
                 ("logits", ctypes.c_void_p), ("ld", ctypes.c_int64),
                 ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
                 ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("uniform", ctypes.c_void_p),
-                ("token", ctypes.c_void_p), ("logprob", ctypes.c_void_p)]
+                ("token", ctypes.c_void_p), ("logprob", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
     max_tokens = 2 ** 31 - 1
+    own_workspace = None                 # made here: kept for the streams of the calls
+    streams = frozenset()
 
 
 _handle = None
@@ -203,6 +206,7 @@ def _lib():
             "lora_kv_workspace_bytes": [vp, ctypes.POINTER(sz)],
             "lora_kv_attention": [vp, i32, vp, i64, vp, i64, vp, ctypes.c_float, vp, i32, i32, vp, i64,
                                   vp, sz, vp],
+            "lora_sample_workspace_bytes": [i32, ctypes.POINTER(sz)],
             "lora_sample": [ctypes.POINTER(_SampleArgs), i32, vp],
             "lora_add_norm": [ctypes.POINTER(_NormArgs), i32, vp],
             "lora_qk_norm_rope_axes": [ctypes.POINTER(_QkArgs), ctypes.POINTER(_RopeAxes), i32, vp],
@@ -804,12 +808,20 @@ def add_norm(args, T: int, stream=None) -> None:
 LOGITS_BF16, LOGITS_FP32 = 0, 1
 
 
+def sample_workspace_bytes(R: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib().lora_sample_workspace_bytes(int(R), ctypes.byref(out)), "lora_sample_workspace_bytes")
+    return int(out.value)
+
+
 def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None, top_p=None, min_p=None,
-                vocab: Optional[int] = None, ld: Optional[int] = None, logits_type: Optional[int] = None, device: int = 0):
+                vocab: Optional[int] = None, ld: Optional[int] = None, logits_type: Optional[int] = None, workspace=None,
+                workspace_bytes: Optional[int] = None, device: int = 0):
     """The argument block of sample (build it once when the same buffers are used again).  logits: bf16 or fp32
     rows; vocab, their type and leading dimension default to the tensor's.  The others hold one entry a row.  The
     tensors must stay alive while the block is used; it keeps them, and a call for more rows than they hold is
-    refused."""
+    refused.  workspace: made here where token is a tensor and none is given (calls with one block are then to be
+    ordered on one stream, as they share their outputs too)."""
     V = int(logits.shape[-1]) if vocab is None else int(vocab)
     ld = _ld("logits", logits, ld, V)
     kind = "bfloat16" if logits_type == LOGITS_BF16 else "float32"
@@ -832,13 +844,30 @@ def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None
                 raise LoraError(1, "%s (needs its values in a row)" % what)
             most = min(most, have)
     a.max_tokens = most
+    if workspace is None and hasattr(token, "new_zeros") and (top_k, top_p, min_p) != (None, None, None):
+        workspace = a.own_workspace = _zeros(token, sample_workspace_bytes(min(most, 1 << 24)))
+    if workspace is not None:
+        a.workspace = _ptr(workspace)
+        a.workspace_bytes = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
     return a
+
+
+def _zeros(like, nbytes: int):
+    """int32 zeros beside a device tensor, ready for calls on any stream."""
+    import torch
+    t = like.new_zeros((nbytes + 3) // 4)
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(t.device).synchronize()
+    return t
 
 
 def sample(args, R: int, stream=None) -> None:
     """The next tokens of R requests; `args` from sample_args."""
     if R > args.max_tokens:
         _too_many(args, R, "sample")
+    if args.own_workspace is not None and stream is not None and stream not in args.streams and type(stream) is not int:
+        args.own_workspace.record_stream(stream)       # (not given back to the allocator while the call may run)
+        args.streams = args.streams | {stream}
     status = _lib().lora_sample(ctypes.byref(args), R, _stream(stream))
     if status:
         _check(status, "lora_sample")

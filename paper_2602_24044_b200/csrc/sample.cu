@@ -24,6 +24,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "fused_ptx.cuh"
 #include "kv_common.cuh"
 
 namespace lora {
@@ -41,6 +42,15 @@ constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as 
 constexpr double SP_ONE = 70368744177664.0;   // 2^46: the largest weight as a whole number
 constexpr double SP_MAGIC = 105553116266496.0;   // 1.5 * 2^46: sums with it are rounded to 1/64
 
+struct SampleQueue {             // rows for the second launch
+    int32_t count, done, reserved[2];
+    struct Row {
+        int32_t row;
+        float max;
+        double total;
+    } rows[1];
+};
+
 struct SampleParams {
     const void *logits;
     int64_t ld;
@@ -49,6 +59,7 @@ struct SampleParams {
     const int32_t *top_k;
     int32_t *token;
     float *logprob;
+    SampleQueue *queue;          // or NULL
 };
 
 // what a row asks for
@@ -160,7 +171,7 @@ struct Step {
         for (int v = 0; v < 4; ++v) {
             const int32_t at = seg * SEG + (v * 32 + (int)(threadIdx.x & 31)) * VEC;
             uint4 q = make_uint4(NOTHING, NOTHING, NOTHING, NOTHING);
-            if (at < row.end && at + VEC > row.off) q = __ldg(reinterpret_cast<const uint4 *>(from + v * 512));
+            if (at < row.end) q = __ldg(reinterpret_cast<const uint4 *>(from + v * 512));
             w[4 * v] = q.x; w[4 * v + 1] = q.y; w[4 * v + 2] = q.z; w[4 * v + 3] = q.w;
         }
         if (seg * SEG < row.off || (seg + 1) * SEG > row.end) mask(row, seg);
@@ -169,12 +180,16 @@ struct Step {
     static __device__ __forceinline__ void ask(const SampleRow &row, int32_t seg, uint4 (*to)[32]) {
         const int lane = threadIdx.x & 31;
         const char *from = row.base + (int64_t)seg * 2048 + lane * 16;
+        const uint32_t at = (uint32_t)__cvta_generic_to_shared(&to[0][lane]);
+        if ((seg + 1) * SEG <= row.end) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int32_t at = seg * SEG + (v * 32 + lane) * VEC;
-            if (at < row.end && at + VEC > row.off)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&to[v][lane])),
-                             "l"(from + v * 512) : "memory");
+            for (int v = 0; v < 4; ++v)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + v * 512), "l"(from + v * 512) : "memory");
+        } else {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (seg * SEG + (v * 32 + lane) * VEC < row.end)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + v * 512), "l"(from + v * 512) : "memory");
         }
     }
     __device__ __forceinline__ void take(const SampleRow &row, int32_t seg, const uint4 (*from)[32]) {
@@ -289,63 +304,68 @@ __device__ __forceinline__ I block_before(I v, I *warp_sum, I &total) {
     return ahead + before;
 }
 
-// E entries a thread of `warps` warps, n = 32 * warps * E in all, in descending or ascending order (a bitonic
-// network): partners in one thread, by shuffles, and only those of other warps through shared memory.  All threads
-// of the block call it.
+// E entries a thread in descending or ascending order (a bitonic network): partners in one thread, by shuffles, and
+// only those of other warps through shared memory.  All threads of the block call it.
 template <bool DOWN, int E>
-__device__ __forceinline__ void sort_blocked(uint64_t *a, int warps) {
-    const int tid = threadIdx.x, n = 32 * warps * E;
-    const bool in = tid < 32 * warps;
+__device__ __forceinline__ void sort_blocked(uint64_t *a) {
+    const int tid = threadIdx.x;
     uint64_t e[E];
 #pragma unroll
-    for (int x = 0; x < E; ++x) e[x] = in ? a[tid * E + x] : 0;
-    for (int k = 2; k <= n; k <<= 1) {
-        for (int j = k >> 1; j >= E; j >>= 1) {
-            const int d = j / E;
-            const bool larger = (((tid * E) & j) == 0) == (((tid * E) & k) == 0);
+    for (int x = 0; x < E; ++x) e[x] = a[tid * E + x];
+#pragma unroll (E == 1 ? 16 : 1)
+    for (int k = 2; k <= SP_THREADS * E; k <<= 1) {
+#pragma unroll (E == 1 ? 16 : 1)
+        for (int d = k / (2 * E); d > 0; d >>= 1) {
+            // the larger entry stays in the lower thread of a descending run
+            const bool larger = (((tid & d) == 0) == (((tid * E) & k) == 0)) == DOWN;
             if (d >= 32) {
                 __syncthreads();
 #pragma unroll
                 for (int x = 0; x < E; ++x) a[tid * E + x] = e[x];
                 __syncthreads();
-            }
 #pragma unroll
-            for (int x = 0; x < E; ++x) {        // (d is the same in the whole block)
-                const uint64_t o = d >= 32 ? a[(tid ^ d) * E + x] : __shfl_xor_sync(0xffffffffu, e[x], d);
-                e[x] = (larger == DOWN) == (e[x] > o) ? e[x] : o;
+                for (int x = 0; x < E; ++x) {
+                    const uint64_t o = a[(tid ^ d) * E + x];
+                    e[x] = (e[x] > o) == larger ? e[x] : o;
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < E; ++x) {
+                    const uint64_t o = __shfl_xor_sync(0xffffffffu, e[x], d);
+                    e[x] = (e[x] > o) == larger ? e[x] : o;
+                }
             }
         }
 #pragma unroll
         for (int j = E / 2; j > 0; j >>= 1) {
-            if (j >= k) continue;
+            if (j < k) {
 #pragma unroll
-            for (int x = 0; x < E; ++x) {
-                if (x & j) continue;
-                const bool first = (((tid * E + x) & k) == 0) == DOWN;       // the larger one first
-                const uint64_t p = e[x], q = e[x | j];
-                const bool swap = first ? p < q : q < p;
-                e[x] = swap ? q : p;
-                e[x | j] = swap ? p : q;
+                for (int x = 0; x < E; ++x) {
+                    if (x & j) continue;
+                    const bool first = (((tid * E + x) & k) == 0) == DOWN;       // the larger one first
+                    const uint64_t p = e[x], q = e[x | j];
+                    const bool swap = (p < q) == first;
+                    e[x] = swap ? q : p;
+                    e[x | j] = swap ? p : q;
+                }
             }
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int x = 0; x < E; ++x)
-        if (in) a[tid * E + x] = e[x];
+    for (int x = 0; x < E; ++x) a[tid * E + x] = e[x];
     __syncthreads();
 }
 // The entries a[0 .. n), n <= SP_LIST, filled up to the size that is sorted, which is returned.
 template <bool DOWN>
 __device__ __noinline__ int sort_entries(uint64_t *a, int n) {
-    const int size = n <= 64 ? 64 : n <= 256 ? 256 : n <= 512 ? 512 : n <= 1024 ? 1024 : 2048;
+    const int size = n <= 256 ? 256 : n <= 512 ? 512 : n <= 1024 ? 1024 : 2048;
     for (int i = n + (int)threadIdx.x; i < size; i += SP_THREADS) a[i] = DOWN ? 0 : ~0ull;
     __syncthreads();
-    if (size == 64) sort_blocked<DOWN, 2>(a, 1);
-    else if (size == 256) sort_blocked<DOWN, 1>(a, SP_WARPS);
-    else if (size == 512) sort_blocked<DOWN, 2>(a, SP_WARPS);
-    else if (size == 1024) sort_blocked<DOWN, 4>(a, SP_WARPS);
-    else sort_blocked<DOWN, 8>(a, SP_WARPS);
+    if (size == 256) sort_blocked<DOWN, 1>(a);
+    else if (size == 512) sort_blocked<DOWN, 2>(a);
+    else if (size == 1024) sort_blocked<DOWN, 4>(a);
+    else sort_blocked<DOWN, 8>(a);
     return size;
 }
 
@@ -451,23 +471,6 @@ __device__ __noinline__ int cut_list(SampleShared &s, uint64_t *a, int n, int ke
     return leave_from(s, a, n, cut);
 }
 
-// A full list: cut to what the row keeps by rank, or to what min_p leaves by now.  s.n is its length afterwards;
-// s.failed_here where it is still nearly full, or where entries had no place.
-__device__ __noinline__ void shorten(SampleShared &s, const RowPlan &R) {
-    const int tid = threadIdx.x;
-    const bool lost = s.n > SP_LIST;
-    int n = min(s.n, SP_LIST);
-    uint32_t cut = s.threshold;
-    if (R.keep) n = cut_list(s, s.list, n, R.keep, SP_LIST / 4, cut);
-    else n = leave_from(s, s.list, n, cut);
-    if (tid == 0) {
-        s.n = n;
-        s.threshold = max(s.threshold, cut);
-        if (lost || n > SP_LIST * 3 / 4) s.failed_here = 1;
-    }
-    __syncthreads();
-}
-
 // A threshold that `keep` values of the block's at least are not below: a lane holds the largest so far of either
 // half of its steps, a warp takes the (keep / warps)-th of its 64, and the lowest of the warps' counts.  It rises with
 // the steps: as many values again pass it in steps 2 .. 3 as in 1, in 4 .. 7 as in 2 .. 3, ..
@@ -500,6 +503,48 @@ __device__ __forceinline__ uint32_t block_threshold(const SampleShared &s) {
     return max(t, *(volatile const uint32_t *)&s.threshold);
 }
 
+// The values of a step that are not below t: a lane takes its places at once.
+template <bool BF16>
+__device__ __forceinline__ void put_step(SampleShared &s, const SampleRow &row, const Step<BF16> &x, const float (&vec)[4],
+                                         int32_t seg, float t) {
+    using S = Step<BF16>;
+    uint32_t in = 0;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        if (vec[v] >= t) {
+#pragma unroll
+            for (int e = v * S::VEC; e < (v + 1) * S::VEC; ++e) in |= x.value(e) >= t ? 1u << e : 0u;
+        }
+    }
+    int at = atomicAdd(&s.n, __popc(in));
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        if (in >> (v * S::VEC) & ((1u << S::VEC) - 1u)) {
+#pragma unroll
+            for (int e = v * S::VEC; e < (v + 1) * S::VEC; ++e)
+                if (in >> e & 1u) {
+                    if (at < SP_LIST) s.list[at] = entry_of(x.value(e), S::index(row, seg, e));
+                    ++at;
+                }
+        }
+    }
+}
+
+// A list that fills up: what the threshold as it is now leaves of it, or (by rank) the best ones.  s.n is its length
+// afterwards; s.failed_here where it is still nearly full, or where entries had no place.
+__device__ __noinline__ void shorten(SampleShared &s, const RowPlan &R) {
+    const bool lost = s.n > SP_LIST;
+    uint32_t cut = block_threshold(s);
+    int n = leave_from(s, s.list, min(s.n, SP_LIST), cut);
+    if (R.keep && n > SP_LIST / 2) n = cut_list(s, s.list, n, R.keep, SP_LIST / 4, cut);
+    if (threadIdx.x == 0) {
+        s.n = n;
+        s.threshold = max(s.threshold, cut);
+        if (lost || n > SP_LIST * 3 / 4) s.failed_here = 1;
+    }
+    __syncthreads();
+}
+
 // ---- finding the token ------------------------------------------------------------------------
 __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t token, double logprob) {
     P.token[r] = token;
@@ -508,56 +553,58 @@ __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t
 
 // The first block, from the cluster's candidates.  False where they do not hold the whole of what is kept.
 //
-// Up to a candidate a thread, everything is counted: how many candidates are in front of one and what they weigh says
-// whether it is kept, what the kept ones of lower index weigh whether u falls on it.
+// Up to half a block of candidates, everything is counted: how many candidates are in front of one and what they weigh
+// says whether it is kept, what the kept ones of lower index weigh whether u falls on it.  2, 4 or 8 threads (a
+// power of two of neighbours) count for one candidate.
 __device__ bool count_candidates(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m, double all,
                                  int n) {
-    const int tid = threadIdx.x;
-    const uint64_t mine = tid < n ? s.merge[tid] : 0;
+    const int tid = threadIdx.x, log_g = n <= 32 ? 3 : n <= 64 ? 2 : 1, g = 1 << log_g, part = tid & (g - 1), me = tid >> log_g;
+    ulonglong2 *const pair = reinterpret_cast<ulonglong2 *>(s.list);         // n <= SP_THREADS / 2
+    const uint64_t mine = me < n ? s.merge[me] : 0;
     uint64_t w = 0;
-    if (tid < n) {
+    if (me < n) {
         const double t = exponent_of(value_of((uint32_t)(mine >> 32)), m, R.c);
         if (t >= R.low) w = whole(weight_of(t, s.table));
     }
-    ulonglong2 *const pair = reinterpret_cast<ulonglong2 *>(s.list);         // n <= SP_THREADS <= SP_LIST / 2
-    pair[tid] = make_ulonglong2(mine, w);
+    if (part == 0) pair[me] = make_ulonglong2(mine, w);
     __syncthreads();
     int rank = 0;
     uint64_t before = 0;
-    if (tid < n) {
-#pragma unroll 8
-        for (int j = 0; j < n; ++j) {
-            const ulonglong2 o = pair[j];
-            if (o.x > mine) {
-                ++rank;
-                before += o.y;
-            }
+#pragma unroll 4
+    for (int j = part; j < n; j += g) {
+        const ulonglong2 o = pair[j];
+        if (o.x > mine) {
+            ++rank;
+            before += o.y;
         }
+    }
+    for (int d = 1; d < g; d <<= 1) {
+        rank += __shfl_xor_sync(0xffffffffu, rank, d);
+        before += __shfl_xor_sync(0xffffffffu, before, d);
     }
     // (what is in front of one of the first k is so too, and has a weight that min_p leaves if this one has)
     if (R.k && rank >= R.k) w = 0;
     uint64_t total;
-    block_before<uint64_t>(w, s.scan_u, total);
+    block_before<uint64_t>(part ? 0 : w, s.scan_u, total);
     if (R.p < 1.0) {
         const double need = R.p * (R.sums ? all : (double)total);
-        if (R.sums && (double)total < need) return false;      // (the same in every thread)
         if (!((double)before < need) && rank > 0) w = 0;
-        block_before<uint64_t>(w, s.scan_u, total);
+        block_before<uint64_t>(part ? 0 : w, s.scan_u, total);
     }
     const uint32_t index = (uint32_t)index_of(mine);
-    pair[tid] = make_ulonglong2(index, w);
+    if (part == 0) pair[me] = make_ulonglong2(index, w);
     __syncthreads();
-    if (w) {
-        uint64_t target = (uint64_t)((double)R.u * (double)total);
-        if (target >= total) target = total - 1;
-        before = 0;
-#pragma unroll 8
-        for (int j = 0; j < n; ++j) {
-            const ulonglong2 o = pair[j];
-            if ((uint32_t)o.x < index) before += o.y;
-        }
-        if (before <= target && target < before + w) answer(P, row, (int32_t)index, log((double)w / (double)total));
+    before = 0;
+#pragma unroll 4
+    for (int j = part; j < n; j += g) {
+        const ulonglong2 o = pair[j];
+        if ((uint32_t)o.x < index) before += o.y;
     }
+    for (int d = 1; d < g; d <<= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
+    uint64_t target = (uint64_t)((double)R.u * (double)total);
+    if (target >= total) target = total - 1;
+    if (part == 0 && w && before <= target && target < before + w)
+        answer(P, row, (int32_t)index, log((double)w / (double)total));
     return true;
 }
 
@@ -579,9 +626,15 @@ __device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams 
         // below the highest of the blocks' thresholds the candidates have gaps (among the first k of all they have none)
         for (int i = 0; i < (int)cg::this_cluster().num_blocks(); ++i) cut = max(cut, s.cut[i]);
         n = leave_from(s, s.merge, n, cut);
+        // do they reach top_p of all?
+        uint64_t sum = 0, reach;
+        for (int i = tid; i < n; i += SP_THREADS)
+            sum += whole(weight_of(exponent_of(value_of((uint32_t)(s.merge[i] >> 32)), m, R.c), s.table));
+        block_before<uint64_t>(sum, s.scan_u, reach);
+        if ((double)reach < R.p * all) return false;
     }
     if (n > SP_THREADS && R.k && R.keep) n = cut_list(s, s.merge, n, R.keep, SP_THREADS, cut);
-    if (n <= SP_THREADS) return count_candidates(s, P, R, row, m, all, n);
+    if (n <= SP_THREADS / 2) return count_candidates(s, P, R, row, m, all, n);
     // more of them: sorted
     int size = sort_entries<true>(s.merge, n);
     const int per = (size + SP_THREADS - 1) / SP_THREADS, first = tid * per;
@@ -601,7 +654,6 @@ __device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams 
     uint64_t before = block_before<uint64_t>(sum, s.scan_u, total);
     if (R.p < 1.0) {
         const double need = R.p * (R.sums ? all : (double)total);
-        if (R.sums && (double)total < need) return false;
         sum = 0;
         uint64_t at = before;
 #pragma unroll
@@ -861,24 +913,36 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     __syncthreads();
     double *const sums = reinterpret_cast<double *>(s.list) + MOST_BAND;
     const bool known = s.total == s.total;     // is the weight of all known?
+    // weights as in the first reading: against the power of two next to the largest, turned into weights against it at
+    // the end (what min_p leaves is decided by the exact exponent)
+    const double base = rint((double)m * R.c), magic = SP_MAGIC - base, turn = exp2(fma(-(double)m, R.c, base));
+    const float floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
+    const bool far = !(fabs(base) < 1e12), by_min = R.by_min;
     double between = 0.0;                      // else: what is behind top_p's band and in front of that of the first k
     read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
-        double sum = 0.0;
+        double sum = 0.0, rest = 0.0;
+        uint32_t in_band = 0;
 #pragma unroll
         for (int e = 0; e < S::N; ++e) {
             const float l = x.value(e);
             const int b = (int)place(l);
-            if (b < p_first || (b > p_last && b < k_bin && !known)) {
-                const double t = exponent_of(l, m, R.c);
-                if (t >= R.low) (b < p_first ? sum : between) += weight_of(t, s.table);
-            } else if (b <= p_last || b == k_bin) {
-                put(s, entry_of(l, S::index(logits, seg, e)), MOST_BAND);
-            }
+            double w = power2((double)fmaxf(l, floor_l), R.c, magic, s.table);
+            if (by_min && !(exponent_of(l, m, R.c) >= R.low)) w = 0.0;
+            sum += b < p_first ? w : 0.0;
+            if (!known) rest += b > p_last && b < k_bin ? w : 0.0;
+            if (b >= p_first && (b <= p_last || b == k_bin)) in_band |= 1u << e;
+        }
+        between += rest;
+        if (in_band) {
+#pragma unroll
+            for (int e = 0; e < S::N; ++e)
+                if (in_band >> e & 1u) put(s, entry_of(x.value(e), S::index(logits, seg, e)), MOST_BAND);
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (lane == 0) sums[it * SP_WARPS + warp] = sum;
+        if (lane == 0) sums[it * SP_WARPS + warp] = sum * turn;
     });
+    between *= turn;
     double block_between;
     block_before<double>(between, s.scan_d, block_between);
     const int n = s.n;
@@ -886,7 +950,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     if (tid == 0) {
         s.found = n ? atomicAdd(&first.merged, n) : 0;
         first.sum[rank] = block_between;
-        first.failed[rank] = n > MOST_BAND || s.found + n > SP_LIST;
+        first.failed[rank] = far || n > MOST_BAND || s.found + n > SP_LIST;
     }
     __syncthreads();
     for (int i = tid; i < min(n, MOST_BAND) && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
@@ -1136,6 +1200,12 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
     return R;
 }
 
+__device__ __forceinline__ void fill_table(SampleShared &s) {
+    if (threadIdx.x >= 64) return;
+    const double e = exp2(threadIdx.x / 64.0);
+    for (int i = 0; i < 16; ++i) s.table[threadIdx.x * 16 + i] = e;
+}
+
 template <bool BF16>
 __device__ __forceinline__ SampleRow row_at(const SampleParams &P, int64_t row) {
     const char *from = reinterpret_cast<const char *>(P.logits) + row * P.ld * (BF16 ? 2 : 4);
@@ -1155,10 +1225,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < 64) {
-        const double e = exp2(tid / 64.0);
-        for (int i = 0; i < 16; ++i) s.table[tid * 16 + i] = e;
-    }
+    fill_table(s);
     // The clusters take the rows in turn; the next row's first steps are asked for before the end of this one's work.
     const int64_t rows_apart = gridDim.x / C;
     SampleRow next = row_at<BF16>(P, blockIdx.x / C);
@@ -1174,50 +1241,63 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     if (tid < SP_WARPS) s.warp_threshold[tid] = 0;
     __syncthreads();
     const RowPlan &R = s.plan;
+    const bool sums = R.sums, by_min = R.by_min;
+    const double c = R.c;
     bool list = R.list;
     float top = -INFINITY, top1 = -INFINITY, t = -FLT_MAX;
     double sum = 0.0, base = 0.0, magic = SP_MAGIC;
     float floor_l = -FLT_MAX;
     double *const segs = reinterpret_cast<double *>(s.list);
-    read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
-        float vec[4];
-        x.tops(vec);
-        const float half = max_or_nan(vec[2], vec[3]);
-        float step_top = max_or_nan(vec[0], vec[1]);
-        top = max_or_nan(top, step_top);
-        top1 = max_or_nan(top1, half);
-        step_top = max_or_nan(step_top, half);
-        if (it == 0 && R.sums) {
-            // what the sums are taken against: the largest of the first steps, as a power of two
-            const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
-            if (lane == 0) atomicMax(&s.best, k);
-            __syncthreads();
-            const float b = s.best ? value_of(s.best) : 0.0f;
-            base = rint((double)b * R.c);
-            if (!(fabs(base) < 1e12)) base = 0.0;
-            magic = SP_MAGIC - base;
-            floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
-        }
-        if (R.sums) {
+    // What sums are taken against: the largest of the first steps, as a power of two.
+    auto set_base = [&](float step_top) {
+        const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
+        if (lane == 0) atomicMax(&s.best, k);
+        __syncthreads();
+        const float b = s.best ? value_of(s.best) : 0.0f;
+        base = rint((double)b * c);
+        if (!(fabs(base) < 1e12)) base = 0.0;
+        magic = SP_MAGIC - base;
+        floor_l = (float)fmax((base - 1000.0) / c, -(double)FLT_MAX);
+    };
+    if (R.segments)
+        read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t, int it) {
+            float vec[4];
+            x.tops(vec);
+            const float step_top = max_or_nan(max_or_nan(vec[0], vec[1]), max_or_nan(vec[2], vec[3]));
+            top = max_or_nan(top, step_top);
+            if (it == 0) set_base(step_top);
+            double w = 0.0;
 #pragma unroll
-            for (int e = 0; e < S::N; ++e) sum += power2((double)fmaxf(x.value(e), floor_l), R.c, magic, s.table);
-            if (R.segments) {
+            for (int e = 0; e < S::N; ++e) w += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
 #pragma unroll
-                for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                if (lane == 0) segs[it * SP_WARPS + warp] = sum;
-                sum = 0.0;
+            for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
+            if (lane == 0) segs[it * SP_WARPS + warp] = w;
+        });
+    else
+        read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
+            float vec[4];
+            x.tops(vec);
+            const float half = max_or_nan(vec[2], vec[3]);
+            float step_top = max_or_nan(vec[0], vec[1]);
+            top = max_or_nan(top, step_top);
+            top1 = max_or_nan(top1, half);
+            step_top = max_or_nan(step_top, half);
+            if (sums) {
+                if (it == 0) set_base(step_top);
+#pragma unroll
+                for (int e = 0; e < S::N; ++e) sum += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
             }
-        }
-        if (list) {
-            if (R.by_min) {
+            if (!list) return;
+            if (by_min) {
                 const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
                 if (lane == 0 && k > s.best && atomicMax(&s.best, k) < k) {
-                    const float m = value_of(k), t = (m - R.drop) - fabsf(m) * 1e-5f;
-                    if (t > -FLT_MAX) atomicMax(&s.threshold, key_of(t));
+                    const float m = value_of(k), least = (m - R.drop) - fabsf(m) * 1e-5f;
+                    if (least > -FLT_MAX) atomicMax(&s.threshold, key_of(least));
                 }
                 __syncwarp();
             }
-            if ((it & (it + 1)) == 0) {          // steps 0, 1, 3, 7, ..
+            const int n = it + 1, low = n & -n;
+            if (n == low || n == 3 * low) {      // behind 1, 2, 3, 4, 6, 8, 12, 16, .. steps
                 if (R.keep) warp_threshold(s, R, top, top1);
                 if (__syncthreads_or(s.n > SP_LIST / 2)) {
                     shorten(s, R);
@@ -1225,19 +1305,9 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 }
                 t = value_of(block_threshold(s));
             }
-            if (R.by_min) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
-            if (list && step_top >= t) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    if (vec[v] >= t) {
-#pragma unroll
-                        for (int e = v * S::VEC; e < (v + 1) * S::VEC; ++e)
-                            if (x.value(e) >= t) put(s, entry_of(x.value(e), S::index(logits, seg, e)));
-                    }
-                }
-            }
-        }
-    });
+            if (by_min) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
+            if (list && step_top >= t) put_step<BF16>(s, logits, x, vec, seg, t);
+        });
     if (row + rows_apart < P.R) {
         next = row_at<BF16>(P, row + rows_apart);
         ask_first_steps<BF16>(s, P, next, C, rank);
@@ -1330,7 +1400,12 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
         }
     }
     cluster_sync(cluster, C);
-    if (s.general) {
+    if (s.general && P.queue) {
+        if (rank == 0 && tid == 0) {
+            const int at = atomicAdd(&P.queue->count, 1);
+            if (at < P.R) P.queue->rows[at] = {(int32_t)row, s.row_max, s.total};
+        }
+    } else if (s.general) {
         // the next row's steps make room, and are asked for again
         asm volatile("cp.async.wait_all;" ::: "memory");
         cluster_sync(cluster, C);
@@ -1338,6 +1413,36 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
         cluster_sync(cluster, C);
         if (row + rows_apart < P.R) ask_first_steps<BF16>(s, P, next, C, rank);
     }
+    }
+}
+
+// The rows that the first launch left over, eight blocks each: few as a rule, so that their time is one row's.
+template <bool BF16>
+__global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(const __grid_constant__ SampleParams P) {
+    extern __shared__ __align__(16) unsigned char sample_smem[];
+    SampleShared &s = *reinterpret_cast<SampleShared *>(sample_smem);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x;
+    fill_table(s);
+    griddep_wait();
+    const int rows = min(*(volatile int32_t *)&P.queue->count, P.R);
+    for (int i = blockIdx.x / C; i < rows; i += gridDim.x / C) {
+        const SampleQueue::Row &r = P.queue->rows[i];
+        const int32_t row = r.row;
+        if (row < 0 || row >= P.R) continue;           // (the caller's memory)
+        if (tid == 64) s.plan = plan_row(P, row);
+        if (tid == 0) {
+            s.row_max = r.max;
+            s.total = r.total;
+        }
+        cluster_sync(cluster, C);
+        const SampleRow logits = row_at<BF16>(P, row);
+        if (!band_row<BF16>(s, cluster, P, s.plan, row, logits)) general_row<BF16>(s, cluster, P, s.plan, row, logits);
+        cluster_sync(cluster, C);
+    }
+    if (rank == 0 && tid == 0 && atomicAdd(&P.queue->done, 1) == (int)gridDim.x / C - 1) {     // every cluster has read it
+        P.queue->count = 0;
+        P.queue->done = 0;
     }
 }
 
@@ -1349,6 +1454,7 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     static std::atomic<bool> allowed[DEVICE_TABLE];
     if (device >= DEVICE_TABLE || !allowed[device].load(std::memory_order_relaxed)) {
         LORA_CUDA_TRY(allow_all_smem(sample_kernel<BF16>, device));
+        LORA_CUDA_TRY(allow_all_smem(sample_rest_kernel<BF16>, device));
         if (device < DEVICE_TABLE) allowed[device].store(true, std::memory_order_relaxed);
     }
     constexpr int SEG = Step<BF16>::SEG;
@@ -1362,24 +1468,44 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
                               P.segs > SP_LIST * C)) C *= 2;
     P.steps = (P.segs + C * SP_WARPS - 1) / (C * SP_WARPS);
     const int32_t clusters = R < SP_BLOCKS * 148 / C ? R : SP_BLOCKS * 148 / C;
+    // What no list holds would take one row's time with few blocks: it goes to a second launch where there is memory
+    // to note it, more blocks would help, and the parameters can ask for it.
+    if (C == SP_CLUSTER || P.segs <= C * SP_WARPS || !(P.top_k || P.top_p || P.min_p)) P.queue = nullptr;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * C));
     cfg.blockDim = dim3(SP_THREADS);
     cfg.dynamicSmemBytes = sizeof(SampleShared);
     cfg.stream = stream;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)C;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
     LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<BF16>, P));
+    lora_status_t s = count_launch();
+    if (s != LORA_OK || !P.queue) return s;
+    const int32_t most = SP_BLOCKS * 148 / SP_CLUSTER;
+    P.steps = (P.segs + SP_CLUSTER * SP_WARPS - 1) / (SP_CLUSTER * SP_WARPS);
+    cfg.gridDim = dim3((unsigned)((R < most ? R : most) * SP_CLUSTER));
+    at[0].val.clusterDim.x = SP_CLUSTER;
+    cfg.numAttrs = 2;
+    LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_rest_kernel<BF16>, P));
     return count_launch();
 }
 
 }  // namespace lora
 
 using namespace lora;
+
+extern "C" lora_status_t lora_sample_workspace_bytes(int32_t R, size_t *bytes) {
+    if (!bytes) return LORA_ERR_INVALID_ARG;
+    if (R < 0 || R > (1 << 24)) return LORA_ERR_SHAPE;
+    *bytes = offsetof(SampleQueue, rows) + (size_t)R * sizeof(SampleQueue::Row);
+    return LORA_OK;
+}
 
 extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, void *stream) {
     if (!args) return LORA_ERR_INVALID_ARG;
@@ -1402,7 +1528,12 @@ extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, 
                                   ((R - 1) * args->ld + args->vocab) * unit, 8, 1))
             return LORA_ERR_INVALID_ARG;
     }
+    size_t need = 0;
+    lora_sample_workspace_bytes(R, &need);
+    if ((uintptr_t)args->workspace & 15) return LORA_ERR_INVALID_ARG;
+    if (args->workspace && args->workspace_bytes < need) return LORA_ERR_BUFFER_TOO_SMALL;
     SampleParams P;
+    P.queue = (SampleQueue *)args->workspace;
     P.logits = args->logits;
     P.ld = args->ld;
     P.R = R;

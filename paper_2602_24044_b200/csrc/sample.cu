@@ -14,7 +14,7 @@
 // A cluster of blocks takes a row, in steps of 2 KB a warp.  Rows with a filter collect candidates in shared memory:
 // whatever is not below a threshold that only rises (one that K values so far are not below, or min_p of the largest
 // so far); K = top_k, or KEEP_P for top_p alone, where the sum of all weights is taken on the way.  The first block
-// sorts what is left at the end.  Rows without a filter only sum, a step's sum by itself: the token's step is looked
+// picks from what is left at the end.  Rows without a filter only sum, a step's sum by itself: the token's step is looked
 // up among the sums and read again.  What does not fit (top_k over KEEP_K, a nucleus of thousands) is found with two
 // more readings of the row, which the second-level cache has in part: band_row.  What does not fit there either
 // (thousands of ties) takes a reading for each digit of the cut: general_row.
@@ -35,7 +35,11 @@ constexpr int SP_THREADS = 256, SP_WARPS = SP_THREADS / 32;
 constexpr int SP_CLUSTER = 8;                 // blocks of a row at most
 constexpr int SP_LIST = 2048;                 // entries of a list
 constexpr int SP_STAGES = 4, SP_BLOCKS = 2;   // steps of a warp in shared memory; blocks on an SM
-constexpr int KEEP_K = 256, KEEP_P = 192;     // what a list is kept to at most, and where top_p alone asks for one
+// What a list is kept to at most by rank.  For top_p alone: to how many, and how far (as a power of two) below the
+// largest at most.
+constexpr int KEEP_K = 256, KEEP_P = 64;
+constexpr double NEAR_P = 12.0;
+constexpr int SP_REST = 4;                    // blocks of a row in the second launch
 constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
 constexpr int SP_MAX_V = (1 << 20) - 8;       // a row's steps have their sums in a list
 constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
@@ -43,7 +47,7 @@ constexpr double SP_ONE = 70368744177664.0;   // 2^46: the largest weight as a w
 constexpr double SP_MAGIC = 105553116266496.0;   // 1.5 * 2^46: sums with it are rounded to 1/64
 
 struct SampleQueue {             // rows for the second launch
-    int32_t count, done, reserved[2];
+    int32_t count, next, done, reserved;
     struct Row {
         int32_t row;
         float max;
@@ -66,12 +70,12 @@ struct SampleParams {
 struct RowPlan {
     double c;                    // log2(e) / temperature
     double low;                  // smallest exponent that min_p keeps, -inf: all
-    float drop;                  // how far below the largest value that is, and a little more
+    float drop;                  // how far below the largest so far candidates may be
     float u;
     double p;
     int32_t k;                   // 0: all
     int32_t keep;                // entries that a list is cut to; 0: not by rank
-    bool greedy, by_p, by_min, list, sums, segments;
+    bool greedy, by_p, by_min, near, list, sums, segments;   // near: candidates by `drop` (too)
 };
 
 struct SampleShared {
@@ -554,11 +558,11 @@ __device__ __forceinline__ void answer(const SampleParams &P, int64_t r, int32_t
 // The first block, from the cluster's candidates.  False where they do not hold the whole of what is kept.
 //
 // Up to half a block of candidates, everything is counted: how many candidates are in front of one and what they weigh
-// says whether it is kept, what the kept ones of lower index weigh whether u falls on it.  2, 4 or 8 threads (a
-// power of two of neighbours) count for one candidate.
+// says whether it is kept, what the kept ones of lower index weigh whether u falls on it.  Two or four neighbouring
+// threads count for one candidate.
 __device__ bool count_candidates(SampleShared &s, const SampleParams &P, const RowPlan &R, int64_t row, float m, double all,
                                  int n) {
-    const int tid = threadIdx.x, log_g = n <= 32 ? 3 : n <= 64 ? 2 : 1, g = 1 << log_g, part = tid & (g - 1), me = tid >> log_g;
+    const int tid = threadIdx.x, log_g = n <= 64 ? 2 : 1, g = 1 << log_g, part = tid & (g - 1), me = tid >> log_g;
     ulonglong2 *const pair = reinterpret_cast<ulonglong2 *>(s.list);         // n <= SP_THREADS / 2
     const uint64_t mine = me < n ? s.merge[me] : 0;
     uint64_t w = 0;
@@ -570,13 +574,17 @@ __device__ bool count_candidates(SampleShared &s, const SampleParams &P, const R
     __syncthreads();
     int rank = 0;
     uint64_t before = 0;
-#pragma unroll 4
-    for (int j = part; j < n; j += g) {
-        const ulonglong2 o = pair[j];
-        if (o.x > mine) {
-            ++rank;
-            before += o.y;
-        }
+    const int rounds = (n + 8 * g - 1) / (8 * g);          // (there are SP_THREADS / g entries, those from n on nothing)
+    for (int j = 0; j < rounds; ++j) {
+        ulonglong2 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = pair[(j * 8 + i) * g + part];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (o[i].x > mine) {
+                ++rank;
+                before += o[i].y;
+            }
     }
     for (int d = 1; d < g; d <<= 1) {
         rank += __shfl_xor_sync(0xffffffffu, rank, d);
@@ -595,10 +603,13 @@ __device__ bool count_candidates(SampleShared &s, const SampleParams &P, const R
     if (part == 0) pair[me] = make_ulonglong2(index, w);
     __syncthreads();
     before = 0;
-#pragma unroll 4
-    for (int j = part; j < n; j += g) {
-        const ulonglong2 o = pair[j];
-        if ((uint32_t)o.x < index) before += o.y;
+    for (int j = 0; j < rounds; ++j) {
+        ulonglong2 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = pair[(j * 8 + i) * g + part];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((uint32_t)o[i].x < index) before += o[i].y;
     }
     for (int d = 1; d < g; d <<= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
     uint64_t target = (uint64_t)((double)R.u * (double)total);
@@ -633,7 +644,8 @@ __device__ __noinline__ bool pick_from_list(SampleShared &s, const SampleParams 
         block_before<uint64_t>(sum, s.scan_u, reach);
         if ((double)reach < R.p * all) return false;
     }
-    if (n > SP_THREADS && R.k && R.keep) n = cut_list(s, s.merge, n, R.keep, SP_THREADS, cut);
+    const int few = R.keep <= SP_THREADS / 3 ? SP_THREADS / 2 : SP_THREADS;
+    if (n > few && R.k && R.keep) n = cut_list(s, s.merge, n, R.keep, few, cut);
     if (n <= SP_THREADS / 2) return count_candidates(s, P, R, row, m, all, n);
     // more of them: sorted
     int size = sort_entries<true>(s.merge, n);
@@ -713,10 +725,11 @@ __device__ __noinline__ void pick_from_sums(SampleShared &s, const SampleParams 
                                const double *sums, W w) {
     constexpr int SEG = Step<BF16>::SEG, PER = SP_LIST / SP_THREADS, MINE = SEG / SP_THREADS;
     const int tid = threadIdx.x;
+    const int per = (P.segs + SP_THREADS - 1) / SP_THREADS;
     double mine[PER], sum = 0.0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        mine[j] = tid * PER + j < P.segs ? sums[tid * PER + j] : 0.0;
+        mine[j] = j < per && tid * per + j < P.segs ? sums[tid * per + j] : 0.0;
         sum += mine[j];
     }
     double total;
@@ -731,7 +744,7 @@ __device__ __noinline__ void pick_from_sums(SampleShared &s, const SampleParams 
     for (int j = 0; j < PER; ++j) {
         if (!here && mine[j] > 0.0 && target < before + mine[j]) {
             here = true;
-            seg = tid * PER + j;
+            seg = tid * per + j;
             rest = target - before;
         }
         before += mine[j];
@@ -814,8 +827,11 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const float m = s.row_max, c64 = (float)(R.c * 64.0);
     if (!(R.c > 1e-30) || !(fabsf(m) <= FLT_MAX) || P.steps * SP_WARPS > MOST_SUMS || !(R.k || R.by_p || R.by_min)) return false;
-    // a value's place below the largest, in 1/64 of a power of two; the last bin is all the rest, masked tokens too
+    // A value's place below the largest, in 1/64 of a power of two, and the nearest bin; the last one is all the rest,
+    // masked tokens too.  (2^23 and a small number is the nearest whole one in the low bits: no conversions, which issue
+    // at an eighth of the rate.)
     auto place = [&](float l) { return fminf((m - l) * c64, (float)(SP_BINS - 1)); };
+    auto bin_of = [&](float l) { return __float_as_int(place(l) + 8388608.0f) - 0x4b000000; };
     const float last = R.by_min ? fminf((float)(-R.low * 64.0), 1e30f) : INFINITY;
     const bool by_k = R.k != 0, by_p = R.by_p;
     uint32_t *const counts = reinterpret_cast<uint32_t *>(s.list), *const weights = counts + SP_BINS;
@@ -825,13 +841,13 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t, int) {
 #pragma unroll
         for (int e = 0; e < S::N; ++e) {
-            const float f = place(x.value(e));
-            const int b = (int)f;
+            const float f = place(x.value(e)), whole_f = f + 8388608.0f;
+            const int b = __float_as_int(whole_f) - 0x4b000000;
             if (by_k) atomicAdd(&counts[b], 1u);
-            // 2^(-r / 64) of the rest r < 1, to its square
-            const float r = f - (float)b;
+            // 2^(-r / 64) of the rest |r| <= 1/2, to its square
+            const float r = f - (whole_f - 8388608.0f);
             if (by_p && f <= last)
-                atomicAdd(&weights[b], (uint32_t)__float2int_rn(fmaf(r, fmaf(r, 3.843576f, -709.7827f), 65536.0f)));
+                atomicAdd(&weights[b], __float_as_uint(fmaf(r, fmaf(r, 3.843576f, -709.7827f), 65536.0f) + 8388608.0f) - 0x4b000000u);
         }
     });
     cluster_sync(cluster, C);
@@ -925,7 +941,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
 #pragma unroll
         for (int e = 0; e < S::N; ++e) {
             const float l = x.value(e);
-            const int b = (int)place(l);
+            const int b = bin_of(l);
             double w = power2((double)fmaxf(l, floor_l), R.c, magic, s.table);
             if (by_min && !(exponent_of(l, m, R.c) >= R.low)) w = 0.0;
             sum += b < p_first ? w : 0.0;
@@ -975,7 +991,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
             const int size = sort_entries<true>(s.merge, found);
             // entries of the bands: those of top_p's first.  How many are in front of the k-th's band?
             int ahead = 0;
-            for (int i = tid; i < found; i += SP_THREADS) ahead += (int)place(value_of((uint32_t)(s.merge[i] >> 32))) < k_bin;
+            for (int i = tid; i < found; i += SP_THREADS) ahead += bin_of(value_of((uint32_t)(s.merge[i] >> 32))) < k_bin;
             uint64_t in_p;
             block_before<uint64_t>((uint64_t)ahead, s.scan_u, in_p);
             constexpr int MOST = SP_LIST / SP_THREADS;
@@ -987,7 +1003,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
                 const int i = at + j;
                 if (j < per && i < found) {
                     const float l = value_of((uint32_t)(s.merge[i] >> 32));
-                    const int b = (int)place(l);
+                    const int b = bin_of(l);
                     const double t = exponent_of(l, m, R.c);
                     const bool counts_in = b < k_bin || (uint64_t)i - in_p + before_k < (uint64_t)R.k;
                     if (counts_in && t >= R.low) w[j] = weight_of(t, s.table);
@@ -1187,14 +1203,15 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
     R.p = R.by_p ? (double)fmaxf(p, 0.0f) : 1.0;
     R.by_min = mp > 0.0f;
     R.low = R.by_min ? log2((double)fminf(mp, 1.0f)) : -INFINITY;
-    // with a little room for the roundings of this bound
-    R.drop = R.by_min ? (float)(-R.low / R.c) * 1.00001f : INFINITY;
     R.u = fminf(fmaxf(__ldg(P.uniform + row), 0.0f), 1.0f);
     // (far temperatures, at which masked tokens do not vanish by themselves, take the general path)
     const bool far = !(R.c > 1e-30);
     const bool by_rank = R.k && R.k <= KEEP_K;
     R.list = !far && (by_rank || R.by_min || (R.by_p && !R.k));
-    R.keep = by_rank ? R.k : R.by_min || !R.list ? 0 : KEEP_P;
+    R.keep = by_rank ? R.k : R.list && !R.by_min ? KEEP_P : 0;
+    R.near = R.list && (!by_rank || R.by_min);
+    // (with a little room for the roundings of this bound)
+    R.drop = (float)((R.by_min ? -R.low : NEAR_P) / R.c) * 1.00001f;
     R.sums = !far && !R.k && !R.by_min;
     R.segments = R.sums && !R.by_p;
     return R;
@@ -1241,7 +1258,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     if (tid < SP_WARPS) s.warp_threshold[tid] = 0;
     __syncthreads();
     const RowPlan &R = s.plan;
-    const bool sums = R.sums, by_min = R.by_min;
+    const bool sums = R.sums, near = R.near;
     const double c = R.c;
     bool list = R.list;
     float top = -INFINITY, top1 = -INFINITY, t = -FLT_MAX;
@@ -1288,7 +1305,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 for (int e = 0; e < S::N; ++e) sum += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
             }
             if (!list) return;
-            if (by_min) {
+            if (near) {
                 const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
                 if (lane == 0 && k > s.best && atomicMax(&s.best, k) < k) {
                     const float m = value_of(k), least = (m - R.drop) - fabsf(m) * 1e-5f;
@@ -1296,8 +1313,8 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 }
                 __syncwarp();
             }
-            const int n = it + 1, low = n & -n;
-            if (n == low || n == 3 * low) {      // behind 1, 2, 3, 4, 6, 8, 12, 16, .. steps
+            const int n = it + 1;
+            if ((n & (n - 1)) == 0) {           // behind 1, 2, 4, 8, .. steps
                 if (R.keep) warp_threshold(s, R, top, top1);
                 if (__syncthreads_or(s.n > SP_LIST / 2)) {
                     shorten(s, R);
@@ -1305,7 +1322,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 }
                 t = value_of(block_threshold(s));
             }
-            if (by_min) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
+            if (near) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
             if (list && step_top >= t) put_step<BF16>(s, logits, x, vec, seg, t);
         });
     if (row + rows_apart < P.R) {
@@ -1416,7 +1433,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     }
 }
 
-// The rows that the first launch left over, eight blocks each: few as a rule, so that their time is one row's.
+// The rows that the first launch left over, SP_REST blocks each: few as a rule, so that their time is one row's.
 template <bool BF16>
 __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(const __grid_constant__ SampleParams P) {
     extern __shared__ __align__(16) unsigned char sample_smem[];
@@ -1426,9 +1443,18 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
     fill_table(s);
     griddep_wait();
     const int rows = min(*(volatile int32_t *)&P.queue->count, P.R);
-    for (int i = blockIdx.x / C; i < rows; i += gridDim.x / C) {
+    // the next row is whichever cluster's comes first: not all of them need to be there at a time
+    for (;;) {
+        if (rank == 0 && tid == 0) {
+            const int i = atomicAdd(&P.queue->next, 1);
+            for (int c = 0; c < C; ++c) cluster.map_shared_rank(&s, c)->found = i;
+        }
+        cluster_sync(cluster, C);
+        const int i = s.found;
+        if (i >= rows) break;
         const SampleQueue::Row &r = P.queue->rows[i];
         const int32_t row = r.row;
+        cluster_sync(cluster, C);
         if (row < 0 || row >= P.R) continue;           // (the caller's memory)
         if (tid == 64) s.plan = plan_row(P, row);
         if (tid == 0) {
@@ -1441,8 +1467,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
         cluster_sync(cluster, C);
     }
     if (rank == 0 && tid == 0 && atomicAdd(&P.queue->done, 1) == (int)gridDim.x / C - 1) {     // every cluster has read it
-        P.queue->count = 0;
-        P.queue->done = 0;
+        P.queue->count = P.queue->next = P.queue->done = 0;
     }
 }
 
@@ -1470,7 +1495,7 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     const int32_t clusters = R < SP_BLOCKS * 148 / C ? R : SP_BLOCKS * 148 / C;
     // What no list holds would take one row's time with few blocks: it goes to a second launch where there is memory
     // to note it, more blocks would help, and the parameters can ask for it.
-    if (C == SP_CLUSTER || P.segs <= C * SP_WARPS || !(P.top_k || P.top_p || P.min_p)) P.queue = nullptr;
+    if (C >= SP_REST || P.segs <= C * SP_WARPS || !(P.top_k || P.top_p || P.min_p)) P.queue = nullptr;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * C));
     cfg.blockDim = dim3(SP_THREADS);
@@ -1487,10 +1512,10 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<BF16>, P));
     lora_status_t s = count_launch();
     if (s != LORA_OK || !P.queue) return s;
-    const int32_t most = SP_BLOCKS * 148 / SP_CLUSTER;
-    P.steps = (P.segs + SP_CLUSTER * SP_WARPS - 1) / (SP_CLUSTER * SP_WARPS);
-    cfg.gridDim = dim3((unsigned)((R < most ? R : most) * SP_CLUSTER));
-    at[0].val.clusterDim.x = SP_CLUSTER;
+    const int32_t most = SP_BLOCKS * 148 / SP_REST;
+    P.steps = (P.segs + SP_REST * SP_WARPS - 1) / (SP_REST * SP_WARPS);
+    cfg.gridDim = dim3((unsigned)((R < most ? R : most) * SP_REST));
+    at[0].val.clusterDim.x = SP_REST;
     cfg.numAttrs = 2;
     LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_rest_kernel<BF16>, P));
     return count_launch();

@@ -93,17 +93,13 @@ enum { ROT_NONE = 0, ROT_HALF = 1, ROT_PART = 2, ROT_PAIRS = 3 };
 template <int ROT>
 struct Angles { uint64_t c[4], s[4]; };      // PAIRS: one cosine and one sine a pair, 4 of each run
 
-// Angles in global memory, or (SH) in shared memory.
-template <bool SH, typename V>
-__device__ __forceinline__ V angle(const V *p) { return SH ? *p : __ldg(p); }
-
-template <int D, int ROT, bool SH>
+template <int D, int ROT>
 __device__ __forceinline__ void load_angles(Angles<ROT> &A, const float *row, int rot_dim, int j) {
     if (ROT == ROT_HALF) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float4 c = angle<SH>(reinterpret_cast<const float4 *>(row + 8 * j + 4 * i));
-            const float4 s = angle<SH>(reinterpret_cast<const float4 *>(row + D / 2 + 8 * j + 4 * i));
+            const float4 c = __ldg(reinterpret_cast<const float4 *>(row + 8 * j + 4 * i));
+            const float4 s = __ldg(reinterpret_cast<const float4 *>(row + D / 2 + 8 * j + 4 * i));
             A.c[2 * i] = pack2f(c.x, c.y); A.c[2 * i + 1] = pack2f(c.z, c.w);
             A.s[2 * i] = pack2f(s.x, s.y); A.s[2 * i + 1] = pack2f(s.z, s.w);
         }
@@ -112,11 +108,51 @@ __device__ __forceinline__ void load_angles(Angles<ROT> &A, const float *row, in
         for (int i = 0; i < 4; ++i) {
             const int p = 4 * j + i, q = D / 4 + 4 * j + i;
             const bool in_p = 2 * p < rot_dim, in_q = 2 * q < rot_dim;
-            A.c[i] = pack2f(in_p ? angle<SH>(row + p) : 1.0f, in_q ? angle<SH>(row + q) : 1.0f);
-            A.s[i] = pack2f(in_p ? angle<SH>(row + rot_dim / 2 + p) : 0.0f, in_q ? angle<SH>(row + rot_dim / 2 + q) : 0.0f);
+            A.c[i] = pack2f(in_p ? __ldg(row + p) : 1.0f, in_q ? __ldg(row + q) : 1.0f);
+            A.s[i] = pack2f(in_p ? __ldg(row + rot_dim / 2 + p) : 0.0f, in_q ? __ldg(row + rot_dim / 2 + q) : 0.0f);
         }
     }
 }
+
+// The same from the rows of several axes: each pair's axis is two bits of `axis`.
+__device__ __forceinline__ const float *axis_row(const float *cos_sin, const int32_t (&pos)[4], uint32_t axis, int rot_dim) {
+    const int32_t lo = axis & 1 ? pos[1] : pos[0], hi = axis & 1 ? pos[3] : pos[2];
+    return cos_sin + (int64_t)(axis & 2 ? hi : lo) * rot_dim;
+}
+template <int D, int ROT>
+__device__ __forceinline__ void load_axes_angles(Angles<ROT> &A, const float *cos_sin, const uint32_t (&axis)[4],
+                                                 const int32_t (&pos)[4], int rot_dim, int j) {
+    if (ROT == ROT_HALF) {
+        const uint32_t mine = axis[j / 2] >> (16 * (j & 1));
+        float c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float *row = axis_row(cos_sin, pos, mine >> (2 * i), rot_dim) + 8 * j + i;
+            c[i] = __ldg(row);
+            s[i] = __ldg(row + D / 2);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            A.c[i] = pack2f(c[2 * i], c[2 * i + 1]);
+            A.s[i] = pack2f(s[2 * i], s[2 * i + 1]);
+        }
+    } else {
+        const uint32_t of_p = axis[j / 4] >> (8 * (j & 3)), of_q = axis[D / 64 + j / 4] >> (8 * (j & 3));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = 4 * j + i, q = D / 4 + 4 * j + i;
+            const float *rp = axis_row(cos_sin, pos, of_p >> (2 * i), rot_dim) + p;
+            const float *rq = axis_row(cos_sin, pos, of_q >> (2 * i), rot_dim) + q;
+            const bool in_p = 2 * p < rot_dim, in_q = 2 * q < rot_dim;
+            A.c[i] = pack2f(in_p ? __ldg(rp) : 1.0f, in_q ? __ldg(rq) : 1.0f);
+            A.s[i] = pack2f(in_p ? __ldg(rp + rot_dim / 2) : 0.0f, in_q ? __ldg(rq + rot_dim / 2) : 0.0f);
+        }
+    }
+}
+
+// Angles in global memory, or (SH) in shared memory.
+template <bool SH, typename V>
+__device__ __forceinline__ V angle(const V *p) { return SH ? *p : __ldg(p); }
 
 // The rotated run (0: x.a, 1: x.b) of a head whose first rot_dim < D elements are rotated: the partner of
 // element e is e +- rot/2.  rot/2 is a multiple of 8, so the eight elements of a run have their partners
@@ -229,12 +265,13 @@ __device__ __forceinline__ void quantise_row(const Row &x, uint32_t &wa, uint32_
 // key and (with a cache) value heads.  All its rows are requested before anything is waited for: position,
 // angles and rows one after the other were 2 us a warp with 2 KB on their way (prefill of 12936 tokens:
 // 94 us a launch, 187 with the cache; bytes alone 41 and 40).
-// AXES: the token's positions on several axes each give some of the pairs their angles.  The block puts the
-// token's row of angles together in shared memory while its rows are on their way, and goes on from there as
-// with one position; a pair's axis is looked up once a token and not once a head.
+// AXES: the token's positions on several axes each give some of the pairs their angles.  A lane fetches its pairs'
+// angles one by one, each from the row of its axis; where a head is rotated in part, every head would fetch them again,
+// and the block puts the token's row together in shared memory once.  (That for all: one barrier a token, 68.8 us
+// against 61.5 for the rotation of 12936 tokens.)
 template <int D, int ROT, bool CACHE, int NP, bool AXES>
 __global__ void __launch_bounds__(256, ROWS_BLOCKS) rows_kernel(const RowParams P) {
-    __shared__ __align__(16) float angle_row[AXES ? D : 4];
+    __shared__ __align__(16) float angle_row[AXES && ROT == ROT_PART ? D : 4];
     constexpr int LPH = D / 16, HPP = 32 / LPH;     // lanes of a head, heads of a pass
     const int lane = threadIdx.x & 31, j = lane % LPH, g = lane / LPH;
     const int heads = P.hq + P.hk + (CACHE ? P.hk : 0);
@@ -260,29 +297,36 @@ __global__ void __launch_bounds__(256, ROWS_BLOCKS) rows_kernel(const RowParams 
         Angles<ROT> A;
         bool turn = false;
         if (ROT != ROT_NONE) {
+            int32_t pos[4] = {0, 0, 0, 0};
             if (AXES) {
                 turn = true;
-                for (int a = 0; a < P.num_axes; ++a) {
-                    const int32_t pos = __ldg(P.positions + a * P.ld_pos + t);
-                    turn = turn && pos >= 0 && pos < P.num_positions;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    if (a < P.num_axes) pos[a] = __ldg(P.positions + a * P.ld_pos + t);
+                    turn = turn && pos[a] >= 0 && pos[a] < P.num_positions;
                 }
-                if (h0 == (int)(threadIdx.x >> 5) * (NP * HPP)) {      // every warp has a first pass
-                    const int half = P.rot_dim / 2;
-                    for (int p = threadIdx.x; turn && p < half; p += blockDim.x) {
-                        const int a = P.axis[p / 16] >> (2 * (p % 16)) & 3;
-                        const float *from = P.cos_sin + (int64_t)__ldg(P.positions + a * P.ld_pos + t) * P.rot_dim + p;
-                        angle_row[p] = __ldg(from);
-                        angle_row[half + p] = __ldg(from + half);
+#pragma unroll
+                for (int a = 0; a < 4; ++a) pos[a] = turn ? pos[a] : 0;
+                if (ROT == ROT_PART) {
+                    if (h0 == (int)(threadIdx.x >> 5) * (NP * HPP)) {      // every warp has a first pass
+                        const int half = P.rot_dim / 2;
+                        for (int p = threadIdx.x; p < half; p += blockDim.x) {
+                            const float *from = axis_row(P.cos_sin, pos, P.axis[p / 16] >> (2 * (p % 16)), P.rot_dim) + p;
+                            angle_row[p] = __ldg(from);
+                            angle_row[half + p] = __ldg(from + half);
+                        }
+                        __syncthreads();
                     }
-                    __syncthreads();
+                    row = angle_row;
+                } else {
+                    load_axes_angles<D, ROT>(A, P.cos_sin, P.axis, pos, P.rot_dim, j);
                 }
-                row = angle_row;
             } else {
-                const int32_t pos = __ldg(P.positions + t);
-                turn = pos >= 0 && pos < P.num_positions;
-                row = P.cos_sin + (int64_t)(turn ? pos : 0) * P.rot_dim;
+                pos[0] = __ldg(P.positions + t);
+                turn = pos[0] >= 0 && pos[0] < P.num_positions;
+                row = P.cos_sin + (int64_t)(turn ? pos[0] : 0) * P.rot_dim;
+                load_angles<D, ROT>(A, row, P.rot_dim, j);
             }
-            load_angles<D, ROT, AXES>(A, row, P.rot_dim, j);
             if (!turn && P.status && h0 == 0 && lane == 0) atomicAdd(&P.status[STATUS_INVALID_TOKENS], 1);
         }
         if (CACHE) {

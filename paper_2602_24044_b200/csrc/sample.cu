@@ -316,9 +316,9 @@ __device__ __forceinline__ void sort_blocked(uint64_t *a) {
     uint64_t e[E];
 #pragma unroll
     for (int x = 0; x < E; ++x) e[x] = a[tid * E + x];
-#pragma unroll (E == 1 ? 16 : 1)
+#pragma unroll 1
     for (int k = 2; k <= SP_THREADS * E; k <<= 1) {
-#pragma unroll (E == 1 ? 16 : 1)
+#pragma unroll 1
         for (int d = k / (2 * E); d > 0; d >>= 1) {
             // the larger entry stays in the lower thread of a descending run
             const bool larger = (((tid & d) == 0) == (((tid * E) & k) == 0)) == DOWN;

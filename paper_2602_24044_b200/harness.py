@@ -379,15 +379,18 @@ class KVCache:
         R, T = self.R, self.T
         if self.block_table is None:
             raise ValueError("axis_positions: no tables have been built")
-        self._ints("spans", spans, 0)
-        self._ints("span_begin", span_begin, R + 1)
-        shape = out.shape
-        if spans.dim() != 2 or (spans.shape[1] != 8 and spans.shape[0]):
-            raise ValueError("spans: needs rows of 8 words")
-        if (out.dtype is not torch.int32 or out.get_device() != self._index or len(shape) != 2 or shape[0] < 3 or
-                shape[1] < T or (shape[1] > 1 and out.stride(1) != 1)):
+        # (as _ints, written out: the time of this call is the host's)
+        index, int32, have, shape = self._index, torch.int32, spans.shape, out.shape
+        if (spans.dtype is not int32 or spans.get_device() != index or not spans.is_contiguous() or len(have) != 2 or
+                have[1] != 8):
+            raise ValueError("spans: needs rows of 8 int32 in a row on %s" % self.device)
+        if (span_begin.dtype is not int32 or span_begin.numel() < R + 1 or span_begin.get_device() != index or
+                not span_begin.is_contiguous()):
+            self._ints("span_begin", span_begin, R + 1)
+        if (out.dtype is not int32 or out.get_device() != index or len(shape) != 2 or shape[0] < 3 or shape[1] < T or
+                not (out.is_contiguous() or out.stride(1) == 1)):
             raise ValueError("out: needs int32 [3, %d] on %s" % (T, self.device))
-        lb.kv_axis_positions(self.kv, self.tables, R, T, spans, span_begin, spans.shape[0], out, out.stride(0),
+        lb.kv_axis_positions(self.kv, self.tables, R, T, spans, span_begin, have[0], out, max(out.stride(0), shape[1]),
                              stream=self._on(stream))
 
     def append(self, layer: int, args, slots=None, T: Optional[int] = None, stream=None) -> None:

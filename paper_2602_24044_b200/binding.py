@@ -861,12 +861,20 @@ def _zeros(like, nbytes: int):
     return t
 
 
+def _record(t, stream) -> None:
+    """A tensor made here is not given back to the allocator while work on `stream` may use it (a bare handle says
+    nothing of how long its stream lives: there the caller keeps the block until the work is done)."""
+    import torch
+    if type(stream) is not int:
+        t.record_stream(torch.cuda.default_stream(t.device) if stream is None else stream)
+
+
 def sample(args, R: int, stream=None) -> None:
     """The next tokens of R requests; `args` from sample_args."""
     if R > args.max_tokens:
         _too_many(args, R, "sample")
-    if args.own_workspace is not None and stream is not None and stream not in args.streams and type(stream) is not int:
-        args.own_workspace.record_stream(stream)       # (not given back to the allocator while the call may run)
+    if args.own_workspace is not None and stream not in args.streams:
+        _record(args.own_workspace, stream)
         args.streams = args.streams | {stream}
     status = _lib().lora_sample(ctypes.byref(args), R, _stream(stream))
     if status:

@@ -38,7 +38,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3",
-           "-std=c++17", "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",
+           "-std=c++17", "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",
            "-I", os.path.join(_ROOT, "include"), "-I", CSRC, "-o", tmp] + sources()
     if verbose:
         cmd.insert(1, "-Xptxas")

@@ -1419,8 +1419,8 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     cluster_sync(cluster, C);
     if (s.general && P.queue) {
         if (rank == 0 && tid == 0) {
-            const int at = atomicAdd(&P.queue->count, 1);
-            if (at < P.R) P.queue->rows[at] = {(int32_t)row, s.row_max, s.total};
+            const uint32_t at = (uint32_t)atomicAdd(&P.queue->count, 1);
+            if (at < (uint32_t)P.R) P.queue->rows[at] = {(int32_t)row, s.row_max, s.total};
         }
     } else if (s.general) {
         // the next row's steps make room, and are asked for again
@@ -1442,7 +1442,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x;
     fill_table(s);
     griddep_wait();
-    const int rows = min(*(volatile int32_t *)&P.queue->count, P.R);
+    const uint32_t rows = min((uint32_t) * (volatile int32_t *)&P.queue->count, (uint32_t)P.R);
     // the next row is whichever cluster's comes first: not all of them need to be there at a time
     for (;;) {
         if (rank == 0 && tid == 0) {
@@ -1450,7 +1450,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
             for (int c = 0; c < C; ++c) cluster.map_shared_rank(&s, c)->found = i;
         }
         cluster_sync(cluster, C);
-        const int i = s.found;
+        const uint32_t i = (uint32_t)s.found;
         if (i >= rows) break;
         const SampleQueue::Row &r = P.queue->rows[i];
         const int32_t row = r.row;

@@ -241,6 +241,52 @@ def test_rows_of_any_stride_and_alignment(V, more, at, bf16):
     _check(rows, **_params(9, 3, [0, 20, 300], [1.0, 0.9], [0.0, 0.1]))
 
 
+@pytest.mark.parametrize("R,V,bf16", [(2, 1048568, False), (3, 1048568, True), (1, 700001, True), (300, 300000, True)])
+def test_largest_vocabularies(R, V, bf16):
+    require_gpu()
+    import torch
+    x = _logits(min(R, 5), V, R, bf16)
+    n = x.shape[0]
+    rng = np.random.default_rng(R)
+    kw = dict(tau=rng.choice([0.6, 1.0, 1.4], n), k=rng.choice([0, 0, 50, 3000], n), p=rng.choice([1.0, 0.9], n),
+              mp=rng.choice([0.0, 0.0, 0.01], n), u=rng.random(n).astype(np.float32))
+    want = _check(x, **kw)
+    if n < R:        # the same few rows over and over: many blocks' work, few references
+        at = np.arange(R) % n
+        got, _ = _run(x[torch.as_tensor(at, device="cuda")], **{key: v[at] for key, v in kw.items()})
+        assert np.array_equal(got, want[at])
+
+
+@pytest.mark.parametrize("with_workspace", [False, True])
+def test_with_and_without_a_workspace(with_workspace):
+    """Rows that no list holds, in a batch that fills the GPU: in one launch, or noted for a second one; twice, as the
+    workspace has to be left as it was."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    R, V = 320, 20000
+    x = _logits(R, V, 1, peaks=False)
+    u = torch.rand(R, device="cuda")
+    one = torch.ones(R, device="cuda")
+    p = torch.where(torch.arange(R, device="cuda") % 3 == 0, 0.95, 1.0)
+    token, lp = torch.empty(R, dtype=torch.int32, device="cuda"), torch.empty(R, device="cuda")
+    args = lb.sample_args(logits=x, temperature=one, top_p=p, uniform=u, token=token, logprob=lp)
+    assert args.workspace
+    if not with_workspace:
+        args.workspace = None
+    before = lb.launch_count()
+    for _ in range(2):
+        token.fill_(-7)
+        lb.sample(args, R, stream=torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        xs, us, ps = x.cpu().numpy(), u.cpu().numpy(), p.cpu().numpy()
+        assert token.tolist() == [_reference(xs[r], 1.0, 0, ps[r], 0.0, us[r])[0] for r in range(R)]
+        if with_workspace:
+            assert not args.own_workspace[:4].any()
+        u.copy_(torch.rand(R, device="cuda"))
+    assert lb.launch_count() == before + (4 if with_workspace else 2)
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

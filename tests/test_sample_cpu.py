@@ -18,7 +18,9 @@ BASE = 1 << 24
     (dict(R=-1), 2), (dict(R=(1 << 24) + 1), 2), (dict(ld=999), 2), (dict(logits=None), 1), (dict(temperature=None), 1),
     (dict(uniform=None), 1), (dict(token=None), 1), (dict(logits=BASE + 2), 1), (dict(token=BASE + (1 << 20) + 2), 1),
     (dict(top_k=BASE + 1), 1), (dict(logprob=BASE + (1 << 20)), 1), (dict(token=BASE + 400), 1),
-    (dict(token=BASE + (2 << 20) + 8), 1), (dict(logprob=BASE + (6 << 20)), 1), (dict(logprob=BASE + 3999 * 3), 1)])
+    (dict(token=BASE + (2 << 20) + 8), 1), (dict(logprob=BASE + (6 << 20)), 1), (dict(logprob=BASE + 3999 * 3), 1),
+    (dict(workspace=BASE + (8 << 20) + 8, workspace_bytes=1 << 20), 1),
+    (dict(workspace=BASE + (8 << 20), workspace_bytes=63), 7)])
 def test_refusals(bad, status):
     """Addresses that are never followed: every one of these is refused on the host."""
     kw = dict(logits=BASE, ld=1000, vocab=1000, logits_type=lb.LOGITS_FP32, token=BASE + (1 << 20),
@@ -28,6 +30,14 @@ def test_refusals(bad, status):
     with pytest.raises(lb.LoraError) as e:
         lb.sample(lb.sample_args(**kw), bad.get("R", 3))
     assert e.value.status == status
+
+
+def test_workspace_bytes():
+    assert lb.sample_workspace_bytes(0) == 16 and lb.sample_workspace_bytes(3) == 16 + 3 * 16
+    for R in (-1, (1 << 24) + 1):
+        with pytest.raises(lb.LoraError) as e:
+            lb.sample_workspace_bytes(R)
+        assert e.value.status == 2
 
 
 def test_nothing_to_do_is_fine():

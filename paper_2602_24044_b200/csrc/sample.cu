@@ -35,11 +35,8 @@ constexpr int SP_THREADS = 256, SP_WARPS = SP_THREADS / 32;
 constexpr int SP_CLUSTER = 8;                 // blocks of a row at most
 constexpr int SP_LIST = 2048;                 // entries of a list
 constexpr int SP_STAGES = 4, SP_BLOCKS = 2;   // steps of a warp in shared memory; blocks on an SM
-// What a list is kept to at most by rank.  For top_p alone: to how many, and how far (as a power of two) below the
-// largest at most.
-constexpr int KEEP_K = 256, KEEP_P = 64;
-constexpr double NEAR_P = 12.0;
-constexpr int SP_REST = 4;                    // blocks of a row in the second launch
+constexpr int KEEP_K = 256, KEEP_P = 64;      // what a list is kept to at most by rank, and where top_p alone asks for one
+constexpr int SP_REST = 8;                    // blocks of a row in the second launch
 constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
 constexpr int SP_MAX_V = (1 << 20) - 8;       // a row's steps have their sums in a list
 constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
@@ -70,12 +67,12 @@ struct SampleParams {
 struct RowPlan {
     double c;                    // log2(e) / temperature
     double low;                  // smallest exponent that min_p keeps, -inf: all
-    float drop;                  // how far below the largest so far candidates may be
+    float drop;                  // min_p: how far below the largest so far candidates may be
     float u;
     double p;
     int32_t k;                   // 0: all
     int32_t keep;                // entries that a list is cut to; 0: not by rank
-    bool greedy, by_p, by_min, near, list, sums, segments;   // near: candidates by `drop` (too)
+    bool greedy, by_p, by_min, list, sums, segments;
 };
 
 struct SampleShared {
@@ -832,7 +829,11 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     // at an eighth of the rate.)
     auto place = [&](float l) { return fminf((m - l) * c64, (float)(SP_BINS - 1)); };
     auto bin_of = [&](float l) { return __float_as_int(place(l) + 8388608.0f) - 0x4b000000; };
-    const float last = R.by_min ? fminf((float)(-R.low * 64.0), 1e30f) : INFINITY;
+    // (weights of a quarter of (1 - p) S / V, S that of all, make up less of it than top_p leaves out, all together: the
+    // cut is in front of them.  An atomic addition in shared memory takes a cycle a lane, which is what this reading takes.)
+    const bool known = s.total == s.total;
+    const float last = R.by_min ? fminf((float)(-R.low * 64.0), 1e30f)
+                       : known && R.by_p ? 64.0f * log2f((float)(4.0 * P.V / ((1.0 - R.p) * s.total))) : INFINITY;
     const bool by_k = R.k != 0, by_p = R.by_p;
     uint32_t *const counts = reinterpret_cast<uint32_t *>(s.list), *const weights = counts + SP_BINS;
     ask_first_steps<BF16>(s, P, logits, C, rank);
@@ -880,7 +881,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
         const double ahead = block_before<double>(weighed, s.scan_d, all_weighed);
         if (tid == 0) {
             s.k_bin = s.p_first = s.p_last = SP_BINS;
-            s.rest = all_weighed;
+            s.rest = known ? 65536.0 * s.total : all_weighed;
             s.pick_count = 0;
             s.merged = 0;
         }
@@ -928,13 +929,12 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     if (tid == 0) s.n = 0;
     __syncthreads();
     double *const sums = reinterpret_cast<double *>(s.list) + MOST_BAND;
-    const bool known = s.total == s.total;     // is the weight of all known?
     // weights as in the first reading: against the power of two next to the largest, turned into weights against it at
     // the end (what min_p leaves is decided by the exact exponent)
     const double base = rint((double)m * R.c), magic = SP_MAGIC - base, turn = exp2(fma(-(double)m, R.c, base));
     const float floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
     const bool far = !(fabs(base) < 1e12), by_min = R.by_min;
-    double between = 0.0;                      // else: what is behind top_p's band and in front of that of the first k
+    double between = 0.0;                      // where the weight of all is not known: what is behind top_p's band and in front of that of the first k
     read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
         double sum = 0.0, rest = 0.0;
         uint32_t in_band = 0;
@@ -1209,9 +1209,8 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
     const bool by_rank = R.k && R.k <= KEEP_K;
     R.list = !far && (by_rank || R.by_min || (R.by_p && !R.k));
     R.keep = by_rank ? R.k : R.list && !R.by_min ? KEEP_P : 0;
-    R.near = R.list && (!by_rank || R.by_min);
     // (with a little room for the roundings of this bound)
-    R.drop = (float)((R.by_min ? -R.low : NEAR_P) / R.c) * 1.00001f;
+    R.drop = (float)(-R.low / R.c) * 1.00001f;
     R.sums = !far && !R.k && !R.by_min;
     R.segments = R.sums && !R.by_p;
     return R;
@@ -1258,7 +1257,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     if (tid < SP_WARPS) s.warp_threshold[tid] = 0;
     __syncthreads();
     const RowPlan &R = s.plan;
-    const bool sums = R.sums, near = R.near;
+    const bool sums = R.sums, by_min = R.by_min;
     const double c = R.c;
     bool list = R.list;
     float top = -INFINITY, top1 = -INFINITY, t = -FLT_MAX;
@@ -1305,7 +1304,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 for (int e = 0; e < S::N; ++e) sum += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
             }
             if (!list) return;
-            if (near) {
+            if (by_min) {
                 const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
                 if (lane == 0 && k > s.best && atomicMax(&s.best, k) < k) {
                     const float m = value_of(k), least = (m - R.drop) - fabsf(m) * 1e-5f;
@@ -1322,7 +1321,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 }
                 t = value_of(block_threshold(s));
             }
-            if (near) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
+            if (by_min) t = fmaxf(t, value_of(*(volatile uint32_t *)&s.threshold));
             if (list && step_top >= t) put_step<BF16>(s, logits, x, vec, seg, t);
         });
     if (row + rows_apart < P.R) {

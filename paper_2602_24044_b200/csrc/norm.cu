@@ -9,6 +9,9 @@
 // fp64 one, and the codes, which a difference in the last bit of fp32 could turn, do not depend on the
 // launch (rounding the fp64 sum to fp32 hides them but once in 10^8 rows).  All of it in fp64 would cost a
 // conversion a value, 16 a cycle and SM: more than the rest of the row.
+//
+// 12937 rows of 4096 with a residual: 67.4 us (6.29 TB/s, 0.98 of a copy's rate), with e4m3 codes and a scale for
+// each 128 values 77.9 us (6.14 TB/s).  16 rows: 8 us, which is the call.
 #include <cuda_fp8.h>
 
 #include <cmath>

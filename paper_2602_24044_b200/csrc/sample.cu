@@ -18,6 +18,10 @@
 // up among the sums and read again.  What does not fit (top_k over KEEP_K, a nucleus of thousands) is found with two
 // more readings of the row, which the second-level cache has in part: band_row.  What does not fit there either
 // (thousands of ties) takes a reading for each digit of the cut: general_row.
+//
+// 256 rows of 128000 fp32 (131 MB, 20 us at a copy's rate): greedy 37 us, top_k 50 48, top_k 200 64, min_p 0.1 41,
+// temperature alone 48, all kinds together with 30 or so wide nuclei 123.  512 rows of 150001 bf16, temperature
+// alone: 91 us, 22 instructions a value.  4 rows of 32000: 11 .. 18 us.
 #include <cooperative_groups.h>
 
 #include <cfloat>

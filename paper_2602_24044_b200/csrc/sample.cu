@@ -237,10 +237,6 @@ struct Step {
             }
         }
     }
-    __device__ __forceinline__ void nothing() {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = NOTHING;
-    }
     __device__ __forceinline__ float value(int e) const {
         if (BF16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
         return __uint_as_float(w[e]);

@@ -387,11 +387,11 @@ class KVCache:
         if (span_begin.dtype is not int32 or span_begin.numel() < R + 1 or span_begin.get_device() != index or
                 not span_begin.is_contiguous()):
             self._ints("span_begin", span_begin, R + 1)
-        if (out.dtype is not int32 or out.get_device() != index or len(shape) != 2 or shape[0] < 3 or shape[1] < T or
+        ld = out.stride(0) if len(shape) == 2 else 0
+        if (out.dtype is not int32 or out.get_device() != index or ld < T or shape[0] < 3 or shape[1] < T or
                 not (out.is_contiguous() or out.stride(1) == 1)):
-            raise ValueError("out: needs int32 [3, %d] on %s" % (T, self.device))
-        lb.kv_axis_positions(self.kv, self.tables, R, T, spans, span_begin, have[0], out, max(out.stride(0), shape[1]),
-                             stream=self._on(stream))
+            raise ValueError("out: needs int32 [3, %d], each axis in a row, on %s" % (T, self.device))
+        lb.kv_axis_positions(self.kv, self.tables, R, T, spans, span_begin, have[0], out, ld, stream=self._on(stream))
 
     def append(self, layer: int, args, slots=None, T: Optional[int] = None, stream=None) -> None:
         """args: binding.qk_args(...); slots: default those of the tables."""

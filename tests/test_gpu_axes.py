@@ -106,6 +106,38 @@ def test_positions_of_failed_requests_odd_spans_and_offsets():
     assert np.array_equal(got[:, 7:], np.stack([p * 0, p * 0, p]))
 
 
+def test_positions_refusals_leave_everything_alone():
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    out = torch.full((3, 8), -7, dtype=torch.int32, device="cuda")
+    spans, begin = _i32(np.zeros((2, 8))), _i32([0, 1, 2])
+    with _cache(num_pages=8) as c:
+        with pytest.raises(ValueError):
+            c.axis_positions(spans, begin, out)                         # no tables yet
+        c.build_tables(_i32([0, 0]), _i32([3, 5]), 8, _i32(np.arange(8)), _i32([8]), _i32(np.zeros((2, 1))))
+        before = lb.launch_count()
+        for bad in (dict(out=out[:2]), dict(out=out[:, :7]), dict(out=out[:1].expand(3, 8)), dict(out=out.t()), dict(out=out[0]),
+                    dict(out=out.float()), dict(spans=spans[:, :7]), dict(spans=spans.long()), dict(spans=spans.view(-1)),
+                    dict(begin=begin[:2]), dict(begin=begin.float())):
+            a = dict(dict(spans=spans, begin=begin, out=out), **bad)
+            with pytest.raises(ValueError):
+                c.axis_positions(a["spans"], a["begin"], a["out"])
+        for (tables, R, T, sp, be, n, to, ld), status in (
+                ((c.tables, 2, 7, spans, begin, 2, out, 8), 1), ((c.tables, 3, 8, spans, begin, 2, out, 8), 1),
+                ((out, 2, 8, spans, begin, 2, out, 8), 1), ((c.tables, 2, 8, spans, None, 2, out, 8), 1),
+                ((c.tables, 2, 8, None, begin, 2, out, 8), 1), ((c.tables, 2, 8, spans, begin, 2, None, 8), 1),
+                ((c.tables, 2, 8, spans, begin, 2, out, 7), 2), ((c.tables, 2, 8, spans, begin, -1, out, 8), 2),
+                ((c.tables, 2, -1, spans, begin, 2, out, 8), 2),
+                ((c.tables, 2, 8, spans.data_ptr() + 4, begin, 1, out, 8), 1)):
+            with pytest.raises(lb.LoraError) as e:
+                lb.kv_axis_positions(c.kv, tables, R, T, sp, be, n, to, ld)
+            assert e.value.status == status
+        assert lb.launch_count() == before and (out == -7).all()
+        c.axis_positions(spans[:0], _i32([0, 0, 0]), out)               # no media at all
+        assert _np(out).tolist() == [[0, 1, 2, 0, 1, 2, 3, 4]] * 3
+
+
 def test_positions_feed_a_captured_step():
     require_gpu()
     import torch

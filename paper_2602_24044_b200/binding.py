@@ -844,8 +844,7 @@ def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None
                 raise LoraError(1, "%s (needs its values in a row)" % what)
             most = min(most, have)
     a.max_tokens = most
-    filters = any(t is not None for t in (top_k, top_p, min_p))
-    if workspace is None and filters and hasattr(token, "new_zeros"):
+    if workspace is None and hasattr(token, "new_zeros"):
         workspace = a.own_workspace = _zeros(token, sample_workspace_bytes(min(most, 1 << 24)))
     if workspace is not None:
         a.workspace = _ptr(workspace)

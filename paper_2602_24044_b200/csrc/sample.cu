@@ -40,6 +40,7 @@ constexpr int SP_CLUSTER = 8;                 // blocks of a row at most
 constexpr int SP_LIST = 2048;                 // entries of a list
 constexpr int SP_STAGES = 4, SP_BLOCKS = 2;   // steps of a warp in shared memory; blocks on an SM
 constexpr int KEEP_K = 256, KEEP_P = 64;      // what a list is kept to at most by rank, and where top_p alone asks for one
+constexpr int SP_SUM_BLOCKS = 4;              // blocks of sample_sum_kernel on an SM
 constexpr int SP_REST = 8;                    // blocks of a row in the second launch
 constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
 constexpr int SP_MAX_V = (1 << 20) - 8;       // a row's steps have their sums in a list
@@ -82,20 +83,6 @@ struct RowPlan {
 struct SampleShared {
     RowPlan plan;
     double table[64 * 16];       // 2^(i / 64), once for each pair of banks
-    uint64_t list[SP_LIST];      // candidates; sums of steps; weights
-    uint64_t merge[SP_LIST];     // (first block) the cluster's candidates; sums of all steps
-    union {
-        uint4 ring[SP_WARPS][SP_STAGES][4][32];   // steps on their way from memory
-        struct {                                  // general path
-            uint64_t digit_weight[2][256];
-            uint32_t digit_count[2][256];
-        };
-        struct {                                  // (first block) band path: of the whole row
-            double bin_weight[SP_BINS];
-            uint32_t bin_count[SP_BINS];
-        };
-        double step_sums[SP_LIST];                // (first block) band path: the sums of all steps
-    };
     uint32_t bins[256];
     uint64_t scan_u[SP_WARPS];
     double scan_d[SP_WARPS];
@@ -118,6 +105,21 @@ struct SampleShared {
     int32_t general, k_bin, p_first, p_last;
     float row_max;
     double total;                // of all weights, NaN where the row was not summed
+    // (from here on not for sample_sum_kernel)
+    alignas(16) uint64_t list[SP_LIST];     // candidates; sums of steps; weights
+    uint64_t merge[SP_LIST];     // (first block) the cluster's candidates; sums of all steps
+    union {
+        uint4 ring[SP_WARPS][SP_STAGES][4][32];   // steps on their way from memory
+        struct {                                  // general path
+            uint64_t digit_weight[2][256];
+            uint32_t digit_count[2][256];
+        };
+        struct {                                  // (first block) band path: of the whole row
+            double bin_weight[SP_BINS];
+            uint32_t bin_count[SP_BINS];
+        };
+        double step_sums[SP_LIST];                // (first block) band path: the sums of all steps
+    };
 };
 
 // ---- values, keys -----------------------------------------------------------------------------
@@ -159,6 +161,11 @@ __device__ __forceinline__ uint64_t whole(double w) { return (uint64_t)(w * SP_O
 __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
 
 struct SampleRow { const char *base; int32_t off, end; };       // see Step::load
+
+// where sample_sum_kernel's steps are in its shared memory, behind the sums
+__host__ __device__ inline size_t sum_ring(int32_t segs) {
+    return offsetof(SampleShared, list) + ((size_t)segs * 8 + 15) / 16 * 16;
+}
 
 
 // ---- a step: 64 bytes a lane ------------------------------------------------------------------
@@ -1470,6 +1477,98 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
     }
 }
 
+// Rows without filters, more of them than blocks of sample_kernel are there at a time: a block a row with no more shared
+// memory than the sums of its steps and two steps a warp, so that four are on an SM.  They end apart, and one's end (a
+// search, a step read again) is hidden behind the others' sums.  512 rows of 150001: LEAN_US us, 91 with sample_kernel.
+template <bool BF16>
+__global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(const __grid_constant__ SampleParams P) {
+    using S = Step<BF16>;
+    extern __shared__ __align__(16) unsigned char sample_smem[];
+    SampleShared &s = *reinterpret_cast<SampleShared *>(sample_smem);      // (up to its list)
+    double *const sums = reinterpret_cast<double *>(s.list);
+    uint4 (*const ring)[4][32] = reinterpret_cast<uint4 (*)[4][32]>(sample_smem + sum_ring(P.segs));
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto ask = [&](const SampleRow &row, int it) {
+        if (it < P.steps) S::ask(row, it * SP_WARPS + warp, ring[warp * 2 + (it & 1)]);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    fill_table(s);
+    SampleRow next = row_at<BF16>(P, blockIdx.x);
+    ask(next, 0);
+    for (int64_t row = blockIdx.x; row < P.R; row += gridDim.x) {
+        const SampleRow logits = next;
+        __syncthreads();
+        if (tid == 64) s.plan = plan_row(P, row);
+        if (tid == 0) {
+            s.best = 0;
+            s.pick_here = 0;
+        }
+        __syncthreads();
+        const RowPlan &R = s.plan;
+        const double c = R.c;
+        const bool add = R.sums, greedy = R.k == 1;
+        float top = -INFINITY, floor_l = -FLT_MAX;
+        double base = 0.0, magic = SP_MAGIC;
+        uint64_t best = 0;
+        for (int it = 0; it < P.steps; ++it) {
+            const int32_t seg = it * SP_WARPS + warp;
+            ask(logits, it + 1);                     // (where the step before this one was)
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            S x;
+            x.take(logits, seg, ring[warp * 2 + (it & 1)]);
+            float vec[4];
+            x.tops(vec);
+            const float step_top = max_or_nan(max_or_nan(vec[0], vec[1]), max_or_nan(vec[2], vec[3]));
+            if (greedy && step_top > top) {          // (a lane's values come in the order of their indices)
+#pragma unroll
+                for (int e = S::N - 1; e >= 0; --e)
+                    if (x.value(e) == step_top) best = entry_of(step_top, S::index(logits, seg, e));
+            }
+            top = max_or_nan(top, step_top);
+            if (!add) continue;
+            if (it == 0) {
+                const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
+                if (lane == 0) atomicMax(&s.best, k);
+                __syncthreads();
+                base = rint((double)(s.best ? value_of(s.best) : 0.0f) * c);
+                if (!(fabs(base) < 1e12)) base = 0.0;
+                magic = SP_MAGIC - base;
+                floor_l = (float)fmax((base - 1000.0) / c, -(double)FLT_MAX);
+            }
+            double w = 0.0;
+#pragma unroll
+            for (int e = 0; e < S::N; ++e) w += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
+#pragma unroll
+            for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
+            if (lane == 0 && seg < P.segs) sums[seg] = w;
+        }
+        if (row + gridDim.x < P.R) {
+            next = row_at<BF16>(P, row + gridDim.x);
+            ask(next, 0);
+        }
+        const bool nan = top != top;
+        const uint32_t block_top = __reduce_max_sync(0xffffffffu, nan ? 0u : key_of(top));
+        if (lane == 0) atomicMax(&s.best, block_top);
+        if (best) atomicMax(reinterpret_cast<unsigned long long *>(&s.pick_here), (unsigned long long)best);
+        const bool bad = __syncthreads_or(nan) || !(value_of(s.best) > -INFINITY);
+        const float m = value_of(s.best);
+        if (bad || greedy) {
+            if (tid == 0) answer(P, row, bad ? -1 : index_of(s.pick_here), bad ? nan_value() : 0.0);
+        } else if (!add || !(fabs((double)m * c - base) < 900.0)) {
+            if (tid == 0) {
+                const uint32_t at = (uint32_t)atomicAdd(&P.queue->count, 1);
+                if (at < (uint32_t)P.R) P.queue->rows[at] = {(int32_t)row, m, nan_value()};
+            }
+        } else {
+            const double scale = exp2(fma(-(double)m, c, base));
+            for (int g = tid; g < P.segs; g += SP_THREADS) sums[g] *= scale;
+            __syncthreads();
+            pick_from_sums<BF16>(s, P, R, row, logits, sums,
+                                 [&](float l, int32_t) { return weight_of(exponent_of(l, m, c), s.table); });
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
@@ -1479,6 +1578,7 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     if (device >= DEVICE_TABLE || !allowed[device].load(std::memory_order_relaxed)) {
         LORA_CUDA_TRY(allow_all_smem(sample_kernel<BF16>, device));
         LORA_CUDA_TRY(allow_all_smem(sample_rest_kernel<BF16>, device));
+        LORA_CUDA_TRY(allow_all_smem(sample_sum_kernel<BF16>, device));
         if (device < DEVICE_TABLE) allowed[device].store(true, std::memory_order_relaxed);
     }
     constexpr int SEG = Step<BF16>::SEG;
@@ -1494,7 +1594,8 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     const int32_t clusters = R < SP_BLOCKS * 148 / C ? R : SP_BLOCKS * 148 / C;
     // What no list holds would take one row's time with few blocks: it goes to a second launch where there is memory
     // to note it, more blocks would help, and the parameters can ask for it.
-    if (C >= SP_REST || P.segs <= C * SP_WARPS || !(P.top_k || P.top_p || P.min_p)) P.queue = nullptr;
+    const bool filters = P.top_k || P.top_p || P.min_p, sums = P.queue && !filters && R > SP_BLOCKS * 148;
+    if (!sums && (C >= SP_REST || P.segs <= C * SP_WARPS || !filters)) P.queue = nullptr;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * C));
     cfg.blockDim = dim3(SP_THREADS);
@@ -1508,11 +1609,20 @@ static lora_status_t launch_sample(SampleParams P, int32_t R, int32_t device, cu
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<BF16>, P));
+    if (sums) {
+        P.steps = (P.segs + SP_WARPS - 1) / SP_WARPS;
+        cfg.gridDim = dim3((unsigned)(R < SP_SUM_BLOCKS * 148 ? R : SP_SUM_BLOCKS * 148));
+        cfg.dynamicSmemBytes = sum_ring(P.segs) + SP_WARPS * 2 * 2048;
+        cfg.numAttrs = 0;
+        LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_sum_kernel<BF16>, P));
+    } else {
+        LORA_CUDA_TRY(cudaLaunchKernelEx(&cfg, sample_kernel<BF16>, P));
+    }
     lora_status_t s = count_launch();
     if (s != LORA_OK || !P.queue) return s;
     const int32_t most = SP_BLOCKS * 148 / SP_REST;
     P.steps = (P.segs + SP_REST * SP_WARPS - 1) / (SP_REST * SP_WARPS);
+    cfg.dynamicSmemBytes = sizeof(SampleShared);
     cfg.gridDim = dim3((unsigned)((R < most ? R : most) * SP_REST));
     at[0].val.clusterDim.x = SP_REST;
     cfg.numAttrs = 2;

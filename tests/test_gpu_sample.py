@@ -117,6 +117,27 @@ def test_whole_vocabulary(V, bf16):
     _check(x, rng.choice([0.3, 1.0, 2.0, 30.0], R), u=rng.random(R).astype(np.float32))
 
 
+@pytest.mark.parametrize("R,V", [(297, 3), (297, 5000), (400, 9001), (592, 2049), (700, 4097), (1300, 777), (300, 60001)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_many_rows_without_filters(R, V, bf16):
+    """Temperatures of all kinds, and rows that need more than a sum."""
+    require_gpu()
+    x = _logits(R, V, R + V, bf16)
+    inf = float("inf")
+    x[0, V // 2], x[1], x[2, V - 1], x[3, 0] = float("nan"), -inf, inf, -inf
+    x[4] = x[4] * 0 - 3.0                                    # all equal
+    x[5, : V - 1] = -inf
+    x[6, V // 3] = 3e38
+    x[7] = x[7] * 1e30
+    rng = np.random.default_rng(V)
+    tau = rng.choice([0.0, 0.3, 1.0, 1.0, 1.0, 5.0], R).astype(np.float32)
+    tau[8:14] = [inf, 1e-30, 3e38, float("nan"), -1.0, 1e-42]
+    tau[[4, 5, 6, 7]] = [1.0, 0.0, 1.0, 1.0]
+    u = rng.random(R).astype(np.float32)
+    u[20:24] = [0.0, 1.0, float("nan"), 2.0 ** -40]
+    _check(x, tau, u=u)
+
+
 @pytest.mark.parametrize("R", [1, 2, 5, 37, 74, 75, 148, 149, 297, 600])
 @pytest.mark.parametrize("bf16", [False, True])
 def test_every_number_of_blocks_a_row(R, bf16):

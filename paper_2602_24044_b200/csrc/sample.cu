@@ -88,7 +88,7 @@ struct SampleShared {
     double scan_d[SP_WARPS];
     int32_t n, failed_here;
     uint32_t threshold, best;    // what candidates are not below, and the block's largest so far, as keys
-    uint32_t warp_threshold[SP_WARPS];
+    uint32_t warp_threshold[4][SP_WARPS];    // for m = 8, 4, 2, 1
     uint32_t key_min, key_max;
     int32_t pick_bin, pick_above, pick_kept;
     uint64_t pick_count, pick_weight, pick_here;
@@ -480,10 +480,13 @@ __device__ __noinline__ int cut_list(SampleShared &s, uint64_t *a, int n, int ke
 }
 
 // A threshold that `keep` values of the block's at least are not below: a lane holds the largest so far of either
-// half of its steps, a warp takes the (keep / warps)-th of its 64, and the lowest of the warps' counts.  It rises with
-// the steps: as many values again pass it in steps 2 .. 3 as in 1, in 4 .. 7 as in 2 .. 3, ..
+// half of its steps, a warp takes the (keep / m)-th of its 64 for m = 8, 4, 2, 1, and the m-th largest of the warps'
+// counts, whichever m gives most.  (The lowest of the eight alone, m = 8, was none where a warp had no values: 256
+// greedy rows took 39 us for 11 with 4096 of bf16, a block's eight warps having four steps, and 335 for 38 with
+// 128000 of fp32 and the first 1024 masked.)  It rises with the steps: as many values again pass it in steps 2 .. 3
+// as in 1, in 4 .. 7 as in 2 .. 3, ..
 __device__ __forceinline__ void warp_threshold(SampleShared &s, const RowPlan &R, float top0, float top1) {
-    const int lane = threadIdx.x & 31, want = (R.keep + SP_WARPS - 1) / SP_WARPS - 1;
+    const int lane = threadIdx.x & 31;
     const uint32_t k0 = top0 == top0 ? key_of(top0) : 0u, k1 = top1 == top1 ? key_of(top1) : 0u;
     // the 64 in descending order, two neighbours a lane
     uint32_t a = (lane & 1) ? min(k0, k1) : max(k0, k1), b = (lane & 1) ? max(k0, k1) : min(k0, k1);
@@ -501,14 +504,20 @@ __device__ __forceinline__ void warp_threshold(SampleShared &s, const RowPlan &R
         a = first ? x : y;
         b = first ? y : x;
     }
-    const uint32_t mine = __shfl_sync(0xffffffffu, (want & 1) ? b : a, want >> 1);
-    if (lane == 0) s.warp_threshold[threadIdx.x >> 5] = mine;
-}
-__device__ __forceinline__ uint32_t block_threshold(const SampleShared &s) {
-    uint32_t t = 0xffffffffu;              // (where nothing is kept by rank all of them are 0)
 #pragma unroll
-    for (int i = 0; i < SP_WARPS; ++i) t = min(t, *(volatile const uint32_t *)&s.warp_threshold[i]);
-    return max(t, *(volatile const uint32_t *)&s.threshold);
+    for (int j = 0; j < 4; ++j) {
+        const int m = SP_WARPS >> j, want = (R.keep + m - 1) / m - 1;
+        const uint32_t mine = __shfl_sync(0xffffffffu, (want & 1) ? b : a, (want >> 1) & 31);
+        if (lane == 0) s.warp_threshold[j][threadIdx.x >> 5] = want < 64 ? mine : 0u;
+    }
+}
+__device__ __forceinline__ uint32_t block_threshold(const SampleShared &s) {      // (by whole warps)
+    const int lane = threadIdx.x & 31, m = SP_WARPS >> (lane >> 3);
+    const uint32_t mine = (&((volatile const SampleShared &)s).warp_threshold[0][0])[lane];
+    int from = 1;                          // (where nothing is kept by rank all of them are 0)
+#pragma unroll
+    for (int i = 1; i < SP_WARPS; ++i) from += __shfl_xor_sync(0xffffffffu, mine, i) >= mine ? 1 : 0;
+    return max(__reduce_max_sync(0xffffffffu, from >= m ? mine : 0u), *(volatile const uint32_t *)&s.threshold);
 }
 
 // The values of a step that are not below t: a lane takes its places at once.
@@ -1261,7 +1270,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
         s.threshold = key_of(-FLT_MAX);
         s.best = 0;
     }
-    if (tid < SP_WARPS) s.warp_threshold[tid] = 0;
+    if (tid < 4 * SP_WARPS) (&s.warp_threshold[0][0])[tid] = 0;
     __syncthreads();
     const RowPlan &R = s.plan;
     const bool sums = R.sums, by_min = R.by_min;
@@ -1356,13 +1365,14 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
             if (tid == 0) s.threshold = max(s.threshold, cut);
         }
     }
+    const uint32_t threshold = block_threshold(s);
     cluster_sync(cluster, C);                  // (the first block's counts of this row are at zero)
     SampleShared &first = *cluster.map_shared_rank(&s, 0);
     if (tid == 0) {
         s.found = n ? atomicAdd(&first.merged, n) : 0;
         first.top[rank] = s.best;
         first.bad[rank] = any_nan;
-        first.cut[rank] = block_threshold(s);
+        first.cut[rank] = threshold;
         first.failed[rank] = list != R.list || s.found + n > SP_LIST;
         first.sum[rank] = block_sum;
         first.base[rank] = base;
@@ -1479,7 +1489,9 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
 
 // Rows without filters, more of them than blocks of sample_kernel are there at a time: a block a row with no more shared
 // memory than the sums of its steps and two steps a warp, so that four are on an SM.  They end apart, and one's end (a
-// search, a step read again) is hidden behind the others' sums.  512 rows of 150001: LEAN_US us, 91 with sample_kernel.
+// search, a step read again) is hidden behind the others' sums.  us, this kernel against sample_kernel: 512 rows of
+// 150001 bf16, greedy 43, 53, temperature alone 93, 91 (the sums' instructions); 1000 of 32000 fp32 32, 54 and 56, 60;
+// 2000 of 1000 fp32 18, 54 and 35, 53.
 template <bool BF16>
 __global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(const __grid_constant__ SampleParams P) {
     using S = Step<BF16>;

@@ -248,6 +248,27 @@ def test_masked_rows(bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("R", [6, 320])
+@pytest.mark.parametrize("V", [2500, 4096, 6001, 10000, 33000])
+def test_steps_without_a_value(R, V, bf16):
+    """Rows that leave some of a block's warps nothing, by their length or by a mask of whole stretches."""
+    import torch
+    rng = np.random.default_rng(V + R + bf16)
+    x = rng.normal(0, 2, (R, V)).astype(np.float32)
+    for r in range(R):
+        step = 1024 if bf16 else 512
+        if r % 3 == 1:
+            x[r, :step * (1 + r % 4)] = -np.inf
+        elif r % 3 == 2:                               # every other stretch, from the second on
+            x[r].reshape(-1)[np.arange(V) // step % 2 == 1] = -np.inf
+    logits = torch.as_tensor(x).to(torch.bfloat16 if bf16 else torch.float32).cuda()
+    tau = np.where(np.arange(R) % 5 == 0, 0.0, 0.8)
+    k = np.array([0, 1, 50, 64, 130, 200, 256])[np.arange(R) % 7]
+    p = np.where(np.arange(R) % 2 == 0, 1.0, 0.7)
+    _check(logits, tau, k, p, 0.0, rng.random(R))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("V,more,at", [(1000, 24, 0), (1001, 0, 0), (1000, 1, 0), (999, 25, 3), (30001, 7, 1)])
 def test_rows_of_any_stride_and_alignment(V, more, at, bf16):
     require_gpu()

@@ -657,8 +657,9 @@ lora_status_t lora_add_norm(const lora_norm_args_t *args, int32_t T, void *strea
  * Parameters that are NaN count as absent, a uniform that is NaN as 0.  A logit of -inf is never taken, and
  * nor is one whose weight is below 2^-46; logits of +inf share the weight.  A row with a NaN, or of -inf
  * alone, gives the token -1 and the logprob NaN.
- * Weights are good to 1e-11 of themselves, sums are held in 64 bits.  The result does not depend on how the
- * rows are split but for borders that are closer than that.
+ * Weights are good to 1e-11 of themselves, sums are held in 64 bits, and a sum within 2^-34 of the border
+ * that top_p or uniform sets counts as on it (where many tokens are left to count: of a few, uniform's
+ * border is exact).  The result does not depend on how the rows are split but for borders that close.
  * Random numbers are the caller's: the same uniform gives the same token.
  * -------------------------------------------------------------------------------------- */
 enum { LORA_LOGITS_BF16 = 0, LORA_LOGITS_FP32 = 1 };

@@ -45,6 +45,9 @@ constexpr int SP_REST = 8;                    // blocks of a row in the second l
 constexpr int SP_BINS = 2048;                 // of the band path: 64 to a power of two below the largest
 constexpr int SP_MAX_V = (1 << 20) - 8;       // a row's steps have their sums in a list
 constexpr double SP_LOW = -46.0;              // a weight below 2^-46 counts as nothing
+// Sums nearer to each other than this, of themselves, count as equal: the weights' errors leave no more, and among equal
+// logits borders do fall together (half of two equal weights is the first of them, not a little more).
+constexpr double SP_SAME = 1.0 / (1ll << 34);
 constexpr double SP_ONE = 70368744177664.0;   // 2^46: the largest weight as a whole number
 constexpr double SP_MAGIC = 105553116266496.0;   // 1.5 * 2^46: sums with it are rounded to 1/64
 
@@ -747,7 +750,7 @@ __device__ __noinline__ void pick_from_sums(SampleShared &s, const SampleParams 
     }
     double total;
     double before = block_before<double>(sum, s.scan_d, total);
-    const double target = (double)R.u * total;
+    const double target = (double)R.u * total * (1.0 + SP_SAME);
     if (tid == 0) { s.found = P.segs; s.rest = 0.0; }
     __syncthreads();
     bool here = false;
@@ -1216,7 +1219,7 @@ __device__ __forceinline__ RowPlan plan_row(const SampleParams &P, int64_t row) 
     R.k = k > 0 && k < P.V ? k : R.greedy ? 1 : 0;
     const float p = R.greedy || !P.top_p ? 1.0f : __ldg(P.top_p + row), mp = R.greedy || !P.min_p ? 0.0f : __ldg(P.min_p + row);
     R.by_p = p < 1.0f;
-    R.p = R.by_p ? (double)fmaxf(p, 0.0f) : 1.0;
+    R.p = R.by_p ? (double)fmaxf(p, 0.0f) * (1.0 - SP_SAME) : 1.0;
     R.by_min = mp > 0.0f;
     R.low = R.by_min ? log2((double)fminf(mp, 1.0f)) : -INFINITY;
     R.u = fminf(fmaxf(__ldg(P.uniform + row), 0.0f), 1.0f);

@@ -183,6 +183,26 @@ def test_ties_go_to_the_lowest_index(R, k, p, mp, kind):
     _check(x, 0.0, k, p, mp, u)
 
 
+@pytest.mark.parametrize("R", [4, 330])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V,held", [(345, 2), (345, 4), (1024, 1024), (5000, 4096), (40000, 64), (40000, 32768)])
+def test_borders_that_fall_together(R, bf16, V, held):
+    """Equal logits, a power of two of them, and shares that are whole numbers of them: every sum in question is exact."""
+    import torch
+    at = np.sort(np.random.default_rng(V + held).permutation(V)[:held])
+    x = np.full(V, -np.inf, np.float32)
+    x[at] = -1.65625
+    logits = torch.as_tensor(x)[None].expand(R, V).to(torch.bfloat16 if bf16 else torch.float32).contiguous().cuda()
+    u = np.array([0.0, 0.25, 0.5, 0.75])[np.arange(R) % 4]
+    tau = np.array([1.0, 0.7, 1.3])[np.arange(R) % 3]
+    for p in (None, 0.5, np.where(np.arange(R) % 2, 0.5, 1.0)):
+        kept = held if p is None else np.where(np.broadcast_to(p, R) < 1, held // 2, held)
+        for k in (None, 0):
+            got, lp = _run(logits, tau, k, p, None, u)
+            np.testing.assert_array_equal(got, at[(u * kept).astype(int)])
+            np.testing.assert_allclose(lp, np.broadcast_to(-np.log(kept), R), rtol=2.0 ** -24, atol=4e-11)
+
+
 def test_zeros_of_both_signs_are_one_value():
     require_gpu()
     import torch

@@ -21,7 +21,7 @@
 //
 // 256 rows of 128000 fp32 (131 MB, 20 us at a copy's rate): greedy 37 us, top_k 50 48, top_k 200 64, min_p 0.1 41,
 // temperature alone 48, all kinds together with 30 or so wide nuclei 123.  512 rows of 150001 bf16, temperature
-// alone: 91 us, 22 instructions a value.  4 rows of 32000: 11 .. 18 us.
+// alone: 93 us, 22 instructions a value.  4 rows of 32000: 11 .. 18 us.
 #include <cooperative_groups.h>
 
 #include <cfloat>

@@ -1461,6 +1461,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x;
     fill_table(s);
     griddep_wait();
+    cluster_sync(cluster, C);                          // every block of the cluster runs: its shared memory may be written
     const uint32_t rows = min((uint32_t) * (volatile int32_t *)&P.queue->count, (uint32_t)P.R);
     // the next row is whichever cluster's comes first: not all of them need to be there at a time
     for (;;) {

@@ -349,6 +349,32 @@ def test_with_and_without_a_workspace(with_workspace):
     assert lb.launch_count() == before + (4 if with_workspace else 2)
 
 
+@pytest.mark.parametrize("R,V", [(150, 9001), (297, 20000), (700, 4097)])
+def test_second_launch_over_and_over(R, V):
+    """Every row is one for the second launch, call behind call with nothing between them: its clusters begin while those
+    of the last call end."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    x = _logits(R, V, R, peaks=False, spread=0.5)
+    tau, p = torch.ones(R, device="cuda"), torch.full((R,), 0.9, device="cuda")
+    u = torch.rand(30, R, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda")
+    token = torch.full((30, R), -7, dtype=torch.int32, device="cuda")
+    work = torch.zeros(lb.sample_workspace_bytes(R) // 4, dtype=torch.int32, device="cuda")
+    blocks = [lb.sample_args(logits=x, temperature=tau, top_p=p, uniform=u[i], token=token[i], workspace=work)
+              for i in range(30)]
+    before = lb.launch_count()
+    for b in blocks:
+        lb.sample(b, R)
+    torch.cuda.synchronize()
+    assert lb.launch_count() == before + 60 and not work[:4].any()
+    xs, us, got = x.cpu().numpy(), u.cpu().numpy(), token.cpu().numpy()
+    for r in range(0, R, 7):
+        for i in (0, 14, 29):
+            assert got[i, r] == _reference(xs[r], 1.0, 0, np.float32(0.9), 0.0, us[i, r])[0], (i, r)
+    assert ((got >= 0) & (got < V)).all()
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

@@ -91,6 +91,7 @@ struct SampleShared {
     double scan_d[SP_WARPS];
     int32_t n, failed_here;
     uint32_t threshold, best;    // what candidates are not below, and the block's largest so far, as keys
+    uint32_t begin;              // the largest of its first steps: what sums are taken against, so nothing raises it later
     uint32_t warp_threshold[4][SP_WARPS];    // for m = 8, 4, 2, 1
     uint32_t key_min, key_max;
     int32_t pick_bin, pick_above, pick_kept;
@@ -1271,7 +1272,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     if (tid == 0) {
         s.n = s.failed_here = s.merged = 0;
         s.threshold = key_of(-FLT_MAX);
-        s.best = 0;
+        s.best = s.begin = 0;
     }
     if (tid < 4 * SP_WARPS) (&s.warp_threshold[0][0])[tid] = 0;
     __syncthreads();
@@ -1286,9 +1287,9 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     // What sums are taken against: the largest of the first steps, as a power of two.
     auto set_base = [&](float step_top) {
         const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
-        if (lane == 0) atomicMax(&s.best, k);
+        if (lane == 0) atomicMax(&s.begin, k);
         __syncthreads();
-        const float b = s.best ? value_of(s.best) : 0.0f;
+        const float b = s.begin ? value_of(s.begin) : 0.0f;
         base = rint((double)b * c);
         if (!(fabs(base) < 1e12)) base = 0.0;
         magic = SP_MAGIC - base;
@@ -1516,7 +1517,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(c
         __syncthreads();
         if (tid == 64) s.plan = plan_row(P, row);
         if (tid == 0) {
-            s.best = 0;
+            s.best = s.begin = 0;
             s.pick_here = 0;
         }
         __syncthreads();
@@ -1544,9 +1545,9 @@ __global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(c
             if (!add) continue;
             if (it == 0) {
                 const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
-                if (lane == 0) atomicMax(&s.best, k);
+                if (lane == 0) atomicMax(&s.begin, k);
                 __syncthreads();
-                base = rint((double)(s.best ? value_of(s.best) : 0.0f) * c);
+                base = rint((double)(s.begin ? value_of(s.begin) : 0.0f) * c);
                 if (!(fabs(base) < 1e12)) base = 0.0;
                 magic = SP_MAGIC - base;
                 floor_l = (float)fmax((base - 1000.0) / c, -(double)FLT_MAX);

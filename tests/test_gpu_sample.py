@@ -375,6 +375,29 @@ def test_second_launch_over_and_over(R, V):
     assert ((got >= 0) & (got < V)).all()
 
 
+@pytest.mark.parametrize("R", [20, 150, 290, 600])
+@pytest.mark.parametrize("p", [None, 0.05])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_rows_whose_values_rise(R, p, bf16):
+    """What a block's sums are taken against comes from its first steps, and later ones hold far larger values: every row
+    is the same one, so that each warp's view of it shows as a row that differs."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    V = 60001
+    x = torch.linspace(-150, 3, V, device="cuda") + torch.rand(V, generator=torch.Generator(device="cuda").manual_seed(R), device="cuda")
+    x = x.bfloat16() if bf16 else x
+    want, want_lp, _ = _reference(x.float().cpu().numpy(), 1.0, 0, 1.0 if p is None else np.float32(p), 0.0, 0.375)
+    rows, one = x.expand(R, V).contiguous(), torch.ones(R, device="cuda")
+    u, share = torch.full((R,), 0.375, device="cuda"), None if p is None else torch.full((R,), p, device="cuda")
+    token, lp = torch.empty(20, R, dtype=torch.int32, device="cuda"), torch.empty(20, R, device="cuda")
+    for i in range(20):
+        lb.sample(lb.sample_args(logits=rows, temperature=one, top_p=share, uniform=u, token=token[i], logprob=lp[i]), R,
+                  stream=torch.cuda.current_stream())
+    assert (token == want).all() and (lp == lp[0, 0]).all()
+    assert abs(float(lp[0, 0]) - want_lp) <= 4e-11 + 2.0 ** -24 * abs(want_lp)
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

@@ -83,6 +83,14 @@ struct RowPlan {
     bool greedy, by_p, by_min, list, sums, segments;
 };
 
+// A sum of weights of a whole vocabulary: in units of 2^-43 and, what these leave of each weight, of 2^-83.  2^20 weights
+// of 1 at most make 2^63, their rests less than 2^60; a weight of 2^-46 is there to 2^-37 of itself.
+struct Exact {
+    unsigned long long units, rest;
+    __device__ __forceinline__ double value() const { return fma((double)units, 1099511627776.0, (double)rest); }   // in units of 2^-83
+    __device__ __forceinline__ Exact operator+(const Exact &o) const { return {units + o.units, rest + o.rest}; }
+};
+
 struct SampleShared {
     RowPlan plan;
     double table[64 * 16];       // 2^(i / 64), once for each pair of banks
@@ -95,7 +103,8 @@ struct SampleShared {
     uint32_t warp_threshold[4][SP_WARPS];    // for m = 8, 4, 2, 1
     uint32_t key_min, key_max;
     int32_t pick_bin, pick_above, pick_kept;
-    uint64_t pick_count, pick_weight, pick_here;
+    uint64_t pick_count, pick_here;
+    Exact pick_weight;
     int32_t found;
     double rest;
     // written by the blocks of the cluster to the first one
@@ -115,7 +124,7 @@ struct SampleShared {
     union {
         uint4 ring[SP_WARPS][SP_STAGES][4][32];   // steps on their way from memory
         struct {                                  // general path
-            uint64_t digit_weight[2][256];
+            Exact digit_weight[2][256];
             uint32_t digit_count[2][256];
         };
         struct {                                  // (first block) band path: of the whole row
@@ -161,6 +170,12 @@ __device__ __forceinline__ double weight_of(double t, const double *table) {
     return t >= SP_LOW ? power2(t, 1.0, SP_MAGIC, table) : 0.0;        // (not a number: nothing)
 }
 __device__ __forceinline__ uint64_t whole(double w) { return (uint64_t)(w * SP_ONE); }
+
+__device__ __forceinline__ Exact exact(double w) {
+    const double units = w * 8796093022208.0;                          // 2^43
+    const uint64_t u = (uint64_t)units;
+    return {u, (uint64_t)((units - (double)u) * 1099511627776.0)};
+}
 
 __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
 
@@ -1094,17 +1109,18 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
     const int tid = threadIdx.x, warp = tid >> 5;
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     SampleCut to = {256, 0};
-    uint64_t base_count = 0, base_weight = 0;
+    uint64_t base_count = 0;
+    Exact base_weight = {0, 0};
     double need = weight ? 0.0 : (double)G.R.k;
     for (int level = 0; level < 8; ++level) {
         // (a digit's sums are read by the whole cluster while the next one's are taken: two sets in turn)
         uint32_t *const digit_count = s.digit_count[turn];
-        uint64_t *const digit_weight = s.digit_weight[turn];
+        Exact *const digit_weight = s.digit_weight[turn];
         turn ^= 1;
         const int shift = level <= 4 ? 64 - 8 * level : 56 - 8 * level;
         if (level == 5) to.from |= 0xff000000u;          // an index has 24 bits, and stands there as its complement
         digit_count[tid] = 0;
-        digit_weight[tid] = 0;
+        digit_weight[tid] = {0, 0};
         __syncthreads();
         for (int it = 0; it < P.steps; ++it) {
             const int32_t seg = (it * C + rank) * SP_WARPS + warp;
@@ -1125,23 +1141,30 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
                     digit = 255 - (int)(entry >> shift & 255u);
                 }
                 atomicAdd(&digit_count[digit], 1u);
-                if (weight)
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&digit_weight[digit]),
-                              (unsigned long long)whole(weight_of(exponent_of(l, G.m, G.R.c), s.table)));
+                if (weight) {
+                    const Exact w = exact(weight_of(exponent_of(l, G.m, G.R.c), s.table));
+                    atomicAdd(&digit_weight[digit].units, w.units);
+                    if (w.rest) atomicAdd(&digit_weight[digit].rest, w.rest);
+                }
             }
         }
         cluster_sync(cluster, C);
-        uint64_t count = 0, sum = 0;
+        uint64_t count = 0;
+        Exact sum = {0, 0};
         for (int r = 0; r < C; ++r) {
             count += *cluster.map_shared_rank(digit_count + tid, r);
-            sum += *cluster.map_shared_rank(digit_weight + tid, r);
+            sum = sum + *cluster.map_shared_rank(digit_weight + tid, r);
         }
-        uint64_t counts, sums;
+        uint64_t counts, units, rests;
         const uint64_t count_before = block_before<uint64_t>(count, s.scan_u, counts);
-        const uint64_t sum_before = block_before<uint64_t>(sum, s.scan_u, sums);
-        if (weight && level == 0) need = G.R.p * (double)sums;
-        const double reached = weight ? (double)(base_weight + sum_before + sum) : (double)(base_count + count_before + count);
-        const double before = weight ? (double)(base_weight + sum_before) : (double)(base_count + count_before);
+        Exact sum_before = base_weight;
+        if (weight) {
+            const uint64_t units_before = block_before<uint64_t>(sum.units, s.scan_u, units);
+            sum_before = sum_before + Exact{units_before, block_before<uint64_t>(sum.rest, s.scan_u, rests)};
+            if (level == 0) need = G.R.p * Exact{units, rests}.value();
+        }
+        const double reached = weight ? (sum_before + sum).value() : (double)(base_count + count_before + count);
+        const double before = weight ? sum_before.value() : (double)(base_count + count_before);
         if (tid == 0) s.found = 256;
         __syncthreads();
         if (count && (before < need || (count_before == 0 && base_count == 0)) && reached >= need) atomicMin(&s.found, tid);
@@ -1150,7 +1173,7 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
         if (digit == 256) return level == 0 ? cut : to;      // all of it
         if (tid == digit) {
             s.pick_count = base_count + count_before;
-            s.pick_weight = base_weight + sum_before;
+            s.pick_weight = sum_before;
             s.pick_here = count;
         }
         __syncthreads();

@@ -398,6 +398,64 @@ def test_rows_whose_values_rise(R, p, bf16):
     assert abs(float(lp[0, 0]) - want_lp) <= 4e-11 + 2.0 ** -24 * abs(want_lp)
 
 
+def _same_rows(x, R, tau, p, mp, us, workspace=True):
+    """R copies of one row, with the numbers `us` in turn: every token and logprob against the definition."""
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    rows = x.expand(R, x.shape[0]).contiguous()
+    us = np.asarray(us, np.float32)
+    u = torch.as_tensor(us[np.arange(R) % len(us)]).cuda()
+    token, lp = torch.full((R,), -7, dtype=torch.int32, device="cuda"), torch.empty(R, device="cuda")
+
+    def each(a):
+        return None if a is None else torch.full((R,), a, device="cuda")
+
+    args = lb.sample_args(logits=rows, temperature=each(tau), top_p=each(p), min_p=each(mp), uniform=u, token=token, logprob=lp)
+    if not workspace:
+        args.workspace = None
+    lb.sample(args, R, stream=torch.cuda.current_stream())
+    got, got_lp, host = token.cpu().numpy(), lp.cpu().numpy(), x.float().cpu().numpy()
+    for i, v in enumerate(us):
+        want, want_lp, _ = _reference(host, np.float32(tau), 0, 1.0 if p is None else np.float32(p),
+                                      0.0 if mp is None else np.float32(mp), v)
+        assert (got[i::len(us)] == want).all(), (tau, p, mp, v, got[i::len(us)][:4], want)
+        assert (np.abs(got_lp[i::len(us)] - want_lp) <= 4e-11 + 2.0 ** -24 * abs(want_lp)).all(), (tau, p, mp, v)
+
+
+@pytest.mark.parametrize("V", [262143, 262144, 262208, 300000, 1048568])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("R,workspace", [(1, True), (300, True), (300, False)])
+def test_flat_rows_of_large_vocabularies(R, workspace, V, bf16):
+    """Rows whose weights add up to 2^18 times the largest and more: equal logits, and ordinary ones at a temperature of 100."""
+    require_gpu()
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(V)
+    for tau, x in ((1.0, torch.full((V,), -3.25, device="cuda")), (100.0, 2 * torch.randn(V, generator=g, device="cuda"))):
+        for p, mp in ((0.5, None), (0.9, None), (0.9, 0.3)):
+            _same_rows(x.bfloat16() if bf16 else x, R, tau, p, mp, [0.05, 0.317, 0.77][:R], workspace)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_shares_of_many_small_weights(bf16):
+    """One token with nearly all the weight, a million others with 10^-12 of it each: top_p ends among them.  A border may
+    be taken 2^-34 of the sum too early (top_p) and too late (uniform), which is 50 of these tokens each."""
+    require_gpu()
+    import torch
+    V = 1000003
+    x = torch.full((V,), -27.5, device="cuda")
+    x[777] = 0.0
+    x = x.bfloat16() if bf16 else x
+    p, u, w = 1 - 2.0 ** -21, 1 - 2.0 ** -24, np.exp(-27.5)
+    kept = np.ceil((p * (1 + (V - 1) * w) - 1) / w)              # of the small ones, by hand: sums one by one would drift
+    want = int((u * (1 + kept * w) - 1) / w) + 1
+    want_lp = np.log(w / (1 + kept * w))
+    got, lp = _run(x.expand(3, V).contiguous(), 1.0, None, p, None, u)
+    most = 2 * 2.0 ** -34 / w
+    assert (np.abs(got - want) <= most + 2).all(), (got, want, most)
+    # the sum of what is kept is 1 and 10^-6 at most, so the tokens more or less do not show in its logarithm
+    assert (np.abs(lp - want_lp) <= 2.0 ** -24 * abs(want_lp) + 2 ** -33).all()
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

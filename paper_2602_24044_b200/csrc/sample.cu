@@ -110,7 +110,7 @@ struct SampleShared {
     // written by the blocks of the cluster to the first one
     uint32_t top[SP_CLUSTER], cut[SP_CLUSTER];
     int32_t bad[SP_CLUSTER], failed[SP_CLUSTER];
-    double sum[SP_CLUSTER], base[SP_CLUSTER];
+    double sum[SP_CLUSTER], above[SP_CLUSTER];
     int32_t merged;
     // of the first block: what turns the blocks' sums into sums against the largest value
     double scale[SP_CLUSTER];
@@ -178,6 +178,35 @@ __device__ __forceinline__ Exact exact(double w) {
 }
 
 __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
+
+// What the sums of a block (or, in the band path, a row) are taken against: a power of two 2^base next to the weight of
+// its largest value `top` so far; values below `low` are taken for it, so that exponents do not leave the numbers.  `c` is
+// the row's, but no more than makes neighbouring fp32 numbers around `top` 2^7 apart: values that differ are as good as
+// nothing beside the larger one either way, and |top c| stays below 2^31, where `low`, rounded to fp32, is within 2^7.1 of
+// the 800 that it is meant to lie below the base.
+struct SumBase {
+    double c, base, magic;
+    float low;
+    __device__ __forceinline__ SumBase() : c(0.0), base(0.0), magic(SP_MAGIC), low(-FLT_MAX) {}
+    __device__ __forceinline__ SumBase(float top, double row_c) {
+        c = row_c;
+        base = rint((double)top * c);
+        if (fabs(base) < 1e12) {                                       // a spacing is 2^(e - 150), e the biased exponent
+            const int e = max((int)(__float_as_uint(top) >> 23 & 255u), 1);
+            c = fmin(c, __hiloint2double((1023 + 157 - e) << 20, 0));
+            base = rint((double)top * c);
+        } else {
+            base = 0.0;
+        }
+        magic = SP_MAGIC - base;
+        low = (float)fmax((base - 800.0) / c, -(double)FLT_MAX);
+    }
+    __device__ __forceinline__ double weight(float l, const double *table) const {
+        return power2((double)fmaxf(l, low), c, magic, table);
+    }
+    // the exponent of a value against the base: what sums are turned by, if it is not far from it
+    __device__ __forceinline__ double above(float l) const { return fma((double)l, c, -base); }
+};
 
 struct SampleRow { const char *base; int32_t off, end; };       // see Step::load
 
@@ -966,9 +995,9 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     double *const sums = reinterpret_cast<double *>(s.list) + MOST_BAND;
     // weights as in the first reading: against the power of two next to the largest, turned into weights against it at
     // the end (what min_p leaves is decided by the exact exponent)
-    const double base = rint((double)m * R.c), magic = SP_MAGIC - base, turn = exp2(fma(-(double)m, R.c, base));
-    const float floor_l = (float)fmax((base - 1000.0) / R.c, -(double)FLT_MAX);
-    const bool far = !(fabs(base) < 1e12), by_min = R.by_min;
+    const SumBase B(m, R.c);
+    const double turn = exp2(-B.above(m));
+    const bool far = !(fabs(B.above(m)) < 1.0), by_min = R.by_min;
     double between = 0.0;                      // where the weight of all is not known: what is behind top_p's band and in front of that of the first k
     read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t seg, int it) {
         double sum = 0.0, rest = 0.0;
@@ -977,7 +1006,7 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
         for (int e = 0; e < S::N; ++e) {
             const float l = x.value(e);
             const int b = bin_of(l);
-            double w = power2((double)fmaxf(l, floor_l), R.c, magic, s.table);
+            double w = B.weight(l, s.table);
             if (by_min && !(exponent_of(l, m, R.c) >= R.low)) w = 0.0;
             sum += b < p_first ? w : 0.0;
             if (!known) rest += b > p_last && b < k_bin ? w : 0.0;
@@ -1301,22 +1330,17 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
     __syncthreads();
     const RowPlan &R = s.plan;
     const bool sums = R.sums, by_min = R.by_min;
-    const double c = R.c;
     bool list = R.list;
     float top = -INFINITY, top1 = -INFINITY, t = -FLT_MAX;
-    double sum = 0.0, base = 0.0, magic = SP_MAGIC;
-    float floor_l = -FLT_MAX;
+    double sum = 0.0;
+    SumBase B;
     double *const segs = reinterpret_cast<double *>(s.list);
     // What sums are taken against: the largest of the first steps, as a power of two.
     auto set_base = [&](float step_top) {
         const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
         if (lane == 0) atomicMax(&s.begin, k);
         __syncthreads();
-        const float b = s.begin ? value_of(s.begin) : 0.0f;
-        base = rint((double)b * c);
-        if (!(fabs(base) < 1e12)) base = 0.0;
-        magic = SP_MAGIC - base;
-        floor_l = (float)fmax((base - 1000.0) / c, -(double)FLT_MAX);
+        B = SumBase(s.begin ? value_of(s.begin) : 0.0f, R.c);
     };
     if (R.segments)
         read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t, int it) {
@@ -1327,7 +1351,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
             if (it == 0) set_base(step_top);
             double w = 0.0;
 #pragma unroll
-            for (int e = 0; e < S::N; ++e) w += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
+            for (int e = 0; e < S::N; ++e) w += B.weight(x.value(e), s.table);
 #pragma unroll
             for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
             if (lane == 0) segs[it * SP_WARPS + warp] = w;
@@ -1344,7 +1368,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
             if (sums) {
                 if (it == 0) set_base(step_top);
 #pragma unroll
-                for (int e = 0; e < S::N; ++e) sum += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
+                for (int e = 0; e < S::N; ++e) sum += B.weight(x.value(e), s.table);
             }
             if (!list) return;
             if (by_min) {
@@ -1402,7 +1426,7 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
         first.cut[rank] = threshold;
         first.failed[rank] = list != R.list || s.found + n > SP_LIST;
         first.sum[rank] = block_sum;
-        first.base[rank] = base;
+        first.above[rank] = B.above(value_of(s.best));
     }
     __syncthreads();
     for (int i = tid; i < n && s.found + i < SP_LIST; i += SP_THREADS) first.merge[s.found + i] = s.list[i];
@@ -1426,9 +1450,8 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_kernel(const __g
                 bool in_range = true;
                 for (int i = 0; i < C; ++i) {
                     const float l = value_of(s.top[i]);
-                    const double b = s.base[i];
-                    if (l > -INFINITY) in_range = in_range && fabs((double)l * R.c - b) < 900.0;
-                    if (tid == i) s.scale[i] = l > -INFINITY ? exp2(fma(-(double)m, R.c, b)) : 0.0;
+                    if (l > -INFINITY) in_range = in_range && fabs(s.above[i]) < 900.0;
+                    if (tid == i) s.scale[i] = l > -INFINITY ? exp2(exponent_of(l, m, R.c) - s.above[i]) : 0.0;
                 }
                 __syncthreads();
                 failed = failed || !in_range;
@@ -1547,8 +1570,8 @@ __global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(c
         const RowPlan &R = s.plan;
         const double c = R.c;
         const bool add = R.sums, greedy = R.k == 1;
-        float top = -INFINITY, floor_l = -FLT_MAX;
-        double base = 0.0, magic = SP_MAGIC;
+        float top = -INFINITY;
+        SumBase B;
         uint64_t best = 0;
         for (int it = 0; it < P.steps; ++it) {
             const int32_t seg = it * SP_WARPS + warp;
@@ -1570,14 +1593,11 @@ __global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(c
                 const uint32_t k = __reduce_max_sync(0xffffffffu, step_top > -INFINITY ? key_of(step_top) : 0u);
                 if (lane == 0) atomicMax(&s.begin, k);
                 __syncthreads();
-                base = rint((double)(s.begin ? value_of(s.begin) : 0.0f) * c);
-                if (!(fabs(base) < 1e12)) base = 0.0;
-                magic = SP_MAGIC - base;
-                floor_l = (float)fmax((base - 1000.0) / c, -(double)FLT_MAX);
+                B = SumBase(s.begin ? value_of(s.begin) : 0.0f, c);
             }
             double w = 0.0;
 #pragma unroll
-            for (int e = 0; e < S::N; ++e) w += power2((double)fmaxf(x.value(e), floor_l), c, magic, s.table);
+            for (int e = 0; e < S::N; ++e) w += B.weight(x.value(e), s.table);
 #pragma unroll
             for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
             if (lane == 0 && seg < P.segs) sums[seg] = w;
@@ -1594,13 +1614,13 @@ __global__ void __launch_bounds__(SP_THREADS, SP_SUM_BLOCKS) sample_sum_kernel(c
         const float m = value_of(s.best);
         if (bad || greedy) {
             if (tid == 0) answer(P, row, bad ? -1 : index_of(s.pick_here), bad ? nan_value() : 0.0);
-        } else if (!add || !(fabs((double)m * c - base) < 900.0)) {
+        } else if (!add || !(fabs(B.above(m)) < 900.0)) {
             if (tid == 0) {
                 const uint32_t at = (uint32_t)atomicAdd(&P.queue->count, 1);
                 if (at < (uint32_t)P.R) P.queue->rows[at] = {(int32_t)row, m, nan_value()};
             }
         } else {
-            const double scale = exp2(fma(-(double)m, c, base));
+            const double scale = exp2(-B.above(m));
             for (int g = tid; g < P.segs; g += SP_THREADS) sums[g] *= scale;
             __syncthreads();
             pick_from_sums<BF16>(s, P, R, row, logits, sums,

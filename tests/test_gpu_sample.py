@@ -456,6 +456,25 @@ def test_shares_of_many_small_weights(bf16):
     assert (np.abs(lp - want_lp) <= 2.0 ** -24 * abs(want_lp) + 2 ** -33).all()
 
 
+@pytest.mark.parametrize("V", [345, 40000])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("R", [4, 320])
+@pytest.mark.parametrize("top,ties", [(20.0, 1), (20.0, 3), (-20.0, 2), (1e4, 1), (1e4, 4), (-0.375, 3)])
+def test_temperatures_next_to_nothing(R, bf16, V, top, ties):
+    """Values next to each other are many powers of two apart: what is not among the largest has no weight."""
+    require_gpu()
+    import torch
+    rng = np.random.default_rng(V + ties)
+    x = torch.as_tensor((top - 0.5 - np.abs(rng.normal(0, 3, V))).astype(np.float32)).cuda()
+    x = x.bfloat16() if bf16 else x
+    x[torch.as_tensor(rng.permutation(V)[:ties]).cuda()] = top
+    below = torch.full((), top, dtype=x.dtype).nextafter(torch.full((), -float("inf"), dtype=x.dtype))
+    x[int(rng.integers(V // 2))] = float(below)
+    for tau in (1e-5, 1e-6, 1e-7, 1e-8, 1e-9, 1e-10, 1e-11, 1e-12):
+        for p in (None, 0.6):
+            _same_rows(x, R, tau, p, None, [0.0, 0.2, 0.55, 0.9])
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

@@ -83,11 +83,11 @@ struct RowPlan {
     bool greedy, by_p, by_min, list, sums, segments;
 };
 
-// A sum of weights of a whole vocabulary: in units of 2^-43 and, what these leave of each weight, of 2^-83.  2^20 weights
-// of 1 at most make 2^63, their rests less than 2^60; a weight of 2^-46 is there to 2^-37 of itself.
+// A sum of weights of a whole vocabulary, 2^20 of them at most: in units of 2^-43 (so 2^63 is the most there can be) and, what
+// is left beside these, of 2^-75.
 struct Exact {
-    unsigned long long units, rest;
-    __device__ __forceinline__ double value() const { return fma((double)units, 1099511627776.0, (double)rest); }   // in units of 2^-83
+    uint64_t units, rest;
+    __device__ __forceinline__ double value() const { return fma((double)units, 4294967296.0, (double)rest); }   // in units of 2^-75
     __device__ __forceinline__ Exact operator+(const Exact &o) const { return {units + o.units, rest + o.rest}; }
 };
 
@@ -124,7 +124,7 @@ struct SampleShared {
     union {
         uint4 ring[SP_WARPS][SP_STAGES][4][32];   // steps on their way from memory
         struct {                                  // general path
-            Exact digit_weight[2][256];
+            uint32_t digit_weight[2][256][3];         // in units of 2^-75
             uint32_t digit_count[2][256];
         };
         struct {                                  // (first block) band path: of the whole row
@@ -171,10 +171,18 @@ __device__ __forceinline__ double weight_of(double t, const double *table) {
 }
 __device__ __forceinline__ uint64_t whole(double w) { return (uint64_t)(w * SP_ONE); }
 
-__device__ __forceinline__ Exact exact(double w) {
+// Adds a weight to a sum of three words in shared memory, whose carries each go with the addition that made them.  (An
+// addition of 64 bits there is a loop in which lanes with one sum wait for one another: with two of them a row of 128000
+// equal logits took 4450 us for 311, one at a temperature of 100 1100 for 207.)
+__device__ __forceinline__ void add_weight(uint32_t *sum, double w) {
     const double units = w * 8796093022208.0;                          // 2^43
-    const uint64_t u = (uint64_t)units;
-    return {u, (uint64_t)((units - (double)u) * 1099511627776.0)};
+    uint64_t u = (uint64_t)units;
+    const uint32_t r = (uint32_t)((units - (double)u) * 4294967296.0);
+    if (r && atomicAdd(&sum[0], r) + r < r) ++u;
+    const uint32_t low = (uint32_t)u;
+    uint32_t high = (uint32_t)(u >> 32);
+    if (low && atomicAdd(&sum[1], low) + low < low) ++high;
+    if (high) atomicAdd(&sum[2], high);
 }
 
 __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7ff8000000000000ll); }
@@ -1144,12 +1152,12 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
     for (int level = 0; level < 8; ++level) {
         // (a digit's sums are read by the whole cluster while the next one's are taken: two sets in turn)
         uint32_t *const digit_count = s.digit_count[turn];
-        Exact *const digit_weight = s.digit_weight[turn];
+        uint32_t (*const digit_weight)[3] = s.digit_weight[turn];
         turn ^= 1;
         const int shift = level <= 4 ? 64 - 8 * level : 56 - 8 * level;
         if (level == 5) to.from |= 0xff000000u;          // an index has 24 bits, and stands there as its complement
         digit_count[tid] = 0;
-        digit_weight[tid] = {0, 0};
+        digit_weight[tid][0] = digit_weight[tid][1] = digit_weight[tid][2] = 0;
         __syncthreads();
         for (int it = 0; it < P.steps; ++it) {
             const int32_t seg = (it * C + rank) * SP_WARPS + warp;
@@ -1170,11 +1178,7 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
                     digit = 255 - (int)(entry >> shift & 255u);
                 }
                 atomicAdd(&digit_count[digit], 1u);
-                if (weight) {
-                    const Exact w = exact(weight_of(exponent_of(l, G.m, G.R.c), s.table));
-                    atomicAdd(&digit_weight[digit].units, w.units);
-                    if (w.rest) atomicAdd(&digit_weight[digit].rest, w.rest);
-                }
+                if (weight) add_weight(digit_weight[digit], weight_of(exponent_of(l, G.m, G.R.c), s.table));
             }
         }
         cluster_sync(cluster, C);
@@ -1182,7 +1186,8 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
         Exact sum = {0, 0};
         for (int r = 0; r < C; ++r) {
             count += *cluster.map_shared_rank(digit_count + tid, r);
-            sum = sum + *cluster.map_shared_rank(digit_weight + tid, r);
+            const uint32_t *w = cluster.map_shared_rank(&digit_weight[tid][0], r);
+            sum = sum + Exact{(uint64_t)w[2] << 32 | w[1], w[0]};
         }
         uint64_t counts, units, rests;
         const uint64_t count_before = block_before<uint64_t>(count, s.scan_u, counts);

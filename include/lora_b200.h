@@ -681,7 +681,8 @@ typedef struct {
  * in a second launch; without one they take their time.  It is zeroed by the caller once, before its first use, and
  * every call leaves it so; calls on one workspace must be ordered on one stream. */
 lora_status_t lora_sample_workspace_bytes(int32_t R, size_t *bytes);
-/* No output may overlap anything.  R <= 2^24.  Errors: INVALID_ARG, SHAPE, BUFFER_TOO_SMALL (workspace), CUDA. */
+/* Neither an output nor the workspace may overlap anything.  R <= 2^24.  Errors: INVALID_ARG, SHAPE, BUFFER_TOO_SMALL
+ * (workspace), CUDA. */
 lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, void *stream);
 
 #ifdef __cplusplus

@@ -1715,22 +1715,27 @@ extern "C" lora_status_t lora_sample(const lora_sample_args_t *args, int32_t R, 
     if (!args->logits || !args->temperature || !args->uniform || !args->token) return LORA_ERR_INVALID_ARG;
     if (args->ld < args->vocab) return LORA_ERR_SHAPE;
     const int64_t unit = bf16 ? 2 : 4;
+    // no output lies on anything else, nor does the workspace (which is written too)
+    const int64_t row_words = 4 * (int64_t)R, logits_bytes = ((R - 1) * args->ld + args->vocab) * unit;
+    auto touch = [](const void *a, int64_t na, const void *b, int64_t nb) { return rows_overlap(a, na, na, b, nb, nb, 1); };
     const void *words[7] = {args->token, args->logprob, args->temperature, args->top_k, args->top_p, args->min_p, args->uniform};
     if ((uintptr_t)args->logits % unit) return LORA_ERR_INVALID_ARG;
     for (int i = 0; i < 7; ++i) {
         if (!words[i]) continue;
         if ((uintptr_t)words[i] & 3) return LORA_ERR_INVALID_ARG;
-        for (int o = 0; o < 2 && o < i; ++o)       // no output lies on anything else
-            if (words[o] && rows_overlap(words[o], 4 * (int64_t)R, 4 * (int64_t)R, words[i], 4 * (int64_t)R, 4 * (int64_t)R, 1))
-                return LORA_ERR_INVALID_ARG;
-        if (i < 2 && rows_overlap(words[i], 4 * (int64_t)R, 4 * (int64_t)R, args->logits,
-                                  ((R - 1) * args->ld + args->vocab) * unit, 8, 1))
-            return LORA_ERR_INVALID_ARG;
+        for (int o = 0; o < 2 && o < i; ++o)
+            if (words[o] && touch(words[o], row_words, words[i], row_words)) return LORA_ERR_INVALID_ARG;
+        if (i < 2 && touch(words[i], row_words, args->logits, logits_bytes)) return LORA_ERR_INVALID_ARG;
     }
     size_t need = 0;
     lora_sample_workspace_bytes(R, &need);
     if ((uintptr_t)args->workspace & 15) return LORA_ERR_INVALID_ARG;
-    if (args->workspace && args->workspace_bytes < need) return LORA_ERR_BUFFER_TOO_SMALL;
+    if (args->workspace) {
+        if (args->workspace_bytes < need) return LORA_ERR_BUFFER_TOO_SMALL;
+        if (touch(args->workspace, (int64_t)need, args->logits, logits_bytes)) return LORA_ERR_INVALID_ARG;
+        for (int i = 0; i < 7; ++i)
+            if (words[i] && touch(args->workspace, (int64_t)need, words[i], row_words)) return LORA_ERR_INVALID_ARG;
+    }
     SampleParams P;
     P.queue = (SampleQueue *)args->workspace;
     P.logits = args->logits;

@@ -32,6 +32,19 @@ def test_refusals(bad, status):
     assert e.value.status == status
 
 
+@pytest.mark.parametrize("other", ["token", "logprob", "temperature", "top_k", "top_p", "min_p", "uniform", "logits"])
+@pytest.mark.parametrize("before", [0, 4, 48])
+def test_workspace_on_other_memory_is_refused(other, before):
+    """64 bytes are written for three rows: they may not begin at, inside or at the end of anything else."""
+    kw = dict(logits=BASE, ld=1000, vocab=1000, logits_type=lb.LOGITS_FP32, token=BASE + (1 << 20),
+              temperature=BASE + (2 << 20), top_k=BASE + (3 << 20), top_p=BASE + (4 << 20), min_p=BASE + (5 << 20),
+              uniform=BASE + (6 << 20), logprob=BASE + (7 << 20), workspace=BASE + (8 << 20), workspace_bytes=64)
+    kw[other] = BASE + (8 << 20) + before
+    with pytest.raises(lb.LoraError) as e:
+        lb.sample(lb.sample_args(**kw), 3)
+    assert e.value.status == 1
+
+
 def test_workspace_bytes():
     assert lb.sample_workspace_bytes(0) == 16 and lb.sample_workspace_bytes(3) == 16 + 3 * 16
     for R in (-1, (1 << 24) + 1):

@@ -894,18 +894,20 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     constexpr int PER = SP_BINS / SP_THREADS, MOST_SUMS = 512, MOST_BAND = SP_LIST - MOST_SUMS;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const float m = s.row_max, c64 = (float)(R.c * 64.0);
+    const float m = s.row_max, c_bins = (float)(R.c * (64.0 / (SP_BINS - 1)));
     if (!(R.c > 1e-30) || !(fabsf(m) <= FLT_MAX) || P.steps * SP_WARPS > MOST_SUMS || !(R.k || R.by_p || R.by_min)) return false;
-    // A value's place below the largest, in 1/64 of a power of two, and the nearest bin; the last one is all the rest,
-    // masked tokens too.  (2^23 and a small number is the nearest whole one in the low bits: no conversions, which issue
-    // at an eighth of the rate.)
-    auto place = [&](float l) { return fminf((m - l) * c64, (float)(SP_BINS - 1)); };
-    auto bin_of = [&](float l) { return __float_as_int(place(l) + 8388608.0f) - 0x4b000000; };
+    // A value's place below the largest, as a part of all bins, and the nearest bin, each 1/64 of a power of two; the last
+    // one is all the rest, masked tokens too.  (2^23 and a small number is the nearest whole one in the low bits: no
+    // conversions, which issue at an eighth of the rate.  The place is clamped at both ends: in the second launch the largest
+    // comes from the caller's memory, and a value above it would have no bin.)
+    auto place = [&](float l) { return __saturatef((m - l) * c_bins); };
+    auto near_bin = [&](float f) { return fmaf(f, (float)(SP_BINS - 1), 8388608.0f); };
+    auto bin_of = [&](float l) { return __float_as_int(near_bin(place(l))) - 0x4b000000; };
     // (weights of a quarter of (1 - p) S / V, S that of all, make up less of it than top_p leaves out, all together: the
     // cut is in front of them.  An atomic addition in shared memory takes a cycle a lane, which is what this reading takes.)
     const bool known = s.total == s.total;
-    const float last = R.by_min ? fminf((float)(-R.low * 64.0), 1e30f)
-                       : known && R.by_p ? 64.0f * log2f((float)(4.0 * P.V / ((1.0 - R.p) * s.total))) : INFINITY;
+    const float last = R.by_min ? fminf((float)(-R.low * (64.0 / (SP_BINS - 1))), 1e30f)
+                       : known && R.by_p ? 64.0f / (SP_BINS - 1) * log2f((float)(4.0 * P.V / ((1.0 - R.p) * s.total))) : INFINITY;
     const bool by_k = R.k != 0, by_p = R.by_p;
     uint32_t *const counts = reinterpret_cast<uint32_t *>(s.list), *const weights = counts + SP_BINS;
     ask_first_steps<BF16>(s, P, logits, C, rank);
@@ -914,11 +916,11 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
     read_steps<BF16>(s, P, logits, C, rank, [&](const S &x, int32_t, int) {
 #pragma unroll
         for (int e = 0; e < S::N; ++e) {
-            const float f = place(x.value(e)), whole_f = f + 8388608.0f;
+            const float f = place(x.value(e)), whole_f = near_bin(f);
             const int b = __float_as_int(whole_f) - 0x4b000000;
             if (by_k) atomicAdd(&counts[b], 1u);
             // 2^(-r / 64) of the rest |r| <= 1/2, to its square
-            const float r = f - (whole_f - 8388608.0f);
+            const float r = fmaf(f, (float)(SP_BINS - 1), 8388608.0f - whole_f);
             if (by_p && f <= last)
                 atomicAdd(&weights[b], __float_as_uint(fmaf(r, fmaf(r, 3.843576f, -709.7827f), 65536.0f) + 8388608.0f) - 0x4b000000u);
         }

@@ -475,6 +475,33 @@ def test_temperatures_next_to_nothing(R, bf16, V, top, ties):
             _same_rows(x, R, tau, p, None, [0.0, 0.2, 0.55, 0.9])
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+def test_rows_noted_by_someone_else(bf16):
+    """A workspace that was not zeroed names rows of its own, with largest values below theirs: those rows' tokens are
+    anything, but tokens, and the other rows' are right."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    R, V, odd = 320, 20000, 6
+    x = _logits(R, V, 1, bf16, peaks=False)
+    one, u = torch.ones(R, device="cuda"), torch.rand(R, device="cuda")
+    p = torch.where(torch.arange(R, device="cuda") % 3 == 0, 0.95, 1.0)
+    words = np.zeros(lb.sample_workspace_bytes(R) // 4, np.int32)
+    words[0] = odd
+    noted = words[4:4 + 4 * odd].reshape(odd, 4)
+    noted[:, 0] = [0, 1, 2, 3, -5, R]
+    noted[:, 1] = np.array([-1000, -3e38, -1, -np.inf, 0, 0], np.float32).view(np.int32)
+    noted[:, 2:] = np.array([1.0, np.nan, -5.0, np.inf, 0, 0]).view(np.int32).reshape(odd, 2)
+    got = []
+    for work in (None, torch.as_tensor(words).cuda()):
+        token = torch.full((R,), 0, dtype=torch.int32, device="cuda")
+        lb.sample(lb.sample_args(logits=x, temperature=one, top_p=p, uniform=u, token=token, workspace=work), R,
+                  stream=torch.cuda.current_stream())
+        got.append(token.cpu().numpy())
+    assert np.array_equal(got[0][4:], got[1][4:])
+    assert ((got[1] >= -1) & (got[1] < V)).all()
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

@@ -131,6 +131,7 @@ class _SampleArgs(ctypes.Structure):
     max_tokens = 2 ** 31 - 1
     own_workspace = None                 # made here: kept for the streams of the calls
     streams = frozenset()
+    zero_first = False                   # made in a capture: no zeros before a call has put them there
 
 
 _handle = None
@@ -821,7 +822,8 @@ def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None
     rows; vocab, their type and leading dimension default to the tensor's.  The others hold one entry a row.  The
     tensors must stay alive while the block is used; it keeps them, and a call for more rows than they hold is
     refused.  workspace: made here where token is a tensor and none is given (calls with one block are then to be
-    ordered on one stream, as they share their outputs too)."""
+    ordered on one stream, as they share their outputs too; a block made in a graph's capture clears its first words
+    with every call; a block called on a bare stream handle is kept until that work is done)."""
     V = int(logits.shape[-1]) if vocab is None else int(vocab)
     ld = _ld("logits", logits, ld, V)
     kind = "bfloat16" if logits_type == LOGITS_BF16 else "float32"
@@ -845,7 +847,8 @@ def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None
             most = min(most, have)
     a.max_tokens = most
     if workspace is None and hasattr(token, "new_zeros"):
-        workspace = a.own_workspace = _zeros(token, sample_workspace_bytes(min(most, 1 << 24)))
+        workspace, a.zero_first = _zeros(token, sample_workspace_bytes(min(most, 1 << 24)))
+        a.own_workspace = workspace
     if workspace is not None:
         a.workspace = _ptr(workspace)
         a.workspace_bytes = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
@@ -853,12 +856,28 @@ def sample_args(*, logits, temperature, uniform, token, logprob=None, top_k=None
 
 
 def _zeros(like, nbytes: int):
-    """int32 zeros beside a device tensor, ready for calls on any stream."""
+    """(int32 zeros beside a device tensor, ready for calls on any stream; False), or in a graph's capture (memory, True):
+    zeros would be there from the graph's first replay on, and not for calls before that or in another graph."""
     import torch
+    if torch.cuda.is_current_stream_capturing():
+        return like.new_empty((nbytes + 3) // 4), True
     t = like.new_zeros((nbytes + 3) // 4)
-    if not torch.cuda.is_current_stream_capturing():
-        torch.cuda.current_stream(t.device).synchronize()
-    return t
+    torch.cuda.current_stream(t.device).synchronize()
+    return t, False
+
+
+def _torch_stream(stream, device):
+    import torch
+    if type(stream) is int and stream:
+        return torch.cuda.ExternalStream(stream, device)
+    return stream if stream else torch.cuda.default_stream(device)
+
+
+def _zero_counts(t, stream) -> None:
+    """The words that a sampling workspace begins with, on the stream of the call that follows."""
+    import torch
+    with torch.cuda.stream(_torch_stream(stream, t.device)):
+        t[:4].zero_()
 
 
 def _record(t, stream) -> None:
@@ -876,6 +895,8 @@ def sample(args, R: int, stream=None) -> None:
     if args.own_workspace is not None and stream not in args.streams:
         _record(args.own_workspace, stream)
         args.streams = args.streams | {stream}
+    if args.zero_first and args.workspace:
+        _zero_counts(args.own_workspace, stream)
     status = _lib().lora_sample(ctypes.byref(args), R, _stream(stream))
     if status:
         _check(status, "lora_sample")

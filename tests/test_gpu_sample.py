@@ -502,6 +502,37 @@ def test_rows_noted_by_someone_else(bf16):
     assert ((got[1] >= -1) & (got[1] < V)).all()
 
 
+def test_a_block_made_in_a_capture():
+    """Its workspace holds whatever was in that memory until the graph is replayed: calls outside of the graph, in another
+    graph and on other streams are right before that too."""
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    R, V = 320, 20000
+    x = _logits(R, V, 1, peaks=False)
+    kw = dict(logits=x, temperature=torch.ones(R, device="cuda"), uniform=torch.rand(R, device="cuda"),
+              top_p=torch.where(torch.arange(R, device="cuda") % 3 == 0, 0.95, 1.0))
+    want, token = (torch.empty(R, dtype=torch.int32, device="cuda") for _ in range(2))
+    lb.sample(lb.sample_args(token=want, **kw), R, stream=torch.cuda.current_stream())
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.graph(graphs[0]):
+        args = lb.sample_args(token=token, **kw)
+        lb.sample(args, R, stream=torch.cuda.current_stream())
+    with torch.cuda.graph(graphs[1]):
+        lb.sample(args, R, stream=torch.cuda.current_stream())
+    side = torch.cuda.Stream()
+    calls = [lambda: lb.sample(args, R), lambda: lb.sample(args, R, stream=torch.cuda.current_stream()),
+             lambda: lb.sample(args, R, stream=side), lambda: lb.sample(args, R, stream=side.cuda_stream),
+             lambda: lb.sample(args, R, stream=0), graphs[1].replay, graphs[0].replay, graphs[1].replay]
+    for call in calls:
+        args.own_workspace.fill_(1 << 20)
+        token.fill_(-7)
+        torch.cuda.synchronize()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(token, want)
+
+
 def test_a_graph_follows_its_inputs():
     require_gpu()
     import torch

@@ -277,6 +277,45 @@ def test_append_bits(D, P, hq, hk, T, inter):
         assert c.status()[0] == 1
 
 
+@pytest.mark.parametrize("D,P,hq,hk,T,rot", [(128, 16, 8, 2, 7, 64), (128, 32, 32, 8, 1500, 32), (64, 64, 7, 1, 40, 16),
+                                             (64, 16, 48, 16, 900, 32), (128, 16, 1, 1, 3, 112)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_append_of_heads_rotated_in_part(D, P, hq, hk, T, rot, inter):
+    require_gpu()
+    import torch
+    from paper_2602_24044_b200 import binding as lb
+    rng = np.random.default_rng(T + D + rot)
+    pages = -(-T // P) + 2
+    width = (hq + 2 * hk) * D
+    x = ref.bf16(rng.standard_normal((T, width)).astype(np.float32))
+    w = [ref.bf16((1 + 0.3 * rng.standard_normal(D)).astype(np.float32)) for _ in range(2)]
+    cs, axis = _angles(40, rot), rng.integers(0, 3, rot // 2)
+    pos = rng.integers(0, 40, (3, T)).astype(np.int32)
+    pos[1, T // 2] = -1                                                 # not rotated, and counted
+    slots = rng.permutation(pages * P)[:T].astype(np.int32)
+    xd = _dev(x, torch.bfloat16)
+    with _cache(num_pages=pages, page_size=P, num_q_heads=hq, num_kv_heads=hk, head_dim=D) as c:
+        q_out, k_out, k_back, v_back = (torch.empty((T, n * D), dtype=torch.bfloat16, device="cuda") for n in (hq, hk, hk, hk))
+        args = lb.qk_args(num_q_heads=hq, num_kv_heads=hk, head_dim=D, q=xd, ldq=width, k=xd[:, hq * D:], ldk=width,
+                          v=xd[:, (hq + hk) * D:], ldv=width, q_weight=_dev(w[0], torch.bfloat16),
+                          k_weight=_dev(w[1], torch.bfloat16), eps=1e-6, cos_sin=_dev(cs), interleaved=inter,
+                          positions=_i32(pos), axis_of_pair=axis, q_out=q_out, k_out=k_out)
+        c.append(0, args, _i32(slots), T)
+        lb.kv_read(c.kv, 0, _i32(slots), T, k_back, hk * D, v_back, hk * D)
+        turn = (pos >= 0).all(0)
+        row = _turned_by(cs, axis, np.where(turn, pos, 0))
+        k = None
+        for out, first, n, wt in ((q_out, 0, hq, w[0]), (k_out, hq, hk, w[1])):
+            y = ref.norm32(x[:, first * D:(first + n) * D].reshape(-1, D), wt, 1e-6)
+            k = np.where(np.repeat(turn, n)[:, None], ref.rotate(y, np.repeat(row, n, 0), rot, inter), y)
+            assert np.array_equal(_np(out).reshape(-1, D), ref.bf16(k))
+        for back, val in ((k_back, k), (v_back, x[:, (hq + hk) * D:].reshape(-1, D))):
+            code, scale, low = ref.quantise(val)
+            want = ref.bf16(np.float32(low)[:, None] + np.float32(scale)[:, None] * code.astype(np.float32))
+            assert np.array_equal(_np(back).reshape(-1, D), want)
+        assert c.status()[0] == 1
+
+
 def test_rotation_in_place_and_on_another_stream():
     require_gpu()
     import torch

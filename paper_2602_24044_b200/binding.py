@@ -652,7 +652,8 @@ def _set_axes(a, axis_of_pair, num_axes, ld_positions, positions) -> None:
     if len(axis) != a.rot_dim // 2 or min(axis, default=0) < 0 or max(axis, default=0) > 255:
         raise LoraError(2, "axis_of_pair (needs the axis of each of the %d rotation pairs)" % (a.rot_dim // 2))
     if hasattr(positions, "stride"):
-        if positions.dim() != 2 or (positions.stride(1) != 1 and positions.shape[1] > 1):
+        if (positions.dim() != 2 or (positions.stride(1) != 1 and positions.shape[1] > 1) or
+                (ld_positions is None and positions.shape[0] > 1 and positions.stride(0) < positions.shape[1])):
             raise LoraError(1, "positions (needs a row of tokens for each axis)")
         num_axes = int(positions.shape[0]) if num_axes is None else num_axes
         if ld_positions is None:

@@ -33,6 +33,17 @@ def test_rotation_refusals(bad, status):
     assert e.value.status == status
 
 
+def test_positions_that_share_memory_are_refused():
+    """Rows closer to each other than the tokens are many (one row expanded to all axes): their distance is no leading
+    dimension."""
+    import torch
+    buf = torch.zeros(5, 8, dtype=torch.int32)
+    for bad in (buf[:1].expand(3, 8), torch.as_strided(buf, (3, 8), (4, 1)), buf.t()[:3], buf[0]):
+        with pytest.raises(lb.LoraError, match="a row of tokens for each axis") as e:
+            lb.qk_args(num_q_heads=1, num_kv_heads=1, head_dim=64, rot_dim=64, axis_of_pair=[0, 1, 2, 0] * 8, positions=bad)
+        assert e.value.status == 1
+
+
 def test_null_arguments_are_rejected():
     a = lb.qk_args(num_q_heads=1, num_kv_heads=1, head_dim=64, rot_dim=64, axis_of_pair=[0] * 32, num_axes=1)
     lib = lb._lib()

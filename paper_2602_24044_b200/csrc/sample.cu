@@ -1513,10 +1513,11 @@ __global__ void __launch_bounds__(SP_THREADS, SP_BLOCKS) sample_rest_kernel(cons
     SampleShared &s = *reinterpret_cast<SampleShared *>(sample_smem);
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), tid = threadIdx.x;
+    cg::cluster_group::barrier_arrive();
     fill_table(s);
     griddep_wait();
-    cluster_sync(cluster, C);                          // every block of the cluster runs: its shared memory may be written
     const uint32_t rows = min((uint32_t) * (volatile int32_t *)&P.queue->count, (uint32_t)P.R);
+    cg::cluster_group::barrier_wait();                 // every block of the cluster runs: its shared memory may be written
     // the next row is whichever cluster's comes first: not all of them need to be there at a time
     for (;;) {
         if (rank == 0 && tid == 0) {

@@ -535,7 +535,8 @@ lora_status_t lora_kv_append(lora_kv_t *kv, int32_t layer, const lora_qk_args_t 
  * The same two with positions on several axes (time, height and width of image and video tokens): rotation
  * pair p of token t turns by the angles of row positions[axis_of_pair[p], t] of cos_sin.  args->positions is
  * then dev int32 [num_axes, ld_positions]; a token with a position outside 0 .. num_positions - 1 on any axis
- * is not rotated.  With equal positions on all axes the results are those of the calls above.
+ * is not rotated.  With equal positions on all axes the results are those of the calls above.  (The axes do not share
+ * memory: one row of positions for all of them is the calls above.)
  * Errors: those of the calls above (SHAPE: an axis that is not there, ld_positions < T).
  */
 #define LORA_ROPE_AXES_MAX 4
@@ -554,7 +555,8 @@ lora_status_t lora_kv_append_axes(lora_kv_t *kv, int32_t layer, const lora_qk_ar
  * ascending by their first token, each 8 words
  *     {first, frames, rows, columns, base, step, 0, 0} :
  * tokens first .. first + frames * rows * columns - 1 of the request are a grid of them, the columns fastest,
- * and base is the position that its first one has.  For a token at position p of its request, with the last
+ * and base is the position that its first one has.  A frame is `step` positions behind the one before, a whole
+ * number (frames a fraction of a position apart cannot be described).  For a token at position p of its request, with the last
  * span that begins at or before it and k = p - first:
  *     inside the span  (base + k / (rows * columns) * step,  base + k / columns % rows,  base + k % columns)
  *     behind it        k - frames * rows * columns + base + max((frames - 1) * step + 1, rows, columns)   three times
@@ -655,11 +657,14 @@ lora_status_t lora_add_norm(const lora_norm_args_t *args, int32_t T, void *strea
  *   logprob log(w_token / sum of the kept weights)
  * A temperature of 0 (or less, or NaN) takes the largest logit, of equal ones the lowest index (logprob 0).
  * Parameters that are NaN count as absent, a uniform that is NaN as 0.  A logit of -inf is never taken, and
- * nor is one whose weight is below 2^-46; logits of +inf share the weight.  A row with a NaN, or of -inf
- * alone, gives the token -1 and the logprob NaN.
- * Weights are good to 1e-11 of themselves, sums are held in 64 bits, and a sum within 2^-34 of the border
- * that top_p or uniform sets counts as on it (where many tokens are left to count: of a few, uniform's
- * border is exact).  The result does not depend on how the rows are split but for borders that close.
+ * nor is one whose weight is below 2^-46, which counts as nothing; logits of +inf share the weight.  A row
+ * with a NaN, or of -inf alone, gives the token -1 and the logprob NaN.
+ * Weights are good to 1e-11 of themselves, sums are held in 64 bits or more, and a sum within 2^-34 of itself of
+ * the border that top_p or uniform sets counts as on it (where many tokens are left to count: of a few,
+ * uniform's border is exact).  The result does not depend on how the rows are split but for borders that close.
+ * (One sum may hold the weights below 2^-46 too: that of all tokens, in a row with neither top_k nor min_p.
+ * They are 2^-26 of it at most, where nearly all of 2^20 tokens have such a weight, and so much its borders and
+ * logprobs may be off then.)
  * Random numbers are the caller's: the same uniform gives the same token.
  * -------------------------------------------------------------------------------------- */
 enum { LORA_LOGITS_BF16 = 0, LORA_LOGITS_FP32 = 1 };

@@ -6,7 +6,9 @@
 // sum.  A row is read once: the time should be the logits' way from memory.
 //
 // What is kept hangs on borders (a sum of thousands of weights against p times another), and a token on where
-// u falls among as many: weights are good to 1e-11 and sums are held in fp64 or in 64-bit whole numbers.
+// u falls among as many: weights are good to 1e-11 and sums are held in fp64 or in whole numbers of 64 bits (candidates)
+// and 96 (a whole vocabulary's).  A weight below 2^-46 counts as nothing, but for the sums of all that the first
+// reading takes: it does not know the largest value yet.
 // 2^t is a table of 64 powers and a polynomial of degree 3 in fp64 (7 fp64 instructions a weight, which issue
 // at half the rate of fp32's; a polynomial alone would be 12).  The table is there once for each pair of
 // banks, so that lanes with different entries do not wait for one another.
@@ -19,9 +21,10 @@
 // more readings of the row, which the second-level cache has in part: band_row.  What does not fit there either
 // (thousands of ties) takes a reading for each digit of the cut: general_row.
 //
-// 256 rows of 128000 fp32 (131 MB, 20 us at a copy's rate): greedy 37 us, top_k 50 48, top_k 200 64, min_p 0.1 41,
-// temperature alone 48, all kinds together with 30 or so wide nuclei 123.  512 rows of 150001 bf16, temperature
-// alone: 93 us, 22 instructions a value.  4 rows of 32000: 11 .. 18 us.
+// 256 rows of 128000 fp32 (131 MB, 20 us at a copy's rate): greedy 31 us, top_k 50 46, top_k 200 64, min_p 0.1 40,
+// temperature alone 45, all kinds together with 30 or so wide nuclei 124.  512 rows of 150001 bf16, temperature
+// alone: 94 us, 22 instructions a value.  4 rows of 32000: 8 us (greedy) .. 23 (top_k 200), with a nucleus of
+// thousands or a top_k over 256 among them 38 .. 47.
 #include <cooperative_groups.h>
 
 #include <cfloat>
@@ -886,7 +889,8 @@ __device__ __noinline__ void pick_from_sums(SampleShared &s, const SampleParams 
 // below the largest says in which of these the first k end, and (weights to 2^-17, a little room at both sides)
 // top_p of them.  The row is read once for that and once more for the values of those bands themselves, with the
 // exact weight before them: sorted, they give the cut.  False (the same in the whole cluster) where a band is too
-// wide for a list, or where the exact sums do not confirm it.
+// wide for a list, or where the exact sums do not confirm it: so it is where over 65535 values of a block fall into one
+// band, whose sum of weights (2^16 each) has 32 bits.
 template <bool BF16>
 __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluster, const SampleParams &P, const RowPlan &R,
                                       int64_t row, const SampleRow &logits) {

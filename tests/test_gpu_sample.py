@@ -502,6 +502,23 @@ def test_rows_noted_by_someone_else(bf16):
     assert ((got[1] >= -1) & (got[1] < V)).all()
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("R", [1, 300])
+def test_weights_that_count_as_nothing(R, bf16):
+    """A million tokens below 2^-46 (2^-46.2) of one: none of them is ever the next, and what they add to the sum of all is
+    no more than 2^-26 of it."""
+    require_gpu()
+    import torch
+    V = 1048568
+    x = torch.full((V,), -32.0, device="cuda")
+    x[V // 3] = 0.0
+    rows = (x.bfloat16() if bf16 else x).expand(R, V).contiguous()
+    for p in (None, 0.9, 1 - 2.0 ** -24):
+        for u in (0.0, 0.5, 1 - 2.0 ** -24, 1.0):
+            got, lp = _run(rows, 1.0, None, p, None, u)
+            assert (got == V // 3).all() and (lp <= 0).all() and (lp >= -2.0 ** -26).all(), (p, u, got[0], lp[0])
+
+
 def test_a_block_made_in_a_capture():
     """Its workspace holds whatever was in that memory until the graph is replayed: calls outside of the graph, in another
     graph and on other streams are right before that too."""

@@ -1125,7 +1125,14 @@ __device__ __noinline__ bool band_row(SampleShared &s, cg::cluster_group &cluste
 
 // ---- the general path -------------------------------------------------------------------------
 // What is kept so far: parts of the range before `part`, and of that one the entries from `from` on.
-struct SampleCut { int32_t part; uint64_t from; };
+struct SampleCut {
+    int32_t part;
+    uint64_t from;
+    // both are beginnings of one order: what is in both is the shorter of them
+    __device__ __forceinline__ SampleCut within(const SampleCut &o) const {
+        return part < o.part ? *this : part > o.part ? o : SampleCut{part, max(from, o.from)};
+    }
+};
 
 struct GeneralRow {
     float m, c32;
@@ -1210,7 +1217,7 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
         if (count && (before < need || (count_before == 0 && base_count == 0)) && reached >= need) atomicMin(&s.found, tid);
         __syncthreads();
         const int digit = s.found;
-        if (digit == 256) return level == 0 ? cut : to;      // all of it
+        if (digit == 256) break;                             // all of it
         if (tid == digit) {
             s.pick_count = base_count + count_before;
             s.pick_weight = sum_before;
@@ -1224,7 +1231,7 @@ __device__ SampleCut general_cut(SampleShared &s, cg::cluster_group &cluster, co
         __syncthreads();
         if (here == 1 || (!weight && (double)(base_count + here) == need)) break;     // all that are left belong to it
     }
-    return to;
+    return to.within(cut);               // (where it ends early, what `cut` left out is still behind it)
 }
 
 template <bool BF16>

@@ -502,6 +502,25 @@ def test_rows_noted_by_someone_else(bf16):
     assert ((got[1] >= -1) & (got[1] < V)).all()
 
 
+@pytest.mark.parametrize("V", [5470, 40000])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("R", [4, 320])
+@pytest.mark.parametrize("k", [1, 2, 256, 257, 513, 3000])
+def test_top_k_and_top_p_among_ties(R, bf16, V, k):
+    """More equal values than a list holds: top_p cuts what top_k left of them, and leaves out what that did."""
+    import torch
+    rng = np.random.default_rng(V + k)
+    x = np.where(rng.random(V) < 0.8, 2.0, rng.normal(0, 1, V)).astype(np.float32)
+    two = np.where(np.arange(V) < 200, 3.0, x)            # a few in front of the ties
+    p = np.array([0.5, 0.9, 0.99, 0.99999])[np.arange(R) % 4]
+    for row in (x, two, np.full(V, -3.25, np.float32)):
+        logits = torch.as_tensor(row.astype(np.float32)).expand(R, V).to(torch.bfloat16 if bf16 else torch.float32).contiguous().cuda()
+        few = logits if R < 10 else logits[:20]
+        want = _check(few, 0.7, k, p[:len(few)], 0.01, 0.77)
+        got, _ = _run(logits, 0.7, k, p, 0.01, 0.77)
+        assert np.array_equal(got, np.resize(want[:4], R))
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("R", [1, 300])
 def test_weights_that_count_as_nothing(R, bf16):

@@ -194,7 +194,8 @@ __device__ __forceinline__ double nan_value() { return __longlong_as_double(0x7f
 // its largest value `top` so far; values below `low` are taken for it, so that exponents do not leave the numbers.  `c` is
 // the row's, but no more than makes neighbouring fp32 numbers around `top` 2^7 apart: values that differ are as good as
 // nothing beside the larger one either way, and |top c| stays below 2^31, where `low`, rounded to fp32, is within 2^7.1 of
-// the 800 that it is meant to lie below the base.
+// the 800 that it is meant to lie below the base.  (With the base at 0 it is as good as exact, and lies 1000 below: the
+// first steps may hold no value at all, and what comes then may lie below the base, up to the 900 that sums are turned by.)
 struct SumBase {
     double c, base, magic;
     float low;
@@ -210,7 +211,7 @@ struct SumBase {
             base = 0.0;
         }
         magic = SP_MAGIC - base;
-        low = (float)fmax((base - 800.0) / c, -(double)FLT_MAX);
+        low = (float)fmax((base - (base == 0.0 ? 1000.0 : 800.0)) / c, -(double)FLT_MAX);
     }
     __device__ __forceinline__ double weight(float l, const double *table) const {
         return power2((double)fmaxf(l, low), c, magic, table);

@@ -502,6 +502,21 @@ def test_rows_noted_by_someone_else(bf16):
     assert ((got[1] >= -1) & (got[1] < V)).all()
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("R", [3, 40, 80, 150, 320])
+@pytest.mark.parametrize("far", [-895.0, -850.0, -700.0, -300.0, 300.0, 850.0, 895.0, 905.0])
+@pytest.mark.parametrize("p", [None, 0.05])
+def test_first_steps_without_a_value_and_logits_far_from_zero(R, far, p, bf16):
+    """A block's sums are then taken against 1, and the weights lie up to 2^900 below or above that."""
+    import torch
+    rng = np.random.default_rng(R)
+    V, tau = 40000, np.float32(0.75)
+    x = (far * np.log(2) * tau + rng.normal(0, 0.5, V)).astype(np.float32)
+    x[:V // 2 + 700] = -np.inf
+    logits = torch.as_tensor(x).to(torch.bfloat16 if bf16 else torch.float32).cuda()
+    _same_rows(logits, R, tau, p, None, [0.03, 0.61, 0.93])
+
+
 @pytest.mark.parametrize("V", [5470, 40000])
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("R", [4, 320])
